@@ -482,6 +482,75 @@ int gws_sample_fwd_compare(const gws_desc* desc, int noise_kind, const void* w, 
  * as written by gws_noise (u32 [rows * cols / 8], |R| <= 3). */
 int gws_noise_compare(const gws_desc* desc, int noise_kind, void* out, void* stream);
 
+/* ---- activations in 8 bits, and the gated feed-forward block --------------------------------------
+ * The sampling pass keeps the weights' side of training at 2 bytes per parameter; what a training step holds besides is the
+ * activations that its backward pass reads.  These calls keep them at one byte per element and use them from there.
+ *
+ * An activation checkpoint is a BF16 [rows, cols] tensor in groups of 32 elements along a row, each with a power-of-two scale
+ * 2^(s - 127), s = max(E - emax, 0), E the biased exponent of the group's largest magnitude:
+ *   GWS_ACT8_INT8   emax 0: code c = rne(64 x / 2^(s-127)) clamped to [-127, 127], value c / 64 * 2^(s-127) (MX INT8)
+ *   GWS_ACT8_E4M3   emax 8: code = x / 2^(s-127) rounded to nearest even onto E4M3, clamped to +-448 (MX FP8)
+ * The last group of a row may be short.  A group with a NaN or an infinity has s = 255 and zero codes and restores as NaN.
+ * Buffer (one device allocation, 32-byte aligned): codes [rows, ld] with ld = cols rounded up to 32 (columns past the width are
+ * zero), then at the next multiple of 256 bytes scales [rows, ld / 32], one byte each.
+ * BF16 tensors of these calls are row-major with a row stride (ld_*) of at least their width, in elements; strides that are a
+ * multiple of 8 want a 16-byte aligned base where a tensor map reads the tensor (x, grad_y, weights) and any other stride
+ * costs a copy into the workspace; outputs and grad_h take any 2-byte alignment.  Sizes may be zero: sums over nothing are zero.
+ * `workspace` is device memory, 256-byte aligned, of the size its *_workspace_bytes call gives for the same arguments (NULL
+ * where that is 0).  `status` is as for gws_gemm_fused.  An output or the workspace that overlaps an input or another output is
+ * GWS_ERR_ALIAS.  NaN and infinities in the inputs follow IEEE arithmetic. */
+typedef enum gws_act_format {
+  GWS_ACT8_INT8 = 0,
+  GWS_ACT8_E4M3 = 1,
+  GWS_SAVE_BF16 = 2, /* where a call says so: a BF16 tensor instead of a checkpoint */
+  GWS_SAVE_NONE = 3  /* gws_gated_fwd: nothing is kept */
+} gws_act_format;
+
+/* Sizes of a checkpoint; any of the outputs may be NULL.  Host arithmetic only. */
+int gws_act8_layout(int64_t rows, int64_t cols, size_t* codes_bytes, size_t* scales_offset, size_t* total_bytes);
+/* BF16 x [rows, ld] -> checkpoint, and back (each restored value rounded to BF16, which only E4M3 values below 2^-126 need). */
+int gws_act8_save(int64_t rows, int64_t cols, int64_t ld, int format, const void* x, void* act8, void* stream);
+int gws_act8_load(int64_t rows, int64_t cols, int64_t ld, int format, const void* act8, void* x, void* stream);
+
+/* Weight gradient of a linear layer y = x W^T whose input is held as a checkpoint:
+ *   grad_w[n, k] = sum over tokens of grad_y[m, n] * x8[m, k]     (BF16 operands, FP32 sums, one rounding to BF16)
+ *   grad_y  device, BF16 [m, ld_y]      x8  device, checkpoint [m, k]      grad_w  device, BF16 [n, ld_w], written */
+int64_t gws_wgrad_act8_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld_y);
+int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad_y, int64_t ld_y, const void* x8, void* grad_w, int64_t ld_w,
+                   void* workspace, size_t workspace_bytes, int* status, void* stream);
+
+/* The gated feed-forward block:  g = x Wg^T,  u = x Wu^T,  h = act(g) * u   over m tokens, k inputs, n hidden units. */
+typedef enum gws_activation {
+  GWS_GATED_SILU = 0,      /* g sigmoid(g)                                             */
+  GWS_GATED_GELU_TANH = 1, /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2          */
+  GWS_GATED_RELU = 2       /* max(g, 0)                                                */
+} gws_activation;
+typedef struct gws_gated_desc {
+  int64_t m, n, k;
+  int64_t ld_x, ld_w, ld_h; /* row strides of x, of both weights, and of h (forward) or grad_h (backward)  */
+  int32_t activation;       /* gws_activation                                                             */
+  int32_t save_format;      /* what g and u are kept as: gws_act_format                                   */
+  int32_t x_format;         /* backward: GWS_SAVE_BF16 = x is a BF16 tensor, GWS_ACT8_* = a checkpoint      */
+  int32_t reserved;
+} gws_gated_desc;
+int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward);
+
+/* Forward: both projections, the activation and the product in one kernel; g and u stay in FP32 until h is rounded.
+ *   x          device, BF16 [m, ld_x]       w_gate, w_up  device, BF16 [n, ld_w]       h  device, BF16 [m, ld_h], written
+ *   save_gate, save_up  what the backward pass reads: device, checkpoints [m, n] or BF16 [m, n] (dense), rounded from the FP32 g and
+ *              u; NULL with GWS_SAVE_NONE */
+int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate, const void* w_up, void* h, void* save_gate, void* save_up,
+                  void* workspace, size_t workspace_bytes, int* status, void* stream);
+
+/* Backward, from the kept g and u (as restored from their format):
+ *   dg = grad_h * u * act'(g),  du = grad_h * act(g)          (computed in FP32, rounded to BF16 for the tensor cores)
+ *   grad_x = dg Wg + du Wu,  grad_w_gate = dg^T x,  grad_w_up = du^T x,  h_out = act(g) * u
+ *   grad_x [m, k], grad_w_gate and grad_w_up [n, k], h_out [m, n]: device, BF16, dense, written; grad_x, the pair of weight gradients
+ *   and h_out may each be NULL, and their work (and for grad_x the weights, for the weight gradients x) is then not needed. */
+int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x, const void* w_gate, const void* w_up, const void* save_gate,
+                  const void* save_up, void* grad_x, void* grad_w_gate, void* grad_w_up, void* h_out, void* workspace, size_t workspace_bytes,
+                  int* status, void* stream);
+
 /* ---- diagnostics -----------------------------------------------------------------------------*/
 
 /* Raw Philox4x32-10 output words for vectors first_vec .. first_vec+n_vec-1 (4 words each):

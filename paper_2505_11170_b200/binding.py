@@ -90,6 +90,14 @@ _SIGNATURES = {
     "gws_bitwidth_grad": (c_int, [c_int64, c_void_p, c_void_p, c_float, c_float, ctypes.c_double, c_void_p, c_void_p]),
     "gws_bitwidth_multi": (c_int, [c_int, c_void_p, c_void_p]),
     "gws_bitwidth_grad_multi": (c_int, [c_int, c_void_p, c_void_p]),
+    "gws_act8_layout": (c_int, [c_int64, c_int64, POINTER(c_size_t), POINTER(c_size_t), POINTER(c_size_t)]),
+    "gws_act8_save": (c_int, [c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
+    "gws_act8_load": (c_int, [c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
+    "gws_wgrad_act8_workspace_bytes": (c_int64, [c_int64, c_int64, c_int64, c_int64]),
+    "gws_wgrad_act8": (c_int, [c_int64, c_int64, c_int64, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_size_t, c_void_p, c_void_p]),
+    "gws_gated_workspace_bytes": (c_int64, [c_void_p, c_int]),
+    "gws_gated_fwd": (c_int, [c_void_p] * 8 + [c_size_t, c_void_p, c_void_p]),
+    "gws_gated_bwd": (c_int, [c_void_p] * 12 + [c_size_t, c_void_p, c_void_p]),
     "gws_layer_seed": (c_uint64, [c_uint64, c_uint64]),
     "gws_sample_fwd_multi_static": (c_int, [c_int, POINTER(Desc), POINTER(_MultiPtrs), c_uint64, c_void_p]),
     "gws_sample_step_host": (c_int, [POINTER(Desc)] + [c_void_p] * 13),
@@ -488,6 +496,246 @@ def sample_step_host(desc: Desc, h_w, h_bt, h_grad, h_w_hat, h_scale, h_grad_bt,
     _check(load_library().gws_sample_step_host(ctypes.byref(desc), _ptr(h_w), _ptr(h_bt), _ptr(h_grad), _ptr(h_w_hat),
                                                _ptr(h_scale), _ptr(h_grad_bt), _ptr(d_w), _ptr(d_w_hat), _ptr(d_grad),
                                                _ptr(d_bt), _ptr(d_scale), _ptr(d_grad_bt), _stream(stream)))
+
+
+# ---- activations in 8 bits and the gated feed-forward block -------------------------------------------------
+
+ACT8_INT8, ACT8_E4M3, SAVE_BF16, SAVE_NONE = 0, 1, 2, 3
+GATED_SILU, GATED_GELU_TANH, GATED_RELU = 0, 1, 2
+
+
+class GatedDesc(Structure):
+    """Mirror of ``gws_gated_desc``."""
+    _fields_ = [("m", c_int64), ("n", c_int64), ("k", c_int64), ("ld_x", c_int64), ("ld_w", c_int64), ("ld_h", c_int64),
+                ("activation", c_int32), ("save_format", c_int32), ("x_format", c_int32), ("reserved", c_int32)]
+
+
+def act8_layout(rows: int, cols: int):
+    """(codes_bytes, scales_offset, total_bytes) of the 8-bit checkpoint of a [rows, cols] activation."""
+    a, b, c = c_size_t(), c_size_t(), c_size_t()
+    _check(load_library().gws_act8_layout(rows, cols, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c)))
+    return int(a.value), int(b.value), int(c.value)
+
+
+class Act8:
+    """An activation held as an 8-bit checkpoint: the uint8 ``buffer`` (layout of :func:`act8_layout`) with its shape and format."""
+    __slots__ = ("buffer", "rows", "cols", "fmt")
+
+    def __init__(self, buffer: torch.Tensor, rows: int, cols: int, fmt: int):
+        if buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < _act8_bytes(rows, cols):
+            raise ValueError("gws: a checkpoint is a contiguous uint8 tensor of at least %d bytes" % _act8_bytes(rows, cols))
+        self.buffer, self.rows, self.cols, self.fmt = buffer, rows, cols, fmt
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        """[rows, cols rounded up to 32] uint8 view."""
+        ld = -(-self.cols // 32) * 32
+        return self.buffer[:self.rows * ld].view(self.rows, ld)
+
+    @property
+    def scales(self) -> torch.Tensor:
+        """[rows, groups] uint8 view."""
+        groups = -(-self.cols // 32)
+        first = -(-self.rows * groups * 32 // 256) * 256
+        return self.buffer[first:first + self.rows * groups].view(self.rows, groups)
+
+
+def _act8_bytes(rows: int, cols: int) -> int:
+    """total_bytes of act8_layout."""
+    groups = rows * -(-cols // 32)
+    return -(-groups * 32 // 256) * 256 + groups
+
+
+class _On:
+    """The stream of a call: allocations made inside belong to it, whichever stream is current."""
+
+    def __init__(self, stream, device):
+        if stream is None:
+            self.handle, self.guard = c_void_p(torch.cuda.current_stream(device).cuda_stream), None
+        else:
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=device)
+            self.handle, self.guard = c_void_p(stream.cuda_stream), torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.handle
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _bf16_rows(t: torch.Tensor, name: str, shape=None, read_by_map: bool = True):
+    """A BF16 matrix as the library takes it, and its row stride.  Whatever its strides cannot say (columns apart, rows that
+    overlap, a base the tensor maps refuse) is copied."""
+    if t.dim() != 2 or t.dtype != torch.bfloat16:
+        raise ValueError("gws: %s must be a 2-D BF16 tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("gws: device pointers expected (tensor is on %s)" % t.device)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("gws: %s must be %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    rows, cols = t.shape
+    if t.numel() and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols)):
+        t = t.contiguous()
+    ld = t.stride(0) if rows > 1 and cols > 0 else max(cols, 1)
+    if read_by_map and t.numel() and t.data_ptr() % 16 and (rows <= 1 or ld % 8 == 0):
+        t = t.contiguous().clone()
+        ld = max(cols, 1)
+    return t, ld
+
+
+def _bf16_out(t: Optional[torch.Tensor], name: str, rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
+    if t is None:
+        return torch.empty((rows, cols), dtype=torch.bfloat16, device=like.device)
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols) or not t.is_contiguous() or t.device != like.device:
+        raise ValueError("gws: %s must be a contiguous BF16 [%d, %d] tensor on %s" % (name, rows, cols, like.device))
+    return t
+
+
+def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("gws: tensors on %s and %s in one call" % (first.device, t.device))
+
+
+def _workspace(nbytes: int, device):
+    if nbytes < 0:
+        raise GwsError(int(nbytes))
+    return (torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes) if nbytes else (None, 0)
+
+
+def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None, stream=None) -> Act8:
+    """BF16 [rows, cols] -> 8-bit checkpoint (``out`` is overwritten if given)."""
+    _require_cuda(x)
+    with _On(stream, x.device) as s:
+        x, ld = _bf16_rows(x, "x", read_by_map=False)
+        rows, cols = x.shape
+        if out is None:
+            out = Act8(torch.empty(_act8_bytes(rows, cols), dtype=torch.uint8, device=x.device), rows, cols, fmt)
+        elif out.shape != (rows, cols) or out.fmt != fmt:
+            raise ValueError("gws: out is a checkpoint of another shape or format")
+        _same_device(x, out.buffer)
+        _check(load_library().gws_act8_save(rows, cols, ld, fmt, x.data_ptr(), out.buffer.data_ptr(), s))
+    return out
+
+
+def act8_load(a: Act8, x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """8-bit checkpoint -> BF16 [rows, cols] (written to ``x`` if given; its rows may be strided)."""
+    _require_cuda(a.buffer, x)
+    with _On(stream, a.buffer.device) as s:
+        if x is None:
+            x = torch.empty((a.rows, a.cols), dtype=torch.bfloat16, device=a.buffer.device)
+        elif x.dtype != torch.bfloat16 or tuple(x.shape) != a.shape or (x.numel() and ((a.cols > 1 and x.stride(1) != 1) or (a.rows > 1 and x.stride(0) < a.cols))):
+            raise ValueError("gws: x must be a BF16 [%d, %d] tensor whose rows are contiguous" % a.shape)
+        _same_device(a.buffer, x)
+        ld = x.stride(0) if a.rows > 1 else max(a.cols, 1)
+        _check(load_library().gws_act8_load(a.rows, a.cols, ld, a.fmt, a.buffer.data_ptr(), x.data_ptr(), s))
+    return x
+
+
+def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """dW = grad_y^T @ x for a linear layer y = x W^T whose input is held as a checkpoint.  BF16 [n, k]."""
+    _require_cuda(grad_y, x8.buffer, grad_w, status)
+    _same_device(grad_y, x8.buffer, status)
+    with _On(stream, grad_y.device) as s:
+        grad_y, ld = _bf16_rows(grad_y, "grad_y")
+        (m, n), k = grad_y.shape, x8.cols
+        if x8.rows != m:
+            raise ValueError("gws: grad_y has %d rows and the checkpoint %d" % (m, x8.rows))
+        grad_w = _bf16_out(grad_w, "grad_w", n, k, grad_y)
+        lib = load_library()
+        ws, nbytes = _workspace(lib.gws_wgrad_act8_workspace_bytes(m, n, k, ld), grad_y.device)
+        _check(lib.gws_wgrad_act8(m, n, k, x8.fmt, grad_y.data_ptr(), ld, x8.buffer.data_ptr(), grad_w.data_ptr(), max(k, 1), _ptr(ws), nbytes,
+                                  _ptr(status), s))
+    return grad_w
+
+
+class GatedSaved:
+    """What the gated block keeps for its backward pass: the gate and the up projection, as checkpoints or BF16 tensors."""
+    __slots__ = ("gate", "up", "fmt")
+
+    def __init__(self, gate, up, fmt: int):
+        self.gate, self.up, self.fmt = gate, up, fmt
+
+    def tensors(self):
+        return (self.gate.buffer, self.up.buffer) if isinstance(self.gate, Act8) else (self.gate, self.up)
+
+
+def _new_saved(m: int, n: int, fmt: int, device) -> Optional[GatedSaved]:
+    if fmt == SAVE_NONE:
+        return None
+    if fmt == SAVE_BF16:
+        make = lambda: torch.empty((m, n), dtype=torch.bfloat16, device=device)
+    else:
+        make = lambda: Act8(torch.empty(_act8_bytes(m, n), dtype=torch.uint8, device=device), m, n, fmt)
+    return GatedSaved(make(), make(), fmt)
+
+
+def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: int = GATED_SILU, save: int = SAVE_NONE,
+              h: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """h = act(x Wg^T) * (x Wu^T) for x [m, k] and weights [n, k], in one kernel.  Returns (h, saved): ``save`` says what the gate
+    and the up projection are kept as for :func:`gated_bwd` (ACT8_INT8, ACT8_E4M3, SAVE_BF16; SAVE_NONE keeps nothing)."""
+    _require_cuda(x, w_gate, w_up, h, status)
+    _same_device(x, w_gate, w_up, status)
+    if save not in (ACT8_INT8, ACT8_E4M3, SAVE_BF16, SAVE_NONE):
+        raise GwsError(ERR_UNSUPPORTED)
+    with _On(stream, x.device) as s:
+        x, ld_x = _bf16_rows(x, "x")
+        m, k = x.shape
+        w_gate, ld_w = _bf16_rows(w_gate, "w_gate", (w_gate.shape[0], k))
+        n = w_gate.shape[0]
+        w_up, ld_up = _bf16_rows(w_up, "w_up", (n, k))
+        if ld_up != ld_w:                                     # one stride for both weights
+            w_gate, w_up, ld_w = w_gate.contiguous(), w_up.contiguous(), max(k, 1)
+        h = _bf16_out(h, "h", m, n, x)
+        saved = _new_saved(m, n, save, x.device)
+        gate, up = saved.tensors() if saved is not None else (None, None)
+        d = GatedDesc(m, n, k, ld_x, ld_w, max(n, 1), activation, save, SAVE_BF16, 0)
+        lib = load_library()
+        ws, nbytes = _workspace(lib.gws_gated_workspace_bytes(ctypes.byref(d), 0), x.device)
+        _check(lib.gws_gated_fwd(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(gate), _ptr(up), _ptr(ws), nbytes,
+                                 _ptr(status), s))
+    return h, saved
+
+
+def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor, saved: GatedSaved, activation: int = GATED_SILU,
+              want_h: bool = False, want_grad_x: bool = True, want_grad_w: bool = True, status: Optional[torch.Tensor] = None, stream=None):
+    """Backward pass of :func:`gated_fwd`.  ``x`` is the BF16 input or its checkpoint.  Returns (grad_x, grad_w_gate, grad_w_up, h);
+    what was not asked for is None.  ``h`` is act(gate) * up again, which the weight gradient of the layer after the block needs."""
+    x_tensor = x.buffer if isinstance(x, Act8) else x
+    _require_cuda(grad_h, x_tensor, w_gate, w_up, status, *saved.tensors())
+    _same_device(grad_h, x_tensor, w_gate, w_up, status, *saved.tensors())
+    with _On(stream, grad_h.device) as s:
+        m, k = x.shape
+        n = w_gate.shape[0]
+        grad_h, ld_h = _bf16_rows(grad_h, "grad_h", (m, n), read_by_map=False)
+        ld_x, x_format = max(k, 1), SAVE_BF16
+        if isinstance(x, Act8):
+            x_format = x.fmt
+        else:
+            x_tensor, ld_x = _bf16_rows(x, "x")
+        w_gate, ld_w = _bf16_rows(w_gate, "w_gate", (n, k))
+        w_up, ld_up = _bf16_rows(w_up, "w_up", (n, k))
+        if ld_up != ld_w:
+            w_gate, w_up, ld_w = w_gate.contiguous(), w_up.contiguous(), max(k, 1)
+        if tuple(saved.gate.shape) != (m, n) or tuple(saved.up.shape) != (m, n):
+            raise ValueError("gws: the kept projections are %s, not (%d, %d)" % (tuple(saved.gate.shape), m, n))
+        gate, up = saved.tensors()
+        new = lambda rows, cols, want: torch.empty((rows, cols), dtype=torch.bfloat16, device=grad_h.device) if want else None
+        grad_x, grad_wg, grad_wu, h = new(m, k, want_grad_x), new(n, k, want_grad_w), new(n, k, want_grad_w), new(m, n, want_h)
+        d = GatedDesc(m, n, k, ld_x, ld_w, ld_h, activation, saved.fmt, x_format, 0)
+        lib = load_library()
+        ws, nbytes = _workspace(lib.gws_gated_workspace_bytes(ctypes.byref(d), 1), grad_h.device)
+        _check(lib.gws_gated_bwd(ctypes.byref(d), grad_h.data_ptr(), x_tensor.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(), up.data_ptr(),
+                                 _ptr(grad_x), _ptr(grad_wg), _ptr(grad_wu), _ptr(h), _ptr(ws), nbytes, _ptr(status), s))
+    return grad_x, grad_wg, grad_wu, h
 
 
 def selfcheck_enabled() -> bool:

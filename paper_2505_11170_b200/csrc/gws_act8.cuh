@@ -1,0 +1,203 @@
+// 8-bit activation checkpoints: the codec and the kernels that only move activations.
+//
+// A group of 32 elements along a row shares one power-of-two scale 2^(s - 127), s = max(E - emax, 0), E the biased exponent
+// of the group's largest magnitude; s = 255 marks a group with a value that is not finite and restores as NaN.
+//   INT8   emax 0, code c = rne(64 x / 2^(s-127)) clamped to [-127, 127], value c / 64 * 2^(s-127)
+//   E4M3   emax 8, code = rne of x / 2^(s-127) onto the E4M3 grid, clamped to +-448
+// Scaling by a power of two is exact, so each element is rounded once, and every restored INT8 value is a BF16 number (7 bits
+// and a sign).  INT8 spaces its codes evenly: its error is at most 1/128 of the group's largest magnitude (half a step; a
+// whole one where the largest itself is clamped), a third of E4M3's on normal data; E4M3 keeps small elements beside a large one.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <stdint.h>
+
+#include "gws.h"
+
+namespace {
+
+constexpr int kGroup = 32;               // elements per scale
+constexpr uint32_t kNanByte = 255u;
+
+struct V8 { uint32_t x[8]; };            // 32 bytes
+
+__device__ __forceinline__ V8 ld32(const void* p) {
+  V8 v;
+  asm volatile("ld.global.nc.v8.u32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(v.x[0]), "=r"(v.x[1]), "=r"(v.x[2]), "=r"(v.x[3]), "=r"(v.x[4]), "=r"(v.x[5]), "=r"(v.x[6]), "=r"(v.x[7])
+               : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void st32(void* p, const V8& v) {
+  asm volatile("st.global.v8.u32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v.x[0]), "r"(v.x[1]), "r"(v.x[2]), "r"(v.x[3]),
+               "r"(v.x[4]), "r"(v.x[5]), "r"(v.x[6]), "r"(v.x[7])
+               : "memory");
+}
+
+__device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// 2^(byte - 127) as a float, exactly; 2^-127 is a subnormal.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  return __uint_as_float(byte == 0u ? 0x00400000u : byte == kNanByte ? 0x7FC00000u : byte << 23);
+}
+// 2^(127 - byte); byte = 254 gives the subnormal 2^-127.
+__device__ __forceinline__ float inverse_scale_of(uint32_t byte) { return __uint_as_float(byte >= 254u ? 0x00400000u : (254u - byte) << 23); }
+// 2^(byte - 133): the weight of one INT8 step, exactly (subnormal below byte 7).
+__device__ __forceinline__ float step_of(uint32_t byte) {
+  return __uint_as_float(byte == kNanByte ? 0x7FC00000u : byte >= 7u ? (byte - 6u) << 23 : 0x10000u << byte);
+}
+
+// Scale byte of a group from the FP32 bit pattern of its largest magnitude (NaN patterns compare above infinity).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top_bits, int format) {
+  if (top_bits >= 0x7F800000u) return kNanByte;
+  const uint32_t e = top_bits >> 23, emax = format == GWS_ACT8_E4M3 ? 8u : 0u;
+  return e > emax ? e - emax : 0u;
+}
+
+// Codes of four elements.  x * inv is exact (a power of two, and |x * inv| < 2); the FMA with 1.5 * 2^23 rounds 64 x once, to
+// nearest even, and leaves the integer in the low byte.
+__device__ __forceinline__ uint32_t encode4_int8(float a, float b, float c, float d, float inv) {
+  const float magic = 12582912.0f;
+  auto one = [&](float v) { return __float_as_uint(fminf(fmaxf(__fmaf_rn(v * inv, 64.0f, magic), magic - 127.0f), magic + 127.0f)); };
+  return __byte_perm(__byte_perm(one(a), one(b), 0x0040), __byte_perm(one(c), one(d), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t encode4_e4m3(float a, float b, float c, float d, float inv) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a * inv, b * inv), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c * inv, d * inv), __NV_SATFINITE, __NV_E4M3);
+  return lo | (hi << 16);
+}
+
+// The four values of a word of codes.  `unit` is step_of (INT8) or scale_of (E4M3) of the group's byte.
+__device__ __forceinline__ void decode4_int8(uint32_t codes, float unit, float* v) {
+  const uint32_t u = codes ^ 0x80808080u;        // c + 128 in every byte; 0x4B0000uu is the float 2^23 + c + 128
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540u + i)) - 8388736.0f) * unit;
+}
+__device__ __forceinline__ void decode4_e4m3(uint32_t codes, float unit, float* v) {
+  const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes & 0xFFFFu), __NV_E4M3);
+  const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes >> 16), __NV_E4M3);
+  const float2 a = __half22float2(__half2(lo)), b = __half22float2(__half2(hi));
+  v[0] = a.x * unit; v[1] = a.y * unit; v[2] = b.x * unit; v[3] = b.y * unit;
+}
+
+template <int FMT>
+__device__ __forceinline__ float unit_of(uint32_t byte) { return FMT == GWS_ACT8_INT8 ? step_of(byte) : scale_of(byte); }
+template <int FMT>
+__device__ __forceinline__ void decode4(uint32_t codes, float unit, float* v) {
+  if (FMT == GWS_ACT8_INT8) decode4_int8(codes, unit, v);
+  else decode4_e4m3(codes, unit, v);
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float inv) {
+  return FMT == GWS_ACT8_INT8 ? encode4_int8(a, b, c, d, inv) : encode4_e4m3(a, b, c, d, inv);
+}
+
+// A whole group held by one thread.
+template <int FMT>
+__device__ __forceinline__ uint32_t encode_group(const float (&v)[kGroup], V8& codes) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  const uint32_t byte = scale_byte(top, FMT);
+  const float inv = inverse_scale_of(byte);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) codes.x[i] = byte == kNanByte ? 0u : encode4<FMT>(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+  return byte;
+}
+
+struct Act8View {                 // a checkpoint in memory
+  uint8_t* codes;                 // [rows, ld]
+  uint8_t* scales;                // [rows, ld / 32]
+  int64_t ld;                     // cols rounded up to 32
+};
+
+// ---- save / load -------------------------------------------------------------------------------------------------------
+// Memory-bound: 2 bytes of activation and 1 + 1/32 of checkpoint per element.  A thread takes a whole group - two 32-byte
+// accesses on the BF16 side, one on the code side, one scale byte - so the maximum needs no exchange between lanes.
+
+template <int FMT>
+__global__ void __launch_bounds__(256) k_act8_save(const uint16_t* x, int64_t ldx, Act8View c, int64_t groups, uint32_t per_row) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (t >= groups) return;
+  int64_t at = t * kGroup;
+  if (ldx != c.ld) {
+    const int64_t row = t / per_row;
+    at = row * ldx + (t - row * per_row) * kGroup;
+  }
+  const V8 a = ld32(x + at), b = ld32(x + at + 16);
+  float v[kGroup];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[2 * i] = bf16_lo(a.x[i]);
+    v[2 * i + 1] = bf16_hi(a.x[i]);
+    v[16 + 2 * i] = bf16_lo(b.x[i]);
+    v[17 + 2 * i] = bf16_hi(b.x[i]);
+  }
+  V8 codes;
+  c.scales[t] = static_cast<uint8_t>(encode_group<FMT>(v, codes));
+  st32(c.codes + t * kGroup, codes);
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(256) k_act8_load(Act8View c, uint16_t* x, int64_t ldx, int64_t groups, uint32_t per_row) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (t >= groups) return;
+  int64_t at = t * kGroup;
+  if (ldx != c.ld) {
+    const int64_t row = t / per_row;
+    at = row * ldx + (t - row * per_row) * kGroup;
+  }
+  const V8 codes = ld32(c.codes + t * kGroup);
+  const float unit = unit_of<FMT>(c.scales[t]);
+  V8 out[2];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float v[4];
+    decode4<FMT>(codes.x[i], unit, v);
+    out[i >> 2].x[2 * (i & 3)] = pack_bf16(v[0], v[1]);
+    out[i >> 2].x[2 * (i & 3) + 1] = pack_bf16(v[2], v[3]);
+  }
+  st32(x + at, out[0]);
+  st32(x + at + 16, out[1]);
+}
+
+// The general forms: any width, row stride and 2-byte alignment.  A warp takes a group, a lane an element, so that rows of
+// any alignment are still read and written side by side.  Columns past the width become zero codes.
+template <int FMT>
+__global__ void __launch_bounds__(256) k_act8_save_lane(const uint16_t* x, int64_t ldx, Act8View c, int64_t groups, uint32_t per_row, int64_t cols) {
+  const uint32_t lane = threadIdx.x & 31u;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (t >= groups) return;
+  const int64_t row = t / per_row, col = (t - row * per_row) * kGroup + lane;
+  const float v = col < cols ? __uint_as_float(static_cast<uint32_t>(x[row * ldx + col]) << 16) : 0.0f;
+  const uint32_t byte = scale_byte(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v) & 0x7FFFFFFFu), FMT);
+  const uint32_t code = byte == kNanByte ? 0u : encode4<FMT>(v, 0.0f, 0.0f, 0.0f, inverse_scale_of(byte));
+  c.codes[t * kGroup + lane] = static_cast<uint8_t>(code);
+  if (lane == 0) c.scales[t] = static_cast<uint8_t>(byte);
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(256) k_act8_load_lane(Act8View c, uint16_t* x, int64_t ldx, int64_t groups, uint32_t per_row, int64_t cols) {
+  const uint32_t lane = threadIdx.x & 31u;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (t >= groups) return;
+  const int64_t row = t / per_row, col = (t - row * per_row) * kGroup + lane;
+  float v[4];
+  decode4<FMT>(c.codes[t * kGroup + lane], unit_of<FMT>(c.scales[t]), v);
+  if (col < cols) x[row * ldx + col] = static_cast<uint16_t>(pack_bf16(v[0], 0.0f));
+}
+
+// ---- BF16 rows brought into the alignment a tensor map wants ---------------------------------------------------------------
+__global__ void __launch_bounds__(256) k_realign(const uint16_t* x, int64_t ldx, uint16_t* out, int64_t ld_out, int64_t rows, int64_t cols) {
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
+    for (int64_t col = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; col < cols; col += static_cast<int64_t>(gridDim.x) * 256)
+      out[row * ld_out + col] = x[row * ldx + col];
+}
+
+}  // namespace

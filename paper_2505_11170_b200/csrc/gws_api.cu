@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "gws.h"
+#include "gws_internal.h"
 #ifndef GWS_FLAT_CPT_FWD
 #define GWS_FLAT_CPT_FWD 2
 #endif
@@ -39,6 +40,19 @@ int check_launch(const char* what) {
   const cudaError_t err = cudaGetLastError();
   return err == cudaSuccess ? GWS_OK : cuda_fail(err, what);
 }
+
+}  // namespace
+
+namespace gws {
+int finish_launch(const char* what) { return check_launch(what); }
+int report_cuda(cudaError_t err, const char* what) { return cuda_fail(err, what); }
+int report_text(const char* text) {
+  g_last_cuda_error = text;
+  return GWS_ERR_CUDA;
+}
+}  // namespace gws
+
+namespace {
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 

@@ -1,0 +1,555 @@
+// Host side of the activation operators declared in gws.h: 8-bit activation checkpoints, the weight gradient from a checkpoint
+// and the gated feed-forward block.  Argument validation, tensor maps, choice of tile and launch geometry; no device memory is
+// allocated here.
+#include <algorithm>
+#include <cstring>
+#include <initializer_list>
+#include <string>
+
+#include "gws.h"
+#include "gws_internal.h"
+#include "gws_tc.cuh"
+
+namespace {
+
+constexpr int64_t kMaxDim = 0x7FFFFFFFLL - 4096;
+constexpr int kJobs = 256;                      // threads of the kernels that only move activations
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+bool on(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+struct Span {
+  const void* p;
+  int64_t bytes;
+};
+Span rows_of(const void* p, int64_t rows, int64_t cols, int64_t ld) { return {p, p == nullptr || rows == 0 || cols == 0 ? 0 : ((rows - 1) * ld + cols) * 2}; }
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes > 0 && b.bytes > 0 && x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
+}
+// No output may overlap an input or another output: blocks re-read inputs while others write.
+bool clash(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+  for (const Span* a = outputs.begin(); a != outputs.end(); ++a) {
+    for (const Span& b : inputs)
+      if (overlap(*a, b)) return true;
+    for (const Span* b = a + 1; b != outputs.end(); ++b)
+      if (overlap(*a, *b)) return true;
+  }
+  return false;
+}
+
+bool is_act8(int format) { return format == GWS_ACT8_INT8 || format == GWS_ACT8_E4M3; }
+
+// ---- layout of a checkpoint --------------------------------------------------------------------------------------------
+int64_t act8_ld(int64_t cols) { return round_up(cols, kGroup); }
+int64_t act8_codes(int64_t rows, int64_t cols) { return rows * act8_ld(cols); }
+int64_t act8_total(int64_t rows, int64_t cols) { return round_up(act8_codes(rows, cols), 256) + rows * (act8_ld(cols) / kGroup); }
+Act8View act8_view(const void* buffer, int64_t rows, int64_t cols) {
+  uint8_t* p = static_cast<uint8_t*>(const_cast<void*>(buffer));
+  return {p, p + round_up(act8_codes(rows, cols), 256), act8_ld(cols)};
+}
+int check_dims(int64_t a, int64_t b, int64_t c) {
+  if (a < 0 || b < 0 || c < 0) return GWS_ERR_SHAPE;
+  return a > kMaxDim || b > kMaxDim || c > kMaxDim ? GWS_ERR_LIMIT : GWS_OK;
+}
+
+int zero(void* p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t s) {
+  if (p == nullptr || rows == 0 || cols == 0) return GWS_OK;
+  const cudaError_t err = cudaMemset2DAsync(p, static_cast<size_t>(ld) * 2u, 0, static_cast<size_t>(cols) * 2u, static_cast<size_t>(rows), s);
+  return err == cudaSuccess ? GWS_OK : gws::report_cuda(err, "clearing a gradient");
+}
+
+// Whether every group of a [rows, cols] BF16 tensor is 64 whole bytes on a 32-byte boundary: a thread then takes a group.
+bool whole_groups(const void* p, int64_t cols, int64_t ld) { return cols % kGroup == 0 && ld % 16 == 0 && on(p, 32); }
+
+unsigned blocks_for(int64_t items, int64_t per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
+
+int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8View& c, int64_t rows, int64_t cols, cudaStream_t s) {
+  const int64_t per_row = c.ld / kGroup, groups = rows * per_row;
+  const bool fast = whole_groups(x, cols, ldx);
+  if (groups / (fast ? kJobs : 8) >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
+  uint16_t* px = static_cast<uint16_t*>(const_cast<void*>(x));
+  const uint32_t pr = static_cast<uint32_t>(per_row);
+  const unsigned grid = blocks_for(groups, fast ? kJobs : 8);
+  const bool i8 = format == GWS_ACT8_INT8;
+  if (fast) {
+    if (save) i8 ? k_act8_save<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr) : k_act8_save<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr);
+    else i8 ? k_act8_load<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr) : k_act8_load<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr);
+  } else {
+    if (save) i8 ? k_act8_save_lane<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr, cols) : k_act8_save_lane<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr, cols);
+    else i8 ? k_act8_load_lane<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr, cols) : k_act8_load_lane<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr, cols);
+  }
+  return gws::finish_launch("activation checkpoint kernel");
+}
+
+// ---- tensor maps ---------------------------------------------------------------------------------------------------------
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                            const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+  static const Encode fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
+    return reinterpret_cast<Encode>(p);
+  }();
+  return fn;
+}
+
+// A BF16 matrix whose copies are boxes of 64 columns by `box_rows` rows, 128-byte swizzle; outside it copies bring zeros.
+int make_map(CUtensorMap& map, const void* p, int64_t rows, int64_t cols, int64_t ld, uint32_t box_rows) {
+  const Encode encode = encoder();
+  if (encode == nullptr) return gws::report_text("cuTensorMapEncodeTiled is not available from this driver");
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2u};
+  const cuuint32_t box[2] = {64u, box_rows}, steps[2] = {1u, 1u};
+  const CUresult res = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (res != CUDA_SUCCESS) return gws::report_text(("cuTensorMapEncodeTiled failed with CUresult " + std::to_string(static_cast<int>(res))).c_str());
+  return GWS_OK;
+}
+
+// A matrix as the GEMM reads it: rows on 16-byte boundaries, in place or in the workspace.
+struct Mat {
+  const void* p;
+  int64_t rows, cols, ld;
+};
+bool in_place(int64_t rows, int64_t ld) { return rows <= 1 || ld % 8 == 0; }
+int64_t packed_bytes(int64_t rows, int64_t cols) { return round_up(rows * round_up(cols, 8) * 2, 256); }
+
+int realign(Mat& m, void* to, cudaStream_t s) {
+  if (in_place(m.rows, m.ld)) {
+    m.ld = round_up(m.rows <= 1 ? m.cols : m.ld, 8);
+    return GWS_OK;
+  }
+  const int64_t ld = round_up(m.cols, 8);
+  const dim3 grid(std::min<unsigned>(blocks_for(m.cols, kJobs), 64u), static_cast<unsigned>(std::min<int64_t>(m.rows, 65535)));
+  k_realign<<<grid, kJobs, 0, s>>>(static_cast<const uint16_t*>(m.p), m.ld, static_cast<uint16_t*>(to), ld, m.rows, m.cols);
+  m.p = to;
+  m.ld = ld;
+  return gws::finish_launch("row alignment kernel");
+}
+
+// ---- choice of tile --------------------------------------------------------------------------------------------------------
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) {
+    (void)cudaGetLastError();
+    return 148;
+  }
+  return n;
+}
+
+struct Tile {
+  int cg, bn;                              // blocks per tile, columns of accumulator
+  uint32_t m_tiles, n_tiles, splits, kb_split;
+};
+
+// The tile and the split of the contraction with the least estimated time.  A step (64 along the contraction) takes a block
+// max(products, operand bytes over what an SM draws from L2); a wave takes a block's steps, and splitting adds the pass that
+// joins the parts.
+Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t kb, int sms) {
+  static const struct { int cg, bn; } kinds[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
+  Tile best{};
+  double least = 0.0;
+  for (const auto& kind : kinds) {
+    const int64_t width = mode == kGated ? kind.bn / 2 : kind.bn;
+    const int64_t mt = outs * ((rows + 128 * kind.cg - 1) / (128 * kind.cg)), nt = (cols + width - 1) / width;
+    const double slots = kind.cg == 2 ? sms / 2 : sms * (kind.bn <= 64 ? 2 : 1);
+    const double step = std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 56.0) * (kind.bn <= 64 ? 2 : 1);
+    const int64_t most = mode == kGated ? 1 : std::min<int64_t>(16, kb / 4);
+    for (int64_t splits = 1; splits <= std::max<int64_t>(1, most); ++splits) {
+      const int64_t per = (kb + splits - 1) / splits;
+      if ((kb + per - 1) / per != splits) continue;
+      const double waves = std::ceil(static_cast<double>(mt * nt * splits) / slots);
+      double cost = waves * (per * step + 300.0) + 1500.0 + 12.0 * kind.bn;
+      if (splits > 1) cost += 5000.0 + outs * static_cast<double>(rows) * cols * (8.0 * splits + 2.0) / 3400.0;
+      if (best.cg == 0 || cost < least) {
+        best = {kind.cg, kind.bn, static_cast<uint32_t>(mt), static_cast<uint32_t>(nt), static_cast<uint32_t>(splits), static_cast<uint32_t>(per)};
+        least = cost;
+      }
+    }
+  }
+  return best;
+}
+
+int64_t part_bytes(const Tile& t, int64_t rows, int64_t cols, int outs) {
+  return t.splits > 1 ? round_up(static_cast<int64_t>(t.splits) * outs * rows * round_up(cols, 32) * 4, 256) : 0;
+}
+
+template <int CG, int BN, int MODE>
+int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStream_t s) {
+  using S = TcShape<CG, BN, MODE>;
+  cudaError_t err = cudaFuncSetAttribute(k_tc<CG, BN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmemBytes));
+  if (err != cudaSuccess) return gws::report_cuda(err, "shared memory of the block GEMM");
+  const uint32_t work = args.m_tiles * args.n_tiles * args.splits;
+  const uint32_t slots = CG == 2 ? static_cast<uint32_t>(sms / 2) : static_cast<uint32_t>(sms) * S::kPerSm;
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3(std::min(work, slots) * CG);
+  cfg.blockDim = dim3(S::kThreads);
+  cfg.dynamicSmemBytes = S::kSmemBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CG;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  err = cudaLaunchKernelEx(&cfg, k_tc<CG, BN, MODE>, maps[0], maps[1], maps[2], maps[3], args);
+  if (err != cudaSuccess) { (void)cudaGetLastError(); return gws::report_cuda(err, "block GEMM"); }
+  return gws::finish_launch("block GEMM");
+}
+
+template <int MODE>
+int launch_mode(const Tile& t, const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStream_t s) {
+  if (t.cg == 2 && t.bn == 256) return launch_tc<2, 256, MODE>(maps, args, sms, s);
+  if (t.cg == 2) return launch_tc<2, 128, MODE>(maps, args, sms, s);
+  if (t.bn == 128) return launch_tc<1, 128, MODE>(maps, args, sms, s);
+  return launch_tc<1, 64, MODE>(maps, args, sms, s);
+}
+
+TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t kb, int* status) {
+  TcArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.m_tiles = t.m_tiles;
+  a.n_tiles = t.n_tiles;
+  a.splits = t.splits;
+  a.tiles_per_out = t.m_tiles;
+  a.kb = static_cast<uint32_t>(kb);
+  a.kb_first = a.kb;
+  a.kb_split = t.kb_split;
+  a.group = 8;
+  a.stage_bytes = static_cast<uint32_t>(t.cg) * kTcABytes + static_cast<uint32_t>(t.bn) * kTcStep * 2u;
+  a.rows = rows;
+  a.cols = cols;
+  a.status = status;
+  return a;
+}
+
+void set_out(TcArgs& a, void* out0, void* out1, int64_t ld) {
+  a.out[0] = out0;
+  a.out[1] = out1;
+  a.ld_out = ld;
+  a.direct = ld % 16 == 0 && on(out0, 32) && on(out1, 32);
+}
+
+int join(const TcArgs& a, cudaStream_t s) {
+  const int64_t items = a.ld_part / 4 * a.rows * (a.out[1] != nullptr ? 2 : 1);
+  const bool wide = a.ld_out % 4 == 0 && on(a.out[0], 8) && on(a.out[1], 8);
+  if ((items + kJobs - 1) / kJobs >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
+  k_join<<<blocks_for(items, kJobs), kJobs, 0, s>>>(a.part, a.ld_part, a.part_stride, a.splits, static_cast<uint16_t*>(a.out[0]),
+                                                    static_cast<uint16_t*>(a.out[1]), a.ld_out, a.rows, a.cols, wide);
+  return gws::finish_launch("join of a split contraction");
+}
+
+// dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
+int64_t steps_of(int64_t len) { return (len + kTcStep - 1) / kTcStep; }
+
+int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, int64_t ld_out, void* part, int* status, int sms, cudaStream_t s) {
+  const int outs = a1 != nullptr ? 2 : 1;
+  const Tile t = choose(kDw, a0.cols, x.cols, outs, steps_of(a0.rows), sms);
+  TcArgs args = base_args(t, a0.cols, x.cols, steps_of(a0.rows), status);
+  args.tiles_per_out = t.m_tiles / outs;
+  set_out(args, out0, out1, ld_out);
+  args.part = static_cast<float*>(part);
+  args.ld_part = round_up(x.cols, 32);
+  args.part_stride = static_cast<int64_t>(outs) * args.rows * args.ld_part;
+  CUtensorMap maps[4];
+  int st = make_map(maps[0], a0.p, a0.rows, a0.cols, a0.ld, kTcStep);
+  if (st == GWS_OK) st = a1 != nullptr ? make_map(maps[1], a1->p, a1->rows, a1->cols, a1->ld, kTcStep) : (maps[1] = maps[0], GWS_OK);
+  if (st == GWS_OK) st = make_map(maps[2], x.p, x.rows, x.cols, x.ld, kTcStep);
+  if (st != GWS_OK) return st;
+  maps[3] = maps[2];
+  st = launch_mode<kDw>(t, maps, args, sms, s);
+  return st == GWS_OK && t.splits > 1 ? join(args, s) : st;
+}
+
+int64_t dw_part_bytes(int64_t m, int64_t rows, int64_t cols, int outs, int sms) {
+  return part_bytes(choose(kDw, rows, cols, outs, steps_of(m), sms), rows, cols, outs);
+}
+
+// ---- the gated block ---------------------------------------------------------------------------------------------------------
+int check_gated(const gws_gated_desc* d) {
+  if (d == nullptr) return GWS_ERR_NULL;
+  const int st = check_dims(d->m, d->n, d->k);
+  if (st != GWS_OK) return st;
+  if ((d->m > 0 && d->k > 0 && d->ld_x < d->k) || (d->n > 0 && d->k > 0 && d->ld_w < d->k) || (d->m > 0 && d->n > 0 && d->ld_h < d->n)) return GWS_ERR_SHAPE;
+  if (d->ld_x > kMaxDim || d->ld_w > kMaxDim || d->ld_h > kMaxDim) return GWS_ERR_LIMIT;
+  if (d->activation < GWS_GATED_SILU || d->activation > GWS_GATED_RELU) return GWS_ERR_UNSUPPORTED;
+  return GWS_OK;
+}
+
+int64_t saved_bytes(const gws_gated_desc* d) {
+  return d->save_format == GWS_SAVE_NONE ? 0 : d->save_format == GWS_SAVE_BF16 ? d->m * d->n * 2 : act8_total(d->m, d->n);
+}
+
+struct BackLayout {
+  int64_t x, w_gate, w_up, grad_gate, grad_up, part, total;
+};
+BackLayout back_layout(const gws_gated_desc* d, int sms) {
+  BackLayout l{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) { const int64_t here = at; at += round_up(bytes, 256); return here; };
+  l.x = take(is_act8(d->x_format) || !in_place(d->m, d->ld_x) ? packed_bytes(d->m, d->k) : 0);
+  const int64_t w = in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k);
+  l.w_gate = take(w);
+  l.w_up = take(w);
+  l.grad_gate = take(packed_bytes(d->m, d->n));
+  l.grad_up = take(packed_bytes(d->m, d->n));
+  const int64_t dx = d->m > 0 && d->k > 0 && d->n > 0 ? part_bytes(choose(kDx, d->m, d->k, 1, 2 * steps_of(d->n), sms), d->m, d->k, 1) : 0;
+  const int64_t dw = d->m > 0 && d->k > 0 && d->n > 0 ? dw_part_bytes(d->m, d->n, d->k, 2, sms) : 0;
+  l.part = take(std::max(dx, dw));
+  l.total = at;
+  return l;
+}
+int64_t forward_bytes(const gws_gated_desc* d) {
+  const int64_t w = in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k);
+  return (in_place(d->m, d->ld_x) ? 0 : packed_bytes(d->m, d->k)) + 2 * w;
+}
+
+template <int SAVE, int ACT>
+void launch_pre(const PreArgs& p, bool fast, cudaStream_t s) {
+  if (fast) k_gated_pre<SAVE, ACT><<<blocks_for(p.groups, kJobs), kJobs, 0, s>>>(p);
+  else k_gated_pre_lane<SAVE, ACT><<<blocks_for(p.groups, 8), kJobs, 0, s>>>(p);
+}
+template <int SAVE>
+void launch_pre_act(const PreArgs& p, int act, bool fast, cudaStream_t s) {
+  if (act == GWS_GATED_SILU) launch_pre<SAVE, GWS_GATED_SILU>(p, fast, s);
+  else if (act == GWS_GATED_GELU_TANH) launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, fast, s);
+  else launch_pre<SAVE, GWS_GATED_RELU>(p, fast, s);
+}
+
+bool workspace_ok(const void* p, size_t have, int64_t need) { return need == 0 || (p != nullptr && on(p, 256) && have >= static_cast<size_t>(need)); }
+
+}  // namespace
+
+extern "C" {
+
+int gws_act8_layout(int64_t rows, int64_t cols, size_t* codes_bytes, size_t* scales_offset, size_t* total_bytes) {
+  const int st = check_dims(rows, cols, 0);
+  if (st != GWS_OK) return st;
+  if (codes_bytes != nullptr) *codes_bytes = static_cast<size_t>(act8_codes(rows, cols));
+  if (scales_offset != nullptr) *scales_offset = static_cast<size_t>(round_up(act8_codes(rows, cols), 256));
+  if (total_bytes != nullptr) *total_bytes = static_cast<size_t>(act8_total(rows, cols));
+  return GWS_OK;
+}
+
+static int act8_move(bool save, int64_t rows, int64_t cols, int64_t ld, int format, const void* x, const void* act8, void* stream) {
+  const int st = check_dims(rows, cols, 0);
+  if (st != GWS_OK) return st;
+  if (!is_act8(format)) return GWS_ERR_UNSUPPORTED;
+  if (rows == 0 || cols == 0) return GWS_OK;
+  if (ld < cols) return GWS_ERR_SHAPE;
+  if (ld > kMaxDim) return GWS_ERR_LIMIT;
+  if (x == nullptr || act8 == nullptr) return GWS_ERR_NULL;
+  if (!on(x, 2) || !on(act8, 32)) return GWS_ERR_ALIGN;
+  if (overlap(rows_of(x, rows, cols, ld), {act8, act8_total(rows, cols)})) return GWS_ERR_ALIAS;
+  return launch_act8(save, format, x, rows == 1 ? act8_ld(cols) : ld, act8_view(act8, rows, cols), rows, cols, static_cast<cudaStream_t>(stream));
+}
+
+int gws_act8_save(int64_t rows, int64_t cols, int64_t ld, int format, const void* x, void* act8, void* stream) {
+  return act8_move(true, rows, cols, ld, format, x, act8, stream);
+}
+
+int gws_act8_load(int64_t rows, int64_t cols, int64_t ld, int format, const void* act8, void* x, void* stream) {
+  return act8_move(false, rows, cols, ld, format, x, act8, stream);
+}
+
+int64_t gws_wgrad_act8_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t ld_y) {
+  const int st = check_dims(m, n, k);
+  if (st != GWS_OK) return st;
+  if (m == 0 || n == 0 || k == 0) return 0;
+  return packed_bytes(m, k) + (in_place(m, ld_y) ? 0 : packed_bytes(m, n)) + dw_part_bytes(m, n, k, 1, sm_count());
+}
+
+int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad_y, int64_t ld_y, const void* x8, void* grad_w, int64_t ld_w,
+                   void* workspace, size_t workspace_bytes, int* status, void* stream) {
+  int st = check_dims(m, n, k);
+  if (st != GWS_OK) return st;
+  if (!is_act8(format)) return GWS_ERR_UNSUPPORTED;
+  if (n == 0 || k == 0) return GWS_OK;
+  if (ld_w < k || (m > 0 && ld_y < n)) return GWS_ERR_SHAPE;
+  if (ld_w > kMaxDim || ld_y > kMaxDim) return GWS_ERR_LIMIT;
+  if (grad_w == nullptr || (m > 0 && (grad_y == nullptr || x8 == nullptr))) return GWS_ERR_NULL;
+  if (!on(grad_w, 2) || !on(status, 4)) return GWS_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (m == 0) return zero(grad_w, n, k, ld_w, s);
+  if (!on(grad_y, in_place(m, ld_y) ? 16 : 2) || !on(x8, 32)) return GWS_ERR_ALIGN;
+  const int64_t need = gws_wgrad_act8_workspace_bytes(m, n, k, ld_y);
+  if (clash({rows_of(grad_w, n, k, ld_w), {workspace, need}}, {rows_of(grad_y, m, n, ld_y), {x8, act8_total(m, k)}})) return GWS_ERR_ALIAS;
+  if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  const int64_t ldx = round_up(k, 8);
+  st = launch_act8(false, format, ws, ldx, act8_view(x8, m, k), m, k, s);
+  if (st != GWS_OK) return st;
+  const Mat x{ws, m, k, ldx};
+  ws += packed_bytes(m, k);
+  Mat y{grad_y, m, n, ld_y};
+  const bool moved = !in_place(m, ld_y);
+  st = realign(y, ws, s);
+  if (st != GWS_OK) return st;
+  if (moved) ws += packed_bytes(m, n);
+  return run_dw(y, nullptr, x, grad_w, nullptr, ld_w, ws, status, sm_count(), s);
+}
+
+int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward) {
+  const int st = check_gated(desc);
+  if (st != GWS_OK) return st;
+  if (desc->m == 0 || desc->n == 0 || desc->k == 0) return 0;
+  return backward != 0 ? back_layout(desc, sm_count()).total : forward_bytes(desc);
+}
+
+int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate, const void* w_up, void* h, void* save_gate, void* save_up,
+                  void* workspace, size_t workspace_bytes, int* status, void* stream) {
+  int st = check_gated(desc);
+  if (st != GWS_OK) return st;
+  const gws_gated_desc& d = *desc;
+  const bool saves = d.save_format != GWS_SAVE_NONE, bytes8 = is_act8(d.save_format);
+  if (saves && !bytes8 && d.save_format != GWS_SAVE_BF16) return GWS_ERR_UNSUPPORTED;
+  if (d.m == 0 || d.n == 0) return GWS_OK;
+  if (h == nullptr || (saves && (save_gate == nullptr || save_up == nullptr))) return GWS_ERR_NULL;
+  if (!on(h, 2) || !on(status, 4) || (saves && (!on(save_gate, bytes8 ? 32 : 2) || !on(save_up, bytes8 ? 32 : 2)))) return GWS_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (d.k == 0) {                              // both projections are zero, and so is act(0)
+    st = zero(h, d.m, d.n, d.ld_h, s);
+    for (void* p : {save_gate, save_up})
+      if (st == GWS_OK && saves) {
+        const cudaError_t err = cudaMemsetAsync(p, 0, static_cast<size_t>(saved_bytes(desc)), s);
+        if (err != cudaSuccess) st = gws::report_cuda(err, "clearing a saved projection");
+      }
+    return st;
+  }
+  if (x == nullptr || w_gate == nullptr || w_up == nullptr) return GWS_ERR_NULL;
+  const bool moves_x = !in_place(d.m, d.ld_x), moves_w = !in_place(d.n, d.ld_w);
+  if (!on(x, moves_x ? 2 : 16) || !on(w_gate, moves_w ? 2 : 16) || !on(w_up, moves_w ? 2 : 16)) return GWS_ERR_ALIGN;
+  const int64_t need = forward_bytes(desc), kept = saved_bytes(desc);
+  if (clash({rows_of(h, d.m, d.n, d.ld_h), {save_gate, kept}, {save_up, kept}, {workspace, need}},
+            {rows_of(x, d.m, d.k, d.ld_x), rows_of(w_gate, d.n, d.k, d.ld_w), rows_of(w_up, d.n, d.k, d.ld_w)}))
+    return GWS_ERR_ALIAS;
+  if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  Mat mx{x, d.m, d.k, d.ld_x}, mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
+  if ((st = realign(mx, ws, s)) != GWS_OK) return st;
+  if (moves_x) ws += packed_bytes(d.m, d.k);
+  if ((st = realign(mg, ws, s)) != GWS_OK) return st;
+  if (moves_w) ws += packed_bytes(d.n, d.k);
+  if ((st = realign(mu, ws, s)) != GWS_OK) return st;
+
+  const int sms = sm_count();
+  const Tile t = choose(kGated, d.m, d.n, 1, steps_of(d.k), sms);
+  TcArgs args = base_args(t, d.m, d.n, steps_of(d.k), status);
+  set_out(args, h, nullptr, d.ld_h);
+  args.activation = d.activation;
+  args.save = d.save_format;
+  if (bytes8) {
+    args.save8[0] = act8_view(save_gate, d.m, d.n);
+    args.save8[1] = act8_view(save_up, d.m, d.n);
+  } else if (saves) {
+    args.save16[0] = static_cast<uint16_t*>(save_gate);
+    args.save16[1] = static_cast<uint16_t*>(save_up);
+    args.save_direct = d.n % 16 == 0 && on(save_gate, 32) && on(save_up, 32);
+  }
+  CUtensorMap maps[4];
+  if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, 128)) != GWS_OK) return st;
+  maps[1] = maps[0];
+  if ((st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, static_cast<uint32_t>(t.bn / 2))) != GWS_OK) return st;
+  if ((st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, static_cast<uint32_t>(t.bn / 2))) != GWS_OK) return st;
+  return launch_mode<kGated>(t, maps, args, sms, s);
+}
+
+int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x, const void* w_gate, const void* w_up, const void* save_gate,
+                  const void* save_up, void* grad_x, void* grad_w_gate, void* grad_w_up, void* h_out, void* workspace, size_t workspace_bytes,
+                  int* status, void* stream) {
+  int st = check_gated(desc);
+  if (st != GWS_OK) return st;
+  const gws_gated_desc& d = *desc;
+  const bool saved8 = is_act8(d.save_format), x8 = is_act8(d.x_format);
+  if ((!saved8 && d.save_format != GWS_SAVE_BF16) || (!x8 && d.x_format != GWS_SAVE_BF16)) return GWS_ERR_UNSUPPORTED;
+  if ((grad_w_gate == nullptr) != (grad_w_up == nullptr)) return GWS_ERR_NULL;
+  if (!on(grad_x, 2) || !on(grad_w_gate, 2) || !on(grad_w_up, 2) || !on(h_out, 2) || !on(status, 4)) return GWS_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (d.m == 0 || d.n == 0 || d.k == 0) {      // empty sums; with k = 0 the projections are zero, and so is h
+    if ((st = zero(grad_x, d.m, d.k, d.k, s)) != GWS_OK || (st = zero(grad_w_gate, d.n, d.k, d.k, s)) != GWS_OK ||
+        (st = zero(grad_w_up, d.n, d.k, d.k, s)) != GWS_OK)
+      return st;
+    return zero(h_out, d.m, d.n, d.n, s);
+  }
+  const bool wants_dw = grad_w_gate != nullptr, wants_dx = grad_x != nullptr;
+  if (grad_h == nullptr || save_gate == nullptr || save_up == nullptr || (wants_dw && x == nullptr) || (wants_dx && (w_gate == nullptr || w_up == nullptr)))
+    return GWS_ERR_NULL;
+  const bool moves_x = x8 || !in_place(d.m, d.ld_x), moves_w = !in_place(d.n, d.ld_w);
+  if (!on(grad_h, 2) || !on(save_gate, saved8 ? 32 : 2) || !on(save_up, saved8 ? 32 : 2) || (wants_dw && !on(x, x8 ? 32 : moves_x ? 2 : 16)) ||
+      (wants_dx && (!on(w_gate, moves_w ? 2 : 16) || !on(w_up, moves_w ? 2 : 16))))
+    return GWS_ERR_ALIGN;
+  const int sms = sm_count();
+  const BackLayout l = back_layout(desc, sms);
+  const int64_t kept = saved_bytes(desc);
+  const Span in_x = x8 ? Span{x, act8_total(d.m, d.k)} : rows_of(x, d.m, d.k, d.ld_x);
+  if (clash({rows_of(grad_x, d.m, d.k, d.k), rows_of(grad_w_gate, d.n, d.k, d.k), rows_of(grad_w_up, d.n, d.k, d.k), rows_of(h_out, d.m, d.n, d.n),
+             {workspace, l.total}},
+            {rows_of(grad_h, d.m, d.n, d.ld_h), in_x, rows_of(w_gate, d.n, d.k, d.ld_w), rows_of(w_up, d.n, d.k, d.ld_w), {save_gate, kept}, {save_up, kept}}))
+    return GWS_ERR_ALIAS;
+  if (!workspace_ok(workspace, workspace_bytes, l.total)) return GWS_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+
+  PreArgs p;
+  std::memset(&p, 0, sizeof p);
+  p.grad_h = static_cast<const uint16_t*>(grad_h);
+  p.ld_grad_h = d.m == 1 ? d.n : d.ld_h;
+  if (saved8) {
+    p.save8[0] = act8_view(save_gate, d.m, d.n);
+    p.save8[1] = act8_view(save_up, d.m, d.n);
+  } else {
+    p.save16[0] = static_cast<const uint16_t*>(save_gate);
+    p.save16[1] = static_cast<const uint16_t*>(save_up);
+  }
+  p.grad_gate = reinterpret_cast<uint16_t*>(ws + l.grad_gate);
+  p.grad_up = reinterpret_cast<uint16_t*>(ws + l.grad_up);
+  p.ld = round_up(d.n, 8);
+  p.h = static_cast<uint16_t*>(h_out);
+  p.cols = d.n;
+  p.per_row = static_cast<uint32_t>(act8_ld(d.n) / kGroup);
+  p.groups = d.m * p.per_row;
+  if (p.groups / 8 >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
+  const bool fast = whole_groups(grad_h, d.n, p.ld_grad_h) && on(h_out, 32) && (saved8 || (on(save_gate, 32) && on(save_up, 32)));
+  if (d.save_format == GWS_ACT8_INT8) launch_pre_act<GWS_ACT8_INT8>(p, d.activation, fast, s);
+  else if (d.save_format == GWS_ACT8_E4M3) launch_pre_act<GWS_ACT8_E4M3>(p, d.activation, fast, s);
+  else launch_pre_act<GWS_SAVE_BF16>(p, d.activation, fast, s);
+  if ((st = gws::finish_launch("gated backward, element-wise part")) != GWS_OK) return st;
+  const Mat dg{p.grad_gate, d.m, d.n, p.ld}, du{p.grad_up, d.m, d.n, p.ld};
+
+  if (wants_dx) {
+    Mat mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
+    if ((st = realign(mg, ws + l.w_gate, s)) != GWS_OK || (st = realign(mu, ws + l.w_up, s)) != GWS_OK) return st;
+    const int64_t kb = steps_of(d.n);
+    const Tile t = choose(kDx, d.m, d.k, 1, 2 * kb, sms);
+    TcArgs args = base_args(t, d.m, d.k, 2 * kb, status);
+    args.kb_first = static_cast<uint32_t>(kb);
+    set_out(args, grad_x, nullptr, d.k);
+    args.part = reinterpret_cast<float*>(ws + l.part);
+    args.ld_part = round_up(d.k, 32);
+    args.part_stride = d.m * args.ld_part;
+    CUtensorMap maps[4];
+    if ((st = make_map(maps[0], dg.p, d.m, d.n, dg.ld, 128)) != GWS_OK || (st = make_map(maps[1], du.p, d.m, d.n, du.ld, 128)) != GWS_OK ||
+        (st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, kTcStep)) != GWS_OK || (st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, kTcStep)) != GWS_OK)
+      return st;
+    if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
+    if (t.splits > 1 && (st = join(args, s)) != GWS_OK) return st;
+  }
+  if (wants_dw) {
+    Mat mx{x, d.m, d.k, d.ld_x};
+    if (x8) {
+      mx = {ws + l.x, d.m, d.k, round_up(d.k, 8)};
+      st = launch_act8(false, d.x_format, mx.p, mx.ld, act8_view(x, d.m, d.k), d.m, d.k, s);
+    } else {
+      st = realign(mx, ws + l.x, s);
+    }
+    if (st != GWS_OK) return st;
+    return run_dw(dg, &du, mx, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
+  }
+  return GWS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,579 @@
+// The tcgen05 GEMM of the gated feed-forward block and of the weight gradients: BF16 operands, FP32 accumulation in tensor
+// memory, one persistent kernel with three uses (MODE):
+//
+//   kGated   h = act(x Wg^T) * (x Wu^T): both projections of a tile of h are two halves of one accumulator, so the activation,
+//            the product and the 8-bit copies for the backward pass happen on registers in the epilogue
+//   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du
+//   kDw      dW = dY^T X: both operands are read along their contiguous (not the contracted) axis, as they lie in memory
+//
+// A tile is 128 * CG rows by BN columns of accumulator; CG = 2 is a pair of SMs working on one tile (cta_group::2: each SM
+// holds its 128 rows of A and half of the columns of B, so an operand byte fetched from L2 feeds twice the products).
+// Warp roles: warp 0 starts the TMA copies (64 elements along the contraction per stage, 128-byte swizzle), warp 1 issues the
+// tcgen05.mma of the pair, warps 4 and up are the epilogue.  The accumulator is double-buffered in tensor memory, so the
+// epilogue of a tile runs under the products of the next one.  Blocks are persistent and take tiles round robin, in groups
+// of rows so that the tiles in flight share operands in L2.
+//
+// With few tiles and a long contraction the contraction is cut into `splits` parts, each written as FP32; k_join adds them in
+// a fixed order, so results do not depend on timing.
+//
+// Every wait is bounded (about a second); a wait that runs out sets the status word, the roles of the block leave their loops,
+// the block gives its copies time to land, frees its tensor memory and returns.
+#pragma once
+#include <cuda.h>
+#include <stdint.h>
+
+#include "gws_act8.cuh"
+
+namespace {
+
+enum { kGated = 0, kDx = 1, kDw = 2 };
+
+constexpr uint32_t kTcStep = 64;                           // elements along the contraction per stage
+constexpr uint32_t kTcABytes = 128u * kTcStep * 2u;
+constexpr uint32_t kTcSmem = 227u * 1024u;
+constexpr uint32_t kTcStagingWarp = 32u * 17u * 4u;        // a 32 x 32 BF16 block per epilogue warp, rows 17 words apart
+constexpr long long kTcWaitCycles = 2000000000LL;
+
+struct TcArgs {
+  uint32_t m_tiles, n_tiles, splits;      // tiles along rows (all outputs), along columns, parts of the contraction
+  uint32_t tiles_per_out;                 // kDw: row tiles of the first output
+  uint32_t kb, kb_first, kb_split;        // steps of the contraction: all, of the first segment (kDx), of one part
+  uint32_t group;                         // row tiles per group of the tile order
+  uint32_t stage_bytes;                   // bytes the copies of one stage bring, over the CG blocks
+  int64_t rows, cols;                     // of one output
+  void* out[2];                           // BF16
+  int64_t ld_out;
+  int32_t direct;                         // rows of `out` take 32-byte stores
+  float* part;                            // splits > 1: FP32 [splits][rows][ld_part]
+  int64_t ld_part, part_stride;           // in elements; part_stride: of one part
+  int32_t activation, save;               // kGated
+  int32_t save_direct;
+  Act8View save8[2];
+  uint16_t* save16[2];                    // BF16 copies, [rows, cols]
+  int* status;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint32_t block_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+// Arrives on a barrier of any block of the pair (shared::cluster address).
+__device__ __forceinline__ void bar_arrive(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// Waits for the phase of the given parity; false if it did not complete within kTcWaitCycles.
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
+  const uint32_t addr = smem_addr(bar);
+  const long long t0 = clock64();
+  for (;;) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    if (done) return true;
+    if (clock64() - t0 > kTcWaitCycles) return false;
+  }
+}
+
+template <int CG>
+__device__ __forceinline__ void copy_in(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y) {
+  if (CG == 2)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
+                 : "memory");
+}
+
+// Shared-memory matrix descriptors, 128-byte swizzle (layout type 2), descriptor version 1.
+// Contraction contiguous: rows of 128 bytes (64 elements along the contraction), 1024 bytes between groups of 8 rows.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
+  return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (static_cast<uint64_t>(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// Other axis contiguous: blocks of 64 elements along it by 64 steps of the contraction (8192 bytes each, one row of 128 bytes
+// per step); 8192 bytes between blocks, 1024 bytes between groups of 8 steps.
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
+  return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(8192u >> 4) << 16) | (static_cast<uint64_t>(1024u >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if (CG == 2)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+// Signals the barrier (in both blocks of a pair) when all products issued so far are done.
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if (CG == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+__device__ __forceinline__ void acc_load(uint32_t addr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+      "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void acc_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// act(g) and its slope.  SiLU is g sigmoid(g); GELU in its tanh form is g sigmoid(z), z = 2 sqrt(2/pi) (g + 0.044715 g^3),
+// because (1 + tanh(z / 2)) / 2 = sigmoid(z).
+constexpr float kGeluLin = 1.59576912160573f;    // 2 sqrt(2 / pi)
+template <int ACT>
+__device__ __forceinline__ float sigmoid_arg(float g) {
+  return ACT == GWS_GATED_SILU ? g : g * __fmaf_rn(kGeluLin * 0.044715f, g * g, kGeluLin);
+}
+template <int ACT>
+__device__ __forceinline__ float act_of(float g) {
+  if (ACT == GWS_GATED_RELU) return g < 0.0f ? 0.0f : g;
+  return __fdividef(g, 1.0f + __expf(-sigmoid_arg<ACT>(g)));
+}
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
+  if (ACT == GWS_GATED_RELU) {
+    a = g < 0.0f ? 0.0f : g;
+    slope = g > 0.0f ? 1.0f : 0.0f;
+    return;
+  }
+  const float s = __fdividef(1.0f, 1.0f + __expf(-sigmoid_arg<ACT>(g)));
+  a = g * s;
+  const float dz = ACT == GWS_GATED_SILU ? 1.0f : __fmaf_rn(3.0f * 0.044715f * kGeluLin, g * g, kGeluLin);
+  slope = __fmaf_rn(a * (1.0f - s), dz, s);
+}
+
+// Writes a 32 x 32 block of BF16 held one row per lane (16 words of two columns each): 32-byte stores where the rows take
+// them, otherwise through shared memory so that the warp still writes one row at a time, side by side.
+__device__ __forceinline__ void store_block(uint16_t* out, int64_t ld, bool direct, int64_t row0, int64_t col0, int64_t rows, int64_t cols,
+                                            const uint32_t (&w)[16], uint32_t* staging, uint32_t lane) {
+  if (direct && col0 + 32 <= cols) {
+    if (row0 + lane < rows) {
+      uint16_t* p = out + (row0 + lane) * ld + col0;
+      V8 a, b;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { a.x[i] = w[i]; b.x[i] = w[8 + i]; }
+      st32(p, a);
+      st32(p + 16, b);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) staging[lane * 17u + i] = w[i];
+  __syncwarp();
+  const uint16_t* s = reinterpret_cast<const uint16_t*>(staging);
+  const int64_t left = rows - row0;
+  const uint32_t n = left < 32 ? (left < 0 ? 0u : static_cast<uint32_t>(left)) : 32u;
+  if (col0 + lane < cols)
+    for (uint32_t r = 0; r < n; ++r) out[(row0 + r) * ld + col0 + lane] = s[r * 34u + lane];
+  __syncwarp();
+}
+
+template <int ACT>
+__device__ __forceinline__ void gate_block(const uint32_t (&g)[32], const uint32_t (&u)[32], uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    w[i] = pack_bf16(act_of<ACT>(__uint_as_float(g[2 * i])) * __uint_as_float(u[2 * i]),
+                     act_of<ACT>(__uint_as_float(g[2 * i + 1])) * __uint_as_float(u[2 * i + 1]));
+}
+
+template <int CG, int BN, int MODE>
+struct TcShape {
+  static constexpr uint32_t kBRows = BN / CG;                              // columns of B each block holds
+  static constexpr uint32_t kStage = kTcABytes + kBRows * kTcStep * 2u;
+  static constexpr uint32_t kPerSm = BN <= 64 ? 2u : 1u;                   // resident blocks
+  static constexpr uint32_t kEpilogueWarps = BN <= 64 ? 4u : 8u;           // one or two per quadrant of the accumulator's rows
+  static constexpr uint32_t kThreads = 128u + 32u * kEpilogueWarps;
+  static constexpr uint32_t kStaging = kEpilogueWarps * kTcStagingWarp;
+  static constexpr uint32_t kFit = (kTcSmem / kPerSm - 4096u - kStaging) / kStage;
+  static constexpr uint32_t kStages = kFit > 8u ? 8u : kFit;
+  static constexpr uint32_t kSmemBytes = kStages * kStage + kStaging + 1024u;
+  static constexpr uint32_t kTmemCols = 2 * BN;
+};
+
+template <int CG, int BN, int MODE>
+__global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG, BN, MODE>::kPerSm))
+    k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
+         const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
+  using S = TcShape<CG, BN, MODE>;
+  constexpr bool kMnA = MODE == kDw, kMnB = MODE != kGated;
+  constexpr uint32_t kStages = S::kStages;
+  // instruction descriptor: FP32 accumulator, BF16 operands, which axis of A and B is contiguous, N, M
+  constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kMnA ? 1u : 0u) << 15) | ((kMnB ? 1u : 0u) << 16) |
+                              (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int failed;
+  const uint32_t raw = smem_addr(smem_raw);
+  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);   // the same offset in both blocks of a pair
+  uint32_t* staging = reinterpret_cast<uint32_t*>(smem + kStages * S::kStage);
+
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint32_t rank = CG == 2 ? block_rank() : 0u;
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < kStages; ++s) {
+      bar_init(&full[s], 1);
+      bar_init(&empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(&acc_full[b], 1);
+      bar_init(&acc_empty[b], S::kEpilogueWarps * CG);
+    }
+    failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    if (CG == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(S::kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(S::kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (CG == 2) pair_sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+
+  const uint32_t tiles = p.m_tiles * p.n_tiles, work = tiles * p.splits;
+  const uint32_t first = blockIdx.x / CG, stride = gridDim.x / CG;
+  // tile -> (row tile, column tile): groups of `group` row tiles, column by column inside a group
+  auto place = [&](uint32_t t, uint32_t& mt, uint32_t& nt, uint32_t& k0, uint32_t& k1) {
+    const uint32_t split = t / tiles;
+    t -= split * tiles;
+    const uint32_t per_group = p.group * p.n_tiles, g = t / per_group, rest = t - g * per_group;
+    const uint32_t height = min(p.group, p.m_tiles - g * p.group);
+    nt = rest / height;
+    mt = g * p.group + (rest - nt * height);
+    k0 = split * p.kb_split;
+    k1 = min(p.kb, k0 + p.kb_split);
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (uint32_t t = first; ok && t < work; t += stride) {
+        uint32_t mt, nt, k0, k1;
+        place(t, mt, nt, k0, k1);
+        const bool second = MODE == kDw && mt >= p.tiles_per_out;
+        const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
+        const int32_t n0 = static_cast<int32_t>(nt * (MODE == kGated ? BN / 2 : BN));
+        for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
+          const uint32_t s = it % kStages;
+          if (it >= kStages && !bar_wait(&empty[s], (it / kStages - 1u) & 1u)) { ok = false; break; }
+          if (rank == 0) bar_expect(&full[s], p.stage_bytes);
+          const uint32_t bar = CG == 2 ? at_rank(smem_addr(&full[s]), 0u) : smem_addr(&full[s]);
+          const uint32_t sa = smem_addr(smem + s * S::kStage), sb = sa + kTcABytes;
+          if (MODE == kGated) {
+            const int32_t k = static_cast<int32_t>(kb * kTcStep);
+            copy_in<CG>(sa, &a0, bar, k, m0);
+            if (CG == 2) {                       // block 0 holds the gate's rows, block 1 the up projection's
+              copy_in<CG>(sb, rank == 0 ? &b0 : &b1, bar, k, n0);
+            } else {
+              copy_in<CG>(sb, &b0, bar, k, n0);
+              copy_in<CG>(sb + (BN / 2) * kTcStep * 2u, &b1, bar, k, n0);
+            }
+          } else if (MODE == kDx) {
+            const bool seg = kb >= p.kb_first;
+            const int32_t k = static_cast<int32_t>((seg ? kb - p.kb_first : kb) * kTcStep);
+            copy_in<CG>(sa, seg ? &a1 : &a0, bar, k, m0);
+#pragma unroll
+            for (uint32_t j = 0; j < S::kBRows / 64u; ++j)
+              copy_in<CG>(sb + j * 8192u, seg ? &b1 : &b0, bar, n0 + static_cast<int32_t>(rank * S::kBRows + j * 64u), k);
+          } else {
+            const int32_t k = static_cast<int32_t>(kb * kTcStep);
+#pragma unroll
+            for (uint32_t j = 0; j < 2u; ++j) copy_in<CG>(sa + j * 8192u, second ? &a1 : &a0, bar, m0 + static_cast<int32_t>(j * 64u), k);
+#pragma unroll
+            for (uint32_t j = 0; j < S::kBRows / 64u; ++j)
+              copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(rank * S::kBRows + j * 64u), k);
+          }
+        }
+      }
+      if (!ok) atomicExch(&failed, 1);
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      uint32_t it = 0, n = 0;
+      bool ok = true;
+      for (uint32_t t = first; ok && t < work; t += stride, ++n) {
+        uint32_t mt, nt, k0, k1;
+        place(t, mt, nt, k0, k1);
+        const uint32_t buf = n & 1u, d = tmem + buf * BN;
+        if (n >= 2 && !bar_wait(&acc_empty[buf], ((n >> 1) - 1u) & 1u)) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
+          const uint32_t s = it % kStages;
+          if (!bar_wait(&full[s], (it / kStages) & 1u)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t sa = smem_addr(smem + s * S::kStage), sb = sa + kTcABytes;
+#pragma unroll
+          for (uint32_t j = 0; j < kTcStep / 16u; ++j)   // 16 steps of the contraction: 32 bytes of a row, or 16 rows of 128 bytes
+            mma<CG>(d, kMnA ? desc_mn(sa + j * 2048u) : desc_k(sa + j * 32u), kMnB ? desc_mn(sb + j * 2048u) : desc_k(sb + j * 32u), kIdesc,
+                    (kb > k0 || j > 0) ? 1u : 0u);
+          commit<CG>(&empty[s]);
+        }
+        if (ok) commit<CG>(&acc_full[buf]);
+      }
+      if (!ok) atomicExch(&failed, 1);
+    }
+  } else if (warp >= 4) {
+    const uint32_t quadrant = warp & 3u, half = (warp - 4u) >> 2;   // a warp reads the 32 accumulator rows of its quadrant
+    uint32_t* stage = staging + (warp - 4u) * 32u * 17u;
+    uint32_t n = 0;
+    for (uint32_t t = first; t < work; t += stride, ++n) {
+      uint32_t mt, nt, k0, k1;
+      place(t, mt, nt, k0, k1);
+      const uint32_t buf = n & 1u;
+      if (__any_sync(0xFFFFFFFFu, !bar_wait(&acc_full[buf], (n >> 1) & 1u))) { atomicExch(&failed, 1); break; }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
+      const bool second = MODE == kDw && mt >= p.tiles_per_out;
+      const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + rank * 128u + quadrant * 32u;
+      if (MODE == kGated) {
+#pragma unroll 1
+        for (uint32_t c = half; c < BN / 64; c += S::kEpilogueWarps / 4u) {
+          uint32_t g[32], u[32], w[16];
+          acc_load(acc + c * 32u, g);
+          acc_load(acc + BN / 2 + c * 32u, u);
+          acc_wait();
+          const int64_t col0 = static_cast<int64_t>(nt) * (BN / 2) + c * 32u;
+          if (col0 >= p.cols) continue;
+          if (p.activation == GWS_GATED_SILU) gate_block<GWS_GATED_SILU>(g, u, w);
+          else if (p.activation == GWS_GATED_GELU_TANH) gate_block<GWS_GATED_GELU_TANH>(g, u, w);
+          else gate_block<GWS_GATED_RELU>(g, u, w);
+          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+          if (p.save == GWS_SAVE_BF16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
+            store_block(p.save16[0], p.cols, p.save_direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+            store_block(p.save16[1], p.cols, p.save_direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+          } else if (p.save != GWS_SAVE_NONE && row0 + lane < p.rows) {
+            // columns past the width are products with rows of zeros: zero codes, as the layout wants them
+            const int64_t row = row0 + lane;
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+              float v[kGroup];
+#pragma unroll
+              for (int i = 0; i < kGroup; ++i) v[i] = __uint_as_float(which == 0 ? g[i] : u[i]);
+              V8 codes;
+              const uint32_t byte = p.save == GWS_ACT8_INT8 ? encode_group<GWS_ACT8_INT8>(v, codes) : encode_group<GWS_ACT8_E4M3>(v, codes);
+              st32(p.save8[which].codes + row * p.save8[which].ld + col0, codes);
+              p.save8[which].scales[row * (p.save8[which].ld >> 5) + (col0 >> 5)] = static_cast<uint8_t>(byte);
+            }
+          }
+        }
+      } else {
+        uint16_t* out = static_cast<uint16_t*>(p.out[second ? 1 : 0]);
+        float* part = p.part + static_cast<int64_t>(t / tiles) * p.part_stride + (second ? p.rows * p.ld_part : 0);
+#pragma unroll 1
+        for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
+          uint32_t v[32];
+          acc_load(acc + c * 32u, v);
+          acc_wait();
+          const int64_t col0 = static_cast<int64_t>(nt) * BN + c * 32u;
+          if (col0 >= p.cols) continue;
+          if (p.splits > 1) {
+            if (row0 + lane < p.rows) {
+              float* q = part + (row0 + lane) * p.ld_part + col0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                V8 x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x.x[e] = v[8 * i + e];
+                st32(q + 8 * i, x);
+              }
+            }
+          } else {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+            store_block(out, p.ld_out, p.direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+          }
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) bar_arrive(at_rank(smem_addr(&acc_empty[buf]), 0u));
+    }
+  }
+  __syncthreads();
+  if (failed) {                          // copies and products that were started get time to end before the memory is given up
+    if (threadIdx.x == 0 && p.status != nullptr) atomicExch(p.status, 1);
+    const long long t0 = clock64();
+    while (clock64() - t0 < kTcWaitCycles / 16) {}
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (CG == 2) pair_sync();              // the other block's products read this block's shared memory until here
+  if (warp == 2) {
+    if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");
+  }
+}
+
+// Adds the parts of a split contraction in order and rounds once.  A thread takes four columns of a row.
+__global__ void __launch_bounds__(256) k_join(const float* part, int64_t ld_part, int64_t part_stride, uint32_t splits, uint16_t* out0, uint16_t* out1,
+                                              int64_t ld_out, int64_t rows, int64_t cols, int32_t wide) {
+  const int64_t quads = ld_part >> 2, t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (t >= quads * rows * (out1 != nullptr ? 2 : 1)) return;
+  const int64_t row = t / quads, col = (t - row * quads) * 4;
+  if (col >= cols) return;
+  const float* q = part + row * ld_part + col;
+  float4 s = *reinterpret_cast<const float4*>(q);
+  for (uint32_t i = 1; i < splits; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(q + i * part_stride);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  uint16_t* o = (row >= rows ? out1 + (row - rows) * ld_out : out0 + row * ld_out) + col;
+  const uint32_t lo = pack_bf16(s.x, s.y), hi = pack_bf16(s.z, s.w);
+  if (wide && col + 4 <= cols) {
+    *reinterpret_cast<uint2*>(o) = make_uint2(lo, hi);
+    return;
+  }
+  o[0] = static_cast<uint16_t>(lo);
+  if (col + 1 < cols) o[1] = static_cast<uint16_t>(lo >> 16);
+  if (col + 2 < cols) o[2] = static_cast<uint16_t>(hi);
+  if (col + 3 < cols) o[3] = static_cast<uint16_t>(hi >> 16);
+}
+
+// ---- the element-wise part of the backward pass ------------------------------------------------------------------------------
+// From dh and the saved g, u:  dg = dh u act'(g),  du = dh act(g),  and h = act(g) u for the next layer's weight gradient.  dg and
+// du are rounded to BF16 because the tensor cores take them in that form; their sums dx and dW are FP32 again.
+struct PreArgs {
+  const uint16_t* grad_h;
+  int64_t ld_grad_h;
+  Act8View save8[2];
+  const uint16_t* save16[2];
+  uint16_t *grad_gate, *grad_up;
+  int64_t ld;                      // of grad_gate and grad_up
+  uint16_t* h;                     // may be null, [rows, cols]
+  int64_t cols, groups;            // groups: rows * ceil(cols / 32)
+  uint32_t per_row;
+};
+
+// Memory-bound, one pass: 2 + 2 (1 + 1/32) bytes in, 4 or 6 bytes out per element.  A thread takes a group of 32 columns.
+template <int SAVE, int ACT>
+__global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreArgs p) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (t >= p.groups) return;
+  int64_t at_dh = t * kGroup;
+  if (p.ld_grad_h != p.cols) {
+    const int64_t row = t / p.per_row;
+    at_dh = row * p.ld_grad_h + (t - row * p.per_row) * kGroup;
+  }
+  const int64_t at = t * kGroup;     // saved values, results: rows side by side
+  V8 cg, cu;
+  float ug = 0.0f, uu = 0.0f;
+  if (SAVE != GWS_SAVE_BF16) {
+    cg = ld32(p.save8[0].codes + at);
+    cu = ld32(p.save8[1].codes + at);
+    ug = unit_of<SAVE>(p.save8[0].scales[t]);
+    uu = unit_of<SAVE>(p.save8[1].scales[t]);
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {      // 16 columns at a time
+    const V8 dh = ld32(p.grad_h + at_dh + 16 * q);
+    float g[16], u[16];
+    if (SAVE == GWS_SAVE_BF16) {
+      const V8 a = ld32(p.save16[0] + at + 16 * q), b = ld32(p.save16[1] + at + 16 * q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        g[2 * i] = bf16_lo(a.x[i]); g[2 * i + 1] = bf16_hi(a.x[i]);
+        u[2 * i] = bf16_lo(b.x[i]); u[2 * i + 1] = bf16_hi(b.x[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        decode4<SAVE>(cg.x[4 * q + i], ug, g + 4 * i);
+        decode4<SAVE>(cu.x[4 * q + i], uu, u + 4 * i);
+      }
+    }
+    V8 dg, du, h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float a[2], d1[2], d2[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float grad = e == 0 ? bf16_lo(dh.x[i]) : bf16_hi(dh.x[i]);
+        float act, slope;
+        act_and_slope<ACT>(g[2 * i + e], act, slope);
+        d1[e] = grad * u[2 * i + e] * slope;
+        d2[e] = grad * act;
+        a[e] = act * u[2 * i + e];
+      }
+      dg.x[i] = pack_bf16(d1[0], d1[1]);
+      du.x[i] = pack_bf16(d2[0], d2[1]);
+      h.x[i] = pack_bf16(a[0], a[1]);
+    }
+    st32(p.grad_gate + at + 16 * q, dg);
+    st32(p.grad_up + at + 16 * q, du);
+    if (p.h != nullptr) st32(p.h + at + 16 * q, h);
+  }
+}
+
+// Any width, stride and alignment: a lane takes an element of a group.
+template <int SAVE, int ACT>
+__global__ void __launch_bounds__(256) k_gated_pre_lane(const __grid_constant__ PreArgs p) {
+  const uint32_t lane = threadIdx.x & 31u;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  if (t >= p.groups) return;
+  const int64_t row = t / p.per_row, col = (t - row * p.per_row) * kGroup + lane;
+  if (col >= p.cols) return;
+  float g[4], u[4];
+  if (SAVE == GWS_SAVE_BF16) {
+    g[0] = __uint_as_float(static_cast<uint32_t>(p.save16[0][row * p.cols + col]) << 16);
+    u[0] = __uint_as_float(static_cast<uint32_t>(p.save16[1][row * p.cols + col]) << 16);
+  } else {
+    decode4<SAVE>(p.save8[0].codes[t * kGroup + lane], unit_of<SAVE>(p.save8[0].scales[t]), g);
+    decode4<SAVE>(p.save8[1].codes[t * kGroup + lane], unit_of<SAVE>(p.save8[1].scales[t]), u);
+  }
+  const float grad = __uint_as_float(static_cast<uint32_t>(p.grad_h[row * p.ld_grad_h + col]) << 16);
+  float act, slope;
+  act_and_slope<ACT>(g[0], act, slope);
+  p.grad_gate[row * p.ld + col] = static_cast<uint16_t>(pack_bf16(grad * u[0] * slope, 0.0f));
+  p.grad_up[row * p.ld + col] = static_cast<uint16_t>(pack_bf16(grad * act, 0.0f));
+  if (p.h != nullptr) p.h[row * p.cols + col] = static_cast<uint16_t>(pack_bf16(act * u[0], 0.0f));
+}
+
+}  // namespace
