@@ -7,6 +7,7 @@ If the library is missing or cannot be loaded the functions raise: there is no C
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int8, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 from typing import List, Optional, Sequence
@@ -550,110 +551,124 @@ def _act8_bytes(rows: int, cols: int) -> int:
     return -(-groups * 32 // 256) * 256 + groups
 
 
-class _On:
-    """The stream of a call: allocations made inside belong to it, whichever stream is current."""
-
-    def __init__(self, stream, device):
-        if stream is None:
-            self.handle, self.guard = c_void_p(torch.cuda.current_stream(device).cuda_stream), None
-        else:
-            if not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream), device=device)
-            self.handle, self.guard = c_void_p(stream.cuda_stream), torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.handle
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_BF16 = torch.bfloat16
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _bf16_rows(t: torch.Tensor, name: str, shape=None, read_by_map: bool = True):
-    """A BF16 matrix as the library takes it, and its row stride.  Whatever its strides cannot say (columns apart, rows that
-    overlap, a base the tensor maps refuse) is copied."""
-    if t.dim() != 2 or t.dtype != torch.bfloat16:
+def _on_stream(stream, device, call, *args, **kwargs):
+    """Runs a call with ``stream`` current, so that what it allocates belongs to the stream it launches on."""
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return call(*args, **kwargs)
+
+
+def _device_of(*tensors: Optional[torch.Tensor]) -> int:
+    """The one device of a call's tensors."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            device = -1
+    if device < 0:
+        _require_cuda(*tensors)
+        raise ValueError("gws: the tensors of a call live on one device")
+    return device
+
+
+def _bf16_rows(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None, read_by_map: bool = True):
+    """A BF16 matrix as the library takes it: (tensor, its address, its row stride).  Whatever its strides cannot say (columns
+    apart, rows that overlap, a base the tensor maps refuse) is copied."""
+    if t.dtype is not _BF16 or t.dim() != 2:
         raise ValueError("gws: %s must be a 2-D BF16 tensor" % name)
-    if not t.is_cuda:
-        raise ValueError("gws: device pointers expected (tensor is on %s)" % t.device)
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("gws: %s must be %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    rows, cols = t.shape
-    if t.numel() and ((cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols)):
-        t = t.contiguous()
-    ld = t.stride(0) if rows > 1 and cols > 0 else max(cols, 1)
-    if read_by_map and t.numel() and t.data_ptr() % 16 and (rows <= 1 or ld % 8 == 0):
-        t = t.contiguous().clone()
-        ld = max(cols, 1)
-    return t, ld
+    r, c = t.shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError("gws: %s must be (%s, %s), not (%d, %d)" % (name, "any" if rows is None else rows, "any" if cols is None else cols, r, c))
+    ld = c
+    if not t.is_contiguous():
+        if (c > 1 and t.stride(1) != 1) or (r > 1 and t.stride(0) < c):
+            t = t.contiguous()
+        elif r > 1:
+            ld = t.stride(0)
+    p = t.data_ptr()
+    if read_by_map and p & 15 and (r <= 1 or ld % 8 == 0):
+        t = t.clone(memory_format=torch.contiguous_format)
+        p, ld = t.data_ptr(), c
+    return t, p, ld or 1
 
 
 def _bf16_out(t: Optional[torch.Tensor], name: str, rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
     if t is None:
-        return torch.empty((rows, cols), dtype=torch.bfloat16, device=like.device)
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols) or not t.is_contiguous() or t.device != like.device:
-        raise ValueError("gws: %s must be a contiguous BF16 [%d, %d] tensor on %s" % (name, rows, cols, like.device))
+        return like.new_empty((rows, cols))
+    if t.dtype is not _BF16 or tuple(t.shape) != (rows, cols) or not t.is_contiguous():
+        raise ValueError("gws: %s must be a contiguous BF16 [%d, %d] tensor" % (name, rows, cols))
     return t
 
 
-def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("gws: tensors on %s and %s in one call" % (first.device, t.device))
-
-
-def _workspace(nbytes: int, device):
+def _workspace(nbytes: int, like: torch.Tensor):
+    """(tensor to keep until the launch, its address)."""
     if nbytes < 0:
         raise GwsError(int(nbytes))
-    return (torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes) if nbytes else (None, 0)
+    if not nbytes:
+        return None, None
+    t = like.new_empty(nbytes, dtype=torch.uint8)
+    return t, t.data_ptr()
+
+
+def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
 
 
 def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None, stream=None) -> Act8:
     """BF16 [rows, cols] -> 8-bit checkpoint (``out`` is overwritten if given)."""
-    _require_cuda(x)
-    with _On(stream, x.device) as s:
-        x, ld = _bf16_rows(x, "x", read_by_map=False)
-        rows, cols = x.shape
-        if out is None:
-            out = Act8(torch.empty(_act8_bytes(rows, cols), dtype=torch.uint8, device=x.device), rows, cols, fmt)
-        elif out.shape != (rows, cols) or out.fmt != fmt:
-            raise ValueError("gws: out is a checkpoint of another shape or format")
-        _same_device(x, out.buffer)
-        _check(load_library().gws_act8_save(rows, cols, ld, fmt, x.data_ptr(), out.buffer.data_ptr(), s))
+    device = _device_of(x, None if out is None else out.buffer)
+    if stream is not None:
+        return _on_stream(stream, device, act8_save, x, fmt, out)
+    x, p, ld = _bf16_rows(x, "x", read_by_map=False)
+    rows, cols = x.shape
+    if out is None:
+        out = Act8(x.new_empty(_act8_bytes(rows, cols), dtype=torch.uint8), rows, cols, fmt)
+    elif out.shape != (rows, cols) or out.fmt != fmt:
+        raise ValueError("gws: out is a checkpoint of another shape or format")
+    _check(load_library().gws_act8_save(rows, cols, ld, fmt, p, out.buffer.data_ptr(), _raw_stream(device)))
     return out
 
 
 def act8_load(a: Act8, x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """8-bit checkpoint -> BF16 [rows, cols] (written to ``x`` if given; its rows may be strided)."""
-    _require_cuda(a.buffer, x)
-    with _On(stream, a.buffer.device) as s:
-        if x is None:
-            x = torch.empty((a.rows, a.cols), dtype=torch.bfloat16, device=a.buffer.device)
-        elif x.dtype != torch.bfloat16 or tuple(x.shape) != a.shape or (x.numel() and ((a.cols > 1 and x.stride(1) != 1) or (a.rows > 1 and x.stride(0) < a.cols))):
+    device = _device_of(a.buffer, x)
+    if stream is not None:
+        return _on_stream(stream, device, act8_load, a, x)
+    rows, cols, ld = a.rows, a.cols, a.cols
+    if x is None:
+        x = a.buffer.new_empty((rows, cols), dtype=_BF16)
+    else:
+        if x.dtype is not _BF16 or tuple(x.shape) != a.shape or (x.numel() and ((cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols))):
             raise ValueError("gws: x must be a BF16 [%d, %d] tensor whose rows are contiguous" % a.shape)
-        _same_device(a.buffer, x)
-        ld = x.stride(0) if a.rows > 1 else max(a.cols, 1)
-        _check(load_library().gws_act8_load(a.rows, a.cols, ld, a.fmt, a.buffer.data_ptr(), x.data_ptr(), s))
+        if rows > 1:
+            ld = x.stride(0)
+    _check(load_library().gws_act8_load(rows, cols, ld or 1, a.fmt, a.buffer.data_ptr(), x.data_ptr(), _raw_stream(device)))
     return x
+
+
+@functools.lru_cache(maxsize=1024)
+def _wgrad_workspace(m: int, n: int, k: int, ld_y: int, device: int) -> int:
+    return load_library().gws_wgrad_act8_workspace_bytes(m, n, k, ld_y)
 
 
 def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
     """dW = grad_y^T @ x for a linear layer y = x W^T whose input is held as a checkpoint.  BF16 [n, k]."""
-    _require_cuda(grad_y, x8.buffer, grad_w, status)
-    _same_device(grad_y, x8.buffer, status)
-    with _On(stream, grad_y.device) as s:
-        grad_y, ld = _bf16_rows(grad_y, "grad_y")
-        (m, n), k = grad_y.shape, x8.cols
-        if x8.rows != m:
-            raise ValueError("gws: grad_y has %d rows and the checkpoint %d" % (m, x8.rows))
-        grad_w = _bf16_out(grad_w, "grad_w", n, k, grad_y)
-        lib = load_library()
-        ws, nbytes = _workspace(lib.gws_wgrad_act8_workspace_bytes(m, n, k, ld), grad_y.device)
-        _check(lib.gws_wgrad_act8(m, n, k, x8.fmt, grad_y.data_ptr(), ld, x8.buffer.data_ptr(), grad_w.data_ptr(), max(k, 1), _ptr(ws), nbytes,
-                                  _ptr(status), s))
+    device = _device_of(grad_y, x8.buffer, grad_w, status)
+    if stream is not None:
+        return _on_stream(stream, device, wgrad_act8, grad_y, x8, grad_w, status)
+    m, k = x8.rows, x8.cols
+    grad_y, p, ld = _bf16_rows(grad_y, "grad_y", m)
+    n = grad_y.shape[1]
+    grad_w = _bf16_out(grad_w, "grad_w", n, k, grad_y)
+    nbytes = _wgrad_workspace(m, n, k, ld, device)
+    ws, ws_p = _workspace(nbytes, grad_y)
+    _check(load_library().gws_wgrad_act8(m, n, k, x8.fmt, p, ld, x8.buffer.data_ptr(), grad_w.data_ptr(), k or 1, ws_p, nbytes, _addr(status),
+                                         _raw_stream(device)))
     return grad_w
 
 
@@ -665,43 +680,53 @@ class GatedSaved:
         self.gate, self.up, self.fmt = gate, up, fmt
 
     def tensors(self):
-        return (self.gate.buffer, self.up.buffer) if isinstance(self.gate, Act8) else (self.gate, self.up)
+        return (self.gate, self.up) if self.fmt == SAVE_BF16 else (self.gate.buffer, self.up.buffer)
 
 
-def _new_saved(m: int, n: int, fmt: int, device) -> Optional[GatedSaved]:
-    if fmt == SAVE_NONE:
-        return None
-    if fmt == SAVE_BF16:
-        make = lambda: torch.empty((m, n), dtype=torch.bfloat16, device=device)
-    else:
-        make = lambda: Act8(torch.empty(_act8_bytes(m, n), dtype=torch.uint8, device=device), m, n, fmt)
-    return GatedSaved(make(), make(), fmt)
+@functools.lru_cache(maxsize=1024)
+def _gated_plan(m: int, n: int, k: int, ld_x: int, ld_w: int, ld_h: int, activation: int, save: int, x_format: int, backward: int, device: int):
+    """(descriptor, its address, workspace bytes) of a call: functions of the sizes alone."""
+    d = GatedDesc(m, n, k, ld_x, ld_w, ld_h, activation, save, x_format, 0)
+    at = ctypes.addressof(d)
+    nbytes = load_library().gws_gated_workspace_bytes(at, backward)
+    if nbytes < 0:
+        raise GwsError(int(nbytes))
+    return d, at, nbytes
+
+
+def _two_weights(w_gate: torch.Tensor, w_up: torch.Tensor, n: int, k: int):
+    w_gate, p_gate, ld = _bf16_rows(w_gate, "w_gate", n, k)
+    w_up, p_up, ld_up = _bf16_rows(w_up, "w_up", n, k)
+    if ld_up != ld:                                       # one stride for both weights
+        w_gate, p_gate, ld = _bf16_rows(w_gate.contiguous(), "w_gate", n, k)
+        w_up, p_up, _ = _bf16_rows(w_up.contiguous(), "w_up", n, k)
+    return w_gate, w_up, p_gate, p_up, ld
 
 
 def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: int = GATED_SILU, save: int = SAVE_NONE,
               h: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
     """h = act(x Wg^T) * (x Wu^T) for x [m, k] and weights [n, k], in one kernel.  Returns (h, saved): ``save`` says what the gate
     and the up projection are kept as for :func:`gated_bwd` (ACT8_INT8, ACT8_E4M3, SAVE_BF16; SAVE_NONE keeps nothing)."""
-    _require_cuda(x, w_gate, w_up, h, status)
-    _same_device(x, w_gate, w_up, status)
-    if save not in (ACT8_INT8, ACT8_E4M3, SAVE_BF16, SAVE_NONE):
-        raise GwsError(ERR_UNSUPPORTED)
-    with _On(stream, x.device) as s:
-        x, ld_x = _bf16_rows(x, "x")
-        m, k = x.shape
-        w_gate, ld_w = _bf16_rows(w_gate, "w_gate", (w_gate.shape[0], k))
-        n = w_gate.shape[0]
-        w_up, ld_up = _bf16_rows(w_up, "w_up", (n, k))
-        if ld_up != ld_w:                                     # one stride for both weights
-            w_gate, w_up, ld_w = w_gate.contiguous(), w_up.contiguous(), max(k, 1)
-        h = _bf16_out(h, "h", m, n, x)
-        saved = _new_saved(m, n, save, x.device)
-        gate, up = saved.tensors() if saved is not None else (None, None)
-        d = GatedDesc(m, n, k, ld_x, ld_w, max(n, 1), activation, save, SAVE_BF16, 0)
-        lib = load_library()
-        ws, nbytes = _workspace(lib.gws_gated_workspace_bytes(ctypes.byref(d), 0), x.device)
-        _check(lib.gws_gated_fwd(ctypes.byref(d), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), h.data_ptr(), _ptr(gate), _ptr(up), _ptr(ws), nbytes,
-                                 _ptr(status), s))
+    device = _device_of(x, w_gate, w_up, h, status)
+    if stream is not None:
+        return _on_stream(stream, device, gated_fwd, x, w_gate, w_up, activation, save, h, status)
+    x, p_x, ld_x = _bf16_rows(x, "x")
+    m, k = x.shape
+    n = w_gate.shape[0]
+    w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
+    _, at, nbytes = _gated_plan(m, n, k, ld_x, ld_w, n or 1, activation, save, SAVE_BF16, 0, device)
+    h = _bf16_out(h, "h", m, n, x)
+    saved = p_sg = p_su = None
+    if save == SAVE_BF16:
+        saved = GatedSaved(x.new_empty((m, n)), x.new_empty((m, n)), save)
+    elif save == ACT8_INT8 or save == ACT8_E4M3:
+        size = _act8_bytes(m, n)
+        saved = GatedSaved(Act8(x.new_empty(size, dtype=torch.uint8), m, n, save), Act8(x.new_empty(size, dtype=torch.uint8), m, n, save), save)
+    if saved is not None:
+        gate, up = saved.tensors()
+        p_sg, p_su = gate.data_ptr(), up.data_ptr()
+    ws, ws_p = _workspace(nbytes, x)
+    _check(load_library().gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, _addr(status), _raw_stream(device)))
     return h, saved
 
 
@@ -709,32 +734,29 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
               want_h: bool = False, want_grad_x: bool = True, want_grad_w: bool = True, status: Optional[torch.Tensor] = None, stream=None):
     """Backward pass of :func:`gated_fwd`.  ``x`` is the BF16 input or its checkpoint.  Returns (grad_x, grad_w_gate, grad_w_up, h);
     what was not asked for is None.  ``h`` is act(gate) * up again, which the weight gradient of the layer after the block needs."""
-    x_tensor = x.buffer if isinstance(x, Act8) else x
-    _require_cuda(grad_h, x_tensor, w_gate, w_up, status, *saved.tensors())
-    _same_device(grad_h, x_tensor, w_gate, w_up, status, *saved.tensors())
-    with _On(stream, grad_h.device) as s:
-        m, k = x.shape
-        n = w_gate.shape[0]
-        grad_h, ld_h = _bf16_rows(grad_h, "grad_h", (m, n), read_by_map=False)
-        ld_x, x_format = max(k, 1), SAVE_BF16
-        if isinstance(x, Act8):
-            x_format = x.fmt
-        else:
-            x_tensor, ld_x = _bf16_rows(x, "x")
-        w_gate, ld_w = _bf16_rows(w_gate, "w_gate", (n, k))
-        w_up, ld_up = _bf16_rows(w_up, "w_up", (n, k))
-        if ld_up != ld_w:
-            w_gate, w_up, ld_w = w_gate.contiguous(), w_up.contiguous(), max(k, 1)
-        if tuple(saved.gate.shape) != (m, n) or tuple(saved.up.shape) != (m, n):
-            raise ValueError("gws: the kept projections are %s, not (%d, %d)" % (tuple(saved.gate.shape), m, n))
-        gate, up = saved.tensors()
-        new = lambda rows, cols, want: torch.empty((rows, cols), dtype=torch.bfloat16, device=grad_h.device) if want else None
-        grad_x, grad_wg, grad_wu, h = new(m, k, want_grad_x), new(n, k, want_grad_w), new(n, k, want_grad_w), new(m, n, want_h)
-        d = GatedDesc(m, n, k, ld_x, ld_w, ld_h, activation, saved.fmt, x_format, 0)
-        lib = load_library()
-        ws, nbytes = _workspace(lib.gws_gated_workspace_bytes(ctypes.byref(d), 1), grad_h.device)
-        _check(lib.gws_gated_bwd(ctypes.byref(d), grad_h.data_ptr(), x_tensor.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(), up.data_ptr(),
-                                 _ptr(grad_x), _ptr(grad_wg), _ptr(grad_wu), _ptr(h), _ptr(ws), nbytes, _ptr(status), s))
+    kept_x = isinstance(x, Act8)
+    gate, up = saved.tensors()
+    device = _device_of(grad_h, x.buffer if kept_x else x, w_gate, w_up, gate, up, status)
+    if stream is not None:
+        return _on_stream(stream, device, gated_bwd, grad_h, x, w_gate, w_up, saved, activation, want_h, want_grad_x, want_grad_w, status)
+    m, k = x.shape
+    n = w_gate.shape[0]
+    grad_h, p_dh, ld_h = _bf16_rows(grad_h, "grad_h", m, n, read_by_map=False)
+    if kept_x:
+        x_t, p_x, ld_x, x_format = x.buffer, x.buffer.data_ptr(), k or 1, x.fmt
+    else:
+        x_t, p_x, ld_x = _bf16_rows(x, "x")
+        x_format = SAVE_BF16
+    w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
+    if tuple(saved.gate.shape) != (m, n) or tuple(saved.up.shape) != (m, n):
+        raise ValueError("gws: the kept projections are %s, not (%d, %d)" % (tuple(saved.gate.shape), m, n))
+    _, at, nbytes = _gated_plan(m, n, k, ld_x, ld_w, ld_h, activation, saved.fmt, x_format, 1, device)
+    grad_x = grad_h.new_empty((m, k)) if want_grad_x else None
+    grad_wg, grad_wu = (grad_h.new_empty((n, k)), grad_h.new_empty((n, k))) if want_grad_w else (None, None)
+    h = grad_h.new_empty((m, n)) if want_h else None
+    ws, ws_p = _workspace(nbytes, grad_h)
+    _check(load_library().gws_gated_bwd(at, p_dh, p_x, p_gate, p_up, gate.data_ptr(), up.data_ptr(), _addr(grad_x), _addr(grad_wg), _addr(grad_wu),
+                                        _addr(h), ws_p, nbytes, _addr(status), _raw_stream(device)))
     return grad_x, grad_wg, grad_wu, h
 
 

@@ -167,37 +167,88 @@ __global__ void __launch_bounds__(256) k_act8_load(Act8View c, uint16_t* x, int6
   st32(x + at + 16, out[1]);
 }
 
-// The general forms: any width, row stride and 2-byte alignment.  A warp takes a group, a lane an element, so that rows of
-// any alignment are still read and written side by side.  Columns past the width become zero codes.
-template <int FMT>
-__global__ void __launch_bounds__(256) k_act8_save_lane(const uint16_t* x, int64_t ldx, Act8View c, int64_t groups, uint32_t per_row, int64_t cols) {
-  const uint32_t lane = threadIdx.x & 31u;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (t >= groups) return;
-  const int64_t row = t / per_row, col = (t - row * per_row) * kGroup + lane;
-  const float v = col < cols ? __uint_as_float(static_cast<uint32_t>(x[row * ldx + col]) << 16) : 0.0f;
-  const uint32_t byte = scale_byte(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v) & 0x7FFFFFFFu), FMT);
-  const uint32_t code = byte == kNanByte ? 0u : encode4<FMT>(v, 0.0f, 0.0f, 0.0f, inverse_scale_of(byte));
-  c.codes[t * kGroup + lane] = static_cast<uint8_t>(code);
-  if (lane == 0) c.scales[t] = static_cast<uint8_t>(byte);
+// t / d; one 32-bit division wherever the numbers allow it (a 64-bit one is a routine of some hundred instructions).
+__device__ __forceinline__ int64_t quotient(int64_t t, uint32_t d) {
+  return (t >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(t) / d) : t / static_cast<int64_t>(d);
 }
 
+// The general forms: any width, row stride and 2-byte alignment of the BF16 side.
+// Save: four lanes share a group, eight elements each, read one by one (a warp's reads cover 512 neighbouring bytes) and written as
+// one 8-byte word of codes; columns past the width become zero codes.
 template <int FMT>
-__global__ void __launch_bounds__(256) k_act8_load_lane(Act8View c, uint16_t* x, int64_t ldx, int64_t groups, uint32_t per_row, int64_t cols) {
+__global__ void __launch_bounds__(256) k_act8_save_any(const uint16_t* x, int64_t ldx, Act8View c, int64_t quarters, uint32_t per_row, int64_t cols) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const bool real = t < quarters;
+  const int64_t row = real ? quotient(t, per_row) : 0, col = real ? (t - row * per_row) * 8 : cols;
+  const uint16_t* p = x + row * ldx + col;
+  float v[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? __uint_as_float(static_cast<uint32_t>(p[i]) << 16) : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+  top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+  if (!real) return;
+  const uint32_t byte = scale_byte(top, FMT);
+  const float inv = inverse_scale_of(byte);
+  const uint2 codes = byte == kNanByte ? make_uint2(0u, 0u) : make_uint2(encode4<FMT>(v[0], v[1], v[2], v[3], inv), encode4<FMT>(v[4], v[5], v[6], v[7], inv));
+  *reinterpret_cast<uint2*>(c.codes + t * 8) = codes;
+  if ((t & 3) == 0) c.scales[t >> 2] = static_cast<uint8_t>(byte);
+}
+
+// Load: a warp takes four neighbouring groups of a row, a lane an element of each, so that rows of any alignment are written side
+// by side (BF16 written one by one by a thread of its own would cost a partial write of a memory sector each).
+constexpr int kRun = 4;
+template <int FMT>
+__global__ void __launch_bounds__(256) k_act8_load_any(Act8View c, uint16_t* x, int64_t ldx, int64_t runs, uint32_t runs_per_row, uint32_t per_row,
+                                                       int64_t cols) {
   const uint32_t lane = threadIdx.x & 31u;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (t >= groups) return;
-  const int64_t row = t / per_row, col = (t - row * per_row) * kGroup + lane;
-  float v[4];
-  decode4<FMT>(c.codes[t * kGroup + lane], unit_of<FMT>(c.scales[t]), v);
-  if (col < cols) x[row * ldx + col] = static_cast<uint16_t>(pack_bf16(v[0], 0.0f));
+  if (t >= runs) return;
+  const int64_t row = quotient(t, runs_per_row);
+  const uint32_t g0 = static_cast<uint32_t>(t - row * runs_per_row) * kRun;
+  const int64_t group = row * per_row + g0, col = static_cast<int64_t>(g0) * kGroup + lane;
+  uint32_t code[kRun], byte[kRun];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    const bool real = g0 + i < per_row;
+    code[i] = real ? c.codes[(group + i) * kGroup + lane] : 0u;
+    byte[i] = real ? c.scales[group + i] : 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    float v[4];
+    decode4<FMT>(code[i], unit_of<FMT>(byte[i]), v);
+    if (col + i * kGroup < cols) x[row * ldx + col + i * kGroup] = static_cast<uint16_t>(pack_bf16(v[0], 0.0f));
+  }
 }
 
 // ---- BF16 rows brought into the alignment a tensor map wants ---------------------------------------------------------------
-__global__ void __launch_bounds__(256) k_realign(const uint16_t* x, int64_t ldx, uint16_t* out, int64_t ld_out, int64_t rows, int64_t cols) {
-  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
-    for (int64_t col = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; col < cols; col += static_cast<int64_t>(gridDim.x) * 256)
-      out[row * ld_out + col] = x[row * ldx + col];
+// Up to three matrices in a launch (the input and both weights).  A thread writes 16 aligned bytes from eight reads; columns past
+// the width are zero.
+struct Moves {
+  const uint16_t* from[3];
+  uint16_t* to[3];
+  int64_t ld_from[3], cols[3];
+  int64_t end[3];               // threads of the first 1, 2, 3 matrices
+  uint32_t per_row[3];          // 16-byte units in a row of the copy
+};
+__global__ void __launch_bounds__(256) k_realign(const __grid_constant__ Moves m) {
+  int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int w = t >= m.end[1] ? 2 : t >= m.end[0] ? 1 : 0;
+  if (t >= m.end[2]) return;
+  const uint16_t* from = w == 0 ? m.from[0] : w == 1 ? m.from[1] : m.from[2];
+  uint16_t* to = w == 0 ? m.to[0] : w == 1 ? m.to[1] : m.to[2];
+  const int64_t ld = w == 0 ? m.ld_from[0] : w == 1 ? m.ld_from[1] : m.ld_from[2], cols = w == 0 ? m.cols[0] : w == 1 ? m.cols[1] : m.cols[2];
+  const uint32_t per_row = w == 0 ? m.per_row[0] : w == 1 ? m.per_row[1] : m.per_row[2];
+  t -= w == 0 ? 0 : w == 1 ? m.end[0] : m.end[1];
+  const int64_t row = quotient(t, per_row), col = (t - row * per_row) * 8;
+  const uint16_t* p = from + row * ld + col;
+  uint32_t v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? p[i] : 0u;
+  *reinterpret_cast<uint4*>(to + t * 8) = make_uint4(v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16));
 }
 
 }  // namespace

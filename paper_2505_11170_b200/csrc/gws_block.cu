@@ -2,6 +2,8 @@
 // and the gated feed-forward block.  Argument validation, tensor maps, choice of tile and launch geometry; no device memory is
 // allocated here.
 #include <algorithm>
+#include <atomic>
+#include <cmath>
 #include <cstring>
 #include <initializer_list>
 #include <string>
@@ -66,18 +68,23 @@ unsigned blocks_for(int64_t items, int64_t per_block) { return static_cast<unsig
 
 int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8View& c, int64_t rows, int64_t cols, cudaStream_t s) {
   const int64_t per_row = c.ld / kGroup, groups = rows * per_row;
-  const bool fast = whole_groups(x, cols, ldx);
-  if (groups / (fast ? kJobs : 8) >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
+  const bool fast = whole_groups(x, cols, ldx), i8 = format == GWS_ACT8_INT8;
+  if (groups / 8 >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
   uint16_t* px = static_cast<uint16_t*>(const_cast<void*>(x));
   const uint32_t pr = static_cast<uint32_t>(per_row);
-  const unsigned grid = blocks_for(groups, fast ? kJobs : 8);
-  const bool i8 = format == GWS_ACT8_INT8;
   if (fast) {
+    const unsigned grid = blocks_for(groups, kJobs);
     if (save) i8 ? k_act8_save<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr) : k_act8_save<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr);
     else i8 ? k_act8_load<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr) : k_act8_load<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr);
+  } else if (save) {
+    const unsigned grid = blocks_for(groups * 4, kJobs);
+    if (i8) k_act8_save_any<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups * 4, pr * 4u, cols);
+    else k_act8_save_any<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups * 4, pr * 4u, cols);
   } else {
-    if (save) i8 ? k_act8_save_lane<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr, cols) : k_act8_save_lane<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr, cols);
-    else i8 ? k_act8_load_lane<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr, cols) : k_act8_load_lane<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr, cols);
+    const uint32_t runs = (pr + kRun - 1) / kRun;
+    const unsigned grid = blocks_for(rows * runs, 8);
+    if (i8) k_act8_load_any<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, rows * runs, runs, pr, cols);
+    else k_act8_load_any<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, rows * runs, runs, pr, cols);
   }
   return gws::finish_launch("activation checkpoint kernel");
 }
@@ -109,24 +116,43 @@ int make_map(CUtensorMap& map, const void* p, int64_t rows, int64_t cols, int64_
   return GWS_OK;
 }
 
-// A matrix as the GEMM reads it: rows on 16-byte boundaries, in place or in the workspace.
+// A matrix as the GEMM reads it: rows on 16-byte boundaries, in place or as a copy in the workspace.  Copies have rows of whole
+// groups of 32, so that checkpoints are restored into them, and gradients written to them, a group at a time whatever the width.
 struct Mat {
   const void* p;
   int64_t rows, cols, ld;
 };
 bool in_place(int64_t rows, int64_t ld) { return rows <= 1 || ld % 8 == 0; }
-int64_t packed_bytes(int64_t rows, int64_t cols) { return round_up(rows * round_up(cols, 8) * 2, 256); }
+int64_t packed_ld(int64_t cols) { return round_up(cols, kGroup); }
+int64_t packed_bytes(int64_t rows, int64_t cols) { return round_up(rows * packed_ld(cols) * 2, 256); }
 
-int realign(Mat& m, void* to, cudaStream_t s) {
-  if (in_place(m.rows, m.ld)) {
-    m.ld = round_up(m.rows <= 1 ? m.cols : m.ld, 8);
-    return GWS_OK;
+// Brings those of up to three matrices that need it into the workspace, one after the other from `to`, in one launch.
+int realign(std::initializer_list<Mat*> mats, char* to, cudaStream_t s) {
+  Moves m;
+  std::memset(&m, 0, sizeof m);
+  int n = 0;
+  int64_t threads = 0;
+  for (Mat* a : mats) {
+    if (in_place(a->rows, a->ld)) {
+      a->ld = round_up(a->rows <= 1 ? a->cols : a->ld, 8);
+      continue;
+    }
+    const int64_t ld = packed_ld(a->cols);
+    m.from[n] = static_cast<const uint16_t*>(a->p);
+    m.to[n] = reinterpret_cast<uint16_t*>(to);
+    m.ld_from[n] = a->ld;
+    m.cols[n] = a->cols;
+    m.per_row[n] = static_cast<uint32_t>(ld / 8);
+    threads += a->rows * (ld / 8);
+    m.end[n++] = threads;
+    a->p = to;
+    a->ld = ld;
+    to += packed_bytes(a->rows, a->cols);
   }
-  const int64_t ld = round_up(m.cols, 8);
-  const dim3 grid(std::min<unsigned>(blocks_for(m.cols, kJobs), 64u), static_cast<unsigned>(std::min<int64_t>(m.rows, 65535)));
-  k_realign<<<grid, kJobs, 0, s>>>(static_cast<const uint16_t*>(m.p), m.ld, static_cast<uint16_t*>(to), ld, m.rows, m.cols);
-  m.p = to;
-  m.ld = ld;
+  if (n == 0) return GWS_OK;
+  for (int i = n; i < 3; ++i) m.end[i] = threads;
+  if (threads / kJobs >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
+  k_realign<<<blocks_for(threads, kJobs), kJobs, 0, s>>>(m);
   return gws::finish_launch("row alignment kernel");
 }
 
@@ -180,7 +206,14 @@ int64_t part_bytes(const Tile& t, int64_t rows, int64_t cols, int outs) {
 template <int CG, int BN, int MODE>
 int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStream_t s) {
   using S = TcShape<CG, BN, MODE>;
-  cudaError_t err = cudaFuncSetAttribute(k_tc<CG, BN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmemBytes));
+  static std::atomic<uint64_t> ready{0};        // devices on which this kernel has been given its shared memory
+  int dev = 0;
+  cudaError_t err = cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (err == cudaSuccess && (dev > 63 || (ready.load(std::memory_order_relaxed) & bit) == 0)) {
+    err = cudaFuncSetAttribute(k_tc<CG, BN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmemBytes));
+    if (err == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
+  }
   if (err != cudaSuccess) return gws::report_cuda(err, "shared memory of the block GEMM");
   const uint32_t work = args.m_tiles * args.n_tiles * args.splits;
   const uint32_t slots = CG == 2 ? static_cast<uint32_t>(sms / 2) : static_cast<uint32_t>(sms) * S::kPerSm;
@@ -312,7 +345,7 @@ int64_t forward_bytes(const gws_gated_desc* d) {
 template <int SAVE, int ACT>
 void launch_pre(const PreArgs& p, bool fast, cudaStream_t s) {
   if (fast) k_gated_pre<SAVE, ACT><<<blocks_for(p.groups, kJobs), kJobs, 0, s>>>(p);
-  else k_gated_pre_lane<SAVE, ACT><<<blocks_for(p.groups, 8), kJobs, 0, s>>>(p);
+  else k_gated_pre_any<SAVE, ACT><<<blocks_for(p.rows * ((p.per_row + kRun - 1) / kRun), 8), kJobs, 0, s>>>(p);
 }
 template <int SAVE>
 void launch_pre_act(const PreArgs& p, int act, bool fast, cudaStream_t s) {
@@ -381,14 +414,14 @@ int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad
   if (clash({rows_of(grad_w, n, k, ld_w), {workspace, need}}, {rows_of(grad_y, m, n, ld_y), {x8, act8_total(m, k)}})) return GWS_ERR_ALIAS;
   if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
-  const int64_t ldx = round_up(k, 8);
-  st = launch_act8(false, format, ws, ldx, act8_view(x8, m, k), m, k, s);
+  const int64_t ldx = packed_ld(k);
+  st = launch_act8(false, format, ws, ldx, act8_view(x8, m, k), m, ldx, s);
   if (st != GWS_OK) return st;
   const Mat x{ws, m, k, ldx};
   ws += packed_bytes(m, k);
   Mat y{grad_y, m, n, ld_y};
   const bool moved = !in_place(m, ld_y);
-  st = realign(y, ws, s);
+  st = realign({&y}, ws, s);
   if (st != GWS_OK) return st;
   if (moved) ws += packed_bytes(m, n);
   return run_dw(y, nullptr, x, grad_w, nullptr, ld_w, ws, status, sm_count(), s);
@@ -429,13 +462,8 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
             {rows_of(x, d.m, d.k, d.ld_x), rows_of(w_gate, d.n, d.k, d.ld_w), rows_of(w_up, d.n, d.k, d.ld_w)}))
     return GWS_ERR_ALIAS;
   if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
-  char* ws = static_cast<char*>(workspace);
   Mat mx{x, d.m, d.k, d.ld_x}, mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
-  if ((st = realign(mx, ws, s)) != GWS_OK) return st;
-  if (moves_x) ws += packed_bytes(d.m, d.k);
-  if ((st = realign(mg, ws, s)) != GWS_OK) return st;
-  if (moves_w) ws += packed_bytes(d.n, d.k);
-  if ((st = realign(mu, ws, s)) != GWS_OK) return st;
+  if ((st = realign({&mx, &mg, &mu}, static_cast<char*>(workspace), s)) != GWS_OK) return st;
 
   const int sms = sm_count();
   const Tile t = choose(kGated, d.m, d.n, 1, steps_of(d.k), sms);
@@ -507,7 +535,8 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   }
   p.grad_gate = reinterpret_cast<uint16_t*>(ws + l.grad_gate);
   p.grad_up = reinterpret_cast<uint16_t*>(ws + l.grad_up);
-  p.ld = round_up(d.n, 8);
+  p.ld = packed_ld(d.n);
+  p.rows = d.m;
   p.h = static_cast<uint16_t*>(h_out);
   p.cols = d.n;
   p.per_row = static_cast<uint32_t>(act8_ld(d.n) / kGroup);
@@ -522,7 +551,7 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
 
   if (wants_dx) {
     Mat mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
-    if ((st = realign(mg, ws + l.w_gate, s)) != GWS_OK || (st = realign(mu, ws + l.w_up, s)) != GWS_OK) return st;
+    if ((st = realign({&mg, &mu}, ws + l.w_gate, s)) != GWS_OK) return st;
     const int64_t kb = steps_of(d.n);
     const Tile t = choose(kDx, d.m, d.k, 1, 2 * kb, sms);
     TcArgs args = base_args(t, d.m, d.k, 2 * kb, status);
@@ -541,10 +570,10 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   if (wants_dw) {
     Mat mx{x, d.m, d.k, d.ld_x};
     if (x8) {
-      mx = {ws + l.x, d.m, d.k, round_up(d.k, 8)};
-      st = launch_act8(false, d.x_format, mx.p, mx.ld, act8_view(x, d.m, d.k), d.m, d.k, s);
+      mx = {ws + l.x, d.m, d.k, packed_ld(d.k)};
+      st = launch_act8(false, d.x_format, mx.p, mx.ld, act8_view(x, d.m, d.k), d.m, mx.ld, s);
     } else {
-      st = realign(mx, ws + l.x, s);
+      st = realign({&mx}, ws + l.x, s);
     }
     if (st != GWS_OK) return st;
     return run_dw(dg, &du, mx, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);

@@ -77,20 +77,30 @@ __device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// Waits for the phase of the given parity; false if it did not complete within kTcWaitCycles.
-__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
-  const uint32_t addr = smem_addr(bar);
+// A whole warp waits for the phase of the given parity; false, for every lane, if it did not complete within kTcWaitCycles.  The
+// clock is only read once the first try has failed: the two warps that feed the tensor cores pass here once per stage.
+__device__ __forceinline__ bool bar_try(uint32_t addr, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done)
+               : "r"(addr), "r"(parity)
+               : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t addr, uint32_t parity) {
+  if (__all_sync(0xFFFFFFFFu, bar_try(addr, parity))) return true;
   const long long t0 = clock64();
   for (;;) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(addr), "r"(parity)
-        : "memory");
-    if (done) return true;
-    if (clock64() - t0 > kTcWaitCycles) return false;
+    if (__all_sync(0xFFFFFFFFu, bar_try(addr, parity))) return true;
+    if (__any_sync(0xFFFFFFFFu, clock64() - t0 > kTcWaitCycles)) return false;
   }
+}
+// One lane of a converged warp.  The loops around it are run by the whole warp, so that addresses and descriptors stay in
+// uniform registers: a loop run by one lane alone spent 346 cycles on the four products and the commit of a stage.
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
 }
 
 template <int CG>
@@ -238,7 +248,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
   __shared__ uint32_t tmem_slot;
-  __shared__ int failed;
+  __shared__ volatile int failed;
   const uint32_t raw = smem_addr(smem_raw);
   uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);   // the same offset in both blocks of a pair
   uint32_t* staging = reinterpret_cast<uint32_t*>(smem + kStages * S::kStage);
@@ -287,25 +297,24 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
   };
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
-      for (uint32_t t = first; ok && t < work; t += stride) {
-        uint32_t mt, nt, k0, k1;
-        place(t, mt, nt, k0, k1);
-        const bool second = MODE == kDw && mt >= p.tiles_per_out;
-        const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
-        const int32_t n0 = static_cast<int32_t>(nt * (MODE == kGated ? BN / 2 : BN));
-        for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
-          const uint32_t s = it % kStages;
-          if (it >= kStages && !bar_wait(&empty[s], (it / kStages - 1u) & 1u)) { ok = false; break; }
+    uint32_t s = 0, parity = 1;                        // stage, and the parity of its last release (none before the first round)
+    bool ok = true;
+    const uint32_t full0 = CG == 2 ? at_rank(smem_addr(&full[0]), 0u) : smem_addr(&full[0]), empty0 = smem_addr(&empty[0]);
+    for (uint32_t t = first; ok && t < work; t += stride) {
+      uint32_t mt, nt, k0, k1;
+      place(t, mt, nt, k0, k1);
+      const bool second = MODE == kDw && mt >= p.tiles_per_out;
+      const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
+      const int32_t n0 = static_cast<int32_t>(nt * (MODE == kGated ? BN / 2 : BN) + (MODE == kGated ? 0u : rank * S::kBRows));
+      for (uint32_t kb = k0; kb < k1; ++kb) {
+        if (!bar_wait(empty0 + 8u * s, parity)) { ok = false; break; }
+        if (elected()) {
           if (rank == 0) bar_expect(&full[s], p.stage_bytes);
-          const uint32_t bar = CG == 2 ? at_rank(smem_addr(&full[s]), 0u) : smem_addr(&full[s]);
-          const uint32_t sa = smem_addr(smem + s * S::kStage), sb = sa + kTcABytes;
+          const uint32_t bar = full0 + 8u * s, sa = smem_addr(smem) + s * S::kStage, sb = sa + kTcABytes;
           if (MODE == kGated) {
             const int32_t k = static_cast<int32_t>(kb * kTcStep);
             copy_in<CG>(sa, &a0, bar, k, m0);
-            if (CG == 2) {                       // block 0 holds the gate's rows, block 1 the up projection's
+            if (CG == 2) {                             // block 0 holds the gate's rows, block 1 the up projection's
               copy_in<CG>(sb, rank == 0 ? &b0 : &b1, bar, k, n0);
             } else {
               copy_in<CG>(sb, &b0, bar, k, n0);
@@ -316,44 +325,52 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
             const int32_t k = static_cast<int32_t>((seg ? kb - p.kb_first : kb) * kTcStep);
             copy_in<CG>(sa, seg ? &a1 : &a0, bar, k, m0);
 #pragma unroll
-            for (uint32_t j = 0; j < S::kBRows / 64u; ++j)
-              copy_in<CG>(sb + j * 8192u, seg ? &b1 : &b0, bar, n0 + static_cast<int32_t>(rank * S::kBRows + j * 64u), k);
+            for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, seg ? &b1 : &b0, bar, n0 + static_cast<int32_t>(j * 64u), k);
           } else {
             const int32_t k = static_cast<int32_t>(kb * kTcStep);
 #pragma unroll
             for (uint32_t j = 0; j < 2u; ++j) copy_in<CG>(sa + j * 8192u, second ? &a1 : &a0, bar, m0 + static_cast<int32_t>(j * 64u), k);
 #pragma unroll
-            for (uint32_t j = 0; j < S::kBRows / 64u; ++j)
-              copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(rank * S::kBRows + j * 64u), k);
+            for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(j * 64u), k);
           }
         }
+        __syncwarp();
+        if (++s == kStages) { s = 0; parity ^= 1u; }
       }
-      if (!ok) atomicExch(&failed, 1);
     }
+    if (!ok) failed = 1;
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
-      uint32_t it = 0, n = 0;
+    if (rank == 0) {
+      uint32_t s = 0, parity = 0, n = 0;
       bool ok = true;
+      const uint32_t full0 = smem_addr(&full[0]), acc_empty0 = smem_addr(&acc_empty[0]);
+      const uint64_t da = kMnA ? desc_mn(smem_addr(smem)) : desc_k(smem_addr(smem));
+      const uint64_t db = kMnB ? desc_mn(smem_addr(smem) + kTcABytes) : desc_k(smem_addr(smem) + kTcABytes);
+      // 16 steps of the contraction in the units of a descriptor's address: 32 bytes of a row, or 16 rows of 128 bytes
+      constexpr uint32_t kStepA = (kMnA ? 2048u : 32u) >> 4, kStepB = (kMnB ? 2048u : 32u) >> 4;
       for (uint32_t t = first; ok && t < work; t += stride, ++n) {
         uint32_t mt, nt, k0, k1;
         place(t, mt, nt, k0, k1);
         const uint32_t buf = n & 1u, d = tmem + buf * BN;
-        if (n >= 2 && !bar_wait(&acc_empty[buf], ((n >> 1) - 1u) & 1u)) { ok = false; break; }
+        if (!bar_wait(acc_empty0 + 8u * buf, ((n >> 1) & 1u) ^ 1u)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
-          const uint32_t s = it % kStages;
-          if (!bar_wait(&full[s], (it / kStages) & 1u)) { ok = false; break; }
+        for (uint32_t kb = k0; kb < k1; ++kb) {
+          if (!bar_wait(full0 + 8u * s, parity)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t sa = smem_addr(smem + s * S::kStage), sb = sa + kTcABytes;
+          if (elected()) {
+            const uint64_t sa = da + s * (S::kStage >> 4), sb = db + s * (S::kStage >> 4);
+            mma<CG>(d, sa, sb, kIdesc, kb > k0 ? 1u : 0u);
 #pragma unroll
-          for (uint32_t j = 0; j < kTcStep / 16u; ++j)   // 16 steps of the contraction: 32 bytes of a row, or 16 rows of 128 bytes
-            mma<CG>(d, kMnA ? desc_mn(sa + j * 2048u) : desc_k(sa + j * 32u), kMnB ? desc_mn(sb + j * 2048u) : desc_k(sb + j * 32u), kIdesc,
-                    (kb > k0 || j > 0) ? 1u : 0u);
-          commit<CG>(&empty[s]);
+            for (uint32_t j = 1; j < kTcStep / 16u; ++j) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
+            commit<CG>(&empty[s]);
+          }
+          __syncwarp();
+          if (++s == kStages) { s = 0; parity ^= 1u; }
         }
-        if (ok) commit<CG>(&acc_full[buf]);
+        if (ok && elected()) commit<CG>(&acc_full[buf]);
+        __syncwarp();
       }
-      if (!ok) atomicExch(&failed, 1);
+      if (!ok) failed = 1;
     }
   } else if (warp >= 4) {
     const uint32_t quadrant = warp & 3u, half = (warp - 4u) >> 2;   // a warp reads the 32 accumulator rows of its quadrant
@@ -363,7 +380,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
       uint32_t mt, nt, k0, k1;
       place(t, mt, nt, k0, k1);
       const uint32_t buf = n & 1u;
-      if (__any_sync(0xFFFFFFFFu, !bar_wait(&acc_full[buf], (n >> 1) & 1u))) { atomicExch(&failed, 1); break; }
+      if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) { failed = 1; break; }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
       const bool second = MODE == kDw && mt >= p.tiles_per_out;
@@ -488,7 +505,7 @@ struct PreArgs {
   uint16_t *grad_gate, *grad_up;
   int64_t ld;                      // of grad_gate and grad_up
   uint16_t* h;                     // may be null, [rows, cols]
-  int64_t cols, groups;            // groups: rows * ceil(cols / 32)
+  int64_t rows, cols, groups;      // groups: rows * ceil(cols / 32)
   uint32_t per_row;
 };
 
@@ -552,28 +569,51 @@ __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreAr
   }
 }
 
-// Any width, stride and alignment: a lane takes an element of a group.
+// Any width, stride and alignment of grad_h, of kept BF16 values and of h: a warp takes four neighbouring groups of a row, a lane an
+// element of each.  (One thread with a group of its own would read and write 64 bytes at 2-byte alignment, 32 separate accesses.)
 template <int SAVE, int ACT>
-__global__ void __launch_bounds__(256) k_gated_pre_lane(const __grid_constant__ PreArgs p) {
-  const uint32_t lane = threadIdx.x & 31u;
+__global__ void __launch_bounds__(256) k_gated_pre_any(const __grid_constant__ PreArgs p) {
+  const uint32_t lane = threadIdx.x & 31u, runs_per_row = (p.per_row + kRun - 1) / kRun;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  if (t >= p.groups) return;
-  const int64_t row = t / p.per_row, col = (t - row * p.per_row) * kGroup + lane;
-  if (col >= p.cols) return;
-  float g[4], u[4];
-  if (SAVE == GWS_SAVE_BF16) {
-    g[0] = __uint_as_float(static_cast<uint32_t>(p.save16[0][row * p.cols + col]) << 16);
-    u[0] = __uint_as_float(static_cast<uint32_t>(p.save16[1][row * p.cols + col]) << 16);
-  } else {
-    decode4<SAVE>(p.save8[0].codes[t * kGroup + lane], unit_of<SAVE>(p.save8[0].scales[t]), g);
-    decode4<SAVE>(p.save8[1].codes[t * kGroup + lane], unit_of<SAVE>(p.save8[1].scales[t]), u);
+  const int64_t row = quotient(t, runs_per_row);
+  if (row >= p.rows) return;
+  const uint32_t g0 = static_cast<uint32_t>(t - row * runs_per_row) * kRun;
+  const int64_t group = row * p.per_row + g0, col = static_cast<int64_t>(g0) * kGroup + lane;
+  const uint16_t* dh = p.grad_h + row * p.ld_grad_h + col;
+  uint32_t cg[kRun], cu[kRun], sg[kRun], su[kRun], d[kRun];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    const bool real = g0 + i < p.per_row, in = col + i * kGroup < p.cols;
+    d[i] = in ? dh[i * kGroup] : 0u;
+    if (SAVE == GWS_SAVE_BF16) {
+      cg[i] = in ? p.save16[0][row * p.cols + col + i * kGroup] : 0u;
+      cu[i] = in ? p.save16[1][row * p.cols + col + i * kGroup] : 0u;
+    } else {
+      cg[i] = real ? p.save8[0].codes[(group + i) * kGroup + lane] : 0u;
+      cu[i] = real ? p.save8[1].codes[(group + i) * kGroup + lane] : 0u;
+      sg[i] = real ? p.save8[0].scales[group + i] : 0u;
+      su[i] = real ? p.save8[1].scales[group + i] : 0u;
+    }
   }
-  const float grad = __uint_as_float(static_cast<uint32_t>(p.grad_h[row * p.ld_grad_h + col]) << 16);
-  float act, slope;
-  act_and_slope<ACT>(g[0], act, slope);
-  p.grad_gate[row * p.ld + col] = static_cast<uint16_t>(pack_bf16(grad * u[0] * slope, 0.0f));
-  p.grad_up[row * p.ld + col] = static_cast<uint16_t>(pack_bf16(grad * act, 0.0f));
-  if (p.h != nullptr) p.h[row * p.cols + col] = static_cast<uint16_t>(pack_bf16(act * u[0], 0.0f));
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    if (col + i * kGroup >= p.cols) break;
+    float g[4], u[4];
+    if (SAVE == GWS_SAVE_BF16) {
+      g[0] = __uint_as_float(cg[i] << 16);
+      u[0] = __uint_as_float(cu[i] << 16);
+    } else {
+      decode4<SAVE>(cg[i], unit_of<SAVE>(sg[i]), g);
+      decode4<SAVE>(cu[i], unit_of<SAVE>(su[i]), u);
+    }
+    const float grad = __uint_as_float(d[i] << 16);
+    float act, slope;
+    act_and_slope<ACT>(g[0], act, slope);
+    const int64_t at = row * p.ld + col + i * kGroup;
+    p.grad_gate[at] = static_cast<uint16_t>(pack_bf16(grad * u[0] * slope, 0.0f));
+    p.grad_up[at] = static_cast<uint16_t>(pack_bf16(grad * act, 0.0f));
+    if (p.h != nullptr) p.h[row * p.cols + col + i * kGroup] = static_cast<uint16_t>(pack_bf16(act * u[0], 0.0f));
+  }
 }
 
 }  // namespace
