@@ -35,6 +35,14 @@ __device__ __forceinline__ void st32(void* p, const V8& v) {
                : "memory");
 }
 
+// Kernels of one call follow each other with programmatic launches: a kernel's blocks may become resident while the one before it on
+// the stream drains, and touch global memory only once that one has completed.  Every kernel of this file set passes here
+// before its first access, so the order along the stream holds transitively.
+__device__ __forceinline__ void after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -123,6 +131,7 @@ struct Act8View {                 // a checkpoint in memory
 
 template <int FMT>
 __global__ void __launch_bounds__(256) k_act8_save(const uint16_t* x, int64_t ldx, Act8View c, int64_t groups, uint32_t per_row) {
+  after_previous();
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (t >= groups) return;
   int64_t at = t * kGroup;
@@ -146,6 +155,7 @@ __global__ void __launch_bounds__(256) k_act8_save(const uint16_t* x, int64_t ld
 
 template <int FMT>
 __global__ void __launch_bounds__(256) k_act8_load(Act8View c, uint16_t* x, int64_t ldx, int64_t groups, uint32_t per_row) {
+  after_previous();
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (t >= groups) return;
   int64_t at = t * kGroup;
@@ -177,6 +187,7 @@ __device__ __forceinline__ int64_t quotient(int64_t t, uint32_t d) {
 // one 8-byte word of codes; columns past the width become zero codes.
 template <int FMT>
 __global__ void __launch_bounds__(256) k_act8_save_any(const uint16_t* x, int64_t ldx, Act8View c, int64_t quarters, uint32_t per_row, int64_t cols) {
+  after_previous();
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   const bool real = t < quarters;
   const int64_t row = real ? quotient(t, per_row) : 0, col = real ? (t - row * per_row) * 8 : cols;
@@ -203,6 +214,7 @@ constexpr int kRun = 4;
 template <int FMT>
 __global__ void __launch_bounds__(256) k_act8_load_any(Act8View c, uint16_t* x, int64_t ldx, int64_t runs, uint32_t runs_per_row, uint32_t per_row,
                                                        int64_t cols) {
+  after_previous();
   const uint32_t lane = threadIdx.x & 31u;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
   if (t >= runs) return;
@@ -235,6 +247,7 @@ struct Moves {
   uint32_t per_row[3];          // 16-byte units in a row of the copy
 };
 __global__ void __launch_bounds__(256) k_realign(const __grid_constant__ Moves m) {
+  after_previous();
   int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   const int w = t >= m.end[1] ? 2 : t >= m.end[0] ? 1 : 0;
   if (t >= m.end[2]) return;

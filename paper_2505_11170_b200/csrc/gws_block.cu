@@ -64,6 +64,29 @@ int zero(void* p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t s) {
 // Whether every group of a [rows, cols] BF16 tensor is 64 whole bytes on a 32-byte boundary: a thread then takes a group.
 bool whole_groups(const void* p, int64_t cols, int64_t ld) { return cols % kGroup == 0 && ld % 16 == 0 && on(p, 32); }
 
+// Launches a kernel that may overlap the end of the one before it on the stream (after_previous in the kernels).
+template <class... P, class... A>
+int launch(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t s, const char* what, const A&... args) {
+  cudaLaunchConfig_t cfg;
+  std::memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+  if (err != cudaSuccess) { (void)cudaGetLastError(); return gws::report_cuda(err, what); }
+  return gws::finish_launch(what);
+}
+
 unsigned blocks_for(int64_t items, int64_t per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
 
 int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8View& c, int64_t rows, int64_t cols, cudaStream_t s) {
@@ -72,21 +95,18 @@ int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8Vie
   if (groups / 8 >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
   uint16_t* px = static_cast<uint16_t*>(const_cast<void*>(x));
   const uint32_t pr = static_cast<uint32_t>(per_row);
+  const char* what = "activation checkpoint kernel";
   if (fast) {
     const unsigned grid = blocks_for(groups, kJobs);
-    if (save) i8 ? k_act8_save<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr) : k_act8_save<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups, pr);
-    else i8 ? k_act8_load<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr) : k_act8_load<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, groups, pr);
-  } else if (save) {
-    const unsigned grid = blocks_for(groups * 4, kJobs);
-    if (i8) k_act8_save_any<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(px, ldx, c, groups * 4, pr * 4u, cols);
-    else k_act8_save_any<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(px, ldx, c, groups * 4, pr * 4u, cols);
-  } else {
-    const uint32_t runs = (pr + kRun - 1) / kRun;
-    const unsigned grid = blocks_for(rows * runs, 8);
-    if (i8) k_act8_load_any<GWS_ACT8_INT8><<<grid, kJobs, 0, s>>>(c, px, ldx, rows * runs, runs, pr, cols);
-    else k_act8_load_any<GWS_ACT8_E4M3><<<grid, kJobs, 0, s>>>(c, px, ldx, rows * runs, runs, pr, cols);
+    if (save) return launch(i8 ? k_act8_save<GWS_ACT8_INT8> : k_act8_save<GWS_ACT8_E4M3>, grid, kJobs, 0, 1, s, what, px, ldx, c, groups, pr);
+    return launch(i8 ? k_act8_load<GWS_ACT8_INT8> : k_act8_load<GWS_ACT8_E4M3>, grid, kJobs, 0, 1, s, what, c, px, ldx, groups, pr);
   }
-  return gws::finish_launch("activation checkpoint kernel");
+  if (save)
+    return launch(i8 ? k_act8_save_any<GWS_ACT8_INT8> : k_act8_save_any<GWS_ACT8_E4M3>, blocks_for(groups * 4, kJobs), kJobs, 0, 1, s, what, px, ldx, c, groups * 4,
+                  pr * 4u, cols);
+  const uint32_t runs = (pr + kRun - 1) / kRun;
+  return launch(i8 ? k_act8_load_any<GWS_ACT8_INT8> : k_act8_load_any<GWS_ACT8_E4M3>, blocks_for(rows * runs, 8), kJobs, 0, 1, s, what, c, px, ldx, rows * runs, runs,
+                pr, cols);
 }
 
 // ---- tensor maps ---------------------------------------------------------------------------------------------------------
@@ -152,8 +172,7 @@ int realign(std::initializer_list<Mat*> mats, char* to, cudaStream_t s) {
   if (n == 0) return GWS_OK;
   for (int i = n; i < 3; ++i) m.end[i] = threads;
   if (threads / kJobs >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
-  k_realign<<<blocks_for(threads, kJobs), kJobs, 0, s>>>(m);
-  return gws::finish_launch("row alignment kernel");
+  return launch(k_realign, blocks_for(threads, kJobs), kJobs, 0, 1, s, "row alignment kernel", m);
 }
 
 // ---- choice of tile --------------------------------------------------------------------------------------------------------
@@ -217,22 +236,7 @@ int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStr
   if (err != cudaSuccess) return gws::report_cuda(err, "shared memory of the block GEMM");
   const uint32_t work = args.m_tiles * args.n_tiles * args.splits;
   const uint32_t slots = CG == 2 ? static_cast<uint32_t>(sms / 2) : static_cast<uint32_t>(sms) * S::kPerSm;
-  cudaLaunchConfig_t cfg;
-  std::memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3(std::min(work, slots) * CG);
-  cfg.blockDim = dim3(S::kThreads);
-  cfg.dynamicSmemBytes = S::kSmemBytes;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CG;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  err = cudaLaunchKernelEx(&cfg, k_tc<CG, BN, MODE>, maps[0], maps[1], maps[2], maps[3], args);
-  if (err != cudaSuccess) { (void)cudaGetLastError(); return gws::report_cuda(err, "block GEMM"); }
-  return gws::finish_launch("block GEMM");
+  return launch(k_tc<CG, BN, MODE>, std::min(work, slots) * CG, S::kThreads, S::kSmemBytes, CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
 }
 
 template <int MODE>
@@ -254,6 +258,7 @@ TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t kb, int* sta
   a.kb_first = a.kb;
   a.kb_split = t.kb_split;
   a.group = 8;
+  a.last_parts = kTcStep / 16;
   a.stage_bytes = static_cast<uint32_t>(t.cg) * kTcABytes + static_cast<uint32_t>(t.bn) * kTcStep * 2u;
   a.rows = rows;
   a.cols = cols;
@@ -272,10 +277,14 @@ int join(const TcArgs& a, cudaStream_t s) {
   const int64_t items = a.ld_part / 4 * a.rows * (a.out[1] != nullptr ? 2 : 1);
   const bool wide = a.ld_out % 4 == 0 && on(a.out[0], 8) && on(a.out[1], 8);
   if ((items + kJobs - 1) / kJobs >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
-  k_join<<<blocks_for(items, kJobs), kJobs, 0, s>>>(a.part, a.ld_part, a.part_stride, a.splits, static_cast<uint16_t*>(a.out[0]),
-                                                    static_cast<uint16_t*>(a.out[1]), a.ld_out, a.rows, a.cols, wide);
-  return gws::finish_launch("join of a split contraction");
+  return launch(k_join, blocks_for(items, kJobs), kJobs, 0, 1, s, "join of a split contraction", a.part, a.ld_part, a.part_stride, a.splits,
+                static_cast<uint16_t*>(a.out[0]), static_cast<uint16_t*>(a.out[1]), a.ld_out, a.rows, a.cols, wide ? 1 : 0);
 }
+
+// Copies fill rows outside a matrix with zeros at a fraction of the speed of rows inside it (one token, 128-row boxes: 31 us
+// where 128 tokens take 14), so a matrix of few rows gets boxes of few rows.  What the rest of the shared memory holds reaches only
+// accumulator rows that are not stored.
+uint32_t a_box(int64_t rows) { return static_cast<uint32_t>(std::min<int64_t>(128, round_up(rows, 8))); }
 
 // dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
 int64_t steps_of(int64_t len) { return (len + kTcStep - 1) / kTcStep; }
@@ -289,10 +298,16 @@ int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, i
   args.part = static_cast<float*>(part);
   args.ld_part = round_up(x.cols, 32);
   args.part_stride = static_cast<int64_t>(outs) * args.rows * args.ld_part;
+  // tokens fewer than a step: boxes and products of only the 16-token parts that hold any
+  const uint32_t box = static_cast<uint32_t>(std::min<int64_t>(kTcStep, round_up(a0.rows, 16)));
+  if (a0.rows < kTcStep) {
+    args.last_parts = box / 16;
+    args.stage_bytes = args.stage_bytes / kTcStep * box;
+  }
   CUtensorMap maps[4];
-  int st = make_map(maps[0], a0.p, a0.rows, a0.cols, a0.ld, kTcStep);
-  if (st == GWS_OK) st = a1 != nullptr ? make_map(maps[1], a1->p, a1->rows, a1->cols, a1->ld, kTcStep) : (maps[1] = maps[0], GWS_OK);
-  if (st == GWS_OK) st = make_map(maps[2], x.p, x.rows, x.cols, x.ld, kTcStep);
+  int st = make_map(maps[0], a0.p, a0.rows, a0.cols, a0.ld, box);
+  if (st == GWS_OK) st = a1 != nullptr ? make_map(maps[1], a1->p, a1->rows, a1->cols, a1->ld, box) : (maps[1] = maps[0], GWS_OK);
+  if (st == GWS_OK) st = make_map(maps[2], x.p, x.rows, x.cols, x.ld, box);
   if (st != GWS_OK) return st;
   maps[3] = maps[2];
   st = launch_mode<kDw>(t, maps, args, sms, s);
@@ -343,15 +358,16 @@ int64_t forward_bytes(const gws_gated_desc* d) {
 }
 
 template <int SAVE, int ACT>
-void launch_pre(const PreArgs& p, bool fast, cudaStream_t s) {
-  if (fast) k_gated_pre<SAVE, ACT><<<blocks_for(p.groups, kJobs), kJobs, 0, s>>>(p);
-  else k_gated_pre_any<SAVE, ACT><<<blocks_for(p.rows * ((p.per_row + kRun - 1) / kRun), 8), kJobs, 0, s>>>(p);
+int launch_pre(const PreArgs& p, bool fast, cudaStream_t s) {
+  const char* what = "gated backward, element-wise part";
+  if (fast) return launch(k_gated_pre<SAVE, ACT>, blocks_for(p.groups, kJobs), kJobs, 0, 1, s, what, p);
+  return launch(k_gated_pre_any<SAVE, ACT>, blocks_for(p.rows * ((p.per_row + kRun - 1) / kRun), 8), kJobs, 0, 1, s, what, p);
 }
 template <int SAVE>
-void launch_pre_act(const PreArgs& p, int act, bool fast, cudaStream_t s) {
-  if (act == GWS_GATED_SILU) launch_pre<SAVE, GWS_GATED_SILU>(p, fast, s);
-  else if (act == GWS_GATED_GELU_TANH) launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, fast, s);
-  else launch_pre<SAVE, GWS_GATED_RELU>(p, fast, s);
+int launch_pre_act(const PreArgs& p, int act, bool fast, cudaStream_t s) {
+  if (act == GWS_GATED_SILU) return launch_pre<SAVE, GWS_GATED_SILU>(p, fast, s);
+  if (act == GWS_GATED_GELU_TANH) return launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, fast, s);
+  return launch_pre<SAVE, GWS_GATED_RELU>(p, fast, s);
 }
 
 bool workspace_ok(const void* p, size_t have, int64_t need) { return need == 0 || (p != nullptr && on(p, 256) && have >= static_cast<size_t>(need)); }
@@ -469,6 +485,7 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   const Tile t = choose(kGated, d.m, d.n, 1, steps_of(d.k), sms);
   TcArgs args = base_args(t, d.m, d.n, steps_of(d.k), status);
   set_out(args, h, nullptr, d.ld_h);
+  args.stage_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcStep * 2u;
   args.activation = d.activation;
   args.save = d.save_format;
   if (bytes8) {
@@ -480,7 +497,7 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
     args.save_direct = d.n % 16 == 0 && on(save_gate, 32) && on(save_up, 32);
   }
   CUtensorMap maps[4];
-  if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, 128)) != GWS_OK) return st;
+  if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, a_box(d.m))) != GWS_OK) return st;
   maps[1] = maps[0];
   if ((st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, static_cast<uint32_t>(t.bn / 2))) != GWS_OK) return st;
   if ((st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, static_cast<uint32_t>(t.bn / 2))) != GWS_OK) return st;
@@ -543,10 +560,10 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   p.groups = d.m * p.per_row;
   if (p.groups / 8 >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
   const bool fast = whole_groups(grad_h, d.n, p.ld_grad_h) && on(h_out, 32) && (saved8 || (on(save_gate, 32) && on(save_up, 32)));
-  if (d.save_format == GWS_ACT8_INT8) launch_pre_act<GWS_ACT8_INT8>(p, d.activation, fast, s);
-  else if (d.save_format == GWS_ACT8_E4M3) launch_pre_act<GWS_ACT8_E4M3>(p, d.activation, fast, s);
-  else launch_pre_act<GWS_SAVE_BF16>(p, d.activation, fast, s);
-  if ((st = gws::finish_launch("gated backward, element-wise part")) != GWS_OK) return st;
+  st = d.save_format == GWS_ACT8_INT8   ? launch_pre_act<GWS_ACT8_INT8>(p, d.activation, fast, s)
+       : d.save_format == GWS_ACT8_E4M3 ? launch_pre_act<GWS_ACT8_E4M3>(p, d.activation, fast, s)
+                                        : launch_pre_act<GWS_SAVE_BF16>(p, d.activation, fast, s);
+  if (st != GWS_OK) return st;
   const Mat dg{p.grad_gate, d.m, d.n, p.ld}, du{p.grad_up, d.m, d.n, p.ld};
 
   if (wants_dx) {
@@ -556,12 +573,13 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
     const Tile t = choose(kDx, d.m, d.k, 1, 2 * kb, sms);
     TcArgs args = base_args(t, d.m, d.k, 2 * kb, status);
     args.kb_first = static_cast<uint32_t>(kb);
+    args.stage_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcStep * 2u;
     set_out(args, grad_x, nullptr, d.k);
     args.part = reinterpret_cast<float*>(ws + l.part);
     args.ld_part = round_up(d.k, 32);
     args.part_stride = d.m * args.ld_part;
     CUtensorMap maps[4];
-    if ((st = make_map(maps[0], dg.p, d.m, d.n, dg.ld, 128)) != GWS_OK || (st = make_map(maps[1], du.p, d.m, d.n, du.ld, 128)) != GWS_OK ||
+    if ((st = make_map(maps[0], dg.p, d.m, d.n, dg.ld, a_box(d.m))) != GWS_OK || (st = make_map(maps[1], du.p, d.m, d.n, du.ld, a_box(d.m))) != GWS_OK ||
         (st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, kTcStep)) != GWS_OK || (st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, kTcStep)) != GWS_OK)
       return st;
     if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;

@@ -39,6 +39,7 @@ struct TcArgs {
   uint32_t tiles_per_out;                 // kDw: row tiles of the first output
   uint32_t kb, kb_first, kb_split;        // steps of the contraction: all, of the first segment (kDx), of one part
   uint32_t group;                         // row tiles per group of the tile order
+  uint32_t last_parts;                    // kDw: 16-step parts of the last step that hold tokens
   uint32_t stage_bytes;                   // bytes the copies of one stage bring, over the CG blocks
   int64_t rows, cols;                     // of one output
   void* out[2];                           // BF16
@@ -82,6 +83,15 @@ __device__ __forceinline__ void bar_arrive(uint32_t cluster_addr) {
 __device__ __forceinline__ bool bar_try(uint32_t addr, uint32_t parity) {
   uint32_t done;
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done)
+               : "r"(addr), "r"(parity)
+               : "memory");
+  return done != 0;
+}
+// The same without waiting at all.
+__device__ __forceinline__ bool bar_peek(uint32_t addr, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                : "=r"(done)
                : "r"(addr), "r"(parity)
                : "memory");
@@ -281,6 +291,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
   if (CG == 2) pair_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
+  after_previous();
 
   const uint32_t tiles = p.m_tiles * p.n_tiles, work = tiles * p.splits;
   const uint32_t first = blockIdx.x / CG, stride = gridDim.x / CG;
@@ -354,18 +365,23 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
         const uint32_t buf = n & 1u, d = tmem + buf * BN;
         if (!bar_wait(acc_empty0 + 8u * buf, ((n >> 1) & 1u) ^ 1u)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        bool ready = bar_try(full0 + 8u * s, parity);
         for (uint32_t kb = k0; kb < k1; ++kb) {
-          if (!bar_wait(full0 + 8u * s, parity)) { ok = false; break; }
+          if (!__all_sync(0xFFFFFFFFu, ready) && !bar_wait(full0 + 8u * s, parity)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t now = s;
+          if (++s == kStages) { s = 0; parity ^= 1u; }
+          if (kb + 1 < k1) ready = bar_peek(full0 + 8u * s, parity);      // answered while the products below are issued
           if (elected()) {
-            const uint64_t sa = da + s * (S::kStage >> 4), sb = db + s * (S::kStage >> 4);
+            const uint64_t sa = da + now * (S::kStage >> 4), sb = db + now * (S::kStage >> 4);
+            const uint32_t parts = MODE == kDw && kb + 1 == p.kb ? p.last_parts : kTcStep / 16u;
             mma<CG>(d, sa, sb, kIdesc, kb > k0 ? 1u : 0u);
 #pragma unroll
-            for (uint32_t j = 1; j < kTcStep / 16u; ++j) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
-            commit<CG>(&empty[s]);
+            for (uint32_t j = 1; j < kTcStep / 16u; ++j)
+              if (MODE != kDw || j < parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
+            commit<CG>(&empty[now]);
           }
           __syncwarp();
-          if (++s == kStages) { s = 0; parity ^= 1u; }
         }
         if (ok && elected()) commit<CG>(&acc_full[buf]);
         __syncwarp();
@@ -472,6 +488,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
 // Adds the parts of a split contraction in order and rounds once.  A thread takes four columns of a row.
 __global__ void __launch_bounds__(256) k_join(const float* part, int64_t ld_part, int64_t part_stride, uint32_t splits, uint16_t* out0, uint16_t* out1,
                                               int64_t ld_out, int64_t rows, int64_t cols, int32_t wide) {
+  after_previous();
   const int64_t quads = ld_part >> 2, t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (t >= quads * rows * (out1 != nullptr ? 2 : 1)) return;
   const int64_t row = t / quads, col = (t - row * quads) * 4;
@@ -512,6 +529,7 @@ struct PreArgs {
 // Memory-bound, one pass: 2 + 2 (1 + 1/32) bytes in, 4 or 6 bytes out per element.  A thread takes a group of 32 columns.
 template <int SAVE, int ACT>
 __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreArgs p) {
+  after_previous();
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (t >= p.groups) return;
   int64_t at_dh = t * kGroup;
@@ -573,6 +591,7 @@ __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreAr
 // element of each.  (One thread with a group of its own would read and write 64 bytes at 2-byte alignment, 32 separate accesses.)
 template <int SAVE, int ACT>
 __global__ void __launch_bounds__(256) k_gated_pre_any(const __grid_constant__ PreArgs p) {
+  after_previous();
   const uint32_t lane = threadIdx.x & 31u, runs_per_row = (p.per_row + kRun - 1) / kRun;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
   const int64_t row = quotient(t, runs_per_row);
