@@ -185,6 +185,9 @@ int sm_count() {
   return n;
 }
 
+// Stages along a contraction (TcShape::kHalves copies of 64 elements each).
+int64_t stages_of(int64_t len, int bn) { const int64_t per = kTcHalf * (bn == 256 ? 1 : 2); return (len + per - 1) / per; }
+
 struct Tile {
   int cg, bn;                              // blocks per tile, columns of accumulator
   uint32_t m_tiles, n_tiles, splits, kb_split;
@@ -193,7 +196,7 @@ struct Tile {
 // The tile and the split of the contraction with the least estimated time.  A step (64 along the contraction) takes a block
 // max(products, operand bytes over what an SM draws from L2); a wave takes a block's steps, and splitting adds the pass that
 // joins the parts.
-Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t kb, int sms) {
+Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int segments, int sms) {
   static const struct { int cg, bn; } kinds[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
   Tile best{};
   double least = 0.0;
@@ -201,8 +204,9 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t kb, int sms)
     const int64_t width = mode == kGated ? kind.bn / 2 : kind.bn;
     const int64_t mt = outs * ((rows + 128 * kind.cg - 1) / (128 * kind.cg)), nt = (cols + width - 1) / width;
     const double slots = kind.cg == 2 ? sms / 2 : sms * (kind.bn <= 64 ? 2 : 1);
-    const double step = std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 56.0) * (kind.bn <= 64 ? 2 : 1);
-    const int64_t most = mode == kGated ? 1 : std::min<int64_t>(16, kb / 4);
+    const int64_t kb = segments * stages_of(len, kind.bn);
+    const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 56.0)) * (kind.bn <= 64 ? 2 : 1);
+    const int64_t most = mode == kGated ? 1 : std::min<int64_t>(16, kb / 2);
     for (int64_t splits = 1; splits <= std::max<int64_t>(1, most); ++splits) {
       const int64_t per = (kb + splits - 1) / splits;
       if ((kb + per - 1) / per != splits) continue;
@@ -247,19 +251,20 @@ int launch_mode(const Tile& t, const CUtensorMap (&maps)[4], const TcArgs& args,
   return launch_tc<1, 64, MODE>(maps, args, sms, s);
 }
 
-TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t kb, int* status) {
+TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t len, int segments, int* status) {
   TcArgs a;
   std::memset(&a, 0, sizeof a);
   a.m_tiles = t.m_tiles;
   a.n_tiles = t.n_tiles;
   a.splits = t.splits;
   a.tiles_per_out = t.m_tiles;
-  a.kb = static_cast<uint32_t>(kb);
-  a.kb_first = a.kb;
+  a.len = static_cast<uint32_t>(len);
+  a.kb_first = static_cast<uint32_t>(stages_of(len, t.bn));
+  a.kb = a.kb_first * segments;
   a.kb_split = t.kb_split;
   a.group = 8;
-  a.last_parts = kTcStep / 16;
-  a.stage_bytes = static_cast<uint32_t>(t.cg) * kTcABytes + static_cast<uint32_t>(t.bn) * kTcStep * 2u;
+  a.parts = kTcHalf / 16;
+  a.half_bytes = static_cast<uint32_t>(t.cg) * kTcABytes + static_cast<uint32_t>(t.bn) * kTcHalf * 2u;
   a.rows = rows;
   a.cols = cols;
   a.status = status;
@@ -287,23 +292,19 @@ int join(const TcArgs& a, cudaStream_t s) {
 uint32_t a_box(int64_t rows) { return static_cast<uint32_t>(std::min<int64_t>(128, round_up(rows, 8))); }
 
 // dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
-int64_t steps_of(int64_t len) { return (len + kTcStep - 1) / kTcStep; }
-
 int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, int64_t ld_out, void* part, int* status, int sms, cudaStream_t s) {
   const int outs = a1 != nullptr ? 2 : 1;
-  const Tile t = choose(kDw, a0.cols, x.cols, outs, steps_of(a0.rows), sms);
-  TcArgs args = base_args(t, a0.cols, x.cols, steps_of(a0.rows), status);
+  const Tile t = choose(kDw, a0.cols, x.cols, outs, a0.rows, 1, sms);
+  TcArgs args = base_args(t, a0.cols, x.cols, a0.rows, 1, status);
   args.tiles_per_out = t.m_tiles / outs;
   set_out(args, out0, out1, ld_out);
   args.part = static_cast<float*>(part);
   args.ld_part = round_up(x.cols, 32);
   args.part_stride = static_cast<int64_t>(outs) * args.rows * args.ld_part;
   // tokens fewer than a step: boxes and products of only the 16-token parts that hold any
-  const uint32_t box = static_cast<uint32_t>(std::min<int64_t>(kTcStep, round_up(a0.rows, 16)));
-  if (a0.rows < kTcStep) {
-    args.last_parts = box / 16;
-    args.stage_bytes = args.stage_bytes / kTcStep * box;
-  }
+  const uint32_t box = static_cast<uint32_t>(std::min<int64_t>(kTcHalf, round_up(a0.rows, 16)));
+  args.parts = box / 16;
+  args.half_bytes = args.half_bytes / kTcHalf * box;
   CUtensorMap maps[4];
   int st = make_map(maps[0], a0.p, a0.rows, a0.cols, a0.ld, box);
   if (st == GWS_OK) st = a1 != nullptr ? make_map(maps[1], a1->p, a1->rows, a1->cols, a1->ld, box) : (maps[1] = maps[0], GWS_OK);
@@ -315,7 +316,7 @@ int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, i
 }
 
 int64_t dw_part_bytes(int64_t m, int64_t rows, int64_t cols, int outs, int sms) {
-  return part_bytes(choose(kDw, rows, cols, outs, steps_of(m), sms), rows, cols, outs);
+  return part_bytes(choose(kDw, rows, cols, outs, m, 1, sms), rows, cols, outs);
 }
 
 // ---- the gated block ---------------------------------------------------------------------------------------------------------
@@ -346,7 +347,7 @@ BackLayout back_layout(const gws_gated_desc* d, int sms) {
   l.w_up = take(w);
   l.grad_gate = take(packed_bytes(d->m, d->n));
   l.grad_up = take(packed_bytes(d->m, d->n));
-  const int64_t dx = d->m > 0 && d->k > 0 && d->n > 0 ? part_bytes(choose(kDx, d->m, d->k, 1, 2 * steps_of(d->n), sms), d->m, d->k, 1) : 0;
+  const int64_t dx = d->m > 0 && d->k > 0 && d->n > 0 ? part_bytes(choose(kDx, d->m, d->k, 1, d->n, 2, sms), d->m, d->k, 1) : 0;
   const int64_t dw = d->m > 0 && d->k > 0 && d->n > 0 ? dw_part_bytes(d->m, d->n, d->k, 2, sms) : 0;
   l.part = take(std::max(dx, dw));
   l.total = at;
@@ -482,10 +483,10 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   if ((st = realign({&mx, &mg, &mu}, static_cast<char*>(workspace), s)) != GWS_OK) return st;
 
   const int sms = sm_count();
-  const Tile t = choose(kGated, d.m, d.n, 1, steps_of(d.k), sms);
-  TcArgs args = base_args(t, d.m, d.n, steps_of(d.k), status);
+  const Tile t = choose(kGated, d.m, d.n, 1, d.k, 1, sms);
+  TcArgs args = base_args(t, d.m, d.n, d.k, 1, status);
   set_out(args, h, nullptr, d.ld_h);
-  args.stage_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcStep * 2u;
+  args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
   args.activation = d.activation;
   args.save = d.save_format;
   if (bytes8) {
@@ -569,18 +570,16 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   if (wants_dx) {
     Mat mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
     if ((st = realign({&mg, &mu}, ws + l.w_gate, s)) != GWS_OK) return st;
-    const int64_t kb = steps_of(d.n);
-    const Tile t = choose(kDx, d.m, d.k, 1, 2 * kb, sms);
-    TcArgs args = base_args(t, d.m, d.k, 2 * kb, status);
-    args.kb_first = static_cast<uint32_t>(kb);
-    args.stage_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcStep * 2u;
+    const Tile t = choose(kDx, d.m, d.k, 1, d.n, 2, sms);
+    TcArgs args = base_args(t, d.m, d.k, d.n, 2, status);
+    args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
     set_out(args, grad_x, nullptr, d.k);
     args.part = reinterpret_cast<float*>(ws + l.part);
     args.ld_part = round_up(d.k, 32);
     args.part_stride = d.m * args.ld_part;
     CUtensorMap maps[4];
     if ((st = make_map(maps[0], dg.p, d.m, d.n, dg.ld, a_box(d.m))) != GWS_OK || (st = make_map(maps[1], du.p, d.m, d.n, du.ld, a_box(d.m))) != GWS_OK ||
-        (st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, kTcStep)) != GWS_OK || (st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, kTcStep)) != GWS_OK)
+        (st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, kTcHalf)) != GWS_OK || (st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, kTcHalf)) != GWS_OK)
       return st;
     if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
     if (t.splits > 1 && (st = join(args, s)) != GWS_OK) return st;

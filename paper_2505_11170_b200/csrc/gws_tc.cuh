@@ -8,7 +8,7 @@
 //
 // A tile is 128 * CG rows by BN columns of accumulator; CG = 2 is a pair of SMs working on one tile (cta_group::2: each SM
 // holds its 128 rows of A and half of the columns of B, so an operand byte fetched from L2 feeds twice the products).
-// Warp roles: warp 0 starts the TMA copies (64 elements along the contraction per stage, 128-byte swizzle), warp 1 issues the
+// Warp roles: warp 0 starts the TMA copies (64 or 128 elements along the contraction per stage, 128-byte swizzle), warp 1 issues the
 // tcgen05.mma of the pair, warps 4 and up are the epilogue.  The accumulator is double-buffered in tensor memory, so the
 // epilogue of a tile runs under the products of the next one.  Blocks are persistent and take tiles round robin, in groups
 // of rows so that the tiles in flight share operands in L2.
@@ -28,8 +28,8 @@ namespace {
 
 enum { kGated = 0, kDx = 1, kDw = 2 };
 
-constexpr uint32_t kTcStep = 64;                           // elements along the contraction per stage
-constexpr uint32_t kTcABytes = 128u * kTcStep * 2u;
+constexpr uint32_t kTcHalf = 64;                           // elements along the contraction per copy: 128 bytes, one swizzle atom
+constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
 constexpr uint32_t kTcSmem = 227u * 1024u;
 constexpr uint32_t kTcStagingWarp = 32u * 17u * 4u;        // a 32 x 32 BF16 block per epilogue warp, rows 17 words apart
 constexpr long long kTcWaitCycles = 2000000000LL;
@@ -37,10 +37,11 @@ constexpr long long kTcWaitCycles = 2000000000LL;
 struct TcArgs {
   uint32_t m_tiles, n_tiles, splits;      // tiles along rows (all outputs), along columns, parts of the contraction
   uint32_t tiles_per_out;                 // kDw: row tiles of the first output
-  uint32_t kb, kb_first, kb_split;        // steps of the contraction: all, of the first segment (kDx), of one part
+  uint32_t kb, kb_first, kb_split;        // stages of the contraction: all, of the first segment (kDx), of one part
+  uint32_t len;                           // elements of the contraction (kDx: of each segment)
   uint32_t group;                         // row tiles per group of the tile order
-  uint32_t last_parts;                    // kDw: 16-step parts of the last step that hold tokens
-  uint32_t stage_bytes;                   // bytes the copies of one stage bring, over the CG blocks
+  uint32_t parts;                         // kDw: 16-step parts of a copy that hold tokens (4 unless there are fewer than 64 tokens)
+  uint32_t half_bytes;                    // bytes the copies of 64 elements along the contraction bring, over the CG blocks
   int64_t rows, cols;                     // of one output
   void* out[2];                           // BF16
   int64_t ld_out;
@@ -234,7 +235,12 @@ __device__ __forceinline__ void gate_block(const uint32_t (&g)[32], const uint32
 template <int CG, int BN, int MODE>
 struct TcShape {
   static constexpr uint32_t kBRows = BN / CG;                              // columns of B each block holds
-  static constexpr uint32_t kStage = kTcABytes + kBRows * kTcStep * 2u;
+  // Copies of 64 elements per stage.  A stage costs the warp that issues the products some 250 cycles whatever it holds; the
+  // products of 64 elements take 512 cycles with 256 columns on a pair of SMs, 128 to 256 with the smaller tiles, which therefore
+  // take two copies per stage (2048 x 5632 into 128 rows, 128 columns: 396 -> 250 cycles per 64 elements).
+  static constexpr uint32_t kHalves = BN == 256 ? 1u : 2u;
+  static constexpr uint32_t kHalf = kTcABytes + kBRows * kTcHalf * 2u;     // A, then B
+  static constexpr uint32_t kStage = kHalves * kHalf;
   static constexpr uint32_t kPerSm = BN <= 64 ? 2u : 1u;                   // resident blocks
   static constexpr uint32_t kEpilogueWarps = BN <= 64 ? 4u : 8u;           // one or two per quadrant of the accumulator's rows
   static constexpr uint32_t kThreads = 128u + 32u * kEpilogueWarps;
@@ -291,6 +297,9 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
   if (CG == 2) pair_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
+  if (warp == 0 && elected()) {          // the descriptions of the operands are on their way before the first copy asks for them
+    for (const CUtensorMap* map : {&a0, &b0, &a1, &b1}) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+  }
   after_previous();
 
   const uint32_t tiles = p.m_tiles * p.n_tiles, work = tiles * p.splits;
@@ -319,30 +328,35 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
       const int32_t n0 = static_cast<int32_t>(nt * (MODE == kGated ? BN / 2 : BN) + (MODE == kGated ? 0u : rank * S::kBRows));
       for (uint32_t kb = k0; kb < k1; ++kb) {
         if (!bar_wait(empty0 + 8u * s, parity)) { ok = false; break; }
+        const bool seg = MODE == kDx && kb >= p.kb_first;
+        const uint32_t k = (seg ? kb - p.kb_first : kb) * (S::kHalves * kTcHalf);
+        const uint32_t halves = S::kHalves == 1u || k + kTcHalf >= p.len ? 1u : 2u;     // a second copy past the end is left out
         if (elected()) {
-          if (rank == 0) bar_expect(&full[s], p.stage_bytes);
-          const uint32_t bar = full0 + 8u * s, sa = smem_addr(smem) + s * S::kStage, sb = sa + kTcABytes;
-          if (MODE == kGated) {
-            const int32_t k = static_cast<int32_t>(kb * kTcStep);
-            copy_in<CG>(sa, &a0, bar, k, m0);
-            if (CG == 2) {                             // block 0 holds the gate's rows, block 1 the up projection's
-              copy_in<CG>(sb, rank == 0 ? &b0 : &b1, bar, k, n0);
+          if (rank == 0) bar_expect(&full[s], halves * p.half_bytes);
+          const uint32_t bar = full0 + 8u * s;
+#pragma unroll
+          for (uint32_t i = 0; i < S::kHalves; ++i) {
+            if (i >= halves) break;
+            const uint32_t sa = smem_addr(smem) + s * S::kStage + i * S::kHalf, sb = sa + kTcABytes;
+            const int32_t ki = static_cast<int32_t>(k + i * kTcHalf);
+            if (MODE == kGated) {
+              copy_in<CG>(sa, &a0, bar, ki, m0);
+              if (CG == 2) {                             // block 0 holds the gate's rows, block 1 the up projection's
+                copy_in<CG>(sb, rank == 0 ? &b0 : &b1, bar, ki, n0);
+              } else {
+                copy_in<CG>(sb, &b0, bar, ki, n0);
+                copy_in<CG>(sb + (BN / 2) * kTcHalf * 2u, &b1, bar, ki, n0);
+              }
+            } else if (MODE == kDx) {
+              copy_in<CG>(sa, seg ? &a1 : &a0, bar, ki, m0);
+#pragma unroll
+              for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, seg ? &b1 : &b0, bar, n0 + static_cast<int32_t>(j * 64u), ki);
             } else {
-              copy_in<CG>(sb, &b0, bar, k, n0);
-              copy_in<CG>(sb + (BN / 2) * kTcStep * 2u, &b1, bar, k, n0);
+#pragma unroll
+              for (uint32_t j = 0; j < 2u; ++j) copy_in<CG>(sa + j * 8192u, second ? &a1 : &a0, bar, m0 + static_cast<int32_t>(j * 64u), ki);
+#pragma unroll
+              for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(j * 64u), ki);
             }
-          } else if (MODE == kDx) {
-            const bool seg = kb >= p.kb_first;
-            const int32_t k = static_cast<int32_t>((seg ? kb - p.kb_first : kb) * kTcStep);
-            copy_in<CG>(sa, seg ? &a1 : &a0, bar, k, m0);
-#pragma unroll
-            for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, seg ? &b1 : &b0, bar, n0 + static_cast<int32_t>(j * 64u), k);
-          } else {
-            const int32_t k = static_cast<int32_t>(kb * kTcStep);
-#pragma unroll
-            for (uint32_t j = 0; j < 2u; ++j) copy_in<CG>(sa + j * 8192u, second ? &a1 : &a0, bar, m0 + static_cast<int32_t>(j * 64u), k);
-#pragma unroll
-            for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(j * 64u), k);
           }
         }
         __syncwarp();
@@ -372,13 +386,19 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
           const uint32_t now = s;
           if (++s == kStages) { s = 0; parity ^= 1u; }
           if (kb + 1 < k1) ready = bar_peek(full0 + 8u * s, parity);      // answered while the products below are issued
+          const bool seg = MODE == kDx && kb >= p.kb_first;
+          const uint32_t k = (seg ? kb - p.kb_first : kb) * (S::kHalves * kTcHalf);
+          const uint32_t halves = S::kHalves == 1u || k + kTcHalf >= p.len ? 1u : 2u;
           if (elected()) {
-            const uint64_t sa = da + now * (S::kStage >> 4), sb = db + now * (S::kStage >> 4);
-            const uint32_t parts = MODE == kDw && kb + 1 == p.kb ? p.last_parts : kTcStep / 16u;
-            mma<CG>(d, sa, sb, kIdesc, kb > k0 ? 1u : 0u);
 #pragma unroll
-            for (uint32_t j = 1; j < kTcStep / 16u; ++j)
-              if (MODE != kDw || j < parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
+            for (uint32_t i = 0; i < S::kHalves; ++i) {
+              if (i >= halves) break;
+              const uint64_t sa = da + ((now * S::kStage + i * S::kHalf) >> 4), sb = db + ((now * S::kStage + i * S::kHalf) >> 4);
+              mma<CG>(d, sa, sb, kIdesc, kb > k0 || i > 0 ? 1u : 0u);
+#pragma unroll
+              for (uint32_t j = 1; j < kTcHalf / 16u; ++j)
+                if (MODE != kDw || j < p.parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
+            }
             commit<CG>(&empty[now]);
           }
           __syncwarp();
