@@ -527,6 +527,12 @@ class Act8:
             raise ValueError("gws: a checkpoint is a contiguous uint8 tensor of at least %d bytes" % _act8_bytes(rows, cols))
         self.buffer, self.rows, self.cols, self.fmt = buffer, rows, cols, fmt
 
+    @classmethod
+    def _new(cls, like: torch.Tensor, rows: int, cols: int, fmt: int) -> "Act8":
+        a = cls.__new__(cls)
+        a.buffer, a.rows, a.cols, a.fmt = like.new_empty(_act8_bytes(rows, cols), dtype=torch.uint8), rows, cols, fmt
+        return a
+
     @property
     def shape(self):
         return (self.rows, self.cols)
@@ -604,6 +610,10 @@ def _bf16_out(t: Optional[torch.Tensor], name: str, rows: int, cols: int, like: 
     return t
 
 
+def _dense_like(t: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty((rows, cols))
+
+
 def _workspace(nbytes: int, like: torch.Tensor):
     """(tensor to keep until the launch, its address)."""
     if nbytes < 0:
@@ -626,7 +636,7 @@ def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None,
     x, p, ld = _bf16_rows(x, "x", read_by_map=False)
     rows, cols = x.shape
     if out is None:
-        out = Act8(x.new_empty(_act8_bytes(rows, cols), dtype=torch.uint8), rows, cols, fmt)
+        out = Act8._new(x, rows, cols, fmt)
     elif out.shape != (rows, cols) or out.fmt != fmt:
         raise ValueError("gws: out is a checkpoint of another shape or format")
     _check(load_library().gws_act8_save(rows, cols, ld, fmt, p, out.buffer.data_ptr(), _raw_stream(device)))
@@ -673,14 +683,36 @@ def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = 
 
 
 class GatedSaved:
-    """What the gated block keeps for its backward pass: the gate and the up projection, as checkpoints or BF16 tensors."""
-    __slots__ = ("gate", "up", "fmt")
+    """What the gated block keeps for its backward pass: the gate and the up projection [m, n], as checkpoints or BF16 tensors, in
+    one ``buffer`` (the up projection's part starts at the next multiple of 256 bytes)."""
+    __slots__ = ("buffer", "m", "n", "fmt")
 
-    def __init__(self, gate, up, fmt: int):
-        self.gate, self.up, self.fmt = gate, up, fmt
+    def __init__(self, buffer: torch.Tensor, m: int, n: int, fmt: int):
+        self.buffer, self.m, self.n, self.fmt = buffer, m, n, fmt
 
-    def tensors(self):
-        return (self.gate, self.up) if self.fmt == SAVE_BF16 else (self.gate.buffer, self.up.buffer)
+    @staticmethod
+    def _part(m: int, n: int, fmt: int) -> int:
+        """Bytes from the gate's part to the up projection's."""
+        return -(-(2 * m * n if fmt == SAVE_BF16 else _act8_bytes(m, n)) // 256) * 256
+
+    def _at(self, which: int):
+        part = self._part(self.m, self.n, self.fmt)
+        piece = self.buffer[which * part:(which + 1) * part]
+        if self.fmt == SAVE_BF16:
+            return piece[:2 * self.m * self.n].view(_BF16).view(self.m, self.n)
+        return Act8(piece, self.m, self.n, self.fmt)
+
+    @property
+    def gate(self):
+        return self._at(0)
+
+    @property
+    def up(self):
+        return self._at(1)
+
+    def _addresses(self):
+        p = self.buffer.data_ptr()
+        return p, p + self._part(self.m, self.n, self.fmt)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -714,17 +746,14 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
     m, k = x.shape
     n = w_gate.shape[0]
     w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
+    if save not in (ACT8_INT8, ACT8_E4M3, SAVE_BF16, SAVE_NONE):
+        raise GwsError(ERR_UNSUPPORTED)
     _, at, nbytes = _gated_plan(m, n, k, ld_x, ld_w, n or 1, activation, save, SAVE_BF16, 0, device)
     h = _bf16_out(h, "h", m, n, x)
     saved = p_sg = p_su = None
-    if save == SAVE_BF16:
-        saved = GatedSaved(x.new_empty((m, n)), x.new_empty((m, n)), save)
-    elif save == ACT8_INT8 or save == ACT8_E4M3:
-        size = _act8_bytes(m, n)
-        saved = GatedSaved(Act8(x.new_empty(size, dtype=torch.uint8), m, n, save), Act8(x.new_empty(size, dtype=torch.uint8), m, n, save), save)
-    if saved is not None:
-        gate, up = saved.tensors()
-        p_sg, p_su = gate.data_ptr(), up.data_ptr()
+    if save != SAVE_NONE:
+        saved = GatedSaved(x.new_empty(2 * GatedSaved._part(m, n, save), dtype=torch.uint8), m, n, save)
+        p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, x)
     _check(load_library().gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, _addr(status), _raw_stream(device)))
     return h, saved
@@ -735,8 +764,7 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     """Backward pass of :func:`gated_fwd`.  ``x`` is the BF16 input or its checkpoint.  Returns (grad_x, grad_w_gate, grad_w_up, h);
     what was not asked for is None.  ``h`` is act(gate) * up again, which the weight gradient of the layer after the block needs."""
     kept_x = isinstance(x, Act8)
-    gate, up = saved.tensors()
-    device = _device_of(grad_h, x.buffer if kept_x else x, w_gate, w_up, gate, up, status)
+    device = _device_of(grad_h, x.buffer if kept_x else x, w_gate, w_up, saved.buffer, status)
     if stream is not None:
         return _on_stream(stream, device, gated_bwd, grad_h, x, w_gate, w_up, saved, activation, want_h, want_grad_x, want_grad_w, status)
     m, k = x.shape
@@ -748,14 +776,15 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
         x_t, p_x, ld_x = _bf16_rows(x, "x")
         x_format = SAVE_BF16
     w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
-    if tuple(saved.gate.shape) != (m, n) or tuple(saved.up.shape) != (m, n):
-        raise ValueError("gws: the kept projections are %s, not (%d, %d)" % (tuple(saved.gate.shape), m, n))
+    if saved.m != m or saved.n != n:
+        raise ValueError("gws: the kept projections are (%d, %d), not (%d, %d)" % (saved.m, saved.n, m, n))
     _, at, nbytes = _gated_plan(m, n, k, ld_x, ld_w, ld_h, activation, saved.fmt, x_format, 1, device)
-    grad_x = grad_h.new_empty((m, k)) if want_grad_x else None
-    grad_wg, grad_wu = (grad_h.new_empty((n, k)), grad_h.new_empty((n, k))) if want_grad_w else (None, None)
-    h = grad_h.new_empty((m, n)) if want_h else None
+    grad_x = (grad_h.new_empty((m, k)) if kept_x else _dense_like(x_t, m, k)) if want_grad_x else None
+    grad_wg, grad_wu = (_dense_like(w_gate, n, k), _dense_like(w_gate, n, k)) if want_grad_w else (None, None)
+    h = _dense_like(grad_h, m, n) if want_h else None
+    p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, grad_h)
-    _check(load_library().gws_gated_bwd(at, p_dh, p_x, p_gate, p_up, gate.data_ptr(), up.data_ptr(), _addr(grad_x), _addr(grad_wg), _addr(grad_wu),
+    _check(load_library().gws_gated_bwd(at, p_dh, p_x, p_gate, p_up, p_sg, p_su, _addr(grad_x), _addr(grad_wg), _addr(grad_wu),
                                         _addr(h), ws_p, nbytes, _addr(status), _raw_stream(device)))
     return grad_x, grad_wg, grad_wu, h
 

@@ -64,24 +64,33 @@ int zero(void* p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t s) {
 // Whether every group of a [rows, cols] BF16 tensor is 64 whole bytes on a 32-byte boundary: a thread then takes a group.
 bool whole_groups(const void* p, int64_t cols, int64_t ld) { return cols % kGroup == 0 && ld % 16 == 0 && on(p, 32); }
 
-// Launches a kernel that may overlap the end of the one before it on the stream (after_previous in the kernels).
+// The launches of one call.  The first is an ordinary one; each later one may become resident while the one before it drains
+// (after_previous in the kernels).
+struct Queue {
+  cudaStream_t s;
+  bool follows = false;
+};
 template <class... P, class... A>
-int launch(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t s, const char* what, const A&... args) {
+int launch(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, unsigned cluster, Queue& q, const char* what, const A&... args) {
   cudaLaunchConfig_t cfg;
   std::memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
+  cfg.stream = q.s;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (q.follows) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 1) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    attr[cfg.numAttrs].val.clusterDim.x = cluster;
+    attr[cfg.numAttrs].val.clusterDim.y = 1;
+    attr[cfg.numAttrs++].val.clusterDim.z = 1;
+  }
+  q.follows = true;
   const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
   if (err != cudaSuccess) { (void)cudaGetLastError(); return gws::report_cuda(err, what); }
   return gws::finish_launch(what);
@@ -89,7 +98,7 @@ int launch(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, uns
 
 unsigned blocks_for(int64_t items, int64_t per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
 
-int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8View& c, int64_t rows, int64_t cols, cudaStream_t s) {
+int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8View& c, int64_t rows, int64_t cols, Queue& s) {
   const int64_t per_row = c.ld / kGroup, groups = rows * per_row;
   const bool fast = whole_groups(x, cols, ldx), i8 = format == GWS_ACT8_INT8;
   if (groups / 8 >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
@@ -147,7 +156,7 @@ int64_t packed_ld(int64_t cols) { return round_up(cols, kGroup); }
 int64_t packed_bytes(int64_t rows, int64_t cols) { return round_up(rows * packed_ld(cols) * 2, 256); }
 
 // Brings those of up to three matrices that need it into the workspace, one after the other from `to`, in one launch.
-int realign(std::initializer_list<Mat*> mats, char* to, cudaStream_t s) {
+int realign(std::initializer_list<Mat*> mats, char* to, Queue& s) {
   Moves m;
   std::memset(&m, 0, sizeof m);
   int n = 0;
@@ -190,44 +199,49 @@ int64_t stages_of(int64_t len, int bn) { const int64_t per = kTcHalf * (bn == 25
 
 struct Tile {
   int cg, bn;                              // blocks per tile, columns of accumulator
-  uint32_t m_tiles, n_tiles, splits, kb_split;
+  uint32_t m_tiles, n_tiles, whole, cut, splits, kb_split;
 };
 
-// The tile and the split of the contraction with the least estimated time.  A step (64 along the contraction) takes a block
-// max(products, operand bytes over what an SM draws from L2); a wave takes a block's steps, and splitting adds the pass that
-// joins the parts.
+// The tile, and the cut of the tiles that do not fill a wave, with the least estimated time, in SM cycles.  A tile takes a block its
+// steps of 64 along the contraction, each the longest of the products (2 cycles a column), the operand bytes over the 67 a cycle that
+// an SM drew from L2 with all SMs busy, and the issue of a stage, but no less than its epilogue (two chunks of 32 columns at a time).
+// Joining costs a launch and the parts' way through memory (3400 bytes a cycle).  Measured on 2048 x 5632 (forward, us): 128 rows
+// {2, 128} 14.7, {1, 128} 11.3, {2, 256} 16.0; 512 rows 21.0, 26.6, 25.1; 1024 rows 35.2, 43.4, 35.8.
 Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int segments, int sms) {
-  static const struct { int cg, bn; } kinds[] = {{2, 256}, {2, 128}, {1, 128}, {1, 64}};
+  static const struct { int cg, bn; } kinds[] = {{2, 256}, {2, 128}, {1, 128}};
   Tile best{};
   double least = 0.0;
   for (const auto& kind : kinds) {
     const int64_t width = mode == kGated ? kind.bn / 2 : kind.bn;
-    const int64_t mt = outs * ((rows + 128 * kind.cg - 1) / (128 * kind.cg)), nt = (cols + width - 1) / width;
-    const double slots = kind.cg == 2 ? sms / 2 : sms * (kind.bn <= 64 ? 2 : 1);
-    const int64_t kb = segments * stages_of(len, kind.bn);
-    const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 56.0)) * (kind.bn <= 64 ? 2 : 1);
-    const int64_t most = mode == kGated ? 1 : std::min<int64_t>(16, kb / 2);
-    for (int64_t splits = 1; splits <= std::max<int64_t>(1, most); ++splits) {
+    const int64_t mt = outs * ((rows + 128 * kind.cg - 1) / (128 * kind.cg)), nt = (cols + width - 1) / width, tiles = mt * nt;
+    const int64_t slots = kind.cg == 2 ? sms / 2 : sms, kb = segments * stages_of(len, kind.bn);
+    const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 67.0));
+    const double epilogue = mode == kGated ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
+    const double tile = std::max(kb * step, epilogue) + 100.0;
+    auto offer = [&](int64_t whole, int64_t splits, double cost) {
+      if (best.cg != 0 && cost >= least) return;
+      least = cost;
+      const int64_t per = (kb + splits - 1) / splits;
+      best = {kind.cg, kind.bn, static_cast<uint32_t>(mt), static_cast<uint32_t>(nt), static_cast<uint32_t>(whole), static_cast<uint32_t>(tiles - whole),
+              static_cast<uint32_t>(splits), static_cast<uint32_t>(per)};
+    };
+    offer(tiles, 1, start + epilogue + std::ceil(static_cast<double>(tiles) / slots) * tile);
+    const int64_t whole = tiles / slots * slots, cut = tiles - whole;
+    for (int64_t splits = 2; cut > 0 && splits <= std::min<int64_t>(32, kb); ++splits) {
       const int64_t per = (kb + splits - 1) / splits;
       if ((kb + per - 1) / per != splits) continue;
-      const double waves = std::ceil(static_cast<double>(mt * nt * splits) / slots);
-      double cost = waves * (per * step + 300.0) + 1500.0 + 12.0 * kind.bn;
-      if (splits > 1) cost += 5000.0 + outs * static_cast<double>(rows) * cols * (8.0 * splits + 2.0) / 3400.0;
-      if (best.cg == 0 || cost < least) {
-        best = {kind.cg, kind.bn, static_cast<uint32_t>(mt), static_cast<uint32_t>(nt), static_cast<uint32_t>(splits), static_cast<uint32_t>(per)};
-        least = cost;
-      }
+      const double part = std::max(per * step, 5.0 * kind.bn + 400.0) + 100.0;
+      offer(whole, splits, start + 5.0 * kind.bn + 400.0 + static_cast<double>(whole / slots) * tile + std::ceil(static_cast<double>(cut * splits) / slots) * part +
+                               4000.0 + 128.0 * kind.cg * kind.bn * cut * (8.0 * splits + 2.0) / 3400.0);
     }
   }
   return best;
 }
 
-int64_t part_bytes(const Tile& t, int64_t rows, int64_t cols, int outs) {
-  return t.splits > 1 ? round_up(static_cast<int64_t>(t.splits) * outs * rows * round_up(cols, 32) * 4, 256) : 0;
-}
+int64_t part_bytes(const Tile& t) { return round_up(static_cast<int64_t>(t.cut) * (t.splits > 1 ? t.splits : 0) * 128 * t.cg * t.bn * 4, 256); }
 
 template <int CG, int BN, int MODE>
-int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStream_t s) {
+int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, Queue& s) {
   using S = TcShape<CG, BN, MODE>;
   static std::atomic<uint64_t> ready{0};        // devices on which this kernel has been given its shared memory
   int dev = 0;
@@ -238,17 +252,18 @@ int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStr
     if (err == cudaSuccess) ready.fetch_or(bit, std::memory_order_relaxed);
   }
   if (err != cudaSuccess) return gws::report_cuda(err, "shared memory of the block GEMM");
-  const uint32_t work = args.m_tiles * args.n_tiles * args.splits;
-  const uint32_t slots = CG == 2 ? static_cast<uint32_t>(sms / 2) : static_cast<uint32_t>(sms) * S::kPerSm;
-  return launch(k_tc<CG, BN, MODE>, std::min(work, slots) * CG, S::kThreads, S::kSmemBytes, CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
+  const uint32_t work = args.whole + args.cut * args.splits, slots = static_cast<uint32_t>(sms / CG);
+  const int st = launch(k_tc<CG, BN, MODE>, std::min(work, slots) * CG, S::kThreads, S::kSmemBytes, CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
+  if (st != GWS_OK || args.cut == 0) return st;
+  constexpr uint32_t kWarps = (MODE == kGated ? BN / 64 : BN / 32) * (128 * CG / kJoinRows);       // per tile
+  return launch(k_join<CG, BN, MODE>, args.cut * (kWarps / 8), 256, 0, 1, s, "join of a cut contraction", args);
 }
 
 template <int MODE>
-int launch_mode(const Tile& t, const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStream_t s) {
+int launch_mode(const Tile& t, const CUtensorMap (&maps)[4], const TcArgs& args, int sms, Queue& s) {
   if (t.cg == 2 && t.bn == 256) return launch_tc<2, 256, MODE>(maps, args, sms, s);
   if (t.cg == 2) return launch_tc<2, 128, MODE>(maps, args, sms, s);
-  if (t.bn == 128) return launch_tc<1, 128, MODE>(maps, args, sms, s);
-  return launch_tc<1, 64, MODE>(maps, args, sms, s);
+  return launch_tc<1, 128, MODE>(maps, args, sms, s);
 }
 
 TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t len, int segments, int* status) {
@@ -256,6 +271,8 @@ TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t len, int seg
   std::memset(&a, 0, sizeof a);
   a.m_tiles = t.m_tiles;
   a.n_tiles = t.n_tiles;
+  a.whole = t.whole;
+  a.cut = t.cut;
   a.splits = t.splits;
   a.tiles_per_out = t.m_tiles;
   a.len = static_cast<uint32_t>(len);
@@ -278,29 +295,19 @@ void set_out(TcArgs& a, void* out0, void* out1, int64_t ld) {
   a.direct = ld % 16 == 0 && on(out0, 32) && on(out1, 32);
 }
 
-int join(const TcArgs& a, cudaStream_t s) {
-  const int64_t items = a.ld_part / 4 * a.rows * (a.out[1] != nullptr ? 2 : 1);
-  const bool wide = a.ld_out % 4 == 0 && on(a.out[0], 8) && on(a.out[1], 8);
-  if ((items + kJobs - 1) / kJobs >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
-  return launch(k_join, blocks_for(items, kJobs), kJobs, 0, 1, s, "join of a split contraction", a.part, a.ld_part, a.part_stride, a.splits,
-                static_cast<uint16_t*>(a.out[0]), static_cast<uint16_t*>(a.out[1]), a.ld_out, a.rows, a.cols, wide ? 1 : 0);
-}
-
 // Copies fill rows outside a matrix with zeros at a fraction of the speed of rows inside it (one token, 128-row boxes: 31 us
 // where 128 tokens take 14), so a matrix of few rows gets boxes of few rows.  What the rest of the shared memory holds reaches only
 // accumulator rows that are not stored.
 uint32_t a_box(int64_t rows) { return static_cast<uint32_t>(std::min<int64_t>(128, round_up(rows, 8))); }
 
 // dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
-int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, int64_t ld_out, void* part, int* status, int sms, cudaStream_t s) {
+int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, int64_t ld_out, void* part, int* status, int sms, Queue& s) {
   const int outs = a1 != nullptr ? 2 : 1;
   const Tile t = choose(kDw, a0.cols, x.cols, outs, a0.rows, 1, sms);
   TcArgs args = base_args(t, a0.cols, x.cols, a0.rows, 1, status);
   args.tiles_per_out = t.m_tiles / outs;
   set_out(args, out0, out1, ld_out);
   args.part = static_cast<float*>(part);
-  args.ld_part = round_up(x.cols, 32);
-  args.part_stride = static_cast<int64_t>(outs) * args.rows * args.ld_part;
   // tokens fewer than a step: boxes and products of only the 16-token parts that hold any
   const uint32_t box = static_cast<uint32_t>(std::min<int64_t>(kTcHalf, round_up(a0.rows, 16)));
   args.parts = box / 16;
@@ -311,12 +318,11 @@ int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, i
   if (st == GWS_OK) st = make_map(maps[2], x.p, x.rows, x.cols, x.ld, box);
   if (st != GWS_OK) return st;
   maps[3] = maps[2];
-  st = launch_mode<kDw>(t, maps, args, sms, s);
-  return st == GWS_OK && t.splits > 1 ? join(args, s) : st;
+  return launch_mode<kDw>(t, maps, args, sms, s);
 }
 
 int64_t dw_part_bytes(int64_t m, int64_t rows, int64_t cols, int outs, int sms) {
-  return part_bytes(choose(kDw, rows, cols, outs, m, 1, sms), rows, cols, outs);
+  return part_bytes(choose(kDw, rows, cols, outs, m, 1, sms));
 }
 
 // ---- the gated block ---------------------------------------------------------------------------------------------------------
@@ -347,25 +353,26 @@ BackLayout back_layout(const gws_gated_desc* d, int sms) {
   l.w_up = take(w);
   l.grad_gate = take(packed_bytes(d->m, d->n));
   l.grad_up = take(packed_bytes(d->m, d->n));
-  const int64_t dx = d->m > 0 && d->k > 0 && d->n > 0 ? part_bytes(choose(kDx, d->m, d->k, 1, d->n, 2, sms), d->m, d->k, 1) : 0;
+  const int64_t dx = d->m > 0 && d->k > 0 && d->n > 0 ? part_bytes(choose(kDx, d->m, d->k, 1, d->n, 2, sms)) : 0;
   const int64_t dw = d->m > 0 && d->k > 0 && d->n > 0 ? dw_part_bytes(d->m, d->n, d->k, 2, sms) : 0;
   l.part = take(std::max(dx, dw));
   l.total = at;
   return l;
 }
-int64_t forward_bytes(const gws_gated_desc* d) {
-  const int64_t w = in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k);
-  return (in_place(d->m, d->ld_x) ? 0 : packed_bytes(d->m, d->k)) + 2 * w;
+// Forward: the copies realign makes, then the parts of cut tiles.
+int64_t forward_copies(const gws_gated_desc* d) {
+  return (in_place(d->m, d->ld_x) ? 0 : packed_bytes(d->m, d->k)) + (in_place(d->n, d->ld_w) ? 0 : 2 * packed_bytes(d->n, d->k));
 }
+int64_t forward_bytes(const gws_gated_desc* d, int sms) { return forward_copies(d) + part_bytes(choose(kGated, d->m, d->n, 1, d->k, 1, sms)); }
 
 template <int SAVE, int ACT>
-int launch_pre(const PreArgs& p, bool fast, cudaStream_t s) {
+int launch_pre(const PreArgs& p, bool fast, Queue& s) {
   const char* what = "gated backward, element-wise part";
   if (fast) return launch(k_gated_pre<SAVE, ACT>, blocks_for(p.groups, kJobs), kJobs, 0, 1, s, what, p);
   return launch(k_gated_pre_any<SAVE, ACT>, blocks_for(p.rows * ((p.per_row + kRun - 1) / kRun), 8), kJobs, 0, 1, s, what, p);
 }
 template <int SAVE>
-int launch_pre_act(const PreArgs& p, int act, bool fast, cudaStream_t s) {
+int launch_pre_act(const PreArgs& p, int act, bool fast, Queue& s) {
   if (act == GWS_GATED_SILU) return launch_pre<SAVE, GWS_GATED_SILU>(p, fast, s);
   if (act == GWS_GATED_GELU_TANH) return launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, fast, s);
   return launch_pre<SAVE, GWS_GATED_RELU>(p, fast, s);
@@ -396,7 +403,8 @@ static int act8_move(bool save, int64_t rows, int64_t cols, int64_t ld, int form
   if (x == nullptr || act8 == nullptr) return GWS_ERR_NULL;
   if (!on(x, 2) || !on(act8, 32)) return GWS_ERR_ALIGN;
   if (overlap(rows_of(x, rows, cols, ld), {act8, act8_total(rows, cols)})) return GWS_ERR_ALIAS;
-  return launch_act8(save, format, x, rows == 1 ? act8_ld(cols) : ld, act8_view(act8, rows, cols), rows, cols, static_cast<cudaStream_t>(stream));
+  Queue q{static_cast<cudaStream_t>(stream)};
+  return launch_act8(save, format, x, rows == 1 ? act8_ld(cols) : ld, act8_view(act8, rows, cols), rows, cols, q);
 }
 
 int gws_act8_save(int64_t rows, int64_t cols, int64_t ld, int format, const void* x, void* act8, void* stream) {
@@ -424,8 +432,8 @@ int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad
   if (ld_w > kMaxDim || ld_y > kMaxDim) return GWS_ERR_LIMIT;
   if (grad_w == nullptr || (m > 0 && (grad_y == nullptr || x8 == nullptr))) return GWS_ERR_NULL;
   if (!on(grad_w, 2) || !on(status, 4)) return GWS_ERR_ALIGN;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (m == 0) return zero(grad_w, n, k, ld_w, s);
+  Queue s{static_cast<cudaStream_t>(stream)};
+  if (m == 0) return zero(grad_w, n, k, ld_w, s.s);
   if (!on(grad_y, in_place(m, ld_y) ? 16 : 2) || !on(x8, 32)) return GWS_ERR_ALIGN;
   const int64_t need = gws_wgrad_act8_workspace_bytes(m, n, k, ld_y);
   if (clash({rows_of(grad_w, n, k, ld_w), {workspace, need}}, {rows_of(grad_y, m, n, ld_y), {x8, act8_total(m, k)}})) return GWS_ERR_ALIAS;
@@ -448,7 +456,7 @@ int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward) {
   const int st = check_gated(desc);
   if (st != GWS_OK) return st;
   if (desc->m == 0 || desc->n == 0 || desc->k == 0) return 0;
-  return backward != 0 ? back_layout(desc, sm_count()).total : forward_bytes(desc);
+  return backward != 0 ? back_layout(desc, sm_count()).total : forward_bytes(desc, sm_count());
 }
 
 int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate, const void* w_up, void* h, void* save_gate, void* save_up,
@@ -461,12 +469,12 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   if (d.m == 0 || d.n == 0) return GWS_OK;
   if (h == nullptr || (saves && (save_gate == nullptr || save_up == nullptr))) return GWS_ERR_NULL;
   if (!on(h, 2) || !on(status, 4) || (saves && (!on(save_gate, bytes8 ? 32 : 2) || !on(save_up, bytes8 ? 32 : 2)))) return GWS_ERR_ALIGN;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  Queue s{static_cast<cudaStream_t>(stream)};
   if (d.k == 0) {                              // both projections are zero, and so is act(0)
-    st = zero(h, d.m, d.n, d.ld_h, s);
+    st = zero(h, d.m, d.n, d.ld_h, s.s);
     for (void* p : {save_gate, save_up})
       if (st == GWS_OK && saves) {
-        const cudaError_t err = cudaMemsetAsync(p, 0, static_cast<size_t>(saved_bytes(desc)), s);
+        const cudaError_t err = cudaMemsetAsync(p, 0, static_cast<size_t>(saved_bytes(desc)), s.s);
         if (err != cudaSuccess) st = gws::report_cuda(err, "clearing a saved projection");
       }
     return st;
@@ -474,7 +482,8 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   if (x == nullptr || w_gate == nullptr || w_up == nullptr) return GWS_ERR_NULL;
   const bool moves_x = !in_place(d.m, d.ld_x), moves_w = !in_place(d.n, d.ld_w);
   if (!on(x, moves_x ? 2 : 16) || !on(w_gate, moves_w ? 2 : 16) || !on(w_up, moves_w ? 2 : 16)) return GWS_ERR_ALIGN;
-  const int64_t need = forward_bytes(desc), kept = saved_bytes(desc);
+  const int sms = sm_count();
+  const int64_t need = forward_bytes(desc, sms), kept = saved_bytes(desc);
   if (clash({rows_of(h, d.m, d.n, d.ld_h), {save_gate, kept}, {save_up, kept}, {workspace, need}},
             {rows_of(x, d.m, d.k, d.ld_x), rows_of(w_gate, d.n, d.k, d.ld_w), rows_of(w_up, d.n, d.k, d.ld_w)}))
     return GWS_ERR_ALIAS;
@@ -482,11 +491,11 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   Mat mx{x, d.m, d.k, d.ld_x}, mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
   if ((st = realign({&mx, &mg, &mu}, static_cast<char*>(workspace), s)) != GWS_OK) return st;
 
-  const int sms = sm_count();
   const Tile t = choose(kGated, d.m, d.n, 1, d.k, 1, sms);
   TcArgs args = base_args(t, d.m, d.n, d.k, 1, status);
   set_out(args, h, nullptr, d.ld_h);
   args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
+  args.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + forward_copies(desc));
   args.activation = d.activation;
   args.save = d.save_format;
   if (bytes8) {
@@ -515,12 +524,12 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   if ((!saved8 && d.save_format != GWS_SAVE_BF16) || (!x8 && d.x_format != GWS_SAVE_BF16)) return GWS_ERR_UNSUPPORTED;
   if ((grad_w_gate == nullptr) != (grad_w_up == nullptr)) return GWS_ERR_NULL;
   if (!on(grad_x, 2) || !on(grad_w_gate, 2) || !on(grad_w_up, 2) || !on(h_out, 2) || !on(status, 4)) return GWS_ERR_ALIGN;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  Queue s{static_cast<cudaStream_t>(stream)};
   if (d.m == 0 || d.n == 0 || d.k == 0) {      // empty sums; with k = 0 the projections are zero, and so is h
-    if ((st = zero(grad_x, d.m, d.k, d.k, s)) != GWS_OK || (st = zero(grad_w_gate, d.n, d.k, d.k, s)) != GWS_OK ||
-        (st = zero(grad_w_up, d.n, d.k, d.k, s)) != GWS_OK)
+    if ((st = zero(grad_x, d.m, d.k, d.k, s.s)) != GWS_OK || (st = zero(grad_w_gate, d.n, d.k, d.k, s.s)) != GWS_OK ||
+        (st = zero(grad_w_up, d.n, d.k, d.k, s.s)) != GWS_OK)
       return st;
-    return zero(h_out, d.m, d.n, d.n, s);
+    return zero(h_out, d.m, d.n, d.n, s.s);
   }
   const bool wants_dw = grad_w_gate != nullptr, wants_dx = grad_x != nullptr;
   if (grad_h == nullptr || save_gate == nullptr || save_up == nullptr || (wants_dw && x == nullptr) || (wants_dx && (w_gate == nullptr || w_up == nullptr)))
@@ -575,14 +584,11 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
     args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
     set_out(args, grad_x, nullptr, d.k);
     args.part = reinterpret_cast<float*>(ws + l.part);
-    args.ld_part = round_up(d.k, 32);
-    args.part_stride = d.m * args.ld_part;
     CUtensorMap maps[4];
     if ((st = make_map(maps[0], dg.p, d.m, d.n, dg.ld, a_box(d.m))) != GWS_OK || (st = make_map(maps[1], du.p, d.m, d.n, du.ld, a_box(d.m))) != GWS_OK ||
         (st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, kTcHalf)) != GWS_OK || (st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, kTcHalf)) != GWS_OK)
       return st;
     if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
-    if (t.splits > 1 && (st = join(args, s)) != GWS_OK) return st;
   }
   if (wants_dw) {
     Mat mx{x, d.m, d.k, d.ld_x};

@@ -13,8 +13,8 @@
 // epilogue of a tile runs under the products of the next one.  Blocks are persistent and take tiles round robin, in groups
 // of rows so that the tiles in flight share operands in L2.
 //
-// With few tiles and a long contraction the contraction is cut into `splits` parts, each written as FP32; k_join adds them in
-// a fixed order, so results do not depend on timing.
+// The tiles that do not fill a last wave of blocks (all of them, when there are few) have their contraction cut into `splits`
+// parts, each written as FP32; k_join adds the parts in a fixed order, so results do not depend on timing, and finishes the tile.
 //
 // Every wait is bounded (about a second); a wait that runs out sets the status word, the roles of the block leave their loops,
 // the block gives its copies time to land, frees its tensor memory and returns.
@@ -35,7 +35,8 @@ constexpr uint32_t kTcStagingWarp = 32u * 17u * 4u;        // a 32 x 32 BF16 blo
 constexpr long long kTcWaitCycles = 2000000000LL;
 
 struct TcArgs {
-  uint32_t m_tiles, n_tiles, splits;      // tiles along rows (all outputs), along columns, parts of the contraction
+  uint32_t m_tiles, n_tiles;              // tiles along rows (all outputs), along columns
+  uint32_t whole, cut, splits;            // tiles computed in one piece, and the rest, cut into `splits` parts
   uint32_t tiles_per_out;                 // kDw: row tiles of the first output
   uint32_t kb, kb_first, kb_split;        // stages of the contraction: all, of the first segment (kDx), of one part
   uint32_t len;                           // elements of the contraction (kDx: of each segment)
@@ -46,8 +47,7 @@ struct TcArgs {
   void* out[2];                           // BF16
   int64_t ld_out;
   int32_t direct;                         // rows of `out` take 32-byte stores
-  float* part;                            // splits > 1: FP32 [splits][rows][ld_part]
-  int64_t ld_part, part_stride;           // in elements; part_stride: of one part
+  float* part;                            // FP32 [splits][cut][128 * CG][BN]
   int32_t activation, save;               // kGated
   int32_t save_direct;
   Act8View save8[2];
@@ -232,6 +232,14 @@ __device__ __forceinline__ void gate_block(const uint32_t (&g)[32], const uint32
                      act_of<ACT>(__uint_as_float(g[2 * i + 1])) * __uint_as_float(u[2 * i + 1]));
 }
 
+// Tile number -> (row tile, column tile): groups of `group` row tiles, column by column inside a group.
+__device__ __forceinline__ void tile_at(const TcArgs& p, uint32_t t, uint32_t& mt, uint32_t& nt) {
+  const uint32_t per_group = p.group * p.n_tiles, g = t / per_group, rest = t - g * per_group;
+  const uint32_t height = min(p.group, p.m_tiles - g * p.group);
+  nt = rest / height;
+  mt = g * p.group + (rest - nt * height);
+}
+
 template <int CG, int BN, int MODE>
 struct TcShape {
   static constexpr uint32_t kBRows = BN / CG;                              // columns of B each block holds
@@ -241,18 +249,17 @@ struct TcShape {
   static constexpr uint32_t kHalves = BN == 256 ? 1u : 2u;
   static constexpr uint32_t kHalf = kTcABytes + kBRows * kTcHalf * 2u;     // A, then B
   static constexpr uint32_t kStage = kHalves * kHalf;
-  static constexpr uint32_t kPerSm = BN <= 64 ? 2u : 1u;                   // resident blocks
-  static constexpr uint32_t kEpilogueWarps = BN <= 64 ? 4u : 8u;           // one or two per quadrant of the accumulator's rows
+  static constexpr uint32_t kEpilogueWarps = 8u;                           // two per quadrant of the accumulator's rows
   static constexpr uint32_t kThreads = 128u + 32u * kEpilogueWarps;
   static constexpr uint32_t kStaging = kEpilogueWarps * kTcStagingWarp;
-  static constexpr uint32_t kFit = (kTcSmem / kPerSm - 4096u - kStaging) / kStage;
+  static constexpr uint32_t kFit = (kTcSmem - 4096u - kStaging) / kStage;
   static constexpr uint32_t kStages = kFit > 8u ? 8u : kFit;
   static constexpr uint32_t kSmemBytes = kStages * kStage + kStaging + 1024u;
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
 template <int CG, int BN, int MODE>
-__global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG, BN, MODE>::kPerSm))
+__global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
          const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
   using S = TcShape<CG, BN, MODE>;
@@ -302,18 +309,19 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
   }
   after_previous();
 
-  const uint32_t tiles = p.m_tiles * p.n_tiles, work = tiles * p.splits;
+  const uint32_t work = p.whole + p.cut * p.splits;
   const uint32_t first = blockIdx.x / CG, stride = gridDim.x / CG;
-  // tile -> (row tile, column tile): groups of `group` row tiles, column by column inside a group
+  // work item -> tile and stages of the contraction
   auto place = [&](uint32_t t, uint32_t& mt, uint32_t& nt, uint32_t& k0, uint32_t& k1) {
-    const uint32_t split = t / tiles;
-    t -= split * tiles;
-    const uint32_t per_group = p.group * p.n_tiles, g = t / per_group, rest = t - g * per_group;
-    const uint32_t height = min(p.group, p.m_tiles - g * p.group);
-    nt = rest / height;
-    mt = g * p.group + (rest - nt * height);
-    k0 = split * p.kb_split;
-    k1 = min(p.kb, k0 + p.kb_split);
+    k0 = 0;
+    k1 = p.kb;
+    if (t >= p.whole) {
+      const uint32_t split = (t - p.whole) / p.cut;
+      t -= split * p.cut;
+      k0 = split * p.kb_split;
+      k1 = min(p.kb, k0 + p.kb_split);
+    }
+    tile_at(p, t, mt, nt);
   };
 
   if (warp == 0) {
@@ -421,7 +429,22 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
       const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
       const bool second = MODE == kDw && mt >= p.tiles_per_out;
       const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + rank * 128u + quadrant * 32u;
-      if (MODE == kGated) {
+      if (t >= p.whole) {                     // a part of a contraction: FP32, joined by k_join
+        float* part = p.part + static_cast<int64_t>(t - p.whole) * (128 * CG * BN) + (rank * 128u + quadrant * 32u + lane) * BN;
+#pragma unroll 1
+        for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
+          uint32_t v[32];
+          acc_load(acc + c * 32u, v);
+          acc_wait();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            V8 x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x.x[e] = v[8 * i + e];
+            st32(part + c * 32u + 8 * i, x);
+          }
+        }
+      } else if (MODE == kGated) {
 #pragma unroll 1
         for (uint32_t c = half; c < BN / 64; c += S::kEpilogueWarps / 4u) {
           uint32_t g[32], u[32], w[16];
@@ -458,31 +481,16 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
         }
       } else {
         uint16_t* out = static_cast<uint16_t*>(p.out[second ? 1 : 0]);
-        float* part = p.part + static_cast<int64_t>(t / tiles) * p.part_stride + (second ? p.rows * p.ld_part : 0);
 #pragma unroll 1
         for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
-          uint32_t v[32];
+          uint32_t v[32], w[16];
           acc_load(acc + c * 32u, v);
           acc_wait();
           const int64_t col0 = static_cast<int64_t>(nt) * BN + c * 32u;
           if (col0 >= p.cols) continue;
-          if (p.splits > 1) {
-            if (row0 + lane < p.rows) {
-              float* q = part + (row0 + lane) * p.ld_part + col0;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                V8 x;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x.x[e] = v[8 * i + e];
-                st32(q + 8 * i, x);
-              }
-            }
-          } else {
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-            store_block(out, p.ld_out, p.direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
-          }
+          for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+          store_block(out, p.ld_out, p.direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -505,30 +513,66 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), (TcShape<CG
   }
 }
 
-// Adds the parts of a split contraction in order and rounds once.  A thread takes four columns of a row.
-__global__ void __launch_bounds__(256) k_join(const float* part, int64_t ld_part, int64_t part_stride, uint32_t splits, uint16_t* out0, uint16_t* out1,
-                                              int64_t ld_out, int64_t rows, int64_t cols, int32_t wide) {
+// Adds the parts of the cut tiles in order and does with the sums what the epilogue does with a whole tile.  A warp takes 32 columns
+// of kJoinRows rows, a lane a column: parts are read, and rows of any alignment written, side by side.
+constexpr int kJoinRows = 4;
+template <int CG, int BN, int MODE>
+__global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) {
   after_previous();
-  const int64_t quads = ld_part >> 2, t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (t >= quads * rows * (out1 != nullptr ? 2 : 1)) return;
-  const int64_t row = t / quads, col = (t - row * quads) * 4;
-  if (col >= cols) return;
-  const float* q = part + row * ld_part + col;
-  float4 s = *reinterpret_cast<const float4*>(q);
-  for (uint32_t i = 1; i < splits; ++i) {
-    const float4 v = *reinterpret_cast<const float4*>(q + i * part_stride);
-    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  constexpr uint32_t kChunks = MODE == kGated ? BN / 64 : BN / 32, kRuns = 128 * CG / kJoinRows;
+  const uint32_t lane = threadIdx.x & 31u, w = blockIdx.x * 8u + (threadIdx.x >> 5);
+  const uint32_t tile = w / (kChunks * kRuns), rest = w % (kChunks * kRuns), c = rest % kChunks, r0 = rest / kChunks * kJoinRows;
+  if (tile >= p.cut) return;
+  uint32_t mt, nt;
+  tile_at(p, p.whole + tile, mt, nt);
+  const bool second = MODE == kDw && mt >= p.tiles_per_out;
+  const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + r0;
+  const int64_t col0 = static_cast<int64_t>(nt) * (MODE == kGated ? BN / 2 : BN) + c * 32u, col = col0 + lane;
+  if (col0 >= p.cols || row0 >= p.rows) return;
+  const float* part = p.part + static_cast<int64_t>(tile) * (128 * CG * BN) + r0 * BN + c * 32u + lane;
+  const int64_t stride = static_cast<int64_t>(p.cut) * (128 * CG * BN);
+  float a[kJoinRows], b[kJoinRows];
+#pragma unroll
+  for (int i = 0; i < kJoinRows; ++i) {
+    a[i] = part[i * BN];
+    b[i] = MODE == kGated ? part[i * BN + BN / 2] : 0.0f;
   }
-  uint16_t* o = (row >= rows ? out1 + (row - rows) * ld_out : out0 + row * ld_out) + col;
-  const uint32_t lo = pack_bf16(s.x, s.y), hi = pack_bf16(s.z, s.w);
-  if (wide && col + 4 <= cols) {
-    *reinterpret_cast<uint2*>(o) = make_uint2(lo, hi);
-    return;
+  for (uint32_t k = 1; k < p.splits; ++k) {
+    part += stride;
+#pragma unroll
+    for (int i = 0; i < kJoinRows; ++i) {
+      a[i] += part[i * BN];
+      if (MODE == kGated) b[i] += part[i * BN + BN / 2];
+    }
   }
-  o[0] = static_cast<uint16_t>(lo);
-  if (col + 1 < cols) o[1] = static_cast<uint16_t>(lo >> 16);
-  if (col + 2 < cols) o[2] = static_cast<uint16_t>(hi);
-  if (col + 3 < cols) o[3] = static_cast<uint16_t>(hi >> 16);
+#pragma unroll
+  for (int i = 0; i < kJoinRows; ++i) {
+    const int64_t row = row0 + i;
+    if (row >= p.rows) break;
+    float v = a[i];
+    if (MODE == kGated) {
+      const float act = p.activation == GWS_GATED_SILU ? act_of<GWS_GATED_SILU>(a[i])
+                        : p.activation == GWS_GATED_GELU_TANH ? act_of<GWS_GATED_GELU_TANH>(a[i]) : act_of<GWS_GATED_RELU>(a[i]);
+      v = act * b[i];
+    }
+    if (col < p.cols) static_cast<uint16_t*>(p.out[second ? 1 : 0])[row * p.ld_out + col] = static_cast<uint16_t>(pack_bf16(v, 0.0f));
+    if (MODE == kGated && p.save != GWS_SAVE_NONE) {
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        const float x = which == 0 ? a[i] : b[i];
+        if (p.save == GWS_SAVE_BF16) {
+          if (col < p.cols) p.save16[which][row * p.cols + col] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
+          continue;
+        }
+        const Act8View& o = p.save8[which];
+        const uint32_t byte = scale_byte(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & 0x7FFFFFFFu), p.save);
+        const float inv = inverse_scale_of(byte);
+        const uint32_t code = byte == kNanByte ? 0u : p.save == GWS_ACT8_INT8 ? encode4_int8(x, 0.0f, 0.0f, 0.0f, inv) : encode4_e4m3(x, 0.0f, 0.0f, 0.0f, inv);
+        o.codes[row * o.ld + col] = static_cast<uint8_t>(code);
+        if (lane == 0) o.scales[row * (o.ld >> 5) + (col0 >> 5)] = static_cast<uint8_t>(byte);
+      }
+    }
+  }
 }
 
 // ---- the element-wise part of the backward pass ------------------------------------------------------------------------------
