@@ -132,17 +132,26 @@ Encode encoder() {
   return fn;
 }
 
-// A BF16 matrix whose copies are boxes of 64 columns by `box_rows` rows, 128-byte swizzle; outside it copies bring zeros.
-int make_map(CUtensorMap& map, const void* p, int64_t rows, int64_t cols, int64_t ld, uint32_t box_rows) {
+int encode_map(CUtensorMap& map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void* p, int64_t rows, int64_t cols, int64_t ld_bytes,
+               uint32_t box_cols, uint32_t box_rows) {
   const Encode encode = encoder();
   if (encode == nullptr) return gws::report_text("cuTensorMapEncodeTiled is not available from this driver");
   const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * 2u};
-  const cuuint32_t box[2] = {64u, box_rows}, steps[2] = {1u, 1u};
-  const CUresult res = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld_bytes)};
+  const cuuint32_t box[2] = {box_cols, box_rows}, steps[2] = {1u, 1u};
+  const CUresult res = encode(&map, type, 2, const_cast<void*>(p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (res != CUDA_SUCCESS) return gws::report_text(("cuTensorMapEncodeTiled failed with CUresult " + std::to_string(static_cast<int>(res))).c_str());
   return GWS_OK;
+}
+// A BF16 matrix whose copies are boxes of 64 columns by `box_rows` rows, 128-byte swizzle; outside it copies bring zeros.
+int make_map(CUtensorMap& map, const void* p, int64_t rows, int64_t cols, int64_t ld, uint32_t box_rows) {
+  return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, p, rows, cols, ld * 2, 64u, box_rows);
+}
+// The codes of a checkpoint in boxes of `box_cols` = 128 or 64 columns, swizzled over that width.
+int make_codes_map(CUtensorMap& map, const Act8View& c, int64_t rows, uint32_t box_cols, uint32_t box_rows) {
+  return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, box_cols == 128u ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, c.codes, rows, c.ld, c.ld,
+                    box_cols, box_rows);
 }
 
 // A matrix as the GEMM reads it: rows on 16-byte boundaries, in place or as a copy in the workspace.  Copies have rows of whole
@@ -301,8 +310,26 @@ void set_out(TcArgs& a, void* out0, void* out1, int64_t ld) {
 uint32_t a_box(int64_t rows) { return static_cast<uint32_t>(std::min<int64_t>(128, round_up(rows, 8))); }
 
 // dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
-int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, int64_t ld_out, void* part, int* status, int sms, Queue& s) {
+// Whether a checkpointed X is converted inside the GEMM, by its own warps, rather than restored into the workspace by a pass before
+// it.  Inside, every tile converts its columns again and the products wait for it a little at each stage; the pass costs a
+// launch and X's way through memory.  Measured, inside against before: 515 tokens, 768 x 768 10.0 against 14.3 us; 3001, 1023 x 2730
+// (8.4e9 products) 30.7 against 30.4; 16384, 2048 x 5632 (1.9e11) 349 against 315.
+bool converts_inside(int64_t tokens, int64_t rows, int64_t cols, int outs) {
+  return static_cast<double>(outs) * static_cast<double>(tokens) * static_cast<double>(rows) * static_cast<double>(cols) < 8e9;
+}
+
+// X: a BF16 matrix, or a checkpoint of the same shape (x8, format), for which `restored` is room in the workspace where
+// converts_inside says so.
+int run_dw(const Mat& a0, const Mat* a1, Mat x, const Act8View* x8, int format, void* restored, void* out0, void* out1, int64_t ld_out, void* part, int* status,
+           int sms, Queue& s) {
   const int outs = a1 != nullptr ? 2 : 1;
+  if (x8 != nullptr && !converts_inside(a0.rows, a0.cols, x.cols, outs)) {
+    x.p = restored;
+    x.ld = packed_ld(x.cols);
+    const int st = launch_act8(false, format, restored, x.ld, *x8, x.rows, x.ld, s);
+    if (st != GWS_OK) return st;
+    x8 = nullptr;
+  }
   const Tile t = choose(kDw, a0.cols, x.cols, outs, a0.rows, 1, sms);
   TcArgs args = base_args(t, a0.cols, x.cols, a0.rows, 1, status);
   args.tiles_per_out = t.m_tiles / outs;
@@ -311,14 +338,20 @@ int run_dw(const Mat& a0, const Mat* a1, const Mat& x, void* out0, void* out1, i
   // tokens fewer than a step: boxes and products of only the 16-token parts that hold any
   const uint32_t box = static_cast<uint32_t>(std::min<int64_t>(kTcHalf, round_up(a0.rows, 16)));
   args.parts = box / 16;
+  args.box_tokens = static_cast<int32_t>(box);
   args.half_bytes = args.half_bytes / kTcHalf * box;
   CUtensorMap maps[4];
   int st = make_map(maps[0], a0.p, a0.rows, a0.cols, a0.ld, box);
   if (st == GWS_OK) st = a1 != nullptr ? make_map(maps[1], a1->p, a1->rows, a1->cols, a1->ld, box) : (maps[1] = maps[0], GWS_OK);
-  if (st == GWS_OK) st = make_map(maps[2], x.p, x.rows, x.cols, x.ld, box);
+  if (st == GWS_OK) st = x8 != nullptr ? make_codes_map(maps[2], *x8, x.rows, static_cast<uint32_t>(t.bn / t.cg), box) : make_map(maps[2], x.p, x.rows, x.cols, x.ld, box);
   if (st != GWS_OK) return st;
   maps[3] = maps[2];
-  return launch_mode<kDw>(t, maps, args, sms, s);
+  if (x8 == nullptr) return launch_mode<kDw>(t, maps, args, sms, s);
+  args.half_bytes = static_cast<uint32_t>(t.cg) * kTcABytes / kTcHalf * box;
+  args.scales = x8->scales;
+  args.scales_ld = x8->ld / kGroup;
+  args.x_format = format;
+  return launch_mode<kDw8>(t, maps, args, sms, s);
 }
 
 int64_t dw_part_bytes(int64_t m, int64_t rows, int64_t cols, int outs, int sms) {
@@ -347,7 +380,8 @@ BackLayout back_layout(const gws_gated_desc* d, int sms) {
   BackLayout l{};
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t here = at; at += round_up(bytes, 256); return here; };
-  l.x = take(is_act8(d->x_format) || !in_place(d->m, d->ld_x) ? packed_bytes(d->m, d->k) : 0);
+  const bool direct_x = is_act8(d->x_format) ? converts_inside(d->m, d->n, d->k, 2) : in_place(d->m, d->ld_x);
+  l.x = take(direct_x ? 0 : packed_bytes(d->m, d->k));
   const int64_t w = in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k);
   l.w_gate = take(w);
   l.w_up = take(w);
@@ -419,7 +453,7 @@ int64_t gws_wgrad_act8_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t 
   const int st = check_dims(m, n, k);
   if (st != GWS_OK) return st;
   if (m == 0 || n == 0 || k == 0) return 0;
-  return packed_bytes(m, k) + (in_place(m, ld_y) ? 0 : packed_bytes(m, n)) + dw_part_bytes(m, n, k, 1, sm_count());
+  return (in_place(m, ld_y) ? 0 : packed_bytes(m, n)) + (converts_inside(m, n, k, 1) ? 0 : packed_bytes(m, k)) + dw_part_bytes(m, n, k, 1, sm_count());
 }
 
 int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad_y, int64_t ld_y, const void* x8, void* grad_w, int64_t ld_w,
@@ -439,17 +473,14 @@ int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad
   if (clash({rows_of(grad_w, n, k, ld_w), {workspace, need}}, {rows_of(grad_y, m, n, ld_y), {x8, act8_total(m, k)}})) return GWS_ERR_ALIAS;
   if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
-  const int64_t ldx = packed_ld(k);
-  st = launch_act8(false, format, ws, ldx, act8_view(x8, m, k), m, ldx, s);
-  if (st != GWS_OK) return st;
-  const Mat x{ws, m, k, ldx};
-  ws += packed_bytes(m, k);
   Mat y{grad_y, m, n, ld_y};
   const bool moved = !in_place(m, ld_y);
   st = realign({&y}, ws, s);
   if (st != GWS_OK) return st;
+  const Act8View x = act8_view(x8, m, k);
   if (moved) ws += packed_bytes(m, n);
-  return run_dw(y, nullptr, x, grad_w, nullptr, ld_w, ws, status, sm_count(), s);
+  char* part = ws + (converts_inside(m, n, k, 1) ? 0 : packed_bytes(m, k));
+  return run_dw(y, nullptr, Mat{nullptr, m, k, 0}, &x, format, ws, grad_w, nullptr, ld_w, part, status, sm_count(), s);
 }
 
 int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward) {
@@ -534,7 +565,7 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   const bool wants_dw = grad_w_gate != nullptr, wants_dx = grad_x != nullptr;
   if (grad_h == nullptr || save_gate == nullptr || save_up == nullptr || (wants_dw && x == nullptr) || (wants_dx && (w_gate == nullptr || w_up == nullptr)))
     return GWS_ERR_NULL;
-  const bool moves_x = x8 || !in_place(d.m, d.ld_x), moves_w = !in_place(d.n, d.ld_w);
+  const bool moves_x = !x8 && !in_place(d.m, d.ld_x), moves_w = !in_place(d.n, d.ld_w);
   if (!on(grad_h, 2) || !on(save_gate, saved8 ? 32 : 2) || !on(save_up, saved8 ? 32 : 2) || (wants_dw && !on(x, x8 ? 32 : moves_x ? 2 : 16)) ||
       (wants_dx && (!on(w_gate, moves_w ? 2 : 16) || !on(w_up, moves_w ? 2 : 16))))
     return GWS_ERR_ALIGN;
@@ -592,14 +623,9 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   }
   if (wants_dw) {
     Mat mx{x, d.m, d.k, d.ld_x};
-    if (x8) {
-      mx = {ws + l.x, d.m, d.k, packed_ld(d.k)};
-      st = launch_act8(false, d.x_format, mx.p, mx.ld, act8_view(x, d.m, d.k), d.m, mx.ld, s);
-    } else {
-      st = realign({&mx}, ws + l.x, s);
-    }
-    if (st != GWS_OK) return st;
-    return run_dw(dg, &du, mx, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
+    const Act8View kept_x = act8_view(x, d.m, d.k);
+    if (!x8 && (st = realign({&mx}, ws + l.x, s)) != GWS_OK) return st;
+    return run_dw(dg, &du, mx, x8 ? &kept_x : nullptr, d.x_format, ws + l.x, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
   }
   return GWS_OK;
 }

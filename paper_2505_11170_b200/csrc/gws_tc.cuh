@@ -5,6 +5,9 @@
 //            the product and the 8-bit copies for the backward pass happen on registers in the epilogue
 //   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du
 //   kDw      dW = dY^T X: both operands are read along their contiguous (not the contracted) axis, as they lie in memory
+//   kDw8     the same with X an 8-bit checkpoint: its codes are copied to shared memory and eight more warps turn them into the BF16
+//            operand there, under the products of earlier stages, so that X crosses L2 and HBM at one byte per element and no BF16
+//            copy of it exists
 //
 // A tile is 128 * CG rows by BN columns of accumulator; CG = 2 is a pair of SMs working on one tile (cta_group::2: each SM
 // holds its 128 rows of A and half of the columns of B, so an operand byte fetched from L2 feeds twice the products).
@@ -26,7 +29,7 @@
 
 namespace {
 
-enum { kGated = 0, kDx = 1, kDw = 2 };
+enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3 };
 
 constexpr uint32_t kTcHalf = 64;                           // elements along the contraction per copy: 128 bytes, one swizzle atom
 constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
@@ -48,6 +51,10 @@ struct TcArgs {
   int64_t ld_out;
   int32_t direct;                         // rows of `out` take 32-byte stores
   float* part;                            // FP32 [splits][cut][128 * CG][BN]
+  const uint8_t* scales;                  // kDw8: scale bytes of X, [tokens, scales_ld]
+  int64_t scales_ld;
+  int32_t x_format;
+  int32_t box_tokens;                     // kDw, kDw8: tokens in a copy
   int32_t activation, save;               // kGated
   int32_t save_direct;
   Act8View save8[2];
@@ -75,15 +82,25 @@ __device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) {
 __device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
 }
-// Arrives on a barrier of any block of the pair (shared::cluster address).
+// Arrives on a barrier of any block of the pair (shared::cluster address).  What it announces is the arriving block's own shared or
+// tensor memory, ordered for the tensor cores by the proxy or tcgen05 fence before it; a release at cluster scope would wait for
+// all of the warp's memory traffic instead (a stage of conversion took 1900 cycles with it, 700 without).
 __device__ __forceinline__ void bar_arrive(uint32_t cluster_addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // A whole warp waits for the phase of the given parity; false, for every lane, if it did not complete within kTcWaitCycles.  The
 // clock is only read once the first try has failed: the two warps that feed the tensor cores pass here once per stage.
+// CLUSTER: what the other block of the pair wrote before it arrived is visible afterwards.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_try(uint32_t addr, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+  if (CLUSTER)
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done)
+                 : "r"(addr), "r"(parity)
+                 : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                : "=r"(done)
                : "r"(addr), "r"(parity)
                : "memory");
@@ -98,11 +115,12 @@ __device__ __forceinline__ bool bar_peek(uint32_t addr, uint32_t parity) {
                : "memory");
   return done != 0;
 }
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint32_t addr, uint32_t parity) {
-  if (__all_sync(0xFFFFFFFFu, bar_try(addr, parity))) return true;
+  if (__all_sync(0xFFFFFFFFu, bar_try<CLUSTER>(addr, parity))) return true;
   const long long t0 = clock64();
   for (;;) {
-    if (__all_sync(0xFFFFFFFFu, bar_try(addr, parity))) return true;
+    if (__all_sync(0xFFFFFFFFu, bar_try<CLUSTER>(addr, parity))) return true;
     if (__any_sync(0xFFFFFFFFu, clock64() - t0 > kTcWaitCycles)) return false;
   }
 }
@@ -243,33 +261,86 @@ __device__ __forceinline__ void tile_at(const TcArgs& p, uint32_t t, uint32_t& m
 template <int CG, int BN, int MODE>
 struct TcShape {
   static constexpr uint32_t kBRows = BN / CG;                              // columns of B each block holds
+  static constexpr uint32_t kEpilogueWarps = 8u;                           // two per quadrant of the accumulator's rows
+  static constexpr uint32_t kConvertWarps = MODE == kDw8 ? 8u : 0u;
+  static constexpr uint32_t kThreads = 128u + 32u * (kEpilogueWarps + kConvertWarps);
+  static constexpr uint32_t kStaging = kEpilogueWarps * kTcStagingWarp;
   // Copies of 64 elements per stage.  A stage costs the warp that issues the products some 250 cycles whatever it holds; the
   // products of 64 elements take 512 cycles with 256 columns on a pair of SMs, 128 to 256 with the smaller tiles, which therefore
   // take two copies per stage (2048 x 5632 into 128 rows, 128 columns: 396 -> 250 cycles per 64 elements).
   static constexpr uint32_t kHalves = BN == 256 ? 1u : 2u;
-  static constexpr uint32_t kHalf = kTcABytes + kBRows * kTcHalf * 2u;     // A, then B
+  static constexpr uint32_t kBBytes = kBRows * kTcHalf * 2u;
+  static constexpr uint32_t kRaw = MODE == kDw8 ? kBRows * kTcHalf : 0u;   // codes of B
+  static constexpr uint32_t kHalf = kTcABytes + kBBytes + kRaw;            // A, B, codes
   static constexpr uint32_t kStage = kHalves * kHalf;
-  static constexpr uint32_t kEpilogueWarps = 8u;                           // two per quadrant of the accumulator's rows
-  static constexpr uint32_t kThreads = 128u + 32u * kEpilogueWarps;
-  static constexpr uint32_t kStaging = kEpilogueWarps * kTcStagingWarp;
   static constexpr uint32_t kFit = (kTcSmem - 4096u - kStaging) / kStage;
   static constexpr uint32_t kStages = kFit > 8u ? 8u : kFit;
   static constexpr uint32_t kSmemBytes = kStages * kStage + kStaging + 1024u;
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
+// Codes of a checkpoint -> BF16 numbers, two at a time in packed BF16 arithmetic; every step is exact.
+// INT8: a code c = low - 128 s (its low 7 bits and its sign bit); with 0x43 above it the byte is a BF16 number, 128 + low without the
+// sign bit and 128 (1 + s) without the low bits, whose difference is c.  2 1/2 instructions a code against 3 3/4 through FP32.
+// E4M3: its exponent and mantissa 4 bits up are those of a BF16 number 2^120 too small (subnormals included).
+template <int FMT>
+struct Units {
+  __nv_bfloat162 unit;
+  __device__ __forceinline__ explicit Units(uint32_t byte) : unit(__float2bfloat162_rn(unit_of<FMT>(byte))) {}
+};
+__device__ __forceinline__ __nv_bfloat162 as_pair(uint32_t v) { return *reinterpret_cast<const __nv_bfloat162*>(&v); }
+__device__ __forceinline__ uint32_t as_word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+template <int FMT>
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t codes, uint32_t half, const Units<FMT>& u) {
+  if (FMT == GWS_ACT8_INT8) {
+    const uint32_t p = __byte_perm(codes, 0x43434343u, half == 0u ? 0x4140u : 0x4342u);
+    return as_word(__hmul2(__hsub2(as_pair(p & 0xFF7FFF7Fu), as_pair(p & 0xFF80FF80u)), u.unit));
+  }
+  const uint32_t p = __byte_perm(codes, 0u, half == 0u ? 0x1404u : 0x3424u), mag = (p >> 4) & 0x07F007F0u;
+  return as_word(__hmul2(__hmul2(as_pair((p & 0x80008000u) | mag), __float2bfloat162_rn(0x1p120f)), u.unit));
+}
+template <int FMT>
+__device__ __forceinline__ uint4 bf16_of_codes(uint32_t lo, uint32_t hi, const Units<FMT>& u) {
+  return make_uint4(bf16_pair<FMT>(lo, 0, u), bf16_pair<FMT>(lo, 1, u), bf16_pair<FMT>(hi, 0, u), bf16_pair<FMT>(hi, 1, u));
+}
+
+// Four warps' conversion of a copy: 64 tokens by COLS columns of codes (as the copy left them, rows of COLS bytes, swizzled) to the
+// BF16 operand (blocks of 64 columns, rows of 128 bytes, swizzled).  A thread takes one token's COLS / 2 columns, so that eight
+// neighbouring lanes touch eight different 16-byte columns of the banks on either side.
+template <int FMT, uint32_t COLS>
+__device__ __forceinline__ void convert_codes(uint32_t raw, uint32_t dst, uint32_t token, uint32_t side, const uint32_t (&bytes)[COLS / 64u]) {
+#pragma unroll
+  for (uint32_t g = 0; g < COLS / 64u; ++g) {
+    const Units<FMT> unit(bytes[g]);
+#pragma unroll
+    for (uint32_t h = 0; h < 2u; ++h) {
+      const uint32_t c = side * (COLS / 32u) + g * 2u + h;                       // 16-byte unit of the row of codes
+      const uint32_t from = raw + token * COLS + ((COLS == 128u ? c ^ (token & 7u) : c ^ ((token >> 1) & 3u)) << 4);
+      uint32_t w[4];
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from));
+#pragma unroll
+      for (uint32_t q = 0; q < 2u; ++q) {
+        const uint4 v = bf16_of_codes<FMT>(w[2 * q], w[2 * q + 1], unit);
+        const uint32_t unit16 = c * 2u + q;                                      // 16-byte unit of the row of BF16 numbers
+        const uint32_t to = dst + (unit16 >> 3) * 8192u + token * 128u + (((unit16 & 7u) ^ (token & 7u)) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w));
+      }
+    }
+  }
+}
+
 template <int CG, int BN, int MODE>
 __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
          const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
   using S = TcShape<CG, BN, MODE>;
-  constexpr bool kMnA = MODE == kDw, kMnB = MODE != kGated;
+  constexpr bool kIsDw = MODE == kDw || MODE == kDw8, kMnA = kIsDw, kMnB = MODE != kGated;
   constexpr uint32_t kStages = S::kStages;
   // instruction descriptor: FP32 accumulator, BF16 operands, which axis of A and B is contiguous, N, M
   constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kMnA ? 1u : 0u) << 15) | ((kMnB ? 1u : 0u) << 16) |
                               (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+  __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], codes_full[kStages], converted[kStages];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int failed;
   const uint32_t raw = smem_addr(smem_raw);
@@ -282,6 +353,8 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     for (uint32_t s = 0; s < kStages; ++s) {
       bar_init(&full[s], 1);
       bar_init(&empty[s], 1);
+      bar_init(&codes_full[s], 1);
+      bar_init(&converted[s], 4 * CG);
     }
     for (int b = 0; b < 2; ++b) {
       bar_init(&acc_full[b], 1);
@@ -331,7 +404,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     for (uint32_t t = first; ok && t < work; t += stride) {
       uint32_t mt, nt, k0, k1;
       place(t, mt, nt, k0, k1);
-      const bool second = MODE == kDw && mt >= p.tiles_per_out;
+      const bool second = kIsDw && mt >= p.tiles_per_out;
       const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
       const int32_t n0 = static_cast<int32_t>(nt * (MODE == kGated ? BN / 2 : BN) + (MODE == kGated ? 0u : rank * S::kBRows));
       for (uint32_t kb = k0; kb < k1; ++kb) {
@@ -341,6 +414,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         const uint32_t halves = S::kHalves == 1u || k + kTcHalf >= p.len ? 1u : 2u;     // a second copy past the end is left out
         if (elected()) {
           if (rank == 0) bar_expect(&full[s], halves * p.half_bytes);
+          if (MODE == kDw8) bar_expect(&codes_full[s], halves * S::kBRows * static_cast<uint32_t>(p.box_tokens));
           const uint32_t bar = full0 + 8u * s;
 #pragma unroll
           for (uint32_t i = 0; i < S::kHalves; ++i) {
@@ -362,8 +436,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
             } else {
 #pragma unroll
               for (uint32_t j = 0; j < 2u; ++j) copy_in<CG>(sa + j * 8192u, second ? &a1 : &a0, bar, m0 + static_cast<int32_t>(j * 64u), ki);
+              if (MODE == kDw8) {
+                copy_in<1>(sb + S::kBBytes, &b0, smem_addr(&codes_full[s]), n0, ki);
+              } else {
 #pragma unroll
-              for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(j * 64u), ki);
+                for (uint32_t j = 0; j < S::kBRows / 64u; ++j) copy_in<CG>(sb + j * 8192u, &b0, bar, n0 + static_cast<int32_t>(j * 64u), ki);
+              }
             }
           }
         }
@@ -385,11 +463,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         uint32_t mt, nt, k0, k1;
         place(t, mt, nt, k0, k1);
         const uint32_t buf = n & 1u, d = tmem + buf * BN;
-        if (!bar_wait(acc_empty0 + 8u * buf, ((n >> 1) & 1u) ^ 1u)) { ok = false; break; }
+        if (!bar_wait<CG == 2>(acc_empty0 + 8u * buf, ((n >> 1) & 1u) ^ 1u)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         bool ready = bar_try(full0 + 8u * s, parity);
         for (uint32_t kb = k0; kb < k1; ++kb) {
           if (!__all_sync(0xFFFFFFFFu, ready) && !bar_wait(full0 + 8u * s, parity)) { ok = false; break; }
+          if (MODE == kDw8 && !bar_wait<CG == 2>(smem_addr(&converted[s]), parity)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t now = s;
           if (++s == kStages) { s = 0; parity ^= 1u; }
@@ -405,7 +484,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
               mma<CG>(d, sa, sb, kIdesc, kb > k0 || i > 0 ? 1u : 0u);
 #pragma unroll
               for (uint32_t j = 1; j < kTcHalf / 16u; ++j)
-                if (MODE != kDw || j < p.parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
+                if (!kIsDw || j < p.parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
             }
             commit<CG>(&empty[now]);
           }
@@ -416,7 +495,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       }
       if (!ok) failed = 1;
     }
-  } else if (warp >= 4) {
+  } else if (warp >= 4 && warp < 4u + S::kEpilogueWarps) {
     const uint32_t quadrant = warp & 3u, half = (warp - 4u) >> 2;   // a warp reads the 32 accumulator rows of its quadrant
     uint32_t* stage = staging + (warp - 4u) * 32u * 17u;
     uint32_t n = 0;
@@ -427,7 +506,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) { failed = 1; break; }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
-      const bool second = MODE == kDw && mt >= p.tiles_per_out;
+      const bool second = kIsDw && mt >= p.tiles_per_out;
       const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + rank * 128u + quadrant * 32u;
       if (t >= p.whole) {                     // a part of a contraction: FP32, joined by k_join
         float* part = p.part + static_cast<int64_t>(t - p.whole) * (128 * CG * BN) + (rank * 128u + quadrant * 32u + lane) * BN;
@@ -497,6 +576,56 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       __syncwarp();
       if (lane == 0) bar_arrive(at_rank(smem_addr(&acc_empty[buf]), 0u));
     }
+  } else if (MODE == kDw8 && warp >= 4u + S::kEpilogueWarps) {
+    // Two teams of four warps take the stages in turn: one waits for codes while the other converts.
+    const uint32_t i = threadIdx.x - 32u * (4u + S::kEpilogueWarps), team = i >> 7, token = i & 63u, side = (i >> 6) & 1u;
+    constexpr uint32_t kGroups = S::kBRows / 64u;        // scale bytes of a thread per copy
+    // They come from global memory kAhead of the team's stages before they are needed.
+    constexpr uint32_t kAhead = 2;
+    uint32_t it = 0;                                     // stages of all tiles before the present one
+    bool ok = true;
+    for (uint32_t t = first; ok && t < work; t += stride) {
+      uint32_t mt, nt, k0, k1;
+      place(t, mt, nt, k0, k1);
+      const uint32_t group = (nt * BN + rank * S::kBRows) / 32u + side * kGroups;
+      const uint8_t* scales = p.scales + group;
+      uint32_t bytes[kAhead][S::kHalves][kGroups];
+      auto fetch = [&](uint32_t kb, uint32_t (&to)[S::kHalves][kGroups]) {
+#pragma unroll
+        for (uint32_t h = 0; h < S::kHalves; ++h)
+#pragma unroll
+          for (uint32_t g = 0; g < kGroups; ++g) {        // tokens and groups outside the checkpoint have zero codes
+            const uint32_t at = kb * (S::kHalves * kTcHalf) + h * kTcHalf + token;
+            to[h][g] = kb < k1 && at < p.len && group + g < p.scales_ld ? scales[static_cast<int64_t>(at) * p.scales_ld + g] : 0u;
+          }
+      };
+      const uint32_t mine = k0 + ((it ^ team) & 1u);      // the team's first stage of this tile
+#pragma unroll
+      for (uint32_t d = 0; d < kAhead; ++d) fetch(mine + 2u * d, bytes[d]);
+      for (uint32_t kb0 = mine; ok && kb0 < k1; kb0 += 2u * kAhead) {
+#pragma unroll
+        for (uint32_t d = 0; d < kAhead; ++d) {
+          const uint32_t kb = kb0 + 2u * d;
+          if (kb >= k1) break;
+          const uint32_t n = it + (kb - k0), s = n % kStages;
+          if (!bar_wait(smem_addr(&codes_full[s]), (n / kStages) & 1u)) { ok = false; break; }
+          const uint32_t halves = S::kHalves == 1u || kb * (S::kHalves * kTcHalf) + kTcHalf >= p.len ? 1u : 2u;
+#pragma unroll
+          for (uint32_t h = 0; h < S::kHalves; ++h) {
+            if (h >= halves) break;
+            const uint32_t b = smem_addr(smem) + s * S::kStage + h * S::kHalf + kTcABytes;
+            if (p.x_format == GWS_ACT8_INT8) convert_codes<GWS_ACT8_INT8, S::kBRows>(b + S::kBBytes, b, token, side, bytes[d][h]);
+            else convert_codes<GWS_ACT8_E4M3, S::kBRows>(b + S::kBBytes, b, token, side, bytes[d][h]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the tensor cores read shared memory through the async proxy
+          __syncwarp();
+          if (lane == 0) bar_arrive(at_rank(smem_addr(&converted[s]), 0u));
+          fetch(kb + 2u * kAhead, bytes[d]);
+        }
+      }
+      it += k1 - k0;
+    }
+    if (!ok) failed = 1;
   }
   __syncthreads();
   if (failed) {                          // copies and products that were started get time to end before the memory is given up
@@ -525,7 +654,7 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
   if (tile >= p.cut) return;
   uint32_t mt, nt;
   tile_at(p, p.whole + tile, mt, nt);
-  const bool second = MODE == kDw && mt >= p.tiles_per_out;
+  const bool second = (MODE == kDw || MODE == kDw8) && mt >= p.tiles_per_out;
   const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + r0;
   const int64_t col0 = static_cast<int64_t>(nt) * (MODE == kGated ? BN / 2 : BN) + c * 32u, col = col0 + lane;
   if (col0 >= p.cols || row0 >= p.rows) return;
