@@ -35,9 +35,9 @@ __device__ __forceinline__ void st32(void* p, const V8& v) {
                : "memory");
 }
 
-// Kernels of one call follow each other with programmatic launches: a kernel's blocks may become resident while the one before it on
-// the stream drains, and touch global memory only once that one has completed.  Every kernel of this file set passes here
-// before its first access, so the order along the stream holds transitively.
+// These kernels are launched programmatically: a kernel's blocks may become resident while the one before it on the stream drains, and
+// touch global memory only once that one has completed.  Every kernel of this file set passes here before its first access, so
+// the order along the stream holds transitively.
 __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -208,32 +208,30 @@ __global__ void __launch_bounds__(256) k_act8_save_any(const uint16_t* x, int64_
   if ((t & 3) == 0) c.scales[t >> 2] = static_cast<uint8_t>(byte);
 }
 
-// Load: a warp takes four neighbouring groups of a row, a lane an element of each, so that rows of any alignment are written side
-// by side (BF16 written one by one by a thread of its own would cost a partial write of a memory sector each).
-constexpr int kRun = 4;
+// Load: a warp takes a run of 256 columns of a row, a lane eight neighbouring ones, which pass through shared memory so that rows of
+// any alignment are written one element at a time but side by side.
 template <int FMT>
-__global__ void __launch_bounds__(256) k_act8_load_any(Act8View c, uint16_t* x, int64_t ldx, int64_t runs, uint32_t runs_per_row, uint32_t per_row,
-                                                       int64_t cols) {
+__global__ void __launch_bounds__(256) k_act8_load_any(Act8View c, uint16_t* x, int64_t ldx, int64_t runs, uint32_t runs_per_row, int64_t cols) {
   after_previous();
-  const uint32_t lane = threadIdx.x & 31u;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  __shared__ uint4 turn[8][32];
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + warp;
   if (t >= runs) return;
-  const int64_t row = quotient(t, runs_per_row);
-  const uint32_t g0 = static_cast<uint32_t>(t - row * runs_per_row) * kRun;
-  const int64_t group = row * per_row + g0, col = static_cast<int64_t>(g0) * kGroup + lane;
-  uint32_t code[kRun], byte[kRun];
-#pragma unroll
-  for (int i = 0; i < kRun; ++i) {
-    const bool real = g0 + i < per_row;
-    code[i] = real ? c.codes[(group + i) * kGroup + lane] : 0u;
-    byte[i] = real ? c.scales[group + i] : 0u;
+  const int64_t row = quotient(t, runs_per_row), run = (t - row * runs_per_row) * 256, at = row * c.ld + run + lane * 8;
+  if (run + lane * 8 < c.ld) {
+    const uint2 codes = *reinterpret_cast<const uint2*>(c.codes + at);
+    const float unit = unit_of<FMT>(c.scales[at >> 5]);
+    float v[8];
+    decode4<FMT>(codes.x, unit, v);
+    decode4<FMT>(codes.y, unit, v + 4);
+    turn[warp][lane] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
   }
+  __syncwarp();
+  const uint16_t* side = reinterpret_cast<const uint16_t*>(turn[warp]) + lane;
+  uint16_t* to = x + row * ldx + run + lane;
 #pragma unroll
-  for (int i = 0; i < kRun; ++i) {
-    float v[4];
-    decode4<FMT>(code[i], unit_of<FMT>(byte[i]), v);
-    if (col + i * kGroup < cols) x[row * ldx + col + i * kGroup] = static_cast<uint16_t>(pack_bf16(v[0], 0.0f));
-  }
+  for (int i = 0; i < 8; ++i)
+    if (run + lane + 32 * i < cols) to[32 * i] = side[32 * i];
 }
 
 // ---- BF16 rows brought into the alignment a tensor map wants ---------------------------------------------------------------
