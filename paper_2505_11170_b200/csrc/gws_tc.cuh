@@ -353,6 +353,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
                               (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], codes_full[kStages], converted[kStages];
+  __shared__ __align__(16) uint8_t scale_bytes[2][2][MODE == kGated ? 128 : 1][4];      // of two tiles, gate and up projection
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int failed;
   const uint32_t raw = smem_addr(smem_raw);
@@ -566,7 +567,25 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
               V8 codes;
               const uint32_t byte = p.save == GWS_ACT8_INT8 ? encode_group<GWS_ACT8_INT8>(v, codes) : encode_group<GWS_ACT8_E4M3>(v, codes);
               st32(p.save8[which].codes + row * p.save8[which].ld + col0, codes);
-              p.save8[which].scales[row * (p.save8[which].ld >> 5) + (col0 >> 5)] = static_cast<uint8_t>(byte);
+              scale_bytes[buf][which][quadrant * 32u + lane][c] = static_cast<uint8_t>(byte);
+            }
+          }
+        }
+        if (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3) {
+          // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
+          // The two warps that share these rows meet; one writes the gate's, the other the up projection's.  A warp that fills the same
+          // buffer again has passed the meeting of the tile between, and so has the other one's store.
+          asm volatile("bar.sync %0, 64;" ::"r"(quadrant + 1u) : "memory");
+          const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (BN / 64);
+          if (row < p.rows) {
+            uint8_t* to = p.save8[half].scales + row * ld + g0;
+            const uint8_t* from = scale_bytes[buf][half][quadrant * 32u + lane];
+            constexpr uint32_t kGroups = BN / 64;
+            if (g0 + kGroups <= ld && ld % kGroups == 0) {            // the buffer's scales start at a multiple of 256 bytes
+              if (kGroups == 4u) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
+              else *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
+            } else {
+              for (uint32_t i = 0; i < kGroups && g0 + i < ld; ++i) to[i] = from[i];
             }
           }
         }
