@@ -9,6 +9,10 @@
 and whose backward pass returns dL/dw = dL/dw_hat, dL/db_i through Eq. 4 (gws_sample_bwd, R regenerated from
 the same (seed, step)) and Eq. 11 / Eq. 12 (gws_bitwidth_grad).  The module only wires tensors to the library:
 every step of the sampling pass runs in its kernels.  The GEMMs are torch's, exactly as the paper keeps them.
+
+``GaussWSGatedMLP`` is the gated feed-forward block on three such layers.  Its gate and up projections, the activation and their product
+run in the library's block kernels, and what the block keeps for its backward pass - its input and the two projections - may be held
+as 8-bit activation checkpoints; ``GaussWSLinear(keep=...)`` keeps a single layer's input that way.
 """
 from __future__ import annotations
 
@@ -58,6 +62,54 @@ class _PresampledWeight(torch.autograd.Function):
         return grad_w_hat, None
 
 
+class _KeptLinear(torch.autograd.Function):
+    """y = x W^T with x kept as an 8-bit checkpoint; dW = dY^T x from it (gws_wgrad_act8)."""
+
+    @staticmethod
+    def forward(ctx, x, w, fmt):
+        rows = x.reshape(-1, x.shape[-1])
+        kept = binding.act8_save(rows, fmt) if ctx.needs_input_grad[1] else None
+        ctx.save_for_backward(w, None if kept is None else kept.buffer)
+        ctx.kept, ctx.x_shape = (rows.shape[0], rows.shape[1], fmt), x.shape
+        return torch.nn.functional.linear(x, w)
+
+    @staticmethod
+    def backward(ctx, grad_y):
+        w, buffer = ctx.saved_tensors
+        rows = grad_y.reshape(-1, grad_y.shape[-1])
+        grad_x = (rows @ w).view(ctx.x_shape) if ctx.needs_input_grad[0] else None
+        grad_w = binding.wgrad_act8(rows, binding.Act8(buffer, *ctx.kept)) if ctx.needs_input_grad[1] else None
+        return grad_x, grad_w, None
+
+
+class _GatedMLP(torch.autograd.Function):
+    """y = (act(x Wg^T) * (x Wu^T)) Wd^T.  Kept for the backward pass: x, x Wg^T and x Wu^T in the given format; the hidden activation is
+    formed again from them."""
+
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, activation, fmt):
+        rows = x.reshape(-1, x.shape[-1])
+        needed = any(ctx.needs_input_grad[:4])
+        h, saved = binding.gated_fwd(rows, w_gate, w_up, activation, save=fmt if needed else binding.SAVE_NONE)
+        if needed:
+            x_kept = rows if fmt == binding.SAVE_BF16 else binding.act8_save(rows, fmt).buffer
+            ctx.save_for_backward(x_kept, w_gate, w_up, w_down, saved.buffer)
+            ctx.kept, ctx.activation, ctx.x_shape = (rows.shape[0], rows.shape[1], w_gate.shape[0], fmt), activation, x.shape
+        return torch.nn.functional.linear(h, w_down).view(*x.shape[:-1], w_down.shape[0])
+
+    @staticmethod
+    def backward(ctx, grad_y):
+        x_kept, w_gate, w_up, w_down, kept = ctx.saved_tensors
+        m, k, n, fmt = ctx.kept
+        need_x, need_gate, need_up, need_down = ctx.needs_input_grad[:4]
+        rows = grad_y.reshape(m, w_down.shape[0])
+        x = x_kept if fmt == binding.SAVE_BF16 else binding.Act8(x_kept, m, k, fmt)
+        grad_x, grad_gate, grad_up, h = binding.gated_bwd(rows @ w_down, x, w_gate, w_up, binding.GatedSaved(kept, m, n, fmt), ctx.activation,
+                                                          want_h=need_down, want_grad_x=need_x, want_grad_w=need_gate or need_up)
+        return (grad_x.view(ctx.x_shape) if need_x else None, grad_gate if need_gate else None, grad_up if need_up else None,
+                rows.t() @ h if need_down else None, None, None)
+
+
 class GaussWSLinear(torch.nn.Module):
     """Linear layer trained with Gaussian weight sampling.
 
@@ -66,12 +118,16 @@ class GaussWSLinear(torch.nn.Module):
     (not per micro-batch) so that forward and backward of one update see the same noise and the next update a new one.
     ``lam`` > 0 adds this layer's term of Eq. 12 to the gradient of ``b_i``, once per update: the first backward pass
     after construction or :meth:`advance` carries it, so accumulating k micro-batches does not multiply lambda by k;
-    :meth:`bitwidth_loss` returns the term's value.
+    :meth:`bitwidth_loss` returns the term's value.  ``keep`` (``binding.ACT8_INT8`` or ``binding.ACT8_E4M3``) holds the layer's input
+    for the backward pass as an 8-bit checkpoint instead of in BF16.
     """
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True, group=(32, 32), b_init: float = 6.0,
-                 b_target: float = 4.0, lam: float = 0.0, user_seed: int = 0, layer_index: int = 0, device="cuda"):
+                 b_target: float = 4.0, lam: float = 0.0, user_seed: int = 0, layer_index: int = 0, device="cuda", keep: Optional[int] = None):
         super().__init__()
+        if keep not in (None, binding.ACT8_INT8, binding.ACT8_E4M3):
+            raise ValueError("gws: keep is None, ACT8_INT8 or ACT8_E4M3")
+        self.keep = keep
         self.in_features, self.out_features = in_features, out_features
         self.group, self.b_init, self.b_target, self.lam = tuple(group), float(b_init), float(b_target), float(lam)
         self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, dtype=torch.bfloat16, device=device))
@@ -105,7 +161,43 @@ class GaussWSLinear(torch.nn.Module):
         return binding.bitwidth_loss(self.bitwidth(), self.b_target)
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        return torch.nn.functional.linear(x, self.sampled_weight(), self.bias)
+        if self.keep is None:
+            return torch.nn.functional.linear(x, self.sampled_weight(), self.bias)
+        y = _KeptLinear.apply(x, self.sampled_weight(), self.keep)
+        return y if self.bias is None else y + self.bias
+
+
+class GaussWSGatedMLP(torch.nn.Module):
+    """Gated feed-forward block, y = (act(x Wg^T) * (x Wu^T)) Wd^T, with its three weights sampled.
+
+    ``gate``, ``up`` and ``down`` are GaussWSLinear layers without bias (``layer_index``, ``layer_index + 1`` and ``layer_index + 2``),
+    to be handed to a GaussWSSet like any other.  ``activation`` is ``binding.GATED_SILU``, ``GATED_GELU_TANH`` or ``GATED_RELU``.
+    ``keep`` says what the block holds for its backward pass: ``binding.ACT8_INT8`` (default) or ``ACT8_E4M3`` - one byte per element
+    of its input and of both projections - or ``SAVE_BF16``; the hidden activation is never held.
+    """
+
+    def __init__(self, features: int, hidden: int, activation: int = binding.GATED_SILU, keep: int = binding.ACT8_INT8, layer_index: int = 0, **layer):
+        super().__init__()
+        if keep not in (binding.ACT8_INT8, binding.ACT8_E4M3, binding.SAVE_BF16):
+            raise ValueError("gws: keep is ACT8_INT8, ACT8_E4M3 or SAVE_BF16")
+        if activation not in (binding.GATED_SILU, binding.GATED_GELU_TANH, binding.GATED_RELU):
+            raise ValueError("gws: unknown activation")
+        self.activation, self.keep = activation, keep
+        self.gate = GaussWSLinear(features, hidden, bias=False, layer_index=layer_index, **layer)
+        self.up = GaussWSLinear(features, hidden, bias=False, layer_index=layer_index + 1, **layer)
+        self.down = GaussWSLinear(hidden, features, bias=False, layer_index=layer_index + 2, **layer)
+
+    @property
+    def layers(self):
+        return [self.gate, self.up, self.down]
+
+    def advance(self) -> None:
+        """One gradient update has been applied (layers of a GaussWSSet are advanced by the set instead)."""
+        for layer in self.layers:
+            layer.advance()
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        return _GatedMLP.apply(x, self.gate.sampled_weight(), self.up.sampled_weight(), self.down.sampled_weight(), self.activation, self.keep)
 
 
 class GaussWSSet:
