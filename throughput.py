@@ -1,6 +1,6 @@
 """Throughput of the sampling pass on the other workload shapes of the paper (one JSON line each).
 
-    python throughput.py [gpt2] [gpt2_single] [stress] [square] [llama] [mx] [gemm] [issue] [compare] [module] [overhead] [--reps N] [--blocks B]
+    python throughput.py [gpt2] [gpt2_single] [stress] [square] [llama] [mx] [gemm] [issue] [compare] [module] [overhead] [ffn] [--reps N] [--blocks B]
 
 gpt2         all GPT2-124M linear weights, one group per row (and the same set with groups of 128)
 gpt2_single  one GPT2-124M MLP weight, both orientations
@@ -13,6 +13,9 @@ compare      forward pass with the method's noise against the same kernel shape 
              (the series "ours", "bm" and the DiffQ-style noise of the paper's forward benchmark), matrices of its range
 module       the sampling part of an update through the module wrappers: layer by layer against all layers at once (GaussWSSet)
 overhead     the three GEMMs of every linear layer for one micro-batch, with and without the sampling pass around them
+ffn          a training update of gated feed-forward blocks (2048 x 5632, 16384 tokens): the block module with 8-bit and with BF16
+             copies of its activations against three sampled linear layers and torch's activation and product, with the bytes held
+             between forward and backward
 issue        cycles per warp instruction of the instruction kinds the passes are made of, and of the passes' arithmetic
              without memory traffic (gws_issue_probe): the terms of the arithmetic ceiling of the backward pass
 
@@ -357,6 +360,71 @@ def run_overhead(reps: int, dev, n_blocks: int, tokens: int = 16384) -> dict:
     return line
 
 
+def run_ffn(reps: int, dev, n_blocks: int, tokens: int = 16384) -> list:
+    """Updates of a stack of gated feed-forward blocks: sample, forward, backward, finish_backward."""
+    from paper_2505_11170_b200.module import GaussWSGatedMLP, GaussWSSet
+
+    class Composed(torch.nn.Module):
+        """The same three layers, joined by torch operations (autograd holds the input, g, act(g), u and h in BF16)."""
+
+        def __init__(self, block):
+            super().__init__()
+            self.block = block
+            self.layers = block.layers
+
+        def forward(self, x):
+            g, u = self.block.gate(x), self.block.up(x)
+            return self.block.down(torch.nn.functional.silu(g) * u)
+
+    torch.manual_seed(0)
+    x = torch.randn(tokens, 2048, device=dev).to(torch.bfloat16)
+    grad_y = (torch.randn(tokens, 2048, device=dev) * 1e-3).to(torch.bfloat16)
+    lines = []
+    for name in ("int8", "e4m3", "bf16", "composed"):
+        keep = {"int8": gws.ACT8_INT8, "e4m3": gws.ACT8_E4M3}.get(name, gws.SAVE_BF16)
+        blocks = [GaussWSGatedMLP(2048, 5632, keep=keep, layer_index=3 * b, group=(1, 128), device=dev) for b in range(n_blocks)]
+        if name == "composed":
+            blocks = [Composed(b) for b in blocks]
+        sampler = GaussWSSet([layer for b in blocks for layer in b.layers])
+
+        def forward(sampler=sampler, blocks=blocks):
+            sampler.sample()
+            y = x
+            for b in blocks:
+                y = b(y)
+            return y
+
+        def update(sampler=sampler):
+            forward().backward(grad_y)
+            sampler.finish_backward()
+            for layer in sampler.layers:
+                layer.weight.grad = layer.b_i.grad = None
+            sampler.advance()
+
+        for _ in range(3):
+            update()
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated(dev)
+        y = forward()
+        held = torch.cuda.memory_allocated(dev) - before
+        del y
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        for _ in range(reps):
+            update()
+        stop.record()
+        torch.cuda.synchronize()
+        us = start.elapsed_time(stop) / reps * 1e3
+        flops = n_blocks * 18.0 * tokens * 2048 * 5632
+        line = {"workload": f"{n_blocks} gated blocks 2048 x 5632, {tokens} tokens, activations {name}", "us_per_update": round(us, 1),
+                "tflops": round(flops / us / 1e6, 1), "bytes_held_for_backward": int(held)}
+        print(json.dumps(line), flush=True)
+        lines.append(line)
+        del blocks, sampler, forward, update
+        torch.cuda.empty_cache()
+    return lines
+
+
 def main(argv=None) -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("which", nargs="*", default=["gpt2", "stress"])
@@ -387,6 +455,8 @@ def main(argv=None) -> None:
             run_gemm(args.reps, dev)
         elif w == "overhead":
             run_overhead(max(1, args.reps // 4), dev, args.blocks)
+        elif w == "ffn":
+            run_ffn(args.reps, dev, min(args.blocks, 4))
         elif w == "module":
             run_module(args.reps, dev, args.blocks)
         elif w == "issue":
