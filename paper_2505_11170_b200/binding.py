@@ -551,6 +551,7 @@ class Act8:
         return self.buffer[first:first + self.rows * groups].view(self.rows, groups)
 
 
+@functools.lru_cache(maxsize=1024)
 def _act8_bytes(rows: int, cols: int) -> int:
     """total_bytes of act8_layout."""
     groups = rows * -(-cols // 32)
@@ -630,7 +631,9 @@ def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None, stream=None) -> Act8:
     """BF16 [rows, cols] -> 8-bit checkpoint (``out`` is overwritten if given)."""
-    device = _device_of(x, None if out is None else out.buffer)
+    device = x.get_device() if out is None else _device_of(x, out.buffer)
+    if device < 0:
+        _require_cuda(x)
     if stream is not None:
         return _on_stream(stream, device, act8_save, x, fmt, out)
     x, p, ld = _bf16_rows(x, "x", read_by_map=False)
@@ -639,13 +642,17 @@ def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None,
         out = Act8._new(x, rows, cols, fmt)
     elif out.shape != (rows, cols) or out.fmt != fmt:
         raise ValueError("gws: out is a checkpoint of another shape or format")
-    _check(load_library().gws_act8_save(rows, cols, ld, fmt, p, out.buffer.data_ptr(), _raw_stream(device)))
+    code = (_lib or load_library()).gws_act8_save(rows, cols, ld, fmt, p, out.buffer.data_ptr(), _raw_stream(device))
+    if code:
+        _check(code)
     return out
 
 
 def act8_load(a: Act8, x: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """8-bit checkpoint -> BF16 [rows, cols] (written to ``x`` if given; its rows may be strided)."""
-    device = _device_of(a.buffer, x)
+    device = a.buffer.get_device() if x is None else _device_of(a.buffer, x)
+    if device < 0:
+        _require_cuda(a.buffer)
     if stream is not None:
         return _on_stream(stream, device, act8_load, a, x)
     rows, cols, ld = a.rows, a.cols, a.cols
@@ -656,7 +663,9 @@ def act8_load(a: Act8, x: Optional[torch.Tensor] = None, stream=None) -> torch.T
             raise ValueError("gws: x must be a BF16 [%d, %d] tensor whose rows are contiguous" % a.shape)
         if rows > 1:
             ld = x.stride(0)
-    _check(load_library().gws_act8_load(rows, cols, ld or 1, a.fmt, a.buffer.data_ptr(), x.data_ptr(), _raw_stream(device)))
+    code = (_lib or load_library()).gws_act8_load(rows, cols, ld or 1, a.fmt, a.buffer.data_ptr(), x.data_ptr(), _raw_stream(device))
+    if code:
+        _check(code)
     return x
 
 
@@ -677,8 +686,10 @@ def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = 
     grad_w = _bf16_out(grad_w, "grad_w", n, k, grad_y)
     nbytes = _wgrad_workspace(m, n, k, ld, device)
     ws, ws_p = _workspace(nbytes, grad_y)
-    _check(load_library().gws_wgrad_act8(m, n, k, x8.fmt, p, ld, x8.buffer.data_ptr(), grad_w.data_ptr(), k or 1, ws_p, nbytes, _addr(status),
-                                         _raw_stream(device)))
+    code = (_lib or load_library()).gws_wgrad_act8(m, n, k, x8.fmt, p, ld, x8.buffer.data_ptr(), grad_w.data_ptr(), k or 1, ws_p, nbytes, _addr(status),
+                                                   _raw_stream(device))
+    if code:
+        _check(code)
     return grad_w
 
 
@@ -727,6 +738,10 @@ def _gated_plan(m: int, n: int, k: int, ld_x: int, ld_w: int, ld_h: int, activat
 
 
 def _two_weights(w_gate: torch.Tensor, w_up: torch.Tensor, n: int, k: int):
+    if w_gate.dtype is _BF16 and w_up.dtype is _BF16 and w_gate.is_contiguous() and w_up.is_contiguous() and w_gate.shape == (n, k) == w_up.shape:
+        p_gate, p_up = w_gate.data_ptr(), w_up.data_ptr()
+        if not (p_gate | p_up) & 15:
+            return w_gate, w_up, p_gate, p_up, k or 1
     w_gate, p_gate, ld = _bf16_rows(w_gate, "w_gate", n, k)
     w_up, p_up, ld_up = _bf16_rows(w_up, "w_up", n, k)
     if ld_up != ld:                                       # one stride for both weights
@@ -755,7 +770,9 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
         saved = GatedSaved(x.new_empty(2 * GatedSaved._part(m, n, save), dtype=torch.uint8), m, n, save)
         p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, x)
-    _check(load_library().gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, _addr(status), _raw_stream(device)))
+    code = (_lib or load_library()).gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, _addr(status), _raw_stream(device))
+    if code:
+        _check(code)
     return h, saved
 
 
@@ -784,8 +801,10 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     h = _dense_like(grad_h, m, n) if want_h else None
     p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, grad_h)
-    _check(load_library().gws_gated_bwd(at, p_dh, p_x, p_gate, p_up, p_sg, p_su, _addr(grad_x), _addr(grad_wg), _addr(grad_wu),
-                                        _addr(h), ws_p, nbytes, _addr(status), _raw_stream(device)))
+    code = (_lib or load_library()).gws_gated_bwd(at, p_dh, p_x, p_gate, p_up, p_sg, p_su, _addr(grad_x), _addr(grad_wg), _addr(grad_wu),
+                                        _addr(h), ws_p, nbytes, _addr(status), _raw_stream(device))
+    if code:
+        _check(code)
     return grad_x, grad_wg, grad_wu, h
 
 

@@ -697,12 +697,13 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
     a[i] = part[i * BN];
     b[i] = MODE == kGated ? part[i * BN + BN / 2] : 0.0f;
   }
+#pragma unroll 4
   for (uint32_t k = 1; k < p.splits; ++k) {
-    part += stride;
+    const float* q = part + k * stride;
 #pragma unroll
     for (int i = 0; i < kJoinRows; ++i) {
-      a[i] += part[i * BN];
-      if (MODE == kGated) b[i] += part[i * BN + BN / 2];
+      a[i] += q[i * BN];
+      if (MODE == kGated) b[i] += q[i * BN + BN / 2];
     }
   }
 #pragma unroll
