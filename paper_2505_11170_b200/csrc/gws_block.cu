@@ -202,6 +202,7 @@ int64_t stages_of(int64_t len, int bn) { const int64_t per = kTcHalf * (bn == 25
 struct Tile {
   int cg, bn;                              // blocks per tile, columns of accumulator
   uint32_t m_tiles, n_tiles, whole, cut, splits, kb_split;
+  bool clustered;                          // the parts of a tile are the blocks of a cluster
 };
 
 // The tile, and the cut of the tiles that do not fill a wave, with the least estimated time, in SM cycles.  A tile takes a block its
@@ -220,27 +221,35 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int seg
     const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 67.0));
     const double epilogue = mode == kGated ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
     const double tile = std::max(kb * step, epilogue) + 100.0;
-    auto offer = [&](int64_t whole, int64_t splits, double cost) {
+    auto offer = [&](int64_t whole, int64_t splits, double cost, bool clustered) {
       if (best.cg != 0 && cost >= least) return;
       least = cost;
       const int64_t per = (kb + splits - 1) / splits;
       best = {kind.cg, kind.bn, static_cast<uint32_t>(mt), static_cast<uint32_t>(nt), static_cast<uint32_t>(whole), static_cast<uint32_t>(tiles - whole),
-              static_cast<uint32_t>(splits), static_cast<uint32_t>(per)};
+              static_cast<uint32_t>(splits), static_cast<uint32_t>(per), clustered};
     };
-    offer(tiles, 1, start + epilogue + std::ceil(static_cast<double>(tiles) / slots) * tile);
+    offer(tiles, 1, start + epilogue + std::ceil(static_cast<double>(tiles) / slots) * tile, false);
     const int64_t whole = tiles / slots * slots, cut = tiles - whole;
     for (int64_t splits = 2; cut > 0 && splits <= std::min<int64_t>(32, kb); ++splits) {
       const int64_t per = (kb + splits - 1) / splits;
       if ((kb + per - 1) / per != splits) continue;
       const double part = std::max(per * step, 5.0 * kind.bn + 400.0) + 100.0;
       offer(whole, splits, start + 5.0 * kind.bn + 400.0 + static_cast<double>(whole / slots) * tile + std::ceil(static_cast<double>(cut * splits) / slots) * part +
-                               4000.0 + 128.0 * kind.cg * kind.bn * cut * (8.0 * splits + 2.0) / 3400.0);
+                               5500.0 + 128.0 * kind.cg * kind.bn * cut * (8.0 * splits + 2.0) / 3400.0,
+            false);
+      // clusters of up to 4 blocks on 120 SMs, of up to 6 on 96: a cluster lives inside a group of some 18 SMs, and 16 clusters of 8 took two
+      // waves (1 token, 5632 x 2048: 17.5 us, 10.9 with 6)
+      if (kind.cg == 1 && mode != kGated && tiles * splits * 148 <= (splits <= 4 ? 120 : splits <= 6 ? 96 : 0) * sms)
+        offer(0, splits, start + part + 5.0 * kind.bn + 2400.0 + 40.0 * std::min<int64_t>(rows, 128), true);
     }
   }
   return best;
 }
 
-int64_t part_bytes(const Tile& t) { return round_up(static_cast<int64_t>(t.cut) * (t.splits > 1 ? t.splits : 0) * 128 * t.cg * t.bn * 4, 256); }
+int64_t part_bytes(const Tile& t) {
+  if (t.clustered) return 0;
+  return round_up(static_cast<int64_t>(t.cut) * (t.splits > 1 ? t.splits : 0) * 128 * t.cg * t.bn * 4, 256);
+}
 
 template <int CG, int BN, int MODE>
 int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStream_t s) {
@@ -255,8 +264,9 @@ int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStr
   }
   if (err != cudaSuccess) return gws::report_cuda(err, "shared memory of the block GEMM");
   const uint32_t work = args.whole + args.cut * args.splits, slots = static_cast<uint32_t>(sms / CG);
-  const int st = launch(k_tc<CG, BN, MODE>, std::min(work, slots) * CG, S::kThreads, S::kSmemBytes, CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
-  if (st != GWS_OK || args.cut == 0) return st;
+  const int st = launch(k_tc<CG, BN, MODE>, args.clustered ? work : std::min(work, slots) * CG, S::kThreads, S::kSmemBytes,
+                        args.clustered ? args.splits : CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
+  if (st != GWS_OK || args.cut == 0 || args.clustered) return st;
   constexpr uint32_t kWarps = (MODE == kGated ? BN / 64 : BN / 32) * (128 * CG / kJoinRows);       // per tile
   return launch(k_join<CG, BN, MODE>, args.cut * (kWarps / 8), 256, 0, 1, s, "join of a cut contraction", args);
 }
@@ -276,6 +286,7 @@ TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t len, int seg
   a.whole = t.whole;
   a.cut = t.cut;
   a.splits = t.splits;
+  a.clustered = t.clustered;
   a.tiles_per_out = t.m_tiles;
   a.len = static_cast<uint32_t>(len);
   a.kb_first = static_cast<uint32_t>(stages_of(len, t.bn));

@@ -18,6 +18,8 @@
 //
 // The tiles that do not fill a last wave of blocks (all of them, when there are few) have their contraction cut into `splits`
 // parts, each written as FP32; k_join adds the parts in a fixed order, so results do not depend on timing, and finishes the tile.
+// Where one wave holds all parts of all tiles, the parts of a tile are the blocks of a cluster instead, which add them through each
+// other's shared memory in the same launch.
 //
 // Every wait is bounded (about a second); a wait that runs out sets the status word, the roles of the block leave their loops,
 // the block gives its copies time to land, frees its tensor memory and returns.
@@ -40,6 +42,7 @@ constexpr long long kTcWaitCycles = 2000000000LL;
 struct TcArgs {
   uint32_t m_tiles, n_tiles;              // tiles along rows (all outputs), along columns
   uint32_t whole, cut, splits;            // tiles computed in one piece, and the rest, cut into `splits` parts
+  int32_t clustered;                      // the parts of a tile are the blocks of a cluster (CG = 1, no whole tiles, one part a block)
   uint32_t tiles_per_out;                 // kDw: row tiles of the first output
   uint32_t kb, kb_first, kb_split;        // stages of the contraction: all, of the first segment (kDx), of one part
   uint32_t len;                           // elements of the contraction (kDx: of each segment)
@@ -291,6 +294,8 @@ struct TcShape {
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
+constexpr uint32_t kPartRow = 128u * 4u + 16u;      // bytes between rows of a part in shared memory: eight lanes' 16 bytes in different banks
+
 // Codes of a checkpoint -> BF16 numbers, two at a time in packed BF16 arithmetic; every step is exact.
 // INT8: a code c = low - 128 s (its low 7 bits and its sign bit); with 0x43 above it the byte is a BF16 number, 128 + low without the
 // sign bit and 128 (1 + s) without the low bits, whose difference is c.  2 1/2 instructions a code against 3 3/4 through FP32.
@@ -402,8 +407,8 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k0 = 0;
     k1 = p.kb;
     if (t >= p.whole) {
-      const uint32_t split = (t - p.whole) / p.cut;
-      t -= split * p.cut;
+      const uint32_t split = p.clustered ? t % p.splits : (t - p.whole) / p.cut;
+      t = p.clustered ? t / p.splits : t - split * p.cut;
       k0 = split * p.kb_split;
       k1 = min(p.kb, k0 + p.kb_split);
     }
@@ -521,7 +526,17 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
       const bool second = kIsDw && mt >= p.tiles_per_out;
       const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + rank * 128u + quadrant * 32u;
-      if (t >= p.whole) {                     // a part of a contraction: FP32, joined by k_join
+      if (CG == 1 && MODE != kGated && p.clustered) {      // a part, into this block's shared memory: its copies and products are done
+#pragma unroll 1
+        for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
+          uint32_t v[32];
+          acc_load(acc + c * 32u, v);
+          acc_wait();
+          uint4* to = reinterpret_cast<uint4*>(smem + (quadrant * 32u + lane) * kPartRow + c * 128u);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+      } else if (t >= p.whole) {              // a part of a contraction: FP32, joined by k_join
         float* part = p.part + static_cast<int64_t>(t - p.whole) * (128 * CG * BN) + (rank * 128u + quadrant * 32u + lane) * BN;
 #pragma unroll 1
         for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
@@ -605,7 +620,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) bar_arrive(at_rank(smem_addr(&acc_empty[buf]), 0u));
+      if (lane == 0) bar_arrive(CG == 2 ? at_rank(smem_addr(&acc_empty[buf]), 0u) : smem_addr(&acc_empty[buf]));
     }
   } else if (MODE == kDw8 && warp >= 4u + S::kEpilogueWarps) {
     // Two teams of four warps take the stages in turn: one waits for codes while the other converts.
@@ -650,13 +665,48 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the tensor cores read shared memory through the async proxy
           __syncwarp();
-          if (lane == 0) bar_arrive(at_rank(smem_addr(&converted[s]), 0u));
+          if (lane == 0) bar_arrive(CG == 2 ? at_rank(smem_addr(&converted[s]), 0u) : smem_addr(&converted[s]));
           fetch(kb + 2u * kAhead, bytes[d]);
         }
       }
       it += k1 - k0;
     }
     if (!ok) failed = 1;
+  }
+  if (CG == 1 && MODE != kGated && p.clustered) {
+    // Every block of the cluster adds its share of the tile's rows, the parts in the order of the contraction; a warp takes a row, a
+    // lane four columns.
+    __syncthreads();
+    pair_sync();
+    const uint32_t per = (128u + p.splits - 1u) / p.splits, r1 = min(128u, (block_rank() + 1u) * per);
+    uint32_t mt, nt, k0, k1;
+    place(first, mt, nt, k0, k1);
+    const bool second = kIsDw && mt >= p.tiles_per_out;
+    const int64_t col = static_cast<int64_t>(nt) * BN + lane * 4u, row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * 128;
+    uint16_t* out = static_cast<uint16_t*>(p.out[second ? 1 : 0]);
+    for (uint32_t r = block_rank() * per + warp; r < r1 && row0 + r < p.rows; r += S::kThreads / 32u) {
+      const uint32_t at = smem_addr(smem) + r * kPartRow + lane * 16u;
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+      for (uint32_t k = 0; k < p.splits; ++k) {
+        float q[4];
+        asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(q[0]), "=f"(q[1]), "=f"(q[2]), "=f"(q[3]) : "r"(at_rank(at, k)) : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = k == 0 ? q[i] : v[i] + q[i];
+      }
+      uint16_t* to = out + (row0 + r) * p.ld_out + col;
+      const uint32_t lo = pack_bf16(v[0], v[1]), hi = pack_bf16(v[2], v[3]);
+      if (p.direct && col + 4 <= p.cols) {
+        *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+      } else {
+        if (col < p.cols) to[0] = static_cast<uint16_t>(lo);
+        if (col + 1 < p.cols) to[1] = static_cast<uint16_t>(lo >> 16);
+        if (col + 2 < p.cols) to[2] = static_cast<uint16_t>(hi);
+        if (col + 3 < p.cols) to[3] = static_cast<uint16_t>(hi >> 16);
+      }
+    }
+    __syncwarp();
+    pair_sync();                         // the other blocks have read this block's part
   }
   __syncthreads();
   if (failed) {                          // copies and products that were started get time to end before the memory is given up
