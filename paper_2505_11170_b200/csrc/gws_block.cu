@@ -206,8 +206,8 @@ struct Tile {
 };
 
 // The tile, and the cut of the tiles that do not fill a wave, with the least estimated time, in SM cycles.  A tile takes a block its
-// steps of 64 along the contraction, each the longest of the products (2 cycles a column), the operand bytes over the 67 a cycle that
-// an SM drew from L2 with all SMs busy, and the issue of a stage, but no less than its epilogue (two chunks of 32 columns at a time).
+// steps of 64 along the contraction, each the longest of the products (2 cycles a column), the operand bytes over the 67 (in pairs 77) a
+// cycle that an SM drew from L2 with all SMs busy, and the issue of a stage, but no less than its epilogue (two chunks of 32 columns at a time).
 // Joining costs a launch and the parts' way through memory (3400 bytes a cycle).  Measured on 2048 x 5632 (forward, us): 128 rows
 // {2, 128} 14.7, {1, 128} 11.3, {2, 256} 16.0; 512 rows 21.0, 26.6, 25.1; 1024 rows 35.2, 43.4, 35.8.
 Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int segments, int sms) {
@@ -218,7 +218,7 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int seg
     const int64_t width = mode == kGated ? kind.bn / 2 : kind.bn;
     const int64_t mt = outs * ((rows + 128 * kind.cg - 1) / (128 * kind.cg)), nt = (cols + width - 1) / width, tiles = mt * nt;
     const int64_t slots = kind.cg == 2 ? sms / 2 : sms, kb = segments * stages_of(len, kind.bn);
-    const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / 67.0));
+    const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / (kind.cg == 2 ? 77.0 : 67.0)));
     const double epilogue = mode == kGated ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
     const double tile = std::max(kb * step, epilogue) + 100.0;
     auto offer = [&](int64_t whole, int64_t splits, double cost, bool clustered) {
