@@ -106,16 +106,44 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, 
   return FMT == GWS_ACT8_INT8 ? encode4_int8(a, b, c, d, inv) : encode4_e4m3(a, b, c, d, inv);
 }
 
-// A whole group held by one thread.
+// max that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// A whole group held by one thread.  For INT8 nearly every group needs one FMA per element: a factor of 64 * 2^(127 - byte) fits a float
+// for bytes above 6, and only a largest magnitude of 255/128 or more of its power of two rounds up to 128.  The other groups (1 in 128
+// on smooth data, subnormal ones, and those that hold a NaN or infinity) bring their elements into that form first.
 template <int FMT>
 __device__ __forceinline__ uint32_t encode_group(const float (&v)[kGroup], V8& codes) {
-  uint32_t top = 0;
+  float most = fabsf(v[0]);
 #pragma unroll
-  for (int i = 0; i < kGroup; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  const uint32_t byte = scale_byte(top, FMT);
-  const float inv = inverse_scale_of(byte);
+  for (int i = 1; i < kGroup; ++i) most = max_nan(most, fabsf(v[i]));
+  const uint32_t top = __float_as_uint(most), byte = scale_byte(top, FMT);
+  if (FMT == GWS_ACT8_E4M3) {
+    const float inv = inverse_scale_of(byte);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) codes.x[i] = byte == kNanByte ? 0u : encode4<FMT>(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+    for (int i = 0; i < 8; ++i) codes.x[i] = byte == kNanByte ? 0u : encode4_e4m3(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+    return byte;
+  }
+  float x[kGroup], to64 = __uint_as_float((260u - byte) << 23);
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) x[i] = v[i];
+  if (byte < 7u || byte == kNanByte || (top & 0x7FFFFFu) >= 0x7F0000u) {
+    const float inv = inverse_scale_of(byte), lim = byte == kNanByte ? 0.0f : 127.0f / 64.0f;
+    to64 = 64.0f;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) x[i] = fminf(fmaxf(v[i] * inv, -lim), lim);      // a NaN becomes -0
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    uint32_t c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = __float_as_uint(__fmaf_rn(x[4 * i + e], to64, 12582912.0f));
+    codes.x[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+  }
   return byte;
 }
 

@@ -206,10 +206,18 @@ template <int ACT>
 __device__ __forceinline__ float sigmoid_arg(float g) {
   return ACT == GWS_GATED_SILU ? g : g * __fmaf_rn(kGeluLin * 0.044715f, g * g, kGeluLin);
 }
+// 1 / (1 + 2^(-z log2 e)): two special-function operations, which set the pace of the forward epilogue where the contraction is short, and
+// two others.  Both flush what is below 2^-126 to zero; an argument beyond the range gives 0 or 1.
+__device__ __forceinline__ float sigmoid(float z) {
+  float e, s;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + e));
+  return s;
+}
 template <int ACT>
 __device__ __forceinline__ float act_of(float g) {
   if (ACT == GWS_GATED_RELU) return g < 0.0f ? 0.0f : g;
-  return __fdividef(g, 1.0f + __expf(-sigmoid_arg<ACT>(g)));
+  return g * sigmoid(sigmoid_arg<ACT>(g));
 }
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
@@ -218,7 +226,7 @@ __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
     slope = g > 0.0f ? 1.0f : 0.0f;
     return;
   }
-  const float s = __fdividef(1.0f, 1.0f + __expf(-sigmoid_arg<ACT>(g)));
+  const float s = sigmoid(sigmoid_arg<ACT>(g));
   a = g * s;
   const float dz = ACT == GWS_GATED_SILU ? 1.0f : __fmaf_rn(3.0f * 0.044715f * kGeluLin, g * g, kGeluLin);
   slope = __fmaf_rn(a * (1.0f - s), dz, s);
