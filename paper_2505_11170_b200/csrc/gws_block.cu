@@ -301,11 +301,18 @@ TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t len, int seg
   return a;
 }
 
+// Elements that a store may take at once in BF16 rows `ld` apart (the second pointer may be null).
+int32_t widest(int64_t ld, const void* p, const void* q) {
+  for (int32_t v = 16; v > 1; v /= 2)
+    if (ld % v == 0 && on(p, static_cast<size_t>(v) * 2) && on(q, static_cast<size_t>(v) * 2)) return v;
+  return 1;
+}
+
 void set_out(TcArgs& a, void* out0, void* out1, int64_t ld) {
   a.out[0] = out0;
   a.out[1] = out1;
   a.ld_out = ld;
-  a.direct = ld % 16 == 0 && on(out0, 32) && on(out1, 32);
+  a.wide = widest(ld, out0, out1);
 }
 
 // Copies fill rows outside a matrix with zeros at a fraction of the speed of rows inside it (one token, 128-row boxes: 31 us
@@ -538,7 +545,7 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   } else if (saves) {
     args.save16[0] = static_cast<uint16_t*>(save_gate);
     args.save16[1] = static_cast<uint16_t*>(save_up);
-    args.save_direct = d.n % 16 == 0 && on(save_gate, 32) && on(save_up, 32);
+    args.save_wide = widest(d.n, save_gate, save_up);
   }
   CUtensorMap maps[4];
   if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, a_box(d.m))) != GWS_OK) return st;

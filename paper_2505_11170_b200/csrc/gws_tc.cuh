@@ -57,14 +57,14 @@ struct TcArgs {
   int64_t rows, cols;                     // of one output
   void* out[2];                           // BF16
   int64_t ld_out;
-  int32_t direct;                         // rows of `out` take 32-byte stores
+  int32_t wide;                           // elements a store to `out` may take: 1, 2, 4, 8, or 16 (32 bytes)
   float* part;                            // FP32 [splits][cut][128 * CG][BN]
   const uint8_t* scales;                  // kDw8: scale bytes of X, [tokens, scales_ld]
   int64_t scales_ld;
   int32_t x_format;
   int32_t box_tokens;                     // kDw, kDw8: tokens in a copy
   int32_t activation, save;               // kGated
-  int32_t save_direct;
+  int32_t save_wide;                      // the same for the BF16 copies
   Act8View save8[2];
   uint16_t* save16[2];                    // BF16 copies, [rows, cols]
   int* status;
@@ -232,11 +232,43 @@ __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
   slope = __fmaf_rn(a * (1.0f - s), dz, s);
 }
 
-// Writes a 32 x 32 block of BF16 held one row per lane (16 words of two columns each): 32-byte stores where the rows take
-// them, otherwise through shared memory so that the warp still writes one row at a time, side by side.
-__device__ __forceinline__ void store_block(uint16_t* out, int64_t ld, bool direct, int64_t row0, int64_t col0, int64_t rows, int64_t cols,
+// A 32 x 32 block of BF16 from shared memory (rows 17 words apart) to rows that take stores of V elements: a lane V columns, a warp V rows
+// at a time.
+template <uint32_t V>
+__device__ __forceinline__ void store_rows(uint16_t* p, int64_t ld, int64_t left, const uint32_t* staging, uint32_t lane) {
+  constexpr uint32_t kLanes = 32u / V, kBatch = V == 1u ? 8u : V == 2u ? 4u : 2u;
+  const uint32_t row = lane / kLanes, word = (lane % kLanes) * V / 2u;
+  const uint32_t* s = staging + row * 17u + word;
+  p += row * ld + (lane % kLanes) * V;
+#pragma unroll
+  for (uint32_t r = 0; r < 32u; r += V * kBatch) {
+    uint32_t v[kBatch][V == 1u ? 1u : V / 2u];
+#pragma unroll
+    for (uint32_t i = 0; i < kBatch; ++i) {
+      if constexpr (V == 1u) {
+        v[i][0] = reinterpret_cast<const uint16_t*>(s + (r + i) * 17u)[lane & 1u];
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < V / 2u; ++e) v[i][e] = s[(r + i * V) * 17u + e];
+      }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kBatch; ++i, p += V * ld) {
+      if (r + i * V + row >= left) continue;
+      if constexpr (V == 1u) *p = static_cast<uint16_t>(v[i][0]);
+      else if constexpr (V == 2u) *reinterpret_cast<uint32_t*>(p) = v[i][0];
+      else if constexpr (V == 4u) *reinterpret_cast<uint2*>(p) = make_uint2(v[i][0], v[i][1]);
+      else *reinterpret_cast<uint4*>(p) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+    }
+  }
+}
+
+// Writes a 32 x 32 block of BF16 held one row per lane (16 words of two columns each).  `wide`: elements that a store may take at once
+// (rows and base aligned to them).  16 of them: straight from the lanes.  Fewer, or a block that reaches past the width: through shared
+// memory, so that the warp still writes neighbouring columns of a row with neighbouring lanes.
+__device__ __forceinline__ void store_block(uint16_t* out, int64_t ld, int32_t wide, int64_t row0, int64_t col0, int64_t rows, int64_t cols,
                                             const uint32_t (&w)[16], uint32_t* staging, uint32_t lane) {
-  if (direct && col0 + 32 <= cols) {
+  if (wide == 16 && col0 + 32 <= cols) {
     if (row0 + lane < rows) {
       uint16_t* p = out + (row0 + lane) * ld + col0;
       V8 a, b;
@@ -250,22 +282,17 @@ __device__ __forceinline__ void store_block(uint16_t* out, int64_t ld, bool dire
 #pragma unroll
   for (int i = 0; i < 16; ++i) staging[lane * 17u + i] = w[i];
   __syncwarp();
-  const uint16_t* s = reinterpret_cast<const uint16_t*>(staging) + lane;
   const int64_t left = rows - row0;
-  uint16_t* p = out + row0 * ld + col0 + lane;
-  if (col0 + lane < cols) {
-    if (left >= 32) {
-#pragma unroll
-      for (uint32_t r = 0; r < 32u; r += 8u) {
-        uint16_t v[8];
-#pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i) v[i] = s[(r + i) * 34u];
-#pragma unroll
-        for (uint32_t i = 0; i < 8u; ++i, p += ld) *p = v[i];
-      }
-    } else {
-      for (int64_t r = 0; r < left; ++r, p += ld) *p = s[r * 34];
-    }
+  uint16_t* p = out + row0 * ld + col0;
+  if (col0 + 32 <= cols) {
+    if (wide >= 8) store_rows<8>(p, ld, left, staging, lane);
+    else if (wide == 4) store_rows<4>(p, ld, left, staging, lane);
+    else if (wide == 2) store_rows<2>(p, ld, left, staging, lane);
+    else store_rows<1>(p, ld, left, staging, lane);
+  } else if (col0 + lane < cols) {
+    const uint16_t* s = reinterpret_cast<const uint16_t*>(staging) + lane;
+    const int64_t n = left < 32 ? left : 32;
+    for (int64_t r = 0; r < n; ++r) p[r * ld + lane] = s[r * 34];
   }
   __syncwarp();
 }
@@ -576,14 +603,14 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           if (p.activation == GWS_GATED_SILU) gate_block<GWS_GATED_SILU>(g, u, w);
           else if (p.activation == GWS_GATED_GELU_TANH) gate_block<GWS_GATED_GELU_TANH>(g, u, w);
           else gate_block<GWS_GATED_RELU>(g, u, w);
-          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
           if (p.save == GWS_SAVE_BF16) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
-            store_block(p.save16[0], p.cols, p.save_direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+            store_block(p.save16[0], p.cols, p.save_wide, row0, col0, p.rows, p.cols, w, stage, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
-            store_block(p.save16[1], p.cols, p.save_direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+            store_block(p.save16[1], p.cols, p.save_wide, row0, col0, p.rows, p.cols, w, stage, lane);
           } else if (p.save != GWS_SAVE_NONE && row0 + lane < p.rows) {
             // columns past the width are products with rows of zeros: zero codes, as the layout wants them
             const int64_t row = row0 + lane;
@@ -628,7 +655,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           if (col0 >= p.cols) continue;
 #pragma unroll
           for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-          store_block(out, p.ld_out, p.direct != 0, row0, col0, p.rows, p.cols, w, stage, lane);
+          store_block(out, p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -709,7 +736,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       }
       uint16_t* to = out + (row0 + r) * p.ld_out + col;
       const uint32_t lo = pack_bf16(v[0], v[1]), hi = pack_bf16(v[2], v[3]);
-      if (p.direct && col + 4 <= p.cols) {
+      if (p.wide >= 4 && col + 4 <= p.cols) {
         *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
       } else {
         if (col < p.cols) to[0] = static_cast<uint16_t>(lo);
