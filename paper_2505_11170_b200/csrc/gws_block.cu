@@ -157,34 +157,50 @@ bool in_place(int64_t rows, int64_t ld) { return rows <= 1 || ld % 8 == 0; }
 int64_t packed_ld(int64_t cols) { return round_up(cols, kGroup); }
 int64_t packed_bytes(int64_t rows, int64_t cols) { return round_up(rows * packed_ld(cols) * 2, 256); }
 
-// Brings those of up to three matrices that need it into the workspace, one after the other from `to`, in one launch.
-int realign(std::initializer_list<Mat*> mats, char* to, cudaStream_t s) {
-  Moves m;
-  std::memset(&m, 0, sizeof m);
+// What has to be made ready before a GEMM of a call: matrices to copy, a checkpoint to restore.
+struct Ready {
+  Prep prep;
   int n = 0;
-  int64_t threads = 0;
-  for (Mat* a : mats) {
-    if (in_place(a->rows, a->ld)) {
-      a->ld = round_up(a->rows <= 1 ? a->cols : a->ld, 8);
-      continue;
+  Ready() { std::memset(&prep, 0, sizeof prep); }
+  // `to`: room of packed_bytes(a) in the workspace, used if the matrix cannot be read in place.
+  void align(Mat& a, void* to) {
+    if (in_place(a.rows, a.ld)) {
+      a.ld = round_up(a.rows <= 1 ? a.cols : a.ld, 8);
+      return;
     }
-    const int64_t ld = packed_ld(a->cols);
-    m.from[n] = static_cast<const uint16_t*>(a->p);
-    m.to[n] = reinterpret_cast<uint16_t*>(to);
-    m.ld_from[n] = a->ld;
-    m.cols[n] = a->cols;
-    m.per_row[n] = static_cast<uint32_t>(ld / 8);
-    threads += a->rows * (ld / 8);
-    m.end[n++] = threads;
-    a->p = to;
-    a->ld = ld;
-    to += packed_bytes(a->rows, a->cols);
+    const int64_t ld = packed_ld(a.cols);
+    prep.from[n] = static_cast<const uint16_t*>(a.p);
+    prep.to[n] = static_cast<uint16_t*>(to);
+    prep.ld_from[n] = a.ld;
+    prep.cols[n] = a.cols;
+    prep.per_row[n] = static_cast<uint32_t>(ld / 8);
+    const int64_t end = (n > 0 ? prep.end[n - 1] : 0) + a.rows * (ld / 8);
+    for (int i = n; i < 3; ++i) prep.end[i] = end;
+    ++n;
+    a.p = to;
+    a.ld = ld;
   }
-  if (n == 0) return GWS_OK;
-  for (int i = n; i < 3; ++i) m.end[i] = threads;
-  if (threads / kJobs >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
-  return launch(k_realign, blocks_for(threads, kJobs), kJobs, 0, 1, s, "row alignment kernel", m);
-}
+  // The checkpoint's matrix, in `to`.
+  Mat restore(const Act8View& kept, int format, int64_t rows, int64_t cols, void* to) {
+    prep.kept = kept;
+    prep.format = format;
+    prep.restored = static_cast<uint16_t*>(to);
+    prep.groups = rows * (kept.ld / kGroup);
+    return {to, rows, cols, kept.ld};
+  }
+  int64_t blocks() {                     // GWS_ERR_LIMIT if there are too many for a launch
+    const int64_t moves = (prep.end[2] + kJobs - 1) / kJobs, restores = (prep.groups + kJobs - 1) / kJobs;
+    if (moves + restores >= 0x3FFFFFFFLL) return GWS_ERR_LIMIT;
+    prep.move_blocks = static_cast<uint32_t>(moves);
+    prep.restore_blocks = static_cast<uint32_t>(restores);
+    return moves + restores;
+  }
+  int run(cudaStream_t s) {
+    const int64_t grid = blocks();
+    if (grid <= 0) return static_cast<int>(grid);
+    return launch(k_prepare, static_cast<unsigned>(grid), kJobs, 0, 1, s, "operand preparation kernel", prep);
+  }
+};
 
 // ---- choice of tile --------------------------------------------------------------------------------------------------------
 int sm_count() {
@@ -329,18 +345,10 @@ bool converts_inside(int64_t tokens, int64_t rows, int64_t cols, int outs) {
   return static_cast<double>(outs) * static_cast<double>(tokens) * static_cast<double>(rows) * static_cast<double>(cols) < 8e9;
 }
 
-// X: a BF16 matrix, or a checkpoint of the same shape (x8, format), for which `restored` is room in the workspace where
-// converts_inside says so.
-int run_dw(const Mat& a0, const Mat* a1, Mat x, const Act8View* x8, int format, void* restored, void* out0, void* out1, int64_t ld_out, void* part, int* status,
+// X: a BF16 matrix, or a checkpoint of the same shape (x8, format) to be converted inside.
+int run_dw(const Mat& a0, const Mat* a1, const Mat& x, const Act8View* x8, int format, void* out0, void* out1, int64_t ld_out, void* part, int* status,
            int sms, cudaStream_t s) {
   const int outs = a1 != nullptr ? 2 : 1;
-  if (x8 != nullptr && !converts_inside(a0.rows, a0.cols, x.cols, outs)) {
-    x.p = restored;
-    x.ld = packed_ld(x.cols);
-    const int st = launch_act8(false, format, restored, x.ld, *x8, x.rows, x.ld, s);
-    if (st != GWS_OK) return st;
-    x8 = nullptr;
-  }
   const Tile t = choose(kDw, a0.cols, x.cols, outs, a0.rows, 1, sms);
   TcArgs args = base_args(t, a0.cols, x.cols, a0.rows, 1, status);
   args.tiles_per_out = t.m_tiles / outs;
@@ -411,16 +419,19 @@ int64_t forward_copies(const gws_gated_desc* d) {
 int64_t forward_bytes(const gws_gated_desc* d, int sms) { return forward_copies(d) + part_bytes(choose(kGated, d->m, d->n, 1, d->k, 1, sms)); }
 
 template <int SAVE, int ACT>
-int launch_pre(const PreArgs& p, bool fast, cudaStream_t s) {
+int launch_pre(const PreArgs& p, Ready& ready, bool fast, cudaStream_t s) {
   const char* what = "gated backward, element-wise part";
-  if (fast) return launch(k_gated_pre<SAVE, ACT>, blocks_for(p.groups, kJobs), kJobs, 0, 1, s, what, p);
-  return launch(k_gated_pre_any<SAVE, ACT>, blocks_for(p.rows * ((p.per_row + 7) / 8), 8), kJobs, 0, 1, s, what, p);
+  const int64_t first = ready.blocks(), items = fast ? p.groups : p.rows * ((p.per_row + 7) / 8), per = fast ? kJobs : 8;
+  if (first < 0) return static_cast<int>(first);
+  if ((items + per - 1) / per >= 0x3FFFFFFFLL) return GWS_ERR_LIMIT;
+  const unsigned grid = static_cast<unsigned>(first) + blocks_for(items, per);
+  return launch(fast ? k_gated_pre<SAVE, ACT> : k_gated_pre_any<SAVE, ACT>, grid, kJobs, 0, 1, s, what, p, ready.prep);
 }
 template <int SAVE>
-int launch_pre_act(const PreArgs& p, int act, bool fast, cudaStream_t s) {
-  if (act == GWS_GATED_SILU) return launch_pre<SAVE, GWS_GATED_SILU>(p, fast, s);
-  if (act == GWS_GATED_GELU_TANH) return launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, fast, s);
-  return launch_pre<SAVE, GWS_GATED_RELU>(p, fast, s);
+int launch_pre_act(const PreArgs& p, Ready& ready, int act, bool fast, cudaStream_t s) {
+  if (act == GWS_GATED_SILU) return launch_pre<SAVE, GWS_GATED_SILU>(p, ready, fast, s);
+  if (act == GWS_GATED_GELU_TANH) return launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, ready, fast, s);
+  return launch_pre<SAVE, GWS_GATED_RELU>(p, ready, fast, s);
 }
 
 bool workspace_ok(const void* p, size_t have, int64_t need) { return need == 0 || (p != nullptr && on(p, 256) && have >= static_cast<size_t>(need)); }
@@ -483,14 +494,18 @@ int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad
   if (clash({rows_of(grad_w, n, k, ld_w), {workspace, need}}, {rows_of(grad_y, m, n, ld_y), {x8, act8_total(m, k)}})) return GWS_ERR_ALIAS;
   if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
-  Mat y{grad_y, m, n, ld_y};
-  const bool moved = !in_place(m, ld_y);
-  st = realign({&y}, ws, s);
-  if (st != GWS_OK) return st;
-  const Act8View x = act8_view(x8, m, k);
-  if (moved) ws += packed_bytes(m, n);
-  char* part = ws + (converts_inside(m, n, k, 1) ? 0 : packed_bytes(m, k));
-  return run_dw(y, nullptr, Mat{nullptr, m, k, 0}, &x, format, ws, grad_w, nullptr, ld_w, part, status, sm_count(), s);
+  const Act8View kept = act8_view(x8, m, k);
+  Ready ready;
+  Mat y{grad_y, m, n, ld_y}, x{nullptr, m, k, 0};
+  ready.align(y, ws);
+  if (!in_place(m, ld_y)) ws += packed_bytes(m, n);
+  const bool inside = converts_inside(m, n, k, 1);
+  if (!inside) {
+    x = ready.restore(kept, format, m, k, ws);
+    ws += packed_bytes(m, k);
+  }
+  if ((st = ready.run(s)) != GWS_OK) return st;
+  return run_dw(y, nullptr, x, inside ? &kept : nullptr, format, grad_w, nullptr, ld_w, ws, status, sm_count(), s);
 }
 
 int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward) {
@@ -530,7 +545,14 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
     return GWS_ERR_ALIAS;
   if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
   Mat mx{x, d.m, d.k, d.ld_x}, mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
-  if ((st = realign({&mx, &mg, &mu}, static_cast<char*>(workspace), s)) != GWS_OK) return st;
+  Ready ready;
+  char* ws = static_cast<char*>(workspace);
+  ready.align(mx, ws);
+  if (moves_x) ws += packed_bytes(d.m, d.k);
+  ready.align(mg, ws);
+  if (moves_w) ws += packed_bytes(d.n, d.k);
+  ready.align(mu, ws);
+  if ((st = ready.run(s)) != GWS_OK) return st;
 
   const Tile t = choose(kGated, d.m, d.n, 1, d.k, 1, sms);
   TcArgs args = base_args(t, d.m, d.n, d.k, 1, status);
@@ -609,19 +631,26 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   p.cols = d.n;
   p.per_row = static_cast<uint32_t>(act8_ld(d.n) / kGroup);
   p.groups = d.m * p.per_row;
-  if (p.groups / 8 >= 0x7FFFFFFFLL) return GWS_ERR_LIMIT;
   // A thread with a group of its own needs some 75,000 groups to fill the GPU; below that its 32 elements in a row are all latency, and
   // the form with eight to a lane takes over (33 x 2048: 5.4 -> 3.5 us).
   const bool fast = p.groups >= 148 * 512 && whole_groups(grad_h, d.n, p.ld_grad_h) && on(h_out, 32) && (saved8 || (on(save_gate, 32) && on(save_up, 32)));
-  st = d.save_format == GWS_ACT8_INT8   ? launch_pre_act<GWS_ACT8_INT8>(p, d.activation, fast, s)
-       : d.save_format == GWS_ACT8_E4M3 ? launch_pre_act<GWS_ACT8_E4M3>(p, d.activation, fast, s)
-                                        : launch_pre_act<GWS_SAVE_BF16>(p, d.activation, fast, s);
+  Ready ready;
+  Mat mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w}, mx{x, d.m, d.k, d.ld_x};
+  const Act8View kept_x = act8_view(x, d.m, d.k);
+  const bool inside = x8 && converts_inside(d.m, d.n, d.k, 2);
+  if (wants_dx) {
+    ready.align(mg, ws + l.w_gate);
+    ready.align(mu, ws + l.w_up);
+  }
+  if (wants_dw && x8 && !inside) mx = ready.restore(kept_x, d.x_format, d.m, d.k, ws + l.x);
+  if (wants_dw && !x8) ready.align(mx, ws + l.x);
+  st = d.save_format == GWS_ACT8_INT8   ? launch_pre_act<GWS_ACT8_INT8>(p, ready, d.activation, fast, s)
+       : d.save_format == GWS_ACT8_E4M3 ? launch_pre_act<GWS_ACT8_E4M3>(p, ready, d.activation, fast, s)
+                                        : launch_pre_act<GWS_SAVE_BF16>(p, ready, d.activation, fast, s);
   if (st != GWS_OK) return st;
   const Mat dg{p.grad_gate, d.m, d.n, p.ld}, du{p.grad_up, d.m, d.n, p.ld};
 
   if (wants_dx) {
-    Mat mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w};
-    if ((st = realign({&mg, &mu}, ws + l.w_gate, s)) != GWS_OK) return st;
     const Tile t = choose(kDx, d.m, d.k, 1, d.n, 2, sms);
     TcArgs args = base_args(t, d.m, d.k, d.n, 2, status);
     args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
@@ -633,12 +662,7 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
       return st;
     if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
   }
-  if (wants_dw) {
-    Mat mx{x, d.m, d.k, d.ld_x};
-    const Act8View kept_x = act8_view(x, d.m, d.k);
-    if (!x8 && (st = realign({&mx}, ws + l.x, s)) != GWS_OK) return st;
-    return run_dw(dg, &du, mx, x8 ? &kept_x : nullptr, d.x_format, ws + l.x, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
-  }
+  if (wants_dw) return run_dw(dg, &du, mx, inside ? &kept_x : nullptr, d.x_format, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
   return GWS_OK;
 }
 

@@ -561,7 +561,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       uint32_t mt, nt, k0, k1;
       place(t, mt, nt, k0, k1);
       const uint32_t buf = n & 1u;
-      if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) { failed = 1; break; }
+      if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) {
+        failed = 1;
+        // the other warp of these rows may have seen the tile complete and wait for this one below
+        if (MODE == kGated) asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
+        break;
+      }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
       const bool second = kIsDw && mt >= p.tiles_per_out;
@@ -631,6 +636,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           // The two warps that share these rows meet; one writes the gate's, the other the up projection's.  A warp that fills the same
           // buffer again has passed the meeting of the tile between, and so has the other one's store.
           asm volatile("bar.sync %0, 64;" ::"r"(quadrant + 1u) : "memory");
+          if (__any_sync(0xFFFFFFFFu, failed != 0)) break;
           const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (BN / 64);
           if (row < p.rows) {
             uint8_t* to = p.save8[half].scales + row * ld + g0;
@@ -827,7 +833,7 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
 }
 
 // ---- the element-wise part of the backward pass ------------------------------------------------------------------------------
-// From dh and the saved g, u:  dg = dh u act'(g),  du = dh act(g),  and h = act(g) u for the next layer's weight gradient.  dg and
+// In one launch with what the products after it need made ready (prepare).  From dh and the saved g, u:  dg = dh u act'(g),  du = dh act(g),  and h = act(g) u for the next layer's weight gradient.  dg and
 // du are rounded to BF16 because the tensor cores take them in that form; their sums dx and dW are FP32 again.
 struct PreArgs {
   const uint16_t* grad_h;
@@ -844,9 +850,10 @@ struct PreArgs {
 // Memory-bound, one pass: 2 + 2 (1 + 1/32) bytes in, 4 or 6 bytes out per element.  A thread takes a group of 32 columns, so that a
 // scale is read once.  16384 x 5632 from INT8, with h: 135 us, 6.9 TB/s of 10.06 bytes per element.
 template <int SAVE, int ACT>
-__global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreArgs p) {
+__global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreArgs p, const __grid_constant__ Prep m) {
   after_previous();
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (prepare(m)) return;
+  const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks - m.restore_blocks) * 256 + threadIdx.x;
   if (t >= p.groups) return;
   int64_t at_dh = t * kGroup;
   if (p.ld_grad_h != p.cols) {
@@ -908,11 +915,12 @@ __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreAr
 // eight elements, or back, in shared memory: 2047 x 2729 from INT8 with h in 13 us (4.3 TB/s), with an element of each group to a lane
 // 23 us.
 template <int SAVE, int ACT>
-__global__ void __launch_bounds__(256) k_gated_pre_any(const __grid_constant__ PreArgs p) {
+__global__ void __launch_bounds__(256) k_gated_pre_any(const __grid_constant__ PreArgs p, const __grid_constant__ Prep m) {
   after_previous();
+  if (prepare(m)) return;
   __shared__ uint4 turn[8][32];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, runs_per_row = (p.per_row + 7u) / 8u;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 8 + warp, row = quotient(t, runs_per_row);
+  const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks - m.restore_blocks) * 8 + warp, row = quotient(t, runs_per_row);
   if (row >= p.rows) return;
   const int64_t run = (t - row * runs_per_row) * 256, col = run + lane * 8;
   uint16_t* side = reinterpret_cast<uint16_t*>(turn[warp]) + lane;
