@@ -583,7 +583,7 @@ def _device_of(*tensors: Optional[torch.Tensor]) -> int:
 
 
 def _bf16_rows(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None, read_by_map: bool = True):
-    """A BF16 matrix as the library takes it: (tensor, its address, its row stride).  Whatever its strides cannot say (columns
+    """A BF16 matrix as the library takes it: (tensor, its address, its row stride, rows, columns).  Whatever its strides cannot say (columns
     apart, rows that overlap, a base the tensor maps refuse) is copied."""
     if t.dtype is not _BF16 or t.dim() != 2:
         raise ValueError("gws: %s must be a 2-D BF16 tensor" % name)
@@ -600,19 +600,19 @@ def _bf16_rows(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Opt
     if read_by_map and p & 15 and (r <= 1 or ld % 8 == 0):
         t = t.clone(memory_format=torch.contiguous_format)
         p, ld = t.data_ptr(), c
-    return t, p, ld or 1
+    return t, p, ld or 1, r, c
 
 
 def _bf16_out(t: Optional[torch.Tensor], name: str, rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
     if t is None:
-        return like.new_empty((rows, cols))
+        return like.new_empty(rows, cols)
     if t.dtype is not _BF16 or tuple(t.shape) != (rows, cols) or not t.is_contiguous():
         raise ValueError("gws: %s must be a contiguous BF16 [%d, %d] tensor" % (name, rows, cols))
     return t
 
 
 def _dense_like(t: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
-    return torch.empty_like(t) if t.is_contiguous() else t.new_empty((rows, cols))
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(rows, cols)
 
 
 def _workspace(nbytes: int, like: torch.Tensor):
@@ -636,8 +636,7 @@ def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None,
         _require_cuda(x)
     if stream is not None:
         return _on_stream(stream, device, act8_save, x, fmt, out)
-    x, p, ld = _bf16_rows(x, "x", read_by_map=False)
-    rows, cols = x.shape
+    x, p, ld, rows, cols = _bf16_rows(x, "x", read_by_map=False)
     if out is None:
         out = Act8._new(x, rows, cols, fmt)
     elif out.shape != (rows, cols) or out.fmt != fmt:
@@ -657,7 +656,7 @@ def act8_load(a: Act8, x: Optional[torch.Tensor] = None, stream=None) -> torch.T
         return _on_stream(stream, device, act8_load, a, x)
     rows, cols, ld = a.rows, a.cols, a.cols
     if x is None:
-        x = a.buffer.new_empty((rows, cols), dtype=_BF16)
+        x = a.buffer.new_empty(rows, cols, dtype=_BF16)
     else:
         if x.dtype is not _BF16 or tuple(x.shape) != a.shape or (x.numel() and ((cols > 1 and x.stride(1) != 1) or (rows > 1 and x.stride(0) < cols))):
             raise ValueError("gws: x must be a BF16 [%d, %d] tensor whose rows are contiguous" % a.shape)
@@ -681,8 +680,7 @@ def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = 
     if stream is not None:
         return _on_stream(stream, device, wgrad_act8, grad_y, x8, grad_w, status)
     m, k = x8.rows, x8.cols
-    grad_y, p, ld = _bf16_rows(grad_y, "grad_y", m)
-    n = grad_y.shape[1]
+    grad_y, p, ld, _, n = _bf16_rows(grad_y, "grad_y", m)
     grad_w = _bf16_out(grad_w, "grad_w", n, k, grad_y)
     nbytes = _wgrad_workspace(m, n, k, ld, device)
     ws, ws_p = _workspace(nbytes, grad_y)
@@ -742,11 +740,11 @@ def _two_weights(w_gate: torch.Tensor, w_up: torch.Tensor, n: int, k: int):
         p_gate, p_up = w_gate.data_ptr(), w_up.data_ptr()
         if not (p_gate | p_up) & 15:
             return w_gate, w_up, p_gate, p_up, k or 1
-    w_gate, p_gate, ld = _bf16_rows(w_gate, "w_gate", n, k)
-    w_up, p_up, ld_up = _bf16_rows(w_up, "w_up", n, k)
+    w_gate, p_gate, ld, _, _ = _bf16_rows(w_gate, "w_gate", n, k)
+    w_up, p_up, ld_up, _, _ = _bf16_rows(w_up, "w_up", n, k)
     if ld_up != ld:                                       # one stride for both weights
-        w_gate, p_gate, ld = _bf16_rows(w_gate.contiguous(), "w_gate", n, k)
-        w_up, p_up, _ = _bf16_rows(w_up.contiguous(), "w_up", n, k)
+        w_gate, p_gate, ld, _, _ = _bf16_rows(w_gate.contiguous(), "w_gate", n, k)
+        w_up, p_up, _, _, _ = _bf16_rows(w_up.contiguous(), "w_up", n, k)
     return w_gate, w_up, p_gate, p_up, ld
 
 
@@ -757,8 +755,7 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
     device = _device_of(x, w_gate, w_up, h, status)
     if stream is not None:
         return _on_stream(stream, device, gated_fwd, x, w_gate, w_up, activation, save, h, status)
-    x, p_x, ld_x = _bf16_rows(x, "x")
-    m, k = x.shape
+    x, p_x, ld_x, m, k = _bf16_rows(x, "x")
     n = w_gate.shape[0]
     w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
     if save not in (ACT8_INT8, ACT8_E4M3, SAVE_BF16, SAVE_NONE):
@@ -786,17 +783,17 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
         return _on_stream(stream, device, gated_bwd, grad_h, x, w_gate, w_up, saved, activation, want_h, want_grad_x, want_grad_w, status)
     m, k = x.shape
     n = w_gate.shape[0]
-    grad_h, p_dh, ld_h = _bf16_rows(grad_h, "grad_h", m, n, read_by_map=False)
+    grad_h, p_dh, ld_h, _, _ = _bf16_rows(grad_h, "grad_h", m, n, read_by_map=False)
     if kept_x:
         x_t, p_x, ld_x, x_format = x.buffer, x.buffer.data_ptr(), k or 1, x.fmt
     else:
-        x_t, p_x, ld_x = _bf16_rows(x, "x")
+        x_t, p_x, ld_x, _, _ = _bf16_rows(x, "x")
         x_format = SAVE_BF16
     w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
     if saved.m != m or saved.n != n:
         raise ValueError("gws: the kept projections are (%d, %d), not (%d, %d)" % (saved.m, saved.n, m, n))
     _, at, nbytes = _gated_plan(m, n, k, ld_x, ld_w, ld_h, activation, saved.fmt, x_format, 1, device)
-    grad_x = (grad_h.new_empty((m, k)) if kept_x else _dense_like(x_t, m, k)) if want_grad_x else None
+    grad_x = (grad_h.new_empty(m, k) if kept_x else _dense_like(x_t, m, k)) if want_grad_x else None
     grad_wg, grad_wu = (_dense_like(w_gate, n, k), _dense_like(w_gate, n, k)) if want_grad_w else (None, None)
     h = _dense_like(grad_h, m, n) if want_h else None
     p_sg, p_su = saved._addresses()
