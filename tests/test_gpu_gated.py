@@ -246,3 +246,55 @@ def test_on_another_stream_than_the_current_one():
     noise = [torch.full((1 << 20,), 3, dtype=torch.uint8, device=DEV) for _ in range(40)]
     side.synchronize()
     assert all(torch.equal(p, q) for outs in got for p, q in zip(outs, want)) and len(noise) == 40
+
+
+# sizes that between them take every tile (one block of 128 x 128, a pair of 256 x 128 and of 256 x 256), in one wave and in several, for each
+# of the three products whole, cut and joined, cut in a cluster, and whole but for a cut last wave
+TILINGS = [(41, 89, 1076), (10781, 73, 68), (772, 1416, 276), (48, 66, 412), (9722, 235, 1350), (1404, 2389, 260), (32, 312, 89), (7448, 79, 526),
+           (170, 4024, 195), (3254, 1779, 686), (6749, 1685, 668), (1487, 90, 139), (34, 3895, 268), (8874, 152, 69), (5522, 3570, 264), (4548, 1834, 1242),
+           (2530, 136, 910), (15024, 1213, 192), (19150, 128, 2048)]
+
+
+@pytest.mark.parametrize("m,n,k", TILINGS)
+def test_every_way_to_tile(m, n, k):
+    test_forward(gws.GATED_SILU, m, n, k)
+    test_what_forward_keeps(gws.ACT8_INT8, m, n, k)
+    test_backward(gws.GATED_SILU, gws.ACT8_INT8, m, n, k)
+
+
+def test_a_captured_step_replays_to_the_same_bits():
+    x, wg, wu, grad_h = _problem(300, 520, 263)                 # copies of unaligned rows, cut contractions: several kernels a call
+
+    def step():
+        x8 = gws.act8_save(x)
+        h, saved = gws.gated_fwd(x, wg, wu, save=gws.ACT8_INT8)
+        return (gws.act8_load(x8), h, *gws.gated_bwd(grad_h, x8, wg, wu, saved, want_h=True), gws.wgrad_act8(grad_h, x8))
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = step()
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_many_steps_in_a_row_without_waiting_give_the_same_bits():
+    # kernels of consecutive calls overlap at their ends; outputs and workspaces come from memory that earlier calls still use
+    x, wg, wu, grad_h = _problem(700, 1000, 520)
+    outs = []
+    for _ in range(60):
+        h, saved = gws.gated_fwd(x, wg, wu, save=gws.ACT8_E4M3)
+        outs.append((h, *gws.gated_bwd(grad_h, gws.act8_save(x, gws.ACT8_E4M3), wg, wu, saved, want_h=True)))
+        if len(outs) > 4:
+            del outs[1]
+    first = outs[0]
+    assert all(torch.equal(p, q) for o in outs for p, q in zip(o, first))
