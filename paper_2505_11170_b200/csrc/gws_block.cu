@@ -219,6 +219,7 @@ struct Tile {
   int cg, bn;                              // blocks per tile, columns of accumulator
   uint32_t m_tiles, n_tiles, whole, cut, splits, kb_split;
   bool clustered;                          // the parts of a tile are the blocks of a cluster
+  double cost;                             // estimated cycles
 };
 
 // The tile, and the cut of the tiles that do not fill a wave, with the least estimated time, in SM cycles.  A tile takes a block its
@@ -234,7 +235,8 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int seg
     const int64_t width = mode == kGated ? kind.bn / 2 : kind.bn;
     const int64_t mt = outs * ((rows + 128 * kind.cg - 1) / (128 * kind.cg)), nt = (cols + width - 1) / width, tiles = mt * nt;
     const int64_t slots = kind.cg == 2 ? sms / 2 : sms, kb = segments * stages_of(len, kind.bn);
-    const double step = (kind.bn == 256 ? 1 : 2) * std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / (kind.cg == 2 ? 77.0 : 67.0)));
+    const double convert = mode == kDw8 ? 220.0 : 0.0;          // what a copy of codes adds to its step
+    const double step = (kind.bn == 256 ? 1 : 2) * (convert + std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / (kind.cg == 2 ? 77.0 : 67.0))));
     const double epilogue = mode == kGated ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
     const double tile = std::max(kb * step, epilogue) + 100.0;
     auto offer = [&](int64_t whole, int64_t splits, double cost, bool clustered) {
@@ -242,7 +244,7 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int seg
       least = cost;
       const int64_t per = (kb + splits - 1) / splits;
       best = {kind.cg, kind.bn, static_cast<uint32_t>(mt), static_cast<uint32_t>(nt), static_cast<uint32_t>(whole), static_cast<uint32_t>(tiles - whole),
-              static_cast<uint32_t>(splits), static_cast<uint32_t>(per), clustered};
+              static_cast<uint32_t>(splits), static_cast<uint32_t>(per), clustered, cost};
     };
     offer(tiles, 1, start + epilogue + std::ceil(static_cast<double>(tiles) / slots) * tile, false);
     const int64_t whole = tiles / slots * slots, cut = tiles - whole;
@@ -337,19 +339,27 @@ void set_out(TcArgs& a, void* out0, void* out1, int64_t ld) {
 uint32_t a_box(int64_t rows) { return static_cast<uint32_t>(std::min<int64_t>(128, round_up(rows, 8))); }
 
 // dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
-// Whether a checkpointed X is converted inside the GEMM, by its own warps, rather than restored into the workspace by a pass before
-// it.  Inside, every tile converts its columns again and the products wait for it a little at each stage; the pass costs a
-// launch and X's way through memory.  Measured, inside against before: 515 tokens, 768 x 768 10.0 against 14.3 us; 3001, 1023 x 2730
-// (8.4e9 products) 30.7 against 30.4; 16384, 2048 x 5632 (1.9e11) 349 against 315.
-bool converts_inside(int64_t tokens, int64_t rows, int64_t cols, int outs) {
-  return static_cast<double>(outs) * static_cast<double>(tokens) * static_cast<double>(rows) * static_cast<double>(cols) < 8e9;
+// Tile of a weight gradient, and whether a checkpointed X is converted inside the GEMM, by its own warps, rather than restored into the
+// workspace by a pass before it.  Inside, every tile converts its columns again, some 220 cycles a copy; the pass moves 3.1 bytes an
+// element and is a launch more unless one is made anyway (`before`).  Measured, inside against before, on the device: 515 tokens, 768 x
+// 768 7.1 against 6.9 us and 2.5 us less on the host; 16384, 512 x 2048 39.8 against 48.8; 2048, 2048 x 1024 15.4 against 13.1; 16384,
+// 2048 x 5632 349 against 315.
+struct DwChoice {
+  Tile tile;
+  bool inside;
+};
+DwChoice choose_dw(int64_t tokens, int64_t rows, int64_t cols, int outs, bool kept, bool before, int sms) {
+  const Tile plain = choose(kDw, rows, cols, outs, tokens, 1, sms);
+  if (!kept) return {plain, false};
+  const Tile inside = choose(kDw8, rows, cols, outs, tokens, 1, sms);
+  const double pass = (before ? 0.0 : 4500.0) + static_cast<double>(tokens) * cols * 3.1 / 3400.0;
+  return inside.cost < plain.cost + pass ? DwChoice{inside, true} : DwChoice{plain, false};
 }
 
 // X: a BF16 matrix, or a checkpoint of the same shape (x8, format) to be converted inside.
-int run_dw(const Mat& a0, const Mat* a1, const Mat& x, const Act8View* x8, int format, void* out0, void* out1, int64_t ld_out, void* part, int* status,
+int run_dw(const Tile& t, const Mat& a0, const Mat* a1, const Mat& x, const Act8View* x8, int format, void* out0, void* out1, int64_t ld_out, void* part, int* status,
            int sms, cudaStream_t s) {
   const int outs = a1 != nullptr ? 2 : 1;
-  const Tile t = choose(kDw, a0.cols, x.cols, outs, a0.rows, 1, sms);
   TcArgs args = base_args(t, a0.cols, x.cols, a0.rows, 1, status);
   args.tiles_per_out = t.m_tiles / outs;
   set_out(args, out0, out1, ld_out);
@@ -373,10 +383,6 @@ int run_dw(const Mat& a0, const Mat* a1, const Mat& x, const Act8View* x8, int f
   return launch_mode<kDw8>(t, maps, args, sms, s);
 }
 
-int64_t dw_part_bytes(int64_t m, int64_t rows, int64_t cols, int outs, int sms) {
-  return part_bytes(choose(kDw, rows, cols, outs, m, 1, sms));
-}
-
 // ---- the gated block ---------------------------------------------------------------------------------------------------------
 int check_gated(const gws_gated_desc* d) {
   if (d == nullptr) return GWS_ERR_NULL;
@@ -394,21 +400,23 @@ int64_t saved_bytes(const gws_gated_desc* d) {
 
 struct BackLayout {
   int64_t x, w_gate, w_up, grad_gate, grad_up, part, total;
+  Tile dx;
+  DwChoice dw;
 };
 BackLayout back_layout(const gws_gated_desc* d, int sms) {
   BackLayout l{};
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t here = at; at += round_up(bytes, 256); return here; };
-  const bool direct_x = is_act8(d->x_format) ? converts_inside(d->m, d->n, d->k, 2) : in_place(d->m, d->ld_x);
+  l.dx = choose(kDx, d->m, d->k, 1, d->n, 2, sms);
+  l.dw = choose_dw(d->m, d->n, d->k, 2, is_act8(d->x_format), true, sms);
+  const bool direct_x = is_act8(d->x_format) ? l.dw.inside : in_place(d->m, d->ld_x);
   l.x = take(direct_x ? 0 : packed_bytes(d->m, d->k));
   const int64_t w = in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k);
   l.w_gate = take(w);
   l.w_up = take(w);
   l.grad_gate = take(packed_bytes(d->m, d->n));
   l.grad_up = take(packed_bytes(d->m, d->n));
-  const int64_t dx = d->m > 0 && d->k > 0 && d->n > 0 ? part_bytes(choose(kDx, d->m, d->k, 1, d->n, 2, sms)) : 0;
-  const int64_t dw = d->m > 0 && d->k > 0 && d->n > 0 ? dw_part_bytes(d->m, d->n, d->k, 2, sms) : 0;
-  l.part = take(std::max(dx, dw));
+  l.part = take(std::max(part_bytes(l.dx), part_bytes(l.dw.tile)));
   l.total = at;
   return l;
 }
@@ -474,7 +482,9 @@ int64_t gws_wgrad_act8_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t 
   const int st = check_dims(m, n, k);
   if (st != GWS_OK) return st;
   if (m == 0 || n == 0 || k == 0) return 0;
-  return (in_place(m, ld_y) ? 0 : packed_bytes(m, n)) + (converts_inside(m, n, k, 1) ? 0 : packed_bytes(m, k)) + dw_part_bytes(m, n, k, 1, sm_count());
+  const bool moved = !in_place(m, ld_y);
+  const DwChoice dw = choose_dw(m, n, k, 1, true, moved, sm_count());
+  return (moved ? packed_bytes(m, n) : 0) + (dw.inside ? 0 : packed_bytes(m, k)) + part_bytes(dw.tile);
 }
 
 int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad_y, int64_t ld_y, const void* x8, void* grad_w, int64_t ld_w,
@@ -498,14 +508,16 @@ int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad
   Ready ready;
   Mat y{grad_y, m, n, ld_y}, x{nullptr, m, k, 0};
   ready.align(y, ws);
-  if (!in_place(m, ld_y)) ws += packed_bytes(m, n);
-  const bool inside = converts_inside(m, n, k, 1);
-  if (!inside) {
+  const bool moved = !in_place(m, ld_y);
+  if (moved) ws += packed_bytes(m, n);
+  const int sms = sm_count();
+  const DwChoice dw = choose_dw(m, n, k, 1, true, moved, sms);
+  if (!dw.inside) {
     x = ready.restore(kept, format, m, k, ws);
     ws += packed_bytes(m, k);
   }
   if ((st = ready.run(s)) != GWS_OK) return st;
-  return run_dw(y, nullptr, x, inside ? &kept : nullptr, format, grad_w, nullptr, ld_w, ws, status, sm_count(), s);
+  return run_dw(dw.tile, y, nullptr, x, dw.inside ? &kept : nullptr, format, grad_w, nullptr, ld_w, ws, status, sms, s);
 }
 
 int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward) {
@@ -637,12 +649,11 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   Ready ready;
   Mat mg{w_gate, d.n, d.k, d.ld_w}, mu{w_up, d.n, d.k, d.ld_w}, mx{x, d.m, d.k, d.ld_x};
   const Act8View kept_x = act8_view(x, d.m, d.k);
-  const bool inside = x8 && converts_inside(d.m, d.n, d.k, 2);
   if (wants_dx) {
     ready.align(mg, ws + l.w_gate);
     ready.align(mu, ws + l.w_up);
   }
-  if (wants_dw && x8 && !inside) mx = ready.restore(kept_x, d.x_format, d.m, d.k, ws + l.x);
+  if (wants_dw && x8 && !l.dw.inside) mx = ready.restore(kept_x, d.x_format, d.m, d.k, ws + l.x);
   if (wants_dw && !x8) ready.align(mx, ws + l.x);
   st = d.save_format == GWS_ACT8_INT8   ? launch_pre_act<GWS_ACT8_INT8>(p, ready, d.activation, fast, s)
        : d.save_format == GWS_ACT8_E4M3 ? launch_pre_act<GWS_ACT8_E4M3>(p, ready, d.activation, fast, s)
@@ -651,7 +662,7 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
   const Mat dg{p.grad_gate, d.m, d.n, p.ld}, du{p.grad_up, d.m, d.n, p.ld};
 
   if (wants_dx) {
-    const Tile t = choose(kDx, d.m, d.k, 1, d.n, 2, sms);
+    const Tile& t = l.dx;
     TcArgs args = base_args(t, d.m, d.k, d.n, 2, status);
     args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
     set_out(args, grad_x, nullptr, d.k);
@@ -662,7 +673,7 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
       return st;
     if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
   }
-  if (wants_dw) return run_dw(dg, &du, mx, inside ? &kept_x : nullptr, d.x_format, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
+  if (wants_dw) return run_dw(l.dw.tile, dg, &du, mx, l.dw.inside ? &kept_x : nullptr, d.x_format, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
   return GWS_OK;
 }
 
