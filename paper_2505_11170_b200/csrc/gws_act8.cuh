@@ -279,8 +279,8 @@ struct Prep {
   uint32_t per_row[3];          // 16-byte units in a row of the copy
   uint32_t move_blocks, restore_blocks;
   Act8View kept;
-  uint16_t* restored;           // [rows, kept.ld]
-  int64_t groups;
+  uint16_t* restored;           // [rows, ld_restored]
+  int64_t ld_restored, groups;
   int32_t format;
 };
 __device__ __forceinline__ void move_unit(const Prep& m, int64_t t) {
@@ -307,8 +307,10 @@ __device__ __forceinline__ bool prepare(const Prep& m) {
   }
   const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks) * 256 + threadIdx.x;
   if (t >= m.groups) return true;
-  if (m.format == GWS_ACT8_INT8) load_group<GWS_ACT8_INT8>(m.kept, m.restored, t, t * kGroup);
-  else load_group<GWS_ACT8_E4M3>(m.kept, m.restored, t, t * kGroup);
+  int64_t at = t * kGroup;
+  if (m.ld_restored != m.kept.ld) at += quotient(t, static_cast<uint32_t>(m.kept.ld / kGroup)) * (m.ld_restored - m.kept.ld);
+  if (m.format == GWS_ACT8_INT8) load_group<GWS_ACT8_INT8>(m.kept, m.restored, t, at);
+  else load_group<GWS_ACT8_E4M3>(m.kept, m.restored, t, at);
   return true;
 }
 __global__ void __launch_bounds__(256) k_prepare(const __grid_constant__ Prep m) {

@@ -232,12 +232,13 @@ __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
   slope = __fmaf_rn(a * (1.0f - s), dz, s);
 }
 
-// A 32 x 32 block of BF16 from shared memory (rows 17 words apart) to rows that take stores of V elements: a lane V columns, a warp V rows
-// at a time.
+// The first `width` columns of a 32 x 32 block of BF16 from shared memory (rows 17 words apart) to rows that take stores of V elements: a
+// lane V columns, a warp V rows at a time.
 template <uint32_t V>
-__device__ __forceinline__ void store_rows(uint16_t* p, int64_t ld, int64_t left, const uint32_t* staging, uint32_t lane) {
+__device__ __forceinline__ void store_rows(uint16_t* p, int64_t ld, int64_t left, uint32_t width, const uint32_t* staging, uint32_t lane) {
   constexpr uint32_t kLanes = 32u / V, kBatch = V == 1u ? 8u : V == 2u ? 4u : 2u;
   const uint32_t row = lane / kLanes, word = (lane % kLanes) * V / 2u;
+  if ((lane % kLanes) * V >= width) return;
   const uint32_t* s = staging + row * 17u + word;
   p += row * ld + (lane % kLanes) * V;
 #pragma unroll
@@ -284,16 +285,11 @@ __device__ __forceinline__ void store_block(uint16_t* out, int64_t ld, int32_t w
   __syncwarp();
   const int64_t left = rows - row0;
   uint16_t* p = out + row0 * ld + col0;
-  if (col0 + 32 <= cols) {
-    if (wide >= 8) store_rows<8>(p, ld, left, staging, lane);
-    else if (wide == 4) store_rows<4>(p, ld, left, staging, lane);
-    else if (wide == 2) store_rows<2>(p, ld, left, staging, lane);
-    else store_rows<1>(p, ld, left, staging, lane);
-  } else if (col0 + lane < cols) {
-    const uint16_t* s = reinterpret_cast<const uint16_t*>(staging) + lane;
-    const int64_t n = left < 32 ? left : 32;
-    for (int64_t r = 0; r < n; ++r) p[r * ld + lane] = s[r * 34];
-  }
+  const uint32_t width = col0 + 32 <= cols ? 32u : static_cast<uint32_t>(cols - col0);
+  if (wide >= 8 && width % 8u == 0) store_rows<8>(p, ld, left, width, staging, lane);
+  else if (wide >= 4 && width % 4u == 0) store_rows<4>(p, ld, left, width, staging, lane);
+  else if (wide >= 2 && width % 2u == 0) store_rows<2>(p, ld, left, width, staging, lane);
+  else store_rows<1>(p, ld, left, width, staging, lane);
   __syncwarp();
 }
 
@@ -855,12 +851,13 @@ __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreAr
   if (prepare(m)) return;
   const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks - m.restore_blocks) * 256 + threadIdx.x;
   if (t >= p.groups) return;
-  int64_t at_dh = t * kGroup;
-  if (p.ld_grad_h != p.cols) {
-    const int64_t row = t / p.per_row;
-    at_dh = row * p.ld_grad_h + (t - row * p.per_row) * kGroup;
+  const int64_t at = t * kGroup;     // saved values and h: rows side by side
+  int64_t at_dh = at, at_out = at;
+  if (p.ld_grad_h != p.cols || p.ld != p.cols) {
+    const int64_t row = quotient(t, p.per_row);
+    at_dh += row * (p.ld_grad_h - p.cols);
+    at_out += row * (p.ld - p.cols);
   }
-  const int64_t at = t * kGroup;     // saved values, results: rows side by side
   V8 cg, cu;
   float ug = 0.0f, uu = 0.0f;
   if (SAVE != GWS_SAVE_BF16) {
@@ -904,8 +901,8 @@ __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreAr
       du.x[i] = pack_bf16(d2[0], d2[1]);
       h.x[i] = pack_bf16(a[0], a[1]);
     }
-    st32(p.grad_gate + at + 16 * q, dg);
-    st32(p.grad_up + at + 16 * q, du);
+    st32(p.grad_gate + at_out + 16 * q, dg);
+    st32(p.grad_up + at_out + 16 * q, du);
     if (p.h != nullptr) st32(p.h + at + 16 * q, h);
   }
 }
