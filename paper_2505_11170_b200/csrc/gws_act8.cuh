@@ -37,10 +37,11 @@ __device__ __forceinline__ void st32(void* p, const V8& v) {
 
 // These kernels are launched programmatically: a kernel's blocks may become resident while the one before it on the stream drains, and
 // touch global memory only once that one has completed.  Every kernel of this file set passes here before its first access, so
-// the order along the stream holds transitively.
+// the order along the stream holds transitively.  The next kernel may follow once this one has seen its predecessor end, so that there
+// are never more than two on the device: blocks of a third would hold shared memory, tensor memory and barriers without a use for them.
 __device__ __forceinline__ void after_previous() {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 __device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }

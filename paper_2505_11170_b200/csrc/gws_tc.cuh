@@ -82,6 +82,7 @@ __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank) {
   return r;
 }
 __device__ __forceinline__ void pair_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) {
@@ -187,6 +188,7 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
 }
 
 __device__ __forceinline__ void acc_load(uint32_t addr, uint32_t (&r)[32]) {
+  __syncwarp();                          // the load is one of the whole warp; lanes may come from rows treated differently
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
       "%25,%26,%27,%28,%29,%30,%31}, [%32];"
@@ -503,6 +505,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         if (++s == kStages) { s = 0; parity ^= 1u; }
       }
     }
+    // Every release of a stage has to have arrived before this block's shared memory may become another block's: the signal of a commit
+    // comes from the other SM of the pair, on its own time, and would count on whatever barrier lies there by then.
+    for (uint32_t i = 0; ok && i < kStages; ++i) {
+      ok = bar_wait(empty0 + 8u * s, parity);
+      if (++s == kStages) { s = 0; parity ^= 1u; }
+    }
     if (!ok) failed = 1;
   } else if (warp == 1) {
     if (rank == 0) {
@@ -547,6 +555,9 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         if (ok && elected()) commit<CG>(&acc_full[buf]);
         __syncwarp();
       }
+      // ... and so does every hand-back of an accumulator
+      for (uint32_t back = 1; ok && back <= 2u && back <= n; ++back)
+        ok = bar_wait<CG == 2>(acc_empty0 + 8u * ((n - back) & 1u), ((n - back) >> 1) & 1u);
       if (!ok) failed = 1;
     }
   } else if (warp >= 4 && warp < 4u + S::kEpilogueWarps) {
@@ -631,8 +642,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
           // The two warps that share these rows meet; one writes the gate's, the other the up projection's.  A warp that fills the same
           // buffer again has passed the meeting of the tile between, and so has the other one's store.
+          __syncwarp();
           asm volatile("bar.sync %0, 64;" ::"r"(quadrant + 1u) : "memory");
-          if (__any_sync(0xFFFFFFFFu, failed != 0)) break;
+          if (__any_sync(0xFFFFFFFFu, failed != 0)) {            // the other warp may have read it a moment earlier, as not set, and go on
+            asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
+            break;
+          }
           const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (BN / 64);
           if (row < p.rows) {
             uint8_t* to = p.save8[half].scales + row * ld + g0;
@@ -759,6 +774,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (CG == 2) pair_sync();              // the other block's products read this block's shared memory until here
+  __syncwarp();
   if (warp == 2) {
     if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemCols) : "memory");
