@@ -223,6 +223,7 @@ struct Tile {
   uint32_t m_tiles, n_tiles, whole, cut, splits, kb_split;
   bool clustered;                          // the parts of a tile are the blocks of a cluster
   double cost;                             // estimated cycles
+  uint32_t width;                          // kGatedFew: columns of h in a tile, else 0
 };
 
 // The tile, and the cut of the tiles that do not fill a wave, with the least estimated time, in SM cycles.  A tile takes a block its
@@ -241,21 +242,24 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int seg
     const double convert = mode == kDw8 ? 220.0 : 0.0;          // what a copy of codes adds to its step
     const double step = (kind.bn == 256 ? 1 : 2) * (convert + std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / (kind.cg == 2 ? 77.0 : 67.0))));
     const double epilogue = mode == kGated ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
-    const double tile = std::max(kb * step, epilogue) + 100.0;
+    // one row of tiles reads the weights once: no faster than from memory
+    const double bytes = mode == kGated && mt == 1 ? width * 4.0 * len / 3400.0 : 0.0, tile = std::max({kb * step, epilogue, std::min(tiles, slots) * bytes}) + 100.0;
     auto offer = [&](int64_t whole, int64_t splits, double cost, bool clustered) {
       if (best.cg != 0 && cost >= least) return;
       least = cost;
       const int64_t per = (kb + splits - 1) / splits;
       best = {kind.cg, kind.bn, static_cast<uint32_t>(mt), static_cast<uint32_t>(nt), static_cast<uint32_t>(whole), static_cast<uint32_t>(tiles - whole),
-              static_cast<uint32_t>(splits), static_cast<uint32_t>(per), clustered, cost};
+              static_cast<uint32_t>(splits), static_cast<uint32_t>(per), clustered, cost, 0};
     };
     offer(tiles, 1, start + epilogue + std::ceil(static_cast<double>(tiles) / slots) * tile, false);
     const int64_t whole = tiles / slots * slots, cut = tiles - whole;
+    if (start + 5.0 * kind.bn + (mode == kGated || kind.cg == 2 ? 5900.0 + static_cast<double>(whole / slots) * tile : 2400.0) >= least) continue;
     for (int64_t splits = 2; cut > 0 && splits <= std::min<int64_t>(32, kb); ++splits) {
       const int64_t per = (kb + splits - 1) / splits;
       if ((kb + per - 1) / per != splits) continue;
       const double part = std::max(per * step, 5.0 * kind.bn + 400.0) + 100.0;
-      offer(whole, splits, start + 5.0 * kind.bn + 400.0 + static_cast<double>(whole / slots) * tile + std::ceil(static_cast<double>(cut * splits) / slots) * part +
+      offer(whole, splits, start + 5.0 * kind.bn + 400.0 + static_cast<double>(whole / slots) * tile +
+                               std::max(std::ceil(static_cast<double>(cut * splits) / slots) * part, cut * bytes) +
                                5500.0 + 128.0 * kind.cg * kind.bn * cut * (8.0 * splits + 2.0) / 3400.0,
             false);
       // clusters of up to 4 blocks on 120 SMs, of up to 6 on 96: a cluster lives inside a group of some 18 SMs, and 16 clusters of 8 took two
@@ -287,6 +291,7 @@ int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStr
   const uint32_t work = args.whole + args.cut * args.splits, slots = static_cast<uint32_t>(sms / CG);
   const int st = launch(k_tc<CG, BN, MODE>, args.clustered ? work : std::min(work, slots) * CG, S::kThreads, S::kSmemBytes,
                         args.clustered ? args.splits : CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
+  if constexpr (MODE == kGatedFew) return st;
   if (st != GWS_OK || args.cut == 0 || args.clustered) return st;
   constexpr uint32_t kWarps = (MODE == kGated ? BN / 64 : BN / 32) * (128 * CG / kJoinRows);       // per tile
   return launch(k_join<CG, BN, MODE>, args.cut * (kWarps / 8), 256, 0, 1, s, "join of a cut contraction", args);
@@ -431,8 +436,40 @@ struct ForwardPlan {
   Tile tile;
   bool move_x, move_w;
 };
+// kGatedFew: bytes of a copy of 64 elements along the contraction, and the stages that fit; the products read 128 rows of A from where the
+// last copy begins.
+uint32_t few_half(int64_t rows, uint32_t width) { return a_box(rows) * kTcHalf * 2u + width * kTcHalf * 4u; }
+uint32_t few_stages(int64_t rows, uint32_t width) {
+  const uint32_t half = few_half(rows, width), ring = TcShape<1, 128, kGatedFew>::kRing;
+  return std::min({8u, ring / (2u * half), (ring + half - kTcABytes) / (2u * half)});
+}
+// The width of tile with the least estimated time, for up to 128 tokens.  A stage of 128 steps costs 620 cycles however narrow the tile (eight
+// products that read 128 rows of A), or its bytes at 67 a cycle; a wave of tiles costs no less than its weights at 3400 bytes a cycle from
+// memory.  What narrow tiles win is an even share for every SM and more weights on their way (us, weights from memory, against the best of
+// choose): one token, 2048 x 5632, 40 columns 12.0 (13.1), 48 11.9, 64 12.3, 32 in two waves 16.1; 128 tokens 13.2 (13.5); one token, 4096 x 11008,
+// 40 columns 33.7 (42), 48 40.3, 64 42.5.  A long contraction into few columns is better cut: 5632 x 2048, 16 columns 18.1 (16.5).
+// Checkpoints want whole groups of 32: 64 columns 13.1 (13.7), 32 16.9.
+Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, int sms) {
+  const int64_t kb = stages_of(len, 128);
+  const uint32_t slots = static_cast<uint32_t>(sms);
+  Tile best{};
+  for (uint32_t width = 64; width >= std::max(unit, 16u); width -= unit) {
+    const uint32_t tiles = (static_cast<uint32_t>(cols) + width - 1) / width, rest = tiles % slots;
+    const double stage = std::max(620.0, 2.0 * few_half(rows, width) / 67.0), epilogue = 20.0 * width + 400.0;
+    auto wave = [&](uint32_t n) { return std::max({static_cast<double>(kb) * stage, epilogue, n * width * 4.0 * len / 3400.0}) + 100.0; };
+    const double cost = 3300.0 + epilogue + static_cast<double>(tiles / slots) * wave(slots) + (rest != 0 ? wave(rest) : 0.0);
+    if (best.cg == 0 || cost < best.cost)
+      best = {1, 128, 1, tiles, tiles, 0, 1, static_cast<uint32_t>(kb), false, cost, width};
+  }
+  return best;
+}
+
 ForwardPlan plan_forward(const gws_gated_desc* d, int sms) {
   ForwardPlan f{choose(kGated, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
+  if (d->m <= 128) {
+    const Tile few = choose_few(d->m, d->n, d->k, 8, sms);
+    if (few.cost < f.tile.cost) f.tile = is_act8(d->save_format) ? choose_few(d->m, d->n, d->k, 32, sms) : few;     // h does not depend on what is kept
+  }
   if (!f.move_x && !f.move_w && d->m > 1 && d->n > 1 && d->ld_x % 16 != 0 && d->ld_w % 16 != 0) {
     const double smaller = static_cast<double>(d->k) * std::min(d->m, 2 * d->n);
     if (0.25 * f.tile.cost > 4500.0 + smaller * 4.0 / 3400.0) (d->m <= 2 * d->n ? f.move_x : f.move_w) = true;
@@ -585,6 +622,7 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   if ((st = ready.run(s)) != GWS_OK) return st;
 
   const Tile& t = f.tile;
+  const uint32_t width = t.width != 0 ? t.width : static_cast<uint32_t>(t.bn / 2);
   TcArgs args = base_args(t, d.m, d.n, d.k, 1, status);
   set_out(args, h, nullptr, d.ld_h);
   args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
@@ -599,12 +637,19 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
     args.save16[1] = static_cast<uint16_t*>(save_up);
     args.save_wide = widest(d.n, save_gate, save_up);
   }
+  if (t.width != 0) {
+    args.width = width;
+    args.a_bytes = a_box(d.m) * kTcHalf * 2u;
+    args.stages = few_stages(d.m, width);
+    args.half_bytes = few_half(d.m, width);
+    if (width % 16 != 0) args.wide = std::min(args.wide, 8), args.save_wide = std::min(args.save_wide, 8);
+  }
   CUtensorMap maps[4];
   if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, a_box(d.m))) != GWS_OK) return st;
   maps[1] = maps[0];
-  if ((st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, static_cast<uint32_t>(t.bn / 2))) != GWS_OK) return st;
-  if ((st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, static_cast<uint32_t>(t.bn / 2))) != GWS_OK) return st;
-  return launch_mode<kGated>(t, maps, args, sms, s);
+  if ((st = make_map(maps[2], mg.p, d.n, d.k, mg.ld, width)) != GWS_OK) return st;
+  if ((st = make_map(maps[3], mu.p, d.n, d.k, mu.ld, width)) != GWS_OK) return st;
+  return t.width != 0 ? launch_tc<1, 128, kGatedFew>(maps, args, sms, s) : launch_mode<kGated>(t, maps, args, sms, s);
 }
 
 int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x, const void* w_gate, const void* w_up, const void* save_gate,

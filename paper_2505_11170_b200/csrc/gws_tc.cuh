@@ -36,7 +36,7 @@
 
 namespace {
 
-enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3 };
+enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4 };
 
 constexpr uint32_t kTcHalf = 64;                           // elements along the contraction per copy: 128 bytes, one swizzle atom
 constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
@@ -64,6 +64,7 @@ struct TcArgs {
   int32_t x_format;
   int32_t box_tokens;                     // kDw, kDw8: tokens in a copy
   int32_t activation, save;               // kGated
+  uint32_t width, stages, a_bytes;        // kGatedFew: columns of h in a tile, stages of the ring, bytes of A in a copy
   int32_t save_wide;                      // the same for the BF16 copies
   Act8View save8[2];
   uint16_t* save16[2];                    // BF16 copies, [rows, cols]
@@ -327,8 +328,10 @@ struct TcShape {
   static constexpr uint32_t kHalf = kTcABytes + kBBytes + kRaw;            // A, B, codes
   static constexpr uint32_t kStage = kHalves * kHalf;
   static constexpr uint32_t kFit = (kTcSmem - 4096u - kStaging) / kStage;
-  static constexpr uint32_t kStages = kFit > 8u ? 8u : kFit;
-  static constexpr uint32_t kSmemBytes = kStages * kStage + kStaging + 1024u;
+  // kGatedFew parts the same memory into as many stages as its narrower copies allow
+  static constexpr uint32_t kStages = kFit > 8u || MODE == kGatedFew ? 8u : kFit;
+  static constexpr uint32_t kRing = (kFit > 8u ? 8u : kFit) * kStage;
+  static constexpr uint32_t kSmemBytes = kRing + kStaging + 1024u;
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
@@ -389,19 +392,21 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
          const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
   using S = TcShape<CG, BN, MODE>;
-  constexpr bool kIsDw = MODE == kDw || MODE == kDw8, kMnA = kIsDw, kMnB = MODE != kGated;
+  constexpr bool kFew = MODE == kGatedFew, kIsGated = MODE == kGated || kFew, kIsDw = MODE == kDw || MODE == kDw8, kMnA = kIsDw, kMnB = !kIsGated;
   constexpr uint32_t kStages = S::kStages;
+  const uint32_t stages = kFew ? p.stages : kStages, width = kFew ? p.width : BN / 2;      // width: columns of h in a tile (kIsGated)
+  const uint32_t a_bytes = kFew ? p.a_bytes : kTcABytes, half_pitch = kFew ? a_bytes + width * (kTcHalf * 4u) : S::kHalf, stage_pitch = S::kHalves * half_pitch;
   // instruction descriptor: FP32 accumulator, BF16 operands, which axis of A and B is contiguous, N, M
-  constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kMnA ? 1u : 0u) << 15) | ((kMnB ? 1u : 0u) << 16) |
-                              (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
+  const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kMnA ? 1u : 0u) << 15) | ((kMnB ? 1u : 0u) << 16) |
+                         ((kFew ? width >> 2 : static_cast<uint32_t>(BN >> 3)) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], codes_full[kStages], converted[kStages];
-  __shared__ __align__(16) uint8_t scale_bytes[2][2][MODE == kGated ? 128 : 1][4];      // of two tiles, gate and up projection
+  __shared__ __align__(16) uint8_t scale_bytes[2][2][kIsGated ? 128 : 1][4];      // of two tiles, gate and up projection
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int failed;
   const uint32_t raw = smem_addr(smem_raw);
   uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);   // the same offset in both blocks of a pair
-  uint32_t* staging = reinterpret_cast<uint32_t*>(smem + kStages * S::kStage);
+  uint32_t* staging = reinterpret_cast<uint32_t*>(smem + S::kRing);
 
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const uint32_t rank = CG == 2 ? block_rank() : 0u;
@@ -462,7 +467,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       place(t, mt, nt, k0, k1);
       const bool second = kIsDw && mt >= p.tiles_per_out;
       const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
-      const int32_t n0 = static_cast<int32_t>(nt * (MODE == kGated ? BN / 2 : BN) + (MODE == kGated ? 0u : rank * S::kBRows));
+      const int32_t n0 = static_cast<int32_t>(nt * (kIsGated ? width : BN) + (kIsGated ? 0u : rank * S::kBRows));
       for (uint32_t kb = k0; kb < k1; ++kb) {
         if (!bar_wait(empty0 + 8u * s, parity)) { ok = false; break; }
         const bool seg = MODE == kDx && kb >= p.kb_first;
@@ -475,15 +480,15 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
 #pragma unroll
           for (uint32_t i = 0; i < S::kHalves; ++i) {
             if (i >= halves) break;
-            const uint32_t sa = smem_addr(smem) + s * S::kStage + i * S::kHalf, sb = sa + kTcABytes;
+            const uint32_t sa = smem_addr(smem) + s * stage_pitch + i * half_pitch, sb = sa + a_bytes;
             const int32_t ki = static_cast<int32_t>(k + i * kTcHalf);
-            if (MODE == kGated) {
+            if (kIsGated) {
               copy_in<CG>(sa, &a0, bar, ki, m0);
               if (CG == 2) {                             // block 0 holds the gate's rows, block 1 the up projection's
                 copy_in<CG>(sb, rank == 0 ? &b0 : &b1, bar, ki, n0);
               } else {
                 copy_in<CG>(sb, &b0, bar, ki, n0);
-                copy_in<CG>(sb + (BN / 2) * kTcHalf * 2u, &b1, bar, ki, n0);
+                copy_in<CG>(sb + width * (kTcHalf * 2u), &b1, bar, ki, n0);
               }
             } else if (MODE == kDx) {
               copy_in<CG>(sa, seg ? &a1 : &a0, bar, ki, m0);
@@ -502,14 +507,14 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           }
         }
         __syncwarp();
-        if (++s == kStages) { s = 0; parity ^= 1u; }
+        if (++s == stages) { s = 0; parity ^= 1u; }
       }
     }
     // Every release of a stage has to have arrived before this block's shared memory may become another block's: the signal of a commit
     // comes from the other SM of the pair, on its own time, and would count on whatever barrier lies there by then.
-    for (uint32_t i = 0; ok && i < kStages; ++i) {
+    for (uint32_t i = 0; ok && i < stages; ++i) {
       ok = bar_wait(empty0 + 8u * s, parity);
-      if (++s == kStages) { s = 0; parity ^= 1u; }
+      if (++s == stages) { s = 0; parity ^= 1u; }
     }
     if (!ok) failed = 1;
   } else if (warp == 1) {
@@ -518,7 +523,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       bool ok = true;
       const uint32_t full0 = smem_addr(&full[0]), acc_empty0 = smem_addr(&acc_empty[0]);
       const uint64_t da = kMnA ? desc_mn(smem_addr(smem)) : desc_k(smem_addr(smem));
-      const uint64_t db = kMnB ? desc_mn(smem_addr(smem) + kTcABytes) : desc_k(smem_addr(smem) + kTcABytes);
+      const uint64_t db = kMnB ? desc_mn(smem_addr(smem) + a_bytes) : desc_k(smem_addr(smem) + a_bytes);
       // 16 steps of the contraction in the units of a descriptor's address: 32 bytes of a row, or 16 rows of 128 bytes
       constexpr uint32_t kStepA = (kMnA ? 2048u : 32u) >> 4, kStepB = (kMnB ? 2048u : 32u) >> 4;
       for (uint32_t t = first; ok && t < work; t += stride, ++n) {
@@ -533,7 +538,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           if (MODE == kDw8 && !bar_wait<CG == 2>(smem_addr(&converted[s]), parity)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t now = s;
-          if (++s == kStages) { s = 0; parity ^= 1u; }
+          if (++s == stages) { s = 0; parity ^= 1u; }
           if (kb + 1 < k1) ready = bar_peek(full0 + 8u * s, parity);      // answered while the products below are issued
           const bool seg = MODE == kDx && kb >= p.kb_first;
           const uint32_t k = (seg ? kb - p.kb_first : kb) * (S::kHalves * kTcHalf);
@@ -542,11 +547,11 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
 #pragma unroll
             for (uint32_t i = 0; i < S::kHalves; ++i) {
               if (i >= halves) break;
-              const uint64_t sa = da + ((now * S::kStage + i * S::kHalf) >> 4), sb = db + ((now * S::kStage + i * S::kHalf) >> 4);
-              mma<CG>(d, sa, sb, kIdesc, kb > k0 || i > 0 ? 1u : 0u);
+              const uint64_t sa = da + ((now * stage_pitch + i * half_pitch) >> 4), sb = db + ((now * stage_pitch + i * half_pitch) >> 4);
+              mma<CG>(d, sa, sb, idesc, kb > k0 || i > 0 ? 1u : 0u);
 #pragma unroll
               for (uint32_t j = 1; j < kTcHalf / 16u; ++j)
-                if (!kIsDw || j < p.parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, kIdesc, 1u);
+                if (!kIsDw || j < p.parts) mma<CG>(d, sa + j * kStepA, sb + j * kStepB, idesc, 1u);
             }
             commit<CG>(&empty[now]);
           }
@@ -571,14 +576,14 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) {
         failed = 1;
         // the other warp of these rows may have seen the tile complete and wait for this one below
-        if (MODE == kGated) asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
+        if (kIsGated) asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t acc = tmem + ((quadrant * 32u) << 16) + buf * BN;
       const bool second = kIsDw && mt >= p.tiles_per_out;
       const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + rank * 128u + quadrant * 32u;
-      if (CG == 1 && MODE != kGated && p.clustered) {      // a part, into this block's shared memory: its copies and products are done
+      if (CG == 1 && !kIsGated && p.clustered) {      // a part, into this block's shared memory: its copies and products are done
 #pragma unroll 1
         for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
           uint32_t v[32];
@@ -588,7 +593,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
 #pragma unroll
           for (int i = 0; i < 8; ++i) to[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         }
-      } else if (t >= p.whole) {              // a part of a contraction: FP32, joined by k_join
+      } else if (!kFew && t >= p.whole) {     // a part of a contraction: FP32, joined by k_join
         float* part = p.part + static_cast<int64_t>(t - p.whole) * (128 * CG * BN) + (rank * 128u + quadrant * 32u + lane) * BN;
 #pragma unroll 1
         for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
@@ -603,26 +608,27 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
             st32(part + c * 32u + 8 * i, x);
           }
         }
-      } else if (MODE == kGated) {
+      } else if (kIsGated) {
+        const int64_t edge = kFew ? min(p.cols, static_cast<int64_t>(nt + 1u) * width) : p.cols;      // where the tile's columns end
 #pragma unroll 1
-        for (uint32_t c = half; c < BN / 64; c += S::kEpilogueWarps / 4u) {
+        for (uint32_t c = half; c < (width + 31u) / 32u; c += S::kEpilogueWarps / 4u) {
           uint32_t g[32], u[32], w[16];
           acc_load(acc + c * 32u, g);
-          acc_load(acc + BN / 2 + c * 32u, u);
+          acc_load(acc + width + c * 32u, u);
           acc_wait();
-          const int64_t col0 = static_cast<int64_t>(nt) * (BN / 2) + c * 32u;
-          if (col0 >= p.cols) continue;
+          const int64_t col0 = static_cast<int64_t>(nt) * width + c * 32u;
+          if (col0 >= edge) continue;
           if (p.activation == GWS_GATED_SILU) gate_block<GWS_GATED_SILU>(g, u, w);
           else if (p.activation == GWS_GATED_GELU_TANH) gate_block<GWS_GATED_GELU_TANH>(g, u, w);
           else gate_block<GWS_GATED_RELU>(g, u, w);
-          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
+          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.wide, row0, col0, p.rows, edge, w, stage, lane);
           if (p.save == GWS_SAVE_BF16) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1]));
-            store_block(p.save16[0], p.cols, p.save_wide, row0, col0, p.rows, p.cols, w, stage, lane);
+            store_block(p.save16[0], p.cols, p.save_wide, row0, col0, p.rows, edge, w, stage, lane);
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
-            store_block(p.save16[1], p.cols, p.save_wide, row0, col0, p.rows, p.cols, w, stage, lane);
+            store_block(p.save16[1], p.cols, p.save_wide, row0, col0, p.rows, edge, w, stage, lane);
           } else if (p.save != GWS_SAVE_NONE && row0 + lane < p.rows) {
             // columns past the width are products with rows of zeros: zero codes, as the layout wants them
             const int64_t row = row0 + lane;
@@ -648,16 +654,16 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
             asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
             break;
           }
-          const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (BN / 64);
+          const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (width / 32u);
           if (row < p.rows) {
             uint8_t* to = p.save8[half].scales + row * ld + g0;
             const uint8_t* from = scale_bytes[buf][half][quadrant * 32u + lane];
-            constexpr uint32_t kGroups = BN / 64;
-            if (g0 + kGroups <= ld && ld % kGroups == 0) {            // the buffer's scales start at a multiple of 256 bytes
-              if (kGroups == 4u) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
+            const uint32_t groups = width / 32u;
+            if (groups > 1u && g0 + groups <= ld && ld % groups == 0) {       // the buffer's scales start at a multiple of 256 bytes
+              if (groups == 4u) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
               else *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
             } else {
-              for (uint32_t i = 0; i < kGroups && g0 + i < ld; ++i) to[i] = from[i];
+              for (uint32_t i = 0; i < groups && g0 + i < ld; ++i) to[i] = from[i];
             }
           }
         }
@@ -730,7 +736,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     }
     if (!ok) failed = 1;
   }
-  if (CG == 1 && MODE != kGated && p.clustered) {
+  if (CG == 1 && !kIsGated && p.clustered) {
     // Every block of the cluster adds its share of the tile's rows, the parts in the order of the contraction; a warp takes a row, a
     // lane four columns.
     __syncthreads();

@@ -262,6 +262,30 @@ def test_every_way_to_tile(m, n, k):
     test_backward(gws.GATED_SILU, gws.ACT8_INT8, m, n, k)
 
 
+# few tokens: narrow tiles of every width, in one wave and in several, the last one ragged, 1 to 128 rows of A in a copy
+FEW = [(1, 2300, 72), (7, 3500, 136), (33, 4713, 64), (128, 5901, 200), (61, 7100, 80), (2, 8202, 96), (100, 9400, 264), (9, 20001, 40), (120, 12000, 1032),
+       (128, 9472, 648), (16, 37, 2056), (1, 1, 1), (5, 65, 4100)]
+
+
+@pytest.mark.parametrize("m,n,k", FEW)
+def test_few_tokens(m, n, k):
+    for act in ACTS:
+        test_forward(act, m, n, k)
+    for save in (gws.ACT8_INT8, gws.ACT8_E4M3, gws.SAVE_BF16):
+        test_what_forward_keeps(save, m, n, k)
+
+
+def test_few_tokens_write_inside_their_output():
+    for m, n, k in ((1, 5632, 256), (3, 5630, 256), (17, 2300, 72)):
+        x, wg, wu, _ = _problem(m, n, k)
+        want, _ = gws.gated_fwd(x, wg, wu)
+        around = torch.full((m * n + 1024,), 7.0, device="cuda", dtype=torch.bfloat16)
+        h = around[512:512 + m * n].view(m, n)
+        gws.gated_fwd(x, wg, wu, h=h)
+        assert torch.equal(h, want)
+        assert bool((around[:512] == 7.0).all()) and bool((around[512 + m * n:] == 7.0).all())
+
+
 def test_a_captured_step_replays_to_the_same_bits():
     x, wg, wu, grad_h = _problem(300, 520, 263)                 # copies of unaligned rows, cut contractions: several kernels a call
 
