@@ -207,12 +207,33 @@ struct Ready {
 
 // ---- choice of tile --------------------------------------------------------------------------------------------------------
 int sm_count() {
+  static std::atomic<int> known[64];             // per device
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) {
+  const bool current = cudaGetDevice(&dev) == cudaSuccess;
+  if (current && dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) != 0) return n;
+  if (!current || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) {
     (void)cudaGetLastError();
     return 148;
   }
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
   return n;
+}
+
+// What make() returns for a key of sizes, options and SM count, which it depends on alone.  The last 64 or so are kept per thread: weighing the
+// tiles of a call takes the host 0.5 to 1.5 us, as long as launching a kernel.
+template <class Value, size_t N, class F>
+const Value& remembered(const int64_t (&key)[N], F&& make) {
+  struct Slot { int64_t key[N]; bool used; Value value; };
+  static thread_local Slot slots[64];
+  uint64_t hash = 0;
+  for (const int64_t v : key) hash = (hash ^ static_cast<uint64_t>(v)) * 0x9E3779B97F4A7C15ull;
+  Slot& slot = slots[hash >> 58];
+  if (!slot.used || std::memcmp(slot.key, key, sizeof key) != 0) {
+    slot.value = make();
+    std::memcpy(slot.key, key, sizeof key);
+    slot.used = true;
+  }
+  return slot.value;
 }
 
 // Stages along a contraction (TcShape::kHalves copies of 64 elements each).
@@ -356,12 +377,15 @@ struct DwChoice {
   Tile tile;
   bool inside;
 };
-DwChoice choose_dw(int64_t tokens, int64_t rows, int64_t cols, int outs, bool kept, bool before, int sms) {
+DwChoice weigh_dw(int64_t tokens, int64_t rows, int64_t cols, int outs, bool kept, bool before, int sms) {
   const Tile plain = choose(kDw, rows, cols, outs, tokens, 1, sms);
   if (!kept) return {plain, false};
   const Tile inside = choose(kDw8, rows, cols, outs, tokens, 1, sms);
   const double pass = (before ? 0.0 : 4500.0) + static_cast<double>(tokens) * cols * 3.1 / 3400.0;
   return inside.cost < plain.cost + pass ? DwChoice{inside, true} : DwChoice{plain, false};
+}
+DwChoice choose_dw(int64_t tokens, int64_t rows, int64_t cols, int outs, bool kept, bool before, int sms) {
+  return remembered<DwChoice>({tokens, rows, cols, outs, kept, before, sms}, [&] { return weigh_dw(tokens, rows, cols, outs, kept, before, sms); });
 }
 
 // X: a BF16 matrix, or a checkpoint of the same shape (x8, format) to be converted inside.
@@ -411,7 +435,7 @@ struct BackLayout {
   Tile dx;
   DwChoice dw;
 };
-BackLayout back_layout(const gws_gated_desc* d, int sms) {
+BackLayout weigh_backward(const gws_gated_desc* d, int sms) {
   BackLayout l{};
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t here = at; at += round_up(bytes, 256); return here; };
@@ -427,6 +451,9 @@ BackLayout back_layout(const gws_gated_desc* d, int sms) {
   l.part = take(std::max(part_bytes(l.dx), part_bytes(l.dw.tile)));
   l.total = at;
   return l;
+}
+const BackLayout& back_layout(const gws_gated_desc* d, int sms) {
+  return remembered<BackLayout>({d->m, d->n, d->k, d->ld_x, d->ld_w, d->x_format, sms}, [&] { return weigh_backward(d, sms); });
 }
 // Forward: tile, and which operands are copied into the workspace - those that no tensor map can read, and, where both operands have rows
 // that start in the middle of a 32-byte sector, the smaller one if that pays.  With the contraction contiguous such rows cost a third more
@@ -464,7 +491,7 @@ Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, int sms)
   return best;
 }
 
-ForwardPlan plan_forward(const gws_gated_desc* d, int sms) {
+ForwardPlan weigh_forward(const gws_gated_desc* d, int sms) {
   ForwardPlan f{choose(kGated, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
   if (d->m <= 128) {
     const Tile few = choose_few(d->m, d->n, d->k, 8, sms);
@@ -475,6 +502,9 @@ ForwardPlan plan_forward(const gws_gated_desc* d, int sms) {
     if (0.25 * f.tile.cost > 4500.0 + smaller * 4.0 / 3400.0) (d->m <= 2 * d->n ? f.move_x : f.move_w) = true;
   }
   return f;
+}
+const ForwardPlan& plan_forward(const gws_gated_desc* d, int sms) {
+  return remembered<ForwardPlan>({d->m, d->n, d->k, d->ld_x, d->ld_w, d->save_format, sms}, [&] { return weigh_forward(d, sms); });
 }
 int64_t forward_copies(const gws_gated_desc* d, const ForwardPlan& f) {
   return (f.move_x ? packed_bytes(d->m, d->k) : 0) + (f.move_w ? 2 * packed_bytes(d->n, d->k) : 0);
@@ -604,7 +634,7 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   }
   if (x == nullptr || w_gate == nullptr || w_up == nullptr) return GWS_ERR_NULL;
   const int sms = sm_count();
-  const ForwardPlan f = plan_forward(desc, sms);
+  const ForwardPlan& f = plan_forward(desc, sms);
   if (!on(x, in_place(d.m, d.ld_x) ? 16 : 2) || !on(w_gate, in_place(d.n, d.ld_w) ? 16 : 2) || !on(w_up, in_place(d.n, d.ld_w) ? 16 : 2)) return GWS_ERR_ALIGN;
   const int64_t need = forward_bytes(desc, f), kept = saved_bytes(desc);
   if (clash({rows_of(h, d.m, d.n, d.ld_h), {save_gate, kept}, {save_up, kept}, {workspace, need}},
@@ -677,7 +707,7 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
       (wants_dx && (!on(w_gate, moves_w ? 2 : 16) || !on(w_up, moves_w ? 2 : 16))))
     return GWS_ERR_ALIGN;
   const int sms = sm_count();
-  const BackLayout l = back_layout(desc, sms);
+  const BackLayout& l = back_layout(desc, sms);
   const int64_t kept = saved_bytes(desc);
   const Span in_x = x8 ? Span{x, act8_total(d.m, d.k)} : rows_of(x, d.m, d.k, d.ld_x);
   if (clash({rows_of(grad_x, d.m, d.k, d.k), rows_of(grad_w_gate, d.n, d.k, d.k), rows_of(grad_w_up, d.n, d.k, d.k), rows_of(h_out, d.m, d.n, d.n),
