@@ -29,8 +29,14 @@
 // large square library product; the tensor pipe is busy 83 % of a launch on 4096 tokens, ends included.  Repeated for half a second
 // the same launches take 564, 609 and 600 us, the library's plain products of these shapes 600, 582 and 595 us.
 //
-// Every wait is bounded (about a second); a wait that runs out sets the status word, the roles of the block leave their loops,
-// the block gives its copies time to land, frees its tensor memory and returns.
+// Every wait of a role is a wait on an mbarrier and has a limit (about a second); one that runs out sets the status word and ends its
+// role, the roles that depend on it run out in turn, the block gives its copies time to land, frees its tensor memory and returns.
+// What has no limit waits for something that does not depend on a role's success:
+//   __syncthreads and the cluster barriers come after the roles' loops (or before them), where every warp arrives whatever happened;
+//   the allocation of tensor memory waits for blocks of other kernels on the SM: none of these kernels, since two blocks of them do not fit
+//   an SM (static_assert at TcShape), and no kernel behind this one on the stream, since none of them starts before all blocks of this one
+//   have their tensor memory;
+//   griddepcontrol.wait waits for the kernel before, which never waits for this one.
 #pragma once
 #include <cuda.h>
 #include <stdint.h>
@@ -336,6 +342,7 @@ struct TcShape {
   static constexpr uint32_t kRing = (kFit > 8u ? 8u : kFit) * kStage;
   static constexpr uint32_t kSmemBytes = kRing + kStaging + 1024u;
   static constexpr uint32_t kTmemCols = 2 * BN;
+  static_assert(2u * kSmemBytes > kTcSmem, "a block that holds tensor memory keeps other blocks of these kernels off its SM");
 };
 
 constexpr uint32_t kPartRow = 128u * 4u + 16u;      // bytes between rows of a part in shared memory: eight lanes' 16 bytes in different banks
@@ -403,7 +410,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
   const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kMnA ? 1u : 0u) << 15) | ((kMnB ? 1u : 0u) << 16) |
                          ((kFew ? width >> 2 : static_cast<uint32_t>(BN >> 3)) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], codes_full[kStages], converted[kStages];
+  __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], meet[4], codes_full[kStages], converted[kStages];
   __shared__ __align__(16) uint8_t scale_bytes[2][2][kIsGated ? 128 : 1][4];      // of two tiles, gate and up projection
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int failed;
@@ -424,6 +431,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       bar_init(&acc_full[b], 1);
       bar_init(&acc_empty[b], S::kEpilogueWarps * CG);
     }
+    for (int q = 0; q < 4; ++q) bar_init(&meet[q], 2);
     failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -578,8 +586,6 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       const uint32_t buf = n & 1u;
       if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) {
         failed = 1;
-        // the other warp of these rows may have seen the tile complete and wait for this one below
-        if (kIsGated) asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -650,13 +656,11 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         if (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3) {
           // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
           // The two warps that share these rows meet; one writes the gate's, the other the up projection's.  A warp that fills the same
-          // buffer again has passed the meeting of the tile between, and so has the other one's store.
+          // buffer again has passed the meeting of the tile between, and so has the other one's store.  They meet at an mbarrier, one
+          // phase a tile, because a wait there has a limit: a warp that left its loop does not leave the other one behind for good.
           __syncwarp();
-          asm volatile("bar.sync %0, 64;" ::"r"(quadrant + 1u) : "memory");
-          if (__any_sync(0xFFFFFFFFu, failed != 0)) {            // the other warp may have read it a moment earlier, as not set, and go on
-            asm volatile("bar.arrive %0, 64;" ::"r"(quadrant + 1u) : "memory");
-            break;
-          }
+          if (lane == 0) bar_arrive(smem_addr(&meet[quadrant]));
+          if (!bar_wait(smem_addr(&meet[quadrant]), n & 1u)) { failed = 1; break; }
           const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (width / 32u);
           if (row < p.rows) {
             uint8_t* to = p.save8[half].scales + row * ld + g0;
