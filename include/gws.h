@@ -498,9 +498,9 @@ int gws_noise_compare(const gws_desc* desc, int noise_kind, void* out, void* str
  * costs a copy into the workspace; outputs and grad_h take any 2-byte alignment.  Sizes may be zero: sums over nothing are zero.
  * `workspace` is device memory, 256-byte aligned, of the size its *_workspace_bytes call gives for the same arguments (NULL
  * where that is 0).  `status` is as for gws_gemm_fused.  An output or the workspace that overlaps an input or another output is
- * GWS_ERR_ALIAS.  NaN and infinities in the inputs follow IEEE arithmetic.  The kernels of these calls are launched so that their blocks
- * may become resident while the kernel before them on the stream drains, and wait for it before they touch memory
- * (gws_set_launch_overlap does not change that).  The self-checking build does not watch them. */
+ * GWS_ERR_ALIAS.  The buffers and the stream belong to the current device.  NaN and infinities in the inputs follow IEEE
+ * arithmetic.  The kernels of these calls are launched so that their blocks may become resident while the kernel before them on
+ * the stream drains, and wait for it before they touch memory (gws_set_launch_overlap does not change that).  The self-checking build does not watch them. */
 typedef enum gws_act_format {
   GWS_ACT8_INT8 = 0,
   GWS_ACT8_E4M3 = 1,

@@ -562,10 +562,20 @@ _BF16 = torch.bfloat16
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _on_stream(stream, device, call, *args, **kwargs):
-    """Runs a call with ``stream`` current, so that what it allocates belongs to the stream it launches on."""
+    """Runs a call with the tensors' device current, and on it ``stream`` (None: that device's current stream), so that what it allocates
+    belongs to the stream it launches on.  The library launches, and asks for the number of SMs, on the current device, and the handle of a
+    default stream does not say whose it is."""
+    if stream is None:
+        with torch.cuda.device(device):
+            return call(*args, **kwargs)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError("gws: the stream belongs to cuda:%d, the tensors to cuda:%d" % (stream.device_index, device))
     with torch.cuda.stream(stream):
         return call(*args, **kwargs)
 
@@ -634,7 +644,7 @@ def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None,
     device = x.get_device() if out is None else _device_of(x, out.buffer)
     if device < 0:
         _require_cuda(x)
-    if stream is not None:
+    if stream is not None or device != _current_device():
         return _on_stream(stream, device, act8_save, x, fmt, out)
     x, p, ld, rows, cols = _bf16_rows(x, "x", read_by_map=False)
     if out is None:
@@ -652,7 +662,7 @@ def act8_load(a: Act8, x: Optional[torch.Tensor] = None, stream=None) -> torch.T
     device = a.buffer.get_device() if x is None else _device_of(a.buffer, x)
     if device < 0:
         _require_cuda(a.buffer)
-    if stream is not None:
+    if stream is not None or device != _current_device():
         return _on_stream(stream, device, act8_load, a, x)
     rows, cols, ld = a.rows, a.cols, a.cols
     if x is None:
@@ -677,7 +687,7 @@ def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = 
                stream=None) -> torch.Tensor:
     """dW = grad_y^T @ x for a linear layer y = x W^T whose input is held as a checkpoint.  BF16 [n, k]."""
     device = _device_of(grad_y, x8.buffer, grad_w, status)
-    if stream is not None:
+    if stream is not None or device != _current_device():
         return _on_stream(stream, device, wgrad_act8, grad_y, x8, grad_w, status)
     m, k = x8.rows, x8.cols
     grad_y, p, ld, _, n = _bf16_rows(grad_y, "grad_y", m)
@@ -753,7 +763,7 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
     """h = act(x Wg^T) * (x Wu^T) for x [m, k] and weights [n, k], in one kernel.  Returns (h, saved): ``save`` says what the gate
     and the up projection are kept as for :func:`gated_bwd` (ACT8_INT8, ACT8_E4M3, SAVE_BF16; SAVE_NONE keeps nothing)."""
     device = _device_of(x, w_gate, w_up, h, status)
-    if stream is not None:
+    if stream is not None or device != _current_device():
         return _on_stream(stream, device, gated_fwd, x, w_gate, w_up, activation, save, h, status)
     x, p_x, ld_x, m, k = _bf16_rows(x, "x")
     n = w_gate.shape[0]
@@ -779,7 +789,7 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     what was not asked for is None.  ``h`` is act(gate) * up again, which the weight gradient of the layer after the block needs."""
     kept_x = isinstance(x, Act8)
     device = _device_of(grad_h, x.buffer if kept_x else x, w_gate, w_up, saved.buffer, status)
-    if stream is not None:
+    if stream is not None or device != _current_device():
         return _on_stream(stream, device, gated_bwd, grad_h, x, w_gate, w_up, saved, activation, want_h, want_grad_x, want_grad_w, status)
     m, k = x.shape
     n = w_gate.shape[0]

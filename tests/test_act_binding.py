@@ -1,0 +1,87 @@
+"""Host side of the activation operators' Python calls, on CPU tensors that claim to live on a GPU and a library that only records."""
+import contextlib
+
+import pytest
+import torch
+
+import paper_2505_11170_b200 as gws
+from paper_2505_11170_b200 import binding
+
+
+class OnDevice(torch.Tensor):
+    """A CPU tensor that names GPU 1 as its device."""
+
+    def get_device(self):
+        return 1
+
+
+def _on_gpu(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnDevice)
+
+
+class FakeLibrary:
+    """Accepts every call and notes its name and the device that was current."""
+
+    def __init__(self, state):
+        self.calls, self.state = [], state
+
+    def __getattr__(self, name):
+        if not name.startswith("gws_"):
+            raise AttributeError(name)
+
+        def call(*args):
+            self.calls.append((name, self.state["device"], args[-1]))
+            return 0
+
+        return call
+
+
+@pytest.fixture
+def fake(monkeypatch):
+    state = {"device": 0}
+
+    @contextlib.contextmanager
+    def use(device):
+        before, state["device"] = state["device"], device
+        yield
+        state["device"] = before
+
+    lib = FakeLibrary(state)
+    monkeypatch.setattr(binding, "_lib", lib)
+    monkeypatch.setattr(binding, "_current_device", lambda: state["device"], raising=False)
+    monkeypatch.setattr(binding, "_raw_stream", lambda device: 1000 + device)
+    monkeypatch.setattr(torch.cuda, "device", use)
+    caches = (binding._wgrad_workspace, binding._gated_plan)
+    for cache in caches:
+        cache.cache_clear()
+    yield lib
+    for cache in caches:
+        cache.cache_clear()
+
+
+def _calls():
+    x, w, dy = _on_gpu(4, 64), _on_gpu(96, 64), _on_gpu(4, 96)
+    x8 = gws.Act8(_on_gpu(1024, dtype=torch.uint8), 4, 64, gws.ACT8_INT8)
+    saved = gws.GatedSaved(_on_gpu(4096, dtype=torch.uint8), 4, 96, gws.ACT8_INT8)
+    return {"act8_save": lambda **kw: gws.act8_save(x, **kw), "act8_load": lambda **kw: gws.act8_load(x8, **kw),
+            "wgrad_act8": lambda **kw: gws.wgrad_act8(dy, x8, **kw), "gated_fwd": lambda **kw: gws.gated_fwd(x, w, w, **kw),
+            "gated_bwd": lambda **kw: gws.gated_bwd(dy, x8, w, w, saved, **kw)}
+
+
+@pytest.mark.parametrize("name", ["act8_save", "act8_load", "wgrad_act8", "gated_fwd", "gated_bwd"])
+def test_tensors_of_another_gpu_than_the_current_one(fake, name):
+    # a default stream's handle is 0 on every device: the launch, and the sizes that depend on the device, need the tensors' device current
+    _calls()[name]()
+    assert fake.calls and all(device == 1 for _, device, _ in fake.calls)
+    assert fake.calls[-1][0] == "gws_" + name and fake.calls[-1][2] == 1001
+    assert fake.state["device"] == 0
+
+
+@pytest.mark.parametrize("name", ["act8_save", "act8_load", "wgrad_act8", "gated_fwd", "gated_bwd"])
+def test_a_stream_of_another_gpu_than_the_tensors_is_refused(fake, name):
+    class OtherStream:
+        cuda_stream, device_index = 5, 0
+
+    with pytest.raises(ValueError):
+        _calls()[name](stream=OtherStream())
+    assert not fake.calls
