@@ -523,6 +523,8 @@ class Act8:
     __slots__ = ("buffer", "rows", "cols", "fmt")
 
     def __init__(self, buffer: torch.Tensor, rows: int, cols: int, fmt: int):
+        if rows < 0 or cols < 0 or fmt not in (ACT8_INT8, ACT8_E4M3):
+            raise ValueError("gws: a checkpoint is (rows, cols) in ACT8_INT8 or ACT8_E4M3")
         if buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < _act8_bytes(rows, cols):
             raise ValueError("gws: a checkpoint is a contiguous uint8 tensor of at least %d bytes" % _act8_bytes(rows, cols))
         self.buffer, self.rows, self.cols, self.fmt = buffer, rows, cols, fmt
@@ -707,7 +709,21 @@ class GatedSaved:
     __slots__ = ("buffer", "m", "n", "fmt")
 
     def __init__(self, buffer: torch.Tensor, m: int, n: int, fmt: int):
+        if m < 0 or n < 0 or fmt not in (ACT8_INT8, ACT8_E4M3, SAVE_BF16):
+            raise ValueError("gws: kept projections are (m, n) in ACT8_INT8, ACT8_E4M3 or SAVE_BF16")
+        if buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < self._bytes(m, n, fmt):
+            raise ValueError("gws: the kept projections are a contiguous uint8 tensor of at least %d bytes" % self._bytes(m, n, fmt))
         self.buffer, self.m, self.n, self.fmt = buffer, m, n, fmt
+
+    @classmethod
+    def _new(cls, like: torch.Tensor, m: int, n: int, fmt: int) -> "GatedSaved":
+        s = cls.__new__(cls)
+        s.buffer, s.m, s.n, s.fmt = like.new_empty(cls._bytes(m, n, fmt), dtype=torch.uint8), m, n, fmt
+        return s
+
+    @staticmethod
+    def _bytes(m: int, n: int, fmt: int) -> int:
+        return 2 * GatedSaved._part(m, n, fmt)
 
     @staticmethod
     def _part(m: int, n: int, fmt: int) -> int:
@@ -774,7 +790,7 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
     h = _bf16_out(h, "h", m, n, x)
     saved = p_sg = p_su = None
     if save != SAVE_NONE:
-        saved = GatedSaved(x.new_empty(2 * GatedSaved._part(m, n, save), dtype=torch.uint8), m, n, save)
+        saved = GatedSaved._new(x, m, n, save)
         p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, x)
     code = (_lib or load_library()).gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, _addr(status), _raw_stream(device))

@@ -85,3 +85,35 @@ def test_a_stream_of_another_gpu_than_the_tensors_is_refused(fake, name):
     with pytest.raises(ValueError):
         _calls()[name](stream=OtherStream())
     assert not fake.calls
+
+
+def _bytes(n):
+    return torch.zeros(n, dtype=torch.uint8)
+
+
+@pytest.mark.parametrize("fmt", [gws.ACT8_INT8, gws.ACT8_E4M3, gws.SAVE_BF16])
+def test_kept_projections_refuse_a_buffer_that_a_kernel_would_read_past(fmt):
+    m, n = 5, 96
+    need = 2 * -(-(2 * m * n if fmt == gws.SAVE_BF16 else gws.act8_layout(m, n)[2]) // 256) * 256
+    kept = gws.GatedSaved(_bytes(need), m, n, fmt)
+    assert tuple(kept.gate.shape) == tuple(kept.up.shape) == (m, n)
+    for bad in (_bytes(need - 1), torch.zeros(need, dtype=torch.int8), torch.zeros(need // 2, dtype=torch.bfloat16), _bytes(2 * need)[::2], _bytes(0)):
+        with pytest.raises(ValueError):
+            gws.GatedSaved(bad, m, n, fmt)
+    for shape in ((-m, -n), (-1, n), (m, -1)):
+        with pytest.raises(ValueError):
+            gws.GatedSaved(_bytes(need), *shape, fmt)
+
+
+@pytest.mark.parametrize("fmt", [gws.SAVE_NONE, -1, 7])
+def test_kept_values_refuse_a_format_they_cannot_have(fmt):
+    with pytest.raises(ValueError):
+        gws.GatedSaved(_bytes(1 << 16), 4, 32, fmt)
+    with pytest.raises(ValueError):
+        gws.Act8(_bytes(1 << 16), 4, 32, fmt)
+
+
+def test_a_checkpoint_refuses_negative_sizes():
+    for shape in ((-4, -32), (-1, 32), (4, -32)):
+        with pytest.raises(ValueError):
+            gws.Act8(_bytes(1 << 16), *shape, gws.ACT8_INT8)
