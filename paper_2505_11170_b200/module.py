@@ -16,6 +16,7 @@ as 8-bit activation checkpoints; ``GaussWSLinear(keep=...)`` keeps a single laye
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional
 
 import torch
@@ -62,8 +63,42 @@ class _PresampledWeight(torch.autograd.Function):
         return grad_w_hat, None
 
 
+class _NoSecondDerivative(torch.autograd.Function):
+    """Passes gradients on and raises where something is differentiated through them.  ``_`` requires grad, so that they do."""
+
+    @staticmethod
+    def forward(ctx, _, *grads):
+        return tuple(g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("gws: the kernels behind this gradient have no derivative of their own (second derivatives are not supported)")
+
+
+def _no_second(*grads):
+    """The gradients that a backward pass returns, as they are, or (under create_graph) such that their differentiation is an error: what
+    the kernels write carries no graph, and would otherwise count as constant.  torch's once_differentiable does not see this where the
+    incoming gradient is a constant, as that of a sum is, and the dependence runs through the saved tensors alone."""
+    if not torch.is_grad_enabled():
+        return grads
+    passed = iter(_NoSecondDerivative.apply(torch.empty(0, requires_grad=True), *[g for g in grads if g is not None]))
+    return tuple(None if g is None else next(passed) for g in grads)
+
+
+def _refuses_a_second(backward):
+    """For the backward of a Function of which no part can be differentiated again."""
+
+    @functools.wraps(backward)
+    def once(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        return _no_second(*out)
+
+    return once
+
+
 class _KeptLinear(torch.autograd.Function):
-    """y = x W^T with x kept as an 8-bit checkpoint; dW = dY^T x from it (gws_wgrad_act8)."""
+    """y = x W^T with x kept as an 8-bit checkpoint; dW = dY^T x from it (gws_wgrad_act8).  Second derivatives are refused."""
 
     @staticmethod
     def forward(ctx, x, w, fmt):
@@ -74,6 +109,7 @@ class _KeptLinear(torch.autograd.Function):
         return torch.nn.functional.linear(x, w)
 
     @staticmethod
+    @_refuses_a_second
     def backward(ctx, grad_y):
         w, buffer = ctx.saved_tensors
         rows = grad_y.reshape(-1, grad_y.shape[-1])
@@ -84,7 +120,7 @@ class _KeptLinear(torch.autograd.Function):
 
 class _GatedMLP(torch.autograd.Function):
     """y = (act(x Wg^T) * (x Wu^T)) Wd^T.  Kept for the backward pass: x, x Wg^T and x Wu^T in the given format; the hidden activation is
-    formed again from them."""
+    formed again from them.  Second derivatives are refused."""
 
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, activation, fmt):
@@ -98,6 +134,7 @@ class _GatedMLP(torch.autograd.Function):
         return torch.nn.functional.linear(h, w_down).view(*x.shape[:-1], w_down.shape[0])
 
     @staticmethod
+    @_refuses_a_second
     def backward(ctx, grad_y):
         x_kept, w_gate, w_up, w_down, kept = ctx.saved_tensors
         m, k, n, fmt = ctx.kept
