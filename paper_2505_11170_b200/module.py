@@ -25,44 +25,6 @@ from . import binding
 from .binding import Desc
 
 
-class _SampledWeight(torch.autograd.Function):
-    """(w, b_i) -> w_hat with the gradients of Eq. 4 and Eq. 11 / Eq. 12."""
-
-    @staticmethod
-    def forward(ctx, w, bi, desc, b_init, b_target, lam, update):
-        bt = binding.bitwidth(bi.detach(), b_init, b_target)
-        w_hat, scale = binding.sample_fwd(desc, w.detach(), bt)
-        ctx.save_for_backward(scale, bt)
-        ctx.desc, ctx.hyper, ctx.update = desc, (b_init, b_target, lam), update
-        return w_hat
-
-    @staticmethod
-    def backward(ctx, grad_w_hat):
-        scale, bt = ctx.saved_tensors
-        b_init, b_target, lam = ctx.hyper
-        g = grad_w_hat.contiguous()
-        _, grad_bt = binding.sample_bwd(ctx.desc, g, scale)                 # dL/dw is dL/dw_hat itself (Eq. 4)
-        # Eq. 12 adds its term once per gradient update, however many micro-batches are accumulated into b_i.grad:
-        # the first backward pass of an update carries it, the others are the plain chain rule.
-        first = ctx.update["lambda_term_due"]
-        ctx.update["lambda_term_due"] = False
-        grad_bi = binding.bitwidth_grad(grad_bt, bt, b_init, b_target, lam if first else 0.0)
-        return g, grad_bi, None, None, None, None, None
-
-
-class _PresampledWeight(torch.autograd.Function):
-    """w -> the w_hat a GaussWSSet has already written for this update; dL/dw = dL/dw_hat (Eq. 4).  The gradient of b_i is
-    formed once per update by GaussWSSet.finish_backward from the accumulated dL/dw."""
-
-    @staticmethod
-    def forward(ctx, w, w_hat):
-        return w_hat.view_as(w_hat)
-
-    @staticmethod
-    def backward(ctx, grad_w_hat):
-        return grad_w_hat, None
-
-
 class _NoSecondDerivative(torch.autograd.Function):
     """Passes gradients on and raises where something is differentiated through them.  ``_`` requires grad, so that they do."""
 
@@ -95,6 +57,44 @@ def _refuses_a_second(backward):
         return _no_second(*out)
 
     return once
+
+
+class _SampledWeight(torch.autograd.Function):
+    """(w, b_i) -> w_hat with the gradients of Eq. 4 and Eq. 11 / Eq. 12."""
+
+    @staticmethod
+    def forward(ctx, w, bi, desc, b_init, b_target, lam, update):
+        bt = binding.bitwidth(bi.detach(), b_init, b_target)
+        w_hat, scale = binding.sample_fwd(desc, w.detach(), bt)
+        ctx.save_for_backward(scale, bt)
+        ctx.desc, ctx.hyper, ctx.update = desc, (b_init, b_target, lam), update
+        return w_hat
+
+    @staticmethod
+    def backward(ctx, grad_w_hat):
+        scale, bt = ctx.saved_tensors
+        b_init, b_target, lam = ctx.hyper
+        g = grad_w_hat.contiguous()
+        _, grad_bt = binding.sample_bwd(ctx.desc, g, scale)                 # dL/dw is dL/dw_hat itself (Eq. 4)
+        # Eq. 12 adds its term once per gradient update, however many micro-batches are accumulated into b_i.grad:
+        # the first backward pass of an update carries it, the others are the plain chain rule.
+        first = ctx.update["lambda_term_due"]
+        ctx.update["lambda_term_due"] = False
+        grad_bi, = _no_second(binding.bitwidth_grad(grad_bt, bt, b_init, b_target, lam if first else 0.0))
+        return g, grad_bi, None, None, None, None, None
+
+
+class _PresampledWeight(torch.autograd.Function):
+    """w -> the w_hat a GaussWSSet has already written for this update; dL/dw = dL/dw_hat (Eq. 4).  The gradient of b_i is
+    formed once per update by GaussWSSet.finish_backward from the accumulated dL/dw."""
+
+    @staticmethod
+    def forward(ctx, w, w_hat):
+        return w_hat.view_as(w_hat)
+
+    @staticmethod
+    def backward(ctx, grad_w_hat):
+        return grad_w_hat, None
 
 
 class _KeptLinear(torch.autograd.Function):

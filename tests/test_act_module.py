@@ -88,3 +88,17 @@ def test_create_graph_alone_changes_nothing(plain):
     frozen = [w.detach() for w in weights]
     grad_x, = torch.autograd.grad(_block(x, frozen).sum(), x, create_graph=True)
     assert grad_x.shape == x.shape and grad_x.requires_grad
+
+
+def test_a_second_derivative_through_the_gradient_of_the_bit_widths_is_refused(monkeypatch):
+    monkeypatch.setattr(binding, "bitwidth", lambda bi, *_: bi)
+    monkeypatch.setattr(binding, "sample_fwd", lambda desc, w, bt: (w.clone(), torch.ones_like(bt)))
+    monkeypatch.setattr(binding, "sample_bwd", lambda desc, g, scale: (None, g.detach().sum(1)))
+    monkeypatch.setattr(binding, "bitwidth_grad", lambda grad_bt, *_: grad_bt.detach())
+    w, bi = _rand(1, 6, 8).requires_grad_(), _rand(2, 6).requires_grad_()
+    w_hat = module._SampledWeight.apply(w, bi, None, 6.0, 4.0, 0.0, {"lambda_term_due": True})
+    grad_w, grad_bi = torch.autograd.grad(w_hat.pow(2).sum(), [w, bi], create_graph=True)
+    second, = torch.autograd.grad(grad_w.sum(), w, retain_graph=True)       # dL/dw is dL/dw_hat: its graph is torch's
+    assert torch.equal(second, torch.full_like(w, 2.0))
+    with pytest.raises(RuntimeError):
+        (grad_bi.pow(2).sum() + w_hat.sum()).backward()
