@@ -605,6 +605,21 @@ int gws_selfcheck_report(uint64_t* out5);
  * 0 flat groups, 1 warp per row, 2 thread block per row, 3 general; negative gws_status on error. */
 int gws_kernel_class(const gws_desc* desc);
 
+/* How the matrix products of the activation operators are carried out for given sizes and strides (host arithmetic; the number of SMs is
+ * the current device's, 148 without one). */
+typedef struct gws_product_plan {
+  int32_t blocks, columns;         /* a tile: 128 * blocks rows (1, or 2 for a pair of SMs) by `columns` of accumulator           */
+  int32_t narrow;                  /* forward, up to 128 tokens: columns of h in a narrow tile, 0 for other tiles                */
+  int32_t whole, cut, splits;      /* tiles computed in one piece, and tiles whose contraction is cut into `splits` parts       */
+  int32_t clustered;               /* the parts of a tile are the blocks of a cluster, not joined by a second launch             */
+  int32_t inside;                  /* weight gradients from a checkpoint: codes converted inside the product, not restored before */
+  int32_t moves_x, moves_w;        /* forward: x, both weights are copied to rows of whole lines first                           */
+  int32_t waves;                   /* times that a block takes a tile or a part                                                  */
+} gws_product_plan;
+/* product: 0 h (forward), 1 grad_x, 2 the pair of weight gradients (backward; x as desc->x_format says) */
+int gws_gated_plan(const gws_gated_desc* desc, int product, gws_product_plan* plan);
+int gws_wgrad_act8_plan(int64_t m, int64_t n, int64_t k, int64_t ld_y, gws_product_plan* plan);
+
 const char* gws_status_string(int status);
 /* Text of the last CUDA error this thread saw inside the library ("" if none). */
 const char* gws_last_cuda_error(void);

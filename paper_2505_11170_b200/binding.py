@@ -97,6 +97,8 @@ _SIGNATURES = {
     "gws_wgrad_act8_workspace_bytes": (c_int64, [c_int64, c_int64, c_int64, c_int64]),
     "gws_wgrad_act8": (c_int, [c_int64, c_int64, c_int64, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_size_t, c_void_p, c_void_p]),
     "gws_gated_workspace_bytes": (c_int64, [c_void_p, c_int]),
+    "gws_gated_plan": (c_int, [c_void_p, c_int, c_void_p]),
+    "gws_wgrad_act8_plan": (c_int, [c_int64, c_int64, c_int64, c_int64, c_void_p]),
     "gws_gated_fwd": (c_int, [c_void_p] * 8 + [c_size_t, c_void_p, c_void_p]),
     "gws_gated_bwd": (c_int, [c_void_p] * 12 + [c_size_t, c_void_p, c_void_p]),
     "gws_layer_seed": (c_uint64, [c_uint64, c_uint64]),
@@ -509,6 +511,29 @@ class GatedDesc(Structure):
     """Mirror of ``gws_gated_desc``."""
     _fields_ = [("m", c_int64), ("n", c_int64), ("k", c_int64), ("ld_x", c_int64), ("ld_w", c_int64), ("ld_h", c_int64),
                 ("activation", c_int32), ("save_format", c_int32), ("x_format", c_int32), ("reserved", c_int32)]
+
+
+class ProductPlan(Structure):
+    """Mirror of ``gws_product_plan``: how a matrix product of these operators is carried out."""
+    _fields_ = [(name, c_int32) for name in ("blocks", "columns", "narrow", "whole", "cut", "splits", "clustered", "inside", "moves_x", "moves_w", "waves")]
+
+    def __repr__(self):
+        return "ProductPlan(%s)" % ", ".join("%s=%d" % (name, getattr(self, name)) for name, _ in self._fields_)
+
+
+def gated_plan(m: int, n: int, k: int, product: str, ld_x: Optional[int] = None, ld_w: Optional[int] = None, save: int = SAVE_NONE,
+               x_format: int = SAVE_BF16) -> ProductPlan:
+    """Plan of a product of the gated block for x [m, k] and weights [n, k]: "h" (forward), "grad_x" or "grad_w".  Host only."""
+    plan, d = ProductPlan(), GatedDesc(m, n, k, k if ld_x is None else ld_x, k if ld_w is None else ld_w, n, GATED_SILU, save, x_format, 0)
+    _check(load_library().gws_gated_plan(ctypes.addressof(d), ("h", "grad_x", "grad_w").index(product), ctypes.addressof(plan)))
+    return plan
+
+
+def wgrad_act8_plan(m: int, n: int, k: int, ld_y: Optional[int] = None) -> ProductPlan:
+    """Plan of :func:`wgrad_act8` for grad_y [m, n] (rows ``ld_y`` apart) and a checkpoint [m, k].  Host only."""
+    plan = ProductPlan()
+    _check(load_library().gws_wgrad_act8_plan(m, n, k, n if ld_y is None else ld_y, ctypes.addressof(plan)))
+    return plan
 
 
 def act8_layout(rows: int, cols: int):

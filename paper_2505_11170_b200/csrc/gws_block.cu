@@ -527,6 +527,19 @@ int launch_pre_act(const PreArgs& p, Ready& ready, int act, bool fast, cudaStrea
   return launch_pre<SAVE, GWS_GATED_RELU>(p, ready, fast, s);
 }
 
+void describe(const Tile& t, int sms, gws_product_plan* p) {
+  std::memset(p, 0, sizeof *p);
+  p->blocks = t.cg;
+  p->columns = t.width != 0 ? static_cast<int32_t>(2 * t.width) : t.bn;
+  p->narrow = static_cast<int32_t>(t.width);
+  p->whole = static_cast<int32_t>(t.whole);
+  p->cut = static_cast<int32_t>(t.cut);
+  p->splits = static_cast<int32_t>(t.splits);
+  p->clustered = t.clustered;
+  const uint32_t work = t.whole + t.cut * t.splits, slots = static_cast<uint32_t>(sms / t.cg);
+  p->waves = t.clustered ? 1 : static_cast<int32_t>((work + slots - 1) / slots);
+}
+
 bool workspace_ok(const void* p, size_t have, int64_t need) { return need == 0 || (p != nullptr && on(p, 256) && have >= static_cast<size_t>(need)); }
 
 }  // namespace
@@ -610,6 +623,40 @@ int64_t gws_gated_workspace_bytes(const gws_gated_desc* desc, int backward) {
   if (st != GWS_OK) return st;
   if (desc->m == 0 || desc->n == 0 || desc->k == 0) return 0;
   return backward != 0 ? back_layout(desc, sm_count()).total : forward_bytes(desc, plan_forward(desc, sm_count()));
+}
+
+int gws_gated_plan(const gws_gated_desc* desc, int product, gws_product_plan* plan) {
+  if (plan == nullptr) return GWS_ERR_NULL;
+  const int st = check_gated(desc);
+  if (st != GWS_OK) return st;
+  if (product < 0 || product > 2) return GWS_ERR_UNSUPPORTED;
+  std::memset(plan, 0, sizeof *plan);
+  if (desc->m == 0 || desc->n == 0 || desc->k == 0) return GWS_OK;
+  const int sms = sm_count();
+  if (product == 0) {
+    const ForwardPlan& f = plan_forward(desc, sms);
+    describe(f.tile, sms, plan);
+    plan->moves_x = f.move_x;
+    plan->moves_w = f.move_w;
+  } else {
+    const BackLayout& l = back_layout(desc, sms);
+    describe(product == 1 ? l.dx : l.dw.tile, sms, plan);
+    plan->inside = product == 2 && l.dw.inside;
+  }
+  return GWS_OK;
+}
+
+int gws_wgrad_act8_plan(int64_t m, int64_t n, int64_t k, int64_t ld_y, gws_product_plan* plan) {
+  if (plan == nullptr) return GWS_ERR_NULL;
+  const int st = check_dims(m, n, k);
+  if (st != GWS_OK) return st;
+  std::memset(plan, 0, sizeof *plan);
+  if (m == 0 || n == 0 || k == 0) return GWS_OK;
+  const int sms = sm_count();
+  const DwChoice dw = choose_dw(m, n, k, 1, true, !in_place(m, ld_y), sms);
+  describe(dw.tile, sms, plan);
+  plan->inside = dw.inside;
+  return GWS_OK;
 }
 
 int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate, const void* w_up, void* h, void* save_gate, void* save_up,

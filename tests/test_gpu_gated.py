@@ -248,8 +248,8 @@ def test_on_another_stream_than_the_current_one():
     assert all(torch.equal(p, q) for outs in got for p, q in zip(outs, want)) and len(noise) == 40
 
 
-# sizes that between them take every tile (one block of 128 x 128, a pair of 256 x 128 and of 256 x 256), in one wave and in several, for each
-# of the three products whole, cut and joined, cut in a cluster, and whole but for a cut last wave
+# sizes that take many of the tiles (one block of 128 x 128, a pair of 256 x 128 and of 256 x 256) and forms (whole, cut and joined, cut in a
+# cluster, whole but for a cut last wave); test_tilings.py holds one for each form of each product and checks that it is taken
 TILINGS = [(41, 89, 1076), (10781, 73, 68), (772, 1416, 276), (48, 66, 412), (9722, 235, 1350), (1404, 2389, 260), (32, 312, 89), (7448, 79, 526),
            (170, 4024, 195), (3254, 1779, 686), (6749, 1685, 668), (1487, 90, 139), (34, 3895, 268), (8874, 152, 69), (5522, 3570, 264), (4548, 1834, 1242),
            (2530, 136, 910), (15024, 1213, 192), (19150, 128, 2048)]
