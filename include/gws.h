@@ -497,10 +497,13 @@ int gws_noise_compare(const gws_desc* desc, int noise_kind, void* out, void* str
  * multiple of 8 want a 16-byte aligned base where a tensor map reads the tensor (x, grad_y, weights) and any other stride
  * costs a copy into the workspace; outputs and grad_h take any 2-byte alignment.  Sizes may be zero: sums over nothing are zero.
  * `workspace` is device memory, 256-byte aligned, of the size its *_workspace_bytes call gives for the same arguments (NULL
- * where that is 0).  `status` is as for gws_gemm_fused.  An output or the workspace that overlaps an input or another output is
+ * where that is 0).  `status`: one int that the device can write (device memory, or pinned host memory, which the host may read while
+ * kernels run) or NULL: set to 1 if a block gave up waiting for a copy, for the tensor core or for another block (about a second); the
+ * outputs of that call are then undefined.  Never set otherwise.  An output or the workspace that overlaps an input or another output is
  * GWS_ERR_ALIAS.  The buffers and the stream belong to the current device.  NaN and infinities in the inputs follow IEEE
  * arithmetic.  The kernels of these calls are launched so that their blocks may become resident while the kernel before them on
- * the stream drains, and wait for it before they touch memory (gws_set_launch_overlap does not change that).  The self-checking build does not watch them. */
+ * the stream drains, and wait for it before they touch memory (gws_set_launch_overlap does not change that).  The self-checking
+ * build does not watch them. */
 typedef enum gws_act_format {
   GWS_ACT8_INT8 = 0,
   GWS_ACT8_E4M3 = 1,
@@ -619,6 +622,11 @@ typedef struct gws_product_plan {
 /* product: 0 h (forward), 1 grad_x, 2 the pair of weight gradients (backward; x as desc->x_format says) */
 int gws_gated_plan(const gws_gated_desc* desc, int product, gws_product_plan* plan);
 int gws_wgrad_act8_plan(int64_t m, int64_t n, int64_t k, int64_t ld_y, gws_product_plan* plan);
+
+/* Limit of the waits inside the matrix products of gws_wgrad_act8, gws_gated_fwd and gws_gated_bwd, in SM cycles; process-wide, read at
+ * every launch, 2e9 when the library is loaded and for cycles <= 0.  Returns the previous one.  For tests of what follows when a wait
+ * runs out: with a limit of a few cycles a sound launch gives up, and ends as it would on a fault. */
+int64_t gws_set_wait_limit(int64_t cycles);
 
 const char* gws_status_string(int status);
 /* Text of the last CUDA error this thread saw inside the library ("" if none). */

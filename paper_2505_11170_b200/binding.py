@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import threading
 from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int8, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 from typing import List, Optional, Sequence
 
@@ -101,6 +102,7 @@ _SIGNATURES = {
     "gws_wgrad_act8_plan": (c_int, [c_int64, c_int64, c_int64, c_int64, c_void_p]),
     "gws_gated_fwd": (c_int, [c_void_p] * 8 + [c_size_t, c_void_p, c_void_p]),
     "gws_gated_bwd": (c_int, [c_void_p] * 12 + [c_size_t, c_void_p, c_void_p]),
+    "gws_set_wait_limit": (c_int64, [c_int64]),
     "gws_layer_seed": (c_uint64, [c_uint64, c_uint64]),
     "gws_sample_fwd_multi_static": (c_int, [c_int, POINTER(Desc), POINTER(_MultiPtrs), c_uint64, c_void_p]),
     "gws_sample_step_host": (c_int, [POINTER(Desc)] + [c_void_p] * 13),
@@ -666,6 +668,53 @@ def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+# The status word of every call that was given none: one int in pinned host memory for the life of the process.  A kernel whose wait runs
+# out writes it there, and the next call (or check_waits) finds it without waiting for the device.
+_watch: Optional[c_int32] = None
+_watch_tensor: Optional[torch.Tensor] = None
+_watch_address: Optional[int] = None
+_watch_lock = threading.Lock()
+
+
+def _start_watch() -> None:
+    global _watch, _watch_tensor, _watch_address
+    with _watch_lock:
+        if _watch is None:
+            _watch_tensor = torch.zeros(1, dtype=torch.int32, pin_memory=True)
+            _watch_address = _watch_tensor.data_ptr()
+            _watch = c_int32.from_address(_watch_address)
+
+
+def _status_of(status: Optional[torch.Tensor]) -> int:
+    """The address of a call's status word.  Raises if a kernel of an earlier call has given up."""
+    if _watch is None:
+        _start_watch()
+    if _watch.value:
+        check_waits(synchronize=False)
+    if status is None:
+        return _watch_address
+    if status.dtype is not torch.int32 or status.numel() < 1:
+        raise ValueError("gws: status is an int32 tensor")
+    return status.data_ptr()
+
+
+def check_waits(synchronize: bool = True) -> None:
+    """Raises GwsError if a kernel of :func:`wgrad_act8`, :func:`gated_fwd` or :func:`gated_bwd` gave up a wait (about a second without an
+    answer inside the GPU), in which case the outputs of its call are undefined.  Every later call of these functions, and a module's
+    ``advance``, check the same without waiting; ``synchronize`` waits for the current device first, so that all calls made so far count.
+    Calls with a ``status`` of their own report there instead."""
+    if synchronize:
+        torch.cuda.synchronize()
+    if _watch is not None and _watch.value:
+        _watch.value = 0
+        raise GwsError(ERR_CUDA, "a kernel of an earlier call gave up a wait; the outputs of that call are undefined")
+
+
+def set_wait_limit(cycles: int) -> int:
+    """Limit of a wait inside those kernels in SM cycles, for tests (0: the default of about a second); returns the previous one."""
+    return int(load_library().gws_set_wait_limit(cycles))
+
+
 def act8_save(x: torch.Tensor, fmt: int = ACT8_INT8, out: Optional[Act8] = None, stream=None) -> Act8:
     """BF16 [rows, cols] -> 8-bit checkpoint (``out`` is overwritten if given)."""
     device = x.get_device() if out is None else _device_of(x, out.buffer)
@@ -716,12 +765,13 @@ def wgrad_act8(grad_y: torch.Tensor, x8: Act8, grad_w: Optional[torch.Tensor] = 
     device = _device_of(grad_y, x8.buffer, grad_w, status)
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, wgrad_act8, grad_y, x8, grad_w, status)
+    p_st = _status_of(status)
     m, k = x8.rows, x8.cols
     grad_y, p, ld, _, n = _bf16_rows(grad_y, "grad_y", m)
     grad_w = _bf16_out(grad_w, "grad_w", n, k, grad_y)
     nbytes = _wgrad_workspace(m, n, k, ld, device)
     ws, ws_p = _workspace(nbytes, grad_y)
-    code = (_lib or load_library()).gws_wgrad_act8(m, n, k, x8.fmt, p, ld, x8.buffer.data_ptr(), grad_w.data_ptr(), k or 1, ws_p, nbytes, _addr(status),
+    code = (_lib or load_library()).gws_wgrad_act8(m, n, k, x8.fmt, p, ld, x8.buffer.data_ptr(), grad_w.data_ptr(), k or 1, ws_p, nbytes, p_st,
                                                    _raw_stream(device))
     if code:
         _check(code)
@@ -806,6 +856,7 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
     device = _device_of(x, w_gate, w_up, h, status)
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, gated_fwd, x, w_gate, w_up, activation, save, h, status)
+    p_st = _status_of(status)
     x, p_x, ld_x, m, k = _bf16_rows(x, "x")
     n = w_gate.shape[0]
     w_gate, w_up, p_gate, p_up, ld_w = _two_weights(w_gate, w_up, n, k)
@@ -818,7 +869,7 @@ def gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
         saved = GatedSaved._new(x, m, n, save)
         p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, x)
-    code = (_lib or load_library()).gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, _addr(status), _raw_stream(device))
+    code = (_lib or load_library()).gws_gated_fwd(at, p_x, p_gate, p_up, h.data_ptr(), p_sg, p_su, ws_p, nbytes, p_st, _raw_stream(device))
     if code:
         _check(code)
     return h, saved
@@ -832,6 +883,7 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     device = _device_of(grad_h, x.buffer if kept_x else x, w_gate, w_up, saved.buffer, status)
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, gated_bwd, grad_h, x, w_gate, w_up, saved, activation, want_h, want_grad_x, want_grad_w, status)
+    p_st = _status_of(status)
     m, k = x.shape
     n = w_gate.shape[0]
     grad_h, p_dh, ld_h, _, _ = _bf16_rows(grad_h, "grad_h", m, n, read_by_map=False)
@@ -850,7 +902,7 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     p_sg, p_su = saved._addresses()
     ws, ws_p = _workspace(nbytes, grad_h)
     code = (_lib or load_library()).gws_gated_bwd(at, p_dh, p_x, p_gate, p_up, p_sg, p_su, _addr(grad_x), _addr(grad_wg), _addr(grad_wu),
-                                        _addr(h), ws_p, nbytes, _addr(status), _raw_stream(device))
+                                        _addr(h), ws_p, nbytes, p_st, _raw_stream(device))
     if code:
         _check(code)
     return grad_x, grad_wg, grad_wu, h

@@ -205,6 +205,8 @@ struct Ready {
   }
 };
 
+std::atomic<int64_t> g_wait_limit{kTcWaitCycles};
+
 // ---- choice of tile --------------------------------------------------------------------------------------------------------
 int sm_count() {
   static std::atomic<int> known[64];             // per device
@@ -345,6 +347,7 @@ TcArgs base_args(const Tile& t, int64_t rows, int64_t cols, int64_t len, int seg
   a.rows = rows;
   a.cols = cols;
   a.status = status;
+  a.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
   return a;
 }
 
@@ -545,6 +548,8 @@ bool workspace_ok(const void* p, size_t have, int64_t need) { return need == 0 |
 }  // namespace
 
 extern "C" {
+
+int64_t gws_set_wait_limit(int64_t cycles) { return g_wait_limit.exchange(cycles > 0 ? cycles : kTcWaitCycles, std::memory_order_relaxed); }
 
 int gws_act8_layout(int64_t rows, int64_t cols, size_t* codes_bytes, size_t* scales_offset, size_t* total_bytes) {
   const int st = check_dims(rows, cols, 0);

@@ -29,7 +29,7 @@
 // large square library product; the tensor pipe is busy 83 % of a launch on 4096 tokens, ends included.  Repeated for half a second
 // the same launches take 564, 609 and 600 us, the library's plain products of these shapes 600, 582 and 595 us.
 //
-// Every wait of a role is a wait on an mbarrier and has a limit (about a second); one that runs out sets the status word and ends its
+// Every wait of a role is a wait on an mbarrier and has a limit (about a second); one that runs out has the status word set and ends its
 // role, the roles that depend on it run out in turn, the block gives its copies time to land, frees its tensor memory and returns.
 // What has no limit waits for something that does not depend on a role's success:
 //   __syncthreads and the cluster barriers come after the roles' loops (or before them), where every warp arrives whatever happened;
@@ -51,7 +51,8 @@ constexpr uint32_t kTcHalf = 64;                           // elements along the
 constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
 constexpr uint32_t kTcSmem = 227u * 1024u;
 constexpr uint32_t kTcStagingWarp = 32u * 17u * 4u;        // a 32 x 32 BF16 block per epilogue warp, rows 17 words apart
-constexpr long long kTcWaitCycles = 2000000000LL;
+constexpr long long kTcWaitCycles = 2000000000LL;         // limit of a wait, unless gws_set_wait_limit gave another one
+constexpr long long kTcLandCycles = 125000000LL;          // what a block that gave up leaves its copies and products to end
 
 struct TcArgs {
   uint32_t m_tiles, n_tiles;              // tiles along rows (all outputs), along columns
@@ -78,6 +79,7 @@ struct TcArgs {
   Act8View save8[2];
   uint16_t* save16[2];                    // BF16 copies, [rows, cols]
   int* status;
+  int64_t wait_limit;
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -107,7 +109,7 @@ __device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void bar_arrive(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// A whole warp waits for the phase of the given parity; false, for every lane, if it did not complete within kTcWaitCycles.  The
+// A whole warp waits for the phase of the given parity; false, for every lane, if it did not complete within `limit` cycles.  The
 // clock is only read once the first try has failed: the two warps that feed the tensor cores pass here once per stage.
 // CLUSTER: what the other block of the pair wrote before it arrived is visible afterwards.
 template <bool CLUSTER = false>
@@ -135,12 +137,12 @@ __device__ __forceinline__ bool bar_peek(uint32_t addr, uint32_t parity) {
   return done != 0;
 }
 template <bool CLUSTER = false>
-__device__ __forceinline__ bool bar_wait(uint32_t addr, uint32_t parity) {
+__device__ __forceinline__ bool bar_wait(uint32_t addr, uint32_t parity, long long limit) {
   if (__all_sync(0xFFFFFFFFu, bar_try<CLUSTER>(addr, parity))) return true;
   const long long t0 = clock64();
   for (;;) {
     if (__all_sync(0xFFFFFFFFu, bar_try<CLUSTER>(addr, parity))) return true;
-    if (__any_sync(0xFFFFFFFFu, clock64() - t0 > kTcWaitCycles)) return false;
+    if (__any_sync(0xFFFFFFFFu, clock64() - t0 > limit)) return false;
   }
 }
 // One lane of a converged warp.  The loops around it are run by the whole warp, so that addresses and descriptors stay in
@@ -480,7 +482,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
       const int32_t n0 = static_cast<int32_t>(nt * (kIsGated ? width : BN) + (kIsGated ? 0u : rank * S::kBRows));
       for (uint32_t kb = k0; kb < k1; ++kb) {
-        if (!bar_wait(empty0 + 8u * s, parity)) { ok = false; break; }
+        if (!bar_wait(empty0 + 8u * s, parity, p.wait_limit)) { ok = false; break; }
         const bool seg = MODE == kDx && kb >= p.kb_first;
         const uint32_t k = (seg ? kb - p.kb_first : kb) * (S::kHalves * kTcHalf);
         const uint32_t halves = S::kHalves == 1u || k + kTcHalf >= p.len ? 1u : 2u;     // a second copy past the end is left out
@@ -524,7 +526,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     // Every release of a stage has to have arrived before this block's shared memory may become another block's: the signal of a commit
     // comes from the other SM of the pair, on its own time, and would count on whatever barrier lies there by then.
     for (uint32_t i = 0; ok && i < stages; ++i) {
-      ok = bar_wait(empty0 + 8u * s, parity);
+      ok = bar_wait(empty0 + 8u * s, parity, p.wait_limit);
       if (++s == stages) { s = 0; parity ^= 1u; }
     }
     if (!ok) failed = 1;
@@ -541,12 +543,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         uint32_t mt, nt, k0, k1;
         place(t, mt, nt, k0, k1);
         const uint32_t buf = n & 1u, d = tmem + buf * BN;
-        if (!bar_wait<CG == 2>(acc_empty0 + 8u * buf, ((n >> 1) & 1u) ^ 1u)) { ok = false; break; }
+        if (!bar_wait<CG == 2>(acc_empty0 + 8u * buf, ((n >> 1) & 1u) ^ 1u, p.wait_limit)) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         bool ready = bar_try(full0 + 8u * s, parity);
         for (uint32_t kb = k0; kb < k1; ++kb) {
-          if (!__all_sync(0xFFFFFFFFu, ready) && !bar_wait(full0 + 8u * s, parity)) { ok = false; break; }
-          if (MODE == kDw8 && !bar_wait<CG == 2>(smem_addr(&converted[s]), parity)) { ok = false; break; }
+          if (!__all_sync(0xFFFFFFFFu, ready) && !bar_wait(full0 + 8u * s, parity, p.wait_limit)) { ok = false; break; }
+          if (MODE == kDw8 && !bar_wait<CG == 2>(smem_addr(&converted[s]), parity, p.wait_limit)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t now = s;
           if (++s == stages) { s = 0; parity ^= 1u; }
@@ -573,7 +575,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       }
       // ... and so does every hand-back of an accumulator
       for (uint32_t back = 1; ok && back <= 2u && back <= n; ++back)
-        ok = bar_wait<CG == 2>(acc_empty0 + 8u * ((n - back) & 1u), ((n - back) >> 1) & 1u);
+        ok = bar_wait<CG == 2>(acc_empty0 + 8u * ((n - back) & 1u), ((n - back) >> 1) & 1u, p.wait_limit);
       if (!ok) failed = 1;
     }
   } else if (warp >= 4 && warp < 4u + S::kEpilogueWarps) {
@@ -584,7 +586,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       uint32_t mt, nt, k0, k1;
       place(t, mt, nt, k0, k1);
       const uint32_t buf = n & 1u;
-      if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u)) {
+      if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u, p.wait_limit)) {
         failed = 1;
         break;
       }
@@ -660,7 +662,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           // phase a tile, because a wait there has a limit: a warp that left its loop does not leave the other one behind for good.
           __syncwarp();
           if (lane == 0) bar_arrive(smem_addr(&meet[quadrant]));
-          if (!bar_wait(smem_addr(&meet[quadrant]), n & 1u)) { failed = 1; break; }
+          if (!bar_wait(smem_addr(&meet[quadrant]), n & 1u, p.wait_limit)) { failed = 1; break; }
           const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (width / 32u);
           if (row < p.rows) {
             uint8_t* to = p.save8[half].scales + row * ld + g0;
@@ -724,7 +726,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           const uint32_t kb = kb0 + 2u * d;
           if (kb >= k1) break;
           const uint32_t n = it + (kb - k0), s = n % kStages;
-          if (!bar_wait(smem_addr(&codes_full[s]), (n / kStages) & 1u)) { ok = false; break; }
+          if (!bar_wait(smem_addr(&codes_full[s]), (n / kStages) & 1u, p.wait_limit)) { ok = false; break; }
           const uint32_t halves = S::kHalves == 1u || kb * (S::kHalves * kTcHalf) + kTcHalf >= p.len ? 1u : 2u;
 #pragma unroll
           for (uint32_t h = 0; h < S::kHalves; ++h) {
@@ -780,9 +782,12 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
   }
   __syncthreads();
   if (failed) {                          // copies and products that were started get time to end before the memory is given up
-    if (threadIdx.x == 0 && p.status != nullptr) atomicExch(p.status, 1);
+    if (threadIdx.x == 0 && p.status != nullptr) {       // device memory, or pinned host memory that the host reads meanwhile
+      *static_cast<volatile int*>(p.status) = 1;
+      __threadfence_system();
+    }
     const long long t0 = clock64();
-    while (clock64() - t0 < kTcWaitCycles / 16) {}
+    while (clock64() - t0 < kTcLandCycles) {}
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();

@@ -181,7 +181,9 @@ class GaussWSLinear(torch.nn.Module):
         return Desc.make(self.out_features, self.in_features, self.group[0], self.group[1], seed=self.seed, step=self.step)
 
     def advance(self) -> None:
-        """One gradient update has been applied: the next forward pass draws new noise."""
+        """One gradient update has been applied: the next forward pass draws new noise.  Raises if a kernel of the update was found to have
+        given up (binding.check_waits)."""
+        binding.check_waits(synchronize=False)
         self.step += 1
         self._update["lambda_term_due"] = True
 
@@ -307,7 +309,9 @@ class GaussWSSet:
 
     def finish_backward(self, stream=None) -> None:
         """Eq. 4 for every layer from the accumulated dL/dw (one launch per kernel class), then Eq. 11 / Eq. 12: adds
-        dL'/db_i of this update to every layer's ``b_i.grad``.  Call once per update, after the last backward pass."""
+        dL'/db_i of this update to every layer's ``b_i.grad``.  Call once per update, after the last backward pass.  Raises, as ``advance``
+        does, if a kernel of the update was found to have given up (binding.check_waits)."""
+        binding.check_waits(synchronize=False)
         step = self._step()
         if self._sampled_step != step:
             raise RuntimeError("gws: finish_backward() belongs to the update that sample() started")

@@ -1,5 +1,6 @@
 """Host side of the activation operators' Python calls, on CPU tensors that claim to live on a GPU and a library that only records."""
 import contextlib
+import ctypes
 
 import pytest
 import torch
@@ -24,6 +25,9 @@ class FakeLibrary:
 
     def __init__(self, state):
         self.calls, self.state = [], state
+
+    def gws_status_string(self, status):
+        return b"status"
 
     def __getattr__(self, name):
         if not name.startswith("gws_"):
@@ -50,6 +54,8 @@ def fake(monkeypatch):
     monkeypatch.setattr(binding, "_lib", lib)
     monkeypatch.setattr(binding, "_current_device", lambda: state["device"], raising=False)
     monkeypatch.setattr(binding, "_raw_stream", lambda device: 1000 + device)
+    monkeypatch.setattr(binding, "_watch", ctypes.c_int32(0), raising=False)
+    monkeypatch.setattr(binding, "_watch_address", 0x7000, raising=False)
     monkeypatch.setattr(torch.cuda, "device", use)
     caches = (binding._wgrad_workspace, binding._gated_plan)
     for cache in caches:
@@ -117,3 +123,40 @@ def test_a_checkpoint_refuses_negative_sizes():
     for shape in ((-4, -32), (-1, 32), (4, -32)):
         with pytest.raises(ValueError):
             gws.Act8(_bytes(1 << 16), *shape, gws.ACT8_INT8)
+
+
+@pytest.mark.parametrize("name", ["wgrad_act8", "gated_fwd", "gated_bwd"])
+def test_a_kernel_that_gave_up_is_reported_by_the_next_call(fake, name):
+    call = _calls()[name]
+    call()
+    launched = len(fake.calls)
+    binding._watch.value = 1                        # as the kernel writes it
+    with pytest.raises(gws.GwsError):
+        call()
+    assert len(fake.calls) == launched              # before anything is launched, and once
+    call()
+    assert len(fake.calls) > launched
+
+
+def test_a_kernel_that_gave_up_is_reported_by_the_modules(fake):
+    from paper_2505_11170_b200.module import GaussWSLinear
+
+    layer = GaussWSLinear.__new__(GaussWSLinear)
+    torch.nn.Module.__init__(layer)
+    layer.step, layer._update = 3, {"lambda_term_due": False}
+    binding._watch.value = 1
+    with pytest.raises(gws.GwsError):
+        layer.advance()
+    assert layer.step == 3
+    layer.advance()
+    assert layer.step == 4
+
+
+@pytest.mark.parametrize("name", ["wgrad_act8", "gated_fwd", "gated_bwd"])
+def test_status_words_of_another_type_are_refused(fake, name):
+    call = _calls()[name]
+    for bad in (_on_gpu(1, dtype=torch.uint8), _on_gpu(1, dtype=torch.int64), _on_gpu(0, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            call(status=bad)
+    assert not fake.calls
+    call(status=_on_gpu(1, dtype=torch.int32))
