@@ -37,8 +37,9 @@ __device__ __forceinline__ void st32(void* p, const V8& v) {
 
 // These kernels are launched programmatically: a kernel's blocks may become resident while the one before it on the stream drains, and
 // touch global memory only once that one has completed.  Every kernel of this file set passes here before its first access, so
-// the order along the stream holds transitively.  The next kernel may follow once this one has seen its predecessor end, so that there
-// are never more than two on the device: blocks of a third would hold shared memory, tensor memory and barriers without a use for them.
+// the order along the stream holds transitively.  The next kernel may follow once this one has seen its predecessor end (as in the
+// kernels of the sampling pass), so that there are never more than two of the library's kernels of a stream on the device: blocks of a
+// third would hold shared memory, tensor memory and barriers without a use for them.
 __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

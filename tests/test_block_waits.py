@@ -24,3 +24,12 @@ def test_every_loop_on_an_mbarrier_reads_the_clock():
     text = open(os.path.join(_build.CSRC, "gws_tc.cuh")).read()
     loops = re.findall(r"for \(;;\) \{(.*?)\n  \}", text, re.S)
     assert loops and all("clock64()" in body for body in loops)
+
+
+def test_a_kernel_lets_the_next_one_in_only_after_its_own_wait():
+    # otherwise a third kernel of a stream becomes resident behind two that have not ended
+    files = [name for name in sorted(os.listdir(_build.CSRC)) if any("griddepcontrol" in p for p in _instructions(name))]
+    assert "gws_act8.cuh" in files and "gws_kernels.cuh" in files
+    for name in files:
+        order = re.findall(r"griddepcontrol\.(\w+)", " ".join(_instructions(name)))
+        assert order == ["wait", "launch_dependents"] * (len(order) // 2), name
