@@ -98,15 +98,15 @@ class _PresampledWeight(torch.autograd.Function):
 
 
 class _KeptLinear(torch.autograd.Function):
-    """y = x W^T with x kept as an 8-bit checkpoint; dW = dY^T x from it (gws_wgrad_act8).  Second derivatives are refused."""
+    """y = x W^T + bias with x kept as an 8-bit checkpoint; dW = dY^T x from it (gws_wgrad_act8).  Second derivatives are refused."""
 
     @staticmethod
-    def forward(ctx, x, w, fmt):
+    def forward(ctx, x, w, bias, fmt):
         rows = x.reshape(-1, x.shape[-1])
         kept = binding.act8_save(rows, fmt) if ctx.needs_input_grad[1] else None
         ctx.save_for_backward(w, None if kept is None else kept.buffer)
         ctx.kept, ctx.x_shape = (rows.shape[0], rows.shape[1], fmt), x.shape
-        return torch.nn.functional.linear(x, w)
+        return torch.nn.functional.linear(x, w, bias)
 
     @staticmethod
     @_refuses_a_second
@@ -115,7 +115,7 @@ class _KeptLinear(torch.autograd.Function):
         rows = grad_y.reshape(-1, grad_y.shape[-1])
         grad_x = (rows @ w).view(ctx.x_shape) if ctx.needs_input_grad[0] else None
         grad_w = binding.wgrad_act8(rows, binding.Act8(buffer, *ctx.kept)) if ctx.needs_input_grad[1] else None
-        return grad_x, grad_w, None
+        return grad_x, grad_w, rows.sum(0) if ctx.needs_input_grad[2] else None, None
 
 
 class _GatedMLP(torch.autograd.Function):
@@ -202,8 +202,7 @@ class GaussWSLinear(torch.nn.Module):
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         if self.keep is None:
             return torch.nn.functional.linear(x, self.sampled_weight(), self.bias)
-        y = _KeptLinear.apply(x, self.sampled_weight(), self.keep)
-        return y if self.bias is None else y + self.bias
+        return _KeptLinear.apply(x, self.sampled_weight(), self.bias, self.keep)
 
 
 class GaussWSGatedMLP(torch.nn.Module):

@@ -74,7 +74,7 @@ def test_a_second_derivative_through_the_block_is_refused(plain):
 @pytest.mark.parametrize("of", ["x", "w"])
 def test_a_second_derivative_through_a_layer_with_a_kept_input_is_refused(plain, of):
     x, w = _rand(1, 6, 8).requires_grad_(), _rand(2, 12, 8).requires_grad_()
-    y = module._KeptLinear.apply(x, w, gws.ACT8_INT8)
+    y = module._KeptLinear.apply(x, w, None, gws.ACT8_INT8)
     grad, = torch.autograd.grad(y.pow(2).sum(), {"x": x, "w": w}[of], create_graph=True)
     with pytest.raises(RuntimeError):
         (grad.pow(2).sum() + y.sum()).backward()
@@ -102,3 +102,21 @@ def test_a_second_derivative_through_the_gradient_of_the_bit_widths_is_refused(m
     assert torch.equal(second, torch.full_like(w, 2.0))
     with pytest.raises(RuntimeError):
         (grad_bi.pow(2).sum() + w_hat.sum()).backward()
+
+
+@pytest.mark.parametrize("bias", [True, False])
+@pytest.mark.parametrize("shape", [(40, 96), (2, 3, 96), (1, 96)])
+def test_a_layer_with_a_kept_input_rounds_its_output_once(plain, monkeypatch, bias, shape):
+    layer = module.GaussWSLinear(96, 72, bias=bias, group=(1, 24), device="cpu", keep=gws.ACT8_INT8)
+    monkeypatch.setattr(layer, "sampled_weight", lambda: layer.weight)
+    if bias:
+        torch.nn.init.normal_(layer.bias)
+    x = _rand(1, *shape).to(torch.bfloat16).requires_grad_()
+    y = layer(x)
+    assert torch.equal(y, torch.nn.functional.linear(x, layer.weight, layer.bias))
+    grad_y = _rand(2, *y.shape).to(torch.bfloat16)
+    tensors = [x, layer.weight] + ([layer.bias] if bias else [])
+    got = torch.autograd.grad(y, tensors, grad_y)
+    want = torch.autograd.grad(torch.nn.functional.linear(x, layer.weight, layer.bias), tensors, grad_y)
+    for p, q in zip(got, want):
+        assert p.shape == q.shape and torch.allclose(p, q, rtol=2.0 ** -6, atol=2.0 ** -6)

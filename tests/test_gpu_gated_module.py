@@ -180,3 +180,14 @@ def test_training_lowers_the_loss():
         sampler.advance()
         losses.append(float(loss))
     assert losses[-1] < 0.5 * losses[0]
+
+
+@pytest.mark.parametrize("shape", [(40, 96), (2, 3, 5, 96), (515, 96)])
+def test_a_kept_input_leaves_the_output_of_the_layer_as_it_was(shape):
+    torch.manual_seed(4)
+    kept = GaussWSLinear(96, 72, group=(1, 24), keep=gws.ACT8_INT8)
+    plain = GaussWSLinear(96, 72, group=(1, 24))
+    torch.nn.init.normal_(kept.bias)
+    plain.load_state_dict(kept.state_dict())
+    x = _x(shape, 8)
+    assert torch.equal(kept(x), plain(x))
