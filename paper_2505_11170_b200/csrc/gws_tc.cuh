@@ -242,7 +242,8 @@ __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
   }
   const float s = sigmoid(sigmoid_arg<ACT>(g));
   a = g * s;
-  const float dz = ACT == GWS_GATED_SILU ? 1.0f : __fmaf_rn(3.0f * 0.044715f * kGeluLin, g * g, kGeluLin);
+  // g^2 stays finite: beyond |g| = 2^50 the sigmoid is 0 or 1 and the term has to vanish, not become 0 times infinity
+  const float dz = ACT == GWS_GATED_SILU ? 1.0f : __fmaf_rn(3.0f * 0.044715f * kGeluLin, fminf(g * g, 0x1p100f), kGeluLin);
   slope = __fmaf_rn(a * (1.0f - s), dz, s);
 }
 

@@ -322,3 +322,21 @@ def test_many_steps_in_a_row_without_waiting_give_the_same_bits():
             del outs[1]
     first = outs[0]
     assert all(torch.equal(p, q) for o in outs for p, q in zip(o, first))
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("m,n", [(3, 70), (1200, 2048)])       # eight elements to a lane, a group to a thread
+def test_slopes_of_the_largest_finite_gates(act, m, n):
+    # from 2^60 to the end of BF16, where the square of a gate passes FP32: the slope is 1 on one side and 0 on the other
+    g = torch.exp2(torch.linspace(60, 127.9, n, device=DEV)).to(torch.bfloat16)
+    g[::2] = -g[::2]
+    buffer = torch.zeros(2 * gws.GatedSaved._part(m, n, gws.SAVE_BF16), dtype=torch.uint8, device=DEV)
+    saved = gws.GatedSaved(buffer, m, n, gws.SAVE_BF16)
+    saved.gate.copy_(g.expand(m, n))
+    saved.up.fill_(1.0)
+    x = torch.zeros(m, 8, dtype=torch.bfloat16, device=DEV)
+    x[0, 0] = 1.0                                               # dWg of the first input is dg of the first token
+    w = torch.zeros(n, 8, dtype=torch.bfloat16, device=DEV)
+    grad_h = torch.full((m, n), 2.0 ** -130, dtype=torch.bfloat16, device=DEV)
+    _, grad_wg, _, _ = gws.gated_bwd(grad_h, x, w, w, saved, act, want_grad_x=False)
+    assert torch.equal(grad_wg[:, 0], torch.where(g > 0, grad_h[0], torch.zeros_like(grad_h[0])))
