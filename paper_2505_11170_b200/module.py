@@ -159,6 +159,8 @@ class GaussWSLinear(torch.nn.Module):
     for the backward pass as an 8-bit checkpoint instead of in BF16.
     """
 
+    keep: Optional[int] = None          # of layers that were pickled whole before there was a choice
+
     def __init__(self, in_features: int, out_features: int, bias: bool = True, group=(32, 32), b_init: float = 6.0,
                  b_target: float = 4.0, lam: float = 0.0, user_seed: int = 0, layer_index: int = 0, device="cuda", keep: Optional[int] = None):
         super().__init__()

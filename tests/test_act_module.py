@@ -120,3 +120,11 @@ def test_a_layer_with_a_kept_input_rounds_its_output_once(plain, monkeypatch, bi
     want = torch.autograd.grad(torch.nn.functional.linear(x, layer.weight, layer.bias), tensors, grad_y)
     for p, q in zip(got, want):
         assert p.shape == q.shape and torch.allclose(p, q, rtol=2.0 ** -6, atol=2.0 ** -6)
+
+
+def test_a_layer_pickled_before_it_had_a_choice_of_keep_still_runs(monkeypatch):
+    layer = module.GaussWSLinear(32, 16, group=(1, 32), device="cpu")
+    del layer.__dict__["keep"]                                  # as such a pickle restores it
+    monkeypatch.setattr(layer, "sampled_weight", lambda: layer.weight)
+    x = _rand(1, 4, 32).to(torch.bfloat16)
+    assert torch.equal(layer(x), torch.nn.functional.linear(x, layer.weight, layer.bias))
