@@ -195,3 +195,14 @@ def test_weight_gradient_on_another_stream_than_the_current_one():
     noise = [torch.full((1 << 20,), 3, dtype=torch.uint8, device=DEV) for _ in range(20)]   # what the current stream allocates meanwhile
     side.synchronize()
     assert all(torch.equal(o, want) for o in outs) and len(noise) == 20
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m,n,k", [(515, 96, 200), (1072, 76, 17), (4369, 176, 200)])    # converted inside the product, restored before it
+def test_a_group_that_restores_as_nan_reaches_its_own_columns_of_the_weight_gradient(fmt, m, n, k):
+    gy, x = _x(m, n, seed=7, spread=False).to(DEV), _x(m, k, seed=8, spread=False).to(DEV)
+    clean = gws.wgrad_act8(gy, gws.act8_save(x, fmt))
+    x[m // 2, k - 1] = math.inf
+    got = gws.wgrad_act8(gy, gws.act8_save(x, fmt))
+    first = (k - 1) // 32 * 32
+    assert bool(torch.isnan(got[:, first:]).all()) and torch.equal(got[:, :first], clean[:, :first])

@@ -191,3 +191,18 @@ def test_a_kept_input_leaves_the_output_of_the_layer_as_it_was(shape):
     plain.load_state_dict(kept.state_dict())
     x = _x(shape, 8)
     assert torch.equal(kept(x), plain(x))
+
+
+def test_no_tokens_and_one():
+    for keep in (gws.ACT8_INT8, gws.SAVE_BF16):
+        block = _block(keep=keep)
+        for shape in ((0, 96), (2, 0, 96), (1, 96)):
+            x = _x(shape, 12).requires_grad_()
+            y = block(x)
+            assert y.shape == x.shape
+            y.sum().backward()
+            assert x.grad.shape == x.shape and all(bool(torch.isfinite(layer.weight.grad.float()).all()) for layer in block.layers)
+    layer = GaussWSLinear(96, 72, keep=gws.ACT8_INT8)
+    x = _x((0, 96), 13).requires_grad_()
+    layer(x).sum().backward()
+    assert x.grad.shape == (0, 96) and not bool(layer.weight.grad.any()) and not bool(layer.bias.grad.any())
