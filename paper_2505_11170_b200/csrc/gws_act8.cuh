@@ -158,7 +158,7 @@ struct Act8View {                 // a checkpoint in memory
 // ---- save / load -------------------------------------------------------------------------------------------------------
 // Memory-bound: 2 bytes of activation and 1 + 1/32 of checkpoint per element.  A thread takes a whole group - two 32-byte
 // accesses on the BF16 side, one on the code side, one scale byte - so the maximum needs no exchange between lanes.
-// 16384 x 5632: save and load together 87 us, 6.4 TB/s, the rate of a plain copy.  One token: latency, 2.5 us each.
+// 16384 x 5632: save and load together 83.5 us, 6.7 TB/s (a plain copy moves 6.5).  One token: latency, 2.5 us each.
 
 template <int FMT>
 __global__ void __launch_bounds__(256) k_act8_save(const uint16_t* x, int64_t ldx, Act8View c, int64_t groups, uint32_t per_row) {

@@ -370,7 +370,6 @@ void set_out(TcArgs& a, void* out0, void* out1, int64_t ld) {
 // accumulator rows that are not stored.
 uint32_t a_box(int64_t rows) { return static_cast<uint32_t>(std::min<int64_t>(128, round_up(rows, 8))); }
 
-// dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
 // Tile of a weight gradient, and whether a checkpointed X is converted inside the GEMM, by its own warps, rather than restored into the
 // workspace by a pass before it.  Inside, every tile converts its columns again, some 220 cycles a copy; the pass moves 3.1 bytes an
 // element and is a launch more unless one is made anyway (`before`).  Measured, inside against before, on the device: 515 tokens, 768 x
@@ -391,6 +390,7 @@ DwChoice choose_dw(int64_t tokens, int64_t rows, int64_t cols, int outs, bool ke
   return remembered<DwChoice>({tokens, rows, cols, outs, kept, before, sms}, [&] { return weigh_dw(tokens, rows, cols, outs, kept, before, sms); });
 }
 
+// dW (one or two outputs) = A^T X, A [m, rows] and X [m, cols] as they lie.
 // X: a BF16 matrix, or a checkpoint of the same shape (x8, format) to be converted inside.
 int run_dw(const Tile& t, const Mat& a0, const Mat* a1, const Mat& x, const Act8View* x8, int format, void* out0, void* out1, int64_t ld_out, void* part, int* status,
            int sms, cudaStream_t s) {
@@ -477,7 +477,7 @@ uint32_t few_stages(int64_t rows, uint32_t width) {
 // products that read 128 rows of A), or its bytes at 67 a cycle; a wave of tiles costs no less than its weights at 3400 bytes a cycle from
 // memory.  What narrow tiles win is an even share for every SM and more weights on their way (us, weights from memory, against the best of
 // choose): one token, 2048 x 5632, 40 columns 12.0 (13.1), 48 11.9, 64 12.3, 32 in two waves 16.1; 128 tokens 13.2 (13.5); one token, 4096 x 11008,
-// 40 columns 33.7 (42), 48 40.3, 64 42.5.  A long contraction into few columns is better cut: 5632 x 2048, 16 columns 18.1 (16.5).
+// 40 columns 33 (42), 48 40.3, 64 42.5.  A long contraction into few columns is better cut: 5632 x 2048, 16 columns 18.1 (16.5).
 // Checkpoints want whole groups of 32: 64 columns 13.1 (13.7), 32 16.9.
 Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, int sms) {
   const int64_t kb = stages_of(len, 128);

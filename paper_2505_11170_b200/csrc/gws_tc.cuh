@@ -5,7 +5,7 @@
 //            the product and the 8-bit copies for the backward pass happen on registers in the epilogue
 //   kGatedFew  the same for up to 128 tokens, tiles of 16 to 64 columns of h: every SM gets its share of the weights, and a copy of A
 //            takes only the rows that exist, so that the ring holds more weights in flight.  It is bound by the weights' way from
-//            memory and some 4 us around it (one token, 2048 x 5632: 46 MB in 11.9 us, 10.1 from L2; 4096 x 11008: 180 MB in 32 us)
+//            memory and some 4 us around it (one token, 2048 x 5632: 46 MB in 12 us, 10 from L2; 4096 x 11008: 180 MB in 33 us)
 //   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du
 //   kDw      dW = dY^T X: both operands are read along their contiguous (not the contracted) axis, as they lie in memory
 //   kDw8     the same with X an 8-bit checkpoint: its codes are copied to shared memory and eight more warps turn them into the BF16
@@ -27,7 +27,9 @@
 // What bounds it (16384 tokens, 2048 x 5632): the tensor cores and, beyond some milliseconds, the 1 kW power cap.  In a burst the forward
 // pass takes 477 us (1.58 PFLOP/s; 497 us with INT8 copies), dx 463 us and both dW 464 us (1.63 PFLOP/s) against 1.68 measured for a
 // large square library product; the tensor pipe is busy 83 % of a launch on 4096 tokens, ends included.  Repeated for half a second
-// the same launches take 564, 609 and 600 us, the library's plain products of these shapes 600, 582 and 595 us.
+// they take 557 to 564, 589 to 609 and 590 to 600 us (dx and dW with the element-wise pass's 137 us taken off), and torch.matmul on BF16
+// operands of the same sizes, [16384, 2048] by [11264, 2048]^T, [16384, 11264] by [11264, 2048] and [16384, 11264]^T by [16384, 2048],
+// 589 to 600, 568 to 582 and 577 to 595 us.
 //
 // Every wait of a role is a wait on an mbarrier and has a limit (about a second); one that runs out has the status word set and ends its
 // role, the roles that depend on it run out in turn, the block gives its copies time to land, frees its tensor memory and returns.
@@ -864,8 +866,10 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
 }
 
 // ---- the element-wise part of the backward pass ------------------------------------------------------------------------------
-// In one launch with what the products after it need made ready (prepare).  From dh and the saved g, u:  dg = dh u act'(g),  du = dh act(g),  and h = act(g) u for the next layer's weight gradient.  dg and
-// du are rounded to BF16 because the tensor cores take them in that form; their sums dx and dW are FP32 again.
+// From dh and the saved g, u:  dg = dh u act'(g),  du = dh act(g),  and h = act(g) u for the next layer's weight gradient.  dg and du are
+// rounded to BF16 because the tensor cores take them in that form; their sums dx and dW are FP32 again.  What that costs: the error of
+// the gradients against 64 bits is 2.3e-3 of their norm instead of the 1.65e-3 of their own rounding.
+// The first blocks of the launch make ready what the products after it read (prepare).
 struct PreArgs {
   const uint16_t* grad_h;
   int64_t ld_grad_h;
