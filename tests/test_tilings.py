@@ -31,12 +31,15 @@ FORWARD = [
     ((2, 256, "whole"), "xw", 904, 1212, 389), ((2, 256, "whole*"), "", 1059, 2912, 288), ((2, 256, "whole*"), "w", 5614, 856, 648),
     ((2, 256, "whole*"), "x", 850, 3944, 856), ((2, 256, "whole+cut"), "", 1044, 1864, 1184), ((2, 256, "whole+cut"), "w", 3761, 1256, 904),
     ((2, 256, "whole+cut"), "x", 1175, 1912, 1304), ((2, 256, "whole+cut"), "xw", 750, 3150, 1206),
+    ((1, 128, "whole+cut"), "", 1, 9495, 19848), ((2, 128, "cut*"), "xw", 6537, 9, 12066), ((2, 256, "cut"), "w", 3149, 72, 7304),
+    ((2, 256, "cut*"), "xw", 274, 1572, 17165),
 ]
 # dx: (path, m, n, k)
 GRAD_X = [
     ((1, 128, "cluster"), 3, 200, 136), ((1, 128, "cut"), 7, 3500, 136), ((1, 128, "whole*"), 1054, 11, 3779), ((2, 128, "cut"), 388, 1678, 140),
     ((2, 128, "cut*"), 1060, 5516, 1034), ((2, 128, "whole"), 129, 130, 72), ((2, 128, "whole*"), 19127, 40, 16), ((2, 128, "whole+cut"), 1259, 1240, 1800),
     ((2, 256, "cut"), 540, 3634, 1552), ((2, 256, "whole"), 9666, 15, 132), ((2, 256, "whole*"), 1157, 154, 3760), ((2, 256, "whole+cut"), 3653, 703, 1223),
+    ((1, 128, "whole"), 1, 8, 9), ((1, 128, "cut*"), 1, 3417, 10539), ((1, 128, "whole+cut"), 1, 402, 19330), ((2, 256, "cut*"), 6301, 7360, 132),
 ]
 # the pair of weight gradients: (path, x converted inside, restored before, or in BF16, m, n, k)
 GRAD_W = [
@@ -54,6 +57,9 @@ GRAD_W = [
     ((2, 128, "whole*"), "restored", 202, 552, 1816), ((2, 128, "whole+cut"), "restored", 1611, 1224, 1840), ((2, 256, "cut"), "restored", 7000, 1061, 446),
     ((2, 256, "cut*"), "restored", 16606, 1720, 408), ((2, 256, "whole"), "restored", 148, 513, 1860), ((2, 256, "whole*"), "restored", 261, 1056, 2144),
     ((2, 256, "whole+cut"), "restored", 1575, 3184, 696),
+    ((1, 128, "whole"), "bf16", 33, 97, 41), ((1, 128, "whole+cut"), "bf16", 1018, 10, 9566), ((1, 128, "whole"), "restored", 33, 97, 41),
+    ((1, 128, "whole*"), "inside", 79, 8, 10805), ((1, 128, "whole+cut"), "inside", 656, 11, 9537), ((2, 128, "whole*"), "inside", 91, 130, 20221),
+    ((2, 128, "whole+cut"), "inside", 4731, 11, 4776), ((2, 256, "whole+cut"), "inside", 1031, 143, 9735),
 ]
 # a layer's weight gradient from a checkpoint; several of the whole waves have an odd number of stages
 WGRAD = [
@@ -68,6 +74,7 @@ WGRAD = [
     ((2, 128, "whole*"), "restored", 209, 2051, 1082), ((2, 128, "whole+cut"), "restored", 2427, 1191, 1816), ((2, 256, "cut"), "restored", 7198, 1126, 937),
     ((2, 256, "cut*"), "restored", 15537, 1203, 1195), ((2, 256, "whole"), "restored", 132, 1300, 1725), ((2, 256, "whole*"), "restored", 285, 1826, 2497),
     ((2, 256, "whole+cut"), "restored", 1666, 3829, 1176),
+    ((1, 128, "whole"), "restored", 2, 10, 8), ((1, 128, "whole+cut"), "inside", 675, 9, 19652),
 ]
 
 
@@ -105,15 +112,22 @@ def test_plan_of_a_weight_gradient(path, x, m, n, k):
     assert (_path(plan), bool(plan.inside)) == (path, x == "inside")
 
 
-def test_the_lists_hold_every_path_there_is():
-    of = lambda entries, *which: {tuple(e[i] for i in which) for e in entries}
-    tiles = [(1, 128), (2, 128), (2, 256)]
-    for t in tiles:
-        assert {f for (*tile, f), in of(GRAD_X, 0) if tuple(tile) == t} >= {"whole*", "cut"} | ({"cluster"} if t == (1, 128) else {"whole+cut"})
-        assert {f for (*tile, f), in of(FORWARD, 0) if tuple(tile) == t} >= {"whole", "whole*"} | ({"cut"} if t != (2, 256) else {"whole+cut"})
-        for entries, kinds in ((GRAD_W, ("bf16", "inside", "restored")), (WGRAD, ("inside", "restored"))):
-            for kind in kinds:
-                assert {f for (*tile, f), x in of(entries, 0, 1) if tuple(tile) == t and x == kind} >= {"cut"} | ({"cluster"} if t == (1, 128) else {"whole"})
+def test_the_lists_hold_every_form_of_every_tile():
+    # what a search over some million sizes up to 70000 x 40000 x 40000 came upon
+    forms = {(1, 128): {"whole", "whole*", "cut", "cut*", "whole+cut", "cluster"}, (2, 128): {"whole", "whole*", "cut", "cut*", "whole+cut"},
+             (2, 256): {"whole", "whole*", "cut", "cut*", "whole+cut"}}
+
+    def held(entries, kind=None):
+        return {t: {e[0][2] for e in entries if e[0][:2] == t and (kind is None or e[1] == kind)} for t in forms}
+
+    without = lambda *left_out: {t: f - {x for tile, x in left_out if tile == t} for t, f in forms.items()}
+    assert {t: f for t, f in held([e for e in FORWARD if e[0][1] != "narrow"]).items()} == without(((1, 128), "cluster"), ((1, 128), "cut*"))
+    assert held(GRAD_X) == forms
+    assert held(GRAD_W, "bf16") == forms
+    assert held(GRAD_W, "restored") == without(((1, 128), "cut*"), ((1, 128), "whole+cut"))
+    assert held(GRAD_W, "inside") == without(((2, 128), "cut*"))
+    assert held(WGRAD, "restored") == without(((1, 128), "cut*"), ((1, 128), "whole+cut"))
+    assert held(WGRAD, "inside") == without(((2, 128), "cut*"))
 
 
 def test_plans_of_empty_and_impossible_sizes():
