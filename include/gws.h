@@ -556,6 +556,77 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
                   const void* save_up, void* grad_x, void* grad_w_gate, void* grad_w_up, void* h_out, void* workspace, size_t workspace_bytes,
                   int* status, void* stream);
 
+/* ---- the rest of a block's training step: layer norm, optimizer -----------------------------------------------------
+ * As above: BF16 tensors row-major with a row stride of at least their width, any 2-byte alignment (rows on 16-byte boundaries are
+ * fastest), sizes may be zero, outputs overlap neither inputs nor each other, everything is enqueued on `stream` of the current device. */
+typedef enum gws_type { GWS_TYPE_BF16 = 0, GWS_TYPE_F32 = 1 } gws_type;
+
+/* Layer norm over the rows of s = bf16(x + residual), or of x itself without a residual:
+ *   y = (s - mean) rstd weight + bias,   rstd = 1 / sqrt(mean((s - mean)^2) + eps)          (FP32; y rounded once) */
+typedef struct gws_norm_desc {
+  int64_t rows, cols;
+  int64_t ld_x, ld_residual;          /* row strides; ld_x is that of s in the backward call */
+  int64_t ld_grad_y, ld_grad_sum;     /* backward */
+  int32_t weight_type;                /* gws_type of weight, bias and their gradients */
+  float eps;
+} gws_norm_desc;
+/*   x         device, BF16 [rows, ld_x]         residual   device, BF16 [rows, ld_residual], or NULL
+ *   weight, bias  device, [cols]; both may be NULL (one and zero), or bias alone
+ *   y, sum    device, BF16 [rows, cols], dense, written; sum is s and only written (and needed) with a residual
+ *   stats     device, FP32 [2, rows], written: mean and rstd, which the backward call reads; may be NULL */
+int gws_layernorm_fwd(const gws_norm_desc* desc, const void* x, const void* residual, const void* weight, const void* bias, void* y, void* sum, float* stats,
+                      void* stream);
+/* Backward, with a = grad_y weight and xh = (s - mean) rstd:
+ *   grad_x = rstd (a - mean(a) - xh mean(a xh)) + grad_sum     (the gradient of x, of the residual and of s alike)
+ *   grad_weight = sum over rows of grad_y xh,   grad_bias = sum over rows of grad_y
+ *   grad_y    device, BF16 [rows, ld_grad_y]    s   device, BF16 [rows, ld_x]    stats  as the forward call wrote them
+ *   grad_sum  device, BF16 [rows, ld_grad_sum], or NULL: the gradient that reaches s past the norm
+ *   grad_x    device, BF16 [rows, cols], dense, written     grad_weight, grad_bias  device, [cols] of weight_type, written
+ * Each of the outputs may be NULL; the workspace is only needed for the last two. */
+int64_t gws_layernorm_workspace_bytes(const gws_norm_desc* desc);
+int gws_layernorm_bwd(const gws_norm_desc* desc, const void* grad_y, const void* s, const void* weight, const float* stats, const void* grad_sum, void* grad_x,
+                      void* grad_weight, void* grad_bias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One AdamW step over many tensors at once (one launch for up to 384 of them):
+ *   g = grad * grad_scale     m = b1 m + (1 - b1) g     v = b2 v + (1 - b2) g g     r = sqrt(v)
+ *   p = p (1 - lr wd) - (m alpha) / (r rho + eps),     alpha = lr / (1 - b1^step),  rho = 1 / sqrt(1 - b2^step)
+ * in FP32, every operation rounded once in the order written (alpha, rho and 1 - lr wd are computed in double and rounded once).
+ *
+ * State: tensor i owns the elements [starts[i], starts[i] + sizes[i] rounded up to 256) of arrays of `total` elements that all tensors share
+ * (starts and total are multiples of 256; the elements past a size are kept zero; all of the state is zero before the first step).
+ *   GWS_ADAMW_F32   moments: FP32 [2, total], m and v
+ *   GWS_ADAMW_8BIT  moments: bytes [2, total], units: FP32 [2, total / 256], one per group of 256 elements.
+ *       m = E4M3 value of its code * unit, unit = max|m| * (1/448).  v = r r, r = q * unit, unit = max r * (1/1.9375), q = (1 + f/16) 2^(e - 15) for
+ *       code 16 e + f, 0 for code 0.  Codes are value * (1 / unit) rounded to nearest even; a root above zero has a code of at least 1.  A group whose
+ *       largest value is below 2^-100 is stored as zeros with unit 0, one that is not finite has a NaN for its unit and restores as NaN.
+ *   rest            int16 [total], or NULL.  With it a BF16 parameter stands for the 32-bit weight whose bits are (its bits << 16) + rest; the
+ *       parameter is the nearest BF16 number to it, the one larger in magnitude of two as near.  Without it a BF16 parameter is rounded to nearest
+ *       even at every step.  FP32 parameters leave it alone. */
+typedef enum gws_adamw_format { GWS_ADAMW_F32 = 0, GWS_ADAMW_8BIT = 1 } gws_adamw_format;
+typedef struct gws_adamw_state {
+  void* moments; /* 32-byte aligned */
+  float* units;
+  void* rest; /* 16-byte aligned */
+  int64_t total;
+  int32_t format;
+  int32_t reserved;
+} gws_adamw_state;
+typedef struct gws_adamw_step_args {
+  double lr, beta1, beta2, eps;
+  int64_t step;            /* from 1 */
+  const float* grad_scale; /* device, one FP32, or NULL: 1 */
+  const float* lr_dev;     /* device, one FP32, instead of lr; or NULL                                                                        */
+  const int64_t* step_dev; /* device, instead of step; or NULL.  A captured step that is replayed reads both as they are then               */
+  float* scalars;          /* device, 3 FP32, written: needed with lr_dev or step_dev                                                        */
+} gws_adamw_step_args;
+/* params, grads, sizes, starts, types (gws_type of the parameter and of its gradient) and weight_decay are host arrays of n_tensors entries, read
+ * before the call returns; a tensor whose gradient is NULL is left alone.  Tensors are dense, in any 2-byte (4-byte) alignment; those of which the parameter and the
+ * gradient lie on boundaries of eight elements are fastest.  A tensor, or a part of the state, that is given twice is GWS_ERR_ALIAS. */
+int gws_adamw_step(int n_tensors, void* const* params, const void* const* grads, const int64_t* sizes, const int64_t* starts, const int32_t* types,
+                   const double* weight_decay, const gws_adamw_state* state, const gws_adamw_step_args* args, void* stream);
+/* What 8-bit moments stand for: m and v, device, FP32 [total], 32-byte aligned, written. */
+int gws_adamw_values(const gws_adamw_state* state, float* m, float* v, void* stream);
+
 /* ---- diagnostics -----------------------------------------------------------------------------*/
 
 /* Raw Philox4x32-10 output words for vectors first_vec .. first_vec+n_vec-1 (4 words each):

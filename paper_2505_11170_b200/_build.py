@@ -10,18 +10,19 @@ _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libgws.so")
-# Two translation units: the sampling pass (gws_api.cu) and the activation operators (gws_block.cu).
+# Translation units: the sampling pass (gws_api.cu), the activation operators (gws_block.cu), layer norm and optimizer (gws_step.cu).
 _UNITS = {
     "gws_api.cu": ["gws_kernels.cuh", "gws_math.cuh", "gws_gemm.cuh", "gws_probe.cuh", "gws_compare.cuh", "gws_gemm_cluster.cuh", "gws_gemm_wide.cuh",
                    "gws_train.cuh", "gws_internal.h"],
-    "gws_block.cu": ["gws_tc.cuh", "gws_act8.cuh", "gws_internal.h"],
+    "gws_block.cu": ["gws_tc.cuh", "gws_act8.cuh", "gws_host.h", "gws_internal.h"],
+    "gws_step.cu": ["gws_norm.cuh", "gws_adamw.cuh", "gws_act8.cuh", "gws_host.h", "gws_internal.h"],
 }
 SOURCES = [os.path.join(CSRC, name) for name in _UNITS]
 HEADERS = sorted({os.path.join(CSRC, h) for hs in _UNITS.values() for h in hs}) + [os.path.join(INCLUDE, "gws.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
 # -fmad=false: the add-then-cast path must round the multiply and the add separately.
-_UNIT_FLAGS = {"gws_api.cu": ["-fmad=false"], "gws_block.cu": []}
+_UNIT_FLAGS = {"gws_api.cu": ["-fmad=false"], "gws_block.cu": [], "gws_step.cu": []}
 
 
 def _nvcc() -> str:

@@ -102,6 +102,11 @@ _SIGNATURES = {
     "gws_wgrad_act8_plan": (c_int, [c_int64, c_int64, c_int64, c_int64, c_void_p]),
     "gws_gated_fwd": (c_int, [c_void_p] * 8 + [c_size_t, c_void_p, c_void_p]),
     "gws_gated_bwd": (c_int, [c_void_p] * 12 + [c_size_t, c_void_p, c_void_p]),
+    "gws_layernorm_workspace_bytes": (c_int64, [c_void_p]),
+    "gws_layernorm_fwd": (c_int, [c_void_p] * 9),
+    "gws_layernorm_bwd": (c_int, [c_void_p] * 10 + [c_size_t, c_void_p]),
+    "gws_adamw_step": (c_int, [c_int] + [c_void_p] * 9),
+    "gws_adamw_values": (c_int, [c_void_p] * 4),
     "gws_set_wait_limit": (c_int64, [c_int64]),
     "gws_layer_seed": (c_uint64, [c_uint64, c_uint64]),
     "gws_sample_fwd_multi_static": (c_int, [c_int, POINTER(Desc), POINTER(_MultiPtrs), c_uint64, c_void_p]),
@@ -906,6 +911,260 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     if code:
         _check(code)
     return grad_x, grad_wg, grad_wu, h
+
+
+class NormDesc(Structure):
+    """Mirror of ``gws_norm_desc``."""
+    _fields_ = [("rows", c_int64), ("cols", c_int64), ("ld_x", c_int64), ("ld_residual", c_int64), ("ld_grad_y", c_int64), ("ld_grad_sum", c_int64),
+                ("weight_type", c_int32), ("eps", c_float)]
+
+
+TYPE_BF16, TYPE_F32 = 0, 1
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_plan(m: int, n: int, ld_x: int, ld_r: int, ld_dy: int, ld_d: int, weight_type: int, eps: float, device: int):
+    """(descriptor, its address, workspace bytes of the backward call)."""
+    d = NormDesc(m, n, ld_x, ld_r, ld_dy, ld_d, weight_type, eps)
+    at = ctypes.addressof(d)
+    nbytes = load_library().gws_layernorm_workspace_bytes(at)
+    if nbytes < 0:
+        raise GwsError(int(nbytes))
+    return d, at, nbytes
+
+
+def _norm_weights(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], n: int):
+    """(weight, bias, gws_type) as the library takes them."""
+    if weight is None:
+        if bias is not None:
+            raise ValueError("gws: a norm with a bias has a weight")
+        return None, None, TYPE_BF16
+    dtype = weight.dtype
+    if dtype is not _BF16 and dtype is not torch.float32:
+        raise ValueError("gws: the weight of a norm is BF16 or FP32")
+    for t in (weight, bias):
+        if t is not None and (t.dtype is not dtype or t.shape != (n,)):
+            raise ValueError("gws: weight and bias of a norm are (%d,) tensors of one type" % n)
+    return weight.contiguous(), None if bias is None else bias.contiguous(), TYPE_BF16 if dtype is _BF16 else TYPE_F32
+
+
+def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  residual: Optional[torch.Tensor] = None, want_stats: bool = True, stream=None):
+    """Layer norm of the rows of s = x + residual, or of x, for BF16 [m, n] tensors; weight and bias are BF16 or FP32 [n], or None.  Returns (y, s, stats): s is x itself
+    without a residual, stats (FP32 [2, m], mean and reciprocal deviation) is what :func:`layernorm_bwd` reads, None if it is not wanted."""
+    device = _device_of(x, weight, bias, residual)
+    if stream is not None or device != _current_device():
+        return _on_stream(stream, device, layernorm_fwd, x, weight, bias, eps, residual, want_stats)
+    x, p_x, ld_x, m, n = _bf16_rows(x, "x", read_by_map=False)
+    weight, bias, kind = _norm_weights(weight, bias, n)
+    total, p_r, ld_r, p_sum = x, None, 0, None
+    if residual is not None:
+        residual, p_r, ld_r, _, _ = _bf16_rows(residual, "residual", m, n, read_by_map=False)
+        total = x.new_empty(m, n)
+        p_sum = total.data_ptr()
+    y = x.new_empty(m, n)
+    stats = x.new_empty(2, m, dtype=torch.float32) if want_stats else None
+    _, at, _ = _norm_plan(m, n, ld_x, ld_r, 0, 0, kind, eps, device)
+    code = (_lib or load_library()).gws_layernorm_fwd(at, p_x, p_r, _addr(weight), _addr(bias), y.data_ptr(), p_sum, _addr(stats), _raw_stream(device))
+    if code:
+        _check(code)
+    return y, total, stats
+
+
+def layernorm_bwd(grad_y: torch.Tensor, s: torch.Tensor, weight: Optional[torch.Tensor], stats: torch.Tensor, grad_sum: Optional[torch.Tensor] = None,
+                  want_grad_x: bool = True, want_grad_weight: bool = True, want_grad_bias: bool = True, stream=None):
+    """Backward pass of :func:`layernorm_fwd` from the s and the stats that it returned.  ``grad_sum`` is the gradient that reaches s past the norm.  Returns
+    (grad_x, grad_weight, grad_bias), None for what is not wanted; grad_x is the gradient of x, of the residual and of s alike.  Without a weight
+    the last two are None."""
+    device = _device_of(grad_y, s, weight, stats, grad_sum)
+    if stream is not None or device != _current_device():
+        return _on_stream(stream, device, layernorm_bwd, grad_y, s, weight, stats, grad_sum, want_grad_x, want_grad_weight, want_grad_bias)
+    s, p_s, ld_s, m, n = _bf16_rows(s, "s", read_by_map=False)
+    grad_y, p_dy, ld_dy, _, _ = _bf16_rows(grad_y, "grad_y", m, n, read_by_map=False)
+    weight, _, kind = _norm_weights(weight, None, n)
+    if stats.dtype is not torch.float32 or stats.shape != (2, m) or not stats.is_contiguous():
+        raise ValueError("gws: stats is the FP32 [2, %d] tensor of the forward call" % m)
+    p_d, ld_d = None, 0
+    if grad_sum is not None:
+        grad_sum, p_d, ld_d, _, _ = _bf16_rows(grad_sum, "grad_sum", m, n, read_by_map=False)
+    grad_x = grad_y.new_empty(m, n) if want_grad_x else None
+    grad_weight = torch.empty_like(weight) if weight is not None and want_grad_weight else None
+    grad_bias = torch.empty_like(weight) if weight is not None and want_grad_bias else None
+    _, at, nbytes = _norm_plan(m, n, ld_s, 0, ld_dy, ld_d, kind, 0.0, device)
+    if grad_weight is None and grad_bias is None:
+        nbytes = 0
+    ws, ws_p = _workspace(nbytes, grad_y)
+    code = (_lib or load_library()).gws_layernorm_bwd(at, p_dy, p_s, _addr(weight), stats.data_ptr(), p_d, _addr(grad_x), _addr(grad_weight), _addr(grad_bias), ws_p,
+                                                      nbytes, _raw_stream(device))
+    if code:
+        _check(code)
+    return grad_x, grad_weight, grad_bias
+
+
+ADAMW_F32, ADAMW_8BIT = 0, 1
+_ADAMW_GROUP = 256
+
+
+class _AdamwState(Structure):
+    _fields_ = [("moments", c_void_p), ("units", c_void_p), ("rest", c_void_p), ("total", c_int64), ("format", c_int32), ("reserved", c_int32)]
+
+
+class _AdamwArgs(Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", c_int64),
+                ("grad_scale", c_void_p), ("lr_dev", c_void_p), ("step_dev", c_void_p), ("scalars", c_void_p)]
+
+
+@functools.lru_cache(maxsize=64)
+def _adamw_layout(sizes: tuple):
+    """(starts, total, sizes and starts as C arrays)."""
+    starts, total = [], 0
+    for n in sizes:
+        if n < 0:
+            raise ValueError("gws: sizes are numbers of elements")
+        starts.append(total)
+        total += -(-n // _ADAMW_GROUP) * _ADAMW_GROUP
+    return tuple(starts), total, (c_int64 * len(sizes))(*sizes), (c_int64 * len(sizes))(*starts)
+
+
+class AdamWState:
+    """The state of :func:`adamw_step` for tensors of the given numbers of elements: arrays of ``total`` elements in which tensor i starts at ``starts[i]``, a
+    multiple of 256.
+
+    ``moments`` and ``units`` are FP32 [2, total] and None (ADAMW_F32), or uint8 [2, total] and FP32 [2, total / 256] (ADAMW_8BIT: one byte per element and moment,
+    groups of 256 with an FP32 unit).  ``rest`` holds the 16 bits that a 32-bit weight has below its BF16 parameter (int16 [total]); without it, None, BF16
+    parameters are rounded at every step and lose updates smaller than half their spacing.  What is not given is allocated, as zeros; ``rest`` may be
+    True, False, or such a tensor."""
+    __slots__ = ("sizes", "starts", "total", "fmt", "moments", "units", "rest", "_c_sizes", "_c_starts", "_c")
+
+    def __init__(self, sizes: Sequence[int], fmt: int = ADAMW_F32, rest=False, device="cuda", moments: Optional[torch.Tensor] = None,
+                 units: Optional[torch.Tensor] = None):
+        if fmt not in (ADAMW_F32, ADAMW_8BIT):
+            raise ValueError("gws: the format of moments is ADAMW_F32 or ADAMW_8BIT")
+        self.sizes, self.fmt = tuple(sizes), fmt
+        self.starts, total, self._c_sizes, self._c_starts = _adamw_layout(self.sizes)
+        self.total = total
+        bits8 = fmt == ADAMW_8BIT
+        if moments is None:
+            if units is not None:
+                raise ValueError("gws: units come with their moments")
+            moments = torch.zeros(2, total, dtype=torch.uint8 if bits8 else torch.float32, device=device)
+            units = torch.zeros(2, total // _ADAMW_GROUP, device=device) if bits8 else None
+        if rest is True:
+            rest = torch.zeros(total, dtype=torch.int16, device=moments.device)
+        elif rest is False:
+            rest = None
+        self._take(moments, "moments", torch.uint8 if bits8 else torch.float32, (2, total))
+        if bits8 or units is not None:
+            self._take(units, "units", torch.float32, (2, total // _ADAMW_GROUP) if bits8 else None)
+        if rest is not None:
+            self._take(rest, "rest", torch.int16, (total,))
+        self.moments, self.units, self.rest = moments, units, rest
+        self._c = _AdamwState(moments.data_ptr(), _addr(units), _addr(rest), total, fmt, 0)
+
+    @staticmethod
+    def _take(t, name, dtype, shape) -> None:
+        if shape is None or not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError("gws: %s must be a contiguous %s tensor of shape %s" % (name, dtype, shape) if shape is not None else "gws: FP32 moments have no units")
+
+    def values(self, stream=None):
+        """(m, v) in FP32, [total] each: of FP32 moments the state's own, of 8-bit ones new tensors."""
+        if self.fmt == ADAMW_F32:
+            return self.moments[0], self.moments[1]
+        device = _device_of(self.moments, self.units)
+        if stream is not None or device != _current_device():
+            return _on_stream(stream, device, self.values)
+        out = torch.empty(2, self.total, dtype=torch.float32, device=self.moments.device)
+        m, v = out[0], out[1]
+        code = (_lib or load_library()).gws_adamw_values(ctypes.addressof(self._c), m.data_ptr(), v.data_ptr(), _raw_stream(device))
+        if code:
+            _check(code)
+        return m, v
+
+    def weight(self, index: int, param: torch.Tensor) -> torch.Tensor:
+        """The 32-bit weight of tensor ``index``: of a BF16 parameter together with its rest."""
+        if param.dtype is not _BF16 or self.rest is None:
+            return param.detach().float()
+        if param.numel() != self.sizes[index]:
+            raise ValueError("gws: tensor %d has %d elements" % (index, self.sizes[index]))
+        low = self.rest[self.starts[index]:self.starts[index] + self.sizes[index]].view(param.shape)
+        return ((param.detach().view(torch.int16).to(torch.int32) << 16) + low.to(torch.int32)).view(torch.float32)
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
+               step=1, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One AdamW step over all tensors, in place, in one launch (for up to 384 of them).
+
+    Parameters are BF16 or FP32 and contiguous, gradients of their type; a tensor whose gradient is None is left alone.  ``weight_decay`` is one number or one per tensor,
+    ``step`` counts from 1.  ``step`` (int64) and ``lr`` (FP32) may be one-element tensors on the device: a captured step that is replayed reads them as they are then.
+    ``grad_scale``, an FP32 one-element tensor on the device, multiplies the gradients (the factor of a clipped gradient norm)."""
+    n = len(state.sizes)
+    if len(params) != n or len(grads) != n:
+        raise ValueError("gws: the state is of %d tensors" % n)
+    device = state.moments.get_device()
+    if device < 0:
+        _require_cuda(state.moments)
+    if stream is not None or device != _current_device():
+        return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale)
+    keep, p_params, p_grads, types = [], [], [], []
+    for p, g, size in zip(params, grads, state.sizes):
+        if g is None:
+            p_params.append(None)
+            p_grads.append(None)
+            types.append(TYPE_BF16)
+            continue
+        dtype = p.dtype
+        if dtype is _BF16:
+            types.append(TYPE_BF16)
+        elif dtype is torch.float32:
+            types.append(TYPE_F32)
+        else:
+            raise ValueError("gws: parameters are BF16 or FP32")
+        if g.dtype is not dtype or g.shape != p.shape or p.numel() != size:
+            raise ValueError("gws: a gradient has its parameter's type and shape, and the parameter the state's size")
+        if not p.is_contiguous():
+            raise ValueError("gws: parameters are contiguous")
+        if p.get_device() != device or g.get_device() != device:
+            _require_cuda(p, g)
+            raise ValueError("gws: the tensors of a call live on one device")
+        if not g.is_contiguous():
+            g = g.contiguous()
+            keep.append(g)
+        p_params.append(p.data_ptr())
+        p_grads.append(g.data_ptr())
+    if isinstance(weight_decay, (int, float)):
+        decays = [float(weight_decay)] * n
+    else:
+        decays = [float(w) for w in weight_decay]
+        if len(decays) != n:
+            raise ValueError("gws: one weight_decay for all tensors, or one for each")
+    args = _AdamwArgs(0.0, betas[0], betas[1], eps, 1, None, None, None, None)
+    on_device = []
+    for t, dtype, name in ((lr, torch.float32, "lr"), (step, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale")):
+        if isinstance(t, torch.Tensor):
+            if t.dtype is not dtype or t.numel() != 1 or t.get_device() != device:
+                raise ValueError("gws: %s on the device is one element of %s" % (name, dtype))
+            on_device.append(name)
+    if grad_scale is not None:
+        if "grad_scale" not in on_device:
+            raise ValueError("gws: grad_scale is a tensor on the device")
+        args.grad_scale = grad_scale.data_ptr()
+    if "lr" in on_device:
+        args.lr_dev = lr.data_ptr()
+    else:
+        args.lr = lr
+    if "step" in on_device:
+        args.step_dev = step.data_ptr()
+    else:
+        args.step = step
+    if args.lr_dev or args.step_dev:
+        scalars = torch.empty(4, dtype=torch.float32, device=state.moments.device)
+        args.scalars = scalars.data_ptr()
+    array = c_void_p * n
+    code = (_lib or load_library()).gws_adamw_step(n, array(*p_params), array(*p_grads), state._c_sizes, state._c_starts, (c_int32 * n)(*types),
+                                                   (ctypes.c_double * n)(*decays), ctypes.addressof(state._c), ctypes.addressof(args), _raw_stream(device))
+    if code:
+        _check(code)
+    torch.autograd.graph.increment_version([p for p, g in zip(params, grads) if g is not None])
 
 
 def selfcheck_enabled() -> bool:

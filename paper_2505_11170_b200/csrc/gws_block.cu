@@ -2,43 +2,15 @@
 // and the gated feed-forward block.  Argument validation, tensor maps, choice of tile and launch geometry; no device memory is
 // allocated here.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstring>
-#include <initializer_list>
 #include <string>
 
 #include "gws.h"
-#include "gws_internal.h"
+#include "gws_host.h"
 #include "gws_tc.cuh"
 
 namespace {
-
-constexpr int64_t kMaxDim = 0x7FFFFFFFLL - 4096;
-constexpr int kJobs = 256;                      // threads of the kernels that only move activations
-
-int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-bool on(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-
-struct Span {
-  const void* p;
-  int64_t bytes;
-};
-Span rows_of(const void* p, int64_t rows, int64_t cols, int64_t ld) { return {p, p == nullptr || rows == 0 || cols == 0 ? 0 : ((rows - 1) * ld + cols) * 2}; }
-bool overlap(const Span& a, const Span& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.bytes > 0 && b.bytes > 0 && x < y + static_cast<uintptr_t>(b.bytes) && y < x + static_cast<uintptr_t>(a.bytes);
-}
-// No output may overlap an input or another output: blocks re-read inputs while others write.
-bool clash(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
-  for (const Span* a = outputs.begin(); a != outputs.end(); ++a) {
-    for (const Span& b : inputs)
-      if (overlap(*a, b)) return true;
-    for (const Span* b = a + 1; b != outputs.end(); ++b)
-      if (overlap(*a, *b)) return true;
-  }
-  return false;
-}
 
 bool is_act8(int format) { return format == GWS_ACT8_INT8 || format == GWS_ACT8_E4M3; }
 
@@ -50,11 +22,6 @@ Act8View act8_view(const void* buffer, int64_t rows, int64_t cols) {
   uint8_t* p = static_cast<uint8_t*>(const_cast<void*>(buffer));
   return {p, p + round_up(act8_codes(rows, cols), 256), act8_ld(cols)};
 }
-int check_dims(int64_t a, int64_t b, int64_t c) {
-  if (a < 0 || b < 0 || c < 0) return GWS_ERR_SHAPE;
-  return a > kMaxDim || b > kMaxDim || c > kMaxDim ? GWS_ERR_LIMIT : GWS_OK;
-}
-
 int zero(void* p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t s) {
   if (p == nullptr || rows == 0 || cols == 0) return GWS_OK;
   const cudaError_t err = cudaMemset2DAsync(p, static_cast<size_t>(ld) * 2u, 0, static_cast<size_t>(cols) * 2u, static_cast<size_t>(rows), s);
@@ -63,33 +30,6 @@ int zero(void* p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t s) {
 
 // Whether every group of a [rows, cols] BF16 tensor is 64 whole bytes on a 32-byte boundary: a thread then takes a group.
 bool whole_groups(const void* p, int64_t cols, int64_t ld) { return cols % kGroup == 0 && ld % 16 == 0 && on(p, 32); }
-
-// Every launch may become resident while the kernel before it on the stream drains (after_previous in the kernels): with ordinary
-// launches calls of a few us follow each other 2 us further apart (517 tokens, 768 x 2730: 12.3 against 10.4 us a call).
-template <class... P, class... A>
-int launch(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, unsigned cluster, cudaStream_t s, const char* what, const A&... args) {
-  cudaLaunchConfig_t cfg;
-  std::memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  cfg.attrs = attr;
-  attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
-  if (cluster > 1) {
-    attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-    attr[cfg.numAttrs].val.clusterDim.x = cluster;
-    attr[cfg.numAttrs].val.clusterDim.y = 1;
-    attr[cfg.numAttrs++].val.clusterDim.z = 1;
-  }
-  const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
-  if (err != cudaSuccess) { (void)cudaGetLastError(); return gws::report_cuda(err, what); }
-  return gws::finish_launch(what);
-}
-
-unsigned blocks_for(int64_t items, int64_t per_block) { return static_cast<unsigned>((items + per_block - 1) / per_block); }
 
 int launch_act8(bool save, int format, const void* x, int64_t ldx, const Act8View& c, int64_t rows, int64_t cols, cudaStream_t s) {
   const int64_t per_row = c.ld / kGroup, groups = rows * per_row;
@@ -208,19 +148,6 @@ struct Ready {
 std::atomic<int64_t> g_wait_limit{kTcWaitCycles};
 
 // ---- choice of tile --------------------------------------------------------------------------------------------------------
-int sm_count() {
-  static std::atomic<int> known[64];             // per device
-  int dev = 0, n = 0;
-  const bool current = cudaGetDevice(&dev) == cudaSuccess;
-  if (current && dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) != 0) return n;
-  if (!current || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) {
-    (void)cudaGetLastError();
-    return 148;
-  }
-  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
-  return n;
-}
-
 // What make() returns for a key of sizes, options and SM count, which it depends on alone.  The last 64 or so are kept per thread: weighing the
 // tiles of a call takes the host 0.5 to 1.5 us, as long as launching a kernel.
 template <class Value, size_t N, class F>
@@ -542,8 +469,6 @@ void describe(const Tile& t, int sms, gws_product_plan* p) {
   const uint32_t work = t.whole + t.cut * t.splits, slots = static_cast<uint32_t>(sms / t.cg);
   p->waves = t.clustered ? 1 : static_cast<int32_t>((work + slots - 1) / slots);
 }
-
-bool workspace_ok(const void* p, size_t have, int64_t need) { return need == 0 || (p != nullptr && on(p, 256) && have >= static_cast<size_t>(need)); }
 
 }  // namespace
 
