@@ -508,7 +508,7 @@ typedef enum gws_act_format {
   GWS_ACT8_INT8 = 0,
   GWS_ACT8_E4M3 = 1,
   GWS_SAVE_BF16 = 2, /* where a call says so: a BF16 tensor instead of a checkpoint */
-  GWS_SAVE_NONE = 3  /* gws_gated_fwd: nothing is kept */
+  GWS_SAVE_NONE = 3  /* gws_gated_fwd, gws_linear_fwd: nothing is kept */
 } gws_act_format;
 
 /* Sizes of a checkpoint; any of the outputs may be NULL.  Host arithmetic only. */
@@ -528,7 +528,8 @@ int gws_wgrad_act8(int64_t m, int64_t n, int64_t k, int format, const void* grad
 typedef enum gws_activation {
   GWS_GATED_SILU = 0,      /* g sigmoid(g)                                             */
   GWS_GATED_GELU_TANH = 1, /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2          */
-  GWS_GATED_RELU = 2       /* max(g, 0)                                                */
+  GWS_GATED_RELU = 2,      /* max(g, 0)                                                */
+  GWS_ACT_NONE = 3         /* gws_linear_*: g itself                                    */
 } gws_activation;
 typedef struct gws_gated_desc {
   int64_t m, n, k;
@@ -556,11 +557,34 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
                   const void* save_up, void* grad_x, void* grad_w_gate, void* grad_w_up, void* h_out, void* workspace, size_t workspace_bytes,
                   int* status, void* stream);
 
+typedef enum gws_type { GWS_TYPE_BF16 = 0, GWS_TYPE_F32 = 1 } gws_type;
+
+/* Linear layer with bias, activation and residual:  z = x W^T + bias,  y = act(z) + residual   over m tokens, k > 0 inputs, n outputs. */
+typedef struct gws_linear_desc {
+  int64_t m, n, k;
+  int64_t ld_x, ld_w, ld_y, ld_residual; /* row strides of x, W, y (forward) or grad_y (backward), residual                   */
+  int32_t activation;                    /* gws_activation                                                                   */
+  int32_t save_format;                   /* what z is kept as: gws_act_format                                                */
+  int32_t x_format;                      /* backward: GWS_SAVE_BF16 = x is a BF16 tensor, GWS_ACT8_* = a checkpoint            */
+  int32_t bias_type;                     /* gws_type of bias and its gradient                                                */
+} gws_linear_desc;
+int64_t gws_linear_workspace_bytes(const gws_linear_desc* desc, int backward);
+/* Forward, in one kernel (a second one joins the parts of tiles whose contraction is cut); z stays in FP32 until y is rounded.
+ *   x  device, BF16 [m, ld_x]      w  device, BF16 [n, ld_w]      bias  device, [n] of bias_type, or NULL      residual  device, BF16 [m, ld_residual], or NULL
+ *   y  device, BF16 [m, ld_y], written      save  device, checkpoint [m, n] or BF16 [m, n] (dense), rounded from the FP32 z, written; NULL with GWS_SAVE_NONE */
+int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, const void* bias, const void* residual, void* y, void* save, void* workspace,
+                   size_t workspace_bytes, int* status, void* stream);
+/* Backward, from the kept z (not read, and save and its format free, with GWS_ACT_NONE unless act_out is wanted):
+ *   dz = grad_y act'(z)     (FP32, rounded to BF16 for the tensor cores)
+ *   grad_x = dz W,   grad_w = dz^T x,   grad_bias = sum over tokens of dz (before its rounding),   act_out = act(z)      (the residual's gradient is grad_y)
+ *   grad_x [m, k], grad_w [n, k], act_out [m, n]: device, BF16, dense, written; grad_bias: device, [n] of bias_type, written.  Each may be NULL, and its work
+ *   (for grad_x the weights, for grad_w x) is then not needed. */
+int gws_linear_bwd(const gws_linear_desc* desc, const void* grad_y, const void* x, const void* w, const void* save, void* grad_x, void* grad_w, void* grad_bias,
+                   void* act_out, void* workspace, size_t workspace_bytes, int* status, void* stream);
+
 /* ---- the rest of a block's training step: layer norm, optimizer -----------------------------------------------------
  * As above: BF16 tensors row-major with a row stride of at least their width, any 2-byte alignment (rows on 16-byte boundaries are
  * fastest), sizes may be zero, outputs overlap neither inputs nor each other, everything is enqueued on `stream` of the current device. */
-typedef enum gws_type { GWS_TYPE_BF16 = 0, GWS_TYPE_F32 = 1 } gws_type;
-
 /* Layer norm over the rows of s = bf16(x + residual), or of x itself without a residual:
  *   y = (s - mean) rstd weight + bias,   rstd = 1 / sqrt(mean((s - mean)^2) + eps)          (FP32; y rounded once) */
 typedef struct gws_norm_desc {
@@ -693,8 +717,10 @@ typedef struct gws_product_plan {
 /* product: 0 h (forward), 1 grad_x, 2 the pair of weight gradients (backward; x as desc->x_format says) */
 int gws_gated_plan(const gws_gated_desc* desc, int product, gws_product_plan* plan);
 int gws_wgrad_act8_plan(int64_t m, int64_t n, int64_t k, int64_t ld_y, gws_product_plan* plan);
+/* product: 0 y (forward), 1 grad_x, 2 grad_w */
+int gws_linear_plan(const gws_linear_desc* desc, int product, gws_product_plan* plan);
 
-/* Limit of the waits inside the matrix products of gws_wgrad_act8, gws_gated_fwd and gws_gated_bwd, in SM cycles; process-wide, read at
+/* Limit of the waits inside the matrix products of gws_wgrad_act8, gws_gated_* and gws_linear_*, in SM cycles; process-wide, read at
  * every launch, 2e9 when the library is loaded and for cycles <= 0.  Returns the previous one.  For tests of what follows when a wait
  * runs out: with a limit of a few cycles a sound launch gives up, and ends as it would on a fault. */
 int64_t gws_set_wait_limit(int64_t cycles);

@@ -27,6 +27,7 @@ class GwsError(RuntimeError):
         super().__init__(msg)
 
 
+TYPE_BF16, TYPE_F32 = 0, 1
 OK, ERR_NULL, ERR_SHAPE, ERR_GROUP, ERR_ALIGN, ERR_ALIAS, ERR_WORKSPACE, ERR_CUDA, ERR_LIMIT, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5, -6, -7, -8, -9
 
 
@@ -102,6 +103,10 @@ _SIGNATURES = {
     "gws_wgrad_act8_plan": (c_int, [c_int64, c_int64, c_int64, c_int64, c_void_p]),
     "gws_gated_fwd": (c_int, [c_void_p] * 8 + [c_size_t, c_void_p, c_void_p]),
     "gws_gated_bwd": (c_int, [c_void_p] * 12 + [c_size_t, c_void_p, c_void_p]),
+    "gws_linear_workspace_bytes": (c_int64, [c_void_p, c_int]),
+    "gws_linear_plan": (c_int, [c_void_p, c_int, c_void_p]),
+    "gws_linear_fwd": (c_int, [c_void_p] * 8 + [c_size_t, c_void_p, c_void_p]),
+    "gws_linear_bwd": (c_int, [c_void_p] * 10 + [c_size_t, c_void_p, c_void_p]),
     "gws_layernorm_workspace_bytes": (c_int64, [c_void_p]),
     "gws_layernorm_fwd": (c_int, [c_void_p] * 9),
     "gws_layernorm_bwd": (c_int, [c_void_p] * 10 + [c_size_t, c_void_p]),
@@ -913,13 +918,123 @@ def gated_bwd(grad_h: torch.Tensor, x, w_gate: torch.Tensor, w_up: torch.Tensor,
     return grad_x, grad_wg, grad_wu, h
 
 
+class LinearDesc(Structure):
+    """Mirror of ``gws_linear_desc``."""
+    _fields_ = [("m", c_int64), ("n", c_int64), ("k", c_int64), ("ld_x", c_int64), ("ld_w", c_int64), ("ld_y", c_int64), ("ld_residual", c_int64),
+                ("activation", c_int32), ("save_format", c_int32), ("x_format", c_int32), ("bias_type", c_int32)]
+
+
+ACT_NONE = 3
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_plan(m: int, n: int, k: int, ld_x: int, ld_w: int, ld_y: int, ld_r: int, activation: int, save: int, x_format: int, bias_type: int, backward: int, device: int):
+    """(descriptor, its address, workspace bytes) of a call: functions of the sizes alone."""
+    d = LinearDesc(m, n, k, ld_x, ld_w, ld_y, ld_r, activation, save, x_format, bias_type)
+    at = ctypes.addressof(d)
+    nbytes = load_library().gws_linear_workspace_bytes(at, backward)
+    if nbytes < 0:
+        raise GwsError(int(nbytes))
+    return d, at, nbytes
+
+
+def linear_plan(m: int, n: int, k: int, product: int, activation: int = ACT_NONE, x_format: int = SAVE_BF16, ld_x: Optional[int] = None, ld_w: Optional[int] = None,
+                ld_y: Optional[int] = None) -> ProductPlan:
+    """How product 0 (y), 1 (grad_x) or 2 (grad_w) of a linear layer is carried out."""
+    d = LinearDesc(m, n, k, ld_x or k, ld_w or k, ld_y or n, 0, activation, SAVE_NONE, x_format, TYPE_BF16)
+    p = ProductPlan()
+    _check(load_library().gws_linear_plan(ctypes.addressof(d), product, ctypes.addressof(p)))
+    return p
+
+
+def _bias_type(bias: Optional[torch.Tensor], n: int) -> int:
+    if bias is None:
+        return TYPE_BF16
+    if (bias.dtype is not _BF16 and bias.dtype is not torch.float32) or bias.shape != (n,):
+        raise ValueError("gws: the bias is a BF16 or FP32 (%d,) tensor" % n)
+    return TYPE_BF16 if bias.dtype is _BF16 else TYPE_F32
+
+
+def linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, activation: int = ACT_NONE,
+               save: int = SAVE_NONE, y: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None):
+    """y = act(z) + residual, z = x W^T + bias, for x [m, k], w [n, k], residual [m, n] in BF16 and a bias [n] in BF16 or FP32, in one kernel.  Returns (y, saved):
+    ``save`` says what z is kept as for :func:`linear_bwd` (ACT8_INT8 or ACT8_E4M3: an Act8, SAVE_BF16: a BF16 tensor, SAVE_NONE: None).  ``activation`` is ACT_NONE,
+    GATED_SILU, GATED_GELU_TANH or GATED_RELU."""
+    device = _device_of(x, w, bias, residual, y, status)
+    if stream is not None or device != _current_device():
+        return _on_stream(stream, device, linear_fwd, x, w, bias, residual, activation, save, y, status)
+    p_st = _status_of(status)
+    x, p_x, ld_x, m, k = _bf16_rows(x, "x")
+    w, p_w, ld_w, n, _ = _bf16_rows(w, "w", None, k)
+    kind = _bias_type(bias, n)
+    if bias is not None:
+        bias = bias.contiguous()
+    p_r, ld_r = None, 0
+    if residual is not None:
+        residual, p_r, ld_r, _, _ = _bf16_rows(residual, "residual", m, n, read_by_map=False)
+    if save not in (ACT8_INT8, ACT8_E4M3, SAVE_BF16, SAVE_NONE):
+        raise GwsError(ERR_UNSUPPORTED)
+    _, at, nbytes = _linear_plan(m, n, k, ld_x, ld_w, n or 1, ld_r, activation, save, SAVE_BF16, kind, 0, device)
+    y = _bf16_out(y, "y", m, n, x)
+    saved = p_s = None
+    if save == SAVE_BF16:
+        saved = x.new_empty(m, n)
+        p_s = saved.data_ptr()
+    elif save != SAVE_NONE:
+        saved = Act8._new(x, m, n, save)
+        p_s = saved.buffer.data_ptr()
+    ws, ws_p = _workspace(nbytes, x)
+    code = (_lib or load_library()).gws_linear_fwd(at, p_x, p_w, _addr(bias), p_r, y.data_ptr(), p_s, ws_p, nbytes, p_st, _raw_stream(device))
+    if code:
+        _check(code)
+    return y, saved
+
+
+def linear_bwd(grad_y: torch.Tensor, x, w: torch.Tensor, saved=None, activation: int = ACT_NONE, want_grad_x: bool = True, want_grad_w: bool = True,
+               want_grad_bias: bool = False, want_act: bool = False, bias_dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None, stream=None):
+    """Backward pass of :func:`linear_fwd`.  ``x`` is the BF16 input or its checkpoint, ``saved`` what the forward call kept of z (not read with ACT_NONE, unless act(z) is
+    wanted).  Returns (grad_x, grad_w, grad_bias, act(z)), None for what was not asked for; grad_bias is of ``bias_dtype``.  The residual's gradient is grad_y.  act(z) is
+    what the weight gradient of the layer after this one needs."""
+    kept_x, kept_z = isinstance(x, Act8), isinstance(saved, Act8)
+    z = saved.buffer if kept_z else saved
+    device = _device_of(grad_y, x.buffer if kept_x else x, w, z, status)
+    if stream is not None or device != _current_device():
+        return _on_stream(stream, device, linear_bwd, grad_y, x, w, saved, activation, want_grad_x, want_grad_w, want_grad_bias, want_act, bias_dtype, status)
+    p_st = _status_of(status)
+    m, k = x.shape
+    w, p_w, ld_w, n, _ = _bf16_rows(w, "w", None, k)
+    grad_y, p_dy, ld_y, _, _ = _bf16_rows(grad_y, "grad_y", m, n, read_by_map=activation == ACT_NONE)
+    if kept_x:
+        p_x, ld_x, x_format = x.buffer.data_ptr(), k or 1, x.fmt
+    else:
+        x, p_x, ld_x, _, _ = _bf16_rows(x, "x")
+        x_format = SAVE_BF16
+    p_z, z_format = None, SAVE_NONE
+    if activation != ACT_NONE or want_act:
+        if saved is None:
+            raise ValueError("gws: the activation's backward pass needs what the forward call kept of z")
+        if tuple(saved.shape) != (m, n) or (not kept_z and (saved.dtype is not _BF16 or not saved.is_contiguous())):
+            raise ValueError("gws: what is kept of z is a checkpoint or a contiguous BF16 tensor of (%d, %d)" % (m, n))
+        p_z, z_format = z.data_ptr(), saved.fmt if kept_z else SAVE_BF16
+    if bias_dtype is not _BF16 and bias_dtype is not torch.float32:
+        raise ValueError("gws: the bias is BF16 or FP32")
+    _, at, nbytes = _linear_plan(m, n, k, ld_x, ld_w, ld_y, 0, activation, z_format, x_format, TYPE_BF16 if bias_dtype is _BF16 else TYPE_F32, 1, device)
+    grad_x = grad_y.new_empty(m, k) if want_grad_x else None
+    grad_w = _dense_like(w, n, k) if want_grad_w else None
+    grad_bias = grad_y.new_empty(n, dtype=bias_dtype) if want_grad_bias else None
+    again = grad_y.new_empty(m, n) if want_act else None
+    ws, ws_p = _workspace(nbytes, grad_y)
+    code = (_lib or load_library()).gws_linear_bwd(at, p_dy, p_x, p_w, p_z, _addr(grad_x), _addr(grad_w), _addr(grad_bias), _addr(again), ws_p, nbytes, p_st,
+                                                   _raw_stream(device))
+    if code:
+        _check(code)
+    return grad_x, grad_w, grad_bias, again
+
+
 class NormDesc(Structure):
     """Mirror of ``gws_norm_desc``."""
     _fields_ = [("rows", c_int64), ("cols", c_int64), ("ld_x", c_int64), ("ld_residual", c_int64), ("ld_grad_y", c_int64), ("ld_grad_sum", c_int64),
                 ("weight_type", c_int32), ("eps", c_float)]
-
-
-TYPE_BF16, TYPE_F32 = 0, 1
 
 
 @functools.lru_cache(maxsize=1024)

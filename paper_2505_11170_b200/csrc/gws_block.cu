@@ -1,5 +1,5 @@
 // Host side of the activation operators declared in gws.h: 8-bit activation checkpoints, the weight gradient from a checkpoint
-// and the gated feed-forward block.  Argument validation, tensor maps, choice of tile and launch geometry; no device memory is
+// the gated feed-forward block and the linear layer with epilogue.  Argument validation, tensor maps, choice of tile and launch geometry; no device memory is
 // allocated here.
 #include <algorithm>
 #include <cmath>
@@ -8,6 +8,7 @@
 
 #include "gws.h"
 #include "gws_host.h"
+#include "gws_linear.cuh"
 #include "gws_tc.cuh"
 
 namespace {
@@ -191,9 +192,9 @@ Tile choose(int mode, int64_t rows, int64_t cols, int outs, int64_t len, int seg
     const int64_t slots = kind.cg == 2 ? sms / 2 : sms, kb = segments * stages_of(len, kind.bn);
     const double convert = mode == kDw8 ? 220.0 : 0.0;          // what a copy of codes adds to its step
     const double step = (kind.bn == 256 ? 1 : 2) * (convert + std::max(250.0, std::max(2.0 * kind.bn, (16384.0 + 128.0 * kind.bn / kind.cg) / (kind.cg == 2 ? 77.0 : 67.0))));
-    const double epilogue = mode == kGated ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
+    const double epilogue = mode == kGated || mode == kLinear ? 10.0 * kind.bn + 400.0 : 5.0 * kind.bn + 400.0, start = kind.cg == 2 ? 4500.0 : 3300.0;
     // one row of tiles reads the weights once: no faster than from memory
-    const double bytes = mode == kGated && mt == 1 ? width * 4.0 * len / 3400.0 : 0.0, tile = std::max({kb * step, epilogue, std::min(tiles, slots) * bytes}) + 100.0;
+    const double bytes = mt == 1 && (mode == kGated || mode == kLinear) ? (mode == kGated ? 4.0 : 2.0) * width * len / 3400.0 : 0.0, tile = std::max({kb * step, epilogue, std::min(tiles, slots) * bytes}) + 100.0;
     auto offer = [&](int64_t whole, int64_t splits, double cost, bool clustered) {
       if (best.cg != 0 && cost >= least) return;
       least = cost;
@@ -455,6 +456,80 @@ int launch_pre_act(const PreArgs& p, Ready& ready, int act, bool fast, cudaStrea
   if (act == GWS_GATED_SILU) return launch_pre<SAVE, GWS_GATED_SILU>(p, ready, fast, s);
   if (act == GWS_GATED_GELU_TANH) return launch_pre<SAVE, GWS_GATED_GELU_TANH>(p, ready, fast, s);
   return launch_pre<SAVE, GWS_GATED_RELU>(p, ready, fast, s);
+}
+
+// ---- the linear layer with epilogue -----------------------------------------------------------------------------------------------
+int check_linear(const gws_linear_desc* d) {
+  if (d == nullptr) return GWS_ERR_NULL;
+  const int st = check_dims(d->m, d->n, d->k);
+  if (st != GWS_OK) return st;
+  if (d->k == 0) return GWS_ERR_SHAPE;
+  for (const int64_t ld : {d->ld_x, d->ld_w, d->ld_y, d->ld_residual}) {
+    if (ld < 0) return GWS_ERR_SHAPE;
+    if (ld > kMaxDim) return GWS_ERR_LIMIT;
+  }
+  if ((d->m > 0 && d->ld_x < d->k) || (d->n > 0 && d->ld_w < d->k) || (d->m > 0 && d->n > 0 && d->ld_y < d->n)) return GWS_ERR_SHAPE;
+  if (d->activation < GWS_GATED_SILU || d->activation > GWS_ACT_NONE) return GWS_ERR_UNSUPPORTED;
+  if (d->bias_type != GWS_TYPE_BF16 && d->bias_type != GWS_TYPE_F32) return GWS_ERR_UNSUPPORTED;
+  return GWS_OK;
+}
+int64_t kept_bytes(int format, int64_t m, int64_t n) { return format == GWS_SAVE_NONE ? 0 : format == GWS_SAVE_BF16 ? m * n * 2 : act8_total(m, n); }
+int64_t bias_bytes(const gws_linear_desc& d) { return d.n * (d.bias_type == GWS_TYPE_F32 ? 4 : 2); }
+
+// Forward: tile, and which operands are copied into the workspace; rows in the middle of a sector as in weigh_forward.
+ForwardPlan weigh_linear(const gws_linear_desc* d, int sms) {
+  ForwardPlan f{choose(kLinear, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
+  if (!f.move_x && !f.move_w && d->m > 1 && d->n > 1 && d->ld_x % 16 != 0 && d->ld_w % 16 != 0) {
+    const double smaller = static_cast<double>(d->k) * std::min(d->m, d->n);
+    if (0.25 * f.tile.cost > 4500.0 + smaller * 4.0 / 3400.0) (d->m <= d->n ? f.move_x : f.move_w) = true;
+  }
+  return f;
+}
+const ForwardPlan& plan_linear(const gws_linear_desc* d, int sms) {
+  return remembered<ForwardPlan>({d->m, d->n, d->k, d->ld_x, d->ld_w, sms}, [&] { return weigh_linear(d, sms); });
+}
+int64_t linear_copies(const gws_linear_desc* d, const ForwardPlan& f) {
+  return (f.move_x ? packed_bytes(d->m, d->k) : 0) + (f.move_w ? packed_bytes(d->n, d->k) : 0);
+}
+
+// Backward: places in the workspace, whatever the call asks for.  dz is grad_y itself without an activation (aligned if its rows are not).
+struct LinearBack {
+  int64_t x, w, dz, part, total;
+  Tile dx;
+  DwChoice dw;
+};
+LinearBack weigh_linear_back(const gws_linear_desc* d, int sms) {
+  LinearBack l{};
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) { const int64_t here = at; at += round_up(bytes, 256); return here; };
+  const bool makes = d->activation != GWS_ACT_NONE, moves = !makes && !in_place(d->m, d->ld_y);
+  l.dx = choose(kDx, d->m, d->k, 1, d->n, 1, sms);
+  l.dw = choose_dw(d->m, d->n, d->k, 1, is_act8(d->x_format), makes || moves, sms);
+  const bool direct_x = is_act8(d->x_format) ? l.dw.inside : in_place(d->m, d->ld_x);
+  l.x = take(direct_x ? 0 : packed_bytes(d->m, d->k));
+  l.w = take(in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k));
+  l.dz = take(makes || moves ? packed_bytes(d->m, d->n) : 0);
+  l.part = take(std::max(part_bytes(l.dx), part_bytes(l.dw.tile)));
+  l.total = at;
+  return l;
+}
+const LinearBack& linear_back(const gws_linear_desc* d, int sms) {
+  return remembered<LinearBack>({d->m, d->n, d->k, d->ld_x, d->ld_w, d->ld_y, d->activation != GWS_ACT_NONE, d->x_format, sms}, [&] { return weigh_linear_back(d, sms); });
+}
+
+// A block's share of a strip is at least 32 rows, a row to eight of its threads.
+int launch_linear_pre(LinearPre p, Ready& ready, int save, bool wide, cudaStream_t s) {
+  const int64_t moved = ready.blocks(), strips = (p.cols + 63) / 64;
+  if (moved < 0) return static_cast<int>(moved);
+  p.shares = p.rows > 128 ? 8u : p.rows > 64 ? 4u : p.rows > 32 ? 2u : 1u;
+  p.first = static_cast<uint32_t>(round_up(moved, p.shares));
+  const unsigned grid = p.first + static_cast<unsigned>(strips) * p.shares;
+  const char* what = "linear backward, element-wise part";
+  auto go = [&](void (*kernel)(LinearPre, Prep)) { return launch(kernel, grid, 256, 0, p.shares, s, what, p, ready.prep); };
+  if (save == GWS_ACT8_INT8) return go(wide ? k_linear_pre<GWS_ACT8_INT8, true> : k_linear_pre<GWS_ACT8_INT8, false>);
+  if (save == GWS_ACT8_E4M3) return go(wide ? k_linear_pre<GWS_ACT8_E4M3, true> : k_linear_pre<GWS_ACT8_E4M3, false>);
+  if (save == GWS_SAVE_BF16) return go(wide ? k_linear_pre<GWS_SAVE_BF16, true> : k_linear_pre<GWS_SAVE_BF16, false>);
+  return go(wide ? k_linear_pre<GWS_SAVE_NONE, true> : k_linear_pre<GWS_SAVE_NONE, false>);
 }
 
 void describe(const Tile& t, int sms, gws_product_plan* p) {
@@ -744,6 +819,176 @@ int gws_gated_bwd(const gws_gated_desc* desc, const void* grad_h, const void* x,
     if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
   }
   if (wants_dw) return run_dw(l.dw.tile, dg, &du, mx, l.dw.inside ? &kept_x : nullptr, d.x_format, grad_w_gate, grad_w_up, d.k, ws + l.part, status, sms, s);
+  return GWS_OK;
+}
+
+int64_t gws_linear_workspace_bytes(const gws_linear_desc* desc, int backward) {
+  const int st = check_linear(desc);
+  if (st != GWS_OK) return st;
+  if (desc->m == 0 || desc->n == 0) return 0;
+  const int sms = sm_count();
+  if (backward != 0) return linear_back(desc, sms).total;
+  const ForwardPlan& f = plan_linear(desc, sms);
+  return linear_copies(desc, f) + part_bytes(f.tile);
+}
+
+int gws_linear_plan(const gws_linear_desc* desc, int product, gws_product_plan* plan) {
+  if (plan == nullptr) return GWS_ERR_NULL;
+  const int st = check_linear(desc);
+  if (st != GWS_OK) return st;
+  if (product < 0 || product > 2) return GWS_ERR_UNSUPPORTED;
+  std::memset(plan, 0, sizeof *plan);
+  if (desc->m == 0 || desc->n == 0) return GWS_OK;
+  const int sms = sm_count();
+  if (product == 0) {
+    const ForwardPlan& f = plan_linear(desc, sms);
+    describe(f.tile, sms, plan);
+    plan->moves_x = f.move_x;
+    plan->moves_w = f.move_w;
+  } else {
+    const LinearBack& l = linear_back(desc, sms);
+    describe(product == 1 ? l.dx : l.dw.tile, sms, plan);
+    plan->inside = product == 2 && l.dw.inside;
+  }
+  return GWS_OK;
+}
+
+int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, const void* bias, const void* residual, void* y, void* save, void* workspace,
+                   size_t workspace_bytes, int* status, void* stream) {
+  int st = check_linear(desc);
+  if (st != GWS_OK) return st;
+  const gws_linear_desc& d = *desc;
+  const bool saves = d.save_format != GWS_SAVE_NONE, bytes8 = is_act8(d.save_format);
+  if (saves && !bytes8 && d.save_format != GWS_SAVE_BF16) return GWS_ERR_UNSUPPORTED;
+  if (d.m == 0 || d.n == 0) return GWS_OK;
+  if (residual != nullptr && d.ld_residual < d.n) return GWS_ERR_SHAPE;
+  if (x == nullptr || w == nullptr || y == nullptr || (saves && save == nullptr)) return GWS_ERR_NULL;
+  const size_t bias_each = d.bias_type == GWS_TYPE_F32 ? 4 : 2;
+  if (!on(y, 2) || !on(residual, 2) || !on(bias, bias_each) || !on(status, 4) || (saves && !on(save, bytes8 ? 32 : 2)) || !on(x, in_place(d.m, d.ld_x) ? 16 : 2) ||
+      !on(w, in_place(d.n, d.ld_w) ? 16 : 2))
+    return GWS_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int sms = sm_count();
+  const ForwardPlan& f = plan_linear(desc, sms);
+  const int64_t copies = linear_copies(desc, f), need = copies + part_bytes(f.tile);
+  if (clash({rows_of(y, d.m, d.n, d.ld_y), {save, kept_bytes(d.save_format, d.m, d.n)}, {workspace, need}},
+            {rows_of(x, d.m, d.k, d.ld_x), rows_of(w, d.n, d.k, d.ld_w), {bias, bias != nullptr ? bias_bytes(d) : 0}, rows_of(residual, d.m, d.n, d.ld_residual)}))
+    return GWS_ERR_ALIAS;
+  if (!workspace_ok(workspace, workspace_bytes, need)) return GWS_ERR_WORKSPACE;
+  Mat mx{x, d.m, d.k, d.ld_x}, mw{w, d.n, d.k, d.ld_w};
+  Ready ready;
+  char* ws = static_cast<char*>(workspace);
+  ready.align(mx, ws, f.move_x);
+  if (f.move_x) ws += packed_bytes(d.m, d.k);
+  ready.align(mw, ws, f.move_w);
+  if ((st = ready.run(s)) != GWS_OK) return st;
+
+  const Tile& t = f.tile;
+  TcArgs args = base_args(t, d.m, d.n, d.k, 1, status);
+  set_out(args, y, nullptr, d.ld_y);
+  args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
+  args.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + copies);
+  args.activation = d.activation;
+  args.bias = bias;
+  args.bias_f32 = d.bias_type == GWS_TYPE_F32;
+  args.residual = static_cast<const uint16_t*>(residual);
+  args.ld_residual = d.ld_residual;
+  args.residual_wide = widest(d.m > 1 ? d.ld_residual : round_up(d.ld_residual, 16), residual, nullptr);
+  args.save = d.save_format;
+  if (bytes8) {
+    args.save8[0] = act8_view(save, d.m, d.n);
+  } else if (saves) {
+    args.save16[0] = static_cast<uint16_t*>(save);
+    args.save_wide = widest(d.n, save, nullptr);
+  }
+  CUtensorMap maps[4];
+  if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, a_box(d.m))) != GWS_OK) return st;
+  maps[1] = maps[0];
+  if ((st = make_map(maps[2], mw.p, d.n, d.k, mw.ld, static_cast<uint32_t>(t.bn / t.cg))) != GWS_OK) return st;
+  maps[3] = maps[2];
+  return launch_mode<kLinear>(t, maps, args, sms, s);
+}
+
+int gws_linear_bwd(const gws_linear_desc* desc, const void* grad_y, const void* x, const void* w, const void* save, void* grad_x, void* grad_w, void* grad_bias,
+                   void* act_out, void* workspace, size_t workspace_bytes, int* status, void* stream) {
+  int st = check_linear(desc);
+  if (st != GWS_OK) return st;
+  const gws_linear_desc& d = *desc;
+  const bool acts = d.activation != GWS_ACT_NONE, reads = acts || act_out != nullptr, saved8 = is_act8(d.save_format), x8 = is_act8(d.x_format);
+  if ((reads && !saved8 && d.save_format != GWS_SAVE_BF16) || (!x8 && d.x_format != GWS_SAVE_BF16)) return GWS_ERR_UNSUPPORTED;
+  const size_t bias_each = d.bias_type == GWS_TYPE_F32 ? 4 : 2;
+  if (!on(grad_x, 2) || !on(grad_w, 2) || !on(grad_bias, bias_each) || !on(act_out, 2) || !on(status, 4)) return GWS_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (d.m == 0 || d.n == 0) {              // empty sums
+    if ((st = zero(grad_x, d.m, d.k, d.k, s)) != GWS_OK || (st = zero(grad_w, d.n, d.k, d.k, s)) != GWS_OK) return st;
+    if (grad_bias == nullptr || d.n == 0) return GWS_OK;
+    const cudaError_t err = cudaMemsetAsync(grad_bias, 0, static_cast<size_t>(bias_bytes(d)), s);
+    return err == cudaSuccess ? GWS_OK : gws::report_cuda(err, "clearing a gradient");
+  }
+  const bool wants_dw = grad_w != nullptr, wants_dx = grad_x != nullptr, products = wants_dw || wants_dx;
+  if (!products && grad_bias == nullptr && act_out == nullptr) return GWS_OK;
+  const bool wants_dy = products || grad_bias != nullptr;
+  if ((wants_dy && grad_y == nullptr) || (reads && save == nullptr) || (wants_dw && x == nullptr) || (wants_dx && w == nullptr)) return GWS_ERR_NULL;
+  // without an activation the products read grad_y where it lies
+  const bool moves_y = !acts && products && !in_place(d.m, d.ld_y), moves_x = !x8 && !in_place(d.m, d.ld_x), moves_w = !in_place(d.n, d.ld_w);
+  if ((wants_dy && !on(grad_y, acts || moves_y || !products ? 2 : 16)) || (reads && !on(save, saved8 ? 32 : 2)) || (wants_dw && !on(x, x8 ? 32 : moves_x ? 2 : 16)) ||
+      (wants_dx && !on(w, moves_w ? 2 : 16)))
+    return GWS_ERR_ALIGN;
+  const int sms = sm_count();
+  const LinearBack& l = linear_back(desc, sms);
+  const Span in_x = x8 ? Span{x, act8_total(d.m, d.k)} : rows_of(x, d.m, d.k, d.ld_x);
+  if (clash({rows_of(grad_x, d.m, d.k, d.k), rows_of(grad_w, d.n, d.k, d.k), {grad_bias, grad_bias != nullptr ? bias_bytes(d) : 0}, rows_of(act_out, d.m, d.n, d.n),
+             {workspace, l.total}},
+            {rows_of(grad_y, d.m, d.n, d.ld_y), in_x, rows_of(w, d.n, d.k, d.ld_w), {save, reads ? kept_bytes(d.save_format, d.m, d.n) : 0}}))
+    return GWS_ERR_ALIAS;
+  if (!workspace_ok(workspace, workspace_bytes, l.total)) return GWS_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+
+  Ready ready;
+  Mat dz{grad_y, d.m, d.n, d.ld_y}, mw{w, d.n, d.k, d.ld_w}, mx{x, d.m, d.k, d.ld_x};
+  const Act8View kept_x = act8_view(x, d.m, d.k);
+  if (wants_dx) ready.align(mw, ws + l.w);
+  if (wants_dw && x8 && !l.dw.inside) mx = ready.restore(kept_x, d.x_format, d.m, d.k, ws + l.x);
+  if (wants_dw && !x8) ready.align(mx, ws + l.x);
+  if (!acts && products) ready.align(dz, ws + l.dz);
+  if ((acts && products) || grad_bias != nullptr || act_out != nullptr) {
+    LinearPre p;
+    std::memset(&p, 0, sizeof p);
+    p.dy = wants_dy ? static_cast<const uint16_t*>(grad_y) : nullptr;
+    p.ld_dy = d.m == 1 ? round_up(d.n, 8) : d.ld_y;
+    if (acts && products) {
+      p.dz = reinterpret_cast<uint16_t*>(ws + l.dz);
+      p.ld_dz = packed_ld(d.n);
+      dz = {p.dz, d.m, d.n, p.ld_dz};
+    }
+    if (saved8) p.save8 = act8_view(save, d.m, d.n);
+    else p.save16 = static_cast<const uint16_t*>(save);
+    p.again = static_cast<uint16_t*>(act_out);
+    p.db = grad_bias;
+    p.db_f32 = d.bias_type == GWS_TYPE_F32;
+    p.rows = d.m;
+    p.cols = d.n;
+    p.activation = d.activation;
+    const bool wide = d.n % 8 == 0 && (p.dy == nullptr || (on(grad_y, 16) && p.ld_dy % 8 == 0)) && (act_out == nullptr || on(act_out, 16)) &&
+                      (!reads || saved8 || on(save, 16));
+    if ((st = launch_linear_pre(p, ready, reads ? d.save_format : GWS_SAVE_NONE, wide, s)) != GWS_OK) return st;
+  } else if ((st = ready.run(s)) != GWS_OK) {
+    return st;
+  }
+
+  if (wants_dx) {
+    const Tile& t = l.dx;
+    TcArgs args = base_args(t, d.m, d.k, d.n, 1, status);
+    args.half_bytes -= static_cast<uint32_t>(t.cg) * (128u - a_box(d.m)) * kTcHalf * 2u;
+    set_out(args, grad_x, nullptr, d.k);
+    args.part = reinterpret_cast<float*>(ws + l.part);
+    CUtensorMap maps[4];
+    if ((st = make_map(maps[0], dz.p, d.m, d.n, dz.ld, a_box(d.m))) != GWS_OK || (st = make_map(maps[2], mw.p, d.n, d.k, mw.ld, kTcHalf)) != GWS_OK) return st;
+    maps[1] = maps[0];
+    maps[3] = maps[2];
+    if ((st = launch_mode<kDx>(t, maps, args, sms, s)) != GWS_OK) return st;
+  }
+  if (wants_dw) return run_dw(l.dw.tile, dz, nullptr, mx, l.dw.inside ? &kept_x : nullptr, d.x_format, grad_w, nullptr, d.k, ws + l.part, status, sms, s);
   return GWS_OK;
 }
 

@@ -1,0 +1,168 @@
+// The element-wise part of the backward pass of a linear layer with epilogue:
+//
+//   dz = dy act'(z)  (BF16: the form in which the tensor cores take it)      db = sum_rows dz  (of the FP32 values)      act(z) once more
+//
+// Memory-bound, one pass: 2 + 1 1/32 bytes in (z from a checkpoint), 2 or 4 out per element.  A block takes a strip of 64 columns of a share of the rows, eight lanes to
+// a row and eight columns to a lane, and keeps the column sums in registers.  The shares of a strip are the blocks of a cluster: they are joined through
+// each other's shared memory in a fixed order, so that db needs no second launch and no atomics.
+// The first blocks of the launch make ready what the products after it read (prepare).
+#pragma once
+#include <stdint.h>
+
+#include "gws_tc.cuh"
+
+namespace {
+
+struct LinearPre {
+  const uint16_t* dy;
+  int64_t ld_dy;
+  Act8View save8;
+  const uint16_t* save16;          // [rows, cols]
+  uint16_t* dz;                    // null where dz is dy
+  int64_t ld_dz;
+  uint16_t* again;                 // act(z), [rows, cols]; may be null
+  void* db;                        // may be null
+  int64_t rows, cols;
+  uint32_t first;                  // blocks that prepare
+  uint32_t shares;                 // blocks of a strip, a cluster
+  int32_t activation, db_f32;
+};
+
+template <int ACT>
+__device__ __forceinline__ void slopes(const float (&z)[8], float (&a)[8], float (&slope)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) act_and_slope<ACT>(z[i], a[i], slope[i]);
+}
+
+// WIDE: rows of dy, of a BF16 z and of act(z) on 16-byte boundaries.  Otherwise a warp reads its four rows an element to a lane, side by side, and turns them in
+// shared memory.
+template <int SAVE, bool WIDE>
+__global__ void __launch_bounds__(256) k_linear_pre(const __grid_constant__ LinearPre p, const __grid_constant__ Prep m) {
+  after_previous();
+  if (blockIdx.x < p.first) {
+    (void)prepare(m);
+    return;
+  }
+  __shared__ uint4 turn[WIDE ? 1 : 8][32];
+  __shared__ __align__(16) float sums[32][68];
+  __shared__ float joined[64];
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, oct = threadIdx.x & 7u, slot = threadIdx.x >> 3;
+  const uint32_t b = blockIdx.x - p.first, strip = b / p.shares, share = b - strip * p.shares;
+  const int64_t col0 = static_cast<int64_t>(strip) * 64, col = col0 + oct * 8;
+  const int64_t per = (p.rows + p.shares - 1) / p.shares, begin = share * per, end = min(p.rows, begin + per);
+  auto bring = [&](const uint16_t* base, int64_t ld, int64_t row) {           // eight elements of a row, zeros outside
+    if (WIDE) return row < end && col < p.cols ? __ldg(reinterpret_cast<const uint4*>(base + row * ld + col)) : make_uint4(0u, 0u, 0u, 0u);
+    const int64_t row0 = row - (lane >> 3);
+    uint16_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = row0 + i / 2, c = col0 + (i & 1) * 32 + lane;
+      v[i] = r < end && c < p.cols ? base[r * ld + c] : static_cast<uint16_t>(0);
+    }
+    uint16_t* side = reinterpret_cast<uint16_t*>(turn[WIDE ? 0 : warp]) + lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) side[32 * i] = v[i];
+    __syncwarp();
+    const uint4 w = turn[WIDE ? 0 : warp][lane];
+    __syncwarp();
+    return w;
+  };
+  float db[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) db[i] = 0.0f;
+  constexpr int kRows = 2;                                                     // rows of a thread in flight
+  for (int64_t at = begin; at < end; at += 32 * kRows) {
+    uint4 g[kRows], z16[kRows];
+    uint2 z8[kRows];
+    uint32_t byte[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int64_t row = at + 32 * k + slot;
+      if (p.dy != nullptr) g[k] = bring(p.dy, p.ld_dy, row);
+      if (SAVE == GWS_SAVE_BF16) z16[k] = bring(p.save16, p.cols, row);
+      if (SAVE == GWS_ACT8_INT8 || SAVE == GWS_ACT8_E4M3) {
+        const bool real = row < end && col < p.save8.ld;
+        z8[k] = real ? __ldg(reinterpret_cast<const uint2*>(p.save8.codes + row * p.save8.ld + col)) : make_uint2(0u, 0u);
+        byte[k] = real ? p.save8.scales[row * (p.save8.ld >> 5) + (col >> 5)] : 0u;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int64_t row = at + 32 * k + slot;
+      float z[8], a[8], slope[8];
+      if (SAVE == GWS_SAVE_BF16) {
+        const uint32_t q[4] = {z16[k].x, z16[k].y, z16[k].z, z16[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { z[2 * i] = bf16_lo(q[i]); z[2 * i + 1] = bf16_hi(q[i]); }
+      } else if (SAVE != GWS_SAVE_NONE) {
+        constexpr int kFmt = SAVE == GWS_ACT8_INT8 ? GWS_ACT8_INT8 : GWS_ACT8_E4M3;
+        const float unit = unit_of<kFmt>(byte[k]);
+        decode4<kFmt>(z8[k].x, unit, z);
+        decode4<kFmt>(z8[k].y, unit, z + 4);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = 0.0f;
+      }
+      if (p.activation == GWS_GATED_SILU) slopes<GWS_GATED_SILU>(z, a, slope);
+      else if (p.activation == GWS_GATED_GELU_TANH) slopes<GWS_GATED_GELU_TANH>(z, a, slope);
+      else if (p.activation == GWS_GATED_RELU) slopes<GWS_GATED_RELU>(z, a, slope);
+      else slopes<GWS_ACT_NONE>(z, a, slope);
+      const uint32_t q[4] = {g[k].x, g[k].y, g[k].z, g[k].w};
+      uint32_t w[4];
+      if (p.dy != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          // an element outside has dy = 0; its z may be a NaN (the group's), which must not reach the sum
+          const float d0 = col + 2 * i < p.cols && row < end ? bf16_lo(q[i]) * slope[2 * i] : 0.0f;
+          const float d1 = col + 2 * i + 1 < p.cols && row < end ? bf16_hi(q[i]) * slope[2 * i + 1] : 0.0f;
+          db[2 * i] += d0;
+          db[2 * i + 1] += d1;
+          w[i] = pack_bf16(d0, d1);
+        }
+        if (p.dz != nullptr && row < end) *reinterpret_cast<uint4*>(p.dz + row * p.ld_dz + col) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      if (p.again != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(a[2 * i], a[2 * i + 1]);
+        if (WIDE) {
+          if (row < end && col < p.cols) *reinterpret_cast<uint4*>(p.again + row * p.cols + col) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+          turn[WIDE ? 0 : warp][lane] = make_uint4(w[0], w[1], w[2], w[3]);
+          __syncwarp();
+          const uint16_t* side = reinterpret_cast<const uint16_t*>(turn[WIDE ? 0 : warp]) + lane;
+          const int64_t row0 = row - (lane >> 3);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int64_t r = row0 + i / 2, c = col0 + (i & 1) * 32 + lane;
+            if (r < end && c < p.cols) p.again[r * p.cols + c] = side[32 * i];
+          }
+          __syncwarp();
+        }
+      }
+    }
+  }
+  if (p.db == nullptr) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(&sums[slot][oct * 8u + 4u * i]) = make_float4(db[4 * i], db[4 * i + 1], db[4 * i + 2], db[4 * i + 3]);
+  __syncthreads();
+  if (threadIdx.x < 64u) {
+    float t = 0.0f;
+#pragma unroll 8
+    for (uint32_t r = 0; r < 32u; ++r) t += sums[r][threadIdx.x];
+    joined[threadIdx.x] = t;
+  }
+  if (p.shares > 1u) pair_sync();
+  if (share == 0u && threadIdx.x < 64u && col0 + threadIdx.x < p.cols) {
+    float t = joined[threadIdx.x];
+    for (uint32_t r = 1; r < p.shares; ++r) {
+      float q;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(q) : "r"(at_rank(smem_addr(&joined[threadIdx.x]), r)) : "memory");
+      t += q;
+    }
+    if (p.db_f32 != 0) static_cast<float*>(p.db)[col0 + threadIdx.x] = t;
+    else static_cast<uint16_t*>(p.db)[col0 + threadIdx.x] = static_cast<uint16_t>(pack_bf16(t, 0.0f));
+  }
+  if (p.shares > 1u) pair_sync();              // rank 0 has read this block's sums
+}
+
+}  // namespace

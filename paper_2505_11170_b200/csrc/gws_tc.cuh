@@ -6,7 +6,8 @@
 //   kGatedFew  the same for up to 128 tokens, tiles of 16 to 64 columns of h: every SM gets its share of the weights, and a copy of A
 //            takes only the rows that exist, so that the ring holds more weights in flight.  It is bound by the weights' way from
 //            memory and some 4 us around it (one token, 2048 x 5632: 46 MB in 12 us, 10 from L2; 4096 x 11008: 180 MB in 33 us)
-//   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du
+//   kLinear  y = act(x W^T + b) + r: bias, activation, residual and the copies of z = x W^T + b for the backward pass on registers in the epilogue
+//   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du; dx = dz W is its first half
 //   kDw      dW = dY^T X: both operands are read along their contiguous (not the contracted) axis, as they lie in memory
 //   kDw8     the same with X an 8-bit checkpoint: its codes are copied to shared memory and eight more warps turn them into the BF16
 //            operand there, under the products of earlier stages, so that X crosses L2 and HBM at one byte per element and no BF16
@@ -47,7 +48,7 @@
 
 namespace {
 
-enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4 };
+enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4, kLinear = 5 };
 
 constexpr uint32_t kTcHalf = 64;                           // elements along the contraction per copy: 128 bytes, one swizzle atom
 constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
@@ -75,10 +76,14 @@ struct TcArgs {
   int64_t scales_ld;
   int32_t x_format;
   int32_t box_tokens;                     // kDw, kDw8: tokens in a copy
-  int32_t activation, save;               // kGated
+  int32_t activation, save;               // kGated, kLinear
+  const void* bias;                       // kLinear: null, or BF16 or FP32 [cols]
+  int32_t bias_f32, residual_wide;        // residual_wide: elements a load from `residual` may take, as `wide`
+  const uint16_t* residual;               // null, or BF16 [rows, ld_residual]
+  int64_t ld_residual;
   uint32_t width, stages, a_bytes;        // kGatedFew: columns of h in a tile, stages of the ring, bytes of A in a copy
   int32_t save_wide;                      // the same for the BF16 copies
-  Act8View save8[2];
+  Act8View save8[2];                      // kLinear: the first of both
   uint16_t* save16[2];                    // BF16 copies, [rows, cols]
   int* status;
   int64_t wait_limit;
@@ -232,11 +237,17 @@ __device__ __forceinline__ float sigmoid(float z) {
 }
 template <int ACT>
 __device__ __forceinline__ float act_of(float g) {
+  if (ACT == GWS_ACT_NONE) return g;
   if (ACT == GWS_GATED_RELU) return g < 0.0f ? 0.0f : g;
   return g * sigmoid(sigmoid_arg<ACT>(g));
 }
 template <int ACT>
 __device__ __forceinline__ void act_and_slope(float g, float& a, float& slope) {
+  if (ACT == GWS_ACT_NONE) {
+    a = g;
+    slope = 1.0f;
+    return;
+  }
   if (ACT == GWS_GATED_RELU) {
     a = g < 0.0f ? 0.0f : g;
     slope = g > 0.0f ? 1.0f : 0.0f;
@@ -308,6 +319,112 @@ __device__ __forceinline__ void store_block(uint16_t* out, int64_t ld, int32_t w
   else if (wide >= 2 && width % 2u == 0) store_rows<2>(p, ld, left, width, staging, lane);
   else store_rows<1>(p, ld, left, width, staging, lane);
   __syncwarp();
+}
+
+// The way back: the first `width` columns of a block's rows into shared memory, zeros around them.
+template <uint32_t V>
+__device__ __forceinline__ void load_rows(const uint16_t* p, int64_t ld, int64_t left, uint32_t width, uint32_t* staging, uint32_t lane) {
+  constexpr uint32_t kLanes = 32u / V, kBatch = V == 1u ? 8u : V == 2u ? 4u : 2u;
+  const uint32_t row = lane / kLanes, col = (lane % kLanes) * V;
+  uint32_t* s = staging + row * 17u + col / 2u;
+  p += row * ld + col;
+#pragma unroll
+  for (uint32_t r = 0; r < 32u; r += V * kBatch) {
+    uint32_t v[kBatch][V == 1u ? 1u : V / 2u];
+#pragma unroll
+    for (uint32_t i = 0; i < kBatch; ++i, p += V * ld) {
+      const bool there = r + i * V + row < left && col < width;
+#pragma unroll
+      for (uint32_t e = 0; e < (V == 1u ? 1u : V / 2u); ++e) v[i][e] = 0u;
+      if (!there) continue;
+      if constexpr (V == 1u) v[i][0] = *p;
+      else if constexpr (V == 2u) v[i][0] = *reinterpret_cast<const uint32_t*>(p);
+      else if constexpr (V == 4u) { const uint2 q = *reinterpret_cast<const uint2*>(p); v[i][0] = q.x; v[i][1] = q.y; }
+      else { const uint4 q = *reinterpret_cast<const uint4*>(p); v[i][0] = q.x; v[i][1] = q.y; v[i][2] = q.z; v[i][3] = q.w; }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kBatch; ++i) {
+      if constexpr (V == 1u) {
+        reinterpret_cast<uint16_t*>(s + (r + i) * 17u)[lane & 1u] = static_cast<uint16_t>(v[i][0]);
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < V / 2u; ++e) s[(r + i * V) * 17u + e] = v[i][e];
+      }
+    }
+  }
+}
+// Reads a 32 x 32 block of BF16, one row to a lane (16 words of two columns each); what is outside [rows, cols] is zero.
+__device__ __forceinline__ void load_block(const uint16_t* in, int64_t ld, int32_t wide, int64_t row0, int64_t col0, int64_t rows, int64_t cols, uint32_t (&w)[16],
+                                           uint32_t* staging, uint32_t lane) {
+  if (wide == 16 && col0 + 32 <= cols) {
+    V8 a, b;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a.x[i] = b.x[i] = 0u;
+    if (row0 + lane < rows) {
+      const uint16_t* p = in + (row0 + lane) * ld + col0;
+      a = ld32(p);
+      b = ld32(p + 16);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { w[i] = a.x[i]; w[8 + i] = b.x[i]; }
+    return;
+  }
+  const int64_t left = rows - row0;
+  const uint16_t* p = in + row0 * ld + col0;
+  const uint32_t width = col0 + 32 <= cols ? 32u : static_cast<uint32_t>(cols - col0);
+  __syncwarp();
+  if (wide >= 8 && width % 8u == 0) load_rows<8>(p, ld, left, width, staging, lane);
+  else if (wide >= 4 && width % 4u == 0) load_rows<4>(p, ld, left, width, staging, lane);
+  else if (wide >= 2 && width % 2u == 0) load_rows<2>(p, ld, left, width, staging, lane);
+  else load_rows<1>(p, ld, left, width, staging, lane);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = staging[lane * 17u + i];
+  __syncwarp();
+}
+
+// y = act(z) + r of a 32 x 32 block, one row to a lane.
+template <int ACT>
+__device__ __forceinline__ void finish_block(const float (&z)[32], const uint32_t (&r)[16], uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = pack_bf16(act_of<ACT>(z[2 * i]) + bf16_lo(r[i]), act_of<ACT>(z[2 * i + 1]) + bf16_hi(r[i]));
+}
+__device__ __forceinline__ float act_of_kind(int32_t kind, float z) {
+  return kind == GWS_ACT_NONE ? z : kind == GWS_GATED_SILU ? act_of<GWS_GATED_SILU>(z) : kind == GWS_GATED_GELU_TANH ? act_of<GWS_GATED_GELU_TANH>(z) : act_of<GWS_GATED_RELU>(z);
+}
+__device__ __forceinline__ float bias_at(const TcArgs& p, int64_t col) {
+  if (p.bias == nullptr || col >= p.cols) return 0.0f;
+  return p.bias_f32 != 0 ? static_cast<const float*>(p.bias)[col] : __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(p.bias)[col]) << 16);
+}
+
+// The same of four columns of a row, from sums without the bias; eight neighbouring lanes hold a group of 32 columns.  Writes the copy of z, leaves y in v.
+__device__ __forceinline__ void finish_four(const TcArgs& p, int64_t row, int64_t col, uint32_t lane, float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] += bias_at(p, col + i);
+  if (p.save == GWS_SAVE_BF16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < p.cols) p.save16[0][row * p.cols + col + i] = static_cast<uint16_t>(pack_bf16(v[i], 0.0f));
+  } else if (p.save != GWS_SAVE_NONE) {
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const Act8View& o = p.save8[0];
+    const uint32_t byte = scale_byte(top, p.save);
+    const float inv = inverse_scale_of(byte);
+    const uint32_t codes = byte == kNanByte ? 0u : p.save == GWS_ACT8_INT8 ? encode4_int8(v[0], v[1], v[2], v[3], inv) : encode4_e4m3(v[0], v[1], v[2], v[3], inv);
+    if (col < o.ld) {
+      *reinterpret_cast<uint32_t*>(o.codes + row * o.ld + col) = codes;
+      if ((lane & 7u) == 0u) o.scales[row * (o.ld >> 5) + (col >> 5)] = static_cast<uint8_t>(byte);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = act_of_kind(p.activation, v[i]);
+    if (p.residual != nullptr && col + i < p.cols) v[i] += __uint_as_float(static_cast<uint32_t>(p.residual[row * p.ld_residual + col + i]) << 16);
+  }
 }
 
 template <int ACT>
@@ -407,7 +524,8 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
          const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
   using S = TcShape<CG, BN, MODE>;
-  constexpr bool kFew = MODE == kGatedFew, kIsGated = MODE == kGated || kFew, kIsDw = MODE == kDw || MODE == kDw8, kMnA = kIsDw, kMnB = !kIsGated;
+  constexpr bool kFew = MODE == kGatedFew, kIsGated = MODE == kGated || kFew, kIsLinear = MODE == kLinear, kIsDw = MODE == kDw || MODE == kDw8;
+  constexpr bool kMnA = kIsDw, kMnB = !kIsGated && !kIsLinear;
   constexpr uint32_t kStages = S::kStages;
   const uint32_t stages = kFew ? p.stages : kStages, width = kFew ? p.width : BN / 2;      // width: columns of h in a tile (kIsGated)
   const uint32_t a_bytes = kFew ? p.a_bytes : kTcABytes, half_pitch = kFew ? a_bytes + width * (kTcHalf * 4u) : S::kHalf, stage_pitch = S::kHalves * half_pitch;
@@ -416,7 +534,8 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
                          ((kFew ? width >> 2 : static_cast<uint32_t>(BN >> 3)) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], meet[4], codes_full[kStages], converted[kStages];
-  __shared__ __align__(16) uint8_t scale_bytes[2][2][kIsGated ? 128 : 1][4];      // of two tiles, gate and up projection
+  __shared__ __align__(16) uint8_t scale_bytes[2][2][kIsGated || kIsLinear ? 128 : 1][4];      // of two tiles, gate and up projection (left and right half)
+  __shared__ __align__(16) float bias_of[kIsLinear ? S::kEpilogueWarps : 1u][kIsLinear ? BN / 2 : 1];     // of a warp's chunks
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int failed;
   const uint32_t raw = smem_addr(smem_raw);
@@ -506,6 +625,9 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
                 copy_in<CG>(sb, &b0, bar, ki, n0);
                 copy_in<CG>(sb + width * (kTcHalf * 2u), &b1, bar, ki, n0);
               }
+            } else if (kIsLinear) {
+              copy_in<CG>(sa, &a0, bar, ki, m0);
+              copy_in<CG>(sb, &b0, bar, ki, n0);
             } else if (MODE == kDx) {
               copy_in<CG>(sa, seg ? &a1 : &a0, bar, ki, m0);
 #pragma unroll
@@ -589,6 +711,11 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       uint32_t mt, nt, k0, k1;
       place(t, mt, nt, k0, k1);
       const uint32_t buf = n & 1u;
+      if (kIsLinear) {                   // under the products
+#pragma unroll
+        for (uint32_t i = 0; i < BN / 64; ++i) bias_of[warp - 4u][i * 32u + lane] = bias_at(p, static_cast<int64_t>(nt) * BN + (half + 2u * i) * 32u + lane);
+        __syncwarp();
+      }
       if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u, p.wait_limit)) {
         failed = 1;
         break;
@@ -620,6 +747,46 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x.x[e] = v[8 * i + e];
             st32(part + c * 32u + 8 * i, x);
+          }
+        }
+      } else if (kIsLinear) {
+#pragma unroll 1
+        for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
+          const int64_t col0 = static_cast<int64_t>(nt) * BN + c * 32u;
+          if (col0 >= p.cols) break;
+          uint32_t v[32], r[16], w[16];
+          acc_load(acc + c * 32u, v);
+          if (p.residual != nullptr) {
+            load_block(p.residual, p.ld_residual, p.residual_wide, row0, col0, p.rows, p.cols, r, stage, lane);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r[e] = 0u;
+          }
+          acc_wait();
+          float z[32];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float4 b = reinterpret_cast<const float4*>(bias_of[warp - 4u] + c / 2u * 32u)[e];
+            z[4 * e] = __uint_as_float(v[4 * e]) + b.x;
+            z[4 * e + 1] = __uint_as_float(v[4 * e + 1]) + b.y;
+            z[4 * e + 2] = __uint_as_float(v[4 * e + 2]) + b.z;
+            z[4 * e + 3] = __uint_as_float(v[4 * e + 3]) + b.w;
+          }
+          if (p.activation == GWS_ACT_NONE) finish_block<GWS_ACT_NONE>(z, r, w);
+          else if (p.activation == GWS_GATED_SILU) finish_block<GWS_GATED_SILU>(z, r, w);
+          else if (p.activation == GWS_GATED_GELU_TANH) finish_block<GWS_GATED_GELU_TANH>(z, r, w);
+          else finish_block<GWS_GATED_RELU>(z, r, w);
+          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
+          if (p.save == GWS_SAVE_BF16) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(z[2 * e], z[2 * e + 1]);
+            store_block(p.save16[0], p.cols, p.save_wide, row0, col0, p.rows, p.cols, w, stage, lane);
+          } else if (p.save != GWS_SAVE_NONE && row0 + lane < p.rows) {
+            // columns past the width are products with rows of zeros and have no bias: zero codes, as the layout wants them
+            V8 codes;
+            const uint32_t byte = p.save == GWS_ACT8_INT8 ? encode_group<GWS_ACT8_INT8>(z, codes) : encode_group<GWS_ACT8_E4M3>(z, codes);
+            st32(p.save8[0].codes + (row0 + lane) * p.save8[0].ld + col0, codes);
+            scale_bytes[buf][c / (BN / 64)][quadrant * 32u + lane][c % (BN / 64)] = static_cast<uint8_t>(byte);
           }
         }
       } else if (kIsGated) {
@@ -658,27 +825,6 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
             }
           }
         }
-        if (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3) {
-          // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
-          // The two warps that share these rows meet; one writes the gate's, the other the up projection's.  A warp that fills the same
-          // buffer again has passed the meeting of the tile between, and so has the other one's store.  They meet at an mbarrier, one
-          // phase a tile, because a wait there has a limit: a warp that left its loop does not leave the other one behind for good.
-          __syncwarp();
-          if (lane == 0) bar_arrive(smem_addr(&meet[quadrant]));
-          if (!bar_wait(smem_addr(&meet[quadrant]), n & 1u, p.wait_limit)) { failed = 1; break; }
-          const int64_t row = row0 + lane, ld = p.save8[half].ld >> 5, g0 = static_cast<int64_t>(nt) * (width / 32u);
-          if (row < p.rows) {
-            uint8_t* to = p.save8[half].scales + row * ld + g0;
-            const uint8_t* from = scale_bytes[buf][half][quadrant * 32u + lane];
-            const uint32_t groups = width / 32u;
-            if (groups > 1u && g0 + groups <= ld && ld % groups == 0) {       // the buffer's scales start at a multiple of 256 bytes
-              if (groups == 4u) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
-              else *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
-            } else {
-              for (uint32_t i = 0; i < groups && g0 + i < ld; ++i) to[i] = from[i];
-            }
-          }
-        }
       } else {
         uint16_t* out = static_cast<uint16_t*>(p.out[second ? 1 : 0]);
 #pragma unroll 1
@@ -691,6 +837,28 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
 #pragma unroll
           for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
           store_block(out, p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
+        }
+      }
+      if ((kIsGated || kIsLinear) && t < p.whole && (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3)) {
+        // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
+        // The two warps that share these rows meet; one writes the gate's (or the left half's), the other the up projection's (the right half's).  A warp that fills the same
+        // buffer again has passed the meeting of the tile between, and so has the other one's store.  They meet at an mbarrier, one
+        // phase a tile, because a wait there has a limit: a warp that left its loop does not leave the other one behind for good.
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_addr(&meet[quadrant]));
+        if (!bar_wait(smem_addr(&meet[quadrant]), n & 1u, p.wait_limit)) { failed = 1; break; }
+        const Act8View& kept = p.save8[kIsLinear ? 0u : half];
+        const uint32_t groups = width / 32u;
+        const int64_t row = row0 + lane, ld = kept.ld >> 5, g0 = kIsLinear ? (static_cast<int64_t>(nt) * 2 + half) * groups : static_cast<int64_t>(nt) * groups;
+        if (row < p.rows) {
+          uint8_t* to = kept.scales + row * ld + g0;
+          const uint8_t* from = scale_bytes[buf][half][quadrant * 32u + lane];
+          if (groups > 1u && g0 + groups <= ld && ld % groups == 0) {       // the buffer's scales start at a multiple of 256 bytes
+            if (groups == 4u) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
+            else *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
+          } else {
+            for (uint32_t i = 0; i < groups && g0 + i < ld; ++i) to[i] = from[i];
+          }
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -770,6 +938,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         for (int i = 0; i < 4; ++i) v[i] = k == 0 ? q[i] : v[i] + q[i];
       }
       uint16_t* to = out + (row0 + r) * p.ld_out + col;
+      if (kIsLinear) finish_four(p, row0 + r, col, lane, v);
       const uint32_t lo = pack_bf16(v[0], v[1]), hi = pack_bf16(v[2], v[3]);
       if (p.wide >= 4 && col + 4 <= p.cols) {
         *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
@@ -840,15 +1009,20 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
     const int64_t row = row0 + i;
     if (row >= p.rows) break;
     float v = a[i];
+    if (MODE == kLinear) {
+      a[i] += bias_at(p, col);
+      v = act_of_kind(p.activation, a[i]);
+      if (p.residual != nullptr && col < p.cols) v += __uint_as_float(static_cast<uint32_t>(p.residual[row * p.ld_residual + col]) << 16);
+    }
     if (MODE == kGated) {
       const float act = p.activation == GWS_GATED_SILU ? act_of<GWS_GATED_SILU>(a[i])
                         : p.activation == GWS_GATED_GELU_TANH ? act_of<GWS_GATED_GELU_TANH>(a[i]) : act_of<GWS_GATED_RELU>(a[i]);
       v = act * b[i];
     }
     if (col < p.cols) static_cast<uint16_t*>(p.out[second ? 1 : 0])[row * p.ld_out + col] = static_cast<uint16_t>(pack_bf16(v, 0.0f));
-    if (MODE == kGated && p.save != GWS_SAVE_NONE) {
+    if ((MODE == kGated || MODE == kLinear) && p.save != GWS_SAVE_NONE) {
 #pragma unroll
-      for (int which = 0; which < 2; ++which) {
+      for (int which = 0; which < (MODE == kGated ? 2 : 1); ++which) {
         const float x = which == 0 ? a[i] : b[i];
         if (p.save == GWS_SAVE_BF16) {
           if (col < p.cols) p.save16[which][row * p.cols + col] = static_cast<uint16_t>(pack_bf16(x, 0.0f));
