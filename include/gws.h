@@ -624,7 +624,8 @@ int gws_layernorm_bwd(const gws_norm_desc* desc, const void* grad_y, const void*
  *       code 16 e + f, 0 for code 0.  Codes are value * (1 / unit) rounded to nearest even; a root above zero has a code of at least 1.  A group whose
  *       largest value is below 2^-100 is stored as zeros with unit 0, one that is not finite has a NaN for its unit and restores as NaN.
  *   rest            int16 [total], or NULL.  With it a BF16 parameter stands for the 32-bit weight whose bits are (its bits << 16) + rest; the
- *       parameter is the nearest BF16 number to it, the one larger in magnitude of two as near.  Without it a BF16 parameter is rounded to nearest
+ *       parameter is the nearest BF16 number to it, the one larger in magnitude of two as near (a zero under a negative
+ *       rest, which no step leaves, counts as zero).  Without it a BF16 parameter is rounded to nearest
  *       even at every step.  FP32 parameters leave it alone. */
 typedef enum gws_adamw_format { GWS_ADAMW_F32 = 0, GWS_ADAMW_8BIT = 1 } gws_adamw_format;
 typedef struct gws_adamw_state {

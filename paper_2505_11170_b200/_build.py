@@ -21,8 +21,8 @@ SOURCES = [os.path.join(CSRC, name) for name in _UNITS]
 HEADERS = sorted({os.path.join(CSRC, h) for hs in _UNITS.values() for h in hs}) + [os.path.join(INCLUDE, "gws.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
-# -fmad=false: the add-then-cast path must round the multiply and the add separately.
-_UNIT_FLAGS = {"gws_api.cu": ["-fmad=false"], "gws_block.cu": [], "gws_step.cu": []}
+# -fmad=false: the add-then-cast path and the optimizer round every multiply and every add separately.
+_UNIT_FLAGS = {"gws_api.cu": ["-fmad=false"], "gws_block.cu": [], "gws_step.cu": ["-fmad=false"]}
 
 
 def _nvcc() -> str:

@@ -28,7 +28,6 @@
 namespace {
 
 constexpr uint32_t kAdamwGroup = 256;             // elements of a group: eight to a lane
-constexpr uint32_t kAdamwGroups = 16;             // groups of a block of eight warps
 constexpr float kAdamwLeast = 0x1p-100f;          // a largest value below this is stored as zero
 
 struct AdamwRec {
@@ -49,6 +48,7 @@ struct AdamwArgs {
   const float* grad_scale;
   const float* scalars;           // alpha, rho, lr on the device, or null
   float b1, to_m, b2, to_v, eps, alpha, rho;
+  uint32_t per;                   // groups of a block of eight warps
   int32_t n;
 };
 template <int CAP>
@@ -66,59 +66,132 @@ __device__ __forceinline__ V8 take32(const void* p) {     // memory that the sam
   return v;
 }
 
-// A lane's eight consecutive elements of a group, as FP32 bits.  `wide`: the whole group exists and lies on boundaries of eight elements; otherwise the warp reads
-// (writes) neighbouring elements with neighbouring lanes and `turn` gives each lane its eight.
-__device__ __forceinline__ void adamw_read(const void* p, bool f32, bool wide, int64_t left, uint32_t lane, uint32_t* turn, float (&x)[8]) {
-  if (wide) {
-    if (f32) {
-      const V8 v = take32(static_cast<const float*>(p) + lane * 8u);
+// A lane's eight consecutive elements of a parameter and of its gradient, as they come from memory.  WIDE: whole groups on boundaries of eight elements, four words of
+// BF16 pairs or eight of FP32.  Otherwise the warp reads neighbouring elements with neighbouring lanes, and `turn` gives each lane its eight.
+template <bool F32, bool WIDE>
+struct AdamwWords {
+  uint32_t x[WIDE && !F32 ? 4 : 8];
+};
+template <bool F32, bool WIDE>
+__device__ __forceinline__ void adamw_fetch(const void* p, int64_t left, uint32_t lane, AdamwWords<F32, WIDE>& w) {
+  if constexpr (WIDE && F32) {
+    const V8 v = take32(static_cast<const float*>(p) + lane * 8u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v.x[i]);
-    } else {
-      const uint4 v = reinterpret_cast<const uint4*>(p)[lane];
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < 8; ++i) w.x[i] = v.x[i];
+  } else if constexpr (WIDE) {
+    const uint4 v = reinterpret_cast<const uint4*>(p)[lane];
+    w.x[0] = v.x; w.x[1] = v.y; w.x[2] = v.z; w.x[3] = v.w;
+  } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t at = lane + 32u * i;
+      w.x[i] = at >= left ? 0u : F32 ? static_cast<const uint32_t*>(p)[at] : static_cast<uint32_t>(static_cast<const uint16_t*>(p)[at]);
     }
-    return;
   }
-  uint32_t v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t at = lane + 32u * i;
-    v[i] = at >= left ? 0u : f32 ? static_cast<const uint32_t*>(p)[at] : static_cast<uint32_t>(static_cast<const uint16_t*>(p)[at]) << 16;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) turn[lane + 32u * i] = v[i];
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(turn[lane * 8u + i]);
-  __syncwarp();
 }
-// x: FP32 bits, or for BF16 the number's 16 bits.
-__device__ __forceinline__ void adamw_write(void* p, bool f32, bool wide, int64_t left, uint32_t lane, uint32_t* turn, const uint32_t (&x)[8]) {
-  if (wide) {
-    if (f32) {
-      V8 v;
+// The lane's own eight: words of BF16 pairs, or FP32.
+template <bool F32, bool WIDE>
+__device__ __forceinline__ void adamw_turn(const AdamwWords<F32, WIDE>& w, uint32_t lane, uint4* turn, uint32_t (&x)[F32 ? 8 : 4]) {
+  if constexpr (WIDE) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v.x[i] = x[i];
-      st32(static_cast<float*>(p) + lane * 8u, v);
-    } else {
-      reinterpret_cast<uint4*>(p)[lane] = make_uint4(x[0] | (x[1] << 16), x[2] | (x[3] << 16), x[4] | (x[5] << 16), x[6] | (x[7] << 16));
+    for (int i = 0; i < (F32 ? 8 : 4); ++i) x[i] = w.x[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (F32) reinterpret_cast<uint32_t*>(turn)[lane + 32 * i] = w.x[i];
+      else reinterpret_cast<uint16_t*>(turn)[lane + 32 * i] = static_cast<uint16_t>(w.x[i]);
     }
-    return;
-  }
+    __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) turn[lane * 8u + i] = x[i];
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t at = lane + 32u * i;
-    if (at >= left) continue;
-    if (f32) static_cast<uint32_t*>(p)[at] = turn[at];
-    else static_cast<uint16_t*>(p)[at] = static_cast<uint16_t>(turn[at]);
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) {
+      const uint4 v = turn[lane * (F32 ? 2 : 1) + i];
+      x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+    }
+    __syncwarp();
   }
-  __syncwarp();
+}
+template <bool F32, bool WIDE>
+__device__ __forceinline__ void adamw_write(void* p, int64_t left, uint32_t lane, uint4* turn, const uint32_t (&x)[F32 ? 8 : 4]) {
+  if constexpr (WIDE && F32) {
+    V8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.x[i] = x[i];
+    st32(static_cast<float*>(p) + lane * 8u, v);
+  } else if constexpr (WIDE) {
+    reinterpret_cast<uint4*>(p)[lane] = make_uint4(x[0], x[1], x[2], x[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) turn[lane * (F32 ? 2 : 1) + i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t at = lane + 32u * i;
+      if (at >= left) continue;
+      if constexpr (F32) static_cast<uint32_t*>(p)[at] = reinterpret_cast<const uint32_t*>(turn)[at];
+      else static_cast<uint16_t*>(p)[at] = reinterpret_cast<const uint16_t*>(turn)[at];
+    }
+    __syncwarp();
+  }
+}
+
+// Two FP32 numbers in a register pair: one instruction rounds both as the scalar ones do.
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 two(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 both(float a) { return two(a, a); }
+__device__ __forceinline__ float first_of(F2 a) {
+  float x;
+  asm("mov.b64 {%0, _}, %1;" : "=f"(x) : "l"(a.v));
+  return x;
+}
+__device__ __forceinline__ float second_of(F2 a) {
+  float y;
+  asm("mov.b64 {_, %0}, %1;" : "=f"(y) : "l"(a.v));
+  return y;
+}
+// Two additions: add.rn.f32x2 would be fused with a mul.rn.f32x2 before it, under -fmad=false too.
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { return two(__fadd_rn(first_of(a), first_of(b)), __fadd_rn(second_of(a), second_of(b))); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
+// Square root and quotient to the nearest, of pairs, by the residual of an approximation (Markstein's method): with g near sqrt(v) and h near 1 / (2 sqrt(v)), g + (v - g g) h
+// rounds as sqrt(v) does, and with y near 1 / d and q near n / d, q + (n - d q) y as n / d.  Both approximations are brought to FP32's own precision by one step (the
+// reciprocal by two) of Newton's iteration before.  v in [2^-100, 2^100], d in [2^-40, 2^81], n up to 2^70; a quotient of an n below 2^-100, whose residual may be below the
+// smallest number, can be one unit of its last place off.  All 2^24 significands of a root and 10^9 quotients agree with sqrt.rn and div.rn.
+__device__ __forceinline__ F2 root2(F2 v) {
+  float y0, y1;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(first_of(v)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(second_of(v)));
+  const F2 y = two(y0, y1);
+  F2 g = mul2(v, y), h = mul2(y, both(-0.5f));                 // h is held with its sign changed
+  const F2 e = fma2(g, h, both(0.5f));
+  g = fma2(g, e, g);
+  h = fma2(h, e, h);
+  return fma2(two(__fmaf_rn(first_of(g), first_of(g), -first_of(v)), __fmaf_rn(second_of(g), second_of(g), -second_of(v))), h, g);
+}
+__device__ __forceinline__ F2 quotient2(F2 n, F2 d) {
+  float y0, y1;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(first_of(d)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(second_of(d)));
+  const F2 minus = mul2(d, both(-1.0f)), one = both(1.0f);
+  F2 y = two(y0, y1);
+  y = fma2(fma2(minus, y, one), y, y);
+  y = fma2(fma2(minus, y, one), y, y);
+  const F2 q = mul2(n, y);
+  return fma2(fma2(minus, q, n), y, q);
 }
 
 // Unit of a group from the FP32 bits of its largest magnitude; NaN where that is not finite.
@@ -129,35 +202,221 @@ __device__ __forceinline__ float adamw_unit(uint32_t top, float step) {
 }
 __device__ __forceinline__ float adamw_inverse(float unit) { return unit > 0.0f ? __frcp_rn(unit) : 0.0f; }
 
-__device__ __forceinline__ uint2 adamw_encode_m(const float (&m)[8], float inv) {
+__device__ __forceinline__ uint2 adamw_encode_m(const F2 (&m)[4], float inv) {
   uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) w[i] = encode4_e4m3(m[4 * i], m[4 * i + 1], m[4 * i + 2], m[4 * i + 3], inv);
-  return make_uint2(w[0], w[1]);
-}
-__device__ __forceinline__ uint2 adamw_encode_r(const float (&r)[8], float inv) {
-  uint32_t w[2] = {0u, 0u};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t bits = __float_as_uint(__fmul_rn(r[i], inv));          // at most a little above 1.9375
-    const int32_t code = static_cast<int32_t>((bits + 0x3FFFFu + ((bits >> 19) & 1u)) >> 19) - (112 << 4);
-    const uint32_t c = r[i] > 0.0f && inv > 0.0f ? static_cast<uint32_t>(min(max(code, 1), 255)) : 0u;
-    w[i >> 2] |= c << (8 * (i & 3));
+  for (int i = 0; i < 2; ++i) {
+    const F2 a = mul2(m[2 * i], both(inv)), b = mul2(m[2 * i + 1], both(inv));
+    w[i] = static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(first_of(a), second_of(a)), __NV_SATFINITE, __NV_E4M3)) |
+           static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(make_float2(first_of(b), second_of(b)), __NV_SATFINITE, __NV_E4M3)) << 16;
   }
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void adamw_decode_m(uint2 c, float unit, float (&m)[8]) {
-  float a[4], b[4];
-  decode4_e4m3(c.x, unit, a);
-  decode4_e4m3(c.y, unit, b);
+// `zeros`: there may be roots of zero among them.
+__device__ __forceinline__ uint2 adamw_encode_r(const F2 (&r)[4], float inv, bool zeros) {
+  uint32_t c[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { m[i] = a[i]; m[4 + i] = b[i]; }
+  for (int i = 0; i < 4; ++i) {
+    const F2 t = mul2(r[i], both(inv));                  // at most a little above 1.9375
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t bits = __float_as_uint(e == 0 ? first_of(t) : second_of(t));
+      // to four bits of mantissa, nearest even; the code is what stands above bit 19
+      const int32_t code = static_cast<int32_t>(bits + ((bits >> 19) & 1u) + (0x3FFFFu - (112u << 23)));
+      c[2 * i + e] = static_cast<uint32_t>(max(code, 1 << 19)) << 5;
+    }
+  }
+  uint2 w = make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410),
+                       __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410));
+  if (zeros) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = (i & 1) == 0 ? first_of(r[i / 2]) : second_of(r[i / 2]);
+      if (!(x > 0.0f)) (i < 4 ? w.x : w.y) &= ~(255u << (8 * (i & 3)));
+    }
+  }
+  return inv > 0.0f ? w : make_uint2(0u, 0u);
 }
-__device__ __forceinline__ void adamw_decode_r(uint2 c, float unit, float (&r)[8]) {
+__device__ __forceinline__ void adamw_decode_m(uint2 c, float unit, F2 (&m)[4]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t code = ((i < 4 ? c.x : c.y) >> (8 * (i & 3))) & 255u;
-    r[i] = __fmul_rn(code != 0u ? __uint_as_float((code + (112u << 4)) << 19) : 0.0f, unit);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = i < 2 ? c.x : c.y;
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>((i & 1) == 0 ? w & 0xFFFFu : w >> 16), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    m[i] = mul2(two(f.x, f.y), both(unit));
+  }
+}
+__device__ __forceinline__ void adamw_decode_r(uint2 c, float unit, F2 (&r)[4]) {
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float((__byte_perm(i < 4 ? c.x : c.y, 0u, 0x4440u + (i & 3)) << 19) + (112u << 23));
+  const auto has_zero = [](uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; };
+  if (has_zero(c.x) || has_zero(c.y)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((((i < 4 ? c.x : c.y) >> (8 * (i & 3))) & 255u) == 0u) x[i] = 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = mul2(two(x[2 * i], x[2 * i + 1]), both(unit));
+}
+
+struct AdamwScalars {
+  float scale, alpha, rho, decay;
+  bool exact;                     // eps, alpha and rho are of sizes at which root2 and quotient2 are exact
+};
+
+// Groups first + warp, first + warp + 8, ... of a tensor, up to `end`.
+template <int FMT, bool F32, bool WIDE>
+__device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e, const AdamwScalars& k, int64_t first, int64_t end, uint4* turn) {
+  // With 8-bit moments a group is 3.6 KB and long arithmetic: the next one's loads are under way meanwhile.
+  constexpr bool kAhead = FMT == GWS_ADAMW_8BIT && !F32;
+  constexpr uint32_t kSize = F32 ? 4u : 2u;
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  const bool keeps = !F32 && a.rest != nullptr;
+  struct Raw {
+    AdamwWords<F32, WIDE> g, p;
+    uint4 low;
+    uint2 cm, cr;
+    float um, ur;
+    V8 m, v;
+  } next;
+  auto fetch = [&](int64_t u, Raw& r) {
+    const int64_t at = u * kAdamwGroup, group = e.group0 + u, s = group * kAdamwGroup + lane * 8u;
+    if (FMT == GWS_ADAMW_8BIT) {
+      r.cm = *reinterpret_cast<const uint2*>(a.codes + s);
+      r.cr = *reinterpret_cast<const uint2*>(a.codes + a.total + s);
+      r.um = a.units[group];
+      r.ur = a.units[a.total / kAdamwGroup + group];
+    } else {
+      r.m = take32(a.codes + s * 4);
+      r.v = take32(a.codes + (a.total + s) * 4);
+    }
+    r.low = make_uint4(0u, 0u, 0u, 0u);
+    if (keeps) r.low = *reinterpret_cast<const uint4*>(a.rest + s);
+    adamw_fetch<F32, WIDE>(static_cast<const char*>(e.g) + at * kSize, e.n - at, lane, r.g);
+    adamw_fetch<F32, WIDE>(static_cast<const char*>(e.p) + at * kSize, e.n - at, lane, r.p);
+  };
+  int64_t u = first + warp;
+  if (kAhead && u < end) fetch(u, next);
+#pragma unroll 1
+  for (; u < end; u += 8) {
+    Raw raw;
+    if (kAhead) {
+      raw = next;
+      if (u + 8 < end) fetch(u + 8, next);
+    } else {
+      fetch(u, raw);
+    }
+    const int64_t group = e.group0 + u, s = group * kAdamwGroup + lane * 8u;
+    uint32_t gw[F32 ? 8 : 4], pw[F32 ? 8 : 4];
+    adamw_turn<F32, WIDE>(raw.g, lane, turn, gw);
+    adamw_turn<F32, WIDE>(raw.p, lane, turn, pw);
+    const uint32_t lw[4] = {raw.low.x, raw.low.y, raw.low.z, raw.low.w};
+    float p[8];
+    F2 m[4], v[4], r[4];
+    if (FMT == GWS_ADAMW_8BIT) {
+      adamw_decode_m(raw.cm, raw.um, m);
+      adamw_decode_r(raw.cr, raw.ur, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m[i] = two(__uint_as_float(raw.m.x[2 * i]), __uint_as_float(raw.m.x[2 * i + 1]));
+        v[i] = two(__uint_as_float(raw.v.x[2 * i]), __uint_as_float(raw.v.x[2 * i + 1]));
+      }
+    }
+    float least = __uint_as_float(0x7F800000u), most = 0.0f, top = 0.0f;      // the last two NaN if any is
+    F2 odd = both(0.0f);                                                      // zero, or NaN if a weight is not finite
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      F2 g;
+      if constexpr (F32) {
+        g = two(__uint_as_float(gw[2 * i]), __uint_as_float(gw[2 * i + 1]));
+        p[2 * i] = __uint_as_float(pw[2 * i]);
+        p[2 * i + 1] = __uint_as_float(pw[2 * i + 1]);
+      } else {
+        g = two(bf16_lo(gw[i]), bf16_hi(gw[i]));
+        // the weight's bits, (p << 16) + rest: the upper halves are one lower where the rest is negative
+        const uint32_t upper = pw[i] - ((lw[i] >> 15) & 0x00010001u);
+        p[2 * i] = __uint_as_float(__byte_perm(lw[i], upper, 0x5410));
+        p[2 * i + 1] = __uint_as_float(__byte_perm(lw[i], upper, 0x7632));
+      }
+      g = mul2(g, both(k.scale));
+      m[i] = add2(mul2(m[i], both(a.b1)), mul2(g, both(a.to_m)));
+      v[i] = add2(mul2(v[i], both(a.b2)), mul2(mul2(g, both(a.to_v)), g));
+      least = fminf(least, fminf(first_of(v[i]), second_of(v[i])));
+      most = max_nan(most, max_nan(first_of(v[i]), second_of(v[i])));
+      top = max_nan(top, max_nan(fabsf(first_of(m[i])), fabsf(second_of(m[i]))));
+      odd = fma2(two(p[2 * i], p[2 * i + 1]), both(0.0f), odd);
+    }
+    // Whether all of this lane's numbers are where root2 and quotient2 are exact; a v of zero is not.
+    const bool plain = k.exact && least >= 0x1p-100f && most <= 0x1p100f && top <= 0x1p40f && first_of(odd) + second_of(odd) == 0.0f;
+    uint32_t top_m = __float_as_uint(top), top_r = 0u;
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r[i] = root2(v[i]);
+        const F2 q = quotient2(mul2(m[i], both(-k.alpha)), add2(mul2(r[i], both(k.rho)), both(a.eps)));
+        const F2 w = add2(mul2(two(p[2 * i], p[2 * i + 1]), both(k.decay)), q);
+        p[2 * i] = first_of(w);
+        p[2 * i + 1] = second_of(w);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (!F32) {                            // a zero under a negative rest, which only a parameter set from outside is: zero
+          const uint32_t half = pw[i / 2] >> (16 * (i & 1)) & 0xFFFFu;
+          const int32_t low = static_cast<int16_t>(lw[i / 2] >> (16 * (i & 1)));
+          p[i] = __uint_as_float((half & 0x7FFFu) == 0u && low < 0 ? half << 16 : (half << 16) + static_cast<uint32_t>(low));
+        }
+        const float mi = (i & 1) == 0 ? first_of(m[i / 2]) : second_of(m[i / 2]), ri = __fsqrt_rn((i & 1) == 0 ? first_of(v[i / 2]) : second_of(v[i / 2]));
+        r[i / 2] = (i & 1) == 0 ? two(ri, ri) : two(first_of(r[i / 2]), ri);
+        p[i] = __fsub_rn(__fmul_rn(p[i], k.decay), __fdiv_rn(__fmul_rn(mi, k.alpha), __fadd_rn(__fmul_rn(ri, k.rho), a.eps)));
+        if (p[i] != p[i]) p[i] = __uint_as_float(0x7FC00000u);         // which stays a NaN when it is rounded
+        top_m = max(top_m, __float_as_uint(mi) & 0x7FFFFFFFu);          // a NaN is above everything
+      }
+    }
+    if (FMT == GWS_ADAMW_8BIT) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top_r = max(top_r, max(__float_as_uint(first_of(r[i])) & 0x7FFFFFFFu, __float_as_uint(second_of(r[i])) & 0x7FFFFFFFu));
+      const float um = adamw_unit(__reduce_max_sync(0xFFFFFFFFu, top_m), 1.0f / 448.0f), ur = adamw_unit(__reduce_max_sync(0xFFFFFFFFu, top_r), 1.0f / 1.9375f);
+      // a group that is not finite has a NaN for its unit and codes of zero: it restores as NaN
+      const float im = adamw_inverse(um), ir = adamw_inverse(ur);
+      *reinterpret_cast<uint2*>(a.codes + s) = im > 0.0f ? adamw_encode_m(m, im) : make_uint2(0u, 0u);
+      *reinterpret_cast<uint2*>(a.codes + a.total + s) = adamw_encode_r(r, ir, !plain);
+      if (lane == 0) {
+        a.units[group] = um;
+        a.units[a.total / kAdamwGroup + group] = ur;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        raw.m.x[2 * i] = __float_as_uint(first_of(m[i]));
+        raw.m.x[2 * i + 1] = __float_as_uint(second_of(m[i]));
+        raw.v.x[2 * i] = __float_as_uint(first_of(v[i]));
+        raw.v.x[2 * i + 1] = __float_as_uint(second_of(v[i]));
+      }
+      st32(a.codes + s * 4, raw.m);
+      st32(a.codes + (a.total + s) * 4, raw.v);
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pw[i] = __float_as_uint(p[i]);
+    } else if (keeps) {                      // the nearest BF16 number (the larger of two as near) and what is left
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t b0 = __float_as_uint(p[2 * i]), b1 = __float_as_uint(p[2 * i + 1]);
+        pw[i] = __byte_perm(b0 + 0x8000u, b1 + 0x8000u, 0x7632);
+        w[i] = __byte_perm(b0, b1, 0x5410);                               // bits - (p << 16), as 16 bits
+      }
+      *reinterpret_cast<uint4*>(a.rest + s) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pw[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+    }
+    adamw_write<F32, WIDE>(static_cast<char*>(e.p) + u * kAdamwGroup * kSize, e.n - u * kAdamwGroup, lane, turn, pw);
   }
 }
 
@@ -165,7 +424,7 @@ __device__ __forceinline__ void adamw_decode_r(uint2 c, float unit, float (&r)[8
 template <int FMT, int CAP>
 __global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamwBatch<CAP> b) {
   after_previous();
-  __shared__ uint32_t turns[8][kAdamwGroup];
+  __shared__ uint4 turns[8][kAdamwGroup / 4];
   const AdamwArgs& a = b.a;
   int lo = 0, hi = a.n - 1;
   while (lo < hi) {
@@ -174,103 +433,29 @@ __global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamwBatc
     else hi = mid - 1;
   }
   const AdamwRec& e = b.e[lo];
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  uint32_t* turn = turns[warp];
-  const bool f32 = (e.flags & kAdamwF32) != 0u, keeps = !f32 && a.rest != nullptr;
-  const float scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
-  float alpha = a.alpha, rho = a.rho, decay = e.decay;
+  AdamwScalars k;
+  k.scale = a.grad_scale != nullptr ? *a.grad_scale : 1.0f;
+  k.alpha = a.alpha;
+  k.rho = a.rho;
+  k.decay = e.decay;
   if (a.scalars != nullptr) {
-    alpha = a.scalars[0];
-    rho = a.scalars[1];
-    decay = static_cast<float>(1.0 - static_cast<double>(a.scalars[2]) * static_cast<double>(decay));
+    k.alpha = a.scalars[0];
+    k.rho = a.scalars[1];
+    k.decay = static_cast<float>(1.0 - static_cast<double>(a.scalars[2]) * static_cast<double>(e.decay));
   }
-  const int64_t first = static_cast<int64_t>(blockIdx.x - e.block0) * kAdamwGroups;
-  for (uint32_t u = warp; u < kAdamwGroups; u += 8u) {
-    const int64_t at = (first + u) * kAdamwGroup, left = e.n - at;
-    if (left <= 0) break;
-    const bool wide = (e.flags & kAdamwWide) != 0u && left >= kAdamwGroup;
-    const int64_t group = e.group0 + first + u, s = group * kAdamwGroup + lane * 8u;
-    const size_t size = f32 ? 4u : 2u;
-    char* pp = static_cast<char*>(e.p) + at * size;
-    float p[8], g[8], m[8], v[8];
-    uint4 low = make_uint4(0u, 0u, 0u, 0u);
-    uint2 cm, cr;
-    float um = 0.0f, ur = 0.0f;
-    V8 wm, wv;
-    if (FMT == GWS_ADAMW_8BIT) {
-      cm = *reinterpret_cast<const uint2*>(a.codes + s);
-      cr = *reinterpret_cast<const uint2*>(a.codes + a.total + s);
-      um = a.units[group];
-      ur = a.units[a.total / kAdamwGroup + group];
-    } else {
-      wm = take32(a.codes + s * 4);
-      wv = take32(a.codes + (a.total + s) * 4);
-    }
-    if (keeps) low = *reinterpret_cast<const uint4*>(a.rest + s);
-    adamw_read(static_cast<const char*>(e.g) + at * size, f32, wide, left, lane, turn, g);
-    adamw_read(pp, f32, wide, left, lane, turn, p);
-    if (FMT == GWS_ADAMW_8BIT) {
-      adamw_decode_m(cm, um, m);
-      adamw_decode_r(cr, ur, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { m[i] = __uint_as_float(wm.x[i]); v[i] = __uint_as_float(wv.x[i]); }
-    }
-    if (keeps) {
-      const uint32_t w[4] = {low.x, low.y, low.z, low.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        p[i] = __uint_as_float(__float_as_uint(p[i]) + static_cast<uint32_t>(static_cast<int32_t>(static_cast<int16_t>(w[i >> 1] >> (16 * (i & 1))))));
-    }
-    float r[8];
-    uint32_t top_m = 0u, top_r = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float gs = a.grad_scale != nullptr ? __fmul_rn(g[i], scale) : g[i];
-      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1), __fmul_rn(gs, a.to_m));
-      v[i] = __fadd_rn(__fmul_rn(v[i], a.b2), __fmul_rn(__fmul_rn(gs, a.to_v), gs));
-      r[i] = __fsqrt_rn(v[i]);
-      p[i] = __fsub_rn(__fmul_rn(p[i], decay), __fdiv_rn(__fmul_rn(m[i], alpha), __fadd_rn(__fmul_rn(r[i], rho), a.eps)));
-      top_m = max(top_m, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-      top_r = max(top_r, __float_as_uint(r[i]) & 0x7FFFFFFFu);
-    }
-    if (FMT == GWS_ADAMW_8BIT) {
-      um = adamw_unit(__reduce_max_sync(0xFFFFFFFFu, top_m), 1.0f / 448.0f);
-      ur = adamw_unit(__reduce_max_sync(0xFFFFFFFFu, top_r), 1.0f / 1.9375f);
-      // a group that is not finite has a NaN for its unit and codes of zero: it restores as NaN
-      const float im = adamw_inverse(um), ir = adamw_inverse(ur);
-      *reinterpret_cast<uint2*>(a.codes + s) = im > 0.0f ? adamw_encode_m(m, im) : make_uint2(0u, 0u);
-      *reinterpret_cast<uint2*>(a.codes + a.total + s) = adamw_encode_r(r, ir);
-      if (lane == 0) {
-        a.units[group] = um;
-        a.units[a.total / kAdamwGroup + group] = ur;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { wm.x[i] = __float_as_uint(m[i]); wv.x[i] = __float_as_uint(v[i]); }
-      st32(a.codes + s * 4, wm);
-      st32(a.codes + (a.total + s) * 4, wv);
-    }
-    uint32_t out[8];
-    if (f32) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) out[i] = __float_as_uint(p[i]);
-    } else if (keeps) {
-      uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {          // the nearest BF16 number (the larger of two as near) and what is left; a NaN as itself
-        const uint32_t bits = p[i] != p[i] ? 0x7FC00000u : __float_as_uint(p[i]);
-        out[i] = (bits + 0x8000u) >> 16;
-        w[i >> 1] |= (bits & 0xFFFFu) << (16 * (i & 1));      // bits - (out << 16), as 16 bits
-      }
-      *reinterpret_cast<uint4*>(a.rest + s) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) out[i] = pack_bf16(p[i], 0.0f) & 0xFFFFu;
-    }
-    adamw_write(pp, f32, wide, left, lane, turn, out);
+  auto sane = [](float x, float least, float most) { return x >= least && x <= most; };
+  k.exact = sane(a.eps, 0x1p-40f, 0x1p30f) && sane(k.alpha, 0x1p-30f, 0x1p30f) && sane(k.rho, 0x1p-30f, 0x1p30f);
+  uint4* turn = turns[threadIdx.x >> 5];
+  const int64_t first = static_cast<int64_t>(blockIdx.x - e.block0) * a.per, groups = (e.n + kAdamwGroup - 1) / kAdamwGroup, end = min(groups, first + a.per);
+  const bool f32 = (e.flags & kAdamwF32) != 0u;
+  int64_t wide = (e.flags & kAdamwWide) != 0u ? min(end, e.n / kAdamwGroup) : first;          // groups up to here are whole and on boundaries
+  if (wide < first) wide = first;
+  if (f32) {
+    adamw_run<FMT, true, true>(a, e, k, first, wide, turn);
+    adamw_run<FMT, true, false>(a, e, k, wide, end, turn);
+  } else {
+    adamw_run<FMT, false, true>(a, e, k, first, wide, turn);
+    adamw_run<FMT, false, false>(a, e, k, wide, end, turn);
   }
 }
 
@@ -289,12 +474,18 @@ __global__ void __launch_bounds__(256) k_adamw_values(const uint8_t* codes, cons
   const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, s = t * 8;
   if (s >= total) return;
   const int64_t group = s / kAdamwGroup;
-  float x[8], r[8];
+  F2 x[4], r[4];
   adamw_decode_m(*reinterpret_cast<const uint2*>(codes + s), units[group], x);
   adamw_decode_r(*reinterpret_cast<const uint2*>(codes + total + s), units[total / kAdamwGroup + group], r);
   V8 a, b;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { a.x[i] = __float_as_uint(x[i]); b.x[i] = __float_as_uint(__fmul_rn(r[i], r[i])); }
+  for (int i = 0; i < 4; ++i) {
+    const F2 q = mul2(r[i], r[i]);
+    a.x[2 * i] = __float_as_uint(first_of(x[i]));
+    a.x[2 * i + 1] = __float_as_uint(second_of(x[i]));
+    b.x[2 * i] = __float_as_uint(first_of(q));
+    b.x[2 * i + 1] = __float_as_uint(second_of(q));
+  }
   st32(m + s, a);
   st32(v + s, b);
 }

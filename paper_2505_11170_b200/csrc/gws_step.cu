@@ -188,12 +188,16 @@ int adamw_step(int n_tensors, void* const* params, const void* const* grads, con
     a.alpha = static_cast<float>(args->lr / (1.0 - std::pow(args->beta1, static_cast<double>(args->step))));
     a.rho = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(args->beta2, static_cast<double>(args->step))));
   }
+  // Few groups: one to a warp, so that every SM has its share.  Many: eight to a warp, which finds its tensor once for all of them.
+  int64_t groups = 0;
+  for (const AdamwRec& r : recs) groups += (r.n + kAdamwGroup - 1) / kAdamwGroup;
+  a.per = groups >= 8 * 64 * 148 ? 64u : groups >= 2 * 16 * 148 ? 16u : 8u;
   for (size_t first = 0; first < recs.size();) {
     int n = 0;
     int64_t blocks = 0;
     for (; first + n < recs.size() && n < kAdamwMany; ++n) {
       AdamwRec& r = recs[first + n];
-      const int64_t more = (r.n + kAdamwGroups * kAdamwGroup - 1) / (kAdamwGroups * kAdamwGroup);
+      const int64_t more = (r.n + a.per * static_cast<int64_t>(kAdamwGroup) - 1) / (a.per * static_cast<int64_t>(kAdamwGroup));
       if (blocks + more > 0x7FFFFFFFLL) break;
       r.block0 = static_cast<uint32_t>(blocks);
       blocks += more;

@@ -223,6 +223,22 @@ def test_a_weight_moves_by_less_than_half_its_spacing_only_with_the_rest():
     assert bool((p == 1).all()) and bool((keeps.weight(0, q) < 1 - 9e-4).all()) and bool((q == 1).all())
 
 
+def test_parameters_set_to_zero_from_outside():
+    p = torch.randn(1000, device=DEV).to(torch.bfloat16)
+    state = gws.AdamWState([1000], rest=True)
+    g = torch.full_like(p, 1e-3)
+    for step in (1, 2):
+        gws.adamw_step([p], [g], state, lr=1e-3, weight_decay=0.0, step=step)
+    assert bool((state.rest < 0).any())
+    rest = state.rest[:1000].clone()
+    p[::3] = 0
+    weight = state.weight(0, p)
+    want = torch.where((p == 0) & (rest < 0), 0.0, weight)
+    gws.adamw_step([p], [g], state, lr=1e-3, weight_decay=0.0, step=3)
+    after = state.weight(0, p)
+    assert bool(p.isfinite().all()) and bool(((want - after) - 1e-3).abs().max() < 1e-4)          # each moved by lr
+
+
 def test_version_counters_see_the_step():
     p = torch.nn.Parameter(torch.ones(300, dtype=torch.bfloat16, device=DEV))
     loss = (p * p).sum()
