@@ -168,18 +168,14 @@ __device__ __forceinline__ F2 mul2(F2 a, F2 b) {
 }
 
 // Square root and quotient to the nearest, of pairs, by the residual of an approximation (Markstein's method): with g near sqrt(v) and h near 1 / (2 sqrt(v)), g + (v - g g) h
-// rounds as sqrt(v) does, and with y near 1 / d and q near n / d, q + (n - d q) y as n / d.  Both approximations are brought to FP32's own precision by one step (the
-// reciprocal by two) of Newton's iteration before.  v in [2^-100, 2^100], d in [2^-40, 2^81], n up to 2^70; a quotient of an n below 2^-100, whose residual may be below the
+// rounds as sqrt(v) does, and with y near 1 / d and q near n / d, q + (n - d q) y as n / d.  The reciprocal is brought to FP32's
+// own precision by two steps of Newton's iteration before; for the root the device's approximation is near enough.  v in [2^-100, 2^100], d in [2^-40, 2^81], n up to 2^70 (or n = 1 and d in [2^-110, 2^110]); a quotient of an n below 2^-100, whose residual may be below the
 // smallest number, can be one unit of its last place off.  All 2^24 significands of a root and 10^9 quotients agree with sqrt.rn and div.rn.
 __device__ __forceinline__ F2 root2(F2 v) {
   float y0, y1;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(first_of(v)));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(second_of(v)));
-  const F2 y = two(y0, y1);
-  F2 g = mul2(v, y), h = mul2(y, both(-0.5f));                 // h is held with its sign changed
-  const F2 e = fma2(g, h, both(0.5f));
-  g = fma2(g, e, g);
-  h = fma2(h, e, h);
+  const F2 y = two(y0, y1), g = mul2(v, y), h = mul2(y, both(-0.5f));         // h is held with its sign changed
   return fma2(two(__fmaf_rn(first_of(g), first_of(g), -first_of(v)), __fmaf_rn(second_of(g), second_of(g), -second_of(v))), h, g);
 }
 __device__ __forceinline__ F2 quotient2(F2 n, F2 d) {
@@ -196,11 +192,9 @@ __device__ __forceinline__ F2 quotient2(F2 n, F2 d) {
 
 // Unit of a group from the FP32 bits of its largest magnitude; NaN where that is not finite.
 __device__ __forceinline__ float adamw_unit(uint32_t top, float step) {
-  if (top >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-  const float m = __uint_as_float(top);
-  return m >= kAdamwLeast ? __fmul_rn(m, step) : 0.0f;
+  const float unit = __uint_as_float(top) >= kAdamwLeast ? __fmul_rn(__uint_as_float(top), step) : 0.0f;
+  return top < 0x7F800000u ? unit : __uint_as_float(0x7FC00000u);
 }
-__device__ __forceinline__ float adamw_inverse(float unit) { return unit > 0.0f ? __frcp_rn(unit) : 0.0f; }
 
 __device__ __forceinline__ uint2 adamw_encode_m(const F2 (&m)[4], float inv) {
   uint32_t w[2];
@@ -212,30 +206,29 @@ __device__ __forceinline__ uint2 adamw_encode_m(const F2 (&m)[4], float inv) {
   }
   return make_uint2(w[0], w[1]);
 }
-// `zeros`: there may be roots of zero among them.
-__device__ __forceinline__ uint2 adamw_encode_r(const F2 (&r)[4], float inv, bool zeros) {
+// `small`: there may be roots of zero among them, or some below the least code's.
+__device__ __forceinline__ uint2 adamw_encode_r(const F2 (&r)[4], float inv, bool small) {
   uint32_t c[8];
+  // 2^19 t - fl(2^19 t - t) is t to four bits of mantissa, nearest even: 2^19 t - t has the last place that t is to be rounded to (a finer one just above a power of two,
+  // where t becomes that power all the same), and 2^19 t is an even number of it where t is half way.  Above 2^-15 the code is then bits 19 to 26.  t is at most a little
+  // above 1.9375.
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const F2 t = mul2(r[i], both(inv));                  // at most a little above 1.9375
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t bits = __float_as_uint(e == 0 ? first_of(t) : second_of(t));
-      // to four bits of mantissa, nearest even; the code is what stands above bit 19
-      const int32_t code = static_cast<int32_t>(bits + ((bits >> 19) & 1u) + (0x3FFFFu - (112u << 23)));
-      c[2 * i + e] = static_cast<uint32_t>(max(code, 1 << 19)) << 5;
-    }
+    const F2 t = mul2(r[i], both(inv)), q = fma2(t, both(0x1p19f), mul2(t, both(-524287.0f)));
+    c[2 * i] = __float_as_uint(first_of(q));
+    c[2 * i + 1] = __float_as_uint(second_of(q));
   }
-  uint2 w = make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410),
-                       __byte_perm(__byte_perm(c[4], c[5], 0x0073), __byte_perm(c[6], c[7], 0x0073), 0x5410));
-  if (zeros) {
+  if (small) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float x = (i & 1) == 0 ? first_of(r[i / 2]) : second_of(r[i / 2]);
-      if (!(x > 0.0f)) (i < 4 ? w.x : w.y) &= ~(255u << (8 * (i & 3)));
+      c[i] = inv > 0.0f && x > 0.0f ? max(c[i], (112u << 23) + (1u << 19)) : 0u;
     }
   }
-  return inv > 0.0f ? w : make_uint2(0u, 0u);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __byte_perm(c[2 * i], c[2 * i + 1], 0x7632) >> 3;       // codes in bytes 0 and 2
+  return make_uint2(__byte_perm(w[0], w[1], 0x6420), __byte_perm(w[2], w[3], 0x6420));
 }
 __device__ __forceinline__ void adamw_decode_m(uint2 c, float unit, F2 (&m)[4]) {
 #pragma unroll
@@ -265,14 +258,23 @@ struct AdamwScalars {
   bool exact;                     // eps, alpha and rho are of sizes at which root2 and quotient2 are exact
 };
 
-// Groups first + warp, first + warp + 8, ... of a tensor, up to `end`.
+// Groups first + warp, first + warp + 8, ... of a tensor, `count` of them over the warps.  Addresses are the block's, plus 32 bits a lane.
 template <int FMT, bool F32, bool WIDE>
-__device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e, const AdamwScalars& k, int64_t first, int64_t end, uint4* turn) {
+__device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e, const AdamwScalars& k, int64_t first, uint32_t count, uint4* turn) {
   // With 8-bit moments a group is 3.6 KB and long arithmetic: the next one's loads are under way meanwhile.
   constexpr bool kAhead = FMT == GWS_ADAMW_8BIT && !F32;
   constexpr uint32_t kSize = F32 ? 4u : 2u;
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   const bool keeps = !F32 && a.rest != nullptr;
+  const int64_t group0 = e.group0 + first, s0 = group0 * kAdamwGroup, left0 = e.n - first * kAdamwGroup;
+  constexpr uint32_t kEach = FMT == GWS_ADAMW_8BIT ? 1u : 4u;                // bytes of a moment
+  char* const at_m = reinterpret_cast<char*>(a.codes) + s0 * kEach;
+  char* const at_v = at_m + a.total * kEach;
+  char* const at_rest = reinterpret_cast<char*>(a.rest) + s0 * 2;
+  char* const at_p = static_cast<char*>(e.p) + first * (kAdamwGroup * kSize);
+  const char* const at_g = static_cast<const char*>(e.g) + first * (kAdamwGroup * kSize);
+  float* const at_um = a.units + group0;
+  float* const at_ur = at_um + a.total / kAdamwGroup;
   struct Raw {
     AdamwWords<F32, WIDE> g, p;
     uint4 low;
@@ -280,34 +282,34 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
     float um, ur;
     V8 m, v;
   } next;
-  auto fetch = [&](int64_t u, Raw& r) {
-    const int64_t at = u * kAdamwGroup, group = e.group0 + u, s = group * kAdamwGroup + lane * 8u;
+  auto fetch = [&](uint32_t u, Raw& r) {
+    const uint32_t s = u * kAdamwGroup + lane * 8u;
     if (FMT == GWS_ADAMW_8BIT) {
-      r.cm = *reinterpret_cast<const uint2*>(a.codes + s);
-      r.cr = *reinterpret_cast<const uint2*>(a.codes + a.total + s);
-      r.um = a.units[group];
-      r.ur = a.units[a.total / kAdamwGroup + group];
+      r.cm = *reinterpret_cast<const uint2*>(at_m + s);
+      r.cr = *reinterpret_cast<const uint2*>(at_v + s);
+      r.um = at_um[u];
+      r.ur = at_ur[u];
     } else {
-      r.m = take32(a.codes + s * 4);
-      r.v = take32(a.codes + (a.total + s) * 4);
+      r.m = take32(at_m + s * 4u);
+      r.v = take32(at_v + s * 4u);
     }
     r.low = make_uint4(0u, 0u, 0u, 0u);
-    if (keeps) r.low = *reinterpret_cast<const uint4*>(a.rest + s);
-    adamw_fetch<F32, WIDE>(static_cast<const char*>(e.g) + at * kSize, e.n - at, lane, r.g);
-    adamw_fetch<F32, WIDE>(static_cast<const char*>(e.p) + at * kSize, e.n - at, lane, r.p);
+    if (keeps) r.low = *reinterpret_cast<const uint4*>(at_rest + s * 2u);
+    adamw_fetch<F32, WIDE>(at_g + u * (kAdamwGroup * kSize), left0 - u * kAdamwGroup, lane, r.g);
+    adamw_fetch<F32, WIDE>(at_p + u * (kAdamwGroup * kSize), left0 - u * kAdamwGroup, lane, r.p);
   };
-  int64_t u = first + warp;
-  if (kAhead && u < end) fetch(u, next);
+  uint32_t u = warp;
+  if (kAhead && u < count) fetch(u, next);
 #pragma unroll 1
-  for (; u < end; u += 8) {
+  for (; u < count; u += 8) {
     Raw raw;
     if (kAhead) {
       raw = next;
-      if (u + 8 < end) fetch(u + 8, next);
+      if (u + 8u < count) fetch(u + 8u, next);
     } else {
       fetch(u, raw);
     }
-    const int64_t group = e.group0 + u, s = group * kAdamwGroup + lane * 8u;
+    const uint32_t s = u * kAdamwGroup + lane * 8u;
     uint32_t gw[F32 ? 8 : 4], pw[F32 ? 8 : 4];
     adamw_turn<F32, WIDE>(raw.g, lane, turn, gw);
     adamw_turn<F32, WIDE>(raw.p, lane, turn, pw);
@@ -382,12 +384,14 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
       for (int i = 0; i < 4; ++i) top_r = max(top_r, max(__float_as_uint(first_of(r[i])) & 0x7FFFFFFFu, __float_as_uint(second_of(r[i])) & 0x7FFFFFFFu));
       const float um = adamw_unit(__reduce_max_sync(0xFFFFFFFFu, top_m), 1.0f / 448.0f), ur = adamw_unit(__reduce_max_sync(0xFFFFFFFFu, top_r), 1.0f / 1.9375f);
       // a group that is not finite has a NaN for its unit and codes of zero: it restores as NaN
-      const float im = adamw_inverse(um), ir = adamw_inverse(ur);
-      *reinterpret_cast<uint2*>(a.codes + s) = im > 0.0f ? adamw_encode_m(m, im) : make_uint2(0u, 0u);
-      *reinterpret_cast<uint2*>(a.codes + a.total + s) = adamw_encode_r(r, ir, !plain);
+      const F2 inverse = quotient2(both(1.0f), two(um, ur));
+      const float im = um > 0.0f ? first_of(inverse) : 0.0f, ir = ur > 0.0f ? second_of(inverse) : 0.0f;
+      const bool small = !plain || !(__fmul_rn(least, __fmul_rn(ir, ir)) >= 0x1.3p-30f);         // (1.0625 2^-15)^2 and some more
+      *reinterpret_cast<uint2*>(at_m + s) = plain || im > 0.0f ? adamw_encode_m(m, im) : make_uint2(0u, 0u);
+      *reinterpret_cast<uint2*>(at_v + s) = adamw_encode_r(r, ir, small);
       if (lane == 0) {
-        a.units[group] = um;
-        a.units[a.total / kAdamwGroup + group] = ur;
+        at_um[u] = um;
+        at_ur[u] = ur;
       }
     } else {
 #pragma unroll
@@ -397,8 +401,8 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
         raw.v.x[2 * i] = __float_as_uint(first_of(v[i]));
         raw.v.x[2 * i + 1] = __float_as_uint(second_of(v[i]));
       }
-      st32(a.codes + s * 4, raw.m);
-      st32(a.codes + (a.total + s) * 4, raw.v);
+      st32(at_m + s * 4u, raw.m);
+      st32(at_v + s * 4u, raw.v);
     }
     if constexpr (F32) {
 #pragma unroll
@@ -411,18 +415,18 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
         pw[i] = __byte_perm(b0 + 0x8000u, b1 + 0x8000u, 0x7632);
         w[i] = __byte_perm(b0, b1, 0x5410);                               // bits - (p << 16), as 16 bits
       }
-      *reinterpret_cast<uint4*>(a.rest + s) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(at_rest + s * 2u) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) pw[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
     }
-    adamw_write<F32, WIDE>(static_cast<char*>(e.p) + u * kAdamwGroup * kSize, e.n - u * kAdamwGroup, lane, turn, pw);
+    adamw_write<F32, WIDE>(at_p + u * (kAdamwGroup * kSize), left0 - u * kAdamwGroup, lane, turn, pw);
   }
 }
 
 // Memory-bound.  A warp takes a group, a lane eight elements of it; a block finds its tensor by bisection in the kernel parameters.
 template <int FMT, int CAP>
-__global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamwBatch<CAP> b) {
+__global__ void __launch_bounds__(256, FMT == GWS_ADAMW_8BIT ? 3 : 4) k_adamw(const __grid_constant__ AdamwBatch<CAP> b) {
   after_previous();
   __shared__ uint4 turns[8][kAdamwGroup / 4];
   const AdamwArgs& a = b.a;
@@ -450,12 +454,13 @@ __global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamwBatc
   const bool f32 = (e.flags & kAdamwF32) != 0u;
   int64_t wide = (e.flags & kAdamwWide) != 0u ? min(end, e.n / kAdamwGroup) : first;          // groups up to here are whole and on boundaries
   if (wide < first) wide = first;
+  const uint32_t n_wide = static_cast<uint32_t>(wide - first), n_rest = static_cast<uint32_t>(end - wide);
   if (f32) {
-    adamw_run<FMT, true, true>(a, e, k, first, wide, turn);
-    adamw_run<FMT, true, false>(a, e, k, wide, end, turn);
+    adamw_run<FMT, true, true>(a, e, k, first, n_wide, turn);
+    adamw_run<FMT, true, false>(a, e, k, wide, n_rest, turn);
   } else {
-    adamw_run<FMT, false, true>(a, e, k, first, wide, turn);
-    adamw_run<FMT, false, false>(a, e, k, wide, end, turn);
+    adamw_run<FMT, false, true>(a, e, k, first, n_wide, turn);
+    adamw_run<FMT, false, false>(a, e, k, wide, n_rest, turn);
   }
 }
 
