@@ -300,14 +300,14 @@ __device__ __forceinline__ void move_unit(const Prep& m, int64_t t) {
   for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? p[i] : 0u;
   *reinterpret_cast<uint4*>(to + t * 8) = make_uint4(v[0] | (v[1] << 16), v[2] | (v[3] << 16), v[4] | (v[5] << 16), v[6] | (v[7] << 16));
 }
-// The first blocks of a launch of 256 threads; true if this block was one of them.
-__device__ __forceinline__ bool prepare(const Prep& m) {
+// The first blocks of a launch, 256 threads' work each (a smaller block does it in turns); true if this block was one of them.
+__device__ __forceinline__ bool prepare(const Prep& m, uint32_t thread) {
   if (blockIdx.x >= m.move_blocks + m.restore_blocks) return false;
   if (blockIdx.x < m.move_blocks) {
-    move_unit(m, static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x);
+    move_unit(m, static_cast<int64_t>(blockIdx.x) * 256 + thread);
     return true;
   }
-  const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks) * 256 + threadIdx.x;
+  const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks) * 256 + thread;
   if (t >= m.groups) return true;
   int64_t at = t * kGroup;
   if (m.ld_restored != m.kept.ld) at += quotient(t, static_cast<uint32_t>(m.kept.ld / kGroup)) * (m.ld_restored - m.kept.ld);
@@ -317,7 +317,7 @@ __device__ __forceinline__ bool prepare(const Prep& m) {
 }
 __global__ void __launch_bounds__(256) k_prepare(const __grid_constant__ Prep m) {
   after_previous();
-  (void)prepare(m);
+  (void)prepare(m, threadIdx.x);
 }
 
 }  // namespace

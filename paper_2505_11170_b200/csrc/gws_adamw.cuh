@@ -24,6 +24,7 @@
 #include <stdint.h>
 
 #include "gws_act8.cuh"
+#include "gws_pair.cuh"
 
 namespace {
 
@@ -132,39 +133,6 @@ __device__ __forceinline__ void adamw_write(void* p, int64_t left, uint32_t lane
     }
     __syncwarp();
   }
-}
-
-// Two FP32 numbers in a register pair: one instruction rounds both as the scalar ones do.
-struct F2 {
-  uint64_t v;
-};
-__device__ __forceinline__ F2 two(float a, float b) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ F2 both(float a) { return two(a, a); }
-__device__ __forceinline__ float first_of(F2 a) {
-  float x;
-  asm("mov.b64 {%0, _}, %1;" : "=f"(x) : "l"(a.v));
-  return x;
-}
-__device__ __forceinline__ float second_of(F2 a) {
-  float y;
-  asm("mov.b64 {_, %0}, %1;" : "=f"(y) : "l"(a.v));
-  return y;
-}
-// Two additions: add.rn.f32x2 would be fused with a mul.rn.f32x2 before it, under -fmad=false too.
-__device__ __forceinline__ F2 add2(F2 a, F2 b) { return two(__fadd_rn(first_of(a), first_of(b)), __fadd_rn(second_of(a), second_of(b))); }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
 }
 
 // Square root and quotient to the nearest, of pairs, by the residual of an approximation (Markstein's method): with g near sqrt(v) and h near 1 / (2 sqrt(v)), g + (v - g g) h

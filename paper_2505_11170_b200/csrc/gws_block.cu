@@ -517,15 +517,15 @@ const LinearBack& linear_back(const gws_linear_desc* d, int sms) {
   return remembered<LinearBack>({d->m, d->n, d->k, d->ld_x, d->ld_w, d->ld_y, d->activation != GWS_ACT_NONE, d->x_format, sms}, [&] { return weigh_linear_back(d, sms); });
 }
 
-// A block's share of a strip is at least 32 rows, a row to eight of its threads.
+// A block's share of a strip is at least 16 rows, a row to eight of its threads.
 int launch_linear_pre(LinearPre p, Ready& ready, int save, bool wide, cudaStream_t s) {
   const int64_t moved = ready.blocks(), strips = (p.cols + 63) / 64;
   if (moved < 0) return static_cast<int>(moved);
-  p.shares = p.rows > 128 ? 8u : p.rows > 64 ? 4u : p.rows > 32 ? 2u : 1u;
+  p.shares = p.rows > 64 ? 8u : p.rows > 32 ? 4u : p.rows > 16 ? 2u : 1u;
   p.first = static_cast<uint32_t>(round_up(moved, p.shares));
   const unsigned grid = p.first + static_cast<unsigned>(strips) * p.shares;
   const char* what = "linear backward, element-wise part";
-  auto go = [&](void (*kernel)(LinearPre, Prep)) { return launch(kernel, grid, 256, 0, p.shares, s, what, p, ready.prep); };
+  auto go = [&](void (*kernel)(LinearPre, Prep)) { return launch(kernel, grid, kPreThreads, 0, p.shares, s, what, p, ready.prep); };
   if (save == GWS_ACT8_INT8) return go(wide ? k_linear_pre<GWS_ACT8_INT8, true> : k_linear_pre<GWS_ACT8_INT8, false>);
   if (save == GWS_ACT8_E4M3) return go(wide ? k_linear_pre<GWS_ACT8_E4M3, true> : k_linear_pre<GWS_ACT8_E4M3, false>);
   if (save == GWS_SAVE_BF16) return go(wide ? k_linear_pre<GWS_SAVE_BF16, true> : k_linear_pre<GWS_SAVE_BF16, false>);

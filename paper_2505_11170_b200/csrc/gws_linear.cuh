@@ -9,6 +9,7 @@
 #pragma once
 #include <stdint.h>
 
+#include "gws_pair.cuh"
 #include "gws_tc.cuh"
 
 namespace {
@@ -28,23 +29,71 @@ struct LinearPre {
   int32_t activation, db_f32;
 };
 
+// act(z) and its slope of eight elements, as act_and_slope in gws_tc.cuh, two at a time.
 template <int ACT>
-__device__ __forceinline__ void slopes(const float (&z)[8], float (&a)[8], float (&slope)[8]) {
+__device__ __forceinline__ void slopes(const F2 (&z)[4], F2 (&a)[4], F2 (&slope)[4]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) act_and_slope<ACT>(z[i], a[i], slope[i]);
+  for (int i = 0; i < 4; ++i) {
+    if (ACT == GWS_ACT_NONE || ACT == GWS_GATED_RELU) {
+      const float x = first_of(z[i]), y = second_of(z[i]);
+      float ax, ay, sx, sy;
+      act_and_slope<ACT>(x, ax, sx);
+      act_and_slope<ACT>(y, ay, sy);
+      a[i] = two(ax, ay);
+      slope[i] = two(sx, sy);
+      continue;
+    }
+    constexpr float kLog2e = 1.44269504f;
+    F2 zz = z[i], x = mul2(z[i], both(-kLog2e));
+    if (ACT == GWS_GATED_GELU_TANH) {
+      zz = two(fminf(first_of(z[i]) * first_of(z[i]), 0x1p100f), fminf(second_of(z[i]) * second_of(z[i]), 0x1p100f));
+      x = mul2(z[i], fma2(zz, both(-kLog2e * kGeluLin * 0.044715f), both(-kLog2e * kGeluLin)));
+    }
+    float e0, e1, s0, s1;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(first_of(x)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(second_of(x)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s0) : "f"(1.0f + e0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s1) : "f"(1.0f + e1));
+    const F2 s = two(s0, s1);
+    a[i] = mul2(z[i], s);
+    F2 t = mul2(a[i], fma2(s, both(-1.0f), both(1.0f)));
+    if (ACT == GWS_GATED_GELU_TANH) t = mul2(t, fma2(zz, both(3.0f * 0.044715f * kGeluLin), both(kGeluLin)));
+    slope[i] = fma2(t, both(1.0f), s);
+  }
 }
+// z of a thread's eight codes.
+template <int FMT>
+__device__ __forceinline__ void decode8(uint2 c, float unit, F2 (&z)[4]) {
+  float v[8];
+  if (FMT == GWS_ACT8_INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = (i < 2 ? c.x : c.y) ^ 0x80808080u;        // as decode4_int8
+      const F2 q = two(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7540u + 2 * (i & 1))), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7541u + 2 * (i & 1))));
+      z[i] = mul2(fma2(q, both(1.0f), both(-8388736.0f)), both(unit));
+    }
+    return;
+  }
+  decode4<FMT>(c.x, unit, v);
+  decode4<FMT>(c.y, unit, v + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = two(v[2 * i], v[2 * i + 1]);
+}
+
+constexpr uint32_t kPreThreads = 128u, kPreSlots = kPreThreads / 8u;
 
 // WIDE: rows of dy, of a BF16 z and of act(z) on 16-byte boundaries.  Otherwise a warp reads its four rows an element to a lane, side by side, and turns them in
 // shared memory.
 template <int SAVE, bool WIDE>
-__global__ void __launch_bounds__(256) k_linear_pre(const __grid_constant__ LinearPre p, const __grid_constant__ Prep m) {
+__global__ void __launch_bounds__(kPreThreads) k_linear_pre(const __grid_constant__ LinearPre p, const __grid_constant__ Prep m) {
   after_previous();
   if (blockIdx.x < p.first) {
-    (void)prepare(m);
+    (void)prepare(m, threadIdx.x);
+    (void)prepare(m, threadIdx.x + kPreThreads);
     return;
   }
-  __shared__ uint4 turn[WIDE ? 1 : 8][32];
-  __shared__ __align__(16) float sums[32][68];
+  __shared__ uint4 turn[WIDE ? 1 : kPreThreads / 32u][32];
+  __shared__ __align__(16) float sums[kPreSlots][68];
   __shared__ float joined[64];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, oct = threadIdx.x & 7u, slot = threadIdx.x >> 3;
   const uint32_t b = blockIdx.x - p.first, strip = b / p.shares, share = b - strip * p.shares;
@@ -67,17 +116,18 @@ __global__ void __launch_bounds__(256) k_linear_pre(const __grid_constant__ Line
     __syncwarp();
     return w;
   };
-  float db[8];
+  F2 db[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) db[i] = 0.0f;
-  constexpr int kRows = 2;                                                     // rows of a thread in flight
-  for (int64_t at = begin; at < end; at += 32 * kRows) {
+  for (int i = 0; i < 4; ++i) db[i] = both(0.0f);
+  constexpr int kRows = 4;                                                     // rows of a thread in flight
+#pragma unroll 1
+  for (int64_t at = begin; at < end; at += kPreSlots * kRows) {
     uint4 g[kRows], z16[kRows];
     uint2 z8[kRows];
     uint32_t byte[kRows];
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      const int64_t row = at + 32 * k + slot;
+      const int64_t row = at + kPreSlots * k + slot;
       if (p.dy != nullptr) g[k] = bring(p.dy, p.ld_dy, row);
       if (SAVE == GWS_SAVE_BF16) z16[k] = bring(p.save16, p.cols, row);
       if (SAVE == GWS_ACT8_INT8 || SAVE == GWS_ACT8_E4M3) {
@@ -88,20 +138,18 @@ __global__ void __launch_bounds__(256) k_linear_pre(const __grid_constant__ Line
     }
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      const int64_t row = at + 32 * k + slot;
-      float z[8], a[8], slope[8];
+      const int64_t row = at + kPreSlots * k + slot;
+      F2 z[4], a[4], slope[4];
       if (SAVE == GWS_SAVE_BF16) {
         const uint32_t q[4] = {z16[k].x, z16[k].y, z16[k].z, z16[k].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { z[2 * i] = bf16_lo(q[i]); z[2 * i + 1] = bf16_hi(q[i]); }
+        for (int i = 0; i < 4; ++i) z[i] = two(bf16_lo(q[i]), bf16_hi(q[i]));
       } else if (SAVE != GWS_SAVE_NONE) {
         constexpr int kFmt = SAVE == GWS_ACT8_INT8 ? GWS_ACT8_INT8 : GWS_ACT8_E4M3;
-        const float unit = unit_of<kFmt>(byte[k]);
-        decode4<kFmt>(z8[k].x, unit, z);
-        decode4<kFmt>(z8[k].y, unit, z + 4);
+        decode8<kFmt>(z8[k], unit_of<kFmt>(byte[k]), z);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = 0.0f;
+        for (int i = 0; i < 4; ++i) z[i] = both(0.0f);
       }
       if (p.activation == GWS_GATED_SILU) slopes<GWS_GATED_SILU>(z, a, slope);
       else if (p.activation == GWS_GATED_GELU_TANH) slopes<GWS_GATED_GELU_TANH>(z, a, slope);
@@ -110,20 +158,20 @@ __global__ void __launch_bounds__(256) k_linear_pre(const __grid_constant__ Line
       const uint32_t q[4] = {g[k].x, g[k].y, g[k].z, g[k].w};
       uint32_t w[4];
       if (p.dy != nullptr) {
+        const bool whole = row < end && col + 8 <= p.cols;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+          F2 d = mul2(two(bf16_lo(q[i]), bf16_hi(q[i])), slope[i]);
           // an element outside has dy = 0; its z may be a NaN (the group's), which must not reach the sum
-          const float d0 = col + 2 * i < p.cols && row < end ? bf16_lo(q[i]) * slope[2 * i] : 0.0f;
-          const float d1 = col + 2 * i + 1 < p.cols && row < end ? bf16_hi(q[i]) * slope[2 * i + 1] : 0.0f;
-          db[2 * i] += d0;
-          db[2 * i + 1] += d1;
-          w[i] = pack_bf16(d0, d1);
+          if (!whole) d = two(row < end && col + 2 * i < p.cols ? first_of(d) : 0.0f, row < end && col + 2 * i + 1 < p.cols ? second_of(d) : 0.0f);
+          db[i] = fma2(d, both(1.0f), db[i]);
+          w[i] = pack_bf16(first_of(d), second_of(d));
         }
         if (p.dz != nullptr && row < end) *reinterpret_cast<uint4*>(p.dz + row * p.ld_dz + col) = make_uint4(w[0], w[1], w[2], w[3]);
       }
       if (p.again != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(a[2 * i], a[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(first_of(a[i]), second_of(a[i]));
         if (WIDE) {
           if (row < end && col < p.cols) *reinterpret_cast<uint4*>(p.again + row * p.cols + col) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
@@ -143,12 +191,12 @@ __global__ void __launch_bounds__(256) k_linear_pre(const __grid_constant__ Line
   }
   if (p.db == nullptr) return;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(&sums[slot][oct * 8u + 4u * i]) = make_float4(db[4 * i], db[4 * i + 1], db[4 * i + 2], db[4 * i + 3]);
+  for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(&sums[slot][oct * 8u + 4u * i]) = make_float4(first_of(db[2 * i]), second_of(db[2 * i]), first_of(db[2 * i + 1]), second_of(db[2 * i + 1]));
   __syncthreads();
   if (threadIdx.x < 64u) {
     float t = 0.0f;
 #pragma unroll 8
-    for (uint32_t r = 0; r < 32u; ++r) t += sums[r][threadIdx.x];
+    for (uint32_t r = 0; r < kPreSlots; ++r) t += sums[r][threadIdx.x];
     joined[threadIdx.x] = t;
   }
   if (p.shares > 1u) pair_sync();

@@ -41,25 +41,32 @@ template <int L, bool WIDE>
 __device__ __forceinline__ int64_t norm_col(uint32_t lane, int c, int i) {
   return WIDE ? static_cast<int64_t>(c * L + lane) * 8 + i : static_cast<int64_t>(8 * c + i) * L + lane;
 }
+// A thread's part of a row as it comes from memory: pairs of neighbouring elements, or one element to a word.
+template <int C, bool WIDE>
+struct NormWords {
+  uint32_t x[WIDE ? 4 * C : 8 * C];
+};
 template <int L, int C, bool WIDE>
-__device__ __forceinline__ void norm_read(const uint16_t* row, int64_t cols, uint32_t lane, float (&v)[8 * C]) {
-  if (WIDE) {
-    uint4 w[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) w[c] = norm_col<L, WIDE>(lane, c, 0) < cols ? __ldg(reinterpret_cast<const uint4*>(row + norm_col<L, WIDE>(lane, c, 0))) : make_uint4(0u, 0u, 0u, 0u);
+__device__ __forceinline__ void norm_load(const uint16_t* row, int64_t cols, uint32_t lane, NormWords<C, WIDE>& w) {
+  if constexpr (WIDE) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const uint32_t q[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[8 * c + 2 * i] = bf16_lo(q[i]); v[8 * c + 2 * i + 1] = bf16_hi(q[i]); }
+      const int64_t col = norm_col<L, WIDE>(lane, c, 0);
+      const uint4 q = col < cols ? __ldg(reinterpret_cast<const uint4*>(row + col)) : make_uint4(0u, 0u, 0u, 0u);
+      w.x[4 * c] = q.x; w.x[4 * c + 1] = q.y; w.x[4 * c + 2] = q.z; w.x[4 * c + 3] = q.w;
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8 * C; ++e) {
       const int64_t col = norm_col<L, WIDE>(lane, 0, e);
-      v[e] = col < cols ? __uint_as_float(static_cast<uint32_t>(__ldg(row + col)) << 16) : 0.0f;
+      w.x[e] = col < cols ? static_cast<uint32_t>(__ldg(row + col)) : 0u;
     }
   }
+}
+template <int C, bool WIDE>
+__device__ __forceinline__ float norm_value(const NormWords<C, WIDE>& w, int e) {
+  if constexpr (WIDE) return (e & 1) == 0 ? bf16_lo(w.x[e / 2]) : bf16_hi(w.x[e / 2]);
+  else return __uint_as_float(w.x[e] << 16);
 }
 template <int L, int C, bool WIDE>
 __device__ __forceinline__ void norm_write(uint16_t* row, int64_t cols, uint32_t lane, const float (&v)[8 * C]) {
@@ -136,13 +143,17 @@ __global__ void __launch_bounds__(kNormThreads<L>) k_norm_fwd(const __grid_const
   const int64_t row = static_cast<int64_t>(blockIdx.x) * (kNormThreads<L> / L) + threadIdx.x / L;
   if (row >= p.rows) return;               // teams of more than a warp have a block to themselves
   float s[8 * C];
-  norm_read<L, C, WIDE>(p.x + row * p.ld_x, p.cols, lane, s);
+  NormWords<C, WIDE> x;
+  norm_load<L, C, WIDE>(p.x + row * p.ld_x, p.cols, lane, x);
   if (p.r != nullptr) {
-    float r[8 * C];
-    norm_read<L, C, WIDE>(p.r + row * p.ld_r, p.cols, lane, r);
+    NormWords<C, WIDE> r;
+    norm_load<L, C, WIDE>(p.r + row * p.ld_r, p.cols, lane, r);
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) s[e] = bf16_lo(pack_bf16(s[e] + r[e], 0.0f));
+    for (int e = 0; e < 8 * C; ++e) s[e] = bf16_lo(pack_bf16(norm_value(x, e) + norm_value(r, e), 0.0f));
     norm_write<L, C, WIDE>(p.sum + row * p.cols, p.cols, lane, s);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8 * C; ++e) s[e] = norm_value(x, e);
   }
   float t = 0.0f;
 #pragma unroll
@@ -208,46 +219,69 @@ __global__ void __launch_bounds__(kNormThreads<L>) k_norm_bwd(const __grid_const
   constexpr uint32_t kTeams = kNormThreads<L> / L;
   __shared__ float2 room[2][kNormThreads<L> / 32u];
   __shared__ float2 joined[kTeams > 1u ? L * C * 8u : 1u];
+  __shared__ float weights[C][8][L];                     // the same for every team: out of the registers, so that the next row's words fit in
   uint32_t turn = 0;
   const uint32_t lane = threadIdx.x % L, team = threadIdx.x / L;
   const float inv = 1.0f / static_cast<float>(p.cols);
-  float w[8 * C], gw[8 * C], gb[8 * C];
+  float gw[8 * C], gb[8 * C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    float q[8];
-    norm_weights<L, WIDE>(p.weight, p.f32 != 0, 1.0f, p.cols, lane, c, q);
+  for (int e = 0; e < 8 * C; ++e) gw[e] = gb[e] = 0.0f;
+  if (team == 0u) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { w[8 * c + i] = q[i]; gw[8 * c + i] = gb[8 * c + i] = 0.0f; }
+    for (int c = 0; c < C; ++c) {
+      float q[8];
+      norm_weights<L, WIDE>(p.weight, p.f32 != 0, 1.0f, p.cols, lane, c, q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) weights[c][i][lane] = q[i];
+    }
   }
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTeams; row0 < p.rows; row0 += static_cast<int64_t>(gridDim.x) * kTeams) {
+  __syncthreads();
+  struct Row {
+    NormWords<C, WIDE> s, dy, d;
+    float mean, rstd;
+  } next;
+  auto fetch = [&](int64_t row, Row& r) {
+    const int64_t cols = row < p.rows ? p.cols : 0;
+    norm_load<L, C, WIDE>(p.x + row * p.ld_x, cols, lane, r.s);
+    norm_load<L, C, WIDE>(p.dy + row * p.ld_dy, cols, lane, r.dy);
+    if (p.d != nullptr) norm_load<L, C, WIDE>(p.d + row * p.ld_d, cols, lane, r.d);
+    r.mean = row < p.rows ? p.stats[row] : 0.0f;
+    r.rstd = row < p.rows ? p.stats[p.rows + row] : 0.0f;
+  };
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
+  int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTeams;
+  if (WIDE) fetch(row0 + team, next);
+#pragma unroll 1
+  for (; row0 < p.rows; row0 += stride) {
+    Row now;
+    if (WIDE) {
+      now = next;
+      if (row0 + stride < p.rows) fetch(row0 + stride + team, next);        // under the sums of this one
+    } else {
+      fetch(row0 + team, now);                                              // an element to a register: there is no room for two rows
+    }
     const int64_t row = row0 + team;
-    const bool real = row < p.rows;
-    const int64_t cols = real ? p.cols : 0;
-    float s[8 * C], dy[8 * C];
-    norm_read<L, C, WIDE>(p.x + row * p.ld_x, cols, lane, s);
-    norm_read<L, C, WIDE>(p.dy + row * p.ld_dy, cols, lane, dy);
-    const float mean = real ? p.stats[row] : 0.0f, rstd = real ? p.stats[p.rows + row] : 0.0f;
     float ta = 0.0f, tb = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8 * C; ++e) {
-      s[e] = (s[e] - mean) * rstd;                       // xh; columns past the width have dy = 0
-      const float a = dy[e] * w[e];
+      const float xh = (norm_value(now.s, e) - now.mean) * now.rstd, dy = norm_value(now.dy, e);          // columns past the width have dy = 0
+      const float a = dy * weights[e / 8][e % 8][lane];
       ta += a;
-      tb = __fmaf_rn(a, s[e], tb);
-      gw[e] = __fmaf_rn(dy[e], s[e], gw[e]);
-      gb[e] += dy[e];
+      tb = __fmaf_rn(a, xh, tb);
+      gw[e] = __fmaf_rn(dy, xh, gw[e]);
+      gb[e] += dy;
     }
     const float2 t = team_sum<L>(ta, tb, room[0], turn);
-    if (p.dx != nullptr) {
+    if (p.dx != nullptr && row < p.rows) {
       const float ma = t.x * inv, mb = t.y * inv;
+      float out[8 * C];
 #pragma unroll
-      for (int e = 0; e < 8 * C; ++e) s[e] = rstd * (dy[e] * w[e] - ma - s[e] * mb);
-      if (p.d != nullptr) {
-        norm_read<L, C, WIDE>(p.d + row * p.ld_d, cols, lane, dy);
-#pragma unroll
-        for (int e = 0; e < 8 * C; ++e) s[e] += dy[e];
+      for (int e = 0; e < 8 * C; ++e) {
+        const float xh = (norm_value(now.s, e) - now.mean) * now.rstd, a = norm_value(now.dy, e) * weights[e / 8][e % 8][lane];
+        out[e] = now.rstd * __fmaf_rn(-xh, mb, a - ma);
+        if (p.d != nullptr) out[e] += norm_value(now.d, e);
       }
-      norm_write<L, C, WIDE>(p.dx + row * p.cols, cols, lane, s);
+      norm_write<L, C, WIDE>(p.dx + row * p.cols, p.cols, lane, out);
     }
   }
   if (p.part == nullptr) return;

@@ -29,16 +29,16 @@ int64_t weight_bytes(const gws_norm_desc& d) { return d.weight_type == GWS_TYPE_
 // Whether rows of a BF16 matrix (absent: null) start on 16-byte boundaries.
 bool wide_rows(const void* p, int64_t rows, int64_t ld) { return p == nullptr || (on(p, 16) && (rows <= 1 || ld % 8 == 0)); }
 
-// Rows of up to 2048 elements to a warp each, or, where that leaves SMs without a row or the row is longer, to a block.
+// Rows of up to 2048 elements (1024, read one by one) to a warp each, or, where that leaves SMs without a row or the row is longer, to a block.
 template <bool WIDE>
 int launch_norm_fwd(const NormArgs& a, cudaStream_t s) {
   const char* what = "layer norm kernel";
   const unsigned rows = static_cast<unsigned>(a.rows), warps = blocks_for(a.rows, 8);
   if (a.cols <= 256) return launch(k_norm_fwd<32, 1, WIDE>, warps, 256, 0, 1, s, what, a);
-  if (a.cols <= 2048 && a.rows >= 2 * sm_count()) {
+  if (a.cols <= (WIDE ? 2048 : 1024) && a.rows >= 2 * sm_count()) {
     if (a.cols <= 512) return launch(k_norm_fwd<32, 2, WIDE>, warps, 256, 0, 1, s, what, a);
     if (a.cols <= 1024) return launch(k_norm_fwd<32, 4, WIDE>, warps, 256, 0, 1, s, what, a);
-    return launch(k_norm_fwd<32, 8, WIDE>, warps, 256, 0, 1, s, what, a);
+    if constexpr (WIDE) return launch(k_norm_fwd<32, 8, true>, warps, 256, 0, 1, s, what, a);
   }
   if (a.cols <= 2048) return launch(k_norm_fwd<256, 1, WIDE>, rows, 256, 0, 1, s, what, a);
   if (a.cols <= 4096) return launch(k_norm_fwd<256, 2, WIDE>, rows, 256, 0, 1, s, what, a);

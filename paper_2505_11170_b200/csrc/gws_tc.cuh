@@ -1061,7 +1061,7 @@ struct PreArgs {
 template <int SAVE, int ACT>
 __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreArgs p, const __grid_constant__ Prep m) {
   after_previous();
-  if (prepare(m)) return;
+  if (prepare(m, threadIdx.x)) return;
   const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks - m.restore_blocks) * 256 + threadIdx.x;
   if (t >= p.groups) return;
   const int64_t at = t * kGroup;     // saved values and h: rows side by side
@@ -1127,7 +1127,7 @@ __global__ void __launch_bounds__(256) k_gated_pre(const __grid_constant__ PreAr
 template <int SAVE, int ACT>
 __global__ void __launch_bounds__(256) k_gated_pre_any(const __grid_constant__ PreArgs p, const __grid_constant__ Prep m) {
   after_previous();
-  if (prepare(m)) return;
+  if (prepare(m, threadIdx.x)) return;
   __shared__ uint4 turn[8][32];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, runs_per_row = (p.per_row + 7u) / 8u;
   const int64_t t = static_cast<int64_t>(blockIdx.x - m.move_blocks - m.restore_blocks) * 8 + warp, row = quotient(t, runs_per_row);
