@@ -14,8 +14,8 @@ LIB_PATH = os.path.join(_PKG, "libgws.so")
 _UNITS = {
     "gws_api.cu": ["gws_kernels.cuh", "gws_math.cuh", "gws_gemm.cuh", "gws_probe.cuh", "gws_compare.cuh", "gws_gemm_cluster.cuh", "gws_gemm_wide.cuh",
                    "gws_train.cuh", "gws_internal.h"],
-    "gws_block.cu": ["gws_linear.cuh", "gws_pair.cuh", "gws_tc.cuh", "gws_act8.cuh", "gws_host.h", "gws_internal.h"],
-    "gws_step.cu": ["gws_norm.cuh", "gws_adamw.cuh", "gws_pair.cuh", "gws_act8.cuh", "gws_host.h", "gws_internal.h"],
+    "gws_block.cu": ["gws_linear.cuh", "gws_pair.cuh", "gws_sums.cuh", "gws_tc.cuh", "gws_act8.cuh", "gws_host.h", "gws_internal.h"],
+    "gws_step.cu": ["gws_norm.cuh", "gws_adamw.cuh", "gws_pair.cuh", "gws_sums.cuh", "gws_act8.cuh", "gws_host.h", "gws_internal.h"],
 }
 SOURCES = [os.path.join(CSRC, name) for name in _UNITS]
 HEADERS = sorted({os.path.join(CSRC, h) for hs in _UNITS.values() for h in hs}) + [os.path.join(INCLUDE, "gws.h")]

@@ -492,9 +492,20 @@ int64_t linear_copies(const gws_linear_desc* d, const ForwardPlan& f) {
   return (f.move_x ? packed_bytes(d->m, d->k) : 0) + (f.move_w ? packed_bytes(d->n, d->k) : 0);
 }
 
+// Shares of a strip's rows: of at least 16 rows, and as many blocks as the SMs hold at once (six each).
+uint32_t pre_shares(int64_t rows, int64_t cols, int sms) {
+  const int64_t strips = (cols + 63) / 64, fill = std::max<int64_t>(1, 6 * sms / strips), most = (rows + 15) / 16;
+  if (most <= 8) return rows > 64 ? 8u : rows > 32 ? 4u : rows > 16 ? 2u : 1u;
+  return static_cast<uint32_t>(std::max<int64_t>(8, std::min(fill, (rows + 63) / 64)));
+}
+int64_t pre_part_bytes(int64_t rows, int64_t cols, int sms) {
+  const uint32_t shares = pre_shares(rows, cols, sms);
+  return shares <= 8u ? 0 : round_up(static_cast<int64_t>(shares) * cols * 4, 256);
+}
+
 // Backward: places in the workspace, whatever the call asks for.  dz is grad_y itself without an activation (aligned if its rows are not).
 struct LinearBack {
-  int64_t x, w, dz, part, total;
+  int64_t x, w, dz, sums, part, total;
   Tile dx;
   DwChoice dw;
 };
@@ -509,6 +520,7 @@ LinearBack weigh_linear_back(const gws_linear_desc* d, int sms) {
   l.x = take(direct_x ? 0 : packed_bytes(d->m, d->k));
   l.w = take(in_place(d->n, d->ld_w) ? 0 : packed_bytes(d->n, d->k));
   l.dz = take(makes || moves ? packed_bytes(d->m, d->n) : 0);
+  l.sums = take(pre_part_bytes(d->m, d->n, sms));
   l.part = take(std::max(part_bytes(l.dx), part_bytes(l.dw.tile)));
   l.total = at;
   return l;
@@ -517,19 +529,30 @@ const LinearBack& linear_back(const gws_linear_desc* d, int sms) {
   return remembered<LinearBack>({d->m, d->n, d->k, d->ld_x, d->ld_w, d->ld_y, d->activation != GWS_ACT_NONE, d->x_format, sms}, [&] { return weigh_linear_back(d, sms); });
 }
 
-// A block's share of a strip is at least 16 rows, a row to eight of its threads.
-int launch_linear_pre(LinearPre p, Ready& ready, int save, bool wide, cudaStream_t s) {
+template <int SAVE, bool WIDE>
+auto pre_kernel(int act) {
+  return act == GWS_GATED_SILU        ? k_linear_pre<SAVE, GWS_GATED_SILU, WIDE>
+         : act == GWS_GATED_GELU_TANH ? k_linear_pre<SAVE, GWS_GATED_GELU_TANH, WIDE>
+         : act == GWS_GATED_RELU      ? k_linear_pre<SAVE, GWS_GATED_RELU, WIDE>
+                                      : k_linear_pre<SAVE, GWS_ACT_NONE, WIDE>;
+}
+// `part`: room of pre_part_bytes.
+int launch_linear_pre(LinearPre p, Ready& ready, int act, int save, bool wide, void* part, int sms, cudaStream_t s) {
   const int64_t moved = ready.blocks(), strips = (p.cols + 63) / 64;
   if (moved < 0) return static_cast<int>(moved);
-  p.shares = p.rows > 64 ? 8u : p.rows > 32 ? 4u : p.rows > 16 ? 2u : 1u;
-  p.first = static_cast<uint32_t>(round_up(moved, p.shares));
+  p.shares = pre_shares(p.rows, p.cols, sms);
+  const bool clustered = p.db != nullptr && p.shares <= 8u;
+  if (p.db != nullptr && !clustered) p.part = static_cast<float*>(part);
+  p.first = static_cast<uint32_t>(clustered ? round_up(moved, p.shares) : moved);
+  if (strips * p.shares >= 0x3FFFFFFFLL) return GWS_ERR_LIMIT;
   const unsigned grid = p.first + static_cast<unsigned>(strips) * p.shares;
-  const char* what = "linear backward, element-wise part";
-  auto go = [&](void (*kernel)(LinearPre, Prep)) { return launch(kernel, grid, kPreThreads, 0, p.shares, s, what, p, ready.prep); };
-  if (save == GWS_ACT8_INT8) return go(wide ? k_linear_pre<GWS_ACT8_INT8, true> : k_linear_pre<GWS_ACT8_INT8, false>);
-  if (save == GWS_ACT8_E4M3) return go(wide ? k_linear_pre<GWS_ACT8_E4M3, true> : k_linear_pre<GWS_ACT8_E4M3, false>);
-  if (save == GWS_SAVE_BF16) return go(wide ? k_linear_pre<GWS_SAVE_BF16, true> : k_linear_pre<GWS_SAVE_BF16, false>);
-  return go(wide ? k_linear_pre<GWS_SAVE_NONE, true> : k_linear_pre<GWS_SAVE_NONE, false>);
+  auto kernel = save == GWS_ACT8_INT8   ? (wide ? pre_kernel<GWS_ACT8_INT8, true>(act) : pre_kernel<GWS_ACT8_INT8, false>(act))
+                : save == GWS_ACT8_E4M3 ? (wide ? pre_kernel<GWS_ACT8_E4M3, true>(act) : pre_kernel<GWS_ACT8_E4M3, false>(act))
+                : save == GWS_SAVE_BF16 ? (wide ? pre_kernel<GWS_SAVE_BF16, true>(act) : pre_kernel<GWS_SAVE_BF16, false>(act))
+                                        : (wide ? k_linear_pre<GWS_SAVE_NONE, GWS_ACT_NONE, true> : k_linear_pre<GWS_SAVE_NONE, GWS_ACT_NONE, false>);
+  const int st = launch(kernel, grid, kPreThreads, 0, clustered ? p.shares : 1, s, "linear backward, element-wise part", p, ready.prep);
+  if (st != GWS_OK || p.part == nullptr) return st;
+  return launch(k_column_sums, blocks_for(p.cols, 32), 256, 0, 1, s, "join of column sums", static_cast<const float*>(p.part), p.shares, p.cols, 1u, p.db, static_cast<void*>(nullptr), p.db_f32);
 }
 
 void describe(const Tile& t, int sms, gws_product_plan* p) {
@@ -968,10 +991,9 @@ int gws_linear_bwd(const gws_linear_desc* desc, const void* grad_y, const void* 
     p.db_f32 = d.bias_type == GWS_TYPE_F32;
     p.rows = d.m;
     p.cols = d.n;
-    p.activation = d.activation;
     const bool wide = d.n % 8 == 0 && (p.dy == nullptr || (on(grad_y, 16) && p.ld_dy % 8 == 0)) && (act_out == nullptr || on(act_out, 16)) &&
                       (!reads || saved8 || on(save, 16));
-    if ((st = launch_linear_pre(p, ready, reads ? d.save_format : GWS_SAVE_NONE, wide, s)) != GWS_OK) return st;
+    if ((st = launch_linear_pre(p, ready, d.activation, reads ? d.save_format : GWS_SAVE_NONE, wide, ws + l.sums, sms, s)) != GWS_OK) return st;
   } else if ((st = ready.run(s)) != GWS_OK) {
     return st;
   }
