@@ -6,6 +6,7 @@ If the library is missing or cannot be loaded the functions raise: there is no C
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -1060,7 +1061,11 @@ def _norm_weights(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], 
     for t in (weight, bias):
         if t is not None and (t.dtype is not dtype or t.shape != (n,)):
             raise ValueError("gws: weight and bias of a norm are (%d,) tensors of one type" % n)
-    return weight.contiguous(), None if bias is None else bias.contiguous(), TYPE_BF16 if dtype is _BF16 else TYPE_F32
+    if not weight.is_contiguous():
+        weight = weight.contiguous()
+    if bias is not None and not bias.is_contiguous():
+        bias = bias.contiguous()
+    return weight, bias, TYPE_BF16 if dtype is _BF16 else TYPE_F32
 
 
 def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -1075,9 +1080,9 @@ def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
     total, p_r, ld_r, p_sum = x, None, 0, None
     if residual is not None:
         residual, p_r, ld_r, _, _ = _bf16_rows(residual, "residual", m, n, read_by_map=False)
-        total = x.new_empty(m, n)
+        total = _dense_like(residual, m, n)
         p_sum = total.data_ptr()
-    y = x.new_empty(m, n)
+    y = _dense_like(x, m, n)
     stats = x.new_empty(2, m, dtype=torch.float32) if want_stats else None
     _, at, _ = _norm_plan(m, n, ld_x, ld_r, 0, 0, kind, eps, device)
     code = (_lib or load_library()).gws_layernorm_fwd(at, p_x, p_r, _addr(weight), _addr(bias), y.data_ptr(), p_sum, _addr(stats), _raw_stream(device))
@@ -1102,7 +1107,7 @@ def layernorm_bwd(grad_y: torch.Tensor, s: torch.Tensor, weight: Optional[torch.
     p_d, ld_d = None, 0
     if grad_sum is not None:
         grad_sum, p_d, ld_d, _, _ = _bf16_rows(grad_sum, "grad_sum", m, n, read_by_map=False)
-    grad_x = grad_y.new_empty(m, n) if want_grad_x else None
+    grad_x = _dense_like(grad_y, m, n) if want_grad_x else None
     grad_weight = torch.empty_like(weight) if weight is not None and want_grad_weight else None
     grad_bias = torch.empty_like(weight) if weight is not None and want_grad_bias else None
     _, at, nbytes = _norm_plan(m, n, ld_s, 0, ld_dy, ld_d, kind, 0.0, device)
@@ -1155,8 +1160,8 @@ class AdamWState:
                  units: Optional[torch.Tensor] = None):
         if fmt not in (ADAMW_F32, ADAMW_8BIT):
             raise ValueError("gws: the format of moments is ADAMW_F32 or ADAMW_8BIT")
-        self.sizes, self.fmt = tuple(sizes), fmt
-        self.starts, total, self._c_sizes, self._c_starts = _adamw_layout(self.sizes)
+        self.sizes, self.fmt = list(sizes), fmt
+        self.starts, total, self._c_sizes, self._c_starts = _adamw_layout(tuple(self.sizes))
         self.total = total
         bits8 = fmt == ADAMW_8BIT
         if moments is None:
@@ -1205,6 +1210,19 @@ class AdamWState:
         return ((param.detach().view(torch.int16).to(torch.int32) << 16) + low.to(torch.int32)).view(torch.float32)
 
 
+@functools.lru_cache(maxsize=64)
+def _adamw_types(dtypes: tuple):
+    known = {_BF16: TYPE_BF16, torch.float32: TYPE_F32}
+    if any(d not in known for d in dtypes):
+        raise ValueError("gws: parameters are BF16 or FP32")
+    return (c_int32 * len(dtypes))(*[known[d] for d in dtypes])
+
+
+@functools.lru_cache(maxsize=64)
+def _adamw_decays(decays: tuple):
+    return (ctypes.c_double * len(decays))(*[float(w) for w in decays])
+
+
 def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
                step=1, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
     """One AdamW step over all tensors, in place, in one launch (for up to 384 of them).
@@ -1220,36 +1238,32 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
         _require_cuda(state.moments)
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale)
-    keep, p_params, p_grads, types = [], [], [], []
-    for p, g, size in zip(params, grads, state.sizes):
-        if g is None:
-            p_params.append(None)
-            p_grads.append(None)
-            types.append(TYPE_BF16)
-            continue
-        dtype = p.dtype
-        if dtype is _BF16:
-            types.append(TYPE_BF16)
-        elif dtype is torch.float32:
-            types.append(TYPE_F32)
-        else:
-            raise ValueError("gws: parameters are BF16 or FP32")
-        if g.dtype is not dtype or g.shape != p.shape or p.numel() != size:
-            raise ValueError("gws: a gradient has its parameter's type and shape, and the parameter the state's size")
-        if not p.is_contiguous():
-            raise ValueError("gws: parameters are contiguous")
-        if p.get_device() != device or g.get_device() != device:
-            _require_cuda(p, g)
-            raise ValueError("gws: the tensors of a call live on one device")
-        if not g.is_contiguous():
-            g = g.contiguous()
-            keep.append(g)
-        p_params.append(p.data_ptr())
-        p_grads.append(g.data_ptr())
+    sizes, where = state.sizes, None
+    if any([g is None for g in grads]):
+        where = [i for i, g in enumerate(grads) if g is not None]
+        params, grads, sizes = [params[i] for i in where], [grads[i] for i in where], [sizes[i] for i in where]
+    dtypes = [p.dtype for p in params]
+    if dtypes != [g.dtype for g in grads] or [p.shape for p in params] != [g.shape for g in grads] or [p.numel() for p in params] != sizes:
+        raise ValueError("gws: a gradient has its parameter's type and shape, and the parameter the state's size")
+    if not all([p.is_contiguous() for p in params]):
+        raise ValueError("gws: parameters are contiguous")
+    if sizes and ({p.get_device() for p in params} != {device} or {g.get_device() for g in grads} != {device}):
+        _require_cuda(*params, *grads)
+        raise ValueError("gws: the tensors of a call live on one device")
+    if not all([g.is_contiguous() for g in grads]):
+        grads = [g.contiguous() for g in grads]
+    types = _adamw_types(tuple(dtypes))
+    p_params, p_grads = array.array("Q", [p.data_ptr() for p in params]), array.array("Q", [g.data_ptr() for g in grads])
+    if where is not None:                                # places without a gradient: null
+        wide = [array.array("Q", bytes(8 * n)) for _ in range(2)] + [(c_int32 * n)()]
+        for i, *entry in zip(where, p_params, p_grads, types):
+            for to, value in zip(wide, entry):
+                to[i] = value
+        p_params, p_grads, types = wide
     if isinstance(weight_decay, (int, float)):
-        decays = [float(weight_decay)] * n
+        decays = _adamw_decays((float(weight_decay),) * n)
     else:
-        decays = [float(w) for w in weight_decay]
+        decays = _adamw_decays(tuple(weight_decay))
         if len(decays) != n:
             raise ValueError("gws: one weight_decay for all tensors, or one for each")
     args = _AdamwArgs(0.0, betas[0], betas[1], eps, 1, None, None, None, None)
@@ -1274,12 +1288,11 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
     if args.lr_dev or args.step_dev:
         scalars = torch.empty(4, dtype=torch.float32, device=state.moments.device)
         args.scalars = scalars.data_ptr()
-    array = c_void_p * n
-    code = (_lib or load_library()).gws_adamw_step(n, array(*p_params), array(*p_grads), state._c_sizes, state._c_starts, (c_int32 * n)(*types),
-                                                   (ctypes.c_double * n)(*decays), ctypes.addressof(state._c), ctypes.addressof(args), _raw_stream(device))
+    code = (_lib or load_library()).gws_adamw_step(n, p_params.buffer_info()[0], p_grads.buffer_info()[0], state._c_sizes, state._c_starts, types, decays,
+                                                   ctypes.addressof(state._c), ctypes.addressof(args), _raw_stream(device))
     if code:
         _check(code)
-    torch.autograd.graph.increment_version([p for p, g in zip(params, grads) if g is not None])
+    torch.autograd.graph.increment_version(params)
 
 
 def selfcheck_enabled() -> bool:

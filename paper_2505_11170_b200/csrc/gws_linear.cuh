@@ -31,8 +31,8 @@ struct LinearPre {
   int32_t db_f32;
 };
 
-// act(z) and its slope of eight elements, as act_and_slope in gws_tc.cuh, two at a time.
-template <int ACT>
+// act(z) and its slope of eight elements, as act_and_slope in gws_tc.cuh, two at a time.  FAR: z^2 may pass FP32.
+template <int ACT, bool FAR>
 __device__ __forceinline__ void slopes(const F2 (&z)[4], F2 (&a)[4], F2 (&slope)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -48,14 +48,16 @@ __device__ __forceinline__ void slopes(const F2 (&z)[4], F2 (&a)[4], F2 (&slope)
     constexpr float kLog2e = 1.44269504f;
     F2 zz = z[i], x = mul2(z[i], both(-kLog2e));
     if (ACT == GWS_GATED_GELU_TANH) {
-      zz = two(fminf(first_of(z[i]) * first_of(z[i]), 0x1p100f), fminf(second_of(z[i]) * second_of(z[i]), 0x1p100f));
+      zz = mul2(z[i], z[i]);
+      if (FAR) zz = two(fminf(first_of(zz), 0x1p100f), fminf(second_of(zz), 0x1p100f));
       x = mul2(z[i], fma2(zz, both(-kLog2e * kGeluLin * 0.044715f), both(-kLog2e * kGeluLin)));
     }
     float e0, e1, s0, s1;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(first_of(x)));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(second_of(x)));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s0) : "f"(1.0f + e0));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s1) : "f"(1.0f + e1));
+    const F2 d = fma2(two(e0, e1), both(1.0f), both(1.0f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s0) : "f"(first_of(d)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s1) : "f"(second_of(d)));
     const F2 s = two(s0, s1);
     a[i] = mul2(z[i], s);
     F2 t = mul2(a[i], fma2(s, both(-1.0f), both(1.0f)));
@@ -87,7 +89,7 @@ constexpr uint32_t kPreThreads = 128u, kPreSlots = kPreThreads / 8u;
 // WIDE: rows of dy, of a BF16 z and of act(z) on 16-byte boundaries.  Otherwise a warp reads its four rows an element to a lane, side by side, and turns them in
 // shared memory.
 template <int SAVE, int ACT, bool WIDE>
-__global__ void __launch_bounds__(kPreThreads) k_linear_pre(const __grid_constant__ LinearPre p, const __grid_constant__ Prep m) {
+__global__ void __launch_bounds__(kPreThreads, 6) k_linear_pre(const __grid_constant__ LinearPre p, const __grid_constant__ Prep m) {
   after_previous();
   if (blockIdx.x < p.first) {
     (void)prepare(m, threadIdx.x);
@@ -104,100 +106,153 @@ __global__ void __launch_bounds__(kPreThreads) k_linear_pre(const __grid_constan
   const int64_t col0 = static_cast<int64_t>(strip) * 64, col = col0 + oct * 8;
   const int64_t per = (p.rows + p.shares - 1) / p.shares, begin = min(p.rows, share * per);
   const int32_t rows = static_cast<int32_t>(min(p.rows, begin + per) - begin);            // of this share
-  const uint16_t* const dy0 = p.dy != nullptr ? p.dy + begin * p.ld_dy : nullptr;
-  const uint16_t* const z0 = SAVE == GWS_SAVE_BF16 ? p.save16 + begin * p.cols : nullptr;
-  const bool mine = col < p.cols, coded = kIs8 && col < p.save8.ld;
-  auto bring = [&](const uint16_t* base, int64_t ld, int32_t row) {           // eight elements of a row, zeros outside
-    if constexpr (WIDE) return row < rows && mine ? __ldg(reinterpret_cast<const uint4*>(base + row * ld + col)) : make_uint4(0u, 0u, 0u, 0u);
-    const int32_t row0 = row - static_cast<int32_t>(lane >> 3);
-    uint16_t v[8];
+  const bool has_dy = p.dy != nullptr;
+  F2 db[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int32_t r = row0 + i / 2;
-      const int64_t c = col0 + (i & 1) * 32 + lane;
-      v[i] = r < rows && c < p.cols ? base[r * ld + c] : static_cast<uint16_t>(0);
-    }
-    uint16_t* side = reinterpret_cast<uint16_t*>(turn[WIDE ? 0 : warp]) + lane;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) side[32 * i] = v[i];
-    __syncwarp();
-    const uint4 w = turn[WIDE ? 0 : warp][lane];
-    __syncwarp();
-    return w;
-  };
+  for (int i = 0; i < 4; ++i) db[i] = both(0.0f);
   struct Raw {
     uint4 g, z16;
     uint2 z8;
     uint32_t byte;
   };
-  auto fetch = [&](int32_t row, Raw& r) {
-    if (dy0 != nullptr) r.g = bring(dy0, p.ld_dy, row);
-    if (SAVE == GWS_SAVE_BF16) r.z16 = bring(z0, p.cols, row);
-    if (kIs8) {
-      const bool real = row < rows && coded;
-      const int64_t at = (begin + row) * p.save8.ld + col;
-      r.z8 = real ? __ldg(reinterpret_cast<const uint2*>(p.save8.codes + at)) : make_uint2(0u, 0u);
-      r.byte = real ? p.save8.scales[at >> 5] : 0u;
+  auto element_wise = [&](const Raw& r, F2 (&a)[4], F2 (&slope)[4]) {
+    F2 z[4];
+    if constexpr (kIs8) {
+      const float unit = unit_of<kFmt>(r.byte);
+      decode8<kFmt>(r.z8, unit, z);
+      if (unit <= 0x1p40f) slopes<ACT, false>(z, a, slope);
+      else slopes<ACT, true>(z, a, slope);
+    } else {
+      const uint32_t q[4] = {r.z16.x, r.z16.y, r.z16.z, r.z16.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[i] = SAVE == GWS_SAVE_BF16 ? two(bf16_lo(q[i]), bf16_hi(q[i])) : both(0.0f);
+      slopes<ACT, true>(z, a, slope);
     }
   };
-  F2 db[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) db[i] = both(0.0f);
-  constexpr int kRows = WIDE ? 3 : 1;                                          // rows of a thread under way
-  Raw next[kRows];
-#pragma unroll
-  for (int k = 0; k < kRows; ++k) fetch(static_cast<int32_t>(slot + kPreSlots * k), next[k]);
-#pragma unroll 1
-  for (int32_t at = 0; at < rows; at += kPreSlots * kRows) {
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-      const int32_t row = at + static_cast<int32_t>(slot + kPreSlots * k);
-      const Raw now = next[k];
-      fetch(row + static_cast<int32_t>(kPreSlots * kRows), next[k]);
-      F2 z[4], a[4], slope[4];
-      if (SAVE == GWS_SAVE_BF16) {
-        const uint32_t q[4] = {now.z16.x, now.z16.y, now.z16.z, now.z16.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = two(bf16_lo(q[i]), bf16_hi(q[i]));
-      } else if (kIs8) {
-        decode8<kFmt>(now.z8, unit_of<kFmt>(now.byte), z);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = both(0.0f);
+  auto packed = [](const F2 (&v)[4]) {
+    return make_uint4(pack_bf16(first_of(v[0]), second_of(v[0])), pack_bf16(first_of(v[1]), second_of(v[1])), pack_bf16(first_of(v[2]), second_of(v[2])),
+                      pack_bf16(first_of(v[3]), second_of(v[3])));
+  };
+  if constexpr (WIDE) {
+    // Rows slot, slot + 16, ... of the share; every stream's address moves on by 16 rows.
+    constexpr int kRows = 3;                               // of a thread, under way
+    const int32_t mine = col < p.cols && rows > static_cast<int32_t>(slot) ? (rows - static_cast<int32_t>(slot) + static_cast<int32_t>(kPreSlots) - 1) / static_cast<int32_t>(kPreSlots) : 0;
+    const int64_t row0 = begin + slot;
+    const uint16_t* dy = p.dy + row0 * p.ld_dy + col;
+    const uint16_t* z16 = p.save16 + row0 * p.cols + col;
+    const uint8_t* z8 = p.save8.codes + row0 * p.save8.ld + col;
+    const uint8_t* byte = p.save8.scales + row0 * (p.save8.ld >> 5) + (col >> 5);
+    uint16_t* dz = p.dz + row0 * p.ld_dz + col;
+    uint16_t* again = p.again + row0 * p.cols + col;
+    const int64_t to_dy = p.ld_dy * kPreSlots, to_z = p.cols * kPreSlots, to_z8 = p.save8.ld * kPreSlots, to_byte = (p.save8.ld >> 5) * kPreSlots, to_dz = p.ld_dz * kPreSlots;
+    auto fetch = [&](Raw& r) {
+      if (has_dy) {
+        r.g = __ldg(reinterpret_cast<const uint4*>(dy));
+        dy += to_dy;
       }
-      slopes<ACT>(z, a, slope);
-      uint32_t w[4];
-      if (dy0 != nullptr) {
-        const uint32_t q[4] = {now.g.x, now.g.y, now.g.z, now.g.w};
+      if (SAVE == GWS_SAVE_BF16) {
+        r.z16 = __ldg(reinterpret_cast<const uint4*>(z16));
+        z16 += to_z;
+      }
+      if (kIs8) {
+        r.z8 = __ldg(reinterpret_cast<const uint2*>(z8));
+        r.byte = __ldg(byte);
+        z8 += to_z8;
+        byte += to_byte;
+      }
+    };
+    Raw next[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
+      if (k < mine) fetch(next[k]);
+#pragma unroll 1
+    for (int32_t j = 0; j < mine; j += kRows) {
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        if (j + k >= mine) break;
+        const Raw now = next[k];
+        if (j + k + kRows < mine) fetch(next[k]);
+        F2 a[4], slope[4];
+        element_wise(now, a, slope);
+        if (has_dy) {
+          const uint32_t q[4] = {now.g.x, now.g.y, now.g.z, now.g.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            slope[i] = mul2(two(bf16_lo(q[i]), bf16_hi(q[i])), slope[i]);
+            db[i] = fma2(slope[i], both(1.0f), db[i]);
+          }
+          if (p.dz != nullptr) {
+            *reinterpret_cast<uint4*>(dz) = packed(slope);
+            dz += to_dz;
+          }
+        }
+        if (p.again != nullptr) {
+          *reinterpret_cast<uint4*>(again) = packed(a);
+          again += to_z;
+        }
+      }
+    }
+  } else {
+    const uint16_t* const dy0 = has_dy ? p.dy + begin * p.ld_dy : nullptr;
+    const uint16_t* const z0 = SAVE == GWS_SAVE_BF16 ? p.save16 + begin * p.cols : nullptr;
+    const int32_t sub = static_cast<int32_t>(lane >> 3);
+    uint16_t* const side = reinterpret_cast<uint16_t*>(turn[WIDE ? 0 : warp]) + lane;
+    auto load = [&](const uint16_t* base, int64_t ld, int32_t row, uint16_t (&v)[8]) {        // neighbouring elements of the warp's four rows, zeros outside
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int32_t r = row - sub + i / 2;
+        const int64_t c = col0 + (i & 1) * 32 + lane;
+        v[i] = r < rows && c < p.cols ? base[r * ld + c] : static_cast<uint16_t>(0);
+      }
+    };
+    auto own = [&](const uint16_t (&v)[8]) {                                                  // this lane's eight
+#pragma unroll
+      for (int i = 0; i < 8; ++i) side[32 * i] = v[i];
+      __syncwarp();
+      const uint4 w = turn[WIDE ? 0 : warp][lane];
+      __syncwarp();
+      return w;
+    };
+#pragma unroll 1
+    for (int32_t at = 0; at < rows; at += kPreSlots) {
+      const int32_t row = at + static_cast<int32_t>(slot);
+      uint16_t vg[8], vz[8];
+      Raw r;
+      if (has_dy) load(dy0, p.ld_dy, row, vg);
+      if (SAVE == GWS_SAVE_BF16) load(z0, p.cols, row, vz);
+      if (kIs8) {
+        const bool real = row < rows && col < p.save8.ld;
+        const int64_t from = (begin + row) * p.save8.ld + col;
+        r.z8 = real ? __ldg(reinterpret_cast<const uint2*>(p.save8.codes + from)) : make_uint2(0u, 0u);
+        r.byte = real ? p.save8.scales[from >> 5] : 0u;
+      }
+      if (has_dy) r.g = own(vg);
+      if (SAVE == GWS_SAVE_BF16) r.z16 = own(vz);
+      F2 a[4], slope[4];
+      element_wise(r, a, slope);
+      if (has_dy) {
+        const uint32_t q[4] = {r.g.x, r.g.y, r.g.z, r.g.w};
         // an element outside has dy = 0; its z may be a NaN (the group's), which must not reach the sum
-        const bool whole = WIDE ? row < rows && mine : row < rows && col + 8 <= p.cols;
+        const bool whole = row < rows && col + 8 <= p.cols;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           F2 d = mul2(two(bf16_lo(q[i]), bf16_hi(q[i])), slope[i]);
-          if (!WIDE && !whole) d = two(row < rows && col + 2 * i < p.cols ? first_of(d) : 0.0f, row < rows && col + 2 * i + 1 < p.cols ? second_of(d) : 0.0f);
-          if (!WIDE || whole) db[i] = fma2(d, both(1.0f), db[i]);
-          w[i] = pack_bf16(first_of(d), second_of(d));
+          if (!whole) d = two(row < rows && col + 2 * i < p.cols ? first_of(d) : 0.0f, row < rows && col + 2 * i + 1 < p.cols ? second_of(d) : 0.0f);
+          db[i] = fma2(d, both(1.0f), db[i]);
+          slope[i] = d;
         }
-        if (p.dz != nullptr && row < rows && (!WIDE || mine)) *reinterpret_cast<uint4*>(p.dz + (begin + row) * p.ld_dz + col) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (p.dz != nullptr && row < rows) *reinterpret_cast<uint4*>(p.dz + (begin + row) * p.ld_dz + col) = packed(slope);
       }
       if (p.again != nullptr) {
+        turn[WIDE ? 0 : warp][lane] = packed(a);
+        __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(first_of(a[i]), second_of(a[i]));
-        if constexpr (WIDE) {
-          if (row < rows && mine) *reinterpret_cast<uint4*>(p.again + (begin + row) * p.cols + col) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-          turn[WIDE ? 0 : warp][lane] = make_uint4(w[0], w[1], w[2], w[3]);
-          __syncwarp();
-          const uint16_t* side = reinterpret_cast<const uint16_t*>(turn[WIDE ? 0 : warp]) + lane;
-          const int32_t row0 = row - static_cast<int32_t>(lane >> 3);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int32_t r = row0 + i / 2;
-            const int64_t c = col0 + (i & 1) * 32 + lane;
-            if (r < rows && c < p.cols) p.again[(begin + r) * p.cols + c] = side[32 * i];
-          }
-          __syncwarp();
+        for (int i = 0; i < 8; ++i) {
+          const int32_t to = row - sub + i / 2;
+          const int64_t c = col0 + (i & 1) * 32 + lane;
+          if (to < rows && c < p.cols) p.again[(begin + to) * p.cols + c] = side[32 * i];
         }
+        __syncwarp();
       }
     }
   }
