@@ -993,7 +993,7 @@ def linear_fwd(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = 
 
 def linear_bwd(grad_y: torch.Tensor, x, w: torch.Tensor, saved=None, activation: int = ACT_NONE, want_grad_x: bool = True, want_grad_w: bool = True,
                want_grad_bias: bool = False, want_act: bool = False, bias_dtype: torch.dtype = torch.bfloat16, status: Optional[torch.Tensor] = None, stream=None):
-    """Backward pass of :func:`linear_fwd`.  ``x`` is the BF16 input or its checkpoint, ``saved`` what the forward call kept of z (not read with ACT_NONE, unless act(z) is
+    """Backward pass of :func:`linear_fwd`.  ``x`` is the BF16 input or its checkpoint (None where grad_w is not wanted), ``saved`` what the forward call kept of z (not read with ACT_NONE, unless act(z) is
     wanted).  Returns (grad_x, grad_w, grad_bias, act(z)), None for what was not asked for; grad_bias is of ``bias_dtype``.  The residual's gradient is grad_y.  act(z) is
     what the weight gradient of the layer after this one needs."""
     kept_x, kept_z = isinstance(x, Act8), isinstance(saved, Act8)
@@ -1002,11 +1002,18 @@ def linear_bwd(grad_y: torch.Tensor, x, w: torch.Tensor, saved=None, activation:
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, linear_bwd, grad_y, x, w, saved, activation, want_grad_x, want_grad_w, want_grad_bias, want_act, bias_dtype, status)
     p_st = _status_of(status)
-    m, k = x.shape
+    if x is None:
+        if want_grad_w:
+            raise ValueError("gws: the gradient of W needs x")
+        m, k = grad_y.shape[0], w.shape[-1]
+    else:
+        m, k = x.shape
     w, p_w, ld_w, n, _ = _bf16_rows(w, "w", None, k)
     grad_y, p_dy, ld_y, _, _ = _bf16_rows(grad_y, "grad_y", m, n, read_by_map=activation == ACT_NONE)
     if kept_x:
         p_x, ld_x, x_format = x.buffer.data_ptr(), k or 1, x.fmt
+    elif x is None:
+        p_x, ld_x, x_format = None, k or 1, SAVE_BF16
     else:
         x, p_x, ld_x, _, _ = _bf16_rows(x, "x")
         x_format = SAVE_BF16
@@ -1180,6 +1187,9 @@ class AdamWState:
             self._take(rest, "rest", torch.int16, (total,))
         self.moments, self.units, self.rest = moments, units, rest
         self._c = _AdamwState(moments.data_ptr(), _addr(units), _addr(rest), total, fmt, 0)
+
+    def __reduce__(self):
+        return AdamWState, (self.sizes, self.fmt, False if self.rest is None else self.rest, self.moments.device, self.moments, self.units)
 
     @staticmethod
     def _take(t, name, dtype, shape) -> None:

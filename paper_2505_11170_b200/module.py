@@ -13,6 +13,9 @@ every step of the sampling pass runs in its kernels.  The GEMMs are torch's, exa
 ``GaussWSGatedMLP`` is the gated feed-forward block on three such layers.  Its gate and up projections, the activation and their product
 run in the library's block kernels, and what the block keeps for its backward pass - its input and the two projections - may be held
 as 8-bit activation checkpoints; ``GaussWSLinear(keep=...)`` keeps a single layer's input that way.
+
+``GaussWSLayerNorm`` and ``GaussWSMLP``, the plain feed-forward block, are the parts of the other kind of transformer block; ``GaussWSAdamW`` (optimizer.py)
+takes the step over all of a model's tensors.
 """
 from __future__ import annotations
 
@@ -147,6 +150,70 @@ class _GatedMLP(torch.autograd.Function):
                 rows.t() @ h if need_down else None, None, None)
 
 
+class _LayerNorm(torch.autograd.Function):
+    """(y, s) with s = x + residual and y the layer norm of s; y alone without a residual.  Second derivatives are refused."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, eps):
+        rows = x.reshape(-1, x.shape[-1])
+        needed = any(ctx.needs_input_grad[:4])
+        y, s, stats = binding.layernorm_fwd(rows, weight, bias, eps, residual=None if residual is None else residual.reshape(rows.shape), want_stats=needed)
+        ctx.set_materialize_grads(False)
+        if needed:
+            ctx.save_for_backward(s, weight, stats)
+        y = y.view(x.shape)
+        return y if residual is None else (y, s.view(x.shape))
+
+    @staticmethod
+    @_refuses_a_second
+    def backward(ctx, grad_y, grad_s=None):
+        s, weight, stats = ctx.saved_tensors
+        need_x, need_r, need_w, need_b = ctx.needs_input_grad[:4]
+        if grad_y is None:
+            return grad_s if need_x else None, grad_s if need_r else None, None, None, None
+        grad_x, grad_w, grad_b = binding.layernorm_bwd(grad_y.reshape(s.shape), s, weight, stats, grad_sum=None if grad_s is None else grad_s.reshape(s.shape),
+                                                       want_grad_x=need_x or need_r, want_grad_weight=need_w, want_grad_bias=need_b)
+        if grad_x is not None:
+            grad_x = grad_x.view(grad_y.shape)
+        return grad_x if need_x else None, grad_x if need_r else None, grad_w, grad_b, None
+
+
+class _MLP(torch.autograd.Function):
+    """y = act(x Wu^T + bu) Wd^T + bd (+ residual).  Kept for the backward pass: x and x Wu^T + bu in the given format; the hidden activation is formed again from the
+    second.  Second derivatives are refused."""
+
+    @staticmethod
+    def forward(ctx, x, residual, w_up, b_up, w_down, b_down, activation, fmt):
+        rows = x.reshape(-1, x.shape[-1])
+        needed = any(ctx.needs_input_grad[:6])
+        h, z = binding.linear_fwd(rows, w_up, b_up, activation=activation, save=fmt if needed else binding.SAVE_NONE)
+        y, _ = binding.linear_fwd(h, w_down, b_down, residual=None if residual is None else residual.reshape(rows.shape[0], w_down.shape[0]))
+        if needed:
+            bf16 = fmt == binding.SAVE_BF16
+            ctx.save_for_backward(rows if bf16 else binding.act8_save(rows, fmt).buffer, z if bf16 else z.buffer, w_up, w_down)
+            ctx.kept, ctx.activation, ctx.x_shape = (rows.shape[0], rows.shape[1], w_up.shape[0], fmt), activation, x.shape
+            ctx.bias_types = [torch.bfloat16 if b is None else b.dtype for b in (b_up, b_down)]
+        return y.view(*x.shape[:-1], w_down.shape[0])
+
+    @staticmethod
+    @_refuses_a_second
+    def backward(ctx, grad_y):
+        x, z, w_up, w_down = ctx.saved_tensors
+        m, k, n, fmt = ctx.kept
+        need_x, need_r, need_wu, need_bu, need_wd, need_bd = ctx.needs_input_grad[:6]
+        if fmt != binding.SAVE_BF16:
+            x, z = binding.Act8(x, m, k, fmt), binding.Act8(z, m, n, fmt)
+        rows = grad_y.reshape(m, w_down.shape[0])
+        through = need_x or need_wu or need_bu
+        grad_h, _, grad_bd, _ = binding.linear_bwd(rows, None, w_down, want_grad_x=through, want_grad_w=False, want_grad_bias=need_bd, bias_dtype=ctx.bias_types[1])
+        if grad_h is None:                               # not read: act(z) is all that may be wanted below
+            grad_h = rows.new_empty(m, n)
+        grad_x, grad_wu, grad_bu, h = binding.linear_bwd(grad_h, x, w_up, z, ctx.activation, want_grad_x=need_x, want_grad_w=need_wu, want_grad_bias=need_bu,
+                                                         want_act=need_wd, bias_dtype=ctx.bias_types[0])
+        grad_wd = binding.linear_bwd(rows, h, w_down, want_grad_x=False)[1] if need_wd else None
+        return (grad_x.view(ctx.x_shape) if need_x else None, grad_y if need_r else None, grad_wu, grad_bu, grad_wd, grad_bd, None, None)
+
+
 class GaussWSLinear(torch.nn.Module):
     """Linear layer trained with Gaussian weight sampling.
 
@@ -238,6 +305,58 @@ class GaussWSGatedMLP(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         return _GatedMLP.apply(x, self.gate.sampled_weight(), self.up.sampled_weight(), self.down.sampled_weight(), self.activation, self.keep)
+
+
+class GaussWSLayerNorm(torch.nn.Module):
+    """Layer norm over the last dimension of BF16 activations, y = (s - mean(s)) / sqrt(var(s) + eps) weight + bias.
+
+    ``forward(x)`` returns y for s = x; ``forward(x, residual)`` adds first, s = x + residual, and returns (y, s), so that the stream goes on from s.
+    ``dtype`` is that of the weight and the bias: BF16 or FP32."""
+
+    def __init__(self, features: int, eps: float = 1e-5, bias: bool = True, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        super().__init__()
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("gws: the weight of a norm is BF16 or FP32")
+        self.features, self.eps = features, float(eps)
+        self.weight = torch.nn.Parameter(torch.ones(features, dtype=dtype, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(features, dtype=dtype, device=device)) if bias else None
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None):
+        if residual is not None and residual.shape != x.shape:
+            raise ValueError("gws: the residual has the shape of x")
+        return _LayerNorm.apply(x, residual, self.weight, self.bias, self.eps)
+
+
+class GaussWSMLP(torch.nn.Module):
+    """Plain feed-forward block, y = act(x Wu^T + bu) Wd^T + bd, with its two weights sampled; ``forward(x, residual)`` adds the residual in the same kernel.
+
+    ``up`` and ``down`` are GaussWSLinear layers (``layer_index`` and ``layer_index + 1``), to be handed to a GaussWSSet like any other.  ``activation`` is
+    ``binding.GATED_GELU_TANH`` (default), ``GATED_SILU`` or ``GATED_RELU``.  ``keep`` says what the block holds for its backward pass: ``binding.ACT8_INT8`` (default) or
+    ``ACT8_E4M3`` - one byte per element of its input and of x Wu^T + bu - or ``SAVE_BF16``; the hidden activation is never held.
+    """
+
+    def __init__(self, features: int, hidden: int, activation: int = binding.GATED_GELU_TANH, keep: int = binding.ACT8_INT8, bias: bool = True, layer_index: int = 0,
+                 **layer):
+        super().__init__()
+        if keep not in (binding.ACT8_INT8, binding.ACT8_E4M3, binding.SAVE_BF16):
+            raise ValueError("gws: keep is ACT8_INT8, ACT8_E4M3 or SAVE_BF16")
+        if activation not in (binding.GATED_SILU, binding.GATED_GELU_TANH, binding.GATED_RELU):
+            raise ValueError("gws: unknown activation")
+        self.activation, self.keep = activation, keep
+        self.up = GaussWSLinear(features, hidden, bias=bias, layer_index=layer_index, **layer)
+        self.down = GaussWSLinear(hidden, features, bias=bias, layer_index=layer_index + 1, **layer)
+
+    @property
+    def layers(self):
+        return [self.up, self.down]
+
+    def advance(self) -> None:
+        """One gradient update has been applied (layers of a GaussWSSet are advanced by the set instead)."""
+        for layer in self.layers:
+            layer.advance()
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return _MLP.apply(x, residual, self.up.sampled_weight(), self.up.bias, self.down.sampled_weight(), self.down.bias, self.activation, self.keep)
 
 
 class GaussWSSet:

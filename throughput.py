@@ -1,6 +1,6 @@
 """Throughput of the sampling pass on the other workload shapes of the paper (one JSON line each).
 
-    python throughput.py [gpt2] [gpt2_single] [stress] [square] [llama] [mx] [gemm] [issue] [compare] [module] [overhead] [ffn] [--reps N] [--blocks B]
+    python throughput.py [gpt2] [gpt2_single] [stress] [square] [llama] [mx] [gemm] [issue] [compare] [module] [overhead] [ffn] [block] [--reps N] [--blocks B]
 
 gpt2         all GPT2-124M linear weights, one group per row (and the same set with groups of 128)
 gpt2_single  one GPT2-124M MLP weight, both orientations
@@ -16,6 +16,9 @@ overhead     the three GEMMs of every linear layer for one micro-batch, with and
 ffn          a training update of gated feed-forward blocks (2048 x 5632, 16384 tokens): the block module with 8-bit and with BF16
              copies of its activations against three sampled linear layers and torch's activation and product, with the bytes held
              between forward and backward
+block        a training update of plain transformer feed-forward blocks (norm, up projection with GELU, down projection onto the residual stream; 2048 x 5632,
+             16384 tokens) and the AdamW step over all of their tensors, with 32-bit and 8-bit moments, against torch's layer norm, linear layers, GELU and fused AdamW
+             around the same sampled weights
 issue        cycles per warp instruction of the instruction kinds the passes are made of, and of the passes' arithmetic
              without memory traffic (gws_issue_probe): the terms of the arithmetic ceiling of the backward pass
 
@@ -425,6 +428,85 @@ def run_ffn(reps: int, dev, n_blocks: int, tokens: int = 16384) -> list:
     return lines
 
 
+def run_block(reps: int, dev, n_blocks: int, tokens: int = 16384) -> list:
+    """Updates of a stack of norm + feed-forward blocks: sample, forward, backward, finish_backward, optimizer step."""
+    from paper_2505_11170_b200.module import GaussWSLayerNorm, GaussWSMLP, GaussWSSet
+    from paper_2505_11170_b200.optimizer import GaussWSAdamW
+
+    class Block(torch.nn.Module):
+        def __init__(self, index, composed):
+            super().__init__()
+            self.norm, self.mlp = GaussWSLayerNorm(2048, device=dev), GaussWSMLP(2048, 5632, layer_index=2 * index, group=(1, 128), device=dev)
+            self.composed = composed
+
+        def forward(self, stream):
+            if not self.composed:
+                return self.mlp(self.norm(stream), stream)
+            f = torch.nn.functional
+            y = f.layer_norm(stream, (2048,), self.norm.weight, self.norm.bias)
+            up, down = self.mlp.layers
+            return f.linear(f.gelu(f.linear(y, up.sampled_weight(), up.bias), approximate="tanh"), down.sampled_weight(), down.bias) + stream
+
+    torch.manual_seed(0)
+    x = torch.randn(tokens, 2048, device=dev).to(torch.bfloat16)
+    grad_y = (torch.randn(tokens, 2048, device=dev) * 1e-3).to(torch.bfloat16)
+    lines = []
+    for name in ("8bit", "f32", "composed"):
+        blocks = [Block(b, name == "composed") for b in range(n_blocks)]
+        params = [p for b in blocks for p in b.parameters()]
+        if name == "composed":
+            optimizer = torch.optim.AdamW(params, lr=1e-4, fused=True)
+        else:
+            optimizer = GaussWSAdamW(params, lr=1e-4, moments=gws.ADAMW_8BIT if name == "8bit" else gws.ADAMW_F32)
+        sampler = GaussWSSet([layer for b in blocks for layer in b.mlp.layers])
+
+        def forward(sampler=sampler, blocks=blocks):
+            sampler.sample()
+            y = x
+            for b in blocks:
+                y = b(y)
+            return y
+
+        def update(sampler=sampler, optimizer=optimizer):
+            forward().backward(grad_y)
+            sampler.finish_backward()
+            optimizer.step()
+            optimizer.zero_grad()
+            sampler.advance()
+
+        for _ in range(3):
+            update()
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated(dev)
+        y = forward()
+        held = torch.cuda.memory_allocated(dev) - before
+        del y
+        start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        for _ in range(reps):
+            update()
+        stop.record()
+        torch.cuda.synchronize()
+        us = start.elapsed_time(stop) / reps * 1e3
+        for p in params:
+            p.grad = torch.zeros_like(p)
+        optimizer.step()
+        torch.cuda.synchronize()
+        start.record()
+        for _ in range(reps):
+            optimizer.step()
+        stop.record()
+        torch.cuda.synchronize()
+        step_us = start.elapsed_time(stop) / reps * 1e3
+        flops = n_blocks * 12.0 * tokens * 2048 * 5632
+        line = {"workload": f"{n_blocks} norm + feed-forward blocks 2048 x 5632, {tokens} tokens, {name}", "us_per_update": round(us, 1), "tflops": round(flops / us / 1e6, 1),
+                "us_of_optimizer": round(step_us, 1), "bytes_held_for_backward": int(held)}
+        print(json.dumps(line), flush=True)
+        lines.append(line)
+        del blocks, sampler, forward, update, optimizer, params
+    return lines
+
+
 def main(argv=None) -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("which", nargs="*", default=["gpt2", "stress"])
@@ -457,6 +539,8 @@ def main(argv=None) -> None:
             run_overhead(max(1, args.reps // 4), dev, args.blocks)
         elif w == "ffn":
             run_ffn(args.reps, dev, min(args.blocks, 4))
+        elif w == "block":
+            run_block(args.reps, dev, min(args.blocks, 4))
         elif w == "module":
             run_module(args.reps, dev, args.blocks)
         elif w == "issue":
