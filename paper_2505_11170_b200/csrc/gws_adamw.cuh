@@ -221,16 +221,23 @@ __device__ __forceinline__ void adamw_decode_r(uint2 c, float unit, F2 (&r)[4]) 
   for (int i = 0; i < 4; ++i) r[i] = mul2(two(x[2 * i], x[2 * i + 1]), both(unit));
 }
 
+constexpr uint32_t kAdamwSlot = 2048u;               // bytes of a group with 8-bit moments: gradient, parameter, rest, codes
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+
 struct AdamwScalars {
   float scale, alpha, rho, decay;
   bool exact;                     // eps, alpha and rho are of sizes at which root2 and quotient2 are exact
 };
 
 // Groups first + warp, first + warp + 8, ... of a tensor, `count` of them over the warps.  Addresses are the block's, plus 32 bits a lane.
-template <int FMT, bool F32, bool WIDE>
+template <int FMT, bool LOOSE, bool F32, bool WIDE>
 __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e, const AdamwScalars& k, int64_t first, uint32_t count, uint4* turn) {
-  // With 8-bit moments a group is 3.6 KB and long arithmetic: the next one's loads are under way meanwhile.
-  constexpr bool kAhead = FMT == GWS_ADAMW_8BIT && !F32;
+  // With 8-bit moments a group is 2 KB and long arithmetic: the next one is under way meanwhile, to shared memory, which leaves the registers to more warps.
+  constexpr bool kStaged = FMT == GWS_ADAMW_8BIT && !F32 && WIDE, kAhead = FMT == GWS_ADAMW_8BIT && !F32 && !WIDE && LOOSE;
   constexpr uint32_t kSize = F32 ? 4u : 2u;
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   const bool keeps = !F32 && a.rest != nullptr;
@@ -267,11 +274,43 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
     adamw_fetch<F32, WIDE>(at_p + u * (kAdamwGroup * kSize), left0 - u * kAdamwGroup, lane, r.p);
   };
   uint32_t u = warp;
+  uint32_t slot = 0;
+  float next_um = 0.0f, next_ur = 0.0f;
+  auto stage = [&](uint32_t u, uint32_t slot) {
+    const uint32_t s = u * kAdamwGroup + lane * 8u, to = static_cast<uint32_t>(__cvta_generic_to_shared(turn)) + slot * kAdamwSlot + lane * 16u;
+    copy_async<16>(to, at_g + s * 2u);
+    copy_async<16>(to + 512u, at_p + s * 2u);
+    if (keeps) copy_async<16>(to + 1024u, at_rest + s * 2u);
+    copy_async<8>(to - lane * 8u + 1536u, at_m + s);
+    copy_async<8>(to - lane * 8u + 1792u, at_v + s);
+    next_um = at_um[u];
+    next_ur = at_ur[u];
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (kStaged && u < count) stage(u, 0);
   if (kAhead && u < count) fetch(u, next);
 #pragma unroll 1
   for (; u < count; u += 8) {
     Raw raw;
-    if (kAhead) {
+    if constexpr (kStaged) {
+      raw.um = next_um;
+      raw.ur = next_ur;
+      if (u + 8u < count) {
+        stage(u + 8u, slot ^ 1u);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+      } else {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+      }
+      const uint4* from = turn + slot * (kAdamwSlot / 16u) + lane;                          // what this lane copied
+      slot ^= 1u;
+      const uint4 g = from[0], p = from[32];
+      raw.g.x[0] = g.x; raw.g.x[1] = g.y; raw.g.x[2] = g.z; raw.g.x[3] = g.w;
+      raw.p.x[0] = p.x; raw.p.x[1] = p.y; raw.p.x[2] = p.z; raw.p.x[3] = p.w;
+      raw.low = keeps ? from[64] : make_uint4(0u, 0u, 0u, 0u);
+      const uint2* codes = reinterpret_cast<const uint2*>(from - lane + 96) + lane;
+      raw.cm = codes[0];
+      raw.cr = codes[32];
+    } else if constexpr (kAhead) {
       raw = next;
       if (u + 8u < count) fetch(u + 8u, next);
     } else {
@@ -393,10 +432,12 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
 }
 
 // Memory-bound.  A warp takes a group, a lane eight elements of it; a block finds its tensor by bisection in the kernel parameters.
-template <int FMT, int CAP>
-__global__ void __launch_bounds__(256, FMT == GWS_ADAMW_8BIT ? 3 : 4) k_adamw(const __grid_constant__ AdamwBatch<CAP> b) {
+// LOOSE: some tensors of the launch are not on boundaries of eight elements.  Groups of those take twice the loads and the registers to have the next ones under way:
+// three blocks an SM, where five of the others fit (8-bit moments, 184.5 M BF16 weights: 498 us with five, 580 with three; 16.8 M unaligned: 68, 61).
+template <int FMT, bool LOOSE, int CAP>
+__global__ void __launch_bounds__(256, FMT == GWS_ADAMW_F32 ? 4 : LOOSE ? 3 : 5) k_adamw(const __grid_constant__ AdamwBatch<CAP> b) {
   after_previous();
-  __shared__ uint4 turns[8][kAdamwGroup / 4];
+  __shared__ uint4 turns[8][FMT == GWS_ADAMW_8BIT ? 2 * kAdamwSlot / 16 : kAdamwGroup / 4];
   const AdamwArgs& a = b.a;
   int lo = 0, hi = a.n - 1;
   while (lo < hi) {
@@ -424,11 +465,11 @@ __global__ void __launch_bounds__(256, FMT == GWS_ADAMW_8BIT ? 3 : 4) k_adamw(co
   if (wide < first) wide = first;
   const uint32_t n_wide = static_cast<uint32_t>(wide - first), n_rest = static_cast<uint32_t>(end - wide);
   if (f32) {
-    adamw_run<FMT, true, true>(a, e, k, first, n_wide, turn);
-    adamw_run<FMT, true, false>(a, e, k, wide, n_rest, turn);
+    adamw_run<FMT, LOOSE, true, true>(a, e, k, first, n_wide, turn);
+    adamw_run<FMT, LOOSE, true, false>(a, e, k, wide, n_rest, turn);
   } else {
-    adamw_run<FMT, false, true>(a, e, k, first, n_wide, turn);
-    adamw_run<FMT, false, false>(a, e, k, wide, n_rest, turn);
+    adamw_run<FMT, LOOSE, false, true>(a, e, k, first, n_wide, turn);
+    adamw_run<FMT, LOOSE, false, false>(a, e, k, wide, n_rest, turn);
   }
 }
 

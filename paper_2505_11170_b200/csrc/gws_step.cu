@@ -102,7 +102,10 @@ int launch_adamw(const AdamwArgs& args, const AdamwRec* recs, int n, unsigned bl
   b.a.n = n;
   std::memcpy(b.e, recs, sizeof(AdamwRec) * static_cast<size_t>(n));
   std::memset(b.e + n, 0, sizeof(AdamwRec) * static_cast<size_t>(CAP - n));
-  return launch(format == GWS_ADAMW_8BIT ? k_adamw<GWS_ADAMW_8BIT, CAP> : k_adamw<GWS_ADAMW_F32, CAP>, blocks, 256, 0, 1, s, "AdamW kernel", b);
+  bool loose = false;
+  for (int i = 0; i < n; ++i) loose = loose || (recs[i].flags & (kAdamwWide | kAdamwF32)) == 0u;
+  auto kernel = format == GWS_ADAMW_F32 ? k_adamw<GWS_ADAMW_F32, false, CAP> : loose ? k_adamw<GWS_ADAMW_8BIT, true, CAP> : k_adamw<GWS_ADAMW_8BIT, false, CAP>;
+  return launch(kernel, blocks, 256, 0, 1, s, "AdamW kernel", b);
 }
 
 // Records of a launch: few tensors travel in 0.7 KB of kernel parameters, many in 15.
