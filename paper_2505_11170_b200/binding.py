@@ -939,12 +939,12 @@ def _linear_plan(m: int, n: int, k: int, ld_x: int, ld_w: int, ld_y: int, ld_r: 
     return d, at, nbytes
 
 
-def linear_plan(m: int, n: int, k: int, product: int, activation: int = ACT_NONE, x_format: int = SAVE_BF16, ld_x: Optional[int] = None, ld_w: Optional[int] = None,
+def linear_plan(m: int, n: int, k: int, product: str = "y", activation: int = ACT_NONE, x_format: int = SAVE_BF16, ld_x: Optional[int] = None, ld_w: Optional[int] = None,
                 ld_y: Optional[int] = None) -> ProductPlan:
-    """How product 0 (y), 1 (grad_x) or 2 (grad_w) of a linear layer is carried out."""
+    """How a product of :func:`linear_fwd` ("y") or :func:`linear_bwd` ("grad_x", "grad_w") is carried out for these sizes."""
     d = LinearDesc(m, n, k, ld_x or k, ld_w or k, ld_y or n, 0, activation, SAVE_NONE, x_format, TYPE_BF16)
     p = ProductPlan()
-    _check(load_library().gws_linear_plan(ctypes.addressof(d), product, ctypes.addressof(p)))
+    _check(load_library().gws_linear_plan(ctypes.addressof(d), ("y", "grad_x", "grad_w").index(product), ctypes.addressof(p)))
     return p
 
 
@@ -1082,11 +1082,19 @@ def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
     device = _device_of(x, weight, bias, residual)
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, layernorm_fwd, x, weight, bias, eps, residual, want_stats)
-    x, p_x, ld_x, m, n = _bf16_rows(x, "x", read_by_map=False)
+    shape = x.shape
+    if x.dtype is _BF16 and len(shape) == 2 and x.is_contiguous():        # as _bf16_rows, without its detours
+        m, n = shape
+        p_x, ld_x = x.data_ptr(), n or 1
+    else:
+        x, p_x, ld_x, m, n = _bf16_rows(x, "x", read_by_map=False)
     weight, bias, kind = _norm_weights(weight, bias, n)
     total, p_r, ld_r, p_sum = x, None, 0, None
     if residual is not None:
-        residual, p_r, ld_r, _, _ = _bf16_rows(residual, "residual", m, n, read_by_map=False)
+        if residual.dtype is _BF16 and residual.shape == shape and residual.is_contiguous():
+            p_r, ld_r = residual.data_ptr(), n or 1
+        else:
+            residual, p_r, ld_r, _, _ = _bf16_rows(residual, "residual", m, n, read_by_map=False)
         total = _dense_like(residual, m, n)
         p_sum = total.data_ptr()
     y = _dense_like(x, m, n)

@@ -552,7 +552,7 @@ int launch_linear_pre(LinearPre p, Ready& ready, int act, int save, bool wide, v
                                         : (wide ? k_linear_pre<GWS_SAVE_NONE, GWS_ACT_NONE, true> : k_linear_pre<GWS_SAVE_NONE, GWS_ACT_NONE, false>);
   const int st = launch(kernel, grid, kPreThreads, 0, clustered ? p.shares : 1, s, "linear backward, element-wise part", p, ready.prep);
   if (st != GWS_OK || p.part == nullptr) return st;
-  return launch(k_column_sums, blocks_for(p.cols, 32), 256, 0, 1, s, "join of column sums", static_cast<const float*>(p.part), p.shares, p.cols, 1u, p.db, static_cast<void*>(nullptr), p.db_f32);
+  return launch(k_column_sums, blocks_for(p.cols, 32), 32 * kSumWarps, 0, 1, s, "join of column sums", static_cast<const float*>(p.part), p.shares, p.cols, 1u, p.db, static_cast<void*>(nullptr), p.db_f32);
 }
 
 void describe(const Tile& t, int sms, gws_product_plan* p) {

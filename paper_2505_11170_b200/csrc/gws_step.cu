@@ -311,7 +311,7 @@ int gws_layernorm_bwd(const gws_norm_desc* desc, const void* grad_y, const void*
     if ((st = wide ? launch_norm_bwd<true>(a, b, s) : launch_norm_bwd<false>(a, b, s)) != GWS_OK) return st;
   }
   if (!sums) return GWS_OK;
-  return launch(k_column_sums, blocks_for(d.cols, 32) * 2u, 256, 0, 1, s, "join of column sums", static_cast<const float*>(a.part), b.blocks, d.cols, 2u, grad_weight,
+  return launch(k_column_sums, blocks_for(d.cols, 32) * 2u, 32 * kSumWarps, 0, 1, s, "join of column sums", static_cast<const float*>(a.part), b.blocks, d.cols, 2u, grad_weight,
                 grad_bias, a.f32);
 }
 

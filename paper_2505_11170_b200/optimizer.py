@@ -118,7 +118,10 @@ class GaussWSAdamW(torch.optim.Optimizer):
         else:
             self._count = kept["count"]
         if s is None:
-            self._state = None
+            if self._state is not None:                   # zeros where they are, for captured steps
+                for t in (self._state.moments, self._state.units, self._state.rest):
+                    if t is not None:
+                        t.zero_()
             return
         mine = self._prepare()
         if (s["rest"] is None) != (mine.rest is None):

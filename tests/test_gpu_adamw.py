@@ -144,6 +144,27 @@ def test_one_step_against_the_formula_in_64_bits(fmt):
         assert np.all(np.abs(np.sqrt(gv) - root) <= 1.0001 * np.maximum(2.0 ** -5 * root, 2.0 ** -15 * 1.0625 * top_r / 1.9375))
 
 
+@pytest.mark.parametrize("fmt", [gws.ADAMW_F32, gws.ADAMW_8BIT])
+@pytest.mark.parametrize("eps", [1e-8, 1e-15, 0.0])
+def test_zeros_and_sizes_far_apart(fmt, eps):
+    """Lanes that leave the fast arithmetic (a zero, tiny or huge second moment, a small eps) beside ones that do not: the same bits."""
+    n = 20000
+    twin = Twin([n, n], ["bf16", "f32"], fmt, True, seed=11)
+    for step in range(1, 4):
+        grads = twin.grads()
+        for g in grads:
+            r = torch.rand(n, generator=torch.Generator().manual_seed(step)).to(DEV)
+            g[r < 0.02] = 0.0
+            g[(r > 0.02) & (r < 0.03)] *= 1e-12
+            g[(r > 0.03) & (r < 0.04)] *= 1e17
+            g[:2048] = 0.0
+        if eps == 0.0:                                         # 0 / 0 only where nothing has moved yet: keep to what has a gradient
+            grads = [torch.where(g == 0, torch.full_like(g, 1e-6), g) for g in grads]
+        gws.adamw_step(twin.params, grads, twin.state, weight_decay=0.1, step=step, lr=1e-3, betas=(0.9, 0.95), eps=eps)
+        twin.step(grads, step, [0.1, 0.1], lr=1e-3, eps=eps)
+        twin.compare()
+
+
 def test_many_tensors_take_several_launches():
     sizes = [5 + 37 * (i % 40) for i in range(900)]
     twin = Twin(sizes, ["bf16" if i % 3 else "f32" for i in range(900)], gws.ADAMW_8BIT, True, seed=2)

@@ -134,7 +134,7 @@ def test_without_an_activation(m, n, k):
 
 @pytest.mark.parametrize("blocks,columns,form,m,n,k", TILINGS)
 def test_every_tiling(blocks, columns, form, m, n, k):
-    p = gws.linear_plan(m, n, k, 0)
+    p = gws.linear_plan(m, n, k)
     got = "cluster" if p.clustered else "whole+cut" if p.cut and p.whole else "cut" if p.cut else "whole*" if p.waves > 1 else "whole"
     assert (p.blocks, p.columns, got) == (blocks, columns, form)
     x, w, b, r, _ = problem(m, n, k)

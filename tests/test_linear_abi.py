@@ -31,7 +31,7 @@ def test_sizes_and_kinds(lib):
     plan = binding.ProductPlan()
     assert lib.gws_linear_plan(ctypes.byref(desc()), 3, ctypes.byref(plan)) == binding.ERR_UNSUPPORTED
     assert lib.gws_linear_plan(ctypes.byref(desc()), 0, None) == binding.ERR_NULL
-    for product in range(3):
+    for product in ("y", "grad_x", "grad_w"):
         p = gws.linear_plan(M, N, K, product)
         assert p.whole + p.cut > 0
 
