@@ -242,7 +242,7 @@ int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStr
   const uint32_t work = args.whole + args.cut * args.splits, slots = static_cast<uint32_t>(sms / CG);
   const int st = launch(k_tc<CG, BN, MODE>, args.clustered ? work : std::min(work, slots) * CG, S::kThreads, S::kSmemBytes,
                         args.clustered ? args.splits : CG, s, "block GEMM", maps[0], maps[1], maps[2], maps[3], args);
-  if constexpr (MODE == kGatedFew) return st;
+  if constexpr (MODE == kGatedFew || MODE == kLinearFew) return st;
   if (st != GWS_OK || args.cut == 0 || args.clustered) return st;
   constexpr uint32_t kWarps = (MODE == kGated ? BN / 64 : BN / 32) * (128 * CG / kJoinRows);       // per tile
   return launch(k_join<CG, BN, MODE>, args.cut * (kWarps / 8), 256, 0, 1, s, "join of a cut contraction", args);
@@ -394,11 +394,11 @@ struct ForwardPlan {
   Tile tile;
   bool move_x, move_w;
 };
-// kGatedFew: bytes of a copy of 64 elements along the contraction, and the stages that fit; the products read 128 rows of A from where the
-// last copy begins.
-uint32_t few_half(int64_t rows, uint32_t width) { return a_box(rows) * kTcHalf * 2u + width * kTcHalf * 4u; }
-uint32_t few_stages(int64_t rows, uint32_t width) {
-  const uint32_t half = few_half(rows, width), ring = TcShape<1, 128, kGatedFew>::kRing;
+// kGatedFew, kLinearFew: bytes of a copy of 64 elements along the contraction (`operands`: weights that a tile reads `width` rows of), and the stages that fit; the products read
+// 128 rows of A from where the last copy begins.
+uint32_t few_half(int64_t rows, uint32_t width, uint32_t operands) { return a_box(rows) * kTcHalf * 2u + width * kTcHalf * 2u * operands; }
+uint32_t few_stages(int64_t rows, uint32_t width, uint32_t operands) {
+  const uint32_t half = few_half(rows, width, operands), ring = TcShape<1, 128, kGatedFew>::kRing;
   return std::min({8u, ring / (2u * half), (ring + half - kTcABytes) / (2u * half)});
 }
 // The width of tile with the least estimated time, for up to 128 tokens.  A stage of 128 steps costs 620 cycles however narrow the tile (eight
@@ -407,14 +407,14 @@ uint32_t few_stages(int64_t rows, uint32_t width) {
 // choose): one token, 2048 x 5632, 40 columns 12.0 (13.1), 48 11.9, 64 12.3, 32 in two waves 16.1; 128 tokens 13.2 (13.5); one token, 4096 x 11008,
 // 40 columns 33 (42), 48 40.3, 64 42.5.  A long contraction into few columns is better cut: 5632 x 2048, 16 columns 18.1 (16.5).
 // Checkpoints want whole groups of 32: 64 columns 13.1 (13.7), 32 16.9.
-Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, int sms) {
+Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, uint32_t operands, int sms) {
   const int64_t kb = stages_of(len, 128);
   const uint32_t slots = static_cast<uint32_t>(sms);
   Tile best{};
-  for (uint32_t width = 64; width >= std::max(unit, 16u); width -= unit) {
+  for (uint32_t width = 128 / operands; width >= std::max(unit, 16u); width -= unit) {
     const uint32_t tiles = (static_cast<uint32_t>(cols) + width - 1) / width, rest = tiles % slots;
-    const double stage = std::max(620.0, 2.0 * few_half(rows, width) / 67.0), epilogue = 20.0 * width + 400.0;
-    auto wave = [&](uint32_t n) { return std::max({static_cast<double>(kb) * stage, epilogue, n * width * 4.0 * len / 3400.0}) + 100.0; };
+    const double stage = std::max(620.0, 2.0 * few_half(rows, width, operands) / 67.0), epilogue = 10.0 * operands * width + 400.0;
+    auto wave = [&](uint32_t n) { return std::max({static_cast<double>(kb) * stage, epilogue, n * width * 2.0 * operands * len / 3400.0}) + 100.0; };
     const double cost = 3300.0 + epilogue + static_cast<double>(tiles / slots) * wave(slots) + (rest != 0 ? wave(rest) : 0.0);
     if (best.cg == 0 || cost < best.cost)
       best = {1, 128, 1, tiles, tiles, 0, 1, static_cast<uint32_t>(kb), false, cost, width};
@@ -425,8 +425,8 @@ Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, int sms)
 ForwardPlan weigh_forward(const gws_gated_desc* d, int sms) {
   ForwardPlan f{choose(kGated, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
   if (d->m <= 128) {
-    const Tile few = choose_few(d->m, d->n, d->k, 8, sms);
-    if (few.cost < f.tile.cost) f.tile = is_act8(d->save_format) ? choose_few(d->m, d->n, d->k, 32, sms) : few;     // h does not depend on what is kept
+    const Tile few = choose_few(d->m, d->n, d->k, 8, 2, sms);
+    if (few.cost < f.tile.cost) f.tile = is_act8(d->save_format) ? choose_few(d->m, d->n, d->k, 32, 2, sms) : few;     // h does not depend on what is kept
   }
   if (!f.move_x && !f.move_w && d->m > 1 && d->n > 1 && d->ld_x % 16 != 0 && d->ld_w % 16 != 0) {
     const double smaller = static_cast<double>(d->k) * std::min(d->m, 2 * d->n);
@@ -479,6 +479,10 @@ int64_t bias_bytes(const gws_linear_desc& d) { return d.n * (d.bias_type == GWS_
 // Forward: tile, and which operands are copied into the workspace; rows in the middle of a sector as in weigh_forward.
 ForwardPlan weigh_linear(const gws_linear_desc* d, int sms) {
   ForwardPlan f{choose(kLinear, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
+  if (d->m <= 128) {                             // widths are multiples of 16 (a product's columns), or of 32 (whole groups of a checkpoint)
+    const Tile few = choose_few(d->m, d->n, d->k, 16, 1, sms);
+    if (few.cost < f.tile.cost) f.tile = is_act8(d->save_format) ? choose_few(d->m, d->n, d->k, 32, 1, sms) : few;     // y does not depend on what is kept
+  }
   if (!f.move_x && !f.move_w && d->m > 1 && d->n > 1 && d->ld_x % 16 != 0 && d->ld_w % 16 != 0) {
     const double smaller = static_cast<double>(d->k) * std::min(d->m, d->n);
     if (0.25 * f.tile.cost > 4500.0 + smaller * 4.0 / 3400.0) (d->m <= d->n ? f.move_x : f.move_w) = true;
@@ -486,7 +490,7 @@ ForwardPlan weigh_linear(const gws_linear_desc* d, int sms) {
   return f;
 }
 const ForwardPlan& plan_linear(const gws_linear_desc* d, int sms) {
-  return remembered<ForwardPlan>({d->m, d->n, d->k, d->ld_x, d->ld_w, sms}, [&] { return weigh_linear(d, sms); });
+  return remembered<ForwardPlan>({d->m, d->n, d->k, d->ld_x, d->ld_w, is_act8(d->save_format), sms}, [&] { return weigh_linear(d, sms); });
 }
 int64_t linear_copies(const gws_linear_desc* d, const ForwardPlan& f) {
   return (f.move_x ? packed_bytes(d->m, d->k) : 0) + (f.move_w ? packed_bytes(d->n, d->k) : 0);
@@ -745,8 +749,8 @@ int gws_gated_fwd(const gws_gated_desc* desc, const void* x, const void* w_gate,
   if (t.width != 0) {
     args.width = width;
     args.a_bytes = a_box(d.m) * kTcHalf * 2u;
-    args.stages = few_stages(d.m, width);
-    args.half_bytes = few_half(d.m, width);
+    args.stages = few_stages(d.m, width, 2);
+    args.half_bytes = few_half(d.m, width, 2);
     if (width % 16 != 0) args.wide = std::min(args.wide, 8), args.save_wide = std::min(args.save_wide, 8);
   }
   CUtensorMap maps[4];
@@ -866,6 +870,7 @@ int gws_linear_plan(const gws_linear_desc* desc, int product, gws_product_plan* 
   if (product == 0) {
     const ForwardPlan& f = plan_linear(desc, sms);
     describe(f.tile, sms, plan);
+    if (f.tile.width != 0) plan->columns = plan->narrow;
     plan->moves_x = f.move_x;
     plan->moves_w = f.move_w;
   } else {
@@ -924,12 +929,18 @@ int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, co
     args.save16[0] = static_cast<uint16_t*>(save);
     args.save_wide = widest(d.n, save, nullptr);
   }
+  if (t.width != 0) {
+    args.width = t.width;
+    args.a_bytes = a_box(d.m) * kTcHalf * 2u;
+    args.stages = few_stages(d.m, t.width, 1);
+    args.half_bytes = few_half(d.m, t.width, 1);
+  }
   CUtensorMap maps[4];
   if ((st = make_map(maps[0], mx.p, d.m, d.k, mx.ld, a_box(d.m))) != GWS_OK) return st;
   maps[1] = maps[0];
-  if ((st = make_map(maps[2], mw.p, d.n, d.k, mw.ld, static_cast<uint32_t>(t.bn / t.cg))) != GWS_OK) return st;
+  if ((st = make_map(maps[2], mw.p, d.n, d.k, mw.ld, t.width != 0 ? t.width : static_cast<uint32_t>(t.bn / t.cg))) != GWS_OK) return st;
   maps[3] = maps[2];
-  return launch_mode<kLinear>(t, maps, args, sms, s);
+  return t.width != 0 ? launch_tc<1, 128, kLinearFew>(maps, args, sms, s) : launch_mode<kLinear>(t, maps, args, sms, s);
 }
 
 int gws_linear_bwd(const gws_linear_desc* desc, const void* grad_y, const void* x, const void* w, const void* save, void* grad_x, void* grad_w, void* grad_bias,

@@ -6,7 +6,7 @@
 //   kGatedFew  the same for up to 128 tokens, tiles of 16 to 64 columns of h: every SM gets its share of the weights, and a copy of A
 //            takes only the rows that exist, so that the ring holds more weights in flight.  It is bound by the weights' way from
 //            memory and some 4 us around it (one token, 2048 x 5632: 46 MB in 12 us, 10 from L2; 4096 x 11008: 180 MB in 33 us)
-//   kLinear  y = act(x W^T + b) + r: bias, activation, residual and the copies of z = x W^T + b for the backward pass on registers in the epilogue
+//   kLinear, kLinearFew  y = act(x W^T + b) + r: bias, activation, residual and the copies of z = x W^T + b for the backward pass on registers in the epilogue
 //   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du; dx = dz W is its first half
 //   kDw      dW = dY^T X: both operands are read along their contiguous (not the contracted) axis, as they lie in memory
 //   kDw8     the same with X an 8-bit checkpoint: its codes are copied to shared memory and eight more warps turn them into the BF16
@@ -48,7 +48,7 @@
 
 namespace {
 
-enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4, kLinear = 5 };
+enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4, kLinear = 5, kLinearFew = 6 };
 
 constexpr uint32_t kTcHalf = 64;                           // elements along the contraction per copy: 128 bytes, one swizzle atom
 constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
@@ -81,7 +81,7 @@ struct TcArgs {
   int32_t bias_f32, residual_wide;        // residual_wide: elements a load from `residual` may take, as `wide`
   const uint16_t* residual;               // null, or BF16 [rows, ld_residual]
   int64_t ld_residual;
-  uint32_t width, stages, a_bytes;        // kGatedFew: columns of h in a tile, stages of the ring, bytes of A in a copy
+  uint32_t width, stages, a_bytes;        // kGatedFew, kLinearFew: columns of h or y in a tile, stages of the ring, bytes of A in a copy
   int32_t save_wide;                      // the same for the BF16 copies
   Act8View save8[2];                      // kLinear: the first of both
   uint16_t* save16[2];                    // BF16 copies, [rows, cols]
@@ -398,9 +398,20 @@ __device__ __forceinline__ float bias_at(const TcArgs& p, int64_t col) {
 }
 
 // The same of four columns of a row, from sums without the bias; eight neighbouring lanes hold a group of 32 columns.  Writes the copy of z, leaves y in v.
-__device__ __forceinline__ void finish_four(const TcArgs& p, int64_t row, int64_t col, uint32_t lane, float (&v)[4]) {
+__device__ __forceinline__ uint2 residual_four(const TcArgs& p, int64_t row, int64_t col) {
+  uint2 r = make_uint2(0u, 0u);
+  if (p.residual == nullptr) return r;
+  const uint16_t* from = p.residual + row * p.ld_residual + col;
+  if (p.residual_wide >= 4 && col + 4 <= p.cols) return *reinterpret_cast<const uint2*>(from);
+  if (col < p.cols) r.x = from[0];
+  if (col + 1 < p.cols) r.x |= static_cast<uint32_t>(from[1]) << 16;
+  if (col + 2 < p.cols) r.y = from[2];
+  if (col + 3 < p.cols) r.y |= static_cast<uint32_t>(from[3]) << 16;
+  return r;
+}
+__device__ __forceinline__ void finish_four(const TcArgs& p, int64_t row, int64_t col, uint32_t lane, const float (&bias)[4], uint2 residual, float (&v)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] += bias_at(p, col + i);
+  for (int i = 0; i < 4; ++i) v[i] += bias[i];
   if (p.save == GWS_SAVE_BF16) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -420,11 +431,9 @@ __device__ __forceinline__ void finish_four(const TcArgs& p, int64_t row, int64_
       if ((lane & 7u) == 0u) o.scales[row * (o.ld >> 5) + (col >> 5)] = static_cast<uint8_t>(byte);
     }
   }
+  const uint32_t r[2] = {residual.x, residual.y};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = act_of_kind(p.activation, v[i]);
-    if (p.residual != nullptr && col + i < p.cols) v[i] += __uint_as_float(static_cast<uint32_t>(p.residual[row * p.ld_residual + col + i]) << 16);
-  }
+  for (int i = 0; i < 4; ++i) v[i] = act_of_kind(p.activation, v[i]) + ((i & 1) == 0 ? bf16_lo(r[i / 2]) : bf16_hi(r[i / 2]));
 }
 
 template <int ACT>
@@ -459,8 +468,8 @@ struct TcShape {
   static constexpr uint32_t kHalf = kTcABytes + kBBytes + kRaw;            // A, B, codes
   static constexpr uint32_t kStage = kHalves * kHalf;
   static constexpr uint32_t kFit = (kTcSmem - 4096u - kStaging) / kStage;
-  // kGatedFew parts the same memory into as many stages as its narrower copies allow
-  static constexpr uint32_t kStages = kFit > 8u || MODE == kGatedFew ? 8u : kFit;
+  // kGatedFew and kLinearFew part the same memory into as many stages as its narrower copies allow
+  static constexpr uint32_t kStages = kFit > 8u || MODE == kGatedFew || MODE == kLinearFew ? 8u : kFit;
   static constexpr uint32_t kRing = (kFit > 8u ? 8u : kFit) * kStage;
   static constexpr uint32_t kSmemBytes = kRing + kStaging + 1024u;
   static constexpr uint32_t kTmemCols = 2 * BN;
@@ -524,14 +533,15 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
          const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
   using S = TcShape<CG, BN, MODE>;
-  constexpr bool kFew = MODE == kGatedFew, kIsGated = MODE == kGated || kFew, kIsLinear = MODE == kLinear, kIsDw = MODE == kDw || MODE == kDw8;
+  constexpr bool kFew = MODE == kGatedFew || MODE == kLinearFew, kIsGated = MODE == kGated || MODE == kGatedFew, kIsLinear = MODE == kLinear || MODE == kLinearFew;
+  constexpr bool kIsDw = MODE == kDw || MODE == kDw8;
   constexpr bool kMnA = kIsDw, kMnB = !kIsGated && !kIsLinear;
   constexpr uint32_t kStages = S::kStages;
-  const uint32_t stages = kFew ? p.stages : kStages, width = kFew ? p.width : BN / 2;      // width: columns of h in a tile (kIsGated)
-  const uint32_t a_bytes = kFew ? p.a_bytes : kTcABytes, half_pitch = kFew ? a_bytes + width * (kTcHalf * 4u) : S::kHalf, stage_pitch = S::kHalves * half_pitch;
+  const uint32_t stages = kFew ? p.stages : kStages, width = kFew ? p.width : kIsLinear ? BN : BN / 2;      // width: columns of h or y in a tile (kIsGated, kIsLinear)
+  const uint32_t a_bytes = kFew ? p.a_bytes : kTcABytes, half_pitch = kFew ? a_bytes + width * (kTcHalf * (kIsGated ? 4u : 2u)) : S::kHalf, stage_pitch = S::kHalves * half_pitch;
   // instruction descriptor: FP32 accumulator, BF16 operands, which axis of A and B is contiguous, N, M
   const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((kMnA ? 1u : 0u) << 15) | ((kMnB ? 1u : 0u) << 16) |
-                         ((kFew ? width >> 2 : static_cast<uint32_t>(BN >> 3)) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
+                         ((kFew ? width >> (kIsGated ? 2 : 3) : static_cast<uint32_t>(BN >> 3)) << 17) | (static_cast<uint32_t>((128 * CG) >> 4) << 24);
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], meet[4], codes_full[kStages], converted[kStages];
   __shared__ __align__(16) uint8_t scale_bytes[2][2][kIsGated || kIsLinear ? 128 : 1][4];      // of two tiles, gate and up projection (left and right half)
@@ -602,7 +612,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       place(t, mt, nt, k0, k1);
       const bool second = kIsDw && mt >= p.tiles_per_out;
       const int32_t m0 = static_cast<int32_t>((second ? mt - p.tiles_per_out : mt) * (128u * CG) + rank * 128u);
-      const int32_t n0 = static_cast<int32_t>(nt * (kIsGated ? width : BN) + (kIsGated ? 0u : rank * S::kBRows));
+      const int32_t n0 = static_cast<int32_t>(nt * (kIsGated || kIsLinear ? width : BN) + (kIsGated ? 0u : rank * S::kBRows));
       for (uint32_t kb = k0; kb < k1; ++kb) {
         if (!bar_wait(empty0 + 8u * s, parity, p.wait_limit)) { ok = false; break; }
         const bool seg = MODE == kDx && kb >= p.kb_first;
@@ -713,7 +723,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       const uint32_t buf = n & 1u;
       if (kIsLinear) {                   // under the products
 #pragma unroll
-        for (uint32_t i = 0; i < BN / 64; ++i) bias_of[warp - 4u][i * 32u + lane] = bias_at(p, static_cast<int64_t>(nt) * BN + (half + 2u * i) * 32u + lane);
+        for (uint32_t i = 0; i < BN / 64; ++i) bias_of[warp - 4u][i * 32u + lane] = bias_at(p, static_cast<int64_t>(nt) * width + (half + 2u * i) * 32u + lane);
         __syncwarp();
       }
       if (!bar_wait(smem_addr(&acc_full[buf]), (n >> 1) & 1u, p.wait_limit)) {
@@ -750,14 +760,15 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           }
         }
       } else if (kIsLinear) {
+        const int64_t edge = kFew ? min(p.cols, static_cast<int64_t>(nt + 1u) * width) : p.cols;      // where the tile's columns end
 #pragma unroll 1
-        for (uint32_t c = half; c < BN / 32; c += S::kEpilogueWarps / 4u) {
-          const int64_t col0 = static_cast<int64_t>(nt) * BN + c * 32u;
-          if (col0 >= p.cols) break;
+        for (uint32_t c = half; c < (width + 31u) / 32u; c += S::kEpilogueWarps / 4u) {
+          const int64_t col0 = static_cast<int64_t>(nt) * width + c * 32u;
+          if (col0 >= edge) break;
           uint32_t v[32], r[16], w[16];
           acc_load(acc + c * 32u, v);
           if (p.residual != nullptr) {
-            load_block(p.residual, p.ld_residual, p.residual_wide, row0, col0, p.rows, p.cols, r, stage, lane);
+            load_block(p.residual, p.ld_residual, p.residual_wide, row0, col0, p.rows, edge, r, stage, lane);
           } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) r[e] = 0u;
@@ -776,17 +787,18 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           else if (p.activation == GWS_GATED_SILU) finish_block<GWS_GATED_SILU>(z, r, w);
           else if (p.activation == GWS_GATED_GELU_TANH) finish_block<GWS_GATED_GELU_TANH>(z, r, w);
           else finish_block<GWS_GATED_RELU>(z, r, w);
-          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
+          store_block(static_cast<uint16_t*>(p.out[0]), p.ld_out, p.wide, row0, col0, p.rows, edge, w, stage, lane);
           if (p.save == GWS_SAVE_BF16) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(z[2 * e], z[2 * e + 1]);
-            store_block(p.save16[0], p.cols, p.save_wide, row0, col0, p.rows, p.cols, w, stage, lane);
+            store_block(p.save16[0], p.cols, p.save_wide, row0, col0, p.rows, edge, w, stage, lane);
           } else if (p.save != GWS_SAVE_NONE && row0 + lane < p.rows) {
             // columns past the width are products with rows of zeros and have no bias: zero codes, as the layout wants them
             V8 codes;
             const uint32_t byte = p.save == GWS_ACT8_INT8 ? encode_group<GWS_ACT8_INT8>(z, codes) : encode_group<GWS_ACT8_E4M3>(z, codes);
             st32(p.save8[0].codes + (row0 + lane) * p.save8[0].ld + col0, codes);
-            scale_bytes[buf][c / (BN / 64)][quadrant * 32u + lane][c % (BN / 64)] = static_cast<uint8_t>(byte);
+            if (kFew) p.save8[0].scales[(row0 + lane) * (p.save8[0].ld >> 5) + (col0 >> 5)] = static_cast<uint8_t>(byte);       // of few rows
+            else scale_bytes[buf][c / (BN / 64)][quadrant * 32u + lane][c % (BN / 64)] = static_cast<uint8_t>(byte);
           }
         }
       } else if (kIsGated) {
@@ -839,7 +851,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           store_block(out, p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
         }
       }
-      if ((kIsGated || kIsLinear) && t < p.whole && (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3)) {
+      if ((kIsGated || MODE == kLinear) && t < p.whole && (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3)) {
         // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
         // The two warps that share these rows meet; one writes the gate's (or the left half's), the other the up projection's (the right half's).  A warp that fills the same
         // buffer again has passed the meeting of the tile between, and so has the other one's store.  They meet at an mbarrier, one
@@ -848,7 +860,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         if (lane == 0) bar_arrive(smem_addr(&meet[quadrant]));
         if (!bar_wait(smem_addr(&meet[quadrant]), n & 1u, p.wait_limit)) { failed = 1; break; }
         const Act8View& kept = p.save8[kIsLinear ? 0u : half];
-        const uint32_t groups = width / 32u;
+        const uint32_t groups = kIsLinear ? width / 64u : width / 32u;
         const int64_t row = row0 + lane, ld = kept.ld >> 5, g0 = kIsLinear ? (static_cast<int64_t>(nt) * 2 + half) * groups : static_cast<int64_t>(nt) * groups;
         if (row < p.rows) {
           uint8_t* to = kept.scales + row * ld + g0;
@@ -919,6 +931,13 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
   if (CG == 1 && !kIsGated && p.clustered) {
     // Every block of the cluster adds its share of the tile's rows, the parts in the order of the contraction; a warp takes a row, a
     // lane four columns.
+    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (kIsLinear) {
+      uint32_t mt, nt, k0, k1;
+      place(first, mt, nt, k0, k1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bias[i] = bias_at(p, static_cast<int64_t>(nt) * BN + lane * 4u + i);
+    }
     __syncthreads();
     pair_sync();
     const uint32_t per = (128u + p.splits - 1u) / p.splits, r1 = min(128u, (block_rank() + 1u) * per);
@@ -930,6 +949,8 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     for (uint32_t r = block_rank() * per + warp; r < r1 && row0 + r < p.rows; r += S::kThreads / 32u) {
       const uint32_t at = smem_addr(smem) + r * kPartRow + lane * 16u;
       float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      uint2 residual = make_uint2(0u, 0u);
+      if (kIsLinear) residual = residual_four(p, row0 + r, col);
 #pragma unroll 4
       for (uint32_t k = 0; k < p.splits; ++k) {
         float q[4];
@@ -938,7 +959,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
         for (int i = 0; i < 4; ++i) v[i] = k == 0 ? q[i] : v[i] + q[i];
       }
       uint16_t* to = out + (row0 + r) * p.ld_out + col;
-      if (kIsLinear) finish_four(p, row0 + r, col, lane, v);
+      if (kIsLinear) finish_four(p, row0 + r, col, lane, bias, residual, v);
       const uint32_t lo = pack_bf16(v[0], v[1]), hi = pack_bf16(v[2], v[3]);
       if (p.wide >= 4 && col + 4 <= p.cols) {
         *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
@@ -989,7 +1010,12 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
   if (col0 >= p.cols || row0 >= p.rows) return;
   const float* part = p.part + static_cast<int64_t>(tile) * (128 * CG * BN) + r0 * BN + c * 32u + lane;
   const int64_t stride = static_cast<int64_t>(p.cut) * (128 * CG * BN);
-  float a[kJoinRows], b[kJoinRows];
+  float a[kJoinRows], b[kJoinRows], beside[kJoinRows];
+  const float bias = MODE == kLinear ? bias_at(p, col) : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kJoinRows; ++i)
+    beside[i] = MODE == kLinear && p.residual != nullptr && col < p.cols && row0 + i < p.rows
+                    ? __uint_as_float(static_cast<uint32_t>(p.residual[(row0 + i) * p.ld_residual + col]) << 16) : 0.0f;
 #pragma unroll
   for (int i = 0; i < kJoinRows; ++i) {
     a[i] = part[i * BN];
@@ -1010,9 +1036,8 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ TcArgs p) 
     if (row >= p.rows) break;
     float v = a[i];
     if (MODE == kLinear) {
-      a[i] += bias_at(p, col);
-      v = act_of_kind(p.activation, a[i]);
-      if (p.residual != nullptr && col < p.cols) v += __uint_as_float(static_cast<uint32_t>(p.residual[row * p.ld_residual + col]) << 16);
+      a[i] += bias;
+      v = act_of_kind(p.activation, a[i]) + beside[i];
     }
     if (MODE == kGated) {
       const float act = p.activation == GWS_GATED_SILU ? act_of<GWS_GATED_SILU>(a[i])

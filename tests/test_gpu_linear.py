@@ -13,11 +13,12 @@ ACTS = [gws.ACT_NONE, gws.GATED_SILU, gws.GATED_GELU_TANH, gws.GATED_RELU]
 # (m, n, k): one token to many, widths that are and are not multiples of the tiles, of 32, of 8; all odd
 SHAPES = [(1, 64, 64), (1, 5632, 256), (3, 8, 8), (33, 96, 40), (128, 128, 128), (129, 130, 72), (200, 1365, 512), (257, 2048, 96), (300, 33, 31), (640, 1000, 333), (1, 1, 1),
           (2048, 256, 768), (1500, 2730, 64), (65, 768, 2730)]
-# every way of tiling the forward product: (blocks, columns, form, m, n, k)
-TILINGS = [(1, 128, "cut", 1, 10, 4009), (1, 128, "cut", 70, 330, 9000), (1, 128, "cluster", 1, 8, 275), (1, 128, "cluster", 40, 130, 1500), (1, 128, "whole", 1, 9, 10),
-           (1, 128, "whole*", 796, 2930, 8), (2, 128, "cut", 906, 9, 5304), (2, 128, "whole+cut", 3002, 864, 3835), (2, 128, "whole", 44, 12, 385), (2, 128, "whole*", 3955, 534, 294),
-           (2, 256, "whole+cut", 1839, 2476, 1938), (2, 256, "whole", 2650, 920, 445), (2, 256, "whole*", 4230, 6137, 20)]
-
+# every way of tiling the forward product: (blocks, columns, form, m, n, k); narrow tiles of 16 to 128 columns, in one wave and in several
+TILINGS = [(1, 48, "narrow", 1, 5632, 2048), (1, 16, "narrow", 33, 2050, 768), (1, 48, "narrow", 72, 5858, 1807), (1, 80, "narrow", 128, 11008, 264), (1, 16, "narrow", 3, 40, 72),
+           (1, 128, "cut", 1, 10, 4009), (1, 128, "cut", 70, 330, 9000), (1, 128, "cluster", 314, 859, 2745), (1, 128, "cluster", 1, 8, 700), (1, 128, "cluster", 40, 130, 1500),
+           (2, 128, "whole", 224, 220, 1139), (1, 128, "whole", 268, 5533, 383), (1, 128, "whole*", 796, 2930, 8), (2, 128, "cut", 477, 701, 5986), (2, 128, "whole+cut", 3002, 864, 3835),
+           (1, 128, "whole", 213, 532, 102), (2, 128, "whole*", 3955, 534, 294), (2, 256, "cut", 267, 1686, 9306), (2, 256, "whole+cut", 1112, 3767, 1200), (2, 256, "whole", 2650, 920, 445),
+           (2, 256, "whole*", 783, 7541, 340)]
 
 def rand(shape, seed, std=1.0, dtype=torch.bfloat16):
     g = torch.Generator().manual_seed(seed)
@@ -135,7 +136,7 @@ def test_without_an_activation(m, n, k):
 @pytest.mark.parametrize("blocks,columns,form,m,n,k", TILINGS)
 def test_every_tiling(blocks, columns, form, m, n, k):
     p = gws.linear_plan(m, n, k)
-    got = "cluster" if p.clustered else "whole+cut" if p.cut and p.whole else "cut" if p.cut else "whole*" if p.waves > 1 else "whole"
+    got = "narrow" if p.narrow else "cluster" if p.clustered else "whole+cut" if p.cut and p.whole else "cut" if p.cut else "whole*" if p.waves > 1 else "whole"
     assert (p.blocks, p.columns, got) == (blocks, columns, form)
     x, w, b, r, _ = problem(m, n, k)
     for save in (gws.ACT8_INT8, gws.ACT8_E4M3, gws.SAVE_BF16):
