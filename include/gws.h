@@ -707,8 +707,9 @@ int gws_kernel_class(const gws_desc* desc);
 /* How the matrix products of the activation operators are carried out for given sizes and strides (host arithmetic; the number of SMs is
  * the current device's, 148 without one). */
 typedef struct gws_product_plan {
-  int32_t blocks, columns;         /* a tile: 128 * blocks rows (1, or 2 for a pair of SMs) by `columns` of accumulator           */
-  int32_t narrow;                  /* forward, up to 128 tokens: columns of h in a narrow tile, 0 for other tiles                */
+  int32_t blocks, columns;         /* a tile: 128 * blocks rows (1, or 2 for a pair of SMs) by `columns` of accumulator; 0 blocks:      */
+                                   /* gws_linear_fwd of up to four tokens, a warp to an output or two, `columns` of y to a thread block */
+  int32_t narrow;                  /* forward, up to 128 tokens: columns of h or y in a narrow tile, 0 for other tiles           */
   int32_t whole, cut, splits;      /* tiles computed in one piece, and tiles whose contraction is cut into `splits` parts       */
   int32_t clustered;               /* the parts of a tile are the blocks of a cluster, not joined by a second launch             */
   int32_t inside;                  /* weight gradients from a checkpoint: codes converted inside the product, not restored before */

@@ -393,6 +393,7 @@ const BackLayout& back_layout(const gws_gated_desc* d, int sms) {
 struct ForwardPlan {
   Tile tile;
   bool move_x, move_w;
+  bool rows;                               // linear layer of a few tokens: k_linear_row
 };
 // kGatedFew, kLinearFew: bytes of a copy of 64 elements along the contraction (`operands`: weights that a tile reads `width` rows of), and the stages that fit; the products read
 // 128 rows of A from where the last copy begins.
@@ -423,7 +424,7 @@ Tile choose_few(int64_t rows, int64_t cols, int64_t len, uint32_t unit, uint32_t
 }
 
 ForwardPlan weigh_forward(const gws_gated_desc* d, int sms) {
-  ForwardPlan f{choose(kGated, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
+  ForwardPlan f{choose(kGated, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w), false};
   if (d->m <= 128) {
     const Tile few = choose_few(d->m, d->n, d->k, 8, 2, sms);
     if (few.cost < f.tile.cost) f.tile = is_act8(d->save_format) ? choose_few(d->m, d->n, d->k, 32, 2, sms) : few;     // h does not depend on what is kept
@@ -476,9 +477,28 @@ int check_linear(const gws_linear_desc* d) {
 int64_t kept_bytes(int format, int64_t m, int64_t n) { return format == GWS_SAVE_NONE ? 0 : format == GWS_SAVE_BF16 ? m * n * 2 : act8_total(m, n); }
 int64_t bias_bytes(const gws_linear_desc& d) { return d.n * (d.bias_type == GWS_TYPE_F32 ? 4 : 2); }
 
+// Whether warps stream the rows of W (k_linear_row).  Each token costs them reads of x, where the narrow tiles of the tensor cores take eight for the price of one but some 4 us more
+// around them.  On the device, us, rows against tiles: one token, 2048 x 5632 6.9, 9.7; two 8.5, 9.7; four 15, 9.7; 768 x 768: one 2.0, 5.8; four 3.3, 5.9.
+bool streams_rows(const gws_linear_desc& d) {
+  return d.k % 8 == 0 && in_place(d.m, d.ld_x) && in_place(d.n, d.ld_w) && (d.m <= 2 || (d.m <= 4 && d.n * d.k <= (1 << 22)));
+}
+// Columns of y to a block of eight warps: one or two to a warp, or to up to four warps where there are few columns and long rows (one token, 5632 x 2048: 11.3 us with a warp to a row,
+// 8.5 with two).  A checkpoint's 32 columns stay within a cluster of eight blocks.
+unsigned row_columns(const gws_linear_desc& d) {
+  const unsigned most = d.m == 1 ? 8u : 16u;
+  const int64_t warps = d.m == 1 ? d.n : (d.n + 1) / 2;
+  unsigned per = most;
+  for (int64_t split = 1; per > 4u && warps * split < 32 * 148 && d.k >= 512 * split; split *= 2) per /= 2;
+  return per;
+}
 // Forward: tile, and which operands are copied into the workspace; rows in the middle of a sector as in weigh_forward.
 ForwardPlan weigh_linear(const gws_linear_desc* d, int sms) {
-  ForwardPlan f{choose(kLinear, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w)};
+  ForwardPlan f{choose(kLinear, d->m, d->n, 1, d->k, 1, sms), !in_place(d->m, d->ld_x), !in_place(d->n, d->ld_w), false};
+  f.rows = streams_rows(*d);
+  if (f.rows) {
+    f.tile.cut = 0;                              // no parts in the workspace
+    return f;
+  }
   if (d->m <= 128) {                             // widths are multiples of 16 (a product's columns), or of 32 (whole groups of a checkpoint)
     const Tile few = choose_few(d->m, d->n, d->k, 16, 1, sms);
     if (few.cost < f.tile.cost) f.tile = is_act8(d->save_format) ? choose_few(d->m, d->n, d->k, 32, 1, sms) : few;     // y does not depend on what is kept
@@ -871,6 +891,11 @@ int gws_linear_plan(const gws_linear_desc* desc, int product, gws_product_plan* 
     const ForwardPlan& f = plan_linear(desc, sms);
     describe(f.tile, sms, plan);
     if (f.tile.width != 0) plan->columns = plan->narrow;
+    if (f.rows) {
+      std::memset(plan, 0, sizeof *plan);
+      plan->columns = static_cast<int32_t>(row_columns(*desc));
+      plan->waves = 1;
+    }
     plan->moves_x = f.move_x;
     plan->moves_w = f.move_w;
   } else {
@@ -911,6 +936,33 @@ int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, co
   ready.align(mw, ws, f.move_w);
   if ((st = ready.run(s)) != GWS_OK) return st;
 
+  if (f.rows) {
+    LinearRow p;
+    std::memset(&p, 0, sizeof p);
+    p.x = static_cast<const uint16_t*>(x);
+    p.w = static_cast<const uint16_t*>(w);
+    p.residual = static_cast<const uint16_t*>(residual);
+    p.bias = bias;
+    p.y = static_cast<uint16_t*>(y);
+    p.save16 = static_cast<uint16_t*>(save);
+    if (bytes8) p.save8 = act8_view(save, d.m, d.n);
+    p.ld_x = round_up(d.ld_x, 8);                // of one token any
+    p.ld_w = d.ld_w;
+    p.ld_y = d.ld_y;
+    p.ld_residual = d.ld_residual;
+    p.cols = d.n;
+    p.octets = static_cast<uint32_t>(d.k / 8);
+    p.tokens = static_cast<int32_t>(d.m);
+    p.activation = d.activation;
+    p.save = d.save_format;
+    p.bias_f32 = d.bias_type == GWS_TYPE_F32;
+    const unsigned per = row_columns(d), cluster = bytes8 ? 32u / per : 1u;
+    const unsigned grid = static_cast<unsigned>(round_up((d.n + per - 1) / per, cluster));
+    auto kernel = d.m == 1   ? (per == 8u ? k_linear_row<1, 1, 1> : k_linear_row<1, 1, 2>)
+                  : d.m == 2 ? (per == 16u ? k_linear_row<2, 2, 1> : per == 8u ? k_linear_row<2, 2, 2> : k_linear_row<2, 2, 4>)
+                             : (per == 16u ? k_linear_row<4, 2, 1> : per == 8u ? k_linear_row<4, 2, 2> : k_linear_row<4, 2, 4>);
+    return launch(kernel, grid, 256, 0, cluster, s, "linear layer of a few tokens", p);
+  }
   const Tile& t = f.tile;
   TcArgs args = base_args(t, d.m, d.n, d.k, 1, status);
   set_out(args, y, nullptr, d.ld_y);

@@ -284,4 +284,109 @@ __global__ void __launch_bounds__(kPreThreads, 6) k_linear_pre(const __grid_cons
   if (p.shares > 1u) pair_sync();              // rank 0 has read this block's sums
 }
 
+// ---- forward pass of a few tokens ------------------------------------------------------------------------------------------------
+// y of up to four tokens without tensor cores: a warp, or SPLIT of them together, streams R rows of W, 16 bytes to a lane at a time, and multiplies them with every token's x, which stays in L1.  One token,
+// 2048 x 5632: all of W (23 MB) is under way at once, and what is left is memory and a launch.  Sums are FP32, each lane's over every 256th octet, then over the lanes.
+struct LinearRow {
+  const uint16_t *x, *w, *residual;
+  const void* bias;
+  uint16_t *y, *save16;
+  Act8View save8;
+  int64_t ld_x, ld_w, ld_y, ld_residual, cols;
+  uint32_t octets;                 // of a row
+  int32_t tokens, activation, save, bias_f32;
+};
+
+// a + b c of both numbers of two pairs, in FP32; the product of two BF16 numbers is exact.
+__device__ __forceinline__ float fma_pair(uint32_t b, uint32_t c, float a) {
+  asm("{\n\t.reg .b16 bl, bh, cl, ch;\n\tmov.b32 {bl, bh}, %1;\n\tmov.b32 {cl, ch}, %2;\n\tfma.rn.f32.bf16 %0, bl, cl, %0;\n\tfma.rn.f32.bf16 %0, bh, ch, %0;\n\t}" : "+f"(a) : "r"(b), "r"(c));
+  return a;
+}
+
+template <int M, int R, int SPLIT>
+__global__ void __launch_bounds__(256) k_linear_row(const __grid_constant__ LinearRow p) {
+  after_previous();
+  constexpr int kAhead = R == 1 ? 8 : 4;                                // octets of a lane and row under way
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  constexpr uint32_t rows = 8u / SPLIT * R, step = 32u * SPLIT;         // rows of a block; octets between two of a lane's
+  const uint32_t part = warp % SPLIT, first = warp / SPLIT * R;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows + first;
+  float sum[M][R];
+#pragma unroll
+  for (int t = 0; t < M; ++t)
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[t][r] = 0.0f;
+  const uint4* w[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) w[r] = reinterpret_cast<const uint4*>(p.w + min(row0 + r, p.cols - 1) * p.ld_w) + part * 32u + lane;
+  const uint4* x = reinterpret_cast<const uint4*>(p.x) + part * 32u + lane;
+#pragma unroll 1
+  for (uint32_t at = part * 32u + lane; at < p.octets; at += step * kAhead) {
+    uint4 q[R][kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int r = 0; r < R; ++r) q[r][i] = at + step * i < p.octets ? __ldg(w[r] + step * i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (at + step * i >= p.octets) break;
+#pragma unroll
+      for (int t = 0; t < M; ++t) {
+        if (t >= p.tokens) break;
+        const uint4 v = __ldg(x + t * (p.ld_x / 8) + step * i);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          sum[t][r] = fma_pair(q[r][i].w, v.w, fma_pair(q[r][i].z, v.z, fma_pair(q[r][i].y, v.y, fma_pair(q[r][i].x, v.x, sum[t][r]))));
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[r] += step * kAhead;
+    x += step * kAhead;
+  }
+  __shared__ float z_of[M][8 * R], parts[8][M * R];
+  float mine = 0.0f;                                                    // lane t R + r: of token t, row r
+#pragma unroll
+  for (int t = 0; t < M; ++t)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float s = sum[t][r];
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+      if (lane == static_cast<uint32_t>(t * R + r)) mine = s;
+    }
+  if (SPLIT > 1) {                                                   // the first warp of a row adds the parts, in their order
+    if (lane < static_cast<uint32_t>(M * R)) parts[warp][lane] = mine;
+    __syncthreads();
+    if (part == 0u && lane < static_cast<uint32_t>(M * R))
+      for (uint32_t k = 1; k < SPLIT; ++k) mine += parts[warp + k][lane];
+  }
+  const uint32_t t = lane / R, r = lane % R;
+  const int64_t col = row0 + r;
+  const bool real = part == 0u && lane < static_cast<uint32_t>(M * R) && t < static_cast<uint32_t>(p.tokens);
+  if (real && col < p.cols) {
+    if (p.bias != nullptr)
+      mine += p.bias_f32 != 0 ? static_cast<const float*>(p.bias)[col] : __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(p.bias)[col]) << 16);
+    float y = act_of_kind(p.activation, mine);
+    if (p.residual != nullptr) y += __uint_as_float(static_cast<uint32_t>(p.residual[t * p.ld_residual + col]) << 16);
+    p.y[t * p.ld_y + col] = static_cast<uint16_t>(pack_bf16(y, 0.0f));
+    if (p.save == GWS_SAVE_BF16) p.save16[t * p.cols + col] = static_cast<uint16_t>(pack_bf16(mine, 0.0f));
+  }
+  if (p.save != GWS_ACT8_INT8 && p.save != GWS_ACT8_E4M3) return;
+  // A checkpoint's group of 32 columns is a cluster's: its first block takes a token to a warp, a column to a lane.
+  if (real) z_of[t][first + r] = col < p.cols ? mine : 0.0f;
+  __syncthreads();
+  pair_sync();
+  if (block_rank() == 0u && warp < static_cast<uint32_t>(p.tokens)) {
+    float z;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(z) : "r"(at_rank(smem_addr(&z_of[warp][lane % rows]), lane / rows)) : "memory");
+    const uint32_t byte = scale_byte(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(z) & 0x7FFFFFFFu), p.save);
+    const float inv = inverse_scale_of(byte);
+    const uint32_t code = byte == kNanByte ? 0u : p.save == GWS_ACT8_INT8 ? encode4_int8(z, 0.0f, 0.0f, 0.0f, inv) : encode4_e4m3(z, 0.0f, 0.0f, 0.0f, inv);
+    const int64_t group = blockIdx.x / (32u / rows);
+    p.save8.codes[warp * p.save8.ld + group * 32 + lane] = static_cast<uint8_t>(code);
+    if (lane == 0u) p.save8.scales[warp * (p.save8.ld >> 5) + group] = static_cast<uint8_t>(byte);
+  }
+  pair_sync();                                                          // rank 0 has read this block's part
+}
+
 }  // namespace

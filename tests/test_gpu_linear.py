@@ -13,8 +13,9 @@ ACTS = [gws.ACT_NONE, gws.GATED_SILU, gws.GATED_GELU_TANH, gws.GATED_RELU]
 # (m, n, k): one token to many, widths that are and are not multiples of the tiles, of 32, of 8; all odd
 SHAPES = [(1, 64, 64), (1, 5632, 256), (3, 8, 8), (33, 96, 40), (128, 128, 128), (129, 130, 72), (200, 1365, 512), (257, 2048, 96), (300, 33, 31), (640, 1000, 333), (1, 1, 1),
           (2048, 256, 768), (1500, 2730, 64), (65, 768, 2730)]
-# every way of tiling the forward product: (blocks, columns, form, m, n, k); narrow tiles of 16 to 128 columns, in one wave and in several
-TILINGS = [(1, 48, "narrow", 1, 5632, 2048), (1, 16, "narrow", 33, 2050, 768), (1, 48, "narrow", 72, 5858, 1807), (1, 80, "narrow", 128, 11008, 264), (1, 16, "narrow", 3, 40, 72),
+# every way of tiling the forward product: (blocks, columns, form, m, n, k); warps that stream rows (0 blocks), narrow tiles of 16 to 128 columns, in one wave and in several
+TILINGS = [(0, 8, "rows", 1, 5632, 2048), (0, 4, "rows", 1, 9, 2104), (0, 8, "rows", 1, 100, 8), (0, 4, "rows", 2, 1000, 4096), (0, 8, "rows", 2, 5000, 1032), (0, 16, "rows", 2, 9601, 264),
+           (0, 16, "rows", 3, 9600, 264), (0, 8, "rows", 3, 770, 768), (0, 4, "rows", 4, 2050, 1032), (0, 16, "rows", 4, 7, 8), (1, 48, "narrow", 5, 5632, 2048), (1, 16, "narrow", 33, 2050, 768), (1, 48, "narrow", 72, 5858, 1807), (1, 80, "narrow", 128, 11008, 264), (1, 16, "narrow", 6, 40, 72),
            (1, 128, "cut", 1, 10, 4009), (1, 128, "cut", 70, 330, 9000), (1, 128, "cluster", 314, 859, 2745), (1, 128, "cluster", 1, 8, 700), (1, 128, "cluster", 40, 130, 1500),
            (2, 128, "whole", 224, 220, 1139), (1, 128, "whole", 268, 5533, 383), (1, 128, "whole*", 796, 2930, 8), (2, 128, "cut", 477, 701, 5986), (2, 128, "whole+cut", 3002, 864, 3835),
            (1, 128, "whole", 213, 532, 102), (2, 128, "whole*", 3955, 534, 294), (2, 256, "cut", 267, 1686, 9306), (2, 256, "whole+cut", 1112, 3767, 1200), (2, 256, "whole", 2650, 920, 445),
@@ -136,7 +137,7 @@ def test_without_an_activation(m, n, k):
 @pytest.mark.parametrize("blocks,columns,form,m,n,k", TILINGS)
 def test_every_tiling(blocks, columns, form, m, n, k):
     p = gws.linear_plan(m, n, k)
-    got = "narrow" if p.narrow else "cluster" if p.clustered else "whole+cut" if p.cut and p.whole else "cut" if p.cut else "whole*" if p.waves > 1 else "whole"
+    got = "rows" if not p.blocks else "narrow" if p.narrow else "cluster" if p.clustered else "whole+cut" if p.cut and p.whole else "cut" if p.cut else "whole*" if p.waves > 1 else "whole"
     assert (p.blocks, p.columns, got) == (blocks, columns, form)
     x, w, b, r, _ = problem(m, n, k)
     for save in (gws.ACT8_INT8, gws.ACT8_E4M3, gws.SAVE_BF16):

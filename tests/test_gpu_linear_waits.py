@@ -32,7 +32,7 @@ def _path(p):
 
 
 # Contractions (or parts of one) of 64 stages and more: 30,000 cycles and more to the first finished tile, against the 16,000 or so that two tries of a wait take.
-FORWARD = [((1, 128, "cluster"), 1, 2048, 32768, gws.ACT8_INT8), ((1, 128, "cut"), 70, 2048, 131072, gws.ACT8_E4M3), ((2, 256, "whole*"), 2100, 4096, 16384, gws.SAVE_BF16),
+FORWARD = [((1, 128, "cluster"), 5, 2048, 32768, gws.ACT8_INT8), ((1, 128, "cut"), 70, 2048, 131072, gws.ACT8_E4M3), ((2, 256, "whole*"), 2100, 4096, 16384, gws.SAVE_BF16),
            ((2, 256, "whole*"), 2100, 4096, 16384, gws.ACT8_INT8), ((2, 256, "whole+cut"), 1500, 4096, 16384, gws.ACT8_INT8)]
 
 
