@@ -478,12 +478,14 @@ int64_t kept_bytes(int format, int64_t m, int64_t n) { return format == GWS_SAVE
 int64_t bias_bytes(const gws_linear_desc& d) { return d.n * (d.bias_type == GWS_TYPE_F32 ? 4 : 2); }
 
 // Whether warps stream the rows of W (k_linear_row).  Each token costs them reads of x, where the narrow tiles of the tensor cores take eight for the price of one but some 4 us more
-// around them.  On the device, us, rows against tiles: one token, 2048 x 5632 6.9, 9.7; two 8.5, 9.7; four 15, 9.7; 768 x 768: one 2.0, 5.8; four 3.3, 5.9.
+// around them.  On the device, us, rows against tiles: one token, 2048 x 5632 6.9, 9.7, 4096 x 11008 20.1, 19.2; two 8.5, 9.7 and 26.7, 19.2; four 15, 9.7; 768 x 768: one 1.8, 5.8;
+// four 3.0, 5.9.
 bool streams_rows(const gws_linear_desc& d) {
-  return d.k % 8 == 0 && in_place(d.m, d.ld_x) && in_place(d.n, d.ld_w) && (d.m <= 2 || (d.m <= 4 && d.n * d.k <= (1 << 22)));
+  const int64_t weights = d.n * d.k, most = d.m == 1 ? 1 << 25 : d.m == 2 ? 1 << 24 : d.m <= 4 ? 1 << 22 : 0;
+  return weights <= most && d.k % 8 == 0 && in_place(d.m, d.ld_x) && in_place(d.n, d.ld_w);
 }
-// Columns of y to a block of eight warps: one or two to a warp, or to up to four warps where there are few columns and long rows (one token, 5632 x 2048: 11.3 us with a warp to a row,
-// 8.5 with two).  A checkpoint's 32 columns stay within a cluster of eight blocks.
+// Columns of y to a block of eight warps: one or two to a warp, or two to four warps where there are few columns and long rows (one token, 5632 x 2048: 11.3 us with a warp to a row,
+// 6.5 with four to two).  A checkpoint's 32 columns stay within a cluster of eight blocks.
 unsigned row_columns(const gws_linear_desc& d) {
   const unsigned most = d.m == 1 ? 8u : 16u;
   const int64_t warps = d.m == 1 ? d.n : (d.n + 1) / 2;
@@ -958,7 +960,7 @@ int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, co
     p.bias_f32 = d.bias_type == GWS_TYPE_F32;
     const unsigned per = row_columns(d), cluster = bytes8 ? 32u / per : 1u;
     const unsigned grid = static_cast<unsigned>(round_up((d.n + per - 1) / per, cluster));
-    auto kernel = d.m == 1   ? (per == 8u ? k_linear_row<1, 1, 1> : k_linear_row<1, 1, 2>)
+    auto kernel = d.m == 1   ? (per == 8u ? k_linear_row<1, 1, 1> : k_linear_row<1, 2, 4>)
                   : d.m == 2 ? (per == 16u ? k_linear_row<2, 2, 1> : per == 8u ? k_linear_row<2, 2, 2> : k_linear_row<2, 2, 4>)
                              : (per == 16u ? k_linear_row<4, 2, 1> : per == 8u ? k_linear_row<4, 2, 2> : k_linear_row<4, 2, 4>);
     return launch(kernel, grid, 256, 0, cluster, s, "linear layer of a few tokens", p);
