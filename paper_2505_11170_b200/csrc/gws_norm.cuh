@@ -15,6 +15,7 @@
 #include <stdint.h>
 
 #include "gws_act8.cuh"
+#include "gws_pair.cuh"
 #include "gws_sums.cuh"
 
 namespace {
@@ -47,69 +48,70 @@ template <int C, bool WIDE>
 struct NormWords {
   uint32_t x[WIDE ? 4 * C : 8 * C];
 };
+// `units`: of eight elements, or elements one by one, that the row has (0: a row past the last).
 template <int L, int C, bool WIDE>
-__device__ __forceinline__ void norm_load(const uint16_t* row, int64_t cols, uint32_t lane, NormWords<C, WIDE>& w) {
+__device__ __forceinline__ void norm_load(const uint16_t* row, uint32_t units, uint32_t lane, NormWords<C, WIDE>& w) {
   if constexpr (WIDE) {
+    const uint4* p = reinterpret_cast<const uint4*>(row) + lane;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = norm_col<L, WIDE>(lane, c, 0);
-      const uint4 q = col < cols ? __ldg(reinterpret_cast<const uint4*>(row + col)) : make_uint4(0u, 0u, 0u, 0u);
+      const uint4 q = lane + c * L < units ? __ldg(p + c * L) : make_uint4(0u, 0u, 0u, 0u);
       w.x[4 * c] = q.x; w.x[4 * c + 1] = q.y; w.x[4 * c + 2] = q.z; w.x[4 * c + 3] = q.w;
     }
   } else {
+    const uint16_t* p = row + lane;
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) {
-      const int64_t col = norm_col<L, WIDE>(lane, 0, e);
-      w.x[e] = col < cols ? static_cast<uint32_t>(__ldg(row + col)) : 0u;
-    }
+    for (int e = 0; e < 8 * C; ++e) w.x[e] = lane + e * L < units ? static_cast<uint32_t>(__ldg(p + e * L)) : 0u;
   }
 }
+// Elements 2 i and 2 i + 1.
 template <int C, bool WIDE>
-__device__ __forceinline__ float norm_value(const NormWords<C, WIDE>& w, int e) {
-  if constexpr (WIDE) return (e & 1) == 0 ? bf16_lo(w.x[e / 2]) : bf16_hi(w.x[e / 2]);
-  else return __uint_as_float(w.x[e] << 16);
+__device__ __forceinline__ F2 norm_pair(const NormWords<C, WIDE>& w, int i) {
+  if constexpr (WIDE) return two(bf16_lo(w.x[i]), bf16_hi(w.x[i]));
+  else return two(__uint_as_float(w.x[2 * i] << 16), __uint_as_float(w.x[2 * i + 1] << 16));
 }
+// v holds pairs of BF16.
 template <int L, int C, bool WIDE>
-__device__ __forceinline__ void norm_write(uint16_t* row, int64_t cols, uint32_t lane, const float (&v)[8 * C]) {
-  if (WIDE) {
+__device__ __forceinline__ void norm_write(uint16_t* row, uint32_t units, uint32_t lane, const uint32_t (&v)[4 * C]) {
+  if constexpr (WIDE) {
+    uint4* p = reinterpret_cast<uint4*>(row) + lane;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t col = norm_col<L, WIDE>(lane, c, 0);
-      if (col < cols)
-        *reinterpret_cast<uint4*>(row + col) = make_uint4(pack_bf16(v[8 * c], v[8 * c + 1]), pack_bf16(v[8 * c + 2], v[8 * c + 3]), pack_bf16(v[8 * c + 4], v[8 * c + 5]),
-                                                          pack_bf16(v[8 * c + 6], v[8 * c + 7]));
-    }
+    for (int c = 0; c < C; ++c)
+      if (lane + c * L < units) p[c * L] = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
   } else {
+    uint16_t* p = row + lane;
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) {
-      const int64_t col = norm_col<L, WIDE>(lane, 0, e);
-      if (col < cols) row[col] = static_cast<uint16_t>(pack_bf16(v[e], 0.0f));
-    }
+    for (int e = 0; e < 8 * C; ++e)
+      if (lane + e * L < units) p[e * L] = static_cast<uint16_t>(v[e / 2] >> (16 * (e & 1)));
   }
 }
-// Eight weights (or biases) of unit c.
+// Eight weights (or biases) of unit c, in pairs.
 template <int L, bool WIDE>
-__device__ __forceinline__ void norm_weights(const void* w, bool f32, float none, int64_t cols, uint32_t lane, int c, float (&v)[8]) {
-  if (w == nullptr) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = none;
-    return;
-  }
+__device__ __forceinline__ void norm_weights(const void* w, bool f32, float none, int64_t cols, uint32_t lane, int c, float4 (&v)[2]) {
+  v[0] = v[1] = make_float4(none, none, none, none);
+  if (w == nullptr) return;
   const int64_t col = norm_col<L, WIDE>(lane, c, 0);
   if (WIDE && f32) {
+    if (col >= cols) return;
     const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(w) + col);
-    const float4 a = col < cols ? __ldg(p) : make_float4(0, 0, 0, 0), b = col < cols ? __ldg(p + 1) : make_float4(0, 0, 0, 0);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = __ldg(p);
+    v[1] = __ldg(p + 1);
   } else if (WIDE) {
-    const uint4 q = col < cols ? __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + col)) : make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t p[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(p[i]); v[2 * i + 1] = bf16_hi(p[i]); }
+    if (col >= cols) return;
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + col));
+    v[0] = make_float4(bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y));
+    v[1] = make_float4(bf16_lo(q.z), bf16_hi(q.z), bf16_lo(q.w), bf16_hi(q.w));
   } else {
+    float t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = norm_col<L, WIDE>(lane, c, i) < cols ? norm_weight(w, f32, norm_col<L, WIDE>(lane, c, i)) : 0.0f;
+    for (int i = 0; i < 8; ++i) t[i] = norm_col<L, WIDE>(lane, c, i) < cols ? norm_weight(w, f32, norm_col<L, WIDE>(lane, c, i)) : 0.0f;
+    v[0] = make_float4(t[0], t[1], t[2], t[3]);
+    v[1] = make_float4(t[4], t[5], t[6], t[7]);
   }
 }
+
+// Blocks of the forward kernel that an SM holds.
+constexpr int norm_blocks(int team, bool wide) { return team <= 256 ? (wide ? 4 : 3) : wide && team <= 512 ? 2 : 1; }
 
 // Sums of two values over a team; every thread of the block calls it the same number of times.  `room`: [2][threads / 32], used in turn.
 template <int L>
@@ -133,53 +135,117 @@ __device__ __forceinline__ float2 team_sum(float a, float b, float2* room, uint3
 }
 
 template <int L>
-constexpr uint32_t kNormThreads = L < 256 ? 256u : static_cast<uint32_t>(L);          // of a block
+constexpr uint32_t kNormThreads = L < 256 ? 256u / L * L : static_cast<uint32_t>(L);          // of a block
 
+// Memory-bound: 2 or 4 bytes in, 2 or 4 out per element.  A team takes rows in turn, with the next row's words under way; weights stay in shared memory where the block's teams (or
+// its rows) share them.
 template <int L, int C, bool WIDE>
-__global__ void __launch_bounds__(kNormThreads<L>) k_norm_fwd(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads<L>, norm_blocks(L, WIDE)) k_norm_fwd(const __grid_constant__ NormArgs p) {
   after_previous();
+  constexpr uint32_t kTeams = kNormThreads<L> / L;
+  constexpr bool kHeld = L <= 256;
   __shared__ float2 room[2][kNormThreads<L> / 32u];
+  __shared__ float4 held[kHeld ? 2 : 1][kHeld ? 2 * C : 1][kHeld ? L : 1];
   uint32_t turn = 0;
-  const uint32_t lane = threadIdx.x % L;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kNormThreads<L> / L) + threadIdx.x / L;
-  if (row >= p.rows) return;               // teams of more than a warp have a block to themselves
-  float s[8 * C];
-  NormWords<C, WIDE> x;
-  norm_load<L, C, WIDE>(p.x + row * p.ld_x, p.cols, lane, x);
-  if (p.r != nullptr) {
-    NormWords<C, WIDE> r;
-    norm_load<L, C, WIDE>(p.r + row * p.ld_r, p.cols, lane, r);
+  const uint32_t lane = threadIdx.x % L, team = threadIdx.x / L;
+  if (kHeld && team < 2u) {
+    if (team == 0u || kTeams == 1u)
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) s[e] = bf16_lo(pack_bf16(norm_value(x, e) + norm_value(r, e), 0.0f));
-    norm_write<L, C, WIDE>(p.sum + row * p.cols, p.cols, lane, s);
-  } else {
+      for (int c = 0; c < C; ++c) {
+        float4 q[2];
+        norm_weights<L, WIDE>(p.weight, p.f32 != 0, 1.0f, p.cols, lane, c, q);
+        held[0][2 * c][lane] = q[0];
+        held[0][2 * c + 1][lane] = q[1];
+      }
+    if (team == 1u || kTeams == 1u)
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) s[e] = norm_value(x, e);
+      for (int c = 0; c < C; ++c) {
+        float4 q[2];
+        norm_weights<L, WIDE>(p.bias, p.f32 != 0, 0.0f, p.cols, lane, c, q);
+        held[kHeld ? 1 : 0][2 * c][lane] = q[0];
+        held[kHeld ? 1 : 0][2 * c + 1][lane] = q[1];
+      }
   }
-  float t = 0.0f;
+  if (kHeld) __syncthreads();
+  struct Row {
+    NormWords<C, WIDE> x, r;
+  } next;
+  const uint32_t all = static_cast<uint32_t>(WIDE ? p.cols / 8 : p.cols);
+  auto fetch = [&](int64_t row, Row& to) {
+    const uint32_t units = row < p.rows ? all : 0u;
+    norm_load<L, C, WIDE>(p.x + row * p.ld_x, units, lane, to.x);
+    if (p.r != nullptr) norm_load<L, C, WIDE>(p.r + row * p.ld_r, units, lane, to.r);
+  };
+  const float inv = 1.0f / static_cast<float>(p.cols);
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
+  int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTeams;
+  if (WIDE) fetch(row0 + team, next);
+#pragma unroll 1
+  for (; row0 < p.rows; row0 += stride) {
+    Row now;
+    if (WIDE) {
+      now = next;
+      if (row0 + stride < p.rows) fetch(row0 + stride + team, next);        // under the sums of this one
+    } else {
+      fetch(row0 + team, now);
+    }
+    const int64_t row = row0 + team;
+    const uint32_t units = row < p.rows ? all : 0u;                                // nothing is written for rows past the last
+    F2 s[4 * C], t = both(0.0f);
+    uint32_t w[4 * C];
+    if (p.r != nullptr) {
 #pragma unroll
-  for (int e = 0; e < 8 * C; ++e) t += s[e];
-  const float inv = 1.0f / static_cast<float>(p.cols), mean = team_sum<L>(t, 0.0f, room[0], turn).x * inv;
-  t = 0.0f;
+      for (int i = 0; i < 4 * C; ++i) {
+        const F2 v = fma2(norm_pair(now.x, i), both(1.0f), norm_pair(now.r, i));
+        w[i] = pack_bf16(first_of(v), second_of(v));
+        s[i] = two(bf16_lo(w[i]), bf16_hi(w[i]));
+      }
+      norm_write<L, C, WIDE>(p.sum + row * p.cols, units, lane, w);
+    } else {
 #pragma unroll
-  for (int e = 0; e < 8 * C; ++e) {
-    s[e] -= mean;
-    if (norm_col<L, WIDE>(lane, e / 8, e % 8) < p.cols) t = __fmaf_rn(s[e], s[e], t);
+      for (int i = 0; i < 4 * C; ++i) s[i] = norm_pair(now.x, i);
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * C; ++i) t = fma2(s[i], both(1.0f), t);
+    const float mean = team_sum<L>(first_of(t) + second_of(t), 0.0f, room[0], turn).x * inv;
+    t = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < 4 * C; ++i) {
+      s[i] = fma2(s[i], both(1.0f), both(-mean));
+      if constexpr (WIDE) {
+        if (lane + i / 4 * L >= units) s[i] = both(0.0f);                                        // outside
+      } else {
+        s[i] = two(lane + 2 * i * L < units ? first_of(s[i]) : 0.0f, lane + (2 * i + 1) * L < units ? second_of(s[i]) : 0.0f);
+      }
+      t = fma2(s[i], s[i], t);
+    }
+    const float rstd = rsqrtf(team_sum<L>(first_of(t) + second_of(t), 0.0f, room[0], turn).x * inv + p.eps);
+    if (lane == 0 && p.stats != nullptr && row < p.rows) {
+      p.stats[row] = mean;
+      p.stats[p.rows + row] = rstd;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float4 q[2], b[2];
+      if constexpr (kHeld) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          q[h] = held[0][2 * c + h][lane];
+          b[h] = held[1][2 * c + h][lane];
+        }
+      } else {
+        norm_weights<L, WIDE>(p.weight, p.f32 != 0, 1.0f, p.cols, lane, c, q);
+        norm_weights<L, WIDE>(p.bias, p.f32 != 0, 0.0f, p.cols, lane, c, b);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 qh = q[i / 2], bh = b[i / 2];
+        const F2 v = fma2(mul2(s[4 * c + i], both(rstd)), (i & 1) == 0 ? two(qh.x, qh.y) : two(qh.z, qh.w), (i & 1) == 0 ? two(bh.x, bh.y) : two(bh.z, bh.w));
+        w[4 * c + i] = pack_bf16(first_of(v), second_of(v));
+      }
+    }
+    norm_write<L, C, WIDE>(p.y + row * p.cols, units, lane, w);
   }
-  const float rstd = rsqrtf(team_sum<L>(t, 0.0f, room[0], turn).x * inv + p.eps);
-  if (lane == 0 && p.stats != nullptr) {
-    p.stats[row] = mean;
-    p.stats[p.rows + row] = rstd;
-  }
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    float w[8], b[8];
-    norm_weights<L, WIDE>(p.weight, p.f32 != 0, 1.0f, p.cols, lane, c, w);
-    norm_weights<L, WIDE>(p.bias, p.f32 != 0, 0.0f, p.cols, lane, c, b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s[8 * c + i] = __fmaf_rn(s[8 * c + i] * rstd, w[i], b[i]);
-  }
-  norm_write<L, C, WIDE>(p.y + row * p.cols, p.cols, lane, s);
 }
 
 // Rows of any length: a block reads its row again for each pass (from L2).
@@ -214,38 +280,44 @@ __global__ void __launch_bounds__(kNormLong) k_norm_fwd_long(const __grid_consta
   }
 }
 
+// Memory-bound: 4 or 6 bytes in, 2 out per element.
 template <int L, int C, bool WIDE>
-__global__ void __launch_bounds__(kNormThreads<L>) k_norm_bwd(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(kNormThreads<L>, L <= 256 ? 2 : 1) k_norm_bwd(const __grid_constant__ NormArgs p) {
   after_previous();
   constexpr uint32_t kTeams = kNormThreads<L> / L;
   __shared__ float2 room[2][kNormThreads<L> / 32u];
-  __shared__ float2 joined[kTeams > 1u ? L * C * 8u : 1u];
-  __shared__ float weights[C][8][L];                     // the same for every team: out of the registers, so that the next row's words fit in
+  __shared__ float4 held[2 * C][L];                      // the weights, the same for every team and row
+  __shared__ float4 joined[kTeams > 1u ? 4 * C : 1u][kTeams > 1u ? L : 1u];
   uint32_t turn = 0;
   const uint32_t lane = threadIdx.x % L, team = threadIdx.x / L;
   const float inv = 1.0f / static_cast<float>(p.cols);
-  float gw[8 * C], gb[8 * C];
+  F2 gw[4 * C], gb[4 * C];
 #pragma unroll
-  for (int e = 0; e < 8 * C; ++e) gw[e] = gb[e] = 0.0f;
+  for (int i = 0; i < 4 * C; ++i) gw[i] = gb[i] = both(0.0f);
   if (team == 0u) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float q[8];
+      float4 q[2];
       norm_weights<L, WIDE>(p.weight, p.f32 != 0, 1.0f, p.cols, lane, c, q);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) weights[c][i][lane] = q[i];
+      held[2 * c][lane] = q[0];
+      held[2 * c + 1][lane] = q[1];
     }
   }
   __syncthreads();
+  auto weight = [&](int i) {
+    const float4 q = held[i / 2][lane];
+    return (i & 1) == 0 ? two(q.x, q.y) : two(q.z, q.w);
+  };
   struct Row {
     NormWords<C, WIDE> s, dy, d;
     float mean, rstd;
   } next;
+  const uint32_t all = static_cast<uint32_t>(WIDE ? p.cols / 8 : p.cols);
   auto fetch = [&](int64_t row, Row& r) {
-    const int64_t cols = row < p.rows ? p.cols : 0;
-    norm_load<L, C, WIDE>(p.x + row * p.ld_x, cols, lane, r.s);
-    norm_load<L, C, WIDE>(p.dy + row * p.ld_dy, cols, lane, r.dy);
-    if (p.d != nullptr) norm_load<L, C, WIDE>(p.d + row * p.ld_d, cols, lane, r.d);
+    const uint32_t units = row < p.rows ? all : 0u;
+    norm_load<L, C, WIDE>(p.x + row * p.ld_x, units, lane, r.s);
+    norm_load<L, C, WIDE>(p.dy + row * p.ld_dy, units, lane, r.dy);
+    if (p.d != nullptr) norm_load<L, C, WIDE>(p.d + row * p.ld_d, units, lane, r.d);
     r.mean = row < p.rows ? p.stats[row] : 0.0f;
     r.rstd = row < p.rows ? p.stats[p.rows + row] : 0.0f;
   };
@@ -262,27 +334,29 @@ __global__ void __launch_bounds__(kNormThreads<L>) k_norm_bwd(const __grid_const
       fetch(row0 + team, now);                                              // an element to a register: there is no room for two rows
     }
     const int64_t row = row0 + team;
-    float ta = 0.0f, tb = 0.0f;
+    // xh = s rstd - mean rstd would lose a row of large mean: the mean is taken off first
+    auto centred = [&](int i) { return mul2(fma2(norm_pair(now.s, i), both(1.0f), both(-now.mean)), both(now.rstd)); };
+    F2 ta = both(0.0f), tb = both(0.0f);
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) {
-      const float xh = (norm_value(now.s, e) - now.mean) * now.rstd, dy = norm_value(now.dy, e);          // columns past the width have dy = 0
-      const float a = dy * weights[e / 8][e % 8][lane];
-      ta += a;
-      tb = __fmaf_rn(a, xh, tb);
-      gw[e] = __fmaf_rn(dy, xh, gw[e]);
-      gb[e] += dy;
+    for (int i = 0; i < 4 * C; ++i) {
+      const F2 xh = centred(i), dy = norm_pair(now.dy, i), a = mul2(dy, weight(i));          // columns past the width have dy = 0
+      ta = fma2(a, both(1.0f), ta);
+      tb = fma2(a, xh, tb);
+      gw[i] = fma2(dy, xh, gw[i]);
+      gb[i] = fma2(dy, both(1.0f), gb[i]);
     }
-    const float2 t = team_sum<L>(ta, tb, room[0], turn);
+    const float2 t = team_sum<L>(first_of(ta) + second_of(ta), first_of(tb) + second_of(tb), room[0], turn);
     if (p.dx != nullptr && row < p.rows) {
-      const float ma = t.x * inv, mb = t.y * inv;
-      float out[8 * C];
+      const F2 ma = both(-t.x * inv), mb = both(-t.y * inv), rstd = both(now.rstd);
+      uint32_t w[4 * C];
 #pragma unroll
-      for (int e = 0; e < 8 * C; ++e) {
-        const float xh = (norm_value(now.s, e) - now.mean) * now.rstd, a = norm_value(now.dy, e) * weights[e / 8][e % 8][lane];
-        out[e] = now.rstd * __fmaf_rn(-xh, mb, a - ma);
-        if (p.d != nullptr) out[e] += norm_value(now.d, e);
+      for (int i = 0; i < 4 * C; ++i) {
+        const F2 a = fma2(norm_pair(now.dy, i), weight(i), ma);
+        F2 v = mul2(fma2(centred(i), mb, a), rstd);
+        if (p.d != nullptr) v = fma2(v, both(1.0f), norm_pair(now.d, i));
+        w[i] = pack_bf16(first_of(v), second_of(v));
       }
-      norm_write<L, C, WIDE>(p.dx + row * p.cols, p.cols, lane, out);
+      norm_write<L, C, WIDE>(p.dx + row * p.cols, all, lane, w);
     }
   }
   if (p.part == nullptr) return;
@@ -290,24 +364,29 @@ __global__ void __launch_bounds__(kNormThreads<L>) k_norm_bwd(const __grid_const
     for (uint32_t t = 0; t < kTeams; ++t) {
       if (team == t) {
 #pragma unroll
-        for (int e = 0; e < 8 * C; ++e) {
-          float2& j = joined[e * L + lane];
-          j = t == 0u ? make_float2(gw[e], gb[e]) : make_float2(j.x + gw[e], j.y + gb[e]);
+        for (int i = 0; i < 4 * C; ++i) {
+          float4& j = joined[i][lane];
+          const float4 g = make_float4(first_of(gw[i]), second_of(gw[i]), first_of(gb[i]), second_of(gb[i]));
+          j = t == 0u ? g : make_float4(j.x + g.x, j.y + g.y, j.z + g.z, j.w + g.w);
         }
       }
       __syncthreads();
     }
     if (team != 0u) return;
 #pragma unroll
-    for (int e = 0; e < 8 * C; ++e) { gw[e] = joined[e * L + lane].x; gb[e] = joined[e * L + lane].y; }
+    for (int i = 0; i < 4 * C; ++i) {
+      const float4 j = joined[i][lane];
+      gw[i] = two(j.x, j.y);
+      gb[i] = two(j.z, j.w);
+    }
   }
   float* part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.cols;
 #pragma unroll
   for (int e = 0; e < 8 * C; ++e) {
     const int64_t col = norm_col<L, WIDE>(lane, e / 8, e % 8);
     if (col < p.cols) {
-      part[col] = gw[e];
-      part[p.cols + col] = gb[e];
+      part[col] = (e & 1) == 0 ? first_of(gw[e / 2]) : second_of(gw[e / 2]);
+      part[p.cols + col] = (e & 1) == 0 ? first_of(gb[e / 2]) : second_of(gb[e / 2]);
     }
   }
 }

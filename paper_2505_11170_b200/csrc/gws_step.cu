@@ -29,22 +29,31 @@ int64_t weight_bytes(const gws_norm_desc& d) { return d.weight_type == GWS_TYPE_
 // Whether rows of a BF16 matrix (absent: null) start on 16-byte boundaries.
 bool wide_rows(const void* p, int64_t rows, int64_t ld) { return p == nullptr || (on(p, 16) && (rows <= 1 || ld % 8 == 0)); }
 
-// Rows of up to 2048 elements (1024, read one by one) to a warp each, or, where that leaves SMs without a row or the row is longer, to a block.
+// Threads of a row; a block of 256 or more holds one row or several.  0: rows that no block holds.
+int norm_team(int64_t cols) {
+  for (const int team : {32, 64, 96, 128, 192, 256, 384, 512})
+    if (cols <= 16 * team) return team;
+  return 0;
+}
+int64_t norm_teams(int team) { return team < 256 ? 256 / team : 1; }
+
 template <bool WIDE>
 int launch_norm_fwd(const NormArgs& a, cudaStream_t s) {
   const char* what = "layer norm kernel";
-  const unsigned rows = static_cast<unsigned>(a.rows), warps = blocks_for(a.rows, 8);
-  if (a.cols <= 256) return launch(k_norm_fwd<32, 1, WIDE>, warps, 256, 0, 1, s, what, a);
-  if (a.cols <= (WIDE ? 2048 : 1024) && a.rows >= 2 * sm_count()) {
-    if (a.cols <= 512) return launch(k_norm_fwd<32, 2, WIDE>, warps, 256, 0, 1, s, what, a);
-    if (a.cols <= 1024) return launch(k_norm_fwd<32, 4, WIDE>, warps, 256, 0, 1, s, what, a);
-    if constexpr (WIDE) return launch(k_norm_fwd<32, 8, true>, warps, 256, 0, 1, s, what, a);
-  }
-  if (a.cols <= 2048) return launch(k_norm_fwd<256, 1, WIDE>, rows, 256, 0, 1, s, what, a);
-  if (a.cols <= 4096) return launch(k_norm_fwd<256, 2, WIDE>, rows, 256, 0, 1, s, what, a);
-  if (a.cols <= 8192) return launch(k_norm_fwd<256, 4, WIDE>, rows, 256, 0, 1, s, what, a);
-  if (a.cols <= 16384) return launch(k_norm_fwd<1024, 2, WIDE>, rows, 1024, 0, 1, s, what, a);
-  return launch(k_norm_fwd_long, rows, kNormLong, 0, 1, s, what, a);
+  const int team = norm_team(a.cols);
+  if (team == 0 && a.cols <= 16384) return launch(k_norm_fwd<1024, 2, WIDE>, static_cast<unsigned>(std::min<int64_t>(a.rows, sm_count())), 1024, 0, 1, s, what, a);
+  if (team == 0) return launch(k_norm_fwd_long, static_cast<unsigned>(a.rows), kNormLong, 0, 1, s, what, a);
+  const int64_t teams = norm_teams(team), fit = static_cast<int64_t>(sm_count()) * norm_blocks(team, WIDE);
+  const unsigned grid = static_cast<unsigned>(std::min((a.rows + teams - 1) / teams, fit));
+  if (team == 32 && a.cols <= 256) return launch(k_norm_fwd<32, 1, WIDE>, grid, 256, 0, 1, s, what, a);
+  if (team == 32) return launch(k_norm_fwd<32, 2, WIDE>, grid, 256, 0, 1, s, what, a);
+  if (team == 64) return launch(k_norm_fwd<64, 2, WIDE>, grid, 256, 0, 1, s, what, a);
+  if (team == 96) return launch(k_norm_fwd<96, 2, WIDE>, grid, kNormThreads<96>, 0, 1, s, what, a);
+  if (team == 128) return launch(k_norm_fwd<128, 2, WIDE>, grid, 256, 0, 1, s, what, a);
+  if (team == 192) return launch(k_norm_fwd<192, 2, WIDE>, grid, kNormThreads<192>, 0, 1, s, what, a);
+  if (team == 256) return launch(k_norm_fwd<256, 2, WIDE>, grid, 256, 0, 1, s, what, a);
+  if (team == 384) return launch(k_norm_fwd<384, 2, WIDE>, grid, 384, 0, 1, s, what, a);
+  return launch(k_norm_fwd<512, 2, WIDE>, grid, 512, 0, 1, s, what, a);
 }
 
 struct NormBack {
@@ -53,9 +62,9 @@ struct NormBack {
 };
 NormBack norm_back(int64_t rows, int64_t cols) {
   const int sms = sm_count();
-  if (cols > 8192) return {0, static_cast<uint32_t>(std::min<int64_t>(64, (rows + 31) / 32))};
-  const int team = cols <= 512 ? 32 : cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512;
-  const int64_t teams = team < 256 ? 256 / team : 1;
+  if (norm_team(cols) == 0) return {0, static_cast<uint32_t>(std::min<int64_t>(64, (rows + 31) / 32))};
+  const int team = norm_team(cols);
+  const int64_t teams = norm_teams(team);
   return {team, static_cast<uint32_t>(std::min<int64_t>((rows + teams - 1) / teams, static_cast<int64_t>(sms) * (team <= 256 ? 2 : 1)))};
 }
 template <bool WIDE>
@@ -64,8 +73,11 @@ int launch_norm_bwd(const NormArgs& a, const NormBack& b, cudaStream_t s) {
   if (b.team == 32 && a.cols <= 256) return launch(k_norm_bwd<32, 1, WIDE>, b.blocks, 256, 0, 1, s, what, a);
   if (b.team == 32) return launch(k_norm_bwd<32, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
   if (b.team == 64) return launch(k_norm_bwd<64, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
+  if (b.team == 96) return launch(k_norm_bwd<96, 2, WIDE>, b.blocks, kNormThreads<96>, 0, 1, s, what, a);
   if (b.team == 128) return launch(k_norm_bwd<128, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
+  if (b.team == 192) return launch(k_norm_bwd<192, 2, WIDE>, b.blocks, kNormThreads<192>, 0, 1, s, what, a);
   if (b.team == 256) return launch(k_norm_bwd<256, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
+  if (b.team == 384) return launch(k_norm_bwd<384, 2, WIDE>, b.blocks, 384, 0, 1, s, what, a);
   return launch(k_norm_bwd<512, 2, WIDE>, b.blocks, 512, 0, 1, s, what, a);
 }
 
