@@ -71,11 +71,16 @@ class GaussWSAdamW(torch.optim.Optimizer):
         count = self._count.add_(1) if on_device else self._count + 1
         decays = [float(g["weight_decay"]) for g in self.param_groups for _ in g["params"]]
         kinds = [(id(g["lr"]) if isinstance(g["lr"], torch.Tensor) else g["lr"], tuple(g["betas"]), g["eps"]) for g in self.param_groups]
-        for kind in dict.fromkeys(kinds):
-            mine = [k == kind for k, g in zip(kinds, self.param_groups) for _ in g["params"]]
-            group = self.param_groups[kinds.index(kind)]
-            binding.adamw_step(params, grads if all(mine) else [g if m else None for g, m in zip(grads, mine)], state, lr=group["lr"], betas=group["betas"],
-                               eps=group["eps"], weight_decay=decays, step=count, grad_scale=grad_scale)
+        try:
+            for kind in dict.fromkeys(kinds):
+                mine = [k == kind for k, g in zip(kinds, self.param_groups) for _ in g["params"]]
+                group = self.param_groups[kinds.index(kind)]
+                binding.adamw_step(params, grads if all(mine) else [g if m else None for g, m in zip(grads, mine)], state, lr=group["lr"], betas=group["betas"],
+                                   eps=group["eps"], weight_decay=decays, step=count, grad_scale=grad_scale)
+        except Exception:                                 # a step that was refused does not count
+            if on_device:
+                count.sub_(1)
+            raise
         self._count = count
         return loss
 
@@ -112,6 +117,9 @@ class GaussWSAdamW(torch.optim.Optimizer):
         s = kept["state"]
         if s is not None and list(s["sizes"]) != sizes:
             raise ValueError("gws: the state is of tensors of other sizes")
+        rest = self._rest and any(p.dtype == torch.bfloat16 for p in self._all())
+        if s is not None and (s["rest"] is not None) != rest:
+            raise ValueError("gws: one of the optimizers keeps the rest of its weights, the other does not")
         super().load_state_dict({k: v for k, v in state_dict.items() if k != "gws"})
         if isinstance(self._count, torch.Tensor):
             self._count.fill_(kept["count"])              # captured steps read it where it is
@@ -124,8 +132,6 @@ class GaussWSAdamW(torch.optim.Optimizer):
                         t.zero_()
             return
         mine = self._prepare()
-        if (s["rest"] is None) != (mine.rest is None):
-            raise ValueError("gws: one of the optimizers keeps the rest of its weights, the other does not")
         for to, source in ((mine.moments, s["moments"]), (mine.units, s["units"]), (mine.rest, s["rest"])):
             if to is not None:
                 to.copy_(source)

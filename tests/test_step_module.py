@@ -211,6 +211,31 @@ def test_a_capture_wants_a_count_on_the_device_and_a_step_before(recorded, monke
     assert int(ready._count) == 2 and recorded[-1]["step"] is ready._count and len(recorded) == 3
 
 
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_refused_step_does_not_count(recorded, capturable, monkeypatch):
+    optimizer = GaussWSAdamW([_parameter(4)], capturable=capturable)
+    optimizer.step()
+
+    def refuses(*args, **more):
+        raise ValueError
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "adamw_step", refuses)
+        with pytest.raises(ValueError):
+            optimizer.step()
+    assert int(optimizer._count) == 1
+    optimizer.step()
+    assert int(recorded[-1]["step"]) == 2
+
+
+def test_a_refused_state_changes_nothing(recorded):
+    source, other = GaussWSAdamW([_parameter(300)], lr=2e-3), GaussWSAdamW([_parameter(300)], lr=1e-3, rest=False)
+    source.step()
+    with pytest.raises(ValueError):
+        other.load_state_dict(source.state_dict())
+    assert other._count == 0 and other.param_groups[0]["lr"] == 1e-3
+
+
 @pytest.mark.parametrize("moments", [gws.ADAMW_F32, gws.ADAMW_8BIT])
 def test_state_travels(recorded, moments):
     p = _parameter(300)
@@ -237,6 +262,8 @@ def test_layout_of_the_state():
     state = gws.AdamWState([1, 256, 257, 0, 300], gws.ADAMW_8BIT, rest=True, device="cpu")
     assert state.starts == (0, 256, 512, 1024, 1024) and state.total == 1536
     assert state.moments.shape == (2, 1536) and state.moments.dtype == torch.uint8 and state.units.shape == (2, 6) and state.rest.shape == (1536,)
+    with pytest.raises(AttributeError):
+        state.moments = state.moments.clone()              # the address is kept
     flat = gws.AdamWState([5], device="cpu")
     assert flat.moments.shape == (2, 256) and flat.units is None and flat.rest is None
     assert [t.shape for t in flat.values()] == [(256,), (256,)]
