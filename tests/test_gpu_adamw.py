@@ -291,6 +291,20 @@ def test_gradients_of_any_strides_and_shapes():
     gws.adamw_step([], [], gws.AdamWState([]), lr=1e-3)
 
 
+def test_offsets_that_pass_32_bits():
+    big, few = (1 << 31) + 300, 1000
+    p, g = (torch.empty(big, dtype=torch.bfloat16, device=DEV).normal_(0, std) for std in (0.02, 1e-3))
+    q, h = (torch.empty(few, dtype=torch.bfloat16, device=DEV).normal_(0, std) for std in (0.02, 1e-3))
+    whole, ends = gws.AdamWState([big, few], gws.ADAMW_8BIT, rest=True), gws.AdamWState([300, few], gws.ADAMW_8BIT, rest=True)
+    p_ends, g_ends = [p[1 << 31:].clone(), q.clone()], [g[1 << 31:].clone(), h]
+    for step in (1, 2):
+        gws.adamw_step([p, q], [g, h], whole, step=step, **HYPER)
+        gws.adamw_step(p_ends, g_ends, ends, step=step, **HYPER)
+    assert torch.equal(p[1 << 31:], p_ends[0]) and torch.equal(q, p_ends[1])
+    assert torch.equal(whole.moments[:, 1 << 31:], ends.moments) and torch.equal(whole.units[:, 1 << 23:], ends.units) and torch.equal(whole.rest[1 << 31:], ends.rest)
+    assert bool(whole.rest[(1 << 31) - 256:1 << 31].any()) and not bool((p[(1 << 31) - 256:1 << 31] == 0).all())
+
+
 def test_refusals():
     p, g = torch.ones(300, device=DEV), torch.ones(300, device=DEV)
     st = gws.AdamWState([300])

@@ -256,6 +256,25 @@ def test_another_stream_a_captured_step_and_steps_in_a_row():
     gws.check_waits()
 
 
+def test_offsets_that_pass_32_bits():
+    m, n, k, kind = (1 << 20) + 77, 2072, 2056, gws.GATED_GELU_TANH
+    ends = torch.cat([torch.arange(200), torch.arange(m - 200, m)]).to(DEV)
+    x = torch.empty(m, k, dtype=torch.bfloat16, device=DEV).normal_()
+    w, b, dy = rand((n, k), 2, 1.5 / math.sqrt(k)), rand((n,), 5, 0.5, torch.float32), torch.zeros(m, n, dtype=torch.bfloat16, device=DEV)
+    dy[ends] = rand((400, n), 4, 1e-2)
+    y, saved = gws.linear_fwd(x, w, b, activation=kind, save=gws.ACT8_INT8)
+    z, e = pre_activation(x[ends], w, b)
+    a, _ = act(z, kind)
+    assert within(y[ends], a, 2.0 ** -8 * a.abs() + 1.2 * e + 2.0 ** -18 * a.abs() + 1e-38)
+    kept = gws.act8_load(saved)[ends].double()
+    top = torch.nn.functional.pad(z.abs() + e, (0, -n % 32)).view(400, -1, 32).amax(-1)
+    assert within(kept, z, (torch.exp2(torch.floor(torch.log2(top))) / 64).repeat_interleave(32, 1)[:, :n] + e)
+    dx, dw, db, again = gws.linear_bwd(dy, x, w, saved, kind, want_grad_bias=True, want_act=True, bias_dtype=torch.float32)
+    # rows without a gradient add nothing to the sums, and no rounding
+    check_backward(dy[ends], x[ends].double(), w, None, kept, kind, (dx[ends], dw, db, again[ends]), torch.float32)
+    assert not bool(dx[200:m - 200].any())
+
+
 def test_refusals():
     x, w, b, r, dy = problem(8, 32, 24)
     y, saved = gws.linear_fwd(x, w, b, activation=gws.GATED_SILU, save=gws.ACT8_INT8)

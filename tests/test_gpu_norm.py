@@ -184,6 +184,22 @@ def test_another_stream_and_a_captured_pass():
     assert all(torch.equal(p, q) for p, q in zip(out, both()))
 
 
+def test_offsets_that_pass_32_bits():
+    m, n = (1 << 20) + 77, 2056
+    ends = torch.cat([torch.arange(200), torch.arange(m - 200, m)]).to(DEV)
+    x, r, dy = (torch.empty(m, n, dtype=torch.bfloat16, device=DEV).normal_() for _ in range(3))
+    w, b = weights(n, "f32 bias")
+    y, s, stats = gws.layernorm_fwd(x, w, b, residual=r)
+    for got, want in zip((y, s), check_forward(x[ends], w, b, r[ends])):
+        assert torch.equal(got[ends], want)
+    dy[200:m - 200] = 0
+    dx, dw, db = gws.layernorm_bwd(dy, s, w, stats)
+    alone = check_backward(dy[ends], s[ends], w, stats[:, ends].contiguous())
+    assert torch.equal(dx[ends], alone[0]) and not bool(dx[200:m - 200].any())
+    (_, want_w, want_b), (_, e_w, e_b) = ref.norm_backward(dy[ends], s[ends], w, 1e-5)          # rows without a gradient add nothing, and no rounding
+    assert within(dw, want_w, e_w + ref.U32 * (want_w.abs() + e_w)) and within(db, want_b, e_b + ref.U32 * (want_b.abs() + e_b))
+
+
 def test_refusals():
     x = rand((4, 64), 1)
     w, b = weights(64, "bf16 bias")
