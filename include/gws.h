@@ -569,7 +569,8 @@ typedef struct gws_linear_desc {
   int32_t bias_type;                     /* gws_type of bias and its gradient                                                */
 } gws_linear_desc;
 int64_t gws_linear_workspace_bytes(const gws_linear_desc* desc, int backward);
-/* Forward, in one kernel (a second one joins the parts of tiles whose contraction is cut); z stays in FP32 until y is rounded.
+/* Forward, in one kernel (a second one joins the parts of tiles whose contraction is cut; up to four tokens take a kernel that streams the rows of W); z stays
+ * in FP32 until y is rounded.
  *   x  device, BF16 [m, ld_x]      w  device, BF16 [n, ld_w]      bias  device, [n] of bias_type, or NULL      residual  device, BF16 [m, ld_residual], or NULL
  *   y  device, BF16 [m, ld_y], written      save  device, checkpoint [m, n] or BF16 [m, n] (dense), rounded from the FP32 z, written; NULL with GWS_SAVE_NONE */
 int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, const void* bias, const void* residual, void* y, void* save, void* workspace,
@@ -614,7 +615,8 @@ int gws_layernorm_bwd(const gws_norm_desc* desc, const void* grad_y, const void*
 /* One AdamW step over many tensors at once (one launch for up to 384 of them):
  *   g = grad * grad_scale     m = b1 m + (1 - b1) g     v = b2 v + (1 - b2) g g     r = sqrt(v)
  *   p = p (1 - lr wd) - (m alpha) / (r rho + eps),     alpha = lr / (1 - b1^step),  rho = 1 / sqrt(1 - b2^step)
- * in FP32, every operation rounded once in the order written (alpha, rho and 1 - lr wd are computed in double and rounded once).
+ * in FP32, every operation rounded once in the order written (alpha, rho and 1 - lr wd are computed in double and rounded once, with lr_dev or step_dev from wd rounded to FP32; where |m alpha| is
+ * below 2^-100 the quotient may be one unit of its last place off).
  *
  * State: tensor i owns the elements [starts[i], starts[i] + sizes[i] rounded up to 256) of arrays of `total` elements that all tensors share
  * (starts and total are multiples of 256; the elements past a size are kept zero; all of the state is zero before the first step).

@@ -32,6 +32,9 @@
 // operands of the same sizes, [16384, 2048] by [11264, 2048]^T, [16384, 11264] by [11264, 2048] and [16384, 11264]^T by [16384, 2048],
 // 589 to 600, 568 to 582 and 577 to 595 us.
 //
+// The linear layer's products are the same tiles: 16384 tokens, 2048 x 5632, in a burst, us (torch.matmul on BF16 operands of the same sizes): forward 275, with GELU, bias and an INT8 copy of z
+// 279 (267); dx 259 (272); dW 270 (295).  Up to 128 tokens take narrow tiles (33 tokens, 768 x 2048: 9.3 -> 5.4 us), up to four k_linear_row (gws_linear.cuh).
+//
 // Every wait of a role is a wait on an mbarrier and has a limit (about a second); one that runs out has the status word set and ends its
 // role, the roles that depend on it run out in turn, the block gives its copies time to land, frees its tensor memory and returns.
 // What has no limit waits for something that does not depend on a role's success:
