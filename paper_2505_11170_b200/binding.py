@@ -1169,7 +1169,7 @@ class AdamWState:
     groups of 256 with an FP32 unit).  ``rest`` holds the 16 bits that a 32-bit weight has below its BF16 parameter (int16 [total]); without it, None, BF16
     parameters are rounded at every step and lose updates smaller than half their spacing.  What is not given is allocated, as zeros; ``rest`` may be
     True, False, or such a tensor.  The tensors of a state are written where they are, and not replaced."""
-    __slots__ = ("sizes", "starts", "total", "fmt", "moments", "units", "rest", "_c_sizes", "_c_starts", "_c")
+    __slots__ = ("sizes", "starts", "total", "fmt", "_moments", "_units", "_rest", "_c_sizes", "_c_starts", "_c")
 
     def __init__(self, sizes: Sequence[int], fmt: int = ADAMW_F32, rest=False, device="cuda", moments: Optional[torch.Tensor] = None,
                  units: Optional[torch.Tensor] = None):
@@ -1193,13 +1193,12 @@ class AdamWState:
             self._take(units, "units", torch.float32, (2, total // _ADAMW_GROUP) if bits8 else None)
         if rest is not None:
             self._take(rest, "rest", torch.int16, (total,))
-        self.moments, self.units, self.rest = moments, units, rest
+        self._moments, self._units, self._rest = moments, units, rest
         self._c = _AdamwState(moments.data_ptr(), _addr(units), _addr(rest), total, fmt, 0)
 
-    def __setattr__(self, name, value) -> None:
-        if hasattr(self, name):
-            raise AttributeError("gws: a state's %s is not replaced" % name)
-        object.__setattr__(self, name, value)
+    moments = property(lambda self: self._moments)       # their addresses are in _c
+    units = property(lambda self: self._units)
+    rest = property(lambda self: self._rest)
 
     def __reduce__(self):
         return AdamWState, (self.sizes, self.fmt, False if self.rest is None else self.rest, self.moments.device, self.moments, self.units)
