@@ -114,7 +114,8 @@ __device__ __forceinline__ void norm_weights(const void* w, bool f32, float none
 // Blocks of the forward kernel that an SM holds.
 constexpr int norm_blocks(int team, bool wide) { return team <= 256 ? (wide ? 4 : 3) : wide && team <= 512 ? 2 : 1; }
 
-// Sums of two values over a team; every thread of the block calls it the same number of times.  `room`: [2][threads / 32], used in turn.
+// Sums of two values over a team; every thread of the team calls it the same number of times.  `room`: [2][threads / 32], used in turn.  The teams of a block wait for themselves alone
+// (16384 x 1024 forward, two teams: 25.8 us when the block met, 23.7 so).
 template <int L>
 __device__ __forceinline__ float2 team_sum(float a, float b, float2* room, uint32_t& turn) {
 #pragma unroll
@@ -127,7 +128,8 @@ __device__ __forceinline__ float2 team_sum(float a, float b, float2* room, uint3
   float2* mine = room + turn * (blockDim.x / 32u);
   turn ^= 1u;
   if ((threadIdx.x & 31u) == 0u) mine[threadIdx.x >> 5] = make_float2(a, b);
-  __syncthreads();
+  if (L < 256) asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.x / L + 1u), "n"(L) : "memory");
+  else __syncthreads();
   const float2* from = mine + (threadIdx.x / L) * kWarps;
   float2 t = from[0];
 #pragma unroll
@@ -141,7 +143,7 @@ constexpr uint32_t kNormThreads = L < 256 ? 256u / L * L : static_cast<uint32_t>
 // Memory-bound: 2 or 4 bytes in, 2 or 4 out per element.  A team takes rows in turn, with the next row's words under way; weights stay in shared memory where the block's teams (or
 // its rows) share them, and the arithmetic is on pairs (one by one, a row to a warp and
 // its weights read for every row, took 41 us where this takes 28).
-// 16384 x 2048: 28 us (4.8 TB/s), with a residual 49 (5.5 TB/s); 16384 x 768 with a residual 22; 16384 x 1365, elements one by one, 56 (3.2 TB/s); one row 2.
+// 16384 x 2048: 28 us (4.8 TB/s), with a residual 49 (5.5 TB/s); 16384 x 768 with a residual 20; 16384 x 1365, elements one by one, 54 (3.3 TB/s); one row 2.
 template <int L, int C, bool WIDE>
 __global__ void __launch_bounds__(kNormThreads<L>, norm_blocks(L, WIDE)) k_norm_fwd(const __grid_constant__ NormArgs p) {
   after_previous();
@@ -284,7 +286,7 @@ __global__ void __launch_bounds__(kNormLong) k_norm_fwd_long(const __grid_consta
 }
 
 // Memory-bound: 4 or 6 bytes in, 2 out per element.  16384 x 2048: with grad_sum 45 us (6.0 TB/s), 52 with the sums of the weight's and the bias's gradients (a launch of a few us);
-// without the next row's loads under way 106.  16384 x 1365, elements one by one, 67.
+// without the next row's loads under way 106.  16384 x 1365, elements one by one, 65.
 template <int L, int C, bool WIDE>
 __global__ void __launch_bounds__(kNormThreads<L>, L <= 256 ? 2 : 1) k_norm_bwd(const __grid_constant__ NormArgs p) {
   after_previous();
