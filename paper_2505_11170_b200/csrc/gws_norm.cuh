@@ -111,8 +111,12 @@ __device__ __forceinline__ void norm_weights(const void* w, bool f32, float none
   }
 }
 
-// Blocks of the forward kernel that an SM holds.
-constexpr int norm_blocks(int team, bool wide) { return team <= 256 ? (wide ? 4 : 3) : wide && team <= 512 ? 2 : 1; }
+// Blocks of the forward kernel that an SM holds: as many as leave a thread registers for its row and the next one.  us with a residual, one block more or less beside it: 16384 x 2048
+// 46 (four: 49), x 768 18 (four: 20.5), 4096 x 3000 17.0 (three: 18.5), 4096 x 4096 22.8 (three: 23.5); elements one by one, 16384 x 1365 46 (three: 54, five: 66), x 767 29 (four:
+// 32.5), 8192 x 4001 67 (three: 72), 4096 x 6001 77 (one: 116).
+constexpr int norm_blocks(int team, bool wide) {
+  return team > 512 ? 1 : team > 256 ? 2 : team == 256 || team == 192 || (team == 96 && !wide) ? 4 : 3;
+}
 
 // Sums of two values over a team; every thread of the team calls it the same number of times.  `room`: [2][threads / 32], used in turn.  The teams of a block wait for themselves alone
 // (16384 x 1024 forward, two teams: 25.8 us when the block met, 23.7 so).
@@ -143,7 +147,7 @@ constexpr uint32_t kNormThreads = L < 256 ? 256u / L * L : static_cast<uint32_t>
 // Memory-bound: 2 or 4 bytes in, 2 or 4 out per element.  A team takes rows in turn, with the next row's words under way; weights stay in shared memory where the block's teams (or
 // its rows) share them, and the arithmetic is on pairs (one by one, a row to a warp and
 // its weights read for every row, took 41 us where this takes 28).
-// 16384 x 2048: 28 us (4.8 TB/s), with a residual 49 (5.5 TB/s); 16384 x 768 with a residual 20; 16384 x 1365, elements one by one, 54 (3.3 TB/s); one row 2.
+// 16384 x 2048: 28 us (4.8 TB/s), with a residual 46 (5.8 TB/s); 16384 x 768 with a residual 18; 16384 x 1365, elements one by one, 46 (3.9 TB/s); one row 2.
 template <int L, int C, bool WIDE>
 __global__ void __launch_bounds__(kNormThreads<L>, norm_blocks(L, WIDE)) k_norm_fwd(const __grid_constant__ NormArgs p) {
   after_previous();
