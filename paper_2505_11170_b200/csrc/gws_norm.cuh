@@ -132,7 +132,7 @@ __device__ __forceinline__ float2 team_sum(float a, float b, float2* room, uint3
   float2* mine = room + turn * (blockDim.x / 32u);
   turn ^= 1u;
   if ((threadIdx.x & 31u) == 0u) mine[threadIdx.x >> 5] = make_float2(a, b);
-  if (L < 256) asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.x / L + 1u), "n"(L) : "memory");
+  if (L <= 256) asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.x / L + 1u), "n"(L) : "memory");
   else __syncthreads();
   const float2* from = mine + (threadIdx.x / L) * kWarps;
   float2 t = from[0];
@@ -143,6 +143,10 @@ __device__ __forceinline__ float2 team_sum(float a, float b, float2* room, uint3
 
 template <int L>
 constexpr uint32_t kNormThreads = L < 256 ? 256u / L * L : static_cast<uint32_t>(L);          // of a block
+// Of a block of the backward kernel, whose sums over its teams are a part each: large blocks leave half of the parts (1000 x 4096 20 -> 15 us), but small teams are joined one after
+// the other (300 x 768 in blocks of eight teams 6.0 us, of four 5.0).
+template <int L>
+constexpr uint32_t kNormBackThreads = L < 128 ? 256u / L * L : L < 512 ? 512u / L * L : static_cast<uint32_t>(L);
 
 // Memory-bound: 2 or 4 bytes in, 2 or 4 out per element.  A team takes rows in turn, with the next row's words under way; weights stay in shared memory where the block's teams (or
 // its rows) share them, and the arithmetic is on pairs (one by one, a row to a warp and
@@ -289,15 +293,14 @@ __global__ void __launch_bounds__(kNormLong) k_norm_fwd_long(const __grid_consta
   }
 }
 
-// Memory-bound: 4 or 6 bytes in, 2 out per element.  16384 x 2048: with grad_sum 45 us (6.0 TB/s), 52 with the sums of the weight's and the bias's gradients (a launch of a few us);
-// without the next row's loads under way 106.  16384 x 1365, elements one by one, 65.
+// Memory-bound: 4 or 6 bytes in, 2 out per element.  16384 x 2048: with grad_sum 45 us (6.0 TB/s), 48 with the sums of the weight's and the bias's gradients (parts in stores of
+// 32 bytes, whose join is a launch; word by word 50); without the next row's loads under way 106.  4096 x 5632 41, 1000 x 4096 10.5.  16384 x 1365, elements one by one, 64.
 template <int L, int C, bool WIDE>
-__global__ void __launch_bounds__(kNormThreads<L>, L <= 256 ? 2 : 1) k_norm_bwd(const __grid_constant__ NormArgs p) {
+__global__ void __launch_bounds__(kNormBackThreads<L>, L < 128 ? 2 : 1) k_norm_bwd(const __grid_constant__ NormArgs p) {
   after_previous();
-  constexpr uint32_t kTeams = kNormThreads<L> / L;
-  __shared__ float2 room[2][kNormThreads<L> / 32u];
-  __shared__ float4 held[2 * C][L];                      // the weights, the same for every team and row
-  __shared__ float4 joined[kTeams > 1u ? 4 * C : 1u][kTeams > 1u ? L : 1u];
+  constexpr uint32_t kTeams = kNormBackThreads<L> / L;
+  __shared__ float2 room[2][kNormBackThreads<L> / 32u];
+  __shared__ float4 held[kTeams > 1u ? 4 * C : 2 * C][L];                      // the weights, the same for every team and row; then the sums over the teams
   uint32_t turn = 0;
   const uint32_t lane = threadIdx.x % L, team = threadIdx.x / L;
   const float inv = 1.0f / static_cast<float>(p.cols);
@@ -370,12 +373,13 @@ __global__ void __launch_bounds__(kNormThreads<L>, L <= 256 ? 2 : 1) k_norm_bwd(
     }
   }
   if (p.part == nullptr) return;
-  if (kTeams > 1u) {
+  if constexpr (kTeams > 1u) {
+    __syncthreads();
     for (uint32_t t = 0; t < kTeams; ++t) {
       if (team == t) {
 #pragma unroll
         for (int i = 0; i < 4 * C; ++i) {
-          float4& j = joined[i][lane];
+          float4& j = held[i][lane];
           const float4 g = make_float4(first_of(gw[i]), second_of(gw[i]), first_of(gb[i]), second_of(gb[i]));
           j = t == 0u ? g : make_float4(j.x + g.x, j.y + g.y, j.z + g.z, j.w + g.w);
         }
@@ -385,12 +389,30 @@ __global__ void __launch_bounds__(kNormThreads<L>, L <= 256 ? 2 : 1) k_norm_bwd(
     if (team != 0u) return;
 #pragma unroll
     for (int i = 0; i < 4 * C; ++i) {
-      const float4 j = joined[i][lane];
+      const float4 j = held[i][lane];
       gw[i] = two(j.x, j.y);
       gb[i] = two(j.z, j.w);
     }
   }
   float* part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.cols;
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = norm_col<L, WIDE>(lane, c, 0);
+      if (col >= p.cols) continue;
+      V8 w, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w.x[2 * i] = __float_as_uint(first_of(gw[4 * c + i]));
+        w.x[2 * i + 1] = __float_as_uint(second_of(gw[4 * c + i]));
+        b.x[2 * i] = __float_as_uint(first_of(gb[4 * c + i]));
+        b.x[2 * i + 1] = __float_as_uint(second_of(gb[4 * c + i]));
+      }
+      st32(part + col, w);
+      st32(part + p.cols + col, b);
+    }
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 8 * C; ++e) {
     const int64_t col = norm_col<L, WIDE>(lane, e / 8, e % 8);

@@ -64,21 +64,21 @@ NormBack norm_back(int64_t rows, int64_t cols) {
   const int sms = sm_count();
   if (norm_team(cols) == 0) return {0, static_cast<uint32_t>(std::min<int64_t>(64, (rows + 31) / 32))};
   const int team = norm_team(cols);
-  const int64_t teams = norm_teams(team);
-  return {team, static_cast<uint32_t>(std::min<int64_t>((rows + teams - 1) / teams, static_cast<int64_t>(sms) * (team <= 256 ? 2 : 1)))};
+  const int64_t teams = team < 128 ? 256 / team : std::max(1, 512 / team);
+  return {team, static_cast<uint32_t>(std::min<int64_t>((rows + teams - 1) / teams, static_cast<int64_t>(sms) * (team < 128 ? 2 : 1)))};
 }
 template <bool WIDE>
 int launch_norm_bwd(const NormArgs& a, const NormBack& b, cudaStream_t s) {
   const char* what = "layer norm backward kernel";
-  if (b.team == 32 && a.cols <= 256) return launch(k_norm_bwd<32, 1, WIDE>, b.blocks, 256, 0, 1, s, what, a);
-  if (b.team == 32) return launch(k_norm_bwd<32, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
-  if (b.team == 64) return launch(k_norm_bwd<64, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
-  if (b.team == 96) return launch(k_norm_bwd<96, 2, WIDE>, b.blocks, kNormThreads<96>, 0, 1, s, what, a);
-  if (b.team == 128) return launch(k_norm_bwd<128, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
-  if (b.team == 192) return launch(k_norm_bwd<192, 2, WIDE>, b.blocks, kNormThreads<192>, 0, 1, s, what, a);
-  if (b.team == 256) return launch(k_norm_bwd<256, 2, WIDE>, b.blocks, 256, 0, 1, s, what, a);
-  if (b.team == 384) return launch(k_norm_bwd<384, 2, WIDE>, b.blocks, 384, 0, 1, s, what, a);
-  return launch(k_norm_bwd<512, 2, WIDE>, b.blocks, 512, 0, 1, s, what, a);
+  if (b.team == 32 && a.cols <= 256) return launch(k_norm_bwd<32, 1, WIDE>, b.blocks, kNormBackThreads<32>, 0, 1, s, what, a);
+  if (b.team == 32) return launch(k_norm_bwd<32, 2, WIDE>, b.blocks, kNormBackThreads<32>, 0, 1, s, what, a);
+  if (b.team == 64) return launch(k_norm_bwd<64, 2, WIDE>, b.blocks, kNormBackThreads<64>, 0, 1, s, what, a);
+  if (b.team == 96) return launch(k_norm_bwd<96, 2, WIDE>, b.blocks, kNormBackThreads<96>, 0, 1, s, what, a);
+  if (b.team == 128) return launch(k_norm_bwd<128, 2, WIDE>, b.blocks, kNormBackThreads<128>, 0, 1, s, what, a);
+  if (b.team == 192) return launch(k_norm_bwd<192, 2, WIDE>, b.blocks, kNormBackThreads<192>, 0, 1, s, what, a);
+  if (b.team == 256) return launch(k_norm_bwd<256, 2, WIDE>, b.blocks, kNormBackThreads<256>, 0, 1, s, what, a);
+  if (b.team == 384) return launch(k_norm_bwd<384, 2, WIDE>, b.blocks, kNormBackThreads<384>, 0, 1, s, what, a);
+  return launch(k_norm_bwd<512, 2, WIDE>, b.blocks, kNormBackThreads<512>, 0, 1, s, what, a);
 }
 
 int clear(void* p, int64_t bytes, cudaStream_t s) {
