@@ -1232,6 +1232,10 @@ class AdamWState:
         return ((param.detach().view(torch.int16).to(torch.int32) << 16) + low.to(torch.int32)).view(torch.float32)
 
 
+# Methods of many tensors at once, by map: a third less time of the host than list comprehensions.
+_numel, _is_contiguous, _get_device, _data_ptr = torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr
+
+
 @functools.lru_cache(maxsize=64)
 def _adamw_types(dtypes: tuple):
     known = {_BF16: TYPE_BF16, torch.float32: TYPE_F32}
@@ -1265,17 +1269,17 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
         where = [i for i, g in enumerate(grads) if g is not None]
         params, grads, sizes = [params[i] for i in where], [grads[i] for i in where], [sizes[i] for i in where]
     dtypes = [p.dtype for p in params]
-    if dtypes != [g.dtype for g in grads] or [p.shape for p in params] != [g.shape for g in grads] or [p.numel() for p in params] != sizes:
+    if dtypes != [g.dtype for g in grads] or [p.shape for p in params] != [g.shape for g in grads] or list(map(_numel, params)) != sizes:
         raise ValueError("gws: a gradient has its parameter's type and shape, and the parameter the state's size")
-    if not all([p.is_contiguous() for p in params]):
+    if not all(map(_is_contiguous, params)):
         raise ValueError("gws: parameters are contiguous")
-    if sizes and ({p.get_device() for p in params} != {device} or {g.get_device() for g in grads} != {device}):
+    if sizes and (set(map(_get_device, params)) != {device} or set(map(_get_device, grads)) != {device}):
         _require_cuda(*params, *grads)
         raise ValueError("gws: the tensors of a call live on one device")
-    if not all([g.is_contiguous() for g in grads]):
+    if not all(map(_is_contiguous, grads)):
         grads = [g.contiguous() for g in grads]
     types = _adamw_types(tuple(dtypes))
-    p_params, p_grads = array.array("Q", [p.data_ptr() for p in params]), array.array("Q", [g.data_ptr() for g in grads])
+    p_params, p_grads = array.array("Q", list(map(_data_ptr, params))), array.array("Q", list(map(_data_ptr, grads)))
     if where is not None:                                # places without a gradient: null
         wide = [array.array("Q", bytes(8 * n)) for _ in range(2)] + [(c_int32 * n)()]
         for i, *entry in zip(where, p_params, p_grads, types):
