@@ -6,7 +6,7 @@
 // a row and eight columns to a lane, has the next rows' loads under way while it works on some, and keeps the column sums in registers.  The shares of a strip, where they
 // are eight at most, are the blocks of a cluster and joined through each other's shared memory in a fixed order; more of them leave their sums to k_column_sums.
 // 16384 x 5632, GELU from INT8 with act(z) and db: 90 us (5.2 TB/s) in calls alone, 113 with the join's launch and its wait; 165 before the loads ran ahead and the arithmetic was on pairs.
-// Odd widths read and write elements one by one: 2047 x 2729 17 us.
+// Odd widths read and write elements one by one: 2047 x 2729 16 us, 8192 x 2729 49 (3.2 TB/s).
 // The first blocks of the launch make ready what the products after it read (prepare).
 #pragma once
 #include <stdint.h>
@@ -215,21 +215,29 @@ __global__ void __launch_bounds__(kPreThreads, 6) k_linear_pre(const __grid_cons
       __syncwarp();
       return w;
     };
-#pragma unroll 1
-    for (int32_t at = 0; at < rows; at += kPreSlots) {
-      const int32_t row = at + static_cast<int32_t>(slot);
-      uint16_t vg[8], vz[8];
-      Raw r;
+    uint16_t vg[8], vz[8];
+    uint2 z8 = make_uint2(0u, 0u);
+    uint32_t byte = 0u;
+    auto fetch = [&](int32_t row) {
       if (has_dy) load(dy0, p.ld_dy, row, vg);
       if (SAVE == GWS_SAVE_BF16) load(z0, p.cols, row, vz);
       if (kIs8) {
         const bool real = row < rows && col < p.save8.ld;
         const int64_t from = (begin + row) * p.save8.ld + col;
-        r.z8 = real ? __ldg(reinterpret_cast<const uint2*>(p.save8.codes + from)) : make_uint2(0u, 0u);
-        r.byte = real ? p.save8.scales[from >> 5] : 0u;
+        z8 = real ? __ldg(reinterpret_cast<const uint2*>(p.save8.codes + from)) : make_uint2(0u, 0u);
+        byte = real ? p.save8.scales[from >> 5] : 0u;
       }
+    };
+    fetch(static_cast<int32_t>(slot));
+#pragma unroll 1
+    for (int32_t at = 0; at < rows; at += kPreSlots) {
+      const int32_t row = at + static_cast<int32_t>(slot);
+      Raw r;
+      r.z8 = z8;
+      r.byte = byte;
       if (has_dy) r.g = own(vg);
       if (SAVE == GWS_SAVE_BF16) r.z16 = own(vz);
+      if (at + static_cast<int32_t>(kPreSlots) < rows) fetch(row + static_cast<int32_t>(kPreSlots));
       F2 a[4], slope[4];
       element_wise(r, a, slope);
       if (has_dy) {
