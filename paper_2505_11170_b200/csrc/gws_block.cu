@@ -245,7 +245,7 @@ int launch_tc(const CUtensorMap (&maps)[4], const TcArgs& args, int sms, cudaStr
   if constexpr (MODE == kGatedFew || MODE == kLinearFew) return st;
   if (st != GWS_OK || args.cut == 0 || args.clustered) return st;
   constexpr uint32_t kWarps = (MODE == kGated ? BN / 64 : BN / 32) * (128 * CG / kJoinRows);       // per tile
-  return launch(k_join<CG, BN, MODE>, args.cut * (kWarps / 8), 256, 0, 1, s, "join of a cut contraction", args);
+  return launch(k_join<CG, BN, MODE == kLinearAlone ? kLinear : MODE>, args.cut * (kWarps / 8), 256, 0, 1, s, "join of a cut contraction", args);
 }
 
 template <int MODE>
@@ -994,7 +994,8 @@ int gws_linear_fwd(const gws_linear_desc* desc, const void* x, const void* w, co
   maps[1] = maps[0];
   if ((st = make_map(maps[2], mw.p, d.n, d.k, mw.ld, t.width != 0 ? t.width : static_cast<uint32_t>(t.bn / t.cg))) != GWS_OK) return st;
   maps[3] = maps[2];
-  return t.width != 0 ? launch_tc<1, 128, kLinearFew>(maps, args, sms, s) : launch_mode<kLinear>(t, maps, args, sms, s);
+  if (t.width != 0) return launch_tc<1, 128, kLinearFew>(maps, args, sms, s);
+  return residual != nullptr ? launch_mode<kLinear>(t, maps, args, sms, s) : launch_mode<kLinearAlone>(t, maps, args, sms, s);
 }
 
 int gws_linear_bwd(const gws_linear_desc* desc, const void* grad_y, const void* x, const void* w, const void* save, void* grad_x, void* grad_w, void* grad_bias,

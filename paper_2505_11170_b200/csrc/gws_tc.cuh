@@ -6,7 +6,7 @@
 //   kGatedFew  the same for up to 128 tokens, tiles of 16 to 64 columns of h: every SM gets its share of the weights, and a copy of A
 //            takes only the rows that exist, so that the ring holds more weights in flight.  It is bound by the weights' way from
 //            memory and some 4 us around it (one token, 2048 x 5632: 46 MB in 12 us, 10 from L2; 4096 x 11008: 180 MB in 33 us)
-//   kLinear, kLinearFew  y = act(x W^T + b) + r: bias, activation, residual and the copies of z = x W^T + b for the backward pass on registers in the epilogue
+//   kLinear, kLinearFew, kLinearAlone (the first without r)  y = act(x W^T + b) + r: bias, activation, residual and the copies of z = x W^T + b for the backward pass on registers in the epilogue
 //   kDx      dx = dg Wg + du Wu: one accumulator, the contraction runs over the columns of dg and then over those of du; dx = dz W is its first half
 //   kDw      dW = dY^T X: both operands are read along their contiguous (not the contracted) axis, as they lie in memory
 //   kDw8     the same with X an 8-bit checkpoint: its codes are copied to shared memory and eight more warps turn them into the BF16
@@ -51,7 +51,7 @@
 
 namespace {
 
-enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4, kLinear = 5, kLinearFew = 6 };
+enum { kGated = 0, kDx = 1, kDw = 2, kDw8 = 3, kGatedFew = 4, kLinear = 5, kLinearFew = 6, kLinearAlone = 7 };
 
 constexpr uint32_t kTcHalf = 64;                           // elements along the contraction per copy: 128 bytes, one swizzle atom
 constexpr uint32_t kTcABytes = 128u * kTcHalf * 2u;
@@ -536,7 +536,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
     k_tc(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b0,
          const __grid_constant__ CUtensorMap b1, const __grid_constant__ TcArgs p) {
   using S = TcShape<CG, BN, MODE>;
-  constexpr bool kFew = MODE == kGatedFew || MODE == kLinearFew, kIsGated = MODE == kGated || MODE == kGatedFew, kIsLinear = MODE == kLinear || MODE == kLinearFew;
+  constexpr bool kFew = MODE == kGatedFew || MODE == kLinearFew, kIsGated = MODE == kGated || MODE == kGatedFew, kIsLinear = MODE == kLinear || MODE == kLinearFew || MODE == kLinearAlone;
   constexpr bool kIsDw = MODE == kDw || MODE == kDw8;
   constexpr bool kMnA = kIsDw, kMnB = !kIsGated && !kIsLinear;
   constexpr uint32_t kStages = S::kStages;
@@ -732,7 +732,8 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
       const bool second = kIsDw && mt >= p.tiles_per_out;
       const int64_t row0 = static_cast<int64_t>(second ? mt - p.tiles_per_out : mt) * (128 * CG) + rank * 128u + quadrant * 32u;
       // The residual of the chunk to come, where a lane reads its own row: under the products, then under the stores of the chunk before.  16384 x 768 x 768: 26.1 -> 24.6 us,
-      // 16384 x 2048 x 768 66 -> 61; without a residual it costs 0 to 1 us.
+      // 16384 x 2048 x 768 66 -> 61.  Its registers would cost a launch
+      // without a residual 1 to 4 %; that has a kernel of its own (16384 x 2048 x 768, GELU and INT8: 58.5 us when one served both, 56.4 so).
       uint32_t r[16];
       const bool ahead = MODE == kLinear && p.residual != nullptr && p.residual_wide == 16 && t < p.whole;
       auto fetch = [&](uint32_t c) {
@@ -788,7 +789,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           if (col0 >= edge) break;
           uint32_t v[32], w[16];
           acc_load(acc + c * 32u, v);
-          if (p.residual != nullptr && (!ahead || col0 + 32 > edge)) load_block(p.residual, p.ld_residual, p.residual_wide, row0, col0, p.rows, edge, r, stage, lane);
+          if (MODE != kLinearAlone && p.residual != nullptr && (!ahead || col0 + 32 > edge)) load_block(p.residual, p.ld_residual, p.residual_wide, row0, col0, p.rows, edge, r, stage, lane);
           acc_wait();
           float z[32];
 #pragma unroll
@@ -868,7 +869,7 @@ __global__ void __launch_bounds__((TcShape<CG, BN, MODE>::kThreads), 1)
           store_block(out, p.ld_out, p.wide, row0, col0, p.rows, p.cols, w, stage, lane);
         }
       }
-      if ((kIsGated || MODE == kLinear) && t < p.whole && (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3)) {
+      if ((kIsGated || MODE == kLinear || MODE == kLinearAlone) && t < p.whole && (p.save == GWS_ACT8_INT8 || p.save == GWS_ACT8_E4M3)) {
         // The scale bytes of a row's groups in this tile leave together: one store of a byte each cost 20 us of 514 (16384 x 2048 x 5632).
         // The two warps that share these rows meet; one writes the gate's (or the left half's), the other the up projection's (the right half's).  A warp that fills the same
         // buffer again has passed the meeting of the tile between, and so has the other one's store.  They meet at an mbarrier, one
