@@ -145,6 +145,25 @@ def test_every_tiling(blocks, columns, form, m, n, k):
         check_kept(saved, save, z, e)
 
 
+@pytest.mark.parametrize("blocks,columns,form,m,n,k", TILINGS[14:])
+def test_every_tiling_without_a_residual(blocks, columns, form, m, n, k):
+    x, w, b, _, _ = problem(m, n, k, "f32")
+    for save in (gws.ACT8_INT8, gws.SAVE_BF16):
+        _, saved, z, e = check_forward(x, w, b, None, gws.GATED_SILU, save)
+        check_kept(saved, save, z, e)
+
+
+# residuals in rows that a lane reads by whole lines: tiles of 128 and 256 columns, one wave and several, whole and cut, widths that end inside a chunk of 32 columns
+@pytest.mark.parametrize("m,n,k", [(300, 528, 136), (2650, 912, 448), (2049, 1008, 64), (1112, 3760, 1200), (3002, 880, 3840), (4100, 2064, 72), (129, 16, 4096)])
+def test_residuals_of_whole_lines(m, n, k):
+    x, w, b, r, _ = problem(m, n, k)
+    first = check_forward(x, w, b, r, gws.ACT_NONE, gws.ACT8_INT8)[0]
+    check_forward(x, w, b, r, gws.GATED_GELU_TANH)
+    wide = torch.cat([r, r], 1)
+    assert torch.equal(gws.linear_fwd(x, w, b, residual=wide[:, n:], save=gws.ACT8_INT8)[0], first)
+    assert torch.equal(gws.linear_fwd(x, w, b, residual=wide[:, :n].t().contiguous().t(), save=gws.ACT8_INT8)[0], first)
+
+
 @pytest.mark.parametrize("n,k", [(136, 72), (137, 71), (64, 2048)])
 def test_strides_and_alignments(n, k):
     m = 45

@@ -76,6 +76,18 @@ def test_residual_stream(m, n):
     check_backward(dy, s, w, stats, True, d)
 
 
+# more rows than the teams of all blocks hold at once, for every kind of team
+@pytest.mark.parametrize("m,n", [(5001, 256), (5003, 255), (3001, 768), (3000, 769), (3001, 1360), (2500, 1365), (1501, 3000), (1500, 3001), (1001, 4096), (1000, 4095), (701, 6000), (700, 6001),
+                                 (501, 8192), (500, 8191)])
+def test_rows_in_turn(m, n):
+    x, r, dy, d = rand((m, n), 1), rand((m, n), 2, 2.0), rand((m, n), 3, 1e-2), rand((m, n), 4, 1e-2)
+    w, b = weights(n, "f32 bias")
+    _, s, stats = check_forward(x, w, b, r)
+    first = check_backward(dy, s, w, stats, True, d)
+    again = gws.layernorm_bwd(dy, s, w, stats, grad_sum=d)
+    assert all(torch.equal(p, q) for p, q in zip(first, again))
+
+
 @pytest.mark.parametrize("n", [96, 1365, 2048, 9000])
 def test_strides_and_alignments(n):
     m = 37
