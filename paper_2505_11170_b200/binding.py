@@ -1193,6 +1193,8 @@ class AdamWState:
             self._take(units, "units", torch.float32, (2, total // _ADAMW_GROUP) if bits8 else None)
         if rest is not None:
             self._take(rest, "rest", torch.int16, (total,))
+        if any(t is not None and t.device != moments.device for t in (units, rest)):
+            raise ValueError("gws: the tensors of a state live on one device")
         self._moments, self._units, self._rest = moments, units, rest
         self._c = _AdamwState(moments.data_ptr(), _addr(units), _addr(rest), total, fmt, 0)
 
