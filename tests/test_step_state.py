@@ -7,8 +7,8 @@ import paper_2505_11170_b200 as gws
 
 def _tensors(fmt, device):
     bits8 = fmt == gws.ADAMW_8BIT
-    return dict(moments=torch.zeros(2, 512, dtype=torch.uint8 if bits8 else torch.float32, device=device), units=torch.zeros(2, 2, device=device) if bits8 else None,
-                rest=torch.zeros(512, dtype=torch.int16, device=device))
+    return dict(moments=torch.zeros(2, 768, dtype=torch.uint8 if bits8 else torch.float32, device=device), units=torch.zeros(2, 3, device=device) if bits8 else None,
+                rest=torch.zeros(768, dtype=torch.int16, device=device))
 
 
 @pytest.mark.parametrize("fmt", [gws.ADAMW_F32, gws.ADAMW_8BIT])
