@@ -109,7 +109,8 @@ class GaussWSAdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def load_state_dict(self, state_dict) -> None:
-        """Takes over the state of an optimizer over tensors of the same sizes and with moments of the same format."""
+        """Takes over the state of an optimizer over tensors of the same sizes and with moments of the same format.  Count, moments, rest and a learning rate that is a tensor are
+        written where they are, so that a captured step goes on from them; its betas, eps and decays stay those of its capture."""
         kept = state_dict.get("gws")
         if kept is None or kept["moments"] != self._moments:
             raise ValueError("gws: the state is of another optimizer or of another format of moments")
@@ -120,7 +121,10 @@ class GaussWSAdamW(torch.optim.Optimizer):
         rest = self._rest and any(p.dtype == torch.bfloat16 for p in self._all())
         if s is not None and (s["rest"] is not None) != rest:
             raise ValueError("gws: one of the optimizers keeps the rest of its weights, the other does not")
+        rates = [g["lr"] for g in self.param_groups]
+        self._check_rates(rates, state_dict["param_groups"])
         super().load_state_dict({k: v for k, v in state_dict.items() if k != "gws"})
+        self._take_rates(rates)
         if isinstance(self._count, torch.Tensor):
             self._count.fill_(kept["count"])              # captured steps read it where it is
         else:
@@ -135,6 +139,30 @@ class GaussWSAdamW(torch.optim.Optimizer):
         for to, source in ((mine.moments, s["moments"]), (mine.units, s["units"]), (mine.rest, s["rest"])):
             if to is not None:
                 to.copy_(source)
+
+    def _check_rates(self, rates, groups) -> None:
+        """Whether groups that share a rate's tensor are to take different rates, where a captured step may read it."""
+        takes = {}
+        for lr, group in zip(rates, groups):
+            if isinstance(group["lr"], torch.Tensor) and group["lr"].numel() != 1:
+                raise ValueError("gws: a learning rate is one number")
+            if isinstance(lr, torch.Tensor) and takes.setdefault(id(lr), float(group["lr"])) != float(group["lr"]) and self._capturable and self._state is not None:
+                raise ValueError("gws: groups share a learning rate on the device, of which captured steps may know, and the state has several")
+
+    def _take_rates(self, rates) -> None:
+        """The groups' loaded rates: into the tensors that the groups had, which captured steps read where they are; as numbers, or FP32 tensors beside the parameters, otherwise."""
+        takes, moved = {}, {}
+        for lr, group in zip(rates, self.param_groups):
+            loaded = group["lr"]
+            if isinstance(lr, torch.Tensor):
+                rate = float(loaded)
+                if takes.setdefault(id(lr), rate) != rate:
+                    lr = torch.full_like(lr, rate)
+                group["lr"] = lr.fill_(rate)
+            elif isinstance(loaded, torch.Tensor):
+                if id(loaded) not in moved:
+                    moved[id(loaded)] = loaded.to(device=group["params"][0].device, dtype=torch.float32)
+                group["lr"] = moved[id(loaded)]
 
     def __getstate__(self):
         return {**super().__getstate__(), "_moments": self._moments, "_rest": self._rest, "_capturable": self._capturable, "_state": self._state, "_count": self._count}

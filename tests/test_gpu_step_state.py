@@ -1,0 +1,54 @@
+"""States of GaussWSAdamW that are loaded between replays of a captured step."""
+import copy
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_11170_b200 as gws
+from paper_2505_11170_b200.optimizer import GaussWSAdamW
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _optimizer(rate, capturable, moments):
+    torch.manual_seed(8)
+    params = [torch.nn.Parameter(torch.randn(n, device=DEV).to(t)) for n, t in ((1000, torch.bfloat16), (77, torch.float32))]
+    for p in params:
+        p.grad = torch.randn_like(p)
+    return params, GaussWSAdamW(params, lr=torch.full((1,), rate, device=DEV) if capturable else rate, capturable=capturable, weight_decay=0.0, moments=moments)
+
+
+@pytest.mark.parametrize("moments", [gws.ADAMW_F32, gws.ADAMW_8BIT])
+def test_a_captured_step_goes_on_from_a_loaded_state(moments):
+    (p, o), (q, e) = _optimizer(1e-3, True, moments), _optimizer(1e-3, True, moments)
+    o.step()
+    e.step()
+    weights, kept = [t.detach().clone() for t in p], copy.deepcopy(o.state_dict())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o.step()
+    graph.replay()
+    for where in ("cuda", "cpu"):
+        there = copy.deepcopy(kept)
+        there["param_groups"][0]["lr"] = kept["param_groups"][0]["lr"].to(where) * 2
+        there["gws"]["state"] = {k: t.to(where) if isinstance(t, torch.Tensor) else t for k, t in kept["gws"]["state"].items()}
+        o.load_state_dict(there)
+        e.load_state_dict(there)
+        with torch.no_grad():
+            for a, b, w in zip(p, q, weights):
+                a.copy_(w)
+                b.copy_(w)
+        rate = e.param_groups[0]["lr"]
+        assert rate.device.type == "cuda" and float(rate) == float(np.float32(1e-3) * 2)
+        for factor in (1.0, 0.5):
+            o.param_groups[0]["lr"].mul_(factor)
+            rate.mul_(factor)
+            graph.replay()
+            e.step()
+            torch.cuda.synchronize()
+            for a, b in zip(p, q):
+                assert torch.equal(a, b) and torch.equal(o.weight(a), e.weight(b))
+        assert o.state_dict()["gws"]["count"] == e.state_dict()["gws"]["count"] == 3
+        assert torch.equal(o._state.moments, e._state.moments)

@@ -3,6 +3,30 @@ import pytest
 import torch
 
 import paper_2505_11170_b200 as gws
+from paper_2505_11170_b200 import binding
+from paper_2505_11170_b200.optimizer import GaussWSAdamW
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    """adamw_step with its arguments written down, and nothing done."""
+    calls = []
+    monkeypatch.setattr(binding, "adamw_step", lambda params, grads, state, **more: calls.append(dict(grads=[g is not None for g in grads], **more)))
+    return calls
+
+
+def _parameter(*shape, dtype=torch.bfloat16):
+    p = torch.nn.Parameter(torch.ones(*shape, dtype=dtype))
+    p.grad = torch.ones_like(p)
+    return p
+
+
+def _rate(value):
+    return torch.full((1,), value)
+
+
+def _two_groups(first, second, **more):
+    return GaussWSAdamW([dict(params=[_parameter(300)], lr=first), dict(params=[_parameter(7)], lr=second)], **more)
 
 
 def _tensors(fmt, device):
@@ -22,3 +46,52 @@ def test_the_tensors_of_a_state_live_on_one_device(fmt):
                 gws.AdamWState([300, 40], fmt, **{**here, name: there[name]})
     with pytest.raises(ValueError, match="one device"):
         gws.AdamWState([300, 40], fmt, device="cpu", rest=there["rest"])
+
+
+def test_a_loaded_rate_goes_where_the_present_one_is(recorded):
+    """A captured step reads a rate on the device by its address."""
+    source, shared = _two_groups(5e-4, _rate(2e-3)), _rate(1e-3)
+    source.step()
+    optimizer = _two_groups(_rate(1e-3), _rate(1e-3), capturable=True)
+    optimizer.step()
+    held = [g["lr"] for g in optimizer.param_groups]
+    optimizer.load_state_dict(source.state_dict())
+    assert [g["lr"] for g in optimizer.param_groups] == held and all(g["lr"] is lr for g, lr in zip(optimizer.param_groups, held))
+    assert torch.equal(held[0], _rate(5e-4)) and torch.equal(held[1], _rate(2e-3))
+    source.param_groups[1]["lr"].fill_(9.0)                   # the loaded one is a copy
+    optimizer.step()
+    assert [c["lr"] for c in recorded[-2:]] == held and torch.equal(held[1], _rate(2e-3))
+    # one tensor for both groups stays one where both take the same
+    alike = _two_groups(3e-3, 3e-3)
+    optimizer = _two_groups(shared, shared, capturable=True)
+    optimizer.step()
+    optimizer.load_state_dict(alike.state_dict())
+    assert all(g["lr"] is shared for g in optimizer.param_groups) and torch.equal(shared, _rate(3e-3))
+
+
+def test_rates_that_a_shared_tensor_cannot_hold(recorded):
+    source, shared = _two_groups(5e-4, 2e-3), _rate(1e-3)
+    source.step()
+    optimizer = _two_groups(shared, shared, capturable=True)
+    optimizer.step()
+    with pytest.raises(ValueError):
+        optimizer.load_state_dict(source.state_dict())
+    assert torch.equal(shared, _rate(1e-3)) and int(optimizer._count) == 1 and all(g["lr"] is shared for g in optimizer.param_groups)
+    fresh = _two_groups(shared, shared)                       # no captured step can know of it: each group its own
+    fresh.load_state_dict(source.state_dict())
+    assert fresh.param_groups[0]["lr"] is shared and [float(g["lr"]) for g in fresh.param_groups] == [float(_rate(5e-4)), float(_rate(2e-3))]
+    state = source.state_dict()
+    state["param_groups"][0]["lr"] = torch.ones(2)
+    with pytest.raises(ValueError):
+        fresh.load_state_dict(state)
+
+
+def test_a_loaded_rate_beside_the_parameters(recorded):
+    """Where the present rate is a number: a tensor stays one, of FP32 and shared as it was."""
+    shared = torch.full((1,), 2e-3, dtype=torch.float64)
+    source, optimizer = _two_groups(shared, shared), _two_groups(1e-3, 1e-3)
+    optimizer.load_state_dict(source.state_dict())
+    rates = [g["lr"] for g in optimizer.param_groups]
+    assert rates[0] is rates[1] and rates[0].dtype == torch.float32 and rates[0].device == optimizer.param_groups[0]["params"][0].device
+    optimizer.step()
+    assert len(recorded) == 1
