@@ -651,6 +651,9 @@ typedef struct gws_adamw_step_args {
  * gradient lie on boundaries of eight elements are fastest.  A tensor, or a part of the state, that is given twice is GWS_ERR_ALIAS. */
 int gws_adamw_step(int n_tensors, void* const* params, const void* const* grads, const int64_t* sizes, const int64_t* starts, const int32_t* types,
                    const double* weight_decay, const gws_adamw_state* state, const gws_adamw_step_args* args, void* stream);
+/* What gws_adamw_step would answer, with nothing launched and `scalars` not needed: for a caller whose step takes several calls and is to be refused as a whole. */
+int gws_adamw_check(int n_tensors, void* const* params, const void* const* grads, const int64_t* sizes, const int64_t* starts, const int32_t* types,
+                    const double* weight_decay, const gws_adamw_state* state, const gws_adamw_step_args* args);
 /* What 8-bit moments stand for: m and v, device, FP32 [total], 32-byte aligned, written. */
 int gws_adamw_values(const gws_adamw_state* state, float* m, float* v, void* stream);
 

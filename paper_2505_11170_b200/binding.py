@@ -112,6 +112,7 @@ _SIGNATURES = {
     "gws_layernorm_fwd": (c_int, [c_void_p] * 9),
     "gws_layernorm_bwd": (c_int, [c_void_p] * 10 + [c_size_t, c_void_p]),
     "gws_adamw_step": (c_int, [c_int] + [c_void_p] * 9),
+    "gws_adamw_check": (c_int, [c_int] + [c_void_p] * 8),
     "gws_adamw_values": (c_int, [c_void_p] * 4),
     "gws_set_wait_limit": (c_int64, [c_int64]),
     "gws_layer_seed": (c_uint64, [c_uint64, c_uint64]),
@@ -1251,21 +1252,14 @@ def _adamw_decays(decays: tuple):
     return (ctypes.c_double * len(decays))(*[float(w) for w in decays])
 
 
-def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
-               step=1, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
-    """One AdamW step over all tensors, in place, in one launch (for up to 384 of them).
+def _adamw_counts(params, grads, state: AdamWState) -> None:
+    if len(params) != len(state.sizes) or len(grads) != len(state.sizes):
+        raise ValueError("gws: the state is of %d tensors" % len(state.sizes))
 
-    Parameters are BF16 or FP32 and contiguous, gradients of their type; a tensor whose gradient is None is left alone.  ``weight_decay`` is one number or one per tensor,
-    ``step`` counts from 1.  ``step`` (int64) and ``lr`` (FP32) may be one-element tensors on the device: a captured step that is replayed reads them as they are then.
-    ``grad_scale``, an FP32 one-element tensor on the device, multiplies the gradients (the factor of a clipped gradient norm)."""
+
+def _adamw_call(params, grads, state: AdamWState, device: int, lr, betas, eps: float, weight_decay, step, grad_scale):
+    """(the library's arguments, the arrays and tensors behind them, the parameters that are stepped), with everything checked that the library cannot see."""
     n = len(state.sizes)
-    if len(params) != n or len(grads) != n:
-        raise ValueError("gws: the state is of %d tensors" % n)
-    device = state.moments.get_device()
-    if device < 0:
-        _require_cuda(state.moments)
-    if stream is not None or device != _current_device():
-        return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale)
     sizes, where = state.sizes, None
     if any([g is None for g in grads]):
         where = [i for i, g in enumerate(grads) if g is not None]
@@ -1313,11 +1307,41 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
         args.step_dev = step.data_ptr()
     else:
         args.step = step
+    call = (n, p_params.buffer_info()[0], p_grads.buffer_info()[0], state._c_sizes, state._c_starts, types, decays, ctypes.addressof(state._c), ctypes.byref(args))
+    return call, args, (p_params, p_grads, grads), params
+
+
+def adamw_check(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
+                step=1, grad_scale: Optional[torch.Tensor] = None) -> None:
+    """Raises what :func:`adamw_step` would raise for these arguments, with nothing launched: for a step that takes several calls and is to be refused as a whole.  Of tensors on
+    the CPU, which only adamw_step itself refuses, the addresses are not checked."""
+    _adamw_counts(params, grads, state)
+    device = state.moments.get_device()
+    call, args, kept, params = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
+    if device >= 0:
+        code = (_lib or load_library()).gws_adamw_check(*call)
+        if code:
+            _check(code)
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
+               step=1, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One AdamW step over all tensors, in place, in one launch (for up to 384 of them).
+
+    Parameters are BF16 or FP32 and contiguous, gradients of their type; a tensor whose gradient is None is left alone.  ``weight_decay`` is one number or one per tensor,
+    ``step`` counts from 1.  ``step`` (int64) and ``lr`` (FP32) may be one-element tensors on the device: a captured step that is replayed reads them as they are then.
+    ``grad_scale``, an FP32 one-element tensor on the device, multiplies the gradients (the factor of a clipped gradient norm)."""
+    _adamw_counts(params, grads, state)
+    device = state.moments.get_device()
+    if device < 0:
+        _require_cuda(state.moments)
+    if stream is not None or device != _current_device():
+        return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale)
+    call, args, kept, params = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
     if args.lr_dev or args.step_dev:
         scalars = torch.empty(4, dtype=torch.float32, device=state.moments.device)
         args.scalars = scalars.data_ptr()
-    code = (_lib or load_library()).gws_adamw_step(n, p_params.buffer_info()[0], p_grads.buffer_info()[0], state._c_sizes, state._c_starts, types, decays,
-                                                   ctypes.addressof(state._c), ctypes.addressof(args), _raw_stream(device))
+    code = (_lib or load_library()).gws_adamw_step(*call, _raw_stream(device))
     if code:
         _check(code)
     torch.autograd.graph.increment_version(params)

@@ -123,8 +123,9 @@ int launch_adamw(const AdamwArgs& args, const AdamwRec* recs, int n, unsigned bl
 // Records of a launch: few tensors travel in 0.7 KB of kernel parameters, many in 15.
 constexpr int kAdamwFew = 16, kAdamwMany = 384;
 
+// `launches`: false for the checks alone.
 int adamw_step(int n_tensors, void* const* params, const void* const* grads, const int64_t* sizes, const int64_t* starts, const int32_t* types, const double* decays,
-               const gws_adamw_state* state, const gws_adamw_step_args* args, cudaStream_t s) {
+               const gws_adamw_state* state, const gws_adamw_step_args* args, bool launches, cudaStream_t s) {
   if (n_tensors < 0) return GWS_ERR_SHAPE;
   if (state == nullptr || args == nullptr) return GWS_ERR_NULL;
   if (state->format != GWS_ADAMW_F32 && state->format != GWS_ADAMW_8BIT) return GWS_ERR_UNSUPPORTED;
@@ -169,7 +170,7 @@ int adamw_step(int n_tensors, void* const* params, const void* const* grads, con
   }
   if (recs.empty()) return GWS_OK;
   const bool bits8 = state->format == GWS_ADAMW_8BIT;
-  if (state->moments == nullptr || (bits8 && state->units == nullptr) || (device && args->scalars == nullptr)) return GWS_ERR_NULL;
+  if (state->moments == nullptr || (bits8 && state->units == nullptr) || (device && launches && args->scalars == nullptr)) return GWS_ERR_NULL;
   if (!on(state->moments, 32) || !on(state->units, 4) || !on(state->rest, 16) || !on(args->grad_scale, 4) || !on(args->lr_dev, 4) || !on(args->step_dev, 8) ||
       !on(args->scalars, 4))
     return GWS_ERR_ALIGN;
@@ -182,6 +183,7 @@ int adamw_step(int n_tensors, void* const* params, const void* const* grads, con
   use(args->step_dev, 8, false);
   if (device) use(args->scalars, 12, true);
   if (any_clash(uses)) return GWS_ERR_ALIAS;
+  if (!launches) return GWS_OK;
 
   AdamwArgs a;
   std::memset(&a, 0, sizeof a);
@@ -330,8 +332,17 @@ int gws_layernorm_bwd(const gws_norm_desc* desc, const void* grad_y, const void*
 int gws_adamw_step(int n_tensors, void* const* params, const void* const* grads, const int64_t* sizes, const int64_t* starts, const int32_t* types,
                    const double* weight_decay, const gws_adamw_state* state, const gws_adamw_step_args* args, void* stream) {
   try {
-    return adamw_step(n_tensors, params, grads, sizes, starts, types, weight_decay, state, args, static_cast<cudaStream_t>(stream));
+    return adamw_step(n_tensors, params, grads, sizes, starts, types, weight_decay, state, args, true, static_cast<cudaStream_t>(stream));
   } catch (...) {                      // host memory for the list of tensors
+    return GWS_ERR_LIMIT;
+  }
+}
+
+int gws_adamw_check(int n_tensors, void* const* params, const void* const* grads, const int64_t* sizes, const int64_t* starts, const int32_t* types,
+                    const double* weight_decay, const gws_adamw_state* state, const gws_adamw_step_args* args) {
+  try {
+    return adamw_step(n_tensors, params, grads, sizes, starts, types, weight_decay, state, args, false, nullptr);
+  } catch (...) {
     return GWS_ERR_LIMIT;
   }
 }

@@ -68,18 +68,29 @@ class GaussWSAdamW(torch.optim.Optimizer):
             return loss
         state = self._prepare()
         on_device = isinstance(self._count, torch.Tensor)
-        count = self._count.add_(1) if on_device else self._count + 1
+        count = self._count if on_device else self._count + 1
         decays = [float(g["weight_decay"]) for g in self.param_groups for _ in g["params"]]
         kinds = [(id(g["lr"]) if isinstance(g["lr"], torch.Tensor) else g["lr"], tuple(g["betas"]), g["eps"]) for g in self.param_groups]
+        calls = []
+        for kind in dict.fromkeys(kinds):
+            mine = [k == kind for k, g in zip(kinds, self.param_groups) for _ in g["params"]]
+            group = self.param_groups[kinds.index(kind)]
+            calls.append((grads if all(mine) else [g if m else None for g, m in zip(grads, mine)],
+                          dict(lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=decays, step=count, grad_scale=grad_scale)))
+        for some, more in calls[1:]:                      # a step is refused as a whole: what follows the first call, which checks itself, is checked before it
+            binding.adamw_check(params, some, state, **more)
+        if on_device:
+            count.add_(1)
+        begun = False
         try:
-            for kind in dict.fromkeys(kinds):
-                mine = [k == kind for k, g in zip(kinds, self.param_groups) for _ in g["params"]]
-                group = self.param_groups[kinds.index(kind)]
-                binding.adamw_step(params, grads if all(mine) else [g if m else None for g, m in zip(grads, mine)], state, lr=group["lr"], betas=group["betas"],
-                                   eps=group["eps"], weight_decay=decays, step=count, grad_scale=grad_scale)
-        except Exception:                                 # a step that was refused does not count
-            if on_device:
+            for some, more in calls:
+                binding.adamw_step(params, some, state, **more)
+                begun = True
+        except Exception:                                 # a step that was refused does not count; one that a launch failed in the middle of does
+            if on_device and not begun:
                 count.sub_(1)
+            if begun:
+                self._count = count
             raise
         self._count = count
         return loss

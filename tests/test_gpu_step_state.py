@@ -52,3 +52,26 @@ def test_a_captured_step_goes_on_from_a_loaded_state(moments):
                 assert torch.equal(a, b) and torch.equal(o.weight(a), e.weight(b))
         assert o.state_dict()["gws"]["count"] == e.state_dict()["gws"]["count"] == 3
         assert torch.equal(o._state.moments, e._state.moments)
+
+
+def test_a_step_of_several_groups_is_refused_as_a_whole():
+    a, b = (torch.nn.Parameter(torch.ones(300, dtype=torch.bfloat16, device=DEV)) for _ in range(2))
+    optimizer = GaussWSAdamW([dict(params=[a], lr=1e-3), dict(params=[b], lr=2e-3)])
+    a.grad, b.grad = torch.ones_like(a), torch.ones_like(b)
+    optimizer.step()
+    tensors = [a, b, optimizer._state.moments, optimizer._state.rest]
+    before = [t.detach().clone() for t in tensors]
+    second, launches = optimizer.param_groups[1], gws.launch_count()
+    for wrong in (dict(betas=(1.0, 0.9)), dict(betas=(0.9, float("nan"))), dict(eps=-1.0), dict(lr=torch.ones(1)), dict(lr=torch.ones(1, dtype=torch.float64, device=DEV))):
+        present = {k: second[k] for k in wrong}
+        second.update(wrong)
+        with pytest.raises((ValueError, gws.GwsError)):
+            optimizer.step()
+        second.update(present)
+    grad, b.grad = b.grad, b.detach()                          # a gradient that is the parameter itself
+    with pytest.raises(gws.GwsError):
+        optimizer.step()
+    b.grad = grad
+    assert gws.launch_count() == launches and all(torch.equal(t, u) for t, u in zip(tensors, before))
+    optimizer.step()
+    assert optimizer.state_dict()["gws"]["count"] == 2 and gws.launch_count() == launches + 2

@@ -95,3 +95,55 @@ def test_a_loaded_rate_beside_the_parameters(recorded):
     assert rates[0] is rates[1] and rates[0].dtype == torch.float32 and rates[0].device == optimizer.param_groups[0]["params"][0].device
     optimizer.step()
     assert len(recorded) == 1
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_step_is_refused_as_a_whole(recorded, capturable):
+    """Groups of different rates are calls of their own: none is made where one would be refused."""
+    optimizer = _two_groups(1e-3, 2e-3, capturable=capturable)
+    optimizer.step()
+    recorded.clear()
+    second = optimizer.param_groups[1]
+    strided = torch.nn.Parameter(torch.ones(4, 14, dtype=torch.bfloat16)[:, ::2])
+    strided.grad = torch.ones(4, 7, dtype=torch.bfloat16)
+    for wrong in (dict(lr=torch.ones(1, dtype=torch.float64)), dict(lr=torch.ones(2)), dict(lr="fast"), dict(betas=(0.9,)), dict(params=[strided])):
+        present = {k: second[k] for k in wrong}
+        second.update(wrong)
+        with pytest.raises((ValueError, TypeError, IndexError)):
+            optimizer.step()
+        second.update(present)
+        assert not recorded and int(optimizer._count) == 1
+    optimizer.step()
+    assert [(c["grads"], int(c["step"])) for c in recorded] == [([True, False], 2), ([False, True], 2)]
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_launch_that_fails_in_the_middle_of_a_step(recorded, capturable, monkeypatch):
+    """The groups before it have been stepped, so the step counts: they are not stepped under the same count again."""
+    optimizer = _two_groups(1e-3, 2e-3, capturable=capturable)
+    optimizer.step()
+    taken = binding.adamw_step
+
+    def fails(params, grads, state, **more):
+        if more["lr"] == 2e-3:
+            raise RuntimeError
+        taken(params, grads, state, **more)
+
+    with monkeypatch.context() as m:
+        m.setattr(binding, "adamw_step", fails)
+        with pytest.raises(RuntimeError):
+            optimizer.step()
+    assert int(optimizer._count) == 2
+
+
+def test_check_of_a_step():
+    """What adamw_step refuses, but that the tensors are on the CPU."""
+    p, g, state = torch.ones(300), torch.ones(300), gws.AdamWState([300], device="cpu")
+    gws.adamw_check([p], [g], state, lr=1e-3)
+    for call in (lambda: gws.adamw_check([p], [g, g], state, lr=1e-3), lambda: gws.adamw_check([p[:299]], [g[:299]], state, lr=1e-3), lambda: gws.adamw_check([p], [g.half()], state, lr=1e-3),
+                 lambda: gws.adamw_check([torch.ones(600)[::2]], [g], state, lr=1e-3), lambda: gws.adamw_check([p], [g], state, lr=1e-3, weight_decay=[0.1, 0.1]),
+                 lambda: gws.adamw_check([p], [g], state, lr=1e-3, grad_scale=0.5), lambda: gws.adamw_check([p], [g], state, lr=1e-3, step=torch.ones(1))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        gws.adamw_step([p], [g], state, lr=1e-3)
