@@ -356,6 +356,8 @@ class GaussWSMLP(torch.nn.Module):
             layer.advance()
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if residual is not None and residual.shape != x.shape:
+            raise ValueError("gws: the residual has the shape of x")
         return _MLP.apply(x, residual, self.up.sampled_weight(), self.up.bias, self.down.sampled_weight(), self.down.bias, self.activation, self.keep)
 
 
