@@ -1100,7 +1100,7 @@ def layernorm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
         p_sum = total.data_ptr()
     y = _dense_like(x, m, n)
     stats = x.new_empty(2, m, dtype=torch.float32) if want_stats else None
-    _, at, _ = _norm_plan(m, n, ld_x, ld_r, 0, 0, kind, eps, device)
+    desc, at, _ = _norm_plan(m, n, ld_x, ld_r, 0, 0, kind, eps, device)
     code = (_lib or load_library()).gws_layernorm_fwd(at, p_x, p_r, _addr(weight), _addr(bias), y.data_ptr(), p_sum, _addr(stats), _raw_stream(device))
     if code:
         _check(code)
