@@ -1232,6 +1232,7 @@ class AdamWState:
         if param.numel() != self.sizes[index]:
             raise ValueError("gws: tensor %d has %d elements" % (index, self.sizes[index]))
         low = self.rest[self.starts[index]:self.starts[index] + self.sizes[index]].view(param.shape)
+        low = torch.where((param == 0) & (low < 0), 0, low)          # a zero set from outside counts as zero
         return ((param.detach().view(torch.int16).to(torch.int32) << 16) + low.to(torch.int32)).view(torch.float32)
 
 

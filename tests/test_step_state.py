@@ -147,3 +147,15 @@ def test_check_of_a_step():
             call()
     with pytest.raises(ValueError):
         gws.adamw_step([p], [g], state, lr=1e-3)
+
+
+def test_the_weight_of_a_parameter_set_to_zero_from_outside():
+    """A zero over a negative rest, which no step leaves, counts as zero, as the step takes it; its bits joined would be a NaN's."""
+    state = gws.AdamWState([6], rest=True, device="cpu")
+    state.rest[:6] = torch.tensor([-3, -3, 4, 0, -5, -5], dtype=torch.int16)
+    p = torch.tensor([0.0, -0.0, 0.0, -0.0, 1.0, -1.0], dtype=torch.bfloat16)
+    below = 1 - 5 * 2.0 ** -24                                 # under a power of two the numbers are twice as dense
+    want = torch.tensor([0.0, -0.0, 4 * 2.0 ** -149, -0.0, below, -below])
+    got = state.weight(0, p)
+    assert torch.equal(got.view(torch.int32), want.view(torch.int32))
+    assert state.weight(0, p.view(2, 3)).shape == (2, 3)
