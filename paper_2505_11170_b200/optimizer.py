@@ -172,7 +172,7 @@ class GaussWSAdamW(torch.optim.Optimizer):
                 group["lr"] = lr.fill_(rate)
             elif isinstance(loaded, torch.Tensor):
                 if id(loaded) not in moved:
-                    moved[id(loaded)] = loaded.to(device=group["params"][0].device, dtype=torch.float32)
+                    moved[id(loaded)] = loaded.to(device=self._all()[0].device, dtype=torch.float32)
                 group["lr"] = moved[id(loaded)]
 
     def __getstate__(self):

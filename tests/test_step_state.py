@@ -159,3 +159,10 @@ def test_the_weight_of_a_parameter_set_to_zero_from_outside():
     got = state.weight(0, p)
     assert torch.equal(got.view(torch.int32), want.view(torch.int32))
     assert state.weight(0, p.view(2, 3)).shape == (2, 3)
+
+
+def test_a_loaded_rate_of_a_group_without_parameters(recorded):
+    groups = lambda lr: [dict(params=[]), dict(params=[_parameter(300)], lr=lr)]
+    source, optimizer = GaussWSAdamW(groups(_rate(1e-3)), lr=_rate(2e-3)), GaussWSAdamW(groups(5e-4), lr=5e-4)
+    optimizer.load_state_dict(source.state_dict())
+    assert [float(g["lr"]) for g in optimizer.param_groups] == [float(_rate(2e-3)), float(_rate(1e-3))]
