@@ -1194,7 +1194,7 @@ class AdamWState:
             self._take(units, "units", torch.float32, (2, total // _ADAMW_GROUP) if bits8 else None)
         if rest is not None:
             self._take(rest, "rest", torch.int16, (total,))
-        if any(t is not None and t.device != moments.device for t in (units, rest)):
+        if (units is not None and units.device != moments.device) or (rest is not None and rest.device != moments.device):
             raise ValueError("gws: the tensors of a state live on one device")
         self._moments, self._units, self._rest = moments, units, rest
         self._c = _AdamwState(moments.data_ptr(), _addr(units), _addr(rest), total, fmt, 0)
@@ -1253,15 +1253,18 @@ def _adamw_decays(decays: tuple):
     return (ctypes.c_double * len(decays))(*[float(w) for w in decays])
 
 
-def _adamw_counts(params, grads, state: AdamWState) -> None:
-    if len(params) != len(state.sizes) or len(grads) != len(state.sizes):
-        raise ValueError("gws: the state is of %d tensors" % len(state.sizes))
+def _adamw_number(t, dtype, name: str, device: int) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() != 1 or t.get_device() != device:
+        raise ValueError("gws: %s on the device is one element of %s" % (name, dtype))
+    return t.data_ptr()
 
 
 def _adamw_call(params, grads, state: AdamWState, device: int, lr, betas, eps: float, weight_decay, step, grad_scale):
     """(the library's arguments, the arrays and tensors behind them, the parameters that are stepped), with everything checked that the library cannot see."""
-    n = len(state.sizes)
     sizes, where = state.sizes, None
+    n = len(sizes)
+    if len(params) != n or len(grads) != n:
+        raise ValueError("gws: the state is of %d tensors" % n)
     if any([g is None for g in grads]):
         where = [i for i, g in enumerate(grads) if g is not None]
         params, grads, sizes = [params[i] for i in where], [grads[i] for i in where], [sizes[i] for i in where]
@@ -1290,55 +1293,47 @@ def _adamw_call(params, grads, state: AdamWState, device: int, lr, betas, eps: f
         if len(decays) != n:
             raise ValueError("gws: one weight_decay for all tensors, or one for each")
     args = _AdamwArgs(0.0, betas[0], betas[1], eps, 1, None, None, None, None)
-    on_device = []
-    for t, dtype, name in ((lr, torch.float32, "lr"), (step, torch.int64, "step"), (grad_scale, torch.float32, "grad_scale")):
-        if isinstance(t, torch.Tensor):
-            if t.dtype is not dtype or t.numel() != 1 or t.get_device() != device:
-                raise ValueError("gws: %s on the device is one element of %s" % (name, dtype))
-            on_device.append(name)
-    if grad_scale is not None:
-        if "grad_scale" not in on_device:
-            raise ValueError("gws: grad_scale is a tensor on the device")
-        args.grad_scale = grad_scale.data_ptr()
-    if "lr" in on_device:
-        args.lr_dev = lr.data_ptr()
+    if isinstance(lr, torch.Tensor):
+        args.lr_dev = _adamw_number(lr, torch.float32, "lr", device)
     else:
         args.lr = lr
-    if "step" in on_device:
-        args.step_dev = step.data_ptr()
+    if isinstance(step, torch.Tensor):
+        args.step_dev = _adamw_number(step, torch.int64, "step", device)
     else:
         args.step = step
-    call = (n, p_params.buffer_info()[0], p_grads.buffer_info()[0], state._c_sizes, state._c_starts, types, decays, ctypes.addressof(state._c), ctypes.byref(args))
-    return call, args, (p_params, p_grads, grads), params
+    if grad_scale is not None:
+        args.grad_scale = _adamw_number(grad_scale, torch.float32, "grad_scale", device)
+    return (n, p_params.buffer_info()[0], p_grads.buffer_info()[0], state._c_sizes, state._c_starts, types, decays, ctypes.addressof(state._c), ctypes.byref(args)), args, \
+        (p_params, p_grads, grads, state, lr, step, grad_scale), params
 
 
 def adamw_check(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
-                step=1, grad_scale: Optional[torch.Tensor] = None) -> None:
-    """Raises what :func:`adamw_step` would raise for these arguments, with nothing launched: for a step that takes several calls and is to be refused as a whole.  Of tensors on
-    the CPU, which only adamw_step itself refuses, the addresses are not checked."""
-    _adamw_counts(params, grads, state)
+                step=1, grad_scale: Optional[torch.Tensor] = None):
+    """Raises what :func:`adamw_step` would raise for these arguments, with nothing launched: for a step that takes several calls and is to be refused as a whole.  What it returns
+    is for ``checked`` of that call.  Of tensors on the CPU, which only adamw_step itself refuses, the addresses are not checked."""
     device = state.moments.get_device()
-    call, args, kept, params = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
+    checked = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
     if device >= 0:
-        code = (_lib or load_library()).gws_adamw_check(*call)
+        code = (_lib or load_library()).gws_adamw_check(*checked[0])
         if code:
             _check(code)
+    return checked
 
 
 def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
-               step=1, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+               step=1, grad_scale: Optional[torch.Tensor] = None, stream=None, checked=None) -> None:
     """One AdamW step over all tensors, in place, in one launch (for up to 384 of them).
 
     Parameters are BF16 or FP32 and contiguous, gradients of their type; a tensor whose gradient is None is left alone.  ``weight_decay`` is one number or one per tensor,
     ``step`` counts from 1.  ``step`` (int64) and ``lr`` (FP32) may be one-element tensors on the device: a captured step that is replayed reads them as they are then.
-    ``grad_scale``, an FP32 one-element tensor on the device, multiplies the gradients (the factor of a clipped gradient norm)."""
-    _adamw_counts(params, grads, state)
+    ``grad_scale``, an FP32 one-element tensor on the device, multiplies the gradients (the factor of a clipped gradient norm).
+    ``checked`` is what :func:`adamw_check` returned for the same arguments, which are then not looked at again."""
     device = state.moments.get_device()
     if device < 0:
         _require_cuda(state.moments)
     if stream is not None or device != _current_device():
-        return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale)
-    call, args, kept, params = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
+        return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale, None, checked)
+    call, args, kept, params = checked or _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
     if args.lr_dev or args.step_dev:
         scalars = torch.empty(4, dtype=torch.float32, device=state.moments.device)
         args.scalars = scalars.data_ptr()

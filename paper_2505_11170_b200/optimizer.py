@@ -78,7 +78,7 @@ class GaussWSAdamW(torch.optim.Optimizer):
             calls.append((grads if all(mine) else [g if m else None for g, m in zip(grads, mine)],
                           dict(lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=decays, step=count, grad_scale=grad_scale)))
         for some, more in calls[1:]:                      # a step is refused as a whole: what follows the first call, which checks itself, is checked before it
-            binding.adamw_check(params, some, state, **more)
+            more["checked"] = binding.adamw_check(params, some, state, **more)
         if on_device:
             count.add_(1)
         begun = False

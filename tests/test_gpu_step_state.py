@@ -75,3 +75,25 @@ def test_a_step_of_several_groups_is_refused_as_a_whole():
     assert gws.launch_count() == launches and all(torch.equal(t, u) for t, u in zip(tensors, before))
     optimizer.step()
     assert optimizer.state_dict()["gws"]["count"] == 2 and gws.launch_count() == launches + 2
+
+
+@pytest.mark.parametrize("on_side", [False, True])
+def test_a_checked_step_is_the_step(on_side):
+    """On the stream of the call, with gradients that need a copy, and places without one."""
+    def made(seed):
+        torch.manual_seed(seed)
+        params = [torch.randn(40, 30, device=DEV), torch.randn(300, device=DEV).bfloat16(), torch.randn(7, device=DEV)]
+        return params, [torch.randn(30, 40, device=DEV).t(), torch.randn(300, device=DEV).bfloat16(), None], gws.AdamWState([1200, 300, 7], gws.ADAMW_8BIT, rest=True)
+
+    (p, g, s), (q, h, t) = made(1), made(1)
+    more = dict(lr=torch.full((1,), 1e-3, device=DEV), step=3, grad_scale=torch.full((1,), 0.5, device=DEV))
+    launches = gws.launch_count()
+    checked = gws.adamw_check(p, g, s, **more)
+    assert gws.launch_count() == launches
+    side = torch.cuda.Stream() if on_side else None
+    if on_side:
+        side.wait_stream(torch.cuda.current_stream())
+    gws.adamw_step(p, g, s, **more, checked=checked, stream=side)
+    gws.adamw_step(q, h, t, **more)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((*p, s.moments, s.units, s.rest), (*q, t.moments, t.units, t.rest)))
