@@ -616,7 +616,8 @@ int gws_layernorm_bwd(const gws_norm_desc* desc, const void* grad_y, const void*
  *   g = grad * grad_scale     m = b1 m + (1 - b1) g     v = b2 v + (1 - b2) g g     r = sqrt(v)
  *   p = p (1 - lr wd) - (m alpha) / (r rho + eps),     alpha = lr / (1 - b1^step),  rho = 1 / sqrt(1 - b2^step)
  * in FP32, every operation rounded once in the order written (alpha, rho and 1 - lr wd are computed in double and rounded once, with lr_dev or step_dev from wd rounded to FP32; where |m alpha| is
- * below 2^-100 the quotient may be one unit of its last place off).
+ * below 2^-100, or the quotient below 2^-126, the quotient may be one unit of its last place off).  That roots and quotients are otherwise those of sqrt and / is tested on
+ * samples, not proven.
  *
  * State: tensor i owns the elements [starts[i], starts[i] + sizes[i] rounded up to 256) of arrays of `total` elements that all tensors share
  * (starts and total are multiples of 256; the elements past a size are kept zero; all of the state is zero before the first step).
