@@ -711,7 +711,7 @@ def _status_of(status: Optional[torch.Tensor]) -> int:
 
 
 def check_waits(synchronize: bool = True) -> None:
-    """Raises GwsError if a kernel of :func:`wgrad_act8`, :func:`gated_fwd` or :func:`gated_bwd` gave up a wait (about a second without an
+    """Raises GwsError if a kernel of :func:`wgrad_act8`, :func:`gated_fwd`, :func:`gated_bwd`, :func:`linear_fwd` or :func:`linear_bwd` gave up a wait (about a second without an
     answer inside the GPU), in which case the outputs of its call are undefined.  Every later call of these functions, and a module's
     ``advance``, check the same without waiting; ``synchronize`` waits for the current device first, so that all calls made so far count.
     Calls with a ``status`` of their own report there instead."""

@@ -436,6 +436,7 @@ __device__ __forceinline__ void adamw_run(const AdamwArgs& a, const AdamwRec& e,
 // A warp takes a group, a lane eight elements of it; a block finds its tensor by bisection in the kernel parameters.  184.5 M BF16 weights with their rest: 32-bit moments 726 us, 6.6 TB/s
 // (the copy rate); 8-bit moments 500 us, 5.2 TB/s of 14.06 bytes a weight: some 66 instructions a weight (roots, quotients, codes) keep the issue slots two thirds busy.  One weight at
 // a time through sqrt.rn and div.rn that took 820.  Six small vectors: 2 us.
+// FP32 weights: 32-bit moments 766 us (28 bytes a weight, 6.7 TB/s); 8-bit moments, whose next group is neither staged nor in registers, 575 (16.06 bytes, 5.2 TB/s).
 // LOOSE: some tensors of the launch are not on boundaries of eight elements.  Groups of those take twice the loads and the registers to have the next ones under way:
 // three blocks an SM, where five of the others fit (8-bit moments, 184.5 M BF16 weights: 498 us with five, 580 with three; 16.8 M unaligned: 68, 61).
 template <int FMT, bool LOOSE, int CAP>

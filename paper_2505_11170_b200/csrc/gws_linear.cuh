@@ -5,8 +5,9 @@
 // Memory-bound, one pass: 2 + 1 1/32 bytes in (z from a checkpoint), 2 or 4 out per element.  A block takes a strip of 64 columns of a share of the rows, eight lanes to
 // a row and eight columns to a lane, has the next rows' loads under way while it works on some, and keeps the column sums in registers.  The shares of a strip, where they
 // are eight at most, are the blocks of a cluster and joined through each other's shared memory in a fixed order; more of them leave their sums to k_column_sums.
-// 16384 x 5632, GELU from INT8 with act(z) and db: 90 us (5.2 TB/s) in calls alone, 113 with the join's launch and its wait; 165 before the loads ran ahead and the arithmetic was on pairs.
-// Odd widths read and write elements one by one: 2047 x 2729 16 us, 8192 x 2729 49 (3.2 TB/s).
+// 16384 x 5632, GELU from INT8, us of a call that wants no product, so that dz is not written: act(z) and db 89 (5.2 TB/s of 464 MB, the join of the sums among it), act(z) alone
+// 75, db alone 80.  With dz too, a call with a narrow product less that product: 152 to 158 (4.2 TB/s of 649 MB).
+// Odd widths read and write elements one by one: 2047 x 2729, act(z) and db 17 us, 8192 x 2729 50 (2.3 TB/s), with dz 57 to 60.
 // The first blocks of the launch make ready what the products after it read (prepare).
 #pragma once
 #include <stdint.h>

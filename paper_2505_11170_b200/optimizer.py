@@ -16,7 +16,7 @@ class GaussWSAdamW(torch.optim.Optimizer):
 
     ``moments`` is ``binding.ADAMW_F32`` (8 bytes per weight) or ``ADAMW_8BIT`` (2 bytes and 1/32).  ``rest`` keeps the 16 bits that a 32-bit weight has below its BF16
     parameter, without which updates smaller than half the spacing of BF16 are lost; :meth:`weight` gives the 32-bit weight.  Parameter groups may differ in lr, betas,
-    eps and weight_decay; groups that share the first three are stepped in one launch.  All parameters are on one CUDA device; parameters without a gradient are left alone, and a
+    eps and weight_decay; groups that share the first three are stepped in one launch, and a step is refused for all groups or for none.  All parameters are on one CUDA device; parameters without a gradient are left alone, and a
     step counts for all others.  ``step(grad_scale=t)`` multiplies the gradients by an FP32 one-element tensor.  ``capturable`` keeps the count of steps on the device, so that a
     captured step can be replayed; a learning rate that is to change between replays is an FP32 one-element tensor on the device.
     """
