@@ -1312,12 +1312,12 @@ def adamw_check(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.T
     """Raises what :func:`adamw_step` would raise for these arguments, with nothing launched: for a step that takes several calls and is to be refused as a whole.  What it returns
     is for ``checked`` of that call.  Of tensors on the CPU, which only adamw_step itself refuses, the addresses are not checked."""
     device = state.moments.get_device()
-    checked = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
+    call, args, kept, stepped = _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
     if device >= 0:
-        code = (_lib or load_library()).gws_adamw_check(*checked[0])
+        code = (_lib or load_library()).gws_adamw_check(*call)
         if code:
             _check(code)
-    return checked
+    return call, args, kept, tuple(stepped), (state, *params, *grads, lr, step, grad_scale)
 
 
 def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], state: AdamWState, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01,
@@ -1327,13 +1327,17 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
     Parameters are BF16 or FP32 and contiguous, gradients of their type; a tensor whose gradient is None is left alone.  ``weight_decay`` is one number or one per tensor,
     ``step`` counts from 1.  ``step`` (int64) and ``lr`` (FP32) may be one-element tensors on the device: a captured step that is replayed reads them as they are then.
     ``grad_scale``, an FP32 one-element tensor on the device, multiplies the gradients (the factor of a clipped gradient norm).
-    ``checked`` is what :func:`adamw_check` returned for the same arguments, which are then not looked at again."""
+    ``checked`` is what :func:`adamw_check` returned for the same tensors, lr, step and grad_scale, which are then not looked at again; nothing has moved them in between."""
+    if checked is not None:
+        these = (state, *params, *grads, lr, step, grad_scale)
+        if len(these) != len(checked[4]) or not all(a is b or (type(a) is type(b) and type(a) in (int, float) and a == b) for a, b in zip(these, checked[4])):
+            raise ValueError("gws: what was checked are other arguments")
     device = state.moments.get_device()
     if device < 0:
         _require_cuda(state.moments)
     if stream is not None or device != _current_device():
         return _on_stream(stream, device, adamw_step, params, grads, state, lr, betas, eps, weight_decay, step, grad_scale, None, checked)
-    call, args, kept, params = checked or _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
+    call, args, kept, params = checked[:4] if checked is not None else _adamw_call(params, grads, state, device, lr, betas, eps, weight_decay, step, grad_scale)
     if args.lr_dev or args.step_dev:
         scalars = torch.empty(4, dtype=torch.float32, device=state.moments.device)
         args.scalars = scalars.data_ptr()

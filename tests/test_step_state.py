@@ -1,4 +1,6 @@
 """The state of the AdamW step and its optimizer on the CPU: the calls that they refuse, and states that are loaded."""
+import weakref
+
 import pytest
 import torch
 
@@ -166,3 +168,20 @@ def test_a_loaded_rate_of_a_group_without_parameters(recorded):
     source, optimizer = GaussWSAdamW(groups(_rate(1e-3)), lr=_rate(2e-3)), GaussWSAdamW(groups(5e-4), lr=5e-4)
     optimizer.load_state_dict(source.state_dict())
     assert [float(g["lr"]) for g in optimizer.param_groups] == [float(_rate(2e-3)), float(_rate(1e-3))]
+
+
+def test_a_check_is_of_its_own_arguments():
+    """adamw_step takes addresses from it: of tensors that it holds, and for the same ones alone."""
+    made = lambda: ([torch.ones(300), torch.ones(7)], [torch.ones(300), None], gws.AdamWState([300, 7], device="cpu"))
+    (p, g, state), (q, h, other) = made(), made()
+    checked = gws.adamw_check(p, g, state, lr=1e-3, step=5)
+    for call in (lambda: gws.adamw_step(q, g, state, lr=1e-3, step=5, checked=checked), lambda: gws.adamw_step(p, h, state, lr=1e-3, step=5, checked=checked),
+                 lambda: gws.adamw_step(p, g, other, lr=1e-3, step=5, checked=checked), lambda: gws.adamw_step(p, g, state, lr=1e-3, step=torch.ones(1), checked=checked),
+                 lambda: gws.adamw_step(p[:1], g[:1], state, lr=1e-3, step=5, checked=checked)):
+        with pytest.raises(ValueError, match="other arguments"):
+            call()
+    with pytest.raises(ValueError, match="device pointers"):                  # as without it
+        gws.adamw_step(p, g, state, lr=float("1e-3"), step=5, checked=checked)
+    held = weakref.ref(p[0])
+    p[0] = q[0]
+    assert held() is not None
